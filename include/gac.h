@@ -417,6 +417,171 @@ int gac_stats_static(const gac_tensor *list, uint32_t n, int g_dtype, int d_dtyp
                      const gac_hparams *hp, uint64_t step, uint32_t staleness, int cuda_device,
                      void *cuda_stream, gac_result *result_dev);
 
+/*
+ * ======================================================================
+ * Around the rule: what a policy update on packed rollouts also computes.
+ * Finished rollouts of different lengths lie one behind the other in one
+ * pack of tokens; cu_seqlens[b] .. cu_seqlens[b+1] are the tokens of
+ * sequence b (cu_seqlens[0] is taken as 0).  Tokens behind the last sequence
+ * (padding of the pack) belong to none.  cu_seqlens lives on the device and
+ * is read there only, so no call waits for the host; an entry outside
+ * [the previous one, n_tokens] is moved to that range, never followed out of
+ * bounds.
+ *
+ * The calls below need no context unless they say so, enqueue on the given
+ * stream, allocate nothing and can be captured in a CUDA graph.  Messages of
+ * failed calls: gac_last_error(NULL).
+ * ======================================================================
+ *
+ * Global gradient norm and clipping over a list of tensors, for steps that do
+ * not go through gac_project's folded clipping: lists without a stored
+ * direction (value functions, baselines) and lists of mixed element types
+ * (float32 norms and biases beside bfloat16 matrices).
+ *     norm = sqrt(sum g_i^2)                     (binary64, fixed order)
+ *     out_i = min(1, max_norm / (norm + eps)) * g_i   (one rounding per element)
+ *
+ * gac_clip_init       builds the chunk table of the list.  Each entry is read at
+ *                     `g` and written at `out`; out == g clips in place, and
+ *                     then nothing is written when the factor is 1.  Ranges
+ *                     must not overlap otherwise.  numel = 0 is allowed.
+ * gac_clip_sumsq      sharded form, first half: writes the sum of squares of this
+ *                     rank's list to sumsq_out (device pointer, one double, 8-byte
+ *                     aligned) for the caller's all-reduce
+ * gac_clip_apply      second half: reads the global sum of squares from sumsq_in
+ *                     (device pointer) and writes the list's `out`
+ * gac_clip_grad_norm  both halves on one rank
+ *   max_norm   > 0; +infinity means: never clip (the norm alone is wanted; an
+ *              out-of-place list is still copied)
+ *   eps        added to the norm in the factor, finite and >= 0 (1e-6 is usual)
+ *   norm_out   device pointer to one float that receives the norm, or NULL
+ *   host_out   as in gac_stats: NULL = asynchronous; else the stream is
+ *              synchronised and the record copied there
+ * A norm that is NaN or infinite: nothing is written to any `out`, the record
+ * says nonfinite, and with host_out the call returns GAC_ERR_NONFINITE.
+ * Errors: INVALID_ARG, DTYPE, CUDA, NONFINITE.
+ */
+typedef struct gac_clip_ctx gac_clip_ctx;   /* opaque, library-owned */
+typedef struct {
+    const void *g;      /* device pointer, element-aligned, caller-owned                     */
+    void *out;          /* device pointer, element-aligned, caller-owned; may equal g         */
+    uint64_t numel;
+    int32_t dtype;      /* gac_dtype of g and out                                             */
+    int32_t reserved;   /* must be 0                                                          */
+} gac_clip_tensor;
+typedef struct {
+    double sumsq;       /* sum of squares over the list                                       */
+    double norm;        /* its square root                                                    */
+    double scale;       /* factor applied                                                     */
+    int32_t nonfinite;  /* 1: the norm is NaN or infinite, nothing was written                */
+    int32_t reserved;
+} gac_clip_result;
+int gac_clip_init(gac_clip_ctx **out, const gac_clip_tensor *list, uint32_t n, int cuda_device);
+int gac_clip_sumsq(gac_clip_ctx *ctx, void *cuda_stream, double *sumsq_out);
+int gac_clip_apply(gac_clip_ctx *ctx, void *cuda_stream, const double *sumsq_in, double max_norm, double eps,
+                   float *norm_out, gac_clip_result *host_out);
+int gac_clip_grad_norm(gac_clip_ctx *ctx, void *cuda_stream, double max_norm, double eps, float *norm_out,
+                       gac_clip_result *host_out);
+int gac_clip_free(gac_clip_ctx *ctx);   /* NULL is accepted */
+
+/*
+ * Rotary positions.  Pair i of the first rot_dim elements of every head turns by
+ * the angle  position * freq[i]:
+ *     (x, y) -> scale * (x cos - y sin, x sin + y cos)
+ * HALF pairs element i with i + rot_dim/2, INTERLEAVED 2i with 2i + 1; the
+ * elements from rot_dim on are copied.  `inverse` turns by the negative
+ * angle: with the same scale that is the transpose, hence the way back of the
+ * gradient.  The angle is reduced to one turn in binary64, so far positions
+ * are as exact as near ones.
+ *
+ * x / y are the input and output of the query heads (0) and of the key heads (1); heads = 0
+ * leaves one out.  y may equal x (in place, same strides), else the two must not overlap.
+ * Positions: `positions` (device, one int32 per token), or, when that is NULL,
+ * the place of each token in its sequence by cu_seqlens (tokens behind the last
+ * sequence: position 0).
+ *
+ * gac_rotary_freqs fills freq[rot_dim/2] (host) with base^(-2i/rot_dim), stretched
+ * for contexts `factor` times as long as the trained one:
+ *   NONE    as they are (factor must be 1)
+ *   LINEAR  all divided by factor
+ *   BASE    the base grows by factor^(rot_dim/(rot_dim-2)): the slowest pair turns
+ *           factor times more slowly, the fastest as before
+ *   PARTS   by the turns r a pair makes over `trained` tokens: r >= high as they are,
+ *           r <= low divided by factor, a linear ramp of the two in between
+ * Errors: INVALID_ARG, DTYPE, CUDA.
+ */
+#define GAC_ROTARY_MAX_DIM 256
+typedef enum { GAC_ROTARY_HALF = 0, GAC_ROTARY_INTERLEAVED = 1 } gac_rotary_layout;
+typedef enum {
+    GAC_ROTARY_NONE = 0, GAC_ROTARY_LINEAR = 1, GAC_ROTARY_BASE = 2, GAC_ROTARY_PARTS = 3
+} gac_rotary_scaling;
+typedef struct {
+    const void *x;                /* device, element-aligned, caller-owned; last dimension contiguous */
+    void *y;
+    int64_t x_token, x_head;      /* strides in elements                                       */
+    int64_t y_token, y_head;
+} gac_rotary_heads;
+typedef struct {
+    gac_rotary_heads qk[2];       /* queries, keys                                             */
+    uint32_t heads[2];
+    uint32_t n_tokens, n_seqs;
+    uint32_t head_dim, rot_dim;   /* rot_dim even, 2..min(head_dim, GAC_ROTARY_MAX_DIM)         */
+    int32_t dtype;                /* gac_dtype of x and y                                      */
+    int32_t layout;               /* gac_rotary_layout                                         */
+    int32_t inverse;              /* 0 or 1                                                    */
+    int32_t reserved;             /* must be 0                                                 */
+    const int32_t *positions;     /* device [n_tokens] or NULL                                 */
+    const int32_t *cu_seqlens;    /* device [n_seqs + 1]; read when positions is NULL           */
+    const double *freqs;          /* HOST [rot_dim/2], radians per position; copied            */
+    double scale;                 /* multiplies cosine and sine; finite                        */
+} gac_rotary_args;
+int gac_rotary_freqs(double *freqs, uint32_t rot_dim, double base, int scaling, double factor, double trained,
+                     double low, double high);
+int gac_rotary(const gac_rotary_args *args, int cuda_device, void *cuda_stream);
+
+/*
+ * Causal attention over a pack, grouped heads: query head h reads key head
+ * h / (q_heads / kv_heads); token i of a sequence sees tokens j <= i of it.
+ *     S = scale q k^T,  o = softmax(S) v,  lse = log sum exp(S)
+ * and the gradients of o with respect to q, k and v (d_k and d_v are summed over
+ * the query heads that share a key head, in a fixed order: two calls give the same
+ * bits).  Softmax statistics and all sums are binary32; the probabilities, and in the gradient
+ * the score gradients, are rounded once to bfloat16 before they are multiplied.
+ * A token behind the last sequence sees nothing: o = 0, lse = -infinity, gradients 0.
+ * Non-finite values stay within their own sequence.
+ *
+ * q, k, v, o and the gradients are bfloat16 [n_tokens][heads][head_dim], last dimension
+ * contiguous, bases 16-byte aligned and strides multiples of 8 elements (views of one
+ * fused projection will do).  Outputs must not overlap inputs.
+ * gac_attn_backward takes the same gac_attn as the forward call that filled o
+ * and lse, and a workspace of gac_attn_workspace bytes (device, 16-byte aligned; its
+ * contents need not be kept).
+ * Errors: INVALID_ARG, DTYPE, CUDA.
+ */
+#define GAC_ATTN_MAX_HEAD_DIM 128
+typedef struct {
+    void *p;                      /* device, caller-owned                                      */
+    int64_t token, head;          /* strides in elements                                       */
+} gac_attn_heads;
+typedef struct {
+    gac_attn_heads q, k, v, o;
+    float *lse;                   /* device [q_heads][n_tokens], contiguous                    */
+    const int32_t *cu_seqlens;    /* device [n_seqs + 1]                                       */
+    uint32_t n_tokens, n_seqs;
+    uint32_t q_heads, kv_heads;   /* q_heads a multiple of kv_heads                            */
+    uint32_t head_dim;            /* multiple of 8, 8..GAC_ATTN_MAX_HEAD_DIM                   */
+    int32_t dtype;                /* GAC_BF16                                                  */
+    float scale;                  /* finite; 1/sqrt(head_dim) is usual                         */
+    int32_t reserved;             /* must be 0                                                 */
+} gac_attn;
+typedef struct {
+    gac_attn_heads d_o, d_q, d_k, d_v;
+    void *workspace;
+    size_t workspace_bytes;
+} gac_attn_grad;
+size_t gac_attn_workspace(const gac_attn *args);   /* 0 for arguments that the calls would refuse */
+int gac_attn_forward(const gac_attn *args, int cuda_device, void *cuda_stream);
+int gac_attn_backward(const gac_attn *args, const gac_attn_grad *grad, int cuda_device, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

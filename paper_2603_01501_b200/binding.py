@@ -71,11 +71,60 @@ class gac_info(ctypes.Structure):
                 ("reserved", ctypes.c_uint32)]
 
 
+GAC_ROTARY_HALF, GAC_ROTARY_INTERLEAVED = 0, 1
+GAC_ROTARY_NONE, GAC_ROTARY_LINEAR, GAC_ROTARY_BASE, GAC_ROTARY_PARTS = 0, 1, 2, 3
+ROTARY_LAYOUTS = {"half": GAC_ROTARY_HALF, "interleaved": GAC_ROTARY_INTERLEAVED}
+ROTARY_SCALINGS = {"none": GAC_ROTARY_NONE, "linear": GAC_ROTARY_LINEAR, "base": GAC_ROTARY_BASE,
+                   "parts": GAC_ROTARY_PARTS}
+
+
+class gac_clip_tensor(ctypes.Structure):
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_uint64),
+                ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class gac_clip_result(ctypes.Structure):
+    _fields_ = [("sumsq", ctypes.c_double), ("norm", ctypes.c_double), ("scale", ctypes.c_double),
+                ("nonfinite", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class gac_rotary_heads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_token", ctypes.c_int64),
+                ("x_head", ctypes.c_int64), ("y_token", ctypes.c_int64), ("y_head", ctypes.c_int64)]
+
+
+class gac_rotary_args(ctypes.Structure):
+    _fields_ = [("qk", gac_rotary_heads * 2), ("heads", ctypes.c_uint32 * 2), ("n_tokens", ctypes.c_uint32),
+                ("n_seqs", ctypes.c_uint32), ("head_dim", ctypes.c_uint32), ("rot_dim", ctypes.c_uint32),
+                ("dtype", ctypes.c_int32), ("layout", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("positions", ctypes.c_void_p), ("cu_seqlens", ctypes.c_void_p),
+                ("freqs", ctypes.c_void_p), ("scale", ctypes.c_double)]
+
+
+class gac_attn_heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class gac_attn(ctypes.Structure):
+    _fields_ = [("q", gac_attn_heads), ("k", gac_attn_heads), ("v", gac_attn_heads), ("o", gac_attn_heads),
+                ("lse", ctypes.c_void_p), ("cu_seqlens", ctypes.c_void_p), ("n_tokens", ctypes.c_uint32),
+                ("n_seqs", ctypes.c_uint32), ("q_heads", ctypes.c_uint32), ("kv_heads", ctypes.c_uint32),
+                ("head_dim", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
+
+
+class gac_attn_grad(ctypes.Structure):
+    _fields_ = [("d_o", gac_attn_heads), ("d_q", gac_attn_heads), ("d_k", gac_attn_heads), ("d_v", gac_attn_heads),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
 EXPORTS = ["gac_default_hparams", "gac_init", "gac_stats", "gac_stats_partial", "gac_decide",
            "gac_project", "gac_free", "gac_last_error", "gac_set_launch", "gac_get_info",
            "gac_stats_static", "gac_default_adamw", "gac_attach_adamw", "gac_project_adamw",
            "gac_rebind", "gac_next_gradient_set", "gac_exchange_bytes", "gac_exchange_attach",
-           "gac_stats_exchange", "gac_decide_exchange"]
+           "gac_stats_exchange", "gac_decide_exchange", "gac_clip_init", "gac_clip_sumsq", "gac_clip_apply",
+           "gac_clip_grad_norm", "gac_clip_free", "gac_rotary_freqs", "gac_rotary", "gac_attn_workspace",
+           "gac_attn_forward", "gac_attn_backward"]
 
 _lib = None
 
@@ -132,6 +181,21 @@ def load_library() -> ctypes.CDLL:
     L.gac_stats_exchange.restype = i32
     L.gac_decide_exchange.argtypes = [vp, vp, ctypes.POINTER(gac_result)]
     L.gac_decide_exchange.restype = i32
+    P, f64 = ctypes.POINTER, ctypes.c_double
+    L.gac_clip_init.argtypes = [P(vp), P(gac_clip_tensor), u32, i32]
+    L.gac_clip_sumsq.argtypes = [vp, vp, vp]
+    L.gac_clip_apply.argtypes = [vp, vp, vp, f64, f64, vp, P(gac_clip_result)]
+    L.gac_clip_grad_norm.argtypes = [vp, vp, f64, f64, vp, P(gac_clip_result)]
+    L.gac_clip_free.argtypes = [vp]
+    L.gac_rotary_freqs.argtypes = [P(f64), u32, f64, i32, f64, f64, f64, f64]
+    L.gac_rotary.argtypes = [P(gac_rotary_args), i32, vp]
+    L.gac_attn_workspace.argtypes = [P(gac_attn)]
+    L.gac_attn_workspace.restype = ctypes.c_size_t
+    L.gac_attn_forward.argtypes = [P(gac_attn), i32, vp]
+    L.gac_attn_backward.argtypes = [P(gac_attn), P(gac_attn_grad), i32, vp]
+    for name in ("gac_clip_init", "gac_clip_sumsq", "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_free",
+                 "gac_rotary_freqs", "gac_rotary", "gac_attn_forward", "gac_attn_backward"):
+        getattr(L, name).restype = i32
     for name in ("gac_init", "gac_stats", "gac_stats_partial", "gac_decide", "gac_project",
                  "gac_free", "gac_set_launch", "gac_get_info"):
         getattr(L, name).restype = i32
@@ -409,3 +473,228 @@ def gac_rebind(ctx: GacContext, g_list: Sequence[torch.Tensor], d_list: Sequence
         arr[i] = gac_tensor(g.data_ptr(), d.data_ptr(), g.numel())
     ctx._check(load_library().gac_rebind(ctx.handle, arr, n))
     ctx._keep = (list(g_list), list(d_list))
+
+
+# ---------------------------------------------------------------- around the rule: packed rollouts
+
+
+def _on(stream, device: torch.device):
+    """The stream to launch on, as a torch stream of the tensors' device.  What a call allocates is allocated on
+    it, so that the caching allocator hands the memory on in that stream's order."""
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    if stream == torch.cuda.current_stream(device):
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _check(rc: int) -> None:
+    if rc != GAC_OK:
+        raise GacError(rc, load_library().gac_last_error(None).decode())
+
+
+class ClipContext:
+    """Owner of one ``gac_clip_ctx``; keeps references to the tensors in its table."""
+
+    def __init__(self, handle: int, g_list, out_list):
+        self.handle = ctypes.c_void_p(handle)
+        self._keep = (list(g_list), list(out_list))
+
+    def __del__(self):
+        try:
+            gac_clip_free(self)
+        except Exception:
+            pass
+
+
+def gac_clip_init(g_list: Sequence[torch.Tensor], out_list: Optional[Sequence[torch.Tensor]] = None,
+                  device: Optional[int] = None) -> ClipContext:
+    """gac_clip_init of the C ABI on a list of contiguous CUDA tensors, float32 and bfloat16 mixed as
+    they come.  ``out_list``: where the clipped gradients go; None clips in place."""
+    L = load_library()
+    outs = g_list if out_list is None else out_list
+    if len(g_list) != len(outs):
+        raise ValueError("gradient and output lists differ in length")
+    n = len(g_list)
+    arr = (gac_clip_tensor * max(n, 1))()
+    for i, (g, o) in enumerate(zip(g_list, outs)):
+        if not (g.is_cuda and o.is_cuda and g.is_contiguous() and o.is_contiguous()):
+            raise ValueError("tensors must be contiguous CUDA tensors")
+        if g.numel() != o.numel() or g.dtype != o.dtype:
+            raise ValueError(f"tensor {i}: gradient and output differ in numel or dtype")
+        if g.dtype not in _DT:
+            raise GacError(GAC_ERR_DTYPE, f"unsupported dtype {g.dtype}")
+        arr[i] = gac_clip_tensor(g.data_ptr(), o.data_ptr(), g.numel(), _DT[g.dtype], 0)
+    if device is None:
+        device = g_list[0].device.index if n else torch.cuda.current_device()
+    if any(t.device.index != device for t in list(g_list) + list(outs)):
+        raise ValueError("all tensors of a list must be on one device")
+    out = ctypes.c_void_p()
+    _check(L.gac_clip_init(ctypes.byref(out), arr, n, device))
+    return ClipContext(out.value, g_list, outs)
+
+
+def _clip_result(rc: int, res) -> Optional[gac_clip_result]:
+    if rc not in (GAC_OK, GAC_ERR_NONFINITE):
+        _check(rc)
+    return res
+
+
+def _norm_ptr(norm_out: Optional[torch.Tensor]) -> Optional[int]:
+    if norm_out is None:
+        return None
+    if not (norm_out.is_cuda and norm_out.dtype == torch.float32 and norm_out.numel() >= 1):
+        raise ValueError("norm_out must be a CUDA float32 tensor")
+    return norm_out.data_ptr()
+
+
+def gac_clip_grad_norm(ctx: ClipContext, max_norm: float, eps: float = 1e-6, norm_out: Optional[torch.Tensor] = None,
+                       stream=None, fetch: bool = False) -> Optional[gac_clip_result]:
+    """Norm of the list, and the list scaled by min(1, max_norm/(norm + eps)).  With fetch=False nothing
+    leaves the device; a non-finite norm leaves every output as it was and is told by the record."""
+    res = gac_clip_result() if fetch else None
+    rc = load_library().gac_clip_grad_norm(ctx.handle, _stream_ptr(stream), max_norm, eps, _norm_ptr(norm_out),
+                                           ctypes.byref(res) if fetch else None)
+    return _clip_result(rc, res)
+
+
+def gac_clip_sumsq(ctx: ClipContext, sumsq_out: torch.Tensor, stream=None) -> None:
+    """Sharded form: this rank's sum of squares into a CUDA float64 tensor, for the caller's all-reduce."""
+    if not (sumsq_out.is_cuda and sumsq_out.dtype == torch.float64 and sumsq_out.numel() >= 1):
+        raise ValueError("sumsq_out must be a CUDA float64 tensor")
+    _check(load_library().gac_clip_sumsq(ctx.handle, _stream_ptr(stream), sumsq_out.data_ptr()))
+
+
+def gac_clip_apply(ctx: ClipContext, sumsq_in: torch.Tensor, max_norm: float, eps: float = 1e-6,
+                   norm_out: Optional[torch.Tensor] = None, stream=None, fetch: bool = False) -> Optional[gac_clip_result]:
+    """Sharded form: scales this rank's list by the factor that follows from the global sum of squares."""
+    if not (sumsq_in.is_cuda and sumsq_in.dtype == torch.float64 and sumsq_in.numel() >= 1):
+        raise ValueError("sumsq_in must be a CUDA float64 tensor")
+    res = gac_clip_result() if fetch else None
+    rc = load_library().gac_clip_apply(ctx.handle, _stream_ptr(stream), sumsq_in.data_ptr(), max_norm, eps,
+                                       _norm_ptr(norm_out), ctypes.byref(res) if fetch else None)
+    return _clip_result(rc, res)
+
+
+def gac_clip_free(ctx: ClipContext) -> None:
+    if ctx.handle:
+        load_library().gac_clip_free(ctx.handle)
+        ctx.handle = ctypes.c_void_p(None)
+    ctx._keep = ([], [])
+
+
+def gac_rotary_freqs(rot_dim: int, base: float = 1e4, scaling: str = "none", factor: float = 1.0,
+                     trained: float = 4096.0, low: float = 1.0, high: float = 4.0):
+    """Radians per position of each pair (a float64 array of rot_dim/2), stretched for contexts ``factor``
+    times as long as the trained one; see gac.h for the scalings."""
+    import numpy as np
+    freqs = np.zeros(max(rot_dim // 2, 1), dtype=np.float64)
+    _check(load_library().gac_rotary_freqs(freqs.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), rot_dim, base,
+                                           ROTARY_SCALINGS[scaling], factor, trained, low, high))
+    return freqs
+
+
+def _int32_ptr(t: Optional[torch.Tensor], name: str, device: torch.device) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.device != device or t.dim() != 1 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 vector on the tensors' device")
+    return t.data_ptr()
+
+
+def _heads(t: torch.Tensor, name: str, like: torch.Tensor) -> None:
+    if t.dim() != 3 or not t.is_cuda or t.device != like.device:
+        raise ValueError(f"{name} must be a CUDA tensor [tokens, heads, head_dim]")
+    if t.dtype != like.dtype or t.shape[0] != like.shape[0] or t.shape[2] != like.shape[2]:
+        raise ValueError(f"{name} differs in dtype, tokens or head_dim")
+    if t.stride(2) != 1 and t.shape[2] > 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+
+
+def gac_rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Optional[torch.Tensor] = None,
+               cu_seqlens: Optional[torch.Tensor] = None, layout: str = "half", scale: float = 1.0,
+               inverse: bool = False, in_place: bool = False, stream=None):
+    """Rotary positions on q (and k, or None), [tokens, heads, head_dim] float32 or bfloat16 views.
+    ``freqs``: float64 radians per position (gac_rotary_freqs); it turns the first 2 * len(freqs) elements of
+    a head.  Positions are given, or follow from ``cu_seqlens``.  Returns (q', k'): new contiguous tensors, or
+    the given ones when ``in_place``."""
+    import numpy as np
+    xs = [q] if k is None else [q, k]
+    if q.dtype not in _DT:
+        raise GacError(GAC_ERR_DTYPE, f"unsupported dtype {q.dtype}")
+    for x, name in zip(xs, ("q", "k")):
+        _heads(x, name, q)
+    if (positions is None) == (cu_seqlens is None):
+        raise ValueError("give positions or cu_seqlens")
+    if positions is not None and positions.numel() != q.shape[0]:
+        raise ValueError("one position per token")
+    freqs = np.ascontiguousarray(freqs, dtype=np.float64)
+    stream = _on(stream, q.device)
+    ys = xs if in_place else [_empty(x.shape, x.dtype, x.device, stream) for x in xs]
+    a = gac_rotary_args()
+    for i, (x, y) in enumerate(zip(xs, ys)):
+        a.qk[i] = gac_rotary_heads(x.data_ptr(), y.data_ptr(), x.stride(0), x.stride(1), y.stride(0), y.stride(1))
+        a.heads[i] = x.shape[1]
+    a.n_tokens, a.head_dim, a.rot_dim = q.shape[0], q.shape[2], 2 * freqs.size
+    a.n_seqs = 0 if cu_seqlens is None else cu_seqlens.numel() - 1
+    a.dtype, a.layout, a.inverse = _DT[q.dtype], ROTARY_LAYOUTS[layout], int(bool(inverse))
+    a.positions = _int32_ptr(positions, "positions", q.device)
+    a.cu_seqlens = _int32_ptr(cu_seqlens, "cu_seqlens", q.device)
+    a.freqs, a.scale = freqs.ctypes.data, scale
+    _check(load_library().gac_rotary(ctypes.byref(a), q.device.index, stream.cuda_stream))
+    return ys[0], (ys[1] if k is not None else None)
+
+
+def _attn_heads(t: torch.Tensor) -> gac_attn_heads:
+    return gac_attn_heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _attn_args(q, k, v, o, lse, cu_seqlens, scale) -> gac_attn:
+    if q.dtype not in _DT:
+        raise GacError(GAC_ERR_DTYPE, f"unsupported dtype {q.dtype}")
+    for t, name in ((q, "q"), (k, "k"), (v, "v"), (o, "o")):
+        _heads(t, name, q)
+    if k.shape != v.shape or o.shape != q.shape:
+        raise ValueError("k and v, and o and q, must have the same shape")
+    if not (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (q.shape[1], q.shape[0])):
+        raise ValueError("lse must be a contiguous float32 tensor [q_heads, tokens]")
+    if cu_seqlens.numel() < 1:
+        raise ValueError("cu_seqlens has one entry more than there are sequences")
+    return gac_attn(_attn_heads(q), _attn_heads(k), _attn_heads(v), _attn_heads(o), lse.data_ptr(),
+                    _int32_ptr(cu_seqlens, "cu_seqlens", q.device), q.shape[0], cu_seqlens.numel() - 1, q.shape[1],
+                    k.shape[1], q.shape[2], _DT[q.dtype], q.shape[2] ** -0.5 if scale is None else scale, 0)
+
+
+def gac_attn_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
+                     scale: Optional[float] = None, stream=None):
+    """Causal attention over packed sequences: q [tokens, q_heads, head_dim], k and v [tokens, kv_heads,
+    head_dim], bfloat16 views.  Returns (o, lse): o like q, contiguous; lse [q_heads, tokens] float32."""
+    _heads(q, "q", q)
+    stream = _on(stream, q.device)
+    o = _empty(q.shape, q.dtype, q.device, stream)
+    lse = _empty((q.shape[1], q.shape[0]), torch.float32, q.device, stream)
+    a = _attn_args(q, k, v, o, lse, cu_seqlens, scale)
+    _check(load_library().gac_attn_forward(ctypes.byref(a), q.device.index, stream.cuda_stream))
+    return o, lse
+
+
+def gac_attn_backward(d_o: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor,
+                      lse: torch.Tensor, cu_seqlens: torch.Tensor, scale: Optional[float] = None, stream=None):
+    """Gradients (d_q, d_k, d_v) of gac_attn_forward's o, given d_o; new contiguous tensors."""
+    L = load_library()
+    a = _attn_args(q, k, v, o, lse, cu_seqlens, scale)
+    _heads(d_o, "d_o", q)
+    if d_o.shape != q.shape:
+        raise ValueError("d_o must have q's shape")
+    stream = _on(stream, q.device)
+    d_q, d_k, d_v = (_empty(t.shape, t.dtype, t.device, stream) for t in (q, k, v))
+    need = L.gac_attn_workspace(ctypes.byref(a))
+    workspace = _empty((max(need, 16),), torch.uint8, q.device, stream)
+    g = gac_attn_grad(_attn_heads(d_o), _attn_heads(d_q), _attn_heads(d_k), _attn_heads(d_v), workspace.data_ptr(), need)
+    _check(L.gac_attn_backward(ctypes.byref(a), ctypes.byref(g), q.device.index, stream.cuda_stream))
+    return d_q, d_k, d_v

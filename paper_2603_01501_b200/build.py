@@ -7,9 +7,9 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = os.path.join(HERE, "csrc", "gac.cu")
-HDR = os.path.join(ROOT, "include", "gac.h")
-KERNELS = os.path.join(HERE, "csrc", "gac_kernels.cuh")
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("gac.cu", "clip.cu", "rotary.cu", "attention.cu")]
+HEADERS = [os.path.join(ROOT, "include", "gac.h")] + \
+          [os.path.join(HERE, "csrc", f) for f in ("gac_host.h", "gac_kernels.cuh")]
 LIB = os.path.join(HERE, "libgac_b200.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -17,12 +17,12 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    newest = max(os.path.getmtime(SRC), os.path.getmtime(HDR), os.path.getmtime(KERNELS))
+    newest = max(os.path.getmtime(f) for f in SOURCES + HEADERS)
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= newest:
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
     cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + \
-          ["-I", os.path.join(ROOT, "include"), "-o", LIB, SRC]
+          ["-I", os.path.join(ROOT, "include"), "-o", LIB] + SOURCES
     proc = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or proc.returncode != 0:
         sys.stderr.write(proc.stdout + proc.stderr)

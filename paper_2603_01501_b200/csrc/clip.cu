@@ -1,0 +1,398 @@
+// Global gradient norm over a list of tensors, and clipping (gac_clip_* of include/gac.h).
+//
+//   norm = sqrt(sum g_i^2),   out_i = min(1, max_norm / (norm + eps)) g_i
+//
+// The norm has to be known before the first element can be written, so a list beyond the chip's
+// memory is read twice and written once: the floor is the HBM traffic of that.  Squares are summed in
+// binary64 (a product of two binary32 values is exact there, and no scale of the gradient overflows or
+// vanishes), in a fixed order: chunk c belongs to CTA c mod grid, each CTA leaves one partial sum, and the
+// last CTA to finish adds the partials in index order.
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+#include <cstddef>
+#include <new>
+#include <utility>
+#include <vector>
+
+#include "gac.h"
+#include "gac_host.h"
+
+static_assert(sizeof(gac_clip_tensor) == 32 && sizeof(gac_clip_result) == 32, "clip structs layout");
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kChunkElems = 16384;
+constexpr int kMinChunkElems = 2048;
+constexpr int kCtasPerSm = 4;
+constexpr uint32_t kBf16 = 1u, kInPlace = 2u;
+
+struct __align__(16) ClipChunk {
+    uint64_t g, out;   // device addresses of the chunk's first element
+    uint32_t n, flags;
+    uint64_t pad;
+};
+static_assert(sizeof(ClipChunk) == 32, "chunk descriptors are read as two 16-byte words");
+
+__device__ __forceinline__ ClipChunk load_chunk(const ClipChunk *table, uint32_t c) {
+    const uint4 *p = reinterpret_cast<const uint4 *>(table + c);
+    const uint4 a = __ldg(p), b = __ldg(p + 1);
+    ClipChunk ch;
+    ch.g = (uint64_t(a.y) << 32) | a.x;
+    ch.out = (uint64_t(a.w) << 32) | a.z;
+    ch.n = b.x;
+    ch.flags = b.y;
+    ch.pad = 0;
+    return ch;
+}
+
+__device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// One element of either type at index i.
+__device__ __forceinline__ float load_one(uint64_t base, uint32_t i, bool bf16) {
+    return bf16 ? __uint_as_float(uint32_t(reinterpret_cast<const uint16_t *>(base)[i]) << 16)
+                : reinterpret_cast<const float *>(base)[i];
+}
+__device__ __forceinline__ void store_one(uint64_t base, uint32_t i, bool bf16, float v) {
+    if (bf16) reinterpret_cast<uint16_t *>(base)[i] = uint16_t(pack_bf16x2(v, 0.0f) & 0xFFFFu);
+    else reinterpret_cast<float *>(base)[i] = v;
+}
+
+// Elements before the first 16-byte boundary of the chunk's input.
+__device__ __forceinline__ uint32_t head_elems(uint64_t base, uint32_t n, bool bf16) {
+    const uint32_t off = uint32_t((16u - (base & 15u)) & 15u) >> (bf16 ? 1 : 2);
+    return off < n ? off : n;
+}
+
+__device__ __forceinline__ void add_square(double &acc, float x) {
+    const double v = double(x);
+    acc = __fma_rn(v, v, acc);
+}
+
+__device__ __forceinline__ void add_squares(double (&acc)[2], uint4 w, bool bf16) {
+    if (bf16) {
+        add_square(acc[0], lo_bf16(w.x)); add_square(acc[1], hi_bf16(w.x));
+        add_square(acc[0], lo_bf16(w.y)); add_square(acc[1], hi_bf16(w.y));
+        add_square(acc[0], lo_bf16(w.z)); add_square(acc[1], hi_bf16(w.z));
+        add_square(acc[0], lo_bf16(w.w)); add_square(acc[1], hi_bf16(w.w));
+    } else {
+        add_square(acc[0], __uint_as_float(w.x)); add_square(acc[1], __uint_as_float(w.y));
+        add_square(acc[0], __uint_as_float(w.z)); add_square(acc[1], __uint_as_float(w.w));
+    }
+}
+
+__device__ double cta_sum(double v, double *shared) {
+    for (int o = 16; o > 0; o >>= 1) v = __dadd_rn(v, __shfl_down_sync(0xFFFFFFFFu, v, o));
+    const int warp = threadIdx.x >> 5;
+    if ((threadIdx.x & 31) == 0) shared[warp] = v;
+    __syncthreads();
+    double s = 0.0;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < kThreads / 32; ++w) s = __dadd_rn(s, shared[w]);
+    __syncthreads();
+    return s;   // valid in thread 0
+}
+
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+clip_sumsq_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, double *partials, unsigned *ticket,
+                  double *sumsq) {
+    __shared__ double shared[kThreads / 32];
+    __shared__ bool last;
+    double acc[2] = {0.0, 0.0};
+    for (uint32_t c = blockIdx.x; c < n_chunks; c += gridDim.x) {
+        const ClipChunk ch = load_chunk(table, c);
+        const bool bf16 = ch.flags & kBf16;
+        const uint32_t head = head_elems(ch.g, ch.n, bf16);
+        const uint32_t per = bf16 ? 8u : 4u, vecs = (ch.n - head) / per;
+        const uint4 *v = reinterpret_cast<const uint4 *>(ch.g + uint64_t(head) * (bf16 ? 2 : 4));
+        if (threadIdx.x < head) add_square(acc[0], load_one(ch.g, threadIdx.x, bf16));
+        uint32_t i = threadIdx.x;
+        for (; i + 7 * kThreads < vecs; i += 8 * kThreads) {
+            uint4 w[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) w[u] = __ldg(v + i + u * kThreads);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) add_squares(acc, w[u], bf16);
+        }
+        for (; i < vecs; i += kThreads) add_squares(acc, __ldg(v + i), bf16);
+        for (uint32_t j = head + vecs * per + threadIdx.x; j < ch.n; j += kThreads)
+            add_square(acc[0], load_one(ch.g, j, bf16));
+    }
+    const double mine = cta_sum(__dadd_rn(acc[0], acc[1]), shared);
+    if (threadIdx.x == 0) {
+        partials[blockIdx.x] = mine;
+        __threadfence();
+        last = (atomicInc(ticket, gridDim.x - 1) == gridDim.x - 1);   // back at 0 for the next call
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double s = 0.0;
+    for (uint32_t i = threadIdx.x; i < gridDim.x; i += kThreads) s = __dadd_rn(s, __ldcg(partials + i));
+    s = cta_sum(s, shared);
+    if (threadIdx.x == 0) *sumsq = s;
+}
+
+__device__ __forceinline__ uint4 scaled(uint4 w, float s, bool bf16) {
+    if (bf16)
+        return make_uint4(pack_bf16x2(lo_bf16(w.x) * s, hi_bf16(w.x) * s), pack_bf16x2(lo_bf16(w.y) * s, hi_bf16(w.y) * s),
+                          pack_bf16x2(lo_bf16(w.z) * s, hi_bf16(w.z) * s), pack_bf16x2(lo_bf16(w.w) * s, hi_bf16(w.w) * s));
+    return make_uint4(__float_as_uint(__uint_as_float(w.x) * s), __float_as_uint(__uint_as_float(w.y) * s),
+                      __float_as_uint(__uint_as_float(w.z) * s), __float_as_uint(__uint_as_float(w.w) * s));
+}
+
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+clip_apply_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, const double *sumsq, double max_norm, double eps,
+                  float *norm_out, gac_clip_result *rec) {
+    __shared__ float factor;
+    __shared__ int nonfinite;
+    if (threadIdx.x == 0) {
+        const double s2 = *sumsq, norm = __dsqrt_rn(s2);
+        const bool bad = !(s2 <= 1.7976931348623157e308);   // NaN or +Inf
+        const double f = __ddiv_rn(max_norm, __dadd_rn(norm, eps));
+        factor = (f < 1.0) ? __double2float_rn(f) : 1.0f;
+        nonfinite = bad;
+        if (blockIdx.x == 0) {
+            rec->sumsq = s2;
+            rec->norm = norm;
+            rec->scale = bad ? 1.0 : double(factor);
+            rec->nonfinite = bad;
+            rec->reserved = 0;
+            if (norm_out) *norm_out = __double2float_rn(norm);
+        }
+    }
+    __syncthreads();
+    if (nonfinite) return;
+    const float s = factor;
+    for (uint32_t c = blockIdx.x; c < n_chunks; c += gridDim.x) {
+        const ClipChunk ch = load_chunk(table, c);
+        const bool bf16 = ch.flags & kBf16;
+        if (s == 1.0f && (ch.flags & kInPlace)) continue;
+        const uint32_t size = bf16 ? 2u : 4u;
+        uint32_t head = head_elems(ch.g, ch.n, bf16);
+        const uint32_t per = 16u / size;
+        uint32_t vecs = (ch.n - head) / per;
+        if ((ch.g ^ ch.out) & 15u) head = vecs = 0;   // input and output never share a 16-byte boundary
+        const uint4 *v = reinterpret_cast<const uint4 *>(ch.g + uint64_t(head) * size);
+        uint4 *o = reinterpret_cast<uint4 *>(ch.out + uint64_t(head) * size);
+        if (threadIdx.x < head) store_one(ch.out, threadIdx.x, bf16, load_one(ch.g, threadIdx.x, bf16) * s);
+        uint32_t i = threadIdx.x;
+        for (; i + 7 * kThreads < vecs; i += 8 * kThreads) {
+            uint4 w[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) w[u] = v[i + u * kThreads];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) o[i + u * kThreads] = scaled(w[u], s, bf16);
+        }
+        for (; i < vecs; i += kThreads) o[i] = scaled(v[i], s, bf16);
+        for (uint32_t j = head + vecs * per + threadIdx.x; j < ch.n; j += kThreads)
+            store_one(ch.out, j, bf16, load_one(ch.g, j, bf16) * s);
+    }
+}
+
+int fail(std::nullptr_t, int code, const char *fmt, const char *a = "", long long b = 0) {
+    snprintf(g_init_err, sizeof(g_init_err), fmt, a, b);
+    return code;
+}
+
+}  // namespace
+
+struct gac_clip_ctx {
+    int device = 0, sms = 0;
+    uint32_t n_chunks = 0;
+    uint32_t grid = 0;
+    ClipChunk *d_chunks = nullptr;
+    double *d_partials = nullptr;      // one per CTA, then the list's sum
+    unsigned *d_ticket = nullptr;
+    gac_clip_result *d_rec = nullptr;
+    gac_clip_result *h_rec = nullptr;  // pinned
+};
+
+namespace {
+
+void release(gac_clip_ctx *c) {
+    if (c->d_chunks) cudaFree(c->d_chunks);
+    if (c->d_partials) cudaFree(c->d_partials);
+    if (c->h_rec) cudaFreeHost(c->h_rec);
+}
+
+int check_list(const gac_clip_tensor *list, uint32_t n) {
+    std::vector<std::pair<uint64_t, uint64_t>> writes, reads;
+    for (uint32_t i = 0; i < n; ++i) {
+        const gac_clip_tensor &t = list[i];
+        if (t.dtype != GAC_F32 && t.dtype != GAC_BF16)
+            return fail(nullptr, GAC_ERR_DTYPE, "tensor %s%lld: gradients are float32 or bfloat16", "", i);
+        if (t.reserved != 0) return fail(nullptr, GAC_ERR_INVALID_ARG, "tensor %s%lld: reserved field must be 0", "", i);
+        if (t.numel == 0) continue;
+        const uint64_t size = t.dtype == GAC_BF16 ? 2 : 4;
+        const uint64_t g = reinterpret_cast<uint64_t>(t.g), o = reinterpret_cast<uint64_t>(t.out);
+        if (!g || !o) return fail(nullptr, GAC_ERR_INVALID_ARG, "tensor %s%lld has a NULL pointer", "", i);
+        if (t.numel > (1ull << 40))
+            return fail(nullptr, GAC_ERR_INVALID_ARG, "tensor %s%lld is larger than 2^40 elements", "", i);
+        if (g % size || o % size) return fail(nullptr, GAC_ERR_INVALID_ARG, "tensor %s%lld is not element-aligned", "", i);
+        writes.emplace_back(o, o + t.numel * size);
+        if (g != o) reads.emplace_back(g, g + t.numel * size);
+    }
+    // what is written must not overlap anything else that is written, nor anything read from elsewhere
+    std::sort(writes.begin(), writes.end());
+    for (size_t i = 1; i < writes.size(); ++i)
+        if (writes[i].first < writes[i - 1].second)
+            return fail(nullptr, GAC_ERR_INVALID_ARG, "output buffers of different tensors overlap%s");
+    for (const auto &r : reads) {
+        auto it = std::lower_bound(writes.begin(), writes.end(), std::make_pair(r.first, uint64_t(0)));
+        if ((it != writes.end() && it->first < r.second) || (it != writes.begin() && std::prev(it)->second > r.first))
+            return fail(nullptr, GAC_ERR_INVALID_ARG, "an output buffer overlaps a gradient other than its own%s");
+    }
+    return GAC_OK;
+}
+
+int setup(gac_clip_ctx *c, const gac_clip_tensor *list, uint32_t n) {
+    GAC_CUDA(nullptr, cudaDeviceGetAttribute(&c->sms, cudaDevAttrMultiProcessorCount, c->device));
+    uint64_t total = 0;
+    for (uint32_t i = 0; i < n; ++i) total += list[i].numel;
+    // short lists get shorter chunks so that every CTA has work
+    uint64_t ce = kChunkElems;
+    while (ce > kMinChunkElems && total / ce < uint64_t(kCtasPerSm) * c->sms) ce /= 2;
+    std::vector<ClipChunk> table;
+    for (uint32_t i = 0; i < n; ++i) {
+        const gac_clip_tensor &t = list[i];
+        const uint64_t size = t.dtype == GAC_BF16 ? 2 : 4;
+        for (uint64_t off = 0; off < t.numel; off += ce) {
+            ClipChunk ch;
+            ch.g = reinterpret_cast<uint64_t>(t.g) + off * size;
+            ch.out = reinterpret_cast<uint64_t>(t.out) + off * size;
+            ch.n = uint32_t(std::min<uint64_t>(ce, t.numel - off));
+            ch.flags = (t.dtype == GAC_BF16 ? kBf16 : 0u) | (t.g == t.out ? kInPlace : 0u);
+            ch.pad = 0;
+            table.push_back(ch);
+        }
+    }
+    if (table.size() > 0xFFFFFFF0ull) return fail(nullptr, GAC_ERR_INVALID_ARG, "too many chunks%s");
+    c->n_chunks = uint32_t(table.size());
+    c->grid = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(uint64_t(c->sms) * kCtasPerSm, table.size())));
+    const size_t work = (size_t(c->grid) + 1) * sizeof(double) + 256 + sizeof(gac_clip_result);
+    GAC_CUDA(nullptr, cudaMalloc(&c->d_chunks, std::max<size_t>(1, table.size()) * sizeof(ClipChunk)));
+    if (!table.empty())
+        GAC_CUDA(nullptr, cudaMemcpy(c->d_chunks, table.data(), table.size() * sizeof(ClipChunk), cudaMemcpyHostToDevice));
+    GAC_CUDA(nullptr, cudaMalloc(&c->d_partials, work));
+    GAC_CUDA(nullptr, cudaMemset(c->d_partials, 0, work));
+    c->d_rec = reinterpret_cast<gac_clip_result *>(c->d_partials + c->grid + 1);
+    c->d_ticket = reinterpret_cast<unsigned *>(c->d_rec + 1);
+    GAC_CUDA(nullptr, cudaMallocHost(&c->h_rec, sizeof(gac_clip_result)));
+    return GAC_OK;
+}
+
+int launch_sumsq(gac_clip_ctx *c, cudaStream_t s, double *out) {
+    clip_sumsq_kernel<<<c->grid, kThreads, 0, s>>>(c->d_chunks, c->n_chunks, c->d_partials, c->d_ticket, out);
+    GAC_CUDA(nullptr, cudaGetLastError());
+    return GAC_OK;
+}
+
+int launch_apply(gac_clip_ctx *c, cudaStream_t s, const double *in, double max_norm, double eps, float *norm_out,
+                 gac_clip_result *host_out) {
+    clip_apply_kernel<<<c->grid, kThreads, 0, s>>>(c->d_chunks, c->n_chunks, in, max_norm, eps, norm_out, c->d_rec);
+    GAC_CUDA(nullptr, cudaGetLastError());
+    if (!host_out) return GAC_OK;
+    GAC_CUDA(nullptr, cudaMemcpyAsync(c->h_rec, c->d_rec, sizeof(gac_clip_result), cudaMemcpyDeviceToHost, s));
+    GAC_CUDA(nullptr, cudaStreamSynchronize(s));
+    *host_out = *c->h_rec;
+    if (host_out->nonfinite) return fail(nullptr, GAC_ERR_NONFINITE, "NaN or Inf met in the gradient norm%s");
+    return GAC_OK;
+}
+
+int check_limits(double max_norm, double eps, const float *norm_out) {
+    if (!(max_norm > 0.0)) return fail(nullptr, GAC_ERR_INVALID_ARG, "max_norm must be > 0%s");
+    if (!(eps >= 0.0) || !isfinite(eps)) return fail(nullptr, GAC_ERR_INVALID_ARG, "eps must be finite and >= 0%s");
+    if (reinterpret_cast<uint64_t>(norm_out) % 4) return fail(nullptr, GAC_ERR_INVALID_ARG, "norm_out must be 4-byte aligned%s");
+    return GAC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gac_clip_init(gac_clip_ctx **out, const gac_clip_tensor *list, uint32_t n, int cuda_device) {
+    if (!out) return fail(nullptr, GAC_ERR_INVALID_ARG, "out is NULL%s");
+    *out = nullptr;
+    if (!list || n == 0) return fail(nullptr, GAC_ERR_INVALID_ARG, "empty tensor list%s");
+    gac_clip_ctx *c = nullptr;
+    try {
+        if (int rc = check_list(list, n)) return rc;
+        int n_dev = 0;
+        if (cudaGetDeviceCount(&n_dev) != cudaSuccess || n_dev == 0)
+            return fail(nullptr, GAC_ERR_CUDA, "no CUDA device is available%s");
+        if (cuda_device < 0 || cuda_device >= n_dev)
+            return fail(nullptr, GAC_ERR_INVALID_ARG, "cuda_device %s%lld out of range", "", cuda_device);
+        DeviceGuard guard(cuda_device);
+        if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
+        c = new gac_clip_ctx;
+        c->device = cuda_device;
+        if (int rc = setup(c, list, n)) {
+            release(c);
+            delete c;
+            return rc;
+        }
+    } catch (const std::bad_alloc &) {   // nothing may be thrown through the C boundary
+        if (c) {
+            release(c);
+            delete c;
+        }
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "out of host memory%s");
+    }
+    *out = c;
+    return GAC_OK;
+}
+
+int gac_clip_sumsq(gac_clip_ctx *ctx, void *cuda_stream, double *sumsq_out) {
+    if (!ctx) return fail(nullptr, GAC_ERR_INVALID_ARG, "ctx is NULL%s");
+    if (!sumsq_out || reinterpret_cast<uint64_t>(sumsq_out) % 8)
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "sumsq_out must be an 8-byte aligned device pointer%s");
+    Range range("gac_clip_sumsq");
+    DeviceGuard guard(ctx->device);
+    return launch_sumsq(ctx, static_cast<cudaStream_t>(cuda_stream), sumsq_out);
+}
+
+int gac_clip_apply(gac_clip_ctx *ctx, void *cuda_stream, const double *sumsq_in, double max_norm, double eps, float *norm_out,
+                   gac_clip_result *host_out) {
+    if (!ctx) return fail(nullptr, GAC_ERR_INVALID_ARG, "ctx is NULL%s");
+    if (!sumsq_in || reinterpret_cast<uint64_t>(sumsq_in) % 8)
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "sumsq_in must be an 8-byte aligned device pointer%s");
+    if (int rc = check_limits(max_norm, eps, norm_out)) return rc;
+    Range range("gac_clip_apply");
+    DeviceGuard guard(ctx->device);
+    return launch_apply(ctx, static_cast<cudaStream_t>(cuda_stream), sumsq_in, max_norm, eps, norm_out, host_out);
+}
+
+int gac_clip_grad_norm(gac_clip_ctx *ctx, void *cuda_stream, double max_norm, double eps, float *norm_out,
+                       gac_clip_result *host_out) {
+    if (!ctx) return fail(nullptr, GAC_ERR_INVALID_ARG, "ctx is NULL%s");
+    if (int rc = check_limits(max_norm, eps, norm_out)) return rc;
+    Range range("gac_clip_grad_norm");
+    DeviceGuard guard(ctx->device);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    double *sum = ctx->d_partials + ctx->grid;
+    if (int rc = launch_sumsq(ctx, s, sum)) return rc;
+    return launch_apply(ctx, s, sum, max_norm, eps, norm_out, host_out);
+}
+
+int gac_clip_free(gac_clip_ctx *ctx) {
+    if (!ctx) return GAC_OK;
+    {
+        DeviceGuard guard(ctx->device);
+        release(ctx);
+    }
+    delete ctx;
+    return GAC_OK;
+}
+
+}  // extern "C"

@@ -17,7 +17,6 @@
 // here, hence no tensor-core path.
 #include <cuda_runtime.h>
 #include <math.h>
-#include <nvtx3/nvToolsExt.h>
 #include <stdint.h>
 #include <stdio.h>
 #include <string.h>
@@ -30,6 +29,7 @@
 
 #include "gac.h"
 
+#include "gac_host.h"
 #include "gac_kernels.cuh"
 
 // The ABI's structs as laid out for callers in other languages (the Python binding mirrors them).
@@ -85,42 +85,13 @@ struct gac_ctx {
 
 namespace {
 
-thread_local char g_init_err[512] = "no error";
-
 int fail(gac_ctx *ctx, int code, const char *fmt, const char *a = "", long long b = 0) {
     char *dst = ctx ? ctx->err : g_init_err;
     snprintf(dst, 512, fmt, a, b);
     return code;
 }
 
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
-        ok = (cudaSetDevice(dev) == cudaSuccess);
-    }
-    ~DeviceGuard() {
-        if (prev >= 0) cudaSetDevice(prev);
-    }
-};
-
-#define GAC_CUDA(ctx, call)                                                          \
-    do {                                                                             \
-        cudaError_t e_ = (call);                                                     \
-        if (e_ != cudaSuccess)                                                       \
-            return fail((ctx), GAC_ERR_CUDA, "%s (CUDA error %lld): " #call,        \
-                        cudaGetErrorString(e_), (long long)e_);                      \
-    } while (0)
-
 size_t elem_size(int dt) { return dt == GAC_BF16 ? 2 : 4; }
-
-// Named range around the host side of a call, visible in a timeline profiler; costs one
-// pointer test when no tool is attached.
-struct Range {
-    explicit Range(const char *name) { nvtxRangePushA(name); }
-    ~Range() { nvtxRangePop(); }
-};
 
 void release_device(gac_ctx *c) {
     if (c->d_chunks) cudaFree(c->d_chunks);

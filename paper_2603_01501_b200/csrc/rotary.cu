@@ -1,0 +1,223 @@
+// Rotary positions on the query and key heads of a pack of tokens (gac_rotary of include/gac.h).
+//
+//   (x, y) -> scale (x cos a - y sin a, x sin a + y cos a),   a = position * freq
+//
+// Bound by HBM: every element is read once and written once, three flops each.  A CTA takes a few tokens at
+// a time: its threads first work out the tokens' sines and cosines once (the angle is reduced to one turn in
+// binary64, then sincospi in binary32: exact to the last bits at any position, no table in memory),
+// leave them in shared memory, and then every head of those tokens is turned with them.
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+#include <cstddef>
+
+#include "gac.h"
+#include "gac_host.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTokens = 4;   // tokens of a CTA's turn
+
+struct RotaryDev {
+    const char *x[2];
+    char *y[2];
+    long long x_token[2], x_head[2], y_token[2], y_head[2];
+    uint32_t heads[2];
+    uint32_t n_tokens, n_seqs, head_dim, pairs;
+    const int32_t *positions, *cu;
+    float scale;
+    int inverse;
+    double turns[GAC_ROTARY_MAX_DIM / 2];   // turns per position of each pair
+};
+
+__device__ __forceinline__ float load_el(const char *p, float) { return *reinterpret_cast<const float *>(p); }
+__device__ __forceinline__ float load_el(const char *p, uint16_t) {
+    return __uint_as_float(uint32_t(*reinterpret_cast<const uint16_t *>(p)) << 16);
+}
+__device__ __forceinline__ void store_el(char *p, float v, float) { *reinterpret_cast<float *>(p) = v; }
+__device__ __forceinline__ void store_el(char *p, float v, uint16_t) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(0.0f), "f"(v));
+    *reinterpret_cast<uint16_t *>(p) = uint16_t(r & 0xFFFFu);
+}
+
+// Place of token t in its sequence; tokens behind the last sequence are at 0.
+__device__ int place_in_sequence(const int32_t *cu, uint32_t n_seqs, uint32_t t) {
+    uint32_t lo = 0, hi = n_seqs;   // the last b with cu[b] <= t, cu[0] taken as 0
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi + 1) / 2;
+        if (uint32_t(max(cu[mid], 0)) <= t) lo = mid;
+        else hi = mid - 1;
+    }
+    if (lo == n_seqs) return 0;
+    return int(t) - (lo ? max(cu[lo], 0) : 0);
+}
+
+template <typename T, bool HALF>
+__global__ void __launch_bounds__(kThreads)
+rotary_kernel(const __grid_constant__ RotaryDev a) {
+    __shared__ float2 wheel[kTokens][GAC_ROTARY_MAX_DIM / 2];
+    const uint32_t t0 = blockIdx.x * kTokens;
+    const uint32_t nt = min(uint32_t(kTokens), a.n_tokens - t0);
+    for (uint32_t w = threadIdx.x; w < nt * a.pairs; w += kThreads) {
+        const uint32_t t = w / a.pairs, i = w % a.pairs;
+        const int pos = a.positions ? a.positions[t0 + t] : place_in_sequence(a.cu, a.n_seqs, t0 + t);
+        const double turns = double(pos) * a.turns[i];
+        float s, c;
+        sincospif(2.0f * float(turns - rint(turns)), &s, &c);
+        wheel[t][i] = make_float2(c * a.scale, (a.inverse ? -s : s) * a.scale);
+    }
+    __syncthreads();
+    const uint32_t rest = a.head_dim - 2 * a.pairs, units = a.pairs + rest;
+    const uint32_t heads = a.heads[0] + a.heads[1];
+    for (uint32_t w = threadIdx.x; w < nt * heads * units; w += kThreads) {
+        const uint32_t u = w % units, h0 = (w / units) % heads, t = w / (units * heads);
+        const int which = h0 >= a.heads[0];
+        const uint32_t h = which ? h0 - a.heads[0] : h0;
+        const char *x = a.x[which] + ((long long)(t0 + t) * a.x_token[which] + (long long)h * a.x_head[which]) * (long long)sizeof(T);
+        char *y = a.y[which] + ((long long)(t0 + t) * a.y_token[which] + (long long)h * a.y_head[which]) * (long long)sizeof(T);
+        if (u < a.pairs) {
+            const uint32_t i = HALF ? u : 2 * u, j = HALF ? u + a.pairs : 2 * u + 1;
+            const float2 cs = wheel[t][u];
+            const float p = load_el(x + i * sizeof(T), T{}), q = load_el(x + j * sizeof(T), T{});
+            store_el(y + i * sizeof(T), p * cs.x - q * cs.y, T{});
+            store_el(y + j * sizeof(T), p * cs.y + q * cs.x, T{});
+        } else {
+            const uint32_t i = a.pairs + u;
+            if (x != y) store_el(y + i * sizeof(T), load_el(x + i * sizeof(T), T{}), T{});
+        }
+    }
+}
+
+int fail(std::nullptr_t, int code, const char *fmt, const char *a = "", long long b = 0) {
+    snprintf(g_init_err, sizeof(g_init_err), fmt, a, b);
+    return code;
+}
+
+// First byte and one past the last byte of a strided [tokens][heads][dim] block.
+void span(const void *p, int64_t token, int64_t head, uint64_t nt, uint64_t nh, uint64_t dim, uint64_t size, uint64_t *lo, uint64_t *hi) {
+    *lo = reinterpret_cast<uint64_t>(p);
+    *hi = *lo + (uint64_t(nt - 1) * uint64_t(token) + uint64_t(nh - 1) * uint64_t(head) + dim) * size;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gac_rotary_freqs(double *freqs, uint32_t rot_dim, double base, int scaling, double factor, double trained, double low,
+                     double high) {
+    if (!freqs) return fail(nullptr, GAC_ERR_INVALID_ARG, "freqs is NULL%s");
+    if (rot_dim < 2 || rot_dim % 2 || rot_dim > GAC_ROTARY_MAX_DIM)
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "rot_dim must be even, 2..%s%lld", "", GAC_ROTARY_MAX_DIM);
+    if (!(base > 1.0) || !isfinite(base)) return fail(nullptr, GAC_ERR_INVALID_ARG, "base must be finite and > 1%s");
+    if (!(factor >= 1.0) || !isfinite(factor)) return fail(nullptr, GAC_ERR_INVALID_ARG, "factor must be finite and >= 1%s");
+    if (scaling < GAC_ROTARY_NONE || scaling > GAC_ROTARY_PARTS) return fail(nullptr, GAC_ERR_INVALID_ARG, "unknown scaling%s");
+    if (scaling == GAC_ROTARY_NONE && factor != 1.0)
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "a factor needs a scaling%s");
+    if (scaling == GAC_ROTARY_BASE && rot_dim == 2)
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "scaling the base needs rot_dim > 2%s");
+    if (scaling == GAC_ROTARY_PARTS && (!(trained > 0.0) || !isfinite(trained) || !(low >= 0.0) || !(high > low) || !isfinite(high)))
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "scaling by parts needs trained > 0 and 0 <= low < high%s");
+    const double r = double(rot_dim);
+    if (scaling == GAC_ROTARY_BASE) base *= pow(factor, r / (r - 2.0));
+    for (uint32_t i = 0; i < rot_dim / 2; ++i) {
+        double f = pow(base, -2.0 * i / r);
+        if (scaling == GAC_ROTARY_LINEAR) f /= factor;
+        if (scaling == GAC_ROTARY_PARTS) {
+            const double turns = trained * f / (2.0 * M_PI);
+            const double keep = std::min(1.0, std::max(0.0, (turns - low) / (high - low)));
+            f *= keep + (1.0 - keep) / factor;
+        }
+        freqs[i] = f;
+    }
+    return GAC_OK;
+}
+
+int gac_rotary(const gac_rotary_args *args, int cuda_device, void *cuda_stream) {
+    if (!args) return fail(nullptr, GAC_ERR_INVALID_ARG, "args is NULL%s");
+    const gac_rotary_args &a = *args;
+    if (a.dtype != GAC_F32 && a.dtype != GAC_BF16) return fail(nullptr, GAC_ERR_DTYPE, "heads are float32 or bfloat16%s");
+    if (a.layout != GAC_ROTARY_HALF && a.layout != GAC_ROTARY_INTERLEAVED) return fail(nullptr, GAC_ERR_INVALID_ARG, "unknown layout%s");
+    if ((a.inverse != 0 && a.inverse != 1) || a.reserved != 0)
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "inverse must be 0 or 1, reserved 0%s");
+    if (a.rot_dim < 2 || a.rot_dim % 2 || a.rot_dim > a.head_dim || a.rot_dim > GAC_ROTARY_MAX_DIM)
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "rot_dim must be even, at least 2, at most head_dim and %s%lld", "", GAC_ROTARY_MAX_DIM);
+    if (a.head_dim > 1024 || a.heads[0] > 4096 || a.heads[1] > 4096 || a.n_tokens > (1u << 30) || a.n_seqs > (1u << 30))
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "head_dim, heads or n_tokens out of range%s");
+    if (!a.freqs) return fail(nullptr, GAC_ERR_INVALID_ARG, "freqs is NULL%s");
+    if (!isfinite(a.scale)) return fail(nullptr, GAC_ERR_INVALID_ARG, "scale must be finite%s");
+    const uint64_t size = a.dtype == GAC_BF16 ? 2 : 4;
+    RotaryDev d;
+    uint64_t lo[4], hi[4];
+    int spans = 0;
+    for (int w = 0; w < 2; ++w) {
+        const gac_rotary_heads &h = a.qk[w];
+        d.heads[w] = a.heads[w];
+        d.x[w] = static_cast<const char *>(h.x);
+        d.y[w] = static_cast<char *>(h.y);
+        d.x_token[w] = h.x_token;
+        d.x_head[w] = h.x_head;
+        d.y_token[w] = h.y_token;
+        d.y_head[w] = h.y_head;
+        if (a.heads[w] == 0 || a.n_tokens == 0) continue;
+        const uint64_t xb = reinterpret_cast<uint64_t>(h.x), yb = reinterpret_cast<uint64_t>(h.y);
+        if (!xb || !yb || xb % size || yb % size)
+            return fail(nullptr, GAC_ERR_INVALID_ARG, "heads have a NULL or misaligned pointer%s");
+        const int64_t most = int64_t(1) << 40;
+        if (h.x_token < 0 || h.x_head < 0 || h.x_token > most || h.x_head > most || h.y_token < 0 || h.y_head < 0 || h.y_token > most || h.y_head > most)
+            return fail(nullptr, GAC_ERR_INVALID_ARG, "strides must be 0..2^40 elements%s");
+        // every output element has a place of its own
+        const int64_t lesser = std::min(h.y_token, h.y_head), larger = std::max(h.y_token, h.y_head);
+        const bool token_less = h.y_token <= h.y_head;
+        const uint64_t n_lesser = token_less ? a.n_tokens : a.heads[w], n_larger = token_less ? a.heads[w] : a.n_tokens;
+        if ((n_lesser > 1 && lesser < int64_t(a.head_dim)) ||
+            (n_larger > 1 && uint64_t(larger) < (n_lesser - 1) * uint64_t(n_lesser > 1 ? lesser : 0) + a.head_dim))
+            return fail(nullptr, GAC_ERR_INVALID_ARG, "output heads overlap one another%s");
+        if (h.x == h.y) {
+            if (h.x_token != h.y_token || h.x_head != h.y_head)
+                return fail(nullptr, GAC_ERR_INVALID_ARG, "in place needs the same strides%s");
+        } else {
+            span(h.x, h.x_token, h.x_head, a.n_tokens, a.heads[w], a.head_dim, size, &lo[spans], &hi[spans]);
+            span(h.y, h.y_token, h.y_head, a.n_tokens, a.heads[w], a.head_dim, size, &lo[spans + 1], &hi[spans + 1]);
+            if (lo[spans] < hi[spans + 1] && lo[spans + 1] < hi[spans])
+                return fail(nullptr, GAC_ERR_INVALID_ARG, "input and output heads overlap without being in place%s");
+            spans += 2;
+        }
+    }
+    // out of place: what one of the two writes must not be what the other reads
+    if (spans == 4 && ((lo[1] < hi[2] && lo[2] < hi[1]) || (lo[3] < hi[0] && lo[0] < hi[3])))
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "output heads overlap the other input%s");
+    if (a.n_tokens == 0 || (a.heads[0] == 0 && a.heads[1] == 0)) return GAC_OK;
+    if (!a.positions && (!a.cu_seqlens || reinterpret_cast<uint64_t>(a.cu_seqlens) % 4))
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "positions or cu_seqlens must be given, 4-byte aligned%s");
+    if (reinterpret_cast<uint64_t>(a.positions) % 4) return fail(nullptr, GAC_ERR_INVALID_ARG, "positions must be 4-byte aligned%s");
+    d.n_tokens = a.n_tokens;
+    d.n_seqs = a.n_seqs;
+    d.head_dim = a.head_dim;
+    d.pairs = a.rot_dim / 2;
+    d.positions = a.positions;
+    d.cu = a.cu_seqlens;
+    d.scale = float(a.scale);
+    d.inverse = a.inverse;
+    for (uint32_t i = 0; i < d.pairs; ++i) {
+        if (!isfinite(a.freqs[i])) return fail(nullptr, GAC_ERR_INVALID_ARG, "frequency %s%lld is not finite", "", i);
+        d.turns[i] = a.freqs[i] / (2.0 * M_PI);
+    }
+    Range range("gac_rotary");
+    DeviceGuard guard(cuda_device);
+    if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const uint32_t grid = (a.n_tokens + kTokens - 1) / kTokens;
+    const bool half = a.layout == GAC_ROTARY_HALF;
+    auto *fn = a.dtype == GAC_BF16 ? (half ? rotary_kernel<uint16_t, true> : rotary_kernel<uint16_t, false>)
+                                   : (half ? rotary_kernel<float, true> : rotary_kernel<float, false>);
+    fn<<<grid, kThreads, 0, s>>>(d);
+    GAC_CUDA(nullptr, cudaGetLastError());
+    return GAC_OK;
+}
+
+}  // extern "C"

@@ -582,6 +582,14 @@ size_t gac_attn_workspace(const gac_attn *args);   /* 0 for arguments that the c
 int gac_attn_forward(const gac_attn *args, int cuda_device, void *cuda_stream);
 int gac_attn_backward(const gac_attn *args, const gac_attn_grad *grad, int cuda_device, void *cuda_stream);
 
+/*
+ * The attention kernels wait inside a CTA for their own copies and matrix products,
+ * each wait bounded.  If one ever ran out, the rows concerned were written as NaN and
+ * this call, which synchronises the stream, returns GAC_ERR_TIMEOUT once; otherwise
+ * GAC_OK.
+ */
+int gac_attn_check(int cuda_device, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -124,7 +124,7 @@ EXPORTS = ["gac_default_hparams", "gac_init", "gac_stats", "gac_stats_partial", 
            "gac_rebind", "gac_next_gradient_set", "gac_exchange_bytes", "gac_exchange_attach",
            "gac_stats_exchange", "gac_decide_exchange", "gac_clip_init", "gac_clip_sumsq", "gac_clip_apply",
            "gac_clip_grad_norm", "gac_clip_free", "gac_rotary_freqs", "gac_rotary", "gac_attn_workspace",
-           "gac_attn_forward", "gac_attn_backward"]
+           "gac_attn_forward", "gac_attn_backward", "gac_attn_check"]
 
 _lib = None
 
@@ -193,8 +193,9 @@ def load_library() -> ctypes.CDLL:
     L.gac_attn_workspace.restype = ctypes.c_size_t
     L.gac_attn_forward.argtypes = [P(gac_attn), i32, vp]
     L.gac_attn_backward.argtypes = [P(gac_attn), P(gac_attn_grad), i32, vp]
+    L.gac_attn_check.argtypes = [i32, vp]
     for name in ("gac_clip_init", "gac_clip_sumsq", "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_free",
-                 "gac_rotary_freqs", "gac_rotary", "gac_attn_forward", "gac_attn_backward"):
+                 "gac_rotary_freqs", "gac_rotary", "gac_attn_forward", "gac_attn_backward", "gac_attn_check"):
         getattr(L, name).restype = i32
     for name in ("gac_init", "gac_stats", "gac_stats_partial", "gac_decide", "gac_project",
                  "gac_free", "gac_set_launch", "gac_get_info"):
@@ -698,3 +699,9 @@ def gac_attn_backward(d_o: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
     g = gac_attn_grad(_attn_heads(d_o), _attn_heads(d_q), _attn_heads(d_k), _attn_heads(d_v), workspace.data_ptr(), need)
     _check(L.gac_attn_backward(ctypes.byref(a), ctypes.byref(g), q.device.index, stream.cuda_stream))
     return d_q, d_k, d_v
+
+
+def gac_attn_check(device: Optional[int] = None, stream=None) -> None:
+    """Synchronises the stream and raises GacError(GAC_ERR_TIMEOUT) if a wait inside an attention kernel ran out."""
+    dev = torch.device("cuda", torch.cuda.current_device() if device is None else device)
+    _check(load_library().gac_attn_check(dev.index, _on(stream, dev).cuda_stream))

@@ -9,6 +9,7 @@
 
 #include "gac.h"
 #include "gac_host.h"
+#include "attention_kernels.cuh"
 
 namespace {
 
@@ -18,7 +19,7 @@ struct HeadsDev {
     char *p;
     long long token, head;   // bytes
 };
-struct AttnDev {
+struct PlainDev {
     HeadsDev q, k, v, o, d_o, d_q, d_k, d_v;
     float *lse, *delta;
     const int32_t *cu;
@@ -27,7 +28,7 @@ struct AttnDev {
 };
 
 // Start and end of the sequence of token t; an empty range for a token that belongs to none.
-__device__ bool sequence_of(const AttnDev &a, uint32_t t, uint32_t *first, uint32_t *end) {
+__device__ bool sequence_of(const PlainDev &a, uint32_t t, uint32_t *first, uint32_t *end) {
     uint32_t lo = 0, hi = a.n_seqs;
     while (lo < hi) {
         const uint32_t mid = (lo + hi + 1) / 2;
@@ -71,38 +72,14 @@ __device__ void add4(float4 &a, float s, float4 b) {
     a.w += s * b.w;
 }
 
-__global__ void attn_forward_kernel(const __grid_constant__ AttnDev a) {
-    const uint32_t h = blockIdx.y, t = blockIdx.x * kWarps + threadIdx.x / 32;
-    if (t >= a.n_tokens) return;
-    const uint32_t kv = h / (a.q_heads / a.kv_heads);
-    uint32_t first, end;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float top = -INFINITY, sum = 0.f;
-    if (sequence_of(a, t, &first, &end)) {
-        const float4 q = row4(a.q, t, h, a.head_dim);
-        for (uint32_t j = first; j <= t; ++j) {
-            const float s = dot4(q, row4(a.k, j, kv, a.head_dim)) * a.scale;
-            const float m = fmaxf(top, s), f = expf(top - m), p = expf(s - m);
-            sum = sum * f + p;
-            acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
-            add4(acc, p, row4(a.v, j, kv, a.head_dim));
-            top = m;
-        }
-        const float inv = 1.f / sum;
-        acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
-    }
-    put4(a.o, t, h, a.head_dim, acc);
-    if ((threadIdx.x & 31) == 0) a.lse[size_t(h) * a.n_tokens + t] = sum > 0.f ? top + logf(sum) : -INFINITY;
-}
-
-__global__ void attn_delta_kernel(const __grid_constant__ AttnDev a) {
+__global__ void attn_delta_kernel(const __grid_constant__ PlainDev a) {
     const uint32_t h = blockIdx.y, t = blockIdx.x * kWarps + threadIdx.x / 32;
     if (t >= a.n_tokens) return;
     const float d = dot4(row4(a.o, t, h, a.head_dim), row4(a.d_o, t, h, a.head_dim));
     if ((threadIdx.x & 31) == 0) a.delta[size_t(h) * a.n_tokens + t] = d;
 }
 
-__global__ void attn_dq_kernel(const __grid_constant__ AttnDev a) {
+__global__ void attn_dq_kernel(const __grid_constant__ PlainDev a) {
     const uint32_t h = blockIdx.y, t = blockIdx.x * kWarps + threadIdx.x / 32;
     if (t >= a.n_tokens) return;
     const uint32_t kv = h / (a.q_heads / a.kv_heads);
@@ -120,7 +97,7 @@ __global__ void attn_dq_kernel(const __grid_constant__ AttnDev a) {
     put4(a.d_q, t, h, a.head_dim, acc);
 }
 
-__global__ void attn_dkv_kernel(const __grid_constant__ AttnDev a) {
+__global__ void attn_dkv_kernel(const __grid_constant__ PlainDev a) {
     const uint32_t kv = blockIdx.y, t = blockIdx.x * kWarps + threadIdx.x / 32;
     if (t >= a.n_tokens) return;
     const uint32_t group = a.q_heads / a.kv_heads;
@@ -156,6 +133,7 @@ int check_heads(const gac_attn_heads &h, const gac_attn &a, uint32_t heads, bool
     if (h.token < 0 || h.head < 0 || h.token > most || h.head > most || h.token % 8 || h.head % 8)
         return fail(nullptr, GAC_ERR_INVALID_ARG, "%s: strides must be multiples of 8 elements, 0..2^38", name);
     const uint64_t nt = a.n_tokens, nh = heads, dim = a.head_dim;
+    if (nt > 1 && h.token == 0) return fail(nullptr, GAC_ERR_INVALID_ARG, "%s: tokens must not share one row", name);
     if (output) {
         const bool token_less = h.token <= h.head;
         const uint64_t less = token_less ? h.token : h.head, more = token_less ? h.head : h.token;
@@ -188,8 +166,8 @@ int check_shape(const gac_attn *args) {
 
 HeadsDev dev(const gac_attn_heads &h) { return HeadsDev{static_cast<char *>(h.p), 2 * h.token, 2 * h.head}; }
 
-AttnDev dev_args(const gac_attn &a) {
-    AttnDev d{};
+PlainDev dev_args(const gac_attn &a) {
+    PlainDev d{};
     d.q = dev(a.q);
     d.k = dev(a.k);
     d.v = dev(a.v);
@@ -203,6 +181,90 @@ AttnDev dev_args(const gac_attn &a) {
     d.head_dim = a.head_dim;
     d.scale = a.scale;
     return d;
+}
+
+// ------------------------------------------------------------ launches
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+// Describes one [tokens][heads][dim] operand for loads of kTile rows x 64 elements of one head.  Heads that
+// share one memory (stride 0) are described as one head, and *mul makes the head coordinate 0.
+int tensor_map(CUtensorMap *map, int *mul, const gac_attn_heads &h, const gac_attn &a, uint32_t heads) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return fail(nullptr, GAC_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled%s");
+    const bool one = heads == 1 || h.head == 0;
+    *mul = one ? 0 : 1;
+    const uint64_t row = (uint64_t(a.head_dim) * 2 + 15) / 16 * 16;
+    const cuuint64_t dims[3] = {a.head_dim, one ? 1u : heads, a.n_tokens};
+    const cuuint64_t strides[2] = {one ? row : uint64_t(h.head) * 2, a.n_tokens == 1 ? row : uint64_t(h.token) * 2};
+    const cuuint32_t box[3] = {64, 1, kTile}, steps[3] = {1, 1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, h.p, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(nullptr, GAC_ERR_CUDA, "cuTensorMapEncodeTiled refused an operand (CUresult %s%lld)", "", (long long)r);
+    return GAC_OK;
+}
+
+RowsOut rows_out(const gac_attn_heads &h) { return RowsOut{static_cast<char *>(h.p), 2 * h.token, 2 * h.head}; }
+
+AttnDev kernel_args(const gac_attn &a) {
+    AttnDev d{};
+    d.cu = a.cu_seqlens;
+    d.n_tokens = a.n_tokens;
+    d.n_seqs = a.n_seqs;
+    d.q_heads = a.q_heads;
+    d.kv_heads = a.kv_heads;
+    d.head_dim = a.head_dim;
+    d.scale = a.scale;
+    d.exp2_scale = std::max(fabsf(a.scale) * kLog2e, 1e-37f);   // above zero, so that a hidden score stays -infinity
+    d.negate = a.scale < 0.0f ? kNegateA : 0u;
+    d.lse = a.lse;
+    d.o = rows_out(a.o);
+    return d;
+}
+
+// More dynamic shared memory than the default, asked for once per kernel and device.
+template <typename K>
+int allow_smem(K kernel, int bytes, int device, bool (&done)[64]) {
+    if (device < 64 && done[device]) return GAC_OK;
+    GAC_CUDA(nullptr, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    if (device < 64) done[device] = true;
+    return GAC_OK;
+}
+
+int grid_of(uint32_t slots, uint32_t heads, uint32_t *grid) {
+    const uint64_t n = uint64_t(slots) * heads;
+    if (n > 0x7FFFFFFFull) return fail(nullptr, GAC_ERR_INVALID_ARG, "too many tokens, sequences and heads for one call%s");
+    *grid = uint32_t(n);
+    return GAC_OK;
+}
+
+template <int DP>
+int launch_forward(const gac_attn &a, int device, cudaStream_t s) {
+    static bool done[64];
+    AttnDev d = kernel_args(a);
+    CUtensorMap mq, mk, mv;
+    if (int rc = tensor_map(&mq, &d.q_mul, a.q, a, a.q_heads)) return rc;
+    if (int rc = tensor_map(&mk, &d.k_mul, a.k, a, a.kv_heads)) return rc;
+    if (int rc = tensor_map(&mv, &d.v_mul, a.v, a, a.kv_heads)) return rc;
+    uint32_t grid;
+    if (int rc = grid_of(slot_count(a.n_tokens, a.n_seqs, 2 * kTile), a.q_heads, &grid)) return rc;
+    if (int rc = allow_smem(attn_forward_kernel<DP>, Fwd<DP>::kSmem, device, done)) return rc;
+    attn_forward_kernel<DP><<<grid, Fwd<DP>::kThreads, Fwd<DP>::kSmem, s>>>(mq, mk, mv, d);
+    GAC_CUDA(nullptr, cudaGetLastError());
+    return GAC_OK;
 }
 
 int check_pointers(const gac_attn &a, Span (&in)[3], Span *o) {
@@ -237,11 +299,22 @@ int gac_attn_forward(const gac_attn *args, int cuda_device, void *cuda_stream) {
     Range range("gac_attn_forward");
     DeviceGuard guard(cuda_device);
     if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
-    const AttnDev d = dev_args(a);
-    const dim3 grid((a.n_tokens + kWarps - 1) / kWarps, a.q_heads);
-    attn_forward_kernel<<<grid, kWarps * 32, 0, static_cast<cudaStream_t>(cuda_stream)>>>(d);
-    GAC_CUDA(nullptr, cudaGetLastError());
-    return GAC_OK;
+    return a.head_dim > 64 ? launch_forward<128>(a, cuda_device, static_cast<cudaStream_t>(cuda_stream))
+                           : launch_forward<64>(a, cuda_device, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int gac_attn_check(int cuda_device, void *cuda_stream) {
+    DeviceGuard guard(cuda_device);
+    if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    int fault = 0;
+    GAC_CUDA(nullptr, cudaMemcpyFromSymbolAsync(&fault, g_attn_fault, sizeof(fault), 0, cudaMemcpyDeviceToHost, s));
+    GAC_CUDA(nullptr, cudaStreamSynchronize(s));
+    if (!fault) return GAC_OK;
+    const int none = 0;
+    GAC_CUDA(nullptr, cudaMemcpyToSymbolAsync(g_attn_fault, &none, sizeof(none), 0, cudaMemcpyHostToDevice, s));
+    GAC_CUDA(nullptr, cudaStreamSynchronize(s));
+    return fail(nullptr, GAC_ERR_TIMEOUT, "a wait inside an attention kernel ran out%s");
 }
 
 int gac_attn_backward(const gac_attn *args, const gac_attn_grad *grad, int cuda_device, void *cuda_stream) {
@@ -269,7 +342,7 @@ int gac_attn_backward(const gac_attn *args, const gac_attn_grad *grad, int cuda_
     DeviceGuard guard(cuda_device);
     if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    AttnDev d = dev_args(a);
+    PlainDev d = dev_args(a);
     d.d_o = dev(g.d_o);
     d.d_q = dev(g.d_q);
     d.d_k = dev(g.d_k);

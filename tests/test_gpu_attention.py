@@ -36,6 +36,7 @@ def run(q, k, v, d_o, cu, scale=None, **kw):
 def check(q, k, v, d_o, cu, scale=None):
     got = run(q, k, v, d_o, cu, scale)
     want = attention(q, k, v, cu, q.shape[2] ** -0.5 if scale is None else scale, d_o)
+    gb.gac_attn_check()
     for name, (value, bound) in want.items():
         within(got[name], value, bound, name)
     return got

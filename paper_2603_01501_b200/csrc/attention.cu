@@ -13,110 +13,6 @@
 
 namespace {
 
-constexpr int kWarps = 4;
-
-struct HeadsDev {
-    char *p;
-    long long token, head;   // bytes
-};
-struct PlainDev {
-    HeadsDev q, k, v, o, d_o, d_q, d_k, d_v;
-    float *lse, *delta;
-    const int32_t *cu;
-    uint32_t n_tokens, n_seqs, q_heads, kv_heads, head_dim;
-    float scale;
-};
-
-// Start and end of the sequence of token t; an empty range for a token that belongs to none.
-__device__ bool sequence_of(const PlainDev &a, uint32_t t, uint32_t *first, uint32_t *end) {
-    uint32_t lo = 0, hi = a.n_seqs;
-    while (lo < hi) {
-        const uint32_t mid = (lo + hi + 1) / 2;
-        if (uint32_t(max(a.cu[mid], 0)) <= t) lo = mid;
-        else hi = mid - 1;
-    }
-    if (lo == a.n_seqs) return false;
-    *first = lo ? uint32_t(max(a.cu[lo], 0)) : 0u;
-    *end = min(uint32_t(max(a.cu[lo + 1], 0)), a.n_tokens);
-    return t < *end;
-}
-
-// Four elements of a row, elements lane*4 .. +3 (zero beyond head_dim).
-__device__ float4 row4(const HeadsDev &h, uint32_t t, uint32_t head, uint32_t dim) {
-    const uint32_t lane = threadIdx.x & 31;
-    if (lane * 4 >= dim) return make_float4(0.f, 0.f, 0.f, 0.f);
-    const uint2 w = *reinterpret_cast<const uint2 *>(h.p + (long long)t * h.token + (long long)head * h.head + lane * 8);
-    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
-                       __uint_as_float(w.y & 0xFFFF0000u));
-}
-__device__ uint32_t pack2(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-__device__ void put4(const HeadsDev &h, uint32_t t, uint32_t head, uint32_t dim, float4 v) {
-    const uint32_t lane = threadIdx.x & 31;
-    if (lane * 4 >= dim) return;
-    *reinterpret_cast<uint2 *>(h.p + (long long)t * h.token + (long long)head * h.head + lane * 8) =
-        make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
-}
-__device__ float dot4(float4 a, float4 b) {
-    float s = a.x * b.x + a.y * b.y + a.z * b.z + a.w * b.w;
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    return s;
-}
-__device__ void add4(float4 &a, float s, float4 b) {
-    a.x += s * b.x;
-    a.y += s * b.y;
-    a.z += s * b.z;
-    a.w += s * b.w;
-}
-
-__global__ void attn_delta_kernel(const __grid_constant__ PlainDev a) {
-    const uint32_t h = blockIdx.y, t = blockIdx.x * kWarps + threadIdx.x / 32;
-    if (t >= a.n_tokens) return;
-    const float d = dot4(row4(a.o, t, h, a.head_dim), row4(a.d_o, t, h, a.head_dim));
-    if ((threadIdx.x & 31) == 0) a.delta[size_t(h) * a.n_tokens + t] = d;
-}
-
-__global__ void attn_dq_kernel(const __grid_constant__ PlainDev a) {
-    const uint32_t h = blockIdx.y, t = blockIdx.x * kWarps + threadIdx.x / 32;
-    if (t >= a.n_tokens) return;
-    const uint32_t kv = h / (a.q_heads / a.kv_heads);
-    uint32_t first, end;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (sequence_of(a, t, &first, &end)) {
-        const float4 q = row4(a.q, t, h, a.head_dim), g = row4(a.d_o, t, h, a.head_dim);
-        const float lse = a.lse[size_t(h) * a.n_tokens + t], delta = a.delta[size_t(h) * a.n_tokens + t];
-        for (uint32_t j = first; j <= t; ++j) {
-            const float4 k = row4(a.k, j, kv, a.head_dim);
-            const float p = expf(dot4(q, k) * a.scale - lse);
-            add4(acc, p * (dot4(g, row4(a.v, j, kv, a.head_dim)) - delta) * a.scale, k);
-        }
-    }
-    put4(a.d_q, t, h, a.head_dim, acc);
-}
-
-__global__ void attn_dkv_kernel(const __grid_constant__ PlainDev a) {
-    const uint32_t kv = blockIdx.y, t = blockIdx.x * kWarps + threadIdx.x / 32;
-    if (t >= a.n_tokens) return;
-    const uint32_t group = a.q_heads / a.kv_heads;
-    uint32_t first, end;
-    float4 dk = make_float4(0.f, 0.f, 0.f, 0.f), dv = dk;
-    if (sequence_of(a, t, &first, &end)) {
-        const float4 k = row4(a.k, t, kv, a.head_dim), v = row4(a.v, t, kv, a.head_dim);
-        for (uint32_t h = kv * group; h < (kv + 1) * group; ++h)
-            for (uint32_t i = t; i < end; ++i) {
-                const float4 q = row4(a.q, i, h, a.head_dim), g = row4(a.d_o, i, h, a.head_dim);
-                const float p = expf(dot4(q, k) * a.scale - a.lse[size_t(h) * a.n_tokens + i]);
-                add4(dv, p, g);
-                add4(dk, p * (dot4(g, v) - a.delta[size_t(h) * a.n_tokens + i]) * a.scale, q);
-            }
-    }
-    put4(a.d_k, t, kv, a.head_dim, dk);
-    put4(a.d_v, t, kv, a.head_dim, dv);
-}
-
 int fail(std::nullptr_t, int code, const char *fmt, const char *a = "", long long b = 0) {
     snprintf(g_init_err, sizeof(g_init_err), fmt, a, b);
     return code;
@@ -160,27 +56,10 @@ int check_shape(const gac_attn *args) {
         return fail(nullptr, GAC_ERR_INVALID_ARG, "q_heads must be a multiple of kv_heads, 1..4096%s");
     if (a.n_tokens > (1u << 26) || a.n_seqs > (1u << 20))
         return fail(nullptr, GAC_ERR_INVALID_ARG, "n_tokens <= 2^26 and n_seqs <= 2^20 are supported%s");
+    if (uint64_t(a.n_tokens) * a.q_heads > (1ull << 31))
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "n_tokens * q_heads <= 2^31 is supported%s");
     if (!isfinite(a.scale)) return fail(nullptr, GAC_ERR_INVALID_ARG, "scale must be finite%s");
     return GAC_OK;
-}
-
-HeadsDev dev(const gac_attn_heads &h) { return HeadsDev{static_cast<char *>(h.p), 2 * h.token, 2 * h.head}; }
-
-PlainDev dev_args(const gac_attn &a) {
-    PlainDev d{};
-    d.q = dev(a.q);
-    d.k = dev(a.k);
-    d.v = dev(a.v);
-    d.o = dev(a.o);
-    d.lse = a.lse;
-    d.cu = a.cu_seqlens;
-    d.n_tokens = a.n_tokens;
-    d.n_seqs = a.n_seqs;
-    d.q_heads = a.q_heads;
-    d.kv_heads = a.kv_heads;
-    d.head_dim = a.head_dim;
-    d.scale = a.scale;
-    return d;
 }
 
 // ------------------------------------------------------------ launches
@@ -260,9 +139,57 @@ int launch_forward(const gac_attn &a, int device, cudaStream_t s) {
     if (int rc = tensor_map(&mk, &d.k_mul, a.k, a, a.kv_heads)) return rc;
     if (int rc = tensor_map(&mv, &d.v_mul, a.v, a, a.kv_heads)) return rc;
     uint32_t grid;
-    if (int rc = grid_of(slot_count(a.n_tokens, a.n_seqs, 2 * kTile), a.q_heads, &grid)) return rc;
+    if (int rc = grid_of(job_count(a.n_tokens, a.n_seqs, 2 * kTile), a.q_heads, &grid)) return rc;
     if (int rc = allow_smem(attn_forward_kernel<DP>, Fwd<DP>::kSmem, device, done)) return rc;
     attn_forward_kernel<DP><<<grid, Fwd<DP>::kThreads, Fwd<DP>::kSmem, s>>>(mq, mk, mv, d);
+    GAC_CUDA(nullptr, cudaGetLastError());
+    return GAC_OK;
+}
+
+// Query heads of a group are summed in one CTA as long as there are enough key tiles to go round; with fewer, parts
+// of the group go to CTAs of their own and a second kernel adds them.
+constexpr uint32_t kEnoughJobs = 370;
+uint32_t parts_of(const gac_attn &a) {
+    const uint32_t group = a.q_heads / a.kv_heads;
+    const uint64_t jobs = uint64_t(job_count(a.n_tokens, a.n_seqs, kTile)) * a.kv_heads;
+    for (uint32_t parts = 1; parts < group; ++parts)
+        if (group % parts == 0 && jobs * parts >= kEnoughJobs) return parts;
+    return group;
+}
+size_t rows_bytes(const gac_attn &a) { return (size_t(a.q_heads) * a.n_tokens * sizeof(float2) + 15) / 16 * 16; }
+
+template <int DP>
+int launch_backward(const gac_attn &a, const gac_attn_grad &g, int device, cudaStream_t s) {
+    static bool done_kv[64], done_q[64];
+    AttnDev d = kernel_args(a);
+    d.d_q = rows_out(g.d_q);
+    d.d_k = rows_out(g.d_k);
+    d.d_v = rows_out(g.d_v);
+    d.do_in = static_cast<const char *>(g.d_o.p);
+    d.do_token = 2 * g.d_o.token;
+    d.do_head = 2 * g.d_o.head;
+    d.rows = static_cast<float2 *>(g.workspace);
+    d.parts = parts_of(a);
+    d.part_sums = reinterpret_cast<float *>(static_cast<char *>(g.workspace) + rows_bytes(a));
+    CUtensorMap mq, mk, mv, mdo;
+    if (int rc = tensor_map(&mq, &d.q_mul, a.q, a, a.q_heads)) return rc;
+    if (int rc = tensor_map(&mk, &d.k_mul, a.k, a, a.kv_heads)) return rc;
+    if (int rc = tensor_map(&mv, &d.v_mul, a.v, a, a.kv_heads)) return rc;
+    if (int rc = tensor_map(&mdo, &d.do_mul, g.d_o, a, a.q_heads)) return rc;
+    const uint32_t jobs = job_count(a.n_tokens, a.n_seqs, kTile);
+    uint32_t grid_q, grid_kv;
+    if (int rc = grid_of(jobs, a.q_heads, &grid_q)) return rc;
+    if (int rc = grid_of(jobs, a.kv_heads * d.parts, &grid_kv)) return rc;
+    if (int rc = allow_smem(attn_dq_kernel<DP>, BwdQ<DP>::kSmem, device, done_q)) return rc;
+    if (int rc = allow_smem(attn_dkv_kernel<DP>, BwdKv<DP>::kSmem, device, done_kv)) return rc;
+    const uint64_t units = uint64_t(a.q_heads) * a.n_tokens, per = kRowThreads / 16;
+    attn_rows_kernel<<<uint32_t((units + per - 1) / per), kRowThreads, 0, s>>>(d);
+    attn_dkv_kernel<DP><<<grid_kv, BwdKv<DP>::kThreads, BwdKv<DP>::kSmem, s>>>(mq, mk, mv, mdo, d);
+    if (d.parts > 1) {
+        const uint64_t n = 2 * uint64_t(a.n_tokens) * a.kv_heads * (a.head_dim / 8);
+        attn_sum_parts_kernel<<<uint32_t((n + 255) / 256), 256, 0, s>>>(d);
+    }
+    attn_dq_kernel<DP><<<grid_q, BwdQ<DP>::kThreads, BwdQ<DP>::kSmem, s>>>(mq, mk, mv, mdo, d);
     GAC_CUDA(nullptr, cudaGetLastError());
     return GAC_OK;
 }
@@ -287,7 +214,10 @@ extern "C" {
 
 size_t gac_attn_workspace(const gac_attn *args) {
     if (check_shape(args)) return 0;
-    return std::max<size_t>(16, (size_t(args->q_heads) * args->n_tokens * 4 + 15) / 16 * 16);
+    const gac_attn &a = *args;
+    const uint32_t parts = parts_of(a);
+    const size_t sums = parts > 1 ? size_t(parts) * 2 * a.n_tokens * a.kv_heads * a.head_dim * sizeof(float) : 0;
+    return std::max<size_t>(16, rows_bytes(a) + sums);
 }
 
 int gac_attn_forward(const gac_attn *args, int cuda_device, void *cuda_stream) {
@@ -342,18 +272,7 @@ int gac_attn_backward(const gac_attn *args, const gac_attn_grad *grad, int cuda_
     DeviceGuard guard(cuda_device);
     if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    PlainDev d = dev_args(a);
-    d.d_o = dev(g.d_o);
-    d.d_q = dev(g.d_q);
-    d.d_k = dev(g.d_k);
-    d.d_v = dev(g.d_v);
-    d.delta = static_cast<float *>(g.workspace);
-    const uint32_t nx = (a.n_tokens + kWarps - 1) / kWarps;
-    attn_delta_kernel<<<dim3(nx, a.q_heads), kWarps * 32, 0, s>>>(d);
-    attn_dq_kernel<<<dim3(nx, a.q_heads), kWarps * 32, 0, s>>>(d);
-    attn_dkv_kernel<<<dim3(nx, a.kv_heads), kWarps * 32, 0, s>>>(d);
-    GAC_CUDA(nullptr, cudaGetLastError());
-    return GAC_OK;
+    return a.head_dim > 64 ? launch_backward<128>(a, g, cuda_device, s) : launch_backward<64>(a, g, cuda_device, s);
 }
 
 }  // extern "C"

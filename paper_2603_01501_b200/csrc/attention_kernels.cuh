@@ -26,9 +26,12 @@ struct AttnDev {
     float scale, exp2_scale;           // exp2_scale = |scale| log2(e); a negative scale negates q in the product
     uint32_t negate;
     RowsOut o, d_q, d_k, d_v;
-    const char *o_in, *do_in;          // backward: for the row terms
+    const char *do_in;                 // backward: for the row terms
     long long do_token, do_head;
-    float *lse, *delta;
+    float *lse;
+    float2 *rows;                      // backward: (-log2(e) lse, row term) of every query head and token
+    uint32_t parts;                    // backward: query heads of a group are summed in this many parts,
+    float *part_sums;                  // kept as binary32 [parts][d_k, d_v][n_tokens][kv_heads][head_dim] when parts > 1
 };
 
 // cu_seqlens entry b, kept in range; entry 0 is taken as 0.
@@ -38,35 +41,91 @@ __device__ __forceinline__ uint32_t seq_bound(const AttnDev &a, uint32_t b) {
     return c < 0 ? 0u : min(uint32_t(c), a.n_tokens);
 }
 
-// Which rows a CTA works on.  Every sequence gets the slots  start/ROWS + b ... : at least as many as it has
-// blocks of ROWS rows, found without a prefix sum over the pack (some slots stay empty).  The rows behind the
-// last sequence are slot range n_seqs.
-struct Slot {
-    uint32_t first, len;   // the sequence
-    uint32_t row;          // first row of the block within it
-    bool tail;
+// Which block of ROWS rows of which sequence a CTA works on.  Block indices are dealt out by height: a block of height u
+// sees u key tiles (or, for a key tile, is seen by u query tiles), and the highest come first, so that the last
+// CTAs to start are the short ones.  The job's height and sequence follow from cu_seqlens alone: the
+// number of blocks of height >= u is  F(u) = sum_b max(0, blocks_b - u + 1), found by bisection over u by a
+// warp whose lanes hold the sequences.  Beyond kRankedSeqs sequences that costs more than it gives, and every
+// sequence gets the indices  start/ROWS + b ...  instead: at least as many as it has blocks (some stay empty).
+// Rows behind the last sequence come last.
+constexpr uint32_t kRankedSeqs = 2048;
+struct Job {
+    uint32_t first, len;   // the sequence (or the rows behind the last one)
+    uint32_t block;        // which block of it
+    bool tail, none;
 };
-template <int ROWS>
-__device__ __forceinline__ Slot find_slot(const AttnDev &a, uint32_t slot) {   // whole warps
-    uint32_t lo = 0, hi = a.n_seqs;   // the last b in [lo, hi] with start(b) <= slot
-    while (hi - lo > 31) {
-        const uint32_t mid = (lo + hi + 1) / 2;
-        if (seq_bound(a, mid) / ROWS + mid <= slot) lo = mid;
-        else hi = mid - 1;
+template <int ROWS, bool HIGH_IS_LATE>
+__device__ __forceinline__ Job find_job(const AttnDev &a, uint32_t index, uint32_t count) {   // whole warps
+    const uint32_t all = 0xFFFFFFFFu, lane = threadIdx.x & 31, n = a.n_seqs;
+    Job job;
+    job.tail = job.none = false;
+    uint32_t b;
+    if (n <= kRankedSeqs) {
+        auto blocks_of = [&](uint32_t i) {
+            if (i >= n) return 0u;
+            const uint32_t from = seq_bound(a, i), to = seq_bound(a, i + 1);
+            return to > from ? (to - from + ROWS - 1) / ROWS : 0u;
+        };
+        const uint32_t mine = blocks_of(lane);   // the first 32 sequences stay in registers
+        uint32_t most = mine;
+        for (uint32_t i = lane + 32; i < n; i += 32) most = max(most, blocks_of(i));
+        most = __reduce_max_sync(all, most);
+        auto at_least = [&](uint32_t u) {
+            uint32_t f = mine >= u ? mine - u + 1 : 0u;
+            for (uint32_t i = lane + 32; i < n; i += 32) {
+                const uint32_t m = blocks_of(i);
+                f += m >= u ? m - u + 1 : 0u;
+            }
+            return __reduce_add_sync(all, f);
+        };
+        const uint32_t total = at_least(1);
+        if (index >= total) {
+            job.tail = true;
+            b = n;
+            job.block = index - total;
+        } else {
+            uint32_t lo = 1, hi = most;   // the largest u with F(u) > index
+            while (lo < hi) {
+                const uint32_t mid = (lo + hi + 1) / 2;
+                if (at_least(mid) > index) lo = mid;
+                else hi = mid - 1;
+            }
+            uint32_t k = index - at_least(lo + 1);   // among the sequences of lo blocks or more, the k-th
+            b = 0;
+            for (uint32_t i0 = 0; i0 < n; i0 += 32) {
+                const uint32_t m = i0 == 0 ? mine : blocks_of(i0 + lane);
+                const uint32_t here = __ballot_sync(all, m >= lo);
+                const uint32_t got = __popc(here);
+                if (k < got) {
+                    b = i0 + __fns(here, 0, int(k) + 1);
+                    break;
+                }
+                k -= got;
+            }
+            job.block = lo - 1;
+        }
+        job.first = seq_bound(a, b);
+    } else {
+        const uint32_t slot = HIGH_IS_LATE ? count - 1 - index : index;
+        uint32_t lo = 0, hi = n;   // the last b with start(b) <= slot
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi + 1) / 2;
+            if (seq_bound(a, mid) / ROWS + mid <= slot) lo = mid;
+            else hi = mid - 1;
+        }
+        b = lo;
+        job.tail = b == n;
+        job.first = seq_bound(a, b);
+        job.block = slot - (job.first / ROWS + b);
     }
-    const uint32_t b0 = lo + (threadIdx.x & 31);
-    const bool here = b0 <= hi && seq_bound(a, b0) / ROWS + b0 <= slot;
-    const uint32_t found = __ballot_sync(0xFFFFFFFFu, here);
-    const uint32_t b = lo + (found ? 31 - __clz(found) : 0);
-    Slot s;
-    s.first = seq_bound(a, b);
-    s.tail = (b == a.n_seqs);
-    const uint32_t end = s.tail ? a.n_tokens : max(s.first, seq_bound(a, b + 1));
-    s.len = end - s.first;
-    s.row = (slot - (s.first / ROWS + b)) * ROWS;
-    return s;
+    const uint32_t end = job.tail ? a.n_tokens : max(job.first, seq_bound(a, b + 1));
+    job.len = end - job.first;
+    const uint32_t blocks = (job.len + ROWS - 1) / ROWS;
+    job.none = job.block >= blocks;
+    if (!HIGH_IS_LATE && !job.tail && !job.none && n <= kRankedSeqs) job.block = blocks - 1 - job.block;
+    return job;
 }
-inline uint32_t slot_count(uint32_t n_tokens, uint32_t n_seqs, uint32_t rows) { return n_tokens / rows + n_seqs + 1; }
+inline uint32_t job_count(uint32_t n_tokens, uint32_t n_seqs, uint32_t rows) { return n_tokens / rows + n_seqs + 1; }
 
 // Writes one bit pattern over `dim` elements of rows [from, to) of one head, by the whole CTA: zero for rows that
 // belong to no sequence, NaN where a wait ran out.
@@ -77,6 +136,17 @@ __device__ __forceinline__ void fill_rows(const RowsOut &o, uint32_t from, uint3
         char *p = o.p + (long long)(from + i / per) * o.token + (long long)head * o.head + (i % per) * 16;
         *reinterpret_cast<uint4 *>(p) = make_uint4(bits, bits, bits, bits);
     }
+}
+
+// Zeroes rows [from, 128) of a tile in shared memory, by one warp, before the matrix unit reads it: rows behind the
+// sequence belong to others, and their zero weight does not cover a NaN.
+template <int SUB>
+__device__ __forceinline__ void zero_tile_rows(uint32_t tile, uint32_t from) {
+    for (int x = 0; x < SUB; ++x)
+        for (uint32_t i = from * 8 + (threadIdx.x & 31); i < kTile * 8; i += 32)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + x * (kTile * 128) + i * 16), "r"(0) : "memory");
+    fence_async_shared();
+    __syncwarp();
 }
 
 // ------------------------------------------------------------------- forward
@@ -109,10 +179,11 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     extern __shared__ char smem_raw[];
     const uint32_t head = blockIdx.x % a.q_heads, kv_head = head / (a.q_heads / a.kv_heads);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Slot s = find_slot<2 * kTile>(a, (gridDim.x - 1 - blockIdx.x) / a.q_heads);   // the longest rows first
-    if (s.row >= s.len) return;
+    const Job s = find_job<2 * kTile, true>(a, blockIdx.x / a.q_heads, gridDim.x / a.q_heads);
+    if (s.none) return;
+    const uint32_t row0 = s.block * 2 * kTile;   // of the sequence
     if (s.tail) {
-        const uint32_t from = s.first + s.row, to = min(s.first + s.len, from + 2 * kTile);
+        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + 2 * kTile);
         fill_rows(a.o, from, to, head, a.head_dim, kZeroBits);
         for (uint32_t t = from + threadIdx.x; t < to; t += blockDim.x) a.lse[size_t(head) * a.n_tokens + t] = -INFINITY;
         return;
@@ -122,8 +193,8 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     const uint32_t bars = sring + C::kStages * C::kBytes;
     const uint32_t q_full = bars, s_full = bars + 8, p_full = bars + 24, o_full = bars + 40, full = bars + 56,
                    empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
-    const bool two = s.row + kTile < s.len;
-    const uint32_t nb0 = s.row / kTile + 1, nb = nb0 + (two ? 1 : 0);   // key tiles of the first tile; of both
+    const bool two = row0 + kTile < s.len;
+    const uint32_t nb0 = row0 / kTile + 1, nb = nb0 + (two ? 1 : 0);   // key tiles of the first tile; of both
 
     if (warp == 8) tmem_alloc(tmem_slot, 512);
     if (threadIdx.x == 0) {
@@ -152,7 +223,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             for (int t = 0; t < (two ? 2 : 1); ++t)
                 for (int x = 0; x < C::kSub; ++x)
                     tma_load(sq + t * C::kBytes + x * (kTile * 128), &mq, q_full, x * 64, int(head) * a.q_mul,
-                             int(s.first + s.row + t * kTile));
+                             int(s.first + row0 + t * kTile));
             uint32_t n = 0;
             for (; n < 2 * nb; ++n) {
                 const uint32_t st = n % C::kStages, use = n / C::kStages;
@@ -204,14 +275,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             if (!(ok = wait_tile(2 * j + 1))) break;
             if (j + 1 < nb && !(ok = wait_tile(2 * j + 2))) break;
             if (j == nb - 1 && s.len < (j + 1) * kTile) {
-                // rows of V behind the sequence belong to others: their P is zero, but zero times a NaN is not
-                const uint32_t from = s.len - j * kTile;
-                const uint32_t v = sring + ((2 * j + 1) % C::kStages) * C::kBytes;
-                for (int x = 0; x < C::kSub; ++x)
-                    for (uint32_t i = from * 8 + lane; i < kTile * 8; i += 32)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v + x * (kTile * 128) + i * 16), "r"(0) : "memory");
-                fence_async_shared();
-                __syncwarp();
+                zero_tile_rows<C::kSub>(sring + ((2 * j + 1) % C::kStages) * C::kBytes, s.len - j * kTile);
             }
             if (j < nb0) {
                 if (!(ok = warp_wait(p_full, j & 1))) break;
@@ -297,7 +361,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
         if (ok) {
             tc_fence_after();
             const float total = sum.x + sum.y, inv = 1.0f / total;
-            const uint32_t row = s.row + t * kTile + local;
+            const uint32_t row = row0 + t * kTile + local;
             const bool mine = row < s.len;
             char *out = a.o.p + (long long)(s.first + row) * a.o.token + (long long)head * a.o.head;
             if (mine)
@@ -322,10 +386,583 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     tc_fence_after();
     if (warp == 8) tmem_free(tmem, 512);
     if (bad) {
-        const uint32_t from = s.first + s.row, to = min(s.first + s.len, from + 2 * kTile);
+        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + 2 * kTile);
         fill_rows(a.o, from, to, head, a.head_dim, kNanBits);
         for (uint32_t t = from + threadIdx.x; t < to; t += blockDim.x)
             a.lse[size_t(head) * a.n_tokens + t] = __int_as_float(0x7FFFFFFF);
+        if (threadIdx.x == 0) g_attn_fault = 1;
+    }
+}
+
+// ------------------------------------------------------------------- backward
+//
+// With P = exp2(c S - log2(e) lse) and the row term D_i = sum_d dO_id O_id:
+//     dV = P^T dO,   dP = dO V^T,   dS = P (dP - D),   dQ = scale dS K,   dK = scale dS^T Q
+// One kernel sums over the query tiles for a key tile (dK, dV), the other over the key tiles for a query tile
+// (dQ).  Both make S and dP again, seven products in all where five would do with dQ added up in memory by
+// atomics; in return every sum has one owner and one order, and two calls give the same bits.
+
+// The row terms, one half warp per row and head.
+constexpr int kRowThreads = 256;
+static __global__ void __launch_bounds__(kRowThreads) attn_rows_kernel(const __grid_constant__ AttnDev a) {
+    const uint32_t unit = blockIdx.x * (kRowThreads / 16) + threadIdx.x / 16, l = threadIdx.x & 15;
+    const uint32_t head = unit % a.q_heads, t = unit / a.q_heads;
+    float s = 0.f;
+    const bool in = t < a.n_tokens;
+    if (in && l * 8 < a.head_dim) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(a.o.p + (long long)t * a.o.token + (long long)head * a.o.head + l * 16);
+        const uint4 y = *reinterpret_cast<const uint4 *>(a.do_in + (long long)t * a.do_token + (long long)head * a.do_head + l * 16);
+        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s = fmaf(__uint_as_float(xs[i] << 16), __uint_as_float(ys[i] << 16), s);
+            s = fmaf(__uint_as_float(xs[i] & 0xFFFF0000u), __uint_as_float(ys[i] & 0xFFFF0000u), s);
+        }
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (in && l == 0) {
+        const size_t i = size_t(head) * a.n_tokens + t;
+        a.rows[i] = make_float2(-kLog2e * a.lse[i], s);
+    }
+}
+
+// d += a b^T over DP columns, both operands in shared memory, rows along the result.
+template <int DP>
+__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+        const uint32_t off = (i / 4) * (kTile * 128) + (i % 4) * 32;
+        mma_ss(d, smem_desc(a + off, 0), smem_desc(b + off, 0), idesc, i > 0);
+    }
+}
+// d += a b with a (bfloat16) in tensor memory, its 128 columns in two halves of 32 words that lie 64 words apart,
+// each where the half of the threads that made it had read its binary32 values from.
+__device__ __forceinline__ void product_cols(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+#pragma unroll
+    for (int i = 0; i < kTile / 16; ++i)
+        mma_ts(d, a + (i / 4) * 64 + (i % 4) * 8, smem_desc(b + i * 2048, kTile * 128), idesc, add || i > 0);
+}
+
+// One CTA: one key tile of a key head, over the query tiles from the diagonal to the end of the sequence, for the query
+// heads of the group (or of one part of it).  Rows of the accumulators are keys, so P^T and dS^T come out of
+// the products as they have to go into the next ones, from tensor memory; nothing is transposed.
+// Warps: 0-3 and 4-7 take the two halves of the query columns, 8 issues the products, 9 the TMA loads, 10 fetches the
+// row terms.  While the threads make dS of one query tile the tensor cores run dV and the next S; while they take
+// the next exponentials, dK and the next dP.
+template <int DP>
+struct BwdKv {
+    static constexpr int kSub = DP / 64;
+    static constexpr int kBytes = kTile * DP * 2;
+    static constexpr int kStages = DP == 128 ? 4 : 8;
+    static constexpr int kRowSlots = 4;
+    static constexpr int kThreads = 352;
+    static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + kRowSlots * 1024 + 256;
+};
+
+template <int DP>
+__global__ void __launch_bounds__(BwdKv<DP>::kThreads, 1)
+attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ AttnDev a) {
+    using C = BwdKv<DP>;
+    extern __shared__ char smem_raw[];
+    const uint32_t lots = a.kv_heads * a.parts, lot = blockIdx.x % lots;
+    const uint32_t kv_head = lot % a.kv_heads, part = lot / a.kv_heads;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Job s = find_job<kTile, false>(a, blockIdx.x / lots, gridDim.x / lots);
+    if (s.none) return;
+    const uint32_t row0 = s.block * kTile;
+    if (s.tail) {
+        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
+        if (part == 0) {
+            fill_rows(a.d_k, from, to, kv_head, a.head_dim, kZeroBits);
+            fill_rows(a.d_v, from, to, kv_head, a.head_dim, kZeroBits);
+        }
+        return;
+    }
+    const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    const uint32_t sk = base, sv = base + C::kBytes, sring = base + 2 * C::kBytes;
+    const uint32_t srows = sring + C::kStages * C::kBytes;   // per slot: 128 x -log2(e) lse, 128 x D
+    const uint32_t bars = srows + C::kRowSlots * 1024;
+    const uint32_t kv_full = bars, s_full = bars + 8, dp_full = bars + 16, p_full = bars + 24, ds_full = bars + 32, done = bars + 40,
+                   rows_full = bars + 48, rows_empty = rows_full + 8 * C::kRowSlots, full = rows_empty + 8 * C::kRowSlots,
+                   empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
+    const uint32_t q_tiles = (s.len + kTile - 1) / kTile - s.block;   // from the diagonal on
+    const uint32_t heads = a.q_heads / a.kv_heads / a.parts, head0 = kv_head * (a.q_heads / a.kv_heads) + part * heads;
+    const uint32_t total = q_tiles * heads;
+
+    if (warp == 8) tmem_alloc(tmem_slot, 512);
+    if (threadIdx.x == 0) {
+        mbar_init(kv_full, 1);
+        mbar_init(s_full, 1);
+        mbar_init(dp_full, 1);
+        mbar_init(p_full, 8);
+        mbar_init(ds_full, 8);
+        mbar_init(done, 1);
+        for (int i = 0; i < C::kRowSlots; ++i) {
+            mbar_init(rows_full + 8 * i, 1);
+            mbar_init(rows_empty + 8 * i, 8);
+        }
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        fence_barrier_init();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
+    const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 384;
+    bool ok = true;
+
+    if (warp == 9) {   // ------------------------------------------------ loads
+        if (lane == 0) {
+            mbar_expect(kv_full, 2 * C::kBytes);
+            for (int x = 0; x < C::kSub; ++x) {
+                tma_load(sk + x * (kTile * 128), &mk, kv_full, x * 64, int(kv_head) * a.k_mul, int(s.first + row0));
+                tma_load(sv + x * (kTile * 128), &mv, kv_full, x * 64, int(kv_head) * a.v_mul, int(s.first + row0));
+            }
+            uint32_t n = 0;
+            for (; n < 2 * total; ++n) {   // Q, dO, Q, dO, ...
+                const uint32_t st = n % C::kStages, use = n / C::kStages;
+                if (use > 0 && !(ok = mbar_wait(empty + 8 * st, (use - 1) & 1))) break;
+                const bool is_q = (n & 1) == 0;
+                const uint32_t h = head0 + (n / 2) / q_tiles, i = s.block + (n / 2) % q_tiles;
+                mbar_expect(full + 8 * st, C::kBytes);
+                for (int x = 0; x < C::kSub; ++x)
+                    tma_load(sring + st * C::kBytes + x * (kTile * 128), is_q ? &mq : &mdo, full + 8 * st, x * 64,
+                             int(h) * (is_q ? a.q_mul : a.do_mul), int(s.first + i * kTile));
+            }
+            if (!ok)
+                for (uint32_t i = n > C::kStages ? n - C::kStages : 0; i < n; ++i)
+                    mbar_wait(full + 8 * (i % C::kStages), (i / C::kStages) & 1);
+        }
+    } else if (warp == 10) {   // ------------------------------------ row terms
+        for (uint32_t n = 0; n < total; ++n) {
+            const uint32_t slot = n % C::kRowSlots, use = n / C::kRowSlots;
+            const uint32_t h = head0 + n / q_tiles, i = s.block + n % q_tiles;
+            const float2 *src = a.rows + size_t(h) * a.n_tokens + s.first + i * kTile;
+            float2 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                v[u] = i * kTile + lane + 32 * u < s.len ? __ldg(src + lane + 32 * u) : make_float2(0.f, 0.f);
+            if (use > 0 && !(ok = warp_wait(rows_empty + 8 * slot, (use - 1) & 1))) break;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t at = srows + slot * 1024 + (lane + 32 * u) * 4;
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v[u].x) : "memory");
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 512), "f"(v[u].y) : "memory");
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(rows_full + 8 * slot);
+        }
+    } else if (warp == 8) {   // ------------------------------------- products
+        const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
+        auto item = [&](uint32_t n) { return sring + (n % C::kStages) * C::kBytes; };
+        auto wait_item = [&](uint32_t n) { return warp_wait(full + 8 * (n % C::kStages), (n / C::kStages) & 1); };
+        auto release = [&](uint32_t n) {
+            if (lane == 0 && n + C::kStages < 2 * total) mma_commit(empty + 8 * (n % C::kStages));
+        };
+        auto fix = [&](uint32_t n) {   // item n belongs to query tile n / 2
+            const uint32_t i = s.block + (n / 2) % q_tiles;
+            if (s.len < (i + 1) * kTile) zero_tile_rows<C::kSub>(item(n), s.len - i * kTile);
+        };
+        auto scores = [&](uint32_t n) {
+            if (lane == 0) {
+                product_rows<DP>(t_s, sk, item(2 * n), id_s | a.negate);
+                mma_commit(s_full);
+            }
+        };
+        auto d_probs = [&](uint32_t n) {
+            if (lane == 0) {
+                product_rows<DP>(t_dp, sv, item(2 * n + 1), id_s);
+                mma_commit(dp_full);
+            }
+        };
+        ok = warp_wait(kv_full, 0) && wait_item(0);
+        if (ok) {
+            fix(0);
+            tc_fence_after();
+            scores(0);
+            ok = wait_item(1);
+        }
+        if (ok) {
+            fix(1);
+            d_probs(0);
+        }
+        for (uint32_t n = 0; ok && n < total; ++n) {
+            const bool more = n + 1 < total;
+            if (!(ok = warp_wait(p_full, n & 1))) break;
+            tc_fence_after();
+            if (lane == 0) product_cols(t_dv, t_s, item(2 * n + 1), id_o, n > 0);
+            release(2 * n + 1);
+            if (more) {
+                if (!(ok = wait_item(2 * n + 2))) break;
+                fix(2 * n + 2);
+                scores(n + 1);
+            }
+            if (!(ok = warp_wait(ds_full, n & 1))) break;
+            tc_fence_after();
+            if (lane == 0) product_cols(t_dk, t_dp, item(2 * n), id_o, n > 0);
+            release(2 * n);
+            if (more) {
+                if (!(ok = wait_item(2 * n + 3))) break;
+                fix(2 * n + 3);
+                d_probs(n + 1);
+            } else if (lane == 0) {
+                mma_commit(done);
+            }
+        }
+    } else {   // ---------------------- a key row, half of the query columns
+        const uint32_t half = warp >> 2, lanes = (warp & 3) << 21, col0 = half * 64;
+        const uint32_t local = (warp & 3) * 32 + lane;
+        const float2 c2 = make_float2(a.exp2_scale, a.exp2_scale);
+        for (uint32_t n = 0; n < total; ++n) {
+            const uint32_t slot = n % C::kRowSlots, i = s.block + n % q_tiles;
+            const uint32_t lo = i == s.block ? local : 0u, hi = min(uint32_t(kTile), s.len - i * kTile);
+            const bool whole = i != s.block && hi == kTile;   // every query of the tile sees every key of this one
+            const uint32_t terms = srows + slot * 1024 + col0 * 4;
+            if (!(ok = warp_wait(rows_full + 8 * slot, (n / C::kRowSlots) & 1))) break;
+            if (!(ok = warp_wait(s_full, n & 1))) break;
+            tc_fence_after();
+            float p[64];
+            {
+                uint32_t r[2][32];
+                tmem_ld32(r[0], t_s + lanes + col0);
+                tmem_ld32(r[1], t_s + lanes + col0 + 32);
+                tmem_wait_ld();
+#pragma unroll
+                for (int u = 0; u < 64; u += 4) {
+                    float4 l;
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l.x), "=f"(l.y), "=f"(l.z), "=f"(l.w) : "r"(terms + u * 4));
+                    const uint32_t *w = &r[u / 32][u % 32];
+                    const float2 x = fma2(make_float2(__uint_as_float(w[0]), __uint_as_float(w[1])), c2, make_float2(l.x, l.y));
+                    const float2 y = fma2(make_float2(__uint_as_float(w[2]), __uint_as_float(w[3])), c2, make_float2(l.z, l.w));
+                    p[u] = exp2_approx(x.x);
+                    p[u + 1] = exp2_approx(x.y);
+                    p[u + 2] = exp2_approx(y.x);
+                    p[u + 3] = exp2_approx(y.y);
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int u = 0; u < 64; ++u)
+                        if (col0 + u < lo || col0 + u >= hi) p[u] = 0.f;
+                }
+#pragma unroll
+                for (int u = 0; u < 32; ++u) r[0][u] = bf16x2(p[2 * u], p[2 * u + 1]);
+                tmem_st32(t_s + lanes + col0, r[0]);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full);
+            if (!(ok = warp_wait(dp_full, n & 1))) break;
+            tc_fence_after();
+            {
+                uint32_t r[2][32];
+                tmem_ld32(r[0], t_dp + lanes + col0);
+                tmem_ld32(r[1], t_dp + lanes + col0 + 32);
+                tmem_wait_ld();
+#pragma unroll
+                for (int u = 0; u < 64; u += 4) {
+                    float4 d;
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(d.x), "=f"(d.y), "=f"(d.z), "=f"(d.w) : "r"(terms + 512 + u * 4));
+                    const uint32_t *w = &r[u / 32][u % 32];
+                    p[u] *= __uint_as_float(w[0]) - d.x;
+                    p[u + 1] *= __uint_as_float(w[1]) - d.y;
+                    p[u + 2] *= __uint_as_float(w[2]) - d.z;
+                    p[u + 3] *= __uint_as_float(w[3]) - d.w;
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int u = 0; u < 64; ++u)
+                        if (col0 + u < lo || col0 + u >= hi) p[u] = 0.f;
+                }
+#pragma unroll
+                for (int u = 0; u < 32; ++u) r[0][u] = bf16x2(p[2 * u], p[2 * u + 1]);
+                tmem_st32(t_dp + lanes + col0, r[0]);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(ds_full);
+                mbar_arrive(rows_empty + 8 * slot);
+            }
+        }
+        if (ok) ok = warp_wait(done, 0);
+        if (ok) {   // the first half of the threads writes dV, the second dK
+            tc_fence_after();
+            const uint32_t row = row0 + local;
+            const bool mine = row < s.len;
+            const float f = half ? a.scale : 1.0f;
+            const RowsOut &o = half ? a.d_k : a.d_v;
+            char *out = o.p + (long long)(s.first + row) * o.token + (long long)kv_head * o.head;
+            float *sums = a.part_sums + (((size_t(part) * 2 + (1 - half)) * a.n_tokens + s.first + row) * a.kv_heads + kv_head) * a.head_dim;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) {
+                uint32_t w[32];
+                tmem_ld32(w, (half ? t_dk : t_dv) + lanes + 32 * i);
+                tmem_wait_ld();
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float *x = reinterpret_cast<const float *>(w + 8 * u);
+                    if (!mine || 32 * i + 8 * u >= int(a.head_dim)) continue;
+                    if (a.parts > 1) {
+                        float4 *to = reinterpret_cast<float4 *>(sums + 32 * i + 8 * u);
+                        to[0] = make_float4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+                        to[1] = make_float4(x[4] * f, x[5] * f, x[6] * f, x[7] * f);
+                    } else {
+                        *reinterpret_cast<uint4 *>(out + (32 * i + 8 * u) * 2) =
+                            make_uint4(bf16x2(x[0] * f, x[1] * f), bf16x2(x[2] * f, x[3] * f), bf16x2(x[4] * f, x[5] * f),
+                                       bf16x2(x[6] * f, x[7] * f));
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    const bool bad = __syncthreads_or(!ok);
+    tc_fence_after();
+    if (warp == 8) tmem_free(tmem, 512);
+    if (bad) {
+        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
+        fill_rows(a.d_k, from, to, kv_head, a.head_dim, kNanBits);
+        fill_rows(a.d_v, from, to, kv_head, a.head_dim, kNanBits);
+        if (a.parts > 1)
+            for (uint32_t which = 0; which < 2; ++which)
+                for (uint32_t i = threadIdx.x; i < (to - from) * a.head_dim; i += blockDim.x)
+                    a.part_sums[(((size_t(part) * 2 + which) * a.n_tokens + from + i / a.head_dim) * a.kv_heads + kv_head) * a.head_dim +
+                                i % a.head_dim] = __int_as_float(0x7FFFFFFF);
+        if (threadIdx.x == 0) g_attn_fault = 1;
+    }
+}
+
+// Adds the parts of dK and dV in order and rounds them once.
+static __global__ void __launch_bounds__(256) attn_sum_parts_kernel(const __grid_constant__ AttnDev a) {
+    const uint32_t per = a.head_dim / 8;
+    const size_t rows = size_t(a.n_tokens) * a.kv_heads, n = 2 * rows * per;
+    const size_t i = size_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= n) return;
+    const uint32_t which = i >= rows * per;   // 0: dK, 1: dV
+    const size_t j = i - which * rows * per, row = j / per;
+    const uint32_t t = uint32_t(row / a.kv_heads), h = uint32_t(row % a.kv_heads), x = uint32_t(j % per) * 8;
+    if (t >= seq_bound(a, a.n_seqs)) return;   // rows of no sequence were written as zero
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (uint32_t part = 0; part < a.parts; ++part) {
+        const float4 *src = reinterpret_cast<const float4 *>(a.part_sums + ((size_t(part) * 2 + which) * rows + row) * a.head_dim + x);
+        const float4 u = __ldcs(src), v = __ldcs(src + 1);
+        s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
+        s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+    }
+    const RowsOut &o = which ? a.d_v : a.d_k;
+    *reinterpret_cast<uint4 *>(o.p + (long long)t * o.token + (long long)h * o.head + x * 2) =
+        make_uint4(bf16x2(s[0], s[1]), bf16x2(s[2], s[3]), bf16x2(s[4], s[5]), bf16x2(s[6], s[7]));
+}
+
+// One CTA: one query tile of a head over the key tiles up to the diagonal.  S is double-buffered, so that the
+// products run ahead: dQ, the next dP and the S after that are issued while the threads work on one tile.
+// Warps: 0-3 and 4-7 take the two halves of the key columns, 8 issues the products, 9 the TMA loads.
+template <int DP>
+struct BwdQ {
+    static constexpr int kSub = DP / 64;
+    static constexpr int kBytes = kTile * DP * 2;
+    static constexpr int kStages = DP == 128 ? 5 : 8;
+    static constexpr int kThreads = 320;
+    static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + 256;
+};
+
+template <int DP>
+__global__ void __launch_bounds__(BwdQ<DP>::kThreads, 1)
+attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+               const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ AttnDev a) {
+    using C = BwdQ<DP>;
+    extern __shared__ char smem_raw[];
+    const uint32_t head = blockIdx.x % a.q_heads, kv_head = head / (a.q_heads / a.kv_heads);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Job s = find_job<kTile, true>(a, blockIdx.x / a.q_heads, gridDim.x / a.q_heads);
+    if (s.none) return;
+    const uint32_t row0 = s.block * kTile;
+    if (s.tail) {
+        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
+        fill_rows(a.d_q, from, to, head, a.head_dim, kZeroBits);
+        return;
+    }
+    const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    const uint32_t sq = base, sdo = base + C::kBytes, sring = base + 2 * C::kBytes;
+    const uint32_t bars = sring + C::kStages * C::kBytes;
+    const uint32_t q_full = bars, s_full = bars + 8, dp_full = bars + 24, ds_full = bars + 32, done = bars + 40, full = bars + 48,
+                   empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
+    const uint32_t total = s.block + 1;
+
+    if (warp == 8) tmem_alloc(tmem_slot, 512);
+    if (threadIdx.x == 0) {
+        mbar_init(q_full, 1);
+        mbar_init(s_full, 1);
+        mbar_init(s_full + 8, 1);
+        mbar_init(dp_full, 1);
+        mbar_init(ds_full, 8);
+        mbar_init(done, 1);
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        fence_barrier_init();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
+    const uint32_t t_dp = tmem + 256, t_dq = tmem + 384;
+    bool ok = true;
+
+    if (warp == 9) {   // ------------------------------------------------ loads
+        if (lane == 0) {
+            mbar_expect(q_full, 2 * C::kBytes);
+            for (int x = 0; x < C::kSub; ++x) {
+                tma_load(sq + x * (kTile * 128), &mq, q_full, x * 64, int(head) * a.q_mul, int(s.first + row0));
+                tma_load(sdo + x * (kTile * 128), &mdo, q_full, x * 64, int(head) * a.do_mul, int(s.first + row0));
+            }
+            uint32_t n = 0;
+            for (; n < 2 * total; ++n) {   // K, V, K, V, ...
+                const uint32_t st = n % C::kStages, use = n / C::kStages;
+                if (use > 0 && !(ok = mbar_wait(empty + 8 * st, (use - 1) & 1))) break;
+                const bool is_k = (n & 1) == 0;
+                mbar_expect(full + 8 * st, C::kBytes);
+                for (int x = 0; x < C::kSub; ++x)
+                    tma_load(sring + st * C::kBytes + x * (kTile * 128), is_k ? &mk : &mv, full + 8 * st, x * 64,
+                             int(kv_head) * (is_k ? a.k_mul : a.v_mul), int(s.first + (n / 2) * kTile));
+            }
+            if (!ok)
+                for (uint32_t i = n > C::kStages ? n - C::kStages : 0; i < n; ++i)
+                    mbar_wait(full + 8 * (i % C::kStages), (i / C::kStages) & 1);
+        }
+    } else if (warp == 8) {   // ------------------------------------- products
+        const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
+        auto item = [&](uint32_t n) { return sring + (n % C::kStages) * C::kBytes; };
+        auto wait_item = [&](uint32_t n) { return warp_wait(full + 8 * (n % C::kStages), (n / C::kStages) & 1); };
+        auto release = [&](uint32_t n) {
+            if (lane == 0 && n + C::kStages < 2 * total) mma_commit(empty + 8 * (n % C::kStages));
+        };
+        auto scores = [&](uint32_t n) {
+            if (s.len < (n + 1) * kTile) zero_tile_rows<C::kSub>(item(2 * n), s.len - n * kTile);   // dS there is zero
+            if (lane == 0) {
+                product_rows<DP>(tmem + (n & 1) * 128, sq, item(2 * n), id_s | a.negate);
+                mma_commit(s_full + 8 * (n & 1));
+            }
+        };
+        auto d_probs = [&](uint32_t n) {
+            if (lane == 0) {
+                product_rows<DP>(t_dp, sdo, item(2 * n + 1), id_s);
+                mma_commit(dp_full);
+            }
+            release(2 * n + 1);
+        };
+        ok = warp_wait(q_full, 0) && wait_item(0) && wait_item(1);
+        if (ok) {
+            tc_fence_after();
+            scores(0);
+            d_probs(0);
+            if (total > 1 && (ok = wait_item(2))) scores(1);
+        }
+        for (uint32_t n = 0; ok && n < total; ++n) {
+            if (!(ok = warp_wait(ds_full, n & 1))) break;
+            tc_fence_after();
+            if (lane == 0) product_cols(t_dq, t_dp, item(2 * n), id_o, n > 0);
+            release(2 * n);
+            if (n + 1 < total) {
+                if (!(ok = wait_item(2 * n + 3))) break;
+                d_probs(n + 1);
+            } else if (lane == 0) {
+                mma_commit(done);
+            }
+            if (n + 2 < total) {
+                if (!(ok = wait_item(2 * n + 4))) break;
+                scores(n + 2);
+            }
+        }
+    } else {   // ---------------------- a query row, half of the key columns
+        const uint32_t half = warp >> 2, lanes = (warp & 3) << 21, col0 = half * 64;
+        const uint32_t local = (warp & 3) * 32 + lane, row = row0 + local;
+        const bool mine = row < s.len;
+        const float2 term = mine ? __ldg(a.rows + size_t(head) * a.n_tokens + s.first + row) : make_float2(0.f, 0.f);
+        const float2 c2 = make_float2(a.exp2_scale, a.exp2_scale), l2 = make_float2(term.x, term.x), d2 = make_float2(-term.y, -term.y);
+        for (uint32_t n = 0; n < total; ++n) {
+            if (!(ok = warp_wait(s_full + 8 * (n & 1), (n >> 1) & 1))) break;
+            tc_fence_after();
+            float2 p[32];
+            {
+                uint32_t r[2][32];
+                tmem_ld32(r[0], tmem + (n & 1) * 128 + lanes + col0);
+                tmem_ld32(r[1], tmem + (n & 1) * 128 + lanes + col0 + 32);
+                tmem_wait_ld();
+#pragma unroll
+                for (int u = 0; u < 32; ++u) {
+                    const uint32_t *w = &r[u / 16][2 * (u % 16)];
+                    const float2 x = fma2(make_float2(__uint_as_float(w[0]), __uint_as_float(w[1])), c2, l2);
+                    p[u] = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+                }
+            }
+            if (!(ok = warp_wait(dp_full, n & 1))) break;
+            tc_fence_after();
+            {
+                uint32_t r[2][32];
+                tmem_ld32(r[0], t_dp + lanes + col0);
+                tmem_ld32(r[1], t_dp + lanes + col0 + 32);
+                tmem_wait_ld();
+#pragma unroll
+                for (int u = 0; u < 32; ++u) {
+                    const uint32_t *w = &r[u / 16][2 * (u % 16)];
+                    p[u] = mul2(p[u], add2(make_float2(__uint_as_float(w[0]), __uint_as_float(w[1])), d2));
+                }
+                if (n == total - 1) {   // the diagonal tile
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) {
+                        if (col0 + 2 * u > local) p[u].x = 0.f;
+                        if (col0 + 2 * u + 1 > local) p[u].y = 0.f;
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 32; ++u) r[0][u] = bf16x2(p[u].x, p[u].y);
+                tmem_st32(t_dp + lanes + col0, r[0]);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_full);
+        }
+        if (ok) ok = warp_wait(done, 0);
+        if (ok) {   // each half writes half of the row
+            tc_fence_after();
+            char *out = a.d_q.p + (long long)(s.first + row) * a.d_q.token + (long long)head * a.d_q.head;
+            const float f = a.scale;
+#pragma unroll
+            for (int i = 0; i < DP / 64; ++i) {
+                const uint32_t col = half * (DP / 2) + 32 * i;
+                uint32_t w[32];
+                tmem_ld32(w, t_dq + lanes + col);
+                tmem_wait_ld();
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float *x = reinterpret_cast<const float *>(w + 8 * u);
+                    if (mine && col + 8 * u < a.head_dim)
+                        *reinterpret_cast<uint4 *>(out + (col + 8 * u) * 2) =
+                            make_uint4(bf16x2(x[0] * f, x[1] * f), bf16x2(x[2] * f, x[3] * f), bf16x2(x[4] * f, x[5] * f),
+                                       bf16x2(x[6] * f, x[7] * f));
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    const bool bad = __syncthreads_or(!ok);
+    tc_fence_after();
+    if (warp == 8) tmem_free(tmem, 512);
+    if (bad) {
+        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
+        fill_rows(a.d_q, from, to, head, a.head_dim, kNanBits);
         if (threadIdx.x == 0) g_attn_fault = 1;
     }
 }

@@ -114,10 +114,14 @@ AttnDev kernel_args(const gac_attn &a) {
     return d;
 }
 
-// More dynamic shared memory than the default, asked for once per kernel and device.
+// Once per kernel and device: more dynamic shared memory than the default, and a look at the registers a CTA is
+// launched with, where its warpgroups count on them.
 template <typename K>
-int allow_smem(K kernel, int bytes, int device, bool (&done)[64]) {
+int allow_smem(K kernel, int bytes, int device, bool (&done)[64], int regs = 0) {
     if (device < 64 && done[device]) return GAC_OK;
+    cudaFuncAttributes attr;
+    GAC_CUDA(nullptr, cudaFuncGetAttributes(&attr, kernel));
+    if (attr.numRegs < regs) return fail(nullptr, GAC_ERR_CUDA, "a kernel was compiled to fewer registers than its warpgroups share out%s");
     GAC_CUDA(nullptr, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
     if (device < 64) done[device] = true;
     return GAC_OK;
@@ -140,7 +144,7 @@ int launch_forward(const gac_attn &a, int device, cudaStream_t s) {
     if (int rc = tensor_map(&mv, &d.v_mul, a.v, a, a.kv_heads)) return rc;
     uint32_t grid;
     if (int rc = grid_of(job_count(a.n_tokens, a.n_seqs, 2 * kTile), a.q_heads, &grid)) return rc;
-    if (int rc = allow_smem(attn_forward_kernel<DP>, Fwd<DP>::kSmem, device, done)) return rc;
+    if (int rc = allow_smem(attn_forward_kernel<DP>, Fwd<DP>::kSmem, device, done, Fwd<DP>::kRegs)) return rc;
     attn_forward_kernel<DP><<<grid, Fwd<DP>::kThreads, Fwd<DP>::kSmem, s>>>(mq, mk, mv, d);
     GAC_CUDA(nullptr, cudaGetLastError());
     return GAC_OK;

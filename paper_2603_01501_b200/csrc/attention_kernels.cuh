@@ -149,6 +149,25 @@ __device__ __forceinline__ void zero_tile_rows(uint32_t tile, uint32_t from) {
     __syncwarp();
 }
 
+// d = a b^T over DP columns, both operands in shared memory, rows along the result.
+template <int DP>
+__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+    const uint32_t da = smem_desc(a, 0), db = smem_desc(b, 0);
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+        const uint32_t off = ((i / 4) * (kTile * 128) + (i % 4) * 32) / 16;
+        mma_ss(d, da + off, db + off, idesc, i > 0);
+    }
+}
+// d (+)= a b with a (128 bfloat16 columns) in tensor memory, its second half HALF words behind the first, and b in
+// shared memory, rows along the summed dimension.
+template <int HALF>
+__device__ __forceinline__ void product_cols(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+    const uint32_t db = smem_desc(b, kTile * 128);
+#pragma unroll
+    for (int i = 0; i < kTile / 16; ++i) mma_ts(d, a + (i / 4) * HALF + (i % 4) * 8, db + i * (2048 / 16), idesc, add || i > 0);
+}
+
 // ------------------------------------------------------------------- forward
 //
 // One CTA: two query tiles of 128 rows (256 consecutive rows of one sequence and head) against the key and
@@ -160,14 +179,17 @@ __device__ __forceinline__ void zero_tile_rows(uint32_t tile, uint32_t from) {
 // exceeds it by more than 2^8 after scaling, so P stays below 256 and the rescaling, which has to wait for the products
 // in flight, is rare.  The two tiles alternate: while one tile's products run on the tensor cores the other tile's
 // exponentials are taken.
-// Warps: 0-3 and 4-7 the rows of the two tiles, 8 issues the products, 9 the TMA loads.
+// Warps: 0-3 and 4-7 the rows of the two tiles, 8 issues the products, 9 the TMA loads; 10 and 11 only make the
+// third warpgroup whole, which hands registers over to the first two (a row of 128 scores stays in registers).
 
 template <int DP>
 struct Fwd {
     static constexpr int kSub = DP / 64;                     // 64-wide blocks of a row
     static constexpr int kBytes = kTile * DP * 2;            // one tile
     static constexpr int kStages = DP == 128 ? 5 : 8;        // key and value tiles in flight
-    static constexpr int kThreads = 320;
+    static constexpr int kThreads = 384;
+    static constexpr int kRegs = 168, kRowRegs = 216, kOtherRegs = 72;   // at launch; then two warpgroups, one
+    static_assert(2 * kRowRegs + kOtherRegs <= 3 * kRegs, "shares of the launch's registers");
     static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + 256;
 };
 
@@ -217,6 +239,8 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
     bool ok = true;
 
+    if (warp >= 8) {
+    registers_down<C::kOtherRegs>();
     if (warp == 9) {   // ------------------------------------------------ loads
         if (lane == 0) {
             mbar_expect(q_full, (two ? 2 : 1) * C::kBytes);
@@ -241,22 +265,14 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     } else if (warp == 8) {   // ------------------------------------- products
         const uint32_t id_s = mma_desc(kTile, false) | a.negate, id_o = mma_desc(DP, true);
         auto scores = [&](int t, uint32_t j) {   // S_t = Q_t K_j^T
-            const uint32_t n = 2 * j, k = sring + (n % C::kStages) * C::kBytes, q = sq + t * C::kBytes;
             if (lane == 0) {
-#pragma unroll
-                for (int i = 0; i < DP / 16; ++i) {
-                    const uint32_t off = (i / 4) * (kTile * 128) + (i % 4) * 32;
-                    mma_ss(tmem + t * 128, smem_desc(q + off, 0), smem_desc(k + off, 0), id_s, i > 0);
-                }
+                product_rows<DP>(tmem + t * 128, sq + t * C::kBytes, sring + ((2 * j) % C::kStages) * C::kBytes, id_s);
                 mma_commit(s_full + 8 * t);
             }
         };
         auto values = [&](int t, uint32_t j) {   // O_t += P_t V_j
-            const uint32_t n = 2 * j + 1, v = sring + (n % C::kStages) * C::kBytes;
             if (lane == 0) {
-#pragma unroll
-                for (int i = 0; i < kTile / 16; ++i)
-                    mma_ts(tmem + 256 + t * 128, tmem + t * 128 + i * 8, smem_desc(v + i * 2048, kTile * 128), id_o, j > 0 || i > 0);
+                product_cols<32>(tmem + 256 + t * 128, tmem + t * 128, sring + ((2 * j + 1) % C::kStages) * C::kBytes, id_o, j > 0);
                 mma_commit(o_full + 8 * t);
             }
         };
@@ -297,7 +313,9 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 if (j + 1 < nb) release(2 * j + 2);
             }
         }
+    }
     } else if (warp < 4 || two) {   // -------------------------- a row of a tile
+        registers_up<C::kRowRegs>();
         const int t = warp >> 2;
         const uint32_t my_blocks = nb0 + t, lanes = (warp & 3) << 21;   // tensor memory lane 32 (warp & 3)
         const uint32_t ts = tmem + t * 128 + lanes, to = tmem + 256 + t * 128 + lanes;
@@ -425,23 +443,6 @@ static __global__ void __launch_bounds__(kRowThreads) attn_rows_kernel(const __g
         const size_t i = size_t(head) * a.n_tokens + t;
         a.rows[i] = make_float2(-kLog2e * a.lse[i], s);
     }
-}
-
-// d += a b^T over DP columns, both operands in shared memory, rows along the result.
-template <int DP>
-__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i) {
-        const uint32_t off = (i / 4) * (kTile * 128) + (i % 4) * 32;
-        mma_ss(d, smem_desc(a + off, 0), smem_desc(b + off, 0), idesc, i > 0);
-    }
-}
-// d += a b with a (bfloat16) in tensor memory, its 128 columns in two halves of 32 words that lie 64 words apart,
-// each where the half of the threads that made it had read its binary32 values from.
-__device__ __forceinline__ void product_cols(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
-#pragma unroll
-    for (int i = 0; i < kTile / 16; ++i)
-        mma_ts(d, a + (i / 4) * 64 + (i % 4) * 8, smem_desc(b + i * 2048, kTile * 128), idesc, add || i > 0);
 }
 
 // One CTA: one key tile of a key head, over the query tiles from the diagonal to the end of the sequence, for the query
@@ -596,7 +597,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             const bool more = n + 1 < total;
             if (!(ok = warp_wait(p_full, n & 1))) break;
             tc_fence_after();
-            if (lane == 0) product_cols(t_dv, t_s, item(2 * n + 1), id_o, n > 0);
+            if (lane == 0) product_cols<64>(t_dv, t_s, item(2 * n + 1), id_o, n > 0);
             release(2 * n + 1);
             if (more) {
                 if (!(ok = wait_item(2 * n + 2))) break;
@@ -605,7 +606,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             }
             if (!(ok = warp_wait(ds_full, n & 1))) break;
             tc_fence_after();
-            if (lane == 0) product_cols(t_dk, t_dp, item(2 * n), id_o, n > 0);
+            if (lane == 0) product_cols<64>(t_dk, t_dp, item(2 * n), id_o, n > 0);
             release(2 * n);
             if (more) {
                 if (!(ok = wait_item(2 * n + 3))) break;
@@ -871,7 +872,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         for (uint32_t n = 0; ok && n < total; ++n) {
             if (!(ok = warp_wait(ds_full, n & 1))) break;
             tc_fence_after();
-            if (lane == 0) product_cols(t_dq, t_dp, item(2 * n), id_o, n > 0);
+            if (lane == 0) product_cols<64>(t_dq, t_dp, item(2 * n), id_o, n > 0);
             release(2 * n);
             if (n + 1 < total) {
                 if (!(ok = wait_item(2 * n + 3))) break;

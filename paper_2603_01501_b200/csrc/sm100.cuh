@@ -29,7 +29,7 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 }
 // Every wait in these kernels is for the CTA's own copies and matrix products, which end by themselves;
 // the limit (two seconds and a number of polls) only keeps a mistake from holding the GPU.
-static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
     unsigned long long t0, t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
     for (uint32_t i = 0; i < (1u << 26); ++i) {
@@ -108,28 +108,38 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]
 // Shared-memory operand, 128-byte swizzle, rows of 64 bfloat16 (128 bytes), 8-row groups 1024 bytes apart.
 // K-major: rows are the operand's rows and 64 wide along the summed dimension (next_block unused).
 // MN-major: rows run along the summed dimension, next_block bytes to the next 64 output columns.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t next_block) {
-    return uint64_t((addr & 0x3FFFFu) >> 4) | (uint64_t((next_block & 0x3FFFFu) >> 4) << 16) | (uint64_t(1024u >> 4) << 32) |
-           (uint64_t(1) << 46) | (uint64_t(2) << 61);
-}
+// Only the lower word depends on the address; kDescHigh is the rest.  Adding bytes / 16 to it moves the operand.
+__device__ __forceinline__ uint32_t smem_desc(uint32_t addr, uint32_t next_block) { return (addr >> 4) | ((next_block >> 4) << 16); }
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
 // bfloat16 x bfloat16 -> binary32, M = 128.
 __host__ __device__ constexpr uint32_t mma_desc(uint32_t n, bool b_mn_major) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn_major ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
 constexpr uint32_t kNegateA = 1u << 13;
 
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add)) : "memory");
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 a, {%1, %5};\nmov.b64 b, {%2, %5};\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(uint32_t(add)), "n"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(uint32_t(add)) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n.reg .pred p;\n.reg .b64 b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 b, {%2, %5};\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(uint32_t(add)), "n"(kDescHigh) : "memory");
 }
 // The barrier gets one arrival when all matrix products issued so far by this thread are done.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+
+// ------------------------------------------------------------------ registers
+
+// A warpgroup's share of the registers the CTA was launched with.  The shares of a kernel's warpgroups add up to at
+// most threads x registers at launch, which the host checks before the launch: a share that is not there is waited for.
+template <int N>
+__device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // ------------------------------------------------------------------- numbers
 

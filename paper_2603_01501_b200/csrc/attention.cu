@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstddef>
 
 #include "gac.h"
@@ -117,7 +118,7 @@ AttnDev kernel_args(const gac_attn &a) {
 // Once per kernel and device: more dynamic shared memory than the default, and a look at the registers a CTA is
 // launched with, where its warpgroups count on them.
 template <typename K>
-int allow_smem(K kernel, int bytes, int device, bool (&done)[64], int regs = 0) {
+int allow_smem(K kernel, int bytes, int device, std::atomic<bool> (&done)[64], int regs = 0) {
     if (device < 64 && done[device]) return GAC_OK;
     cudaFuncAttributes attr;
     GAC_CUDA(nullptr, cudaFuncGetAttributes(&attr, kernel));
@@ -127,8 +128,8 @@ int allow_smem(K kernel, int bytes, int device, bool (&done)[64], int regs = 0) 
     return GAC_OK;
 }
 
-int grid_of(uint32_t slots, uint32_t heads, uint32_t *grid) {
-    const uint64_t n = uint64_t(slots) * heads;
+int grid_of(uint32_t count, uint32_t heads, uint32_t *grid) {
+    const uint64_t n = uint64_t(count) * heads;
     if (n > 0x7FFFFFFFull) return fail(nullptr, GAC_ERR_INVALID_ARG, "too many tokens, sequences and heads for one call%s");
     *grid = uint32_t(n);
     return GAC_OK;
@@ -136,7 +137,7 @@ int grid_of(uint32_t slots, uint32_t heads, uint32_t *grid) {
 
 template <int DP>
 int launch_forward(const gac_attn &a, int device, cudaStream_t s) {
-    static bool done[64];
+    static std::atomic<bool> done[64];
     AttnDev d = kernel_args(a);
     CUtensorMap mq, mk, mv;
     if (int rc = tensor_map(&mq, &d.q_mul, a.q, a, a.q_heads)) return rc;
@@ -164,7 +165,7 @@ size_t rows_bytes(const gac_attn &a) { return (size_t(a.q_heads) * a.n_tokens * 
 
 template <int DP>
 int launch_backward(const gac_attn &a, const gac_attn_grad &g, int device, cudaStream_t s) {
-    static bool done_kv[64], done_q[64];
+    static std::atomic<bool> done_kv[64], done_q[64];
     AttnDev d = kernel_args(a);
     d.d_q = rows_out(g.d_q);
     d.d_k = rows_out(g.d_k);

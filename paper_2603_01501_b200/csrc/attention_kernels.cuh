@@ -127,14 +127,96 @@ __device__ __forceinline__ Job find_job(const AttnDev &a, uint32_t index, uint32
 }
 inline uint32_t job_count(uint32_t n_tokens, uint32_t n_seqs, uint32_t rows) { return n_tokens / rows + n_seqs + 1; }
 
-// Writes one bit pattern over `dim` elements of rows [from, to) of one head, by the whole CTA: zero for rows that
+// The grid has one CTA per possible job (highest first, heads fastest), but a CTA that has started takes over jobs whose
+// CTA has not (cluster launch control), so that the loads and first products of one job run while the rows of the last
+// are written, and no barrier, tensor memory or pipeline is set up twice.  One warp asks for the next job as soon as
+// the current one has begun, and tells the others.
+enum JobKind : uint32_t { kJobNone = 0, kJobWork = 1, kJobTail = 2, kJobStop = 3 };
+struct JobWord {
+    uint32_t first, len, block, kind, head;
+};
+template <int ROWS, bool HIGH_IS_LATE>
+__device__ __forceinline__ JobWord job_at(const AttnDev &a, uint32_t index, uint32_t heads) {   // whole warps
+    const Job j = find_job<ROWS, HIGH_IS_LATE>(a, index / heads, gridDim.x / heads);
+    JobWord w;
+    w.first = j.first;
+    w.len = j.len;
+    w.block = j.block;
+    w.head = index % heads;
+    w.kind = j.none ? kJobNone : j.tail ? kJobTail : kJobWork;
+    return w;
+}
+struct Jobs {
+    uint32_t word, answer, full, empty, asked;   // shared memory addresses; `readers` warps read every job
+    __device__ __forceinline__ explicit Jobs(uint32_t at) : word(at), answer(at + 16), full(at + 32), empty(at + 40), asked(at + 48) {}
+    static constexpr uint32_t kBytes = 64;
+    __device__ __forceinline__ void init(uint32_t readers) const {
+        mbar_init(full, 1);
+        mbar_init(empty, readers);
+        mbar_init(asked, 1);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(word), "r"(0) : "memory");
+    }
+    // The warp that hands the jobs out: from this CTA's own index on, until there is none left.
+    template <int ROWS, bool HIGH_IS_LATE>
+    __device__ __forceinline__ bool run(const AttnDev &a, uint32_t heads) const {
+        const uint32_t lane = threadIdx.x & 31;
+        int index = int(blockIdx.x);
+        uint32_t given = 0, questions = 0;
+        while (true) {
+            JobWord w;
+            w.first = w.len = w.block = w.head = 0;
+            w.kind = kJobStop;
+            if (index >= 0) w = job_at<ROWS, HIGH_IS_LATE>(a, uint32_t(index), heads);
+            if (w.kind != kJobNone) {
+                if (lane == 0) {
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(word), "r"(w.first), "r"(w.len), "r"(w.block), "r"(w.kind | (w.head << 2)) : "memory");
+                    mbar_arrive(full);
+                }
+                if (w.kind == kJobStop) return true;
+                if (!warp_wait(empty, given & 1)) return false;   // all have begun it
+                ++given;
+            }
+            if (lane == 0) {
+                mbar_expect(asked, 16);
+                ask_next_cta(answer, asked);
+            }
+            if (!warp_wait(asked, questions & 1)) return false;
+            ++questions;
+            index = next_cta(answer);
+            __syncwarp();
+            fence_async_shared();   // the answer has been read before the next one overwrites it
+        }
+    }
+    __device__ __forceinline__ bool get(uint32_t k, JobWord *w) const {         // whole warp
+        if (!warp_wait(full, k & 1)) return false;
+        uint32_t last;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w->first), "=r"(w->len), "=r"(w->block), "=r"(last) : "r"(word) : "memory");
+        w->kind = last & 3u;
+        w->head = last >> 2;
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(empty);
+        return true;
+    }
+};
+
+// Writes one bit pattern over `dim` elements of rows [from, to) of one head, by the first `threads` threads of the CTA: zero for rows that
 // belong to no sequence, NaN where a wait ran out.
 constexpr uint32_t kZeroBits = 0u, kNanBits = 0x7FFF7FFFu;
-__device__ __forceinline__ void fill_rows(const RowsOut &o, uint32_t from, uint32_t to, uint32_t head, uint32_t dim, uint32_t bits) {
+__device__ __forceinline__ void fill_rows(const RowsOut &o, uint32_t from, uint32_t to, uint32_t head, uint32_t dim, uint32_t bits,
+                                          uint32_t threads) {
     const uint32_t per = dim / 8, n = (to - from) * per;
-    for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
+    for (uint32_t i = threadIdx.x; i < n; i += threads) {
         char *p = o.p + (long long)(from + i / per) * o.token + (long long)head * o.head + (i % per) * 16;
         *reinterpret_cast<uint4 *>(p) = make_uint4(bits, bits, bits, bits);
+    }
+}
+
+// Writes NaN over the rows, by one warp: what a wait that ran out leaves of a job.
+__device__ __forceinline__ void poison_rows(const RowsOut &o, uint32_t from, uint32_t to, uint32_t head, uint32_t dim) {
+    const uint32_t per = dim / 8, n = (to - from) * per;
+    for (uint32_t i = threadIdx.x & 31; i < n; i += 32) {
+        char *p = o.p + (long long)(from + i / per) * o.token + (long long)head * o.head + (i % per) * 16;
+        *reinterpret_cast<uint4 *>(p) = make_uint4(0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu);
     }
 }
 
@@ -179,8 +261,8 @@ __device__ __forceinline__ void product_cols(uint32_t d, uint32_t a, uint32_t b,
 // exceeds it by more than 2^8 after scaling, so P stays below 256 and the rescaling, which has to wait for the products
 // in flight, is rare.  The two tiles alternate: while one tile's products run on the tensor cores the other tile's
 // exponentials are taken.
-// Warps: 0-3 and 4-7 the rows of the two tiles, 8 issues the products, 9 the TMA loads; 10 and 11 only make the
-// third warpgroup whole, which hands registers over to the first two (a row of 128 scores stays in registers).
+// Warps: 0-3 and 4-7 the rows of the two tiles, 8 issues the products, 9 the TMA loads, 10 finds the jobs; 11 only makes
+// the third warpgroup whole, which hands registers over to the first two (a row of 128 scores stays in registers).
 
 template <int DP>
 struct Fwd {
@@ -188,9 +270,9 @@ struct Fwd {
     static constexpr int kBytes = kTile * DP * 2;            // one tile
     static constexpr int kStages = DP == 128 ? 5 : 8;        // key and value tiles in flight
     static constexpr int kThreads = 384;
-    static constexpr int kRegs = 168, kRowRegs = 216, kOtherRegs = 72;   // at launch; then two warpgroups, one
+    static constexpr int kRegs = 168, kRowRegs = 208, kOtherRegs = 88;   // at launch; then two warpgroups, one
     static_assert(2 * kRowRegs + kOtherRegs <= 3 * kRegs, "shares of the launch's registers");
-    static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + 256;
+    static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + 512;
 };
 
 template <int DP>
@@ -199,28 +281,19 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                     const __grid_constant__ CUtensorMap mv, const __grid_constant__ AttnDev a) {
     using C = Fwd<DP>;
     extern __shared__ char smem_raw[];
-    const uint32_t head = blockIdx.x % a.q_heads, kv_head = head / (a.q_heads / a.kv_heads);
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Job s = find_job<2 * kTile, true>(a, blockIdx.x / a.q_heads, gridDim.x / a.q_heads);
-    if (s.none) return;
-    const uint32_t row0 = s.block * 2 * kTile;   // of the sequence
-    if (s.tail) {
-        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + 2 * kTile);
-        fill_rows(a.o, from, to, head, a.head_dim, kZeroBits);
-        for (uint32_t t = from + threadIdx.x; t < to; t += blockDim.x) a.lse[size_t(head) * a.n_tokens + t] = -INFINITY;
-        return;
-    }
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = a.q_heads / a.kv_heads;
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t sq = base, sring = base + 2 * C::kBytes;
     const uint32_t bars = sring + C::kStages * C::kBytes;
-    const uint32_t q_full = bars, s_full = bars + 8, p_full = bars + 24, o_full = bars + 40, full = bars + 56,
-                   empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
-    const bool two = row0 + kTile < s.len;
-    const uint32_t nb0 = row0 / kTile + 1, nb = nb0 + (two ? 1 : 0);   // key tiles of the first tile; of both
+    const Jobs jobs(bars);
+    const uint32_t q_full = bars + Jobs::kBytes, q_empty = q_full + 8, s_full = q_full + 16, p_full = q_full + 32, o_full = q_full + 48,
+                   full = q_full + 64, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
 
     if (warp == 8) tmem_alloc(tmem_slot, 512);
     if (threadIdx.x == 0) {
+        jobs.init(10);
         mbar_init(q_full, 1);
+        mbar_init(q_empty, 1);
         for (int t = 0; t < 2; ++t) {
             mbar_init(s_full + 8 * t, 1);
             mbar_init(p_full + 8 * t, 4);
@@ -238,165 +311,201 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
     bool ok = true;
+    JobWord w;
+    w.kind = kJobNone;
 
     if (warp >= 8) {
-    registers_down<C::kOtherRegs>();
-    if (warp == 9) {   // ------------------------------------------------ loads
-        if (lane == 0) {
-            mbar_expect(q_full, (two ? 2 : 1) * C::kBytes);
-            for (int t = 0; t < (two ? 2 : 1); ++t)
-                for (int x = 0; x < C::kSub; ++x)
-                    tma_load(sq + t * C::kBytes + x * (kTile * 128), &mq, q_full, x * 64, int(head) * a.q_mul,
-                             int(s.first + row0 + t * kTile));
-            uint32_t n = 0;
-            for (; n < 2 * nb; ++n) {
-                const uint32_t st = n % C::kStages, use = n / C::kStages;
-                if (use > 0 && !(ok = mbar_wait(empty + 8 * st, (use - 1) & 1))) break;
-                const bool is_k = (n & 1) == 0;
-                mbar_expect(full + 8 * st, C::kBytes);
-                for (int x = 0; x < C::kSub; ++x)
-                    tma_load(sring + st * C::kBytes + x * (kTile * 128), is_k ? &mk : &mv, full + 8 * st, x * 64,
-                             int(kv_head) * (is_k ? a.k_mul : a.v_mul), int(s.first + (n / 2) * kTile));
-            }
-            if (!ok)   // the copies in flight have to land before the memory is given back
-                for (uint32_t i = n > C::kStages ? n - C::kStages : 0; i < n; ++i)
-                    mbar_wait(full + 8 * (i % C::kStages), (i / C::kStages) & 1);
-        }
-    } else if (warp == 8) {   // ------------------------------------- products
-        const uint32_t id_s = mma_desc(kTile, false) | a.negate, id_o = mma_desc(DP, true);
-        auto scores = [&](int t, uint32_t j) {   // S_t = Q_t K_j^T
-            if (lane == 0) {
-                product_rows<DP>(tmem + t * 128, sq + t * C::kBytes, sring + ((2 * j) % C::kStages) * C::kBytes, id_s);
-                mma_commit(s_full + 8 * t);
-            }
-        };
-        auto values = [&](int t, uint32_t j) {   // O_t += P_t V_j
-            if (lane == 0) {
-                product_cols<32>(tmem + 256 + t * 128, tmem + t * 128, sring + ((2 * j + 1) % C::kStages) * C::kBytes, id_o, j > 0);
-                mma_commit(o_full + 8 * t);
-            }
-        };
-        auto wait_tile = [&](uint32_t n) { return warp_wait(full + 8 * (n % C::kStages), (n / C::kStages) & 1); };
-        auto release = [&](uint32_t n) {
-            if (lane == 0 && n + C::kStages < 2 * nb) mma_commit(empty + 8 * (n % C::kStages));   // somebody waits for it
-        };
-        ok = warp_wait(q_full, 0) && wait_tile(0);
-        if (ok) {
-            tc_fence_after();
-            scores(0, 0);
-            if (two) scores(1, 0);
-            release(0);
-        }
-        for (uint32_t j = 0; ok && j < nb; ++j) {
-            if (!(ok = wait_tile(2 * j + 1))) break;
-            if (j + 1 < nb && !(ok = wait_tile(2 * j + 2))) break;
-            if (j == nb - 1 && s.len < (j + 1) * kTile) {
-                zero_tile_rows<C::kSub>(sring + ((2 * j + 1) % C::kStages) * C::kBytes, s.len - j * kTile);
-            }
-            if (j < nb0) {
-                if (!(ok = warp_wait(p_full, j & 1))) break;
-                tc_fence_after();
-                values(0, j);
-                if (j + 1 < nb0) scores(0, j + 1);
-            }
-            if (two) {
-                if (!(ok = warp_wait(p_full + 8, j & 1))) break;
-                tc_fence_after();
-                values(1, j);
-                release(2 * j + 1);
-                if (j + 1 < nb) {
-                    scores(1, j + 1);
-                    release(2 * j + 2);
+        registers_down<C::kOtherRegs>();
+        if (warp == 9) {   // -------------------------------------------- loads
+            uint32_t n = 0, tiles = 0;   // ring items so far, jobs so far
+            for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+                if (w.kind != kJobWork) continue;
+                const uint32_t row0 = w.block * 2 * kTile, kv_head = w.head / group;
+                const bool two = row0 + kTile < w.len;
+                const uint32_t items = 2 * (w.block * 2 + 1 + (two ? 1 : 0));
+                if (tiles > 0 && !(ok = warp_wait(q_empty, (tiles - 1) & 1))) break;
+                ++tiles;
+                if (lane == 0) {
+                    mbar_expect(q_full, (two ? 2 : 1) * C::kBytes);
+                    for (int t = 0; t < (two ? 2 : 1); ++t)
+                        for (int x = 0; x < C::kSub; ++x)
+                            tma_load(sq + t * C::kBytes + x * (kTile * 128), &mq, q_full, x * 64, int(w.head) * a.q_mul,
+                                     int(w.first + row0 + t * kTile));
                 }
-            } else {
-                release(2 * j + 1);
-                if (j + 1 < nb) release(2 * j + 2);
+                for (uint32_t i = 0; i < items; ++i, ++n) {
+                    const uint32_t st = n % C::kStages, use = n / C::kStages;
+                    if (use > 0 && !(ok = warp_wait(empty + 8 * st, (use - 1) & 1))) break;
+                    const bool is_k = (i & 1) == 0;
+                    if (lane == 0) {
+                        mbar_expect(full + 8 * st, C::kBytes);
+                        for (int x = 0; x < C::kSub; ++x)
+                            tma_load(sring + st * C::kBytes + x * (kTile * 128), is_k ? &mk : &mv, full + 8 * st, x * 64,
+                                     int(kv_head) * (is_k ? a.k_mul : a.v_mul), int(w.first + (i / 2) * kTile));
+                    }
+                }
+                if (!ok) break;
             }
+            // the CTA must not end, nor its memory be given back, before the last loads and releases have arrived
+            if (tiles > 0) {
+                mbar_wait(q_full, (tiles - 1) & 1);
+                if (ok) ok = warp_wait(q_empty, (tiles - 1) & 1);
+            }
+            for (uint32_t i = n > C::kStages ? n - C::kStages : 0; i < n; ++i) {
+                mbar_wait(full + 8 * (i % C::kStages), (i / C::kStages) & 1);
+                if (ok) ok = warp_wait(empty + 8 * (i % C::kStages), (i / C::kStages) & 1);
+            }
+        } else if (warp == 8) {   // --------------------------------- products
+            const uint32_t id_s = mma_desc(kTile, false) | a.negate, id_o = mma_desc(DP, true);
+            uint32_t n0 = 0, tiles = 0, done[2] = {0, 0};   // first ring item of the job; jobs, row blocks so far
+            auto item = [&](uint32_t n) { return sring + (n % C::kStages) * C::kBytes; };
+            auto wait_item = [&](uint32_t n) { return warp_wait(full + 8 * (n % C::kStages), (n / C::kStages) & 1); };
+            auto release = [&](uint32_t n) {
+                if (lane == 0) mma_commit(empty + 8 * (n % C::kStages));
+            };
+            for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+                if (w.kind != kJobWork) continue;
+                const bool two = w.block * 2 * kTile + kTile < w.len;
+                const uint32_t nb0 = w.block * 2 + 1, nb = nb0 + (two ? 1 : 0);   // key tiles of the first tile; of both
+                auto scores = [&](int t, uint32_t j) {   // S_t = Q_t K_j^T
+                    if (lane == 0) {
+                        product_rows<DP>(tmem + t * 128, sq + t * C::kBytes, item(n0 + 2 * j), id_s);
+                        mma_commit(s_full + 8 * t);
+                    }
+                };
+                auto values = [&](int t, uint32_t j) {   // O_t += P_t V_j
+                    if (lane == 0) {
+                        product_cols<32>(tmem + 256 + t * 128, tmem + t * 128, item(n0 + 2 * j + 1), id_o, j > 0);
+                        mma_commit(o_full + 8 * t);
+                    }
+                    ++done[t];
+                };
+                if (!(ok = warp_wait(q_full, tiles & 1) && wait_item(n0))) break;
+                ++tiles;
+                tc_fence_after();
+                scores(0, 0);
+                if (two) scores(1, 0);
+                release(n0);
+                if (nb == 1 && lane == 0) mma_commit(q_empty);
+                for (uint32_t j = 0; j < nb; ++j) {
+                    if (!(ok = wait_item(n0 + 2 * j + 1))) break;
+                    if (j + 1 < nb && !(ok = wait_item(n0 + 2 * j + 2))) break;
+                    if (j == nb - 1 && w.len < nb * kTile) zero_tile_rows<C::kSub>(item(n0 + 2 * j + 1), w.len - j * kTile);
+                    if (j < nb0) {
+                        if (!(ok = warp_wait(p_full, done[0] & 1))) break;
+                        tc_fence_after();
+                        values(0, j);
+                        if (j + 1 < nb0) scores(0, j + 1);
+                    }
+                    if (two) {
+                        if (!(ok = warp_wait(p_full + 8, done[1] & 1))) break;
+                        tc_fence_after();
+                        values(1, j);
+                    }
+                    release(n0 + 2 * j + 1);
+                    if (j + 1 < nb) {
+                        if (two) scores(1, j + 1);
+                        release(n0 + 2 * j + 2);
+                        if (j + 2 == nb && lane == 0) mma_commit(q_empty);   // the last use of Q
+                    }
+                }
+                if (!ok) break;
+                n0 += 2 * nb;
+            }
+        } else if (warp == 10) {   // ------------------------------------ jobs
+            ok = jobs.template run<2 * kTile, true>(a, a.q_heads);
         }
-    }
-    } else if (warp < 4 || two) {   // -------------------------- a row of a tile
+    } else {   // ------------------------------------------- a row of a tile
         registers_up<C::kRowRegs>();
         const int t = warp >> 2;
-        const uint32_t my_blocks = nb0 + t, lanes = (warp & 3) << 21;   // tensor memory lane 32 (warp & 3)
+        const uint32_t lanes = (warp & 3) << 21;   // tensor memory lane 32 (warp & 3)
         const uint32_t ts = tmem + t * 128 + lanes, to = tmem + 256 + t * 128 + lanes;
         const uint32_t local = (warp & 3) * 32 + lane;
         const float c = a.exp2_scale;
-        float m = -INFINITY;
-        float2 sum = make_float2(0.f, 0.f);
-        for (uint32_t j = 0; j < my_blocks; ++j) {
-            if (!(ok = warp_wait(s_full + 8 * t, j & 1))) break;
-            tc_fence_after();
-            uint32_t r[4][32];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld32(r[i], ts + 32 * i);
-            tmem_wait_ld();
-            if (j == my_blocks - 1) {   // the diagonal tile
-#pragma unroll
-                for (int i = 0; i < 128; ++i)
-                    if (uint32_t(i) > local) r[i / 32][i % 32] = __float_as_uint(-INFINITY);
+        uint32_t it = 0;   // row blocks of this tile so far
+        for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+            const uint32_t row0 = w.block * 2 * kTile;
+            if (w.kind == kJobTail) {
+                const uint32_t from = w.first + row0, end = min(w.first + w.len, from + 2 * kTile);
+                fill_rows(a.o, from, end, w.head, a.head_dim, kZeroBits, 256);
+                for (uint32_t i = from + threadIdx.x; i < end; i += 256) a.lse[size_t(w.head) * a.n_tokens + i] = -INFINITY;
             }
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int i = 0; i < 128; ++i) mx[i % 4] = fmaxf(mx[i % 4], __uint_as_float(r[i / 32][i % 32]));
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-            if (j == 0) m = top;
-            else if (__any_sync(0xFFFFFFFFu, (top - m) * c > 8.0f)) {
-                if (!(ok = warp_wait(o_full + 8 * t, (j - 1) & 1))) break;
+            if (w.kind != kJobWork || row0 + t * kTile >= w.len) continue;
+            const uint32_t my_blocks = w.block * 2 + 1 + t;
+            float m = -INFINITY;
+            float2 sum = make_float2(0.f, 0.f);
+            for (uint32_t j = 0; j < my_blocks; ++j, ++it) {
+                if (!(ok = warp_wait(s_full + 8 * t, it & 1))) break;
                 tc_fence_after();
-                const float next = fmaxf(m, top), f = exp2_approx((m - next) * c);
-                const float2 f2 = make_float2(f, f);
-                sum = mul2(sum, f2);
-                m = next;
+                uint32_t r[4][32];
 #pragma unroll
-                for (int i = 0; i < DP / 32; ++i) {
-                    uint32_t w[32];
-                    tmem_ld32(w, to + 32 * i);
-                    tmem_wait_ld();
+                for (int i = 0; i < 4; ++i) tmem_ld32(r[i], ts + 32 * i);
+                tmem_wait_ld();
+                if (j == my_blocks - 1) {   // the diagonal tile
 #pragma unroll
-                    for (int u = 0; u < 32; ++u) w[u] = __float_as_uint(__uint_as_float(w[u]) * f);
-                    tmem_st32(to + 32 * i, w);
+                    for (int i = 0; i < 128; ++i)
+                        if (uint32_t(i) > local) r[i / 32][i % 32] = __float_as_uint(-INFINITY);
                 }
-            }
-            const float2 c2 = make_float2(c, c), mc = make_float2(-m * c, -m * c);
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                uint32_t p[16];
+                for (int i = 0; i < 128; i += 2)
+                    mx[(i / 2) % 4] = max3(mx[(i / 2) % 4], __uint_as_float(r[i / 32][i % 32]), __uint_as_float(r[i / 32][i % 32 + 1]));
+                const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]);
+                if (j == 0) m = top;
+                else if (__any_sync(0xFFFFFFFFu, (top - m) * c > 8.0f)) {
+                    if (!(ok = warp_wait(o_full + 8 * t, (it - 1) & 1))) break;
+                    tc_fence_after();
+                    const float next = fmaxf(m, top), f = exp2_approx((m - next) * c);
+                    sum = mul2(sum, make_float2(f, f));
+                    m = next;
+#pragma unroll 1
+                    for (int i = 0; i < DP / 16; ++i) {   // rare: few registers matter more than speed
+                        uint32_t x[16];
+                        tmem_ld16(x, to + 16 * i);
+                        tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float2 x = fma2(make_float2(__uint_as_float(r[h][2 * i]), __uint_as_float(r[h][2 * i + 1])), c2, mc);
-                    const float2 e = make_float2(exp2_approx(x.x), exp2_approx(x.y));
-                    sum = add2(sum, e);
-                    p[i] = bf16x2(e.x, e.y);
+                        for (int u = 0; u < 16; ++u) x[u] = __float_as_uint(__uint_as_float(x[u]) * f);
+                        tmem_st16(to + 16 * i, x);
+                    }
                 }
-                tmem_st16(ts + 16 * h, p);
+                const float2 c2 = make_float2(c, c), mc = make_float2(-m * c, -m * c);
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float2 x = fma2(make_float2(__uint_as_float(r[h][2 * i]), __uint_as_float(r[h][2 * i + 1])), c2, mc);
+                        const float2 e = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+                        sum = add2(sum, e);
+                        p[i] = bf16x2(e.x, e.y);
+                    }
+                    tmem_st16(ts + 16 * h, p);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + 8 * t);
             }
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + 8 * t);
-        }
-        if (ok) ok = warp_wait(o_full + 8 * t, (my_blocks - 1) & 1);
-        if (ok) {
+            if (!ok || !(ok = warp_wait(o_full + 8 * t, (it - 1) & 1))) break;
             tc_fence_after();
             const float total = sum.x + sum.y, inv = 1.0f / total;
             const uint32_t row = row0 + t * kTile + local;
-            const bool mine = row < s.len;
-            char *out = a.o.p + (long long)(s.first + row) * a.o.token + (long long)head * a.o.head;
-            if (mine)
-                a.lse[size_t(head) * a.n_tokens + s.first + row] = m * fabsf(a.scale) + logf(total);
+            const bool mine = row < w.len;
+            char *out = a.o.p + (long long)(w.first + row) * a.o.token + (long long)w.head * a.o.head;
+            if (mine) a.lse[size_t(w.head) * a.n_tokens + w.first + row] = m * fabsf(a.scale) + logf(total);
 #pragma unroll
             for (int i = 0; i < DP / 32; ++i) {
-                uint32_t w[32];
-                tmem_ld32(w, to + 32 * i);
+                uint32_t x[32];
+                tmem_ld32(x, to + 32 * i);
                 tmem_wait_ld();
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    const float *f = reinterpret_cast<const float *>(w + 8 * u);
+                    const float *f = reinterpret_cast<const float *>(x + 8 * u);
                     const uint4 v = make_uint4(bf16x2(f[0] * inv, f[1] * inv), bf16x2(f[2] * inv, f[3] * inv),
                                                bf16x2(f[4] * inv, f[5] * inv), bf16x2(f[6] * inv, f[7] * inv));
                     if (mine && 32 * i + 8 * u < int(a.head_dim)) *reinterpret_cast<uint4 *>(out + (32 * i + 8 * u) * 2) = v;
                 }
             }
+            tc_fence_before();   // O has been read: the next job's first product, after this warp's next arrival, may overwrite it
         }
     }
     tc_fence_before();
@@ -404,10 +513,11 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     tc_fence_after();
     if (warp == 8) tmem_free(tmem, 512);
     if (bad) {
-        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + 2 * kTile);
-        fill_rows(a.o, from, to, head, a.head_dim, kNanBits);
-        for (uint32_t t = from + threadIdx.x; t < to; t += blockDim.x)
-            a.lse[size_t(head) * a.n_tokens + t] = __int_as_float(0x7FFFFFFF);
+        if (w.kind == kJobWork) {   // each warp's own last job
+            const uint32_t from = w.first + w.block * 2 * kTile, end = min(w.first + w.len, from + 2 * kTile);
+            poison_rows(a.o, from, end, w.head, a.head_dim);
+            for (uint32_t i = from + lane; i < end; i += 32) a.lse[size_t(w.head) * a.n_tokens + i] = __int_as_float(0x7FFFFFFF);
+        }
         if (threadIdx.x == 0) g_attn_fault = 1;
     }
 }
@@ -476,8 +586,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     if (s.tail) {
         const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
         if (part == 0) {
-            fill_rows(a.d_k, from, to, kv_head, a.head_dim, kZeroBits);
-            fill_rows(a.d_v, from, to, kv_head, a.head_dim, kZeroBits);
+            fill_rows(a.d_k, from, to, kv_head, a.head_dim, kZeroBits, blockDim.x);
+            fill_rows(a.d_v, from, to, kv_head, a.head_dim, kZeroBits, blockDim.x);
         }
         return;
     }
@@ -730,8 +840,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     if (warp == 8) tmem_free(tmem, 512);
     if (bad) {
         const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
-        fill_rows(a.d_k, from, to, kv_head, a.head_dim, kNanBits);
-        fill_rows(a.d_v, from, to, kv_head, a.head_dim, kNanBits);
+        fill_rows(a.d_k, from, to, kv_head, a.head_dim, kNanBits, blockDim.x);
+        fill_rows(a.d_v, from, to, kv_head, a.head_dim, kNanBits, blockDim.x);
         if (a.parts > 1)
             for (uint32_t which = 0; which < 2; ++which)
                 for (uint32_t i = threadIdx.x; i < (to - from) * a.head_dim; i += blockDim.x)
@@ -788,7 +898,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     const uint32_t row0 = s.block * kTile;
     if (s.tail) {
         const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
-        fill_rows(a.d_q, from, to, head, a.head_dim, kZeroBits);
+        fill_rows(a.d_q, from, to, head, a.head_dim, kZeroBits, blockDim.x);
         return;
     }
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -963,7 +1073,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     if (warp == 8) tmem_free(tmem, 512);
     if (bad) {
         const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
-        fill_rows(a.d_q, from, to, head, a.head_dim, kNanBits);
+        fill_rows(a.d_q, from, to, head, a.head_dim, kNanBits, blockDim.x);
         if (threadIdx.x == 0) g_attn_fault = 1;
     }
 }

@@ -231,6 +231,43 @@ __device__ __forceinline__ void zero_tile_rows(uint32_t tile, uint32_t from) {
     __syncwarp();
 }
 
+// Writes 32 accumulator rows (one per lane) as bfloat16 rows, by one warp: 64 columns at a time go through 4 KB of shared
+// memory, so that eight lanes write one row's 128 bytes together.  Written straight from the lanes, 32 rows at a
+// time, the same stores take 4800 cycles for a tile of 128 x 128 instead of 900.
+constexpr uint32_t kStageBytes = 4096;   // per warp
+template <int DP>
+__device__ __forceinline__ void store_rows(uint32_t stage, uint32_t tmem, float f, const RowsOut &o, uint32_t token, uint32_t head,
+                                           uint32_t rows, uint32_t dim) {
+    const uint32_t lane = threadIdx.x & 31;
+    char *out = o.p + (long long)token * o.token + (long long)head * o.head;
+#pragma unroll 1
+    for (uint32_t col = 0; col < DP; col += 64) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t x[32];
+            tmem_ld32(x, tmem + col + 32 * h);
+            tmem_wait_ld();
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float *v = reinterpret_cast<const float *>(x + 8 * u);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                             ::"r"(stage + lane * 128 + (((4 * h + u) ^ (lane & 7)) * 16)), "r"(bf16x2(v[0] * f, v[1] * f)),
+                               "r"(bf16x2(v[2] * f, v[3] * f)), "r"(bf16x2(v[4] * f, v[5] * f)), "r"(bf16x2(v[6] * f, v[7] * f)) : "memory");
+            }
+        }
+        __syncwarp();
+        const uint32_t c = lane & 7;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            const uint32_t r = 4 * i + lane / 8;
+            uint4 v;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(stage + r * 128 + ((c ^ (r & 7)) * 16)) : "memory");
+            if (r < rows && col + 8 * c < dim) *reinterpret_cast<uint4 *>(out + (long long)r * o.token + (col + 8 * c) * 2) = v;
+        }
+        __syncwarp();
+    }
+}
+
 // d = a b^T over DP columns, both operands in shared memory, rows along the result.
 template <int DP>
 __device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
@@ -268,11 +305,11 @@ template <int DP>
 struct Fwd {
     static constexpr int kSub = DP / 64;                     // 64-wide blocks of a row
     static constexpr int kBytes = kTile * DP * 2;            // one tile
-    static constexpr int kStages = DP == 128 ? 5 : 8;        // key and value tiles in flight
+    static constexpr int kStages = DP == 128 ? 4 : 8;        // key and value tiles in flight
     static constexpr int kThreads = 384;
     static constexpr int kRegs = 168, kRowRegs = 208, kOtherRegs = 88;   // at launch; then two warpgroups, one
     static_assert(2 * kRowRegs + kOtherRegs <= 3 * kRegs, "shares of the launch's registers");
-    static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + 512;
+    static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + 8 * kStageBytes + 512;
 };
 
 template <int DP>
@@ -284,7 +321,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = a.q_heads / a.kv_heads;
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t sq = base, sring = base + 2 * C::kBytes;
-    const uint32_t bars = sring + C::kStages * C::kBytes;
+    const uint32_t stage = sring + C::kStages * C::kBytes, bars = stage + 8 * kStageBytes;
     const Jobs jobs(bars);
     const uint32_t q_full = bars + Jobs::kBytes, q_empty = q_full + 8, s_full = q_full + 16, p_full = q_full + 32, o_full = q_full + 48,
                    full = q_full + 64, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
@@ -448,13 +485,14 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int i = 0; i < 128; i += 2)
-                    mx[(i / 2) % 4] = max3(mx[(i / 2) % 4], __uint_as_float(r[i / 32][i % 32]), __uint_as_float(r[i / 32][i % 32 + 1]));
-                const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]);
+                    mx[(i / 2) % 4] = max3_nan(mx[(i / 2) % 4], __uint_as_float(r[i / 32][i % 32]), __uint_as_float(r[i / 32][i % 32 + 1]));
+                float top = max3_nan(max3_nan(mx[0], mx[1], mx[1]), mx[2], mx[3]);
+                top += top - top;   // an infinite score, like a NaN, makes its whole row NaN
                 if (j == 0) m = top;
-                else if (__any_sync(0xFFFFFFFFu, (top - m) * c > 8.0f)) {
+                else if (__any_sync(0xFFFFFFFFu, !((top - m) * c <= 8.0f))) {
                     if (!(ok = warp_wait(o_full + 8 * t, (it - 1) & 1))) break;
                     tc_fence_after();
-                    const float next = fmaxf(m, top), f = exp2_approx((m - next) * c);
+                    const float next = max3_nan(m, top, top), f = exp2_approx((m - next) * c);
                     sum = mul2(sum, make_float2(f, f));
                     m = next;
 #pragma unroll 1
@@ -489,22 +527,9 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             tc_fence_after();
             const float total = sum.x + sum.y, inv = 1.0f / total;
             const uint32_t row = row0 + t * kTile + local;
-            const bool mine = row < w.len;
-            char *out = a.o.p + (long long)(w.first + row) * a.o.token + (long long)w.head * a.o.head;
-            if (mine) a.lse[size_t(w.head) * a.n_tokens + w.first + row] = m * fabsf(a.scale) + logf(total);
-#pragma unroll
-            for (int i = 0; i < DP / 32; ++i) {
-                uint32_t x[32];
-                tmem_ld32(x, to + 32 * i);
-                tmem_wait_ld();
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const float *f = reinterpret_cast<const float *>(x + 8 * u);
-                    const uint4 v = make_uint4(bf16x2(f[0] * inv, f[1] * inv), bf16x2(f[2] * inv, f[3] * inv),
-                                               bf16x2(f[4] * inv, f[5] * inv), bf16x2(f[6] * inv, f[7] * inv));
-                    if (mine && 32 * i + 8 * u < int(a.head_dim)) *reinterpret_cast<uint4 *>(out + (32 * i + 8 * u) * 2) = v;
-                }
-            }
+            if (row < w.len) a.lse[size_t(w.head) * a.n_tokens + w.first + row] = m * fabsf(a.scale) + logf(total);
+            const uint32_t row_w = row - lane;   // the warp's first row
+            store_rows<DP>(stage + warp * kStageBytes, to, inv, a.o, w.first + row_w, w.head, w.len > row_w ? w.len - row_w : 0u, a.head_dim);
             tc_fence_before();   // O has been read: the next job's first product, after this warp's next arrival, may overwrite it
         }
     }

@@ -186,7 +186,7 @@ int launch_backward(const gac_attn &a, const gac_attn_grad &g, int device, cudaS
     if (int rc = grid_of(jobs, a.q_heads, &grid_q)) return rc;
     if (int rc = grid_of(jobs, a.kv_heads * d.parts, &grid_kv)) return rc;
     if (int rc = allow_smem(attn_dq_kernel<DP>, BwdQ<DP>::kSmem, device, done_q)) return rc;
-    if (int rc = allow_smem(attn_dkv_kernel<DP>, BwdKv<DP>::kSmem, device, done_kv)) return rc;
+    if (int rc = allow_smem(attn_dkv_kernel<DP>, BwdKv<DP>::kSmem, device, done_kv, BwdKv<DP>::kRegs)) return rc;
     const uint64_t units = uint64_t(a.q_heads) * a.n_tokens, per = kRowThreads / 16;
     attn_rows_kernel<<<uint32_t((units + per - 1) / per), kRowThreads, 0, s>>>(d);
     attn_dkv_kernel<DP><<<grid_kv, BwdKv<DP>::kThreads, BwdKv<DP>::kSmem, s>>>(mq, mk, mv, mdo, d);

@@ -231,19 +231,19 @@ __device__ __forceinline__ void zero_tile_rows(uint32_t tile, uint32_t from) {
     __syncwarp();
 }
 
-// Writes 32 accumulator rows (one per lane) as bfloat16 rows, by one warp: 64 columns at a time go through 4 KB of shared
-// memory, so that eight lanes write one row's 128 bytes together.  Written straight from the lanes, 32 rows at a
-// time, the same stores take 4800 cycles for a tile of 128 x 128 instead of 900.
-constexpr uint32_t kStageBytes = 4096;   // per warp
-template <int DP>
+// Writes 32 accumulator rows (one per lane) as bfloat16 rows, by one warp: COLS columns at a time go through 64 COLS bytes
+// of shared memory, so that COLS/8 lanes write one row's COLS columns together.  Written straight from the lanes, 32
+// rows at a time, the same stores take 4800 cycles for a tile of 128 x 128 instead of 900.
+template <int DP, int COLS>
 __device__ __forceinline__ void store_rows(uint32_t stage, uint32_t tmem, float f, const RowsOut &o, uint32_t token, uint32_t head,
                                            uint32_t rows, uint32_t dim) {
+    constexpr uint32_t kPer = COLS / 8, kSpread = 8 / kPer;   // 16-byte pieces of a row; rows that share a bank line
     const uint32_t lane = threadIdx.x & 31;
     char *out = o.p + (long long)token * o.token + (long long)head * o.head;
 #pragma unroll 1
-    for (uint32_t col = 0; col < DP; col += 64) {
+    for (uint32_t col = 0; col < DP; col += COLS) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < COLS / 32; ++h) {
             uint32_t x[32];
             tmem_ld32(x, tmem + col + 32 * h);
             tmem_wait_ld();
@@ -251,18 +251,47 @@ __device__ __forceinline__ void store_rows(uint32_t stage, uint32_t tmem, float 
             for (int u = 0; u < 4; ++u) {
                 const float *v = reinterpret_cast<const float *>(x + 8 * u);
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                             ::"r"(stage + lane * 128 + (((4 * h + u) ^ (lane & 7)) * 16)), "r"(bf16x2(v[0] * f, v[1] * f)),
+                             ::"r"(stage + lane * (COLS * 2) + (((4 * h + u) ^ ((lane / kSpread) % kPer)) * 16)), "r"(bf16x2(v[0] * f, v[1] * f)),
                                "r"(bf16x2(v[2] * f, v[3] * f)), "r"(bf16x2(v[4] * f, v[5] * f)), "r"(bf16x2(v[6] * f, v[7] * f)) : "memory");
             }
         }
         __syncwarp();
-        const uint32_t c = lane & 7;
+        const uint32_t c = lane % kPer;
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) {
-            const uint32_t r = 4 * i + lane / 8;
+        for (uint32_t i = 0; i < kPer; ++i) {
+            const uint32_t r = i * (32 / kPer) + lane / kPer;
             uint4 v;
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(stage + r * 128 + ((c ^ (r & 7)) * 16)) : "memory");
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                         : "r"(stage + r * (COLS * 2) + ((c ^ ((r / kSpread) % kPer)) * 16)) : "memory");
             if (r < rows && col + 8 * c < dim) *reinterpret_cast<uint4 *>(out + (long long)r * o.token + (col + 8 * c) * 2) = v;
+        }
+        __syncwarp();
+    }
+}
+// The same as binary32 rows `pitch` elements apart, 16 columns (2 KB of shared memory) at a time.
+template <int DP>
+__device__ __forceinline__ void store_rows_f32(uint32_t stage, uint32_t tmem, float f, float *out, size_t pitch, uint32_t rows, uint32_t dim) {
+    const uint32_t lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (uint32_t col = 0; col < DP; col += 16) {
+        uint32_t x[16];
+        tmem_ld16(x, tmem + col);
+        tmem_wait_ld();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float *v = reinterpret_cast<const float *>(x + 4 * u);
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 64 + ((u ^ ((lane / 2) % 4)) * 16)),
+                         "f"(v[0] * f), "f"(v[1] * f), "f"(v[2] * f), "f"(v[3] * f) : "memory");
+        }
+        __syncwarp();
+        const uint32_t c = lane % 4;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint32_t r = i * 8 + lane / 4;
+            float4 v;
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                         : "r"(stage + r * 64 + ((c ^ ((r / 2) % 4)) * 16)) : "memory");
+            if (r < rows && col + 4 * c < dim) *reinterpret_cast<float4 *>(out + r * pitch + col + 4 * c) = v;
         }
         __syncwarp();
     }
@@ -306,6 +335,7 @@ struct Fwd {
     static constexpr int kSub = DP / 64;                     // 64-wide blocks of a row
     static constexpr int kBytes = kTile * DP * 2;            // one tile
     static constexpr int kStages = DP == 128 ? 4 : 8;        // key and value tiles in flight
+    static constexpr int kStageBytes = 4096;                 // per warp, on the way out
     static constexpr int kThreads = 384;
     static constexpr int kRegs = 168, kRowRegs = 208, kOtherRegs = 88;   // at launch; then two warpgroups, one
     static_assert(2 * kRowRegs + kOtherRegs <= 3 * kRegs, "shares of the launch's registers");
@@ -321,7 +351,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = a.q_heads / a.kv_heads;
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t sq = base, sring = base + 2 * C::kBytes;
-    const uint32_t stage = sring + C::kStages * C::kBytes, bars = stage + 8 * kStageBytes;
+    const uint32_t stage = sring + C::kStages * C::kBytes, bars = stage + 8 * C::kStageBytes;
     const Jobs jobs(bars);
     const uint32_t q_full = bars + Jobs::kBytes, q_empty = q_full + 8, s_full = q_full + 16, p_full = q_full + 32, o_full = q_full + 48,
                    full = q_full + 64, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
@@ -529,7 +559,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             const uint32_t row = row0 + t * kTile + local;
             if (row < w.len) a.lse[size_t(w.head) * a.n_tokens + w.first + row] = m * fabsf(a.scale) + logf(total);
             const uint32_t row_w = row - lane;   // the warp's first row
-            store_rows<DP>(stage + warp * kStageBytes, to, inv, a.o, w.first + row_w, w.head, w.len > row_w ? w.len - row_w : 0u, a.head_dim);
+            store_rows<DP, 64>(stage + warp * C::kStageBytes, to, inv, a.o, w.first + row_w, w.head, w.len > row_w ? w.len - row_w : 0u, a.head_dim);
             tc_fence_before();   // O has been read: the next job's first product, after this warp's next arrival, may overwrite it
         }
     }
@@ -584,16 +614,19 @@ static __global__ void __launch_bounds__(kRowThreads) attn_rows_kernel(const __g
 // heads of the group (or of one part of it).  Rows of the accumulators are keys, so P^T and dS^T come out of
 // the products as they have to go into the next ones, from tensor memory; nothing is transposed.
 // Warps: 0-3 and 4-7 take the two halves of the query columns, 8 issues the products, 9 the TMA loads, 10 fetches the
-// row terms.  While the threads make dS of one query tile the tensor cores run dV and the next S; while they take
-// the next exponentials, dK and the next dP.
+// row terms, 11 finds the jobs.  While the threads make dS of one query tile the tensor cores run dV and the next S;
+// while they take the next exponentials, dK and the next dP.
 template <int DP>
 struct BwdKv {
     static constexpr int kSub = DP / 64;
     static constexpr int kBytes = kTile * DP * 2;
     static constexpr int kStages = DP == 128 ? 4 : 8;
     static constexpr int kRowSlots = 4;
-    static constexpr int kThreads = 352;
-    static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + kRowSlots * 1024 + 256;
+    static constexpr int kStageBytes = 2048;   // per warp, on the way out
+    static constexpr int kThreads = 384;
+    static constexpr int kRegs = 168, kRowRegs = 208, kOtherRegs = 88;   // at launch; then two warpgroups, one
+    static_assert(2 * kRowRegs + kOtherRegs <= 3 * kRegs, "shares of the launch's registers");
+    static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + kRowSlots * 1024 + 8 * kStageBytes + 512;
 };
 
 template <int DP>
@@ -602,34 +635,23 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ AttnDev a) {
     using C = BwdKv<DP>;
     extern __shared__ char smem_raw[];
-    const uint32_t lots = a.kv_heads * a.parts, lot = blockIdx.x % lots;
-    const uint32_t kv_head = lot % a.kv_heads, part = lot / a.kv_heads;
+    const uint32_t lots = a.kv_heads * a.parts;   // a job's head names the key head and the part of its group
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Job s = find_job<kTile, false>(a, blockIdx.x / lots, gridDim.x / lots);
-    if (s.none) return;
-    const uint32_t row0 = s.block * kTile;
-    if (s.tail) {
-        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
-        if (part == 0) {
-            fill_rows(a.d_k, from, to, kv_head, a.head_dim, kZeroBits, blockDim.x);
-            fill_rows(a.d_v, from, to, kv_head, a.head_dim, kZeroBits, blockDim.x);
-        }
-        return;
-    }
+    const uint32_t heads = a.q_heads / a.kv_heads / a.parts;
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t sk = base, sv = base + C::kBytes, sring = base + 2 * C::kBytes;
     const uint32_t srows = sring + C::kStages * C::kBytes;   // per slot: 128 x -log2(e) lse, 128 x D
-    const uint32_t bars = srows + C::kRowSlots * 1024;
-    const uint32_t kv_full = bars, s_full = bars + 8, dp_full = bars + 16, p_full = bars + 24, ds_full = bars + 32, done = bars + 40,
-                   rows_full = bars + 48, rows_empty = rows_full + 8 * C::kRowSlots, full = rows_empty + 8 * C::kRowSlots,
-                   empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
-    const uint32_t q_tiles = (s.len + kTile - 1) / kTile - s.block;   // from the diagonal on
-    const uint32_t heads = a.q_heads / a.kv_heads / a.parts, head0 = kv_head * (a.q_heads / a.kv_heads) + part * heads;
-    const uint32_t total = q_tiles * heads;
+    const uint32_t stage = srows + C::kRowSlots * 1024, bars = stage + 8 * C::kStageBytes;
+    const Jobs jobs(bars);
+    const uint32_t kv_full = bars + Jobs::kBytes, kv_empty = kv_full + 8, s_full = kv_full + 16, dp_full = kv_full + 24, p_full = kv_full + 32,
+                   ds_full = kv_full + 40, done = kv_full + 48, rows_full = kv_full + 56, rows_empty = rows_full + 8 * C::kRowSlots,
+                   full = rows_empty + 8 * C::kRowSlots, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
 
     if (warp == 8) tmem_alloc(tmem_slot, 512);
     if (threadIdx.x == 0) {
+        jobs.init(11);
         mbar_init(kv_full, 1);
+        mbar_init(kv_empty, 1);
         mbar_init(s_full, 1);
         mbar_init(dp_full, 1);
         mbar_init(p_full, 8);
@@ -652,211 +674,255 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
     const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 384;
     bool ok = true;
+    JobWord w;
+    w.kind = kJobNone;
+    auto q_tiles_of = [](const JobWord &j) { return (j.len + kTile - 1) / kTile - j.block; };   // from the diagonal on
+    auto kv_head_of = [&](const JobWord &j) { return j.head % a.kv_heads; };
+    auto head0_of = [&](const JobWord &j) { return kv_head_of(j) * (a.q_heads / a.kv_heads) + (j.head / a.kv_heads) * heads; };
 
-    if (warp == 9) {   // ------------------------------------------------ loads
-        if (lane == 0) {
-            mbar_expect(kv_full, 2 * C::kBytes);
-            for (int x = 0; x < C::kSub; ++x) {
-                tma_load(sk + x * (kTile * 128), &mk, kv_full, x * 64, int(kv_head) * a.k_mul, int(s.first + row0));
-                tma_load(sv + x * (kTile * 128), &mv, kv_full, x * 64, int(kv_head) * a.v_mul, int(s.first + row0));
+    if (warp >= 8) {
+        registers_down<C::kOtherRegs>();
+        if (warp == 9) {   // -------------------------------------------- loads
+            uint32_t n = 0, tiles = 0;
+            for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+                if (w.kind != kJobWork) continue;
+                if (tiles > 0 && !(ok = warp_wait(kv_empty, (tiles - 1) & 1))) break;
+                ++tiles;
+                const uint32_t q_tiles = q_tiles_of(w), kv_head = kv_head_of(w);
+                if (lane == 0) {
+                    mbar_expect(kv_full, 2 * C::kBytes);
+                    for (int x = 0; x < C::kSub; ++x) {
+                        tma_load(sk + x * (kTile * 128), &mk, kv_full, x * 64, int(kv_head) * a.k_mul, int(w.first + w.block * kTile));
+                        tma_load(sv + x * (kTile * 128), &mv, kv_full, x * 64, int(kv_head) * a.v_mul, int(w.first + w.block * kTile));
+                    }
+                }
+                uint32_t h = head0_of(w), i = w.block;
+                for (uint32_t u = 0; u < 2 * heads * q_tiles; ++u, ++n) {   // Q, dO, Q, dO, ...
+                    const uint32_t st = n % C::kStages, use = n / C::kStages;
+                    if (use > 0 && !(ok = warp_wait(empty + 8 * st, (use - 1) & 1))) break;
+                    const bool is_q = (u & 1) == 0;
+                    if (lane == 0) {
+                        mbar_expect(full + 8 * st, C::kBytes);
+                        for (int x = 0; x < C::kSub; ++x)
+                            tma_load(sring + st * C::kBytes + x * (kTile * 128), is_q ? &mq : &mdo, full + 8 * st, x * 64,
+                                     int(h) * (is_q ? a.q_mul : a.do_mul), int(w.first + i * kTile));
+                    }
+                    if (!is_q && ++i == w.block + q_tiles) {
+                        i = w.block;
+                        ++h;
+                    }
+                }
+                if (!ok) break;
             }
+            // the CTA must not end, nor its memory be given back, before the last loads and releases have arrived
+            if (tiles > 0) {
+                mbar_wait(kv_full, (tiles - 1) & 1);
+                if (ok) ok = warp_wait(kv_empty, (tiles - 1) & 1);
+            }
+            for (uint32_t i = n > C::kStages ? n - C::kStages : 0; i < n; ++i) {
+                mbar_wait(full + 8 * (i % C::kStages), (i / C::kStages) & 1);
+                if (ok) ok = warp_wait(empty + 8 * (i % C::kStages), (i / C::kStages) & 1);
+            }
+        } else if (warp == 10) {   // -------------------------------- row terms
             uint32_t n = 0;
-            for (; n < 2 * total; ++n) {   // Q, dO, Q, dO, ...
-                const uint32_t st = n % C::kStages, use = n / C::kStages;
-                if (use > 0 && !(ok = mbar_wait(empty + 8 * st, (use - 1) & 1))) break;
-                const bool is_q = (n & 1) == 0;
-                const uint32_t h = head0 + (n / 2) / q_tiles, i = s.block + (n / 2) % q_tiles;
-                mbar_expect(full + 8 * st, C::kBytes);
-                for (int x = 0; x < C::kSub; ++x)
-                    tma_load(sring + st * C::kBytes + x * (kTile * 128), is_q ? &mq : &mdo, full + 8 * st, x * 64,
-                             int(h) * (is_q ? a.q_mul : a.do_mul), int(s.first + i * kTile));
-            }
-            if (!ok)
-                for (uint32_t i = n > C::kStages ? n - C::kStages : 0; i < n; ++i)
-                    mbar_wait(full + 8 * (i % C::kStages), (i / C::kStages) & 1);
-        }
-    } else if (warp == 10) {   // ------------------------------------ row terms
-        for (uint32_t n = 0; n < total; ++n) {
-            const uint32_t slot = n % C::kRowSlots, use = n / C::kRowSlots;
-            const uint32_t h = head0 + n / q_tiles, i = s.block + n % q_tiles;
-            const float2 *src = a.rows + size_t(h) * a.n_tokens + s.first + i * kTile;
-            float2 v[4];
+            for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+                if (w.kind != kJobWork) continue;
+                const uint32_t q_tiles = q_tiles_of(w);
+                uint32_t h = head0_of(w), i = w.block;
+                for (uint32_t u = 0; u < heads * q_tiles; ++u, ++n) {
+                    const uint32_t slot = n % C::kRowSlots, use = n / C::kRowSlots;
+                    const float2 *src = a.rows + size_t(h) * a.n_tokens + w.first + i * kTile;
+                    float2 v[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                v[u] = i * kTile + lane + 32 * u < s.len ? __ldg(src + lane + 32 * u) : make_float2(0.f, 0.f);
-            if (use > 0 && !(ok = warp_wait(rows_empty + 8 * slot, (use - 1) & 1))) break;
+                    for (int x = 0; x < 4; ++x)
+                        v[x] = i * kTile + lane + 32 * x < w.len ? __ldg(src + lane + 32 * x) : make_float2(0.f, 0.f);
+                    if (use > 0 && !(ok = warp_wait(rows_empty + 8 * slot, (use - 1) & 1))) break;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const uint32_t at = srows + slot * 1024 + (lane + 32 * u) * 4;
-                asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v[u].x) : "memory");
-                asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 512), "f"(v[u].y) : "memory");
+                    for (int x = 0; x < 4; ++x) {
+                        const uint32_t at = srows + slot * 1024 + (lane + 32 * x) * 4;
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v[x].x) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 512), "f"(v[x].y) : "memory");
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(rows_full + 8 * slot);
+                    if (++i == w.block + q_tiles) {
+                        i = w.block;
+                        ++h;
+                    }
+                }
+                if (!ok) break;
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(rows_full + 8 * slot);
-        }
-    } else if (warp == 8) {   // ------------------------------------- products
-        const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
-        auto item = [&](uint32_t n) { return sring + (n % C::kStages) * C::kBytes; };
-        auto wait_item = [&](uint32_t n) { return warp_wait(full + 8 * (n % C::kStages), (n / C::kStages) & 1); };
-        auto release = [&](uint32_t n) {
-            if (lane == 0 && n + C::kStages < 2 * total) mma_commit(empty + 8 * (n % C::kStages));
-        };
-        auto fix = [&](uint32_t n) {   // item n belongs to query tile n / 2
-            const uint32_t i = s.block + (n / 2) % q_tiles;
-            if (s.len < (i + 1) * kTile) zero_tile_rows<C::kSub>(item(n), s.len - i * kTile);
-        };
-        auto scores = [&](uint32_t n) {
-            if (lane == 0) {
-                product_rows<DP>(t_s, sk, item(2 * n), id_s | a.negate);
-                mma_commit(s_full);
+        } else if (warp == 8) {   // --------------------------------- products
+            const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
+            uint32_t n0 = 0, tiles = 0, it = 0;   // first ring item of the job; jobs, query tiles so far
+            auto item = [&](uint32_t n) { return sring + (n % C::kStages) * C::kBytes; };
+            auto wait_item = [&](uint32_t n) { return warp_wait(full + 8 * (n % C::kStages), (n / C::kStages) & 1); };
+            auto release = [&](uint32_t n) {
+                if (lane == 0) mma_commit(empty + 8 * (n % C::kStages));
+            };
+            for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+                if (w.kind != kJobWork) continue;
+                const uint32_t q_tiles = q_tiles_of(w), total = q_tiles * heads;
+                const bool ragged = w.len % kTile != 0;
+                uint32_t left = q_tiles;   // query tiles of this head from the one about to be made ready on
+                auto make_ready = [&](uint32_t u, bool last_of_tile) {   // item u of the job (Q and dO of query tile u / 2) is there
+                    if (left == 1 && ragged) zero_tile_rows<C::kSub>(item(n0 + u), w.len % kTile);
+                    if (last_of_tile && --left == 0) left = q_tiles;
+                };
+                auto scores = [&](uint32_t u) {
+                    if (lane == 0) {
+                        product_rows<DP>(t_s, sk, item(n0 + 2 * u), id_s | a.negate);
+                        mma_commit(s_full);
+                    }
+                };
+                auto d_probs = [&](uint32_t u) {
+                    if (lane == 0) {
+                        product_rows<DP>(t_dp, sv, item(n0 + 2 * u + 1), id_s);
+                        mma_commit(dp_full);
+                        if (u + 1 == total) mma_commit(kv_empty);   // the last use of K and V
+                    }
+                };
+                if (!(ok = warp_wait(kv_full, tiles & 1) && wait_item(n0))) break;
+                ++tiles;
+                tc_fence_after();
+                make_ready(0, false);
+                scores(0);
+                if (!(ok = wait_item(n0 + 1))) break;
+                make_ready(1, true);
+                d_probs(0);
+                for (uint32_t u = 0; u < total; ++u, ++it) {
+                    const bool more = u + 1 < total;
+                    if (!(ok = warp_wait(p_full, it & 1))) break;
+                    tc_fence_after();
+                    if (lane == 0) product_cols<64>(t_dv, t_s, item(n0 + 2 * u + 1), id_o, u > 0);
+                    release(n0 + 2 * u + 1);
+                    if (more) {
+                        if (!(ok = wait_item(n0 + 2 * u + 2))) break;
+                        make_ready(2 * u + 2, false);
+                        scores(u + 1);
+                    }
+                    if (!(ok = warp_wait(ds_full, it & 1))) break;
+                    tc_fence_after();
+                    if (lane == 0) product_cols<64>(t_dk, t_dp, item(n0 + 2 * u), id_o, u > 0);
+                    release(n0 + 2 * u);
+                    if (more) {
+                        if (!(ok = wait_item(n0 + 2 * u + 3))) break;
+                        make_ready(2 * u + 3, true);
+                        d_probs(u + 1);
+                    } else if (lane == 0) {
+                        mma_commit(done);
+                    }
+                }
+                if (!ok) break;
+                n0 += 2 * total;
             }
-        };
-        auto d_probs = [&](uint32_t n) {
-            if (lane == 0) {
-                product_rows<DP>(t_dp, sv, item(2 * n + 1), id_s);
-                mma_commit(dp_full);
-            }
-        };
-        ok = warp_wait(kv_full, 0) && wait_item(0);
-        if (ok) {
-            fix(0);
-            tc_fence_after();
-            scores(0);
-            ok = wait_item(1);
-        }
-        if (ok) {
-            fix(1);
-            d_probs(0);
-        }
-        for (uint32_t n = 0; ok && n < total; ++n) {
-            const bool more = n + 1 < total;
-            if (!(ok = warp_wait(p_full, n & 1))) break;
-            tc_fence_after();
-            if (lane == 0) product_cols<64>(t_dv, t_s, item(2 * n + 1), id_o, n > 0);
-            release(2 * n + 1);
-            if (more) {
-                if (!(ok = wait_item(2 * n + 2))) break;
-                fix(2 * n + 2);
-                scores(n + 1);
-            }
-            if (!(ok = warp_wait(ds_full, n & 1))) break;
-            tc_fence_after();
-            if (lane == 0) product_cols<64>(t_dk, t_dp, item(2 * n), id_o, n > 0);
-            release(2 * n);
-            if (more) {
-                if (!(ok = wait_item(2 * n + 3))) break;
-                fix(2 * n + 3);
-                d_probs(n + 1);
-            } else if (lane == 0) {
-                mma_commit(done);
-            }
+        } else {   // ------------------------------------------------ jobs
+            ok = jobs.template run<kTile, false>(a, lots);
         }
     } else {   // ---------------------- a key row, half of the query columns
+        registers_up<C::kRowRegs>();
         const uint32_t half = warp >> 2, lanes = (warp & 3) << 21, col0 = half * 64;
         const uint32_t local = (warp & 3) * 32 + lane;
         const float2 c2 = make_float2(a.exp2_scale, a.exp2_scale);
-        for (uint32_t n = 0; n < total; ++n) {
-            const uint32_t slot = n % C::kRowSlots, i = s.block + n % q_tiles;
-            const uint32_t lo = i == s.block ? local : 0u, hi = min(uint32_t(kTile), s.len - i * kTile);
-            const bool whole = i != s.block && hi == kTile;   // every query of the tile sees every key of this one
-            const uint32_t terms = srows + slot * 1024 + col0 * 4;
-            if (!(ok = warp_wait(rows_full + 8 * slot, (n / C::kRowSlots) & 1))) break;
-            if (!(ok = warp_wait(s_full, n & 1))) break;
-            tc_fence_after();
-            float p[64];
-            {
-                uint32_t r[2][32];
-                tmem_ld32(r[0], t_s + lanes + col0);
-                tmem_ld32(r[1], t_s + lanes + col0 + 32);
-                tmem_wait_ld();
-#pragma unroll
-                for (int u = 0; u < 64; u += 4) {
-                    float4 l;
-                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l.x), "=f"(l.y), "=f"(l.z), "=f"(l.w) : "r"(terms + u * 4));
-                    const uint32_t *w = &r[u / 32][u % 32];
-                    const float2 x = fma2(make_float2(__uint_as_float(w[0]), __uint_as_float(w[1])), c2, make_float2(l.x, l.y));
-                    const float2 y = fma2(make_float2(__uint_as_float(w[2]), __uint_as_float(w[3])), c2, make_float2(l.z, l.w));
-                    p[u] = exp2_approx(x.x);
-                    p[u + 1] = exp2_approx(x.y);
-                    p[u + 2] = exp2_approx(y.x);
-                    p[u + 3] = exp2_approx(y.y);
-                }
-                if (!whole) {
-#pragma unroll
-                    for (int u = 0; u < 64; ++u)
-                        if (col0 + u < lo || col0 + u >= hi) p[u] = 0.f;
-                }
-#pragma unroll
-                for (int u = 0; u < 32; ++u) r[0][u] = bf16x2(p[2 * u], p[2 * u + 1]);
-                tmem_st32(t_s + lanes + col0, r[0]);
+        uint32_t it = 0, tiles = 0;
+        for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+            const uint32_t kv_head = kv_head_of(w), part = w.head / a.kv_heads;
+            if (w.kind == kJobTail && part == 0) {
+                const uint32_t from = w.first + w.block * kTile, to = min(w.first + w.len, from + kTile);
+                fill_rows(a.d_k, from, to, kv_head, a.head_dim, kZeroBits, 256);
+                fill_rows(a.d_v, from, to, kv_head, a.head_dim, kZeroBits, 256);
             }
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full);
-            if (!(ok = warp_wait(dp_full, n & 1))) break;
-            tc_fence_after();
-            {
-                uint32_t r[2][32];
-                tmem_ld32(r[0], t_dp + lanes + col0);
-                tmem_ld32(r[1], t_dp + lanes + col0 + 32);
-                tmem_wait_ld();
+            if (w.kind != kJobWork) continue;
+            const uint32_t q_tiles = q_tiles_of(w), total = q_tiles * heads, last = (w.len % kTile) ? w.len % kTile : kTile;
+            uint32_t tile = 0;   // query tiles behind the diagonal one, of the current head
+            for (uint32_t u = 0; u < total; ++u, ++it) {
+                const uint32_t slot = it % C::kRowSlots;
+                const uint32_t lo = tile == 0 ? local : 0u, hi = tile + 1 == q_tiles ? last : uint32_t(kTile);
+                const bool whole = tile != 0 && hi == kTile;   // every query of the tile sees every key of this one
+                if (++tile == q_tiles) tile = 0;
+                const uint32_t terms = srows + slot * 1024 + col0 * 4;
+                if (!(ok = warp_wait(rows_full + 8 * slot, (it / C::kRowSlots) & 1))) break;
+                if (!(ok = warp_wait(s_full, it & 1))) break;
+                tc_fence_after();
+                float p[64];
+                {
+                    uint32_t r[2][32];
+                    tmem_ld32(r[0], t_s + lanes + col0);
+                    tmem_ld32(r[1], t_s + lanes + col0 + 32);
+                    tmem_wait_ld();
 #pragma unroll
-                for (int u = 0; u < 64; u += 4) {
-                    float4 d;
-                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(d.x), "=f"(d.y), "=f"(d.z), "=f"(d.w) : "r"(terms + 512 + u * 4));
-                    const uint32_t *w = &r[u / 32][u % 32];
-                    p[u] *= __uint_as_float(w[0]) - d.x;
-                    p[u + 1] *= __uint_as_float(w[1]) - d.y;
-                    p[u + 2] *= __uint_as_float(w[2]) - d.z;
-                    p[u + 3] *= __uint_as_float(w[3]) - d.w;
-                }
-                if (!whole) {
-#pragma unroll
-                    for (int u = 0; u < 64; ++u)
-                        if (col0 + u < lo || col0 + u >= hi) p[u] = 0.f;
-                }
-#pragma unroll
-                for (int u = 0; u < 32; ++u) r[0][u] = bf16x2(p[2 * u], p[2 * u + 1]);
-                tmem_st32(t_dp + lanes + col0, r[0]);
-            }
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(ds_full);
-                mbar_arrive(rows_empty + 8 * slot);
-            }
-        }
-        if (ok) ok = warp_wait(done, 0);
-        if (ok) {   // the first half of the threads writes dV, the second dK
-            tc_fence_after();
-            const uint32_t row = row0 + local;
-            const bool mine = row < s.len;
-            const float f = half ? a.scale : 1.0f;
-            const RowsOut &o = half ? a.d_k : a.d_v;
-            char *out = o.p + (long long)(s.first + row) * o.token + (long long)kv_head * o.head;
-            float *sums = a.part_sums + (((size_t(part) * 2 + (1 - half)) * a.n_tokens + s.first + row) * a.kv_heads + kv_head) * a.head_dim;
-#pragma unroll
-            for (int i = 0; i < DP / 32; ++i) {
-                uint32_t w[32];
-                tmem_ld32(w, (half ? t_dk : t_dv) + lanes + 32 * i);
-                tmem_wait_ld();
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const float *x = reinterpret_cast<const float *>(w + 8 * u);
-                    if (!mine || 32 * i + 8 * u >= int(a.head_dim)) continue;
-                    if (a.parts > 1) {
-                        float4 *to = reinterpret_cast<float4 *>(sums + 32 * i + 8 * u);
-                        to[0] = make_float4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
-                        to[1] = make_float4(x[4] * f, x[5] * f, x[6] * f, x[7] * f);
-                    } else {
-                        *reinterpret_cast<uint4 *>(out + (32 * i + 8 * u) * 2) =
-                            make_uint4(bf16x2(x[0] * f, x[1] * f), bf16x2(x[2] * f, x[3] * f), bf16x2(x[4] * f, x[5] * f),
-                                       bf16x2(x[6] * f, x[7] * f));
+                    for (int x = 0; x < 64; x += 4) {
+                        float4 l;
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(l.x), "=f"(l.y), "=f"(l.z), "=f"(l.w) : "r"(terms + x * 4));
+                        const uint32_t *v = &r[x / 32][x % 32];
+                        const float2 y = fma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), c2, make_float2(l.x, l.y));
+                        const float2 z = fma2(make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])), c2, make_float2(l.z, l.w));
+                        p[x] = exp2_approx(y.x);
+                        p[x + 1] = exp2_approx(y.y);
+                        p[x + 2] = exp2_approx(z.x);
+                        p[x + 3] = exp2_approx(z.y);
                     }
+                    if (!whole) {
+#pragma unroll
+                        for (int x = 0; x < 64; ++x)
+                            if (col0 + x < lo || col0 + x >= hi) p[x] = 0.f;
+                    }
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) r[0][x] = bf16x2(p[2 * x], p[2 * x + 1]);
+                    tmem_st32(t_s + lanes + col0, r[0]);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full);
+                if (!(ok = warp_wait(dp_full, it & 1))) break;
+                tc_fence_after();
+                {
+                    uint32_t r[2][32];
+                    tmem_ld32(r[0], t_dp + lanes + col0);
+                    tmem_ld32(r[1], t_dp + lanes + col0 + 32);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int x = 0; x < 64; x += 4) {
+                        float4 d;
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(d.x), "=f"(d.y), "=f"(d.z), "=f"(d.w) : "r"(terms + 512 + x * 4));
+                        const uint32_t *v = &r[x / 32][x % 32];
+                        p[x] *= __uint_as_float(v[0]) - d.x;
+                        p[x + 1] *= __uint_as_float(v[1]) - d.y;
+                        p[x + 2] *= __uint_as_float(v[2]) - d.z;
+                        p[x + 3] *= __uint_as_float(v[3]) - d.w;
+                    }
+                    if (!whole) {
+#pragma unroll
+                        for (int x = 0; x < 64; ++x)
+                            if (col0 + x < lo || col0 + x >= hi) p[x] = 0.f;
+                    }
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) r[0][x] = bf16x2(p[2 * x], p[2 * x + 1]);
+                    tmem_st32(t_dp + lanes + col0, r[0]);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(ds_full);
+                    mbar_arrive(rows_empty + 8 * slot);
                 }
             }
+            if (!ok || !(ok = warp_wait(done, tiles & 1))) break;
+            ++tiles;
+            tc_fence_after();
+            // the first half of the threads writes dV, the second dK
+            const uint32_t row_w = w.block * kTile + local - lane, rows = w.len > row_w ? w.len - row_w : 0u;
+            const float f = half ? a.scale : 1.0f;
+            const uint32_t acc = (half ? t_dk : t_dv) + lanes;
+            if (a.parts > 1)
+                store_rows_f32<DP>(stage + warp * C::kStageBytes, acc, f,
+                                   a.part_sums + (((size_t(part) * 2 + (1 - half)) * a.n_tokens + w.first + row_w) * a.kv_heads + kv_head) * a.head_dim,
+                                   size_t(a.kv_heads) * a.head_dim, rows, a.head_dim);
+            else
+                store_rows<DP, 32>(stage + warp * C::kStageBytes, acc, f, half ? a.d_k : a.d_v, w.first + row_w, kv_head, rows, a.head_dim);
+            tc_fence_before();
         }
     }
     tc_fence_before();
@@ -864,14 +930,19 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     tc_fence_after();
     if (warp == 8) tmem_free(tmem, 512);
     if (bad) {
-        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
-        fill_rows(a.d_k, from, to, kv_head, a.head_dim, kNanBits, blockDim.x);
-        fill_rows(a.d_v, from, to, kv_head, a.head_dim, kNanBits, blockDim.x);
-        if (a.parts > 1)
-            for (uint32_t which = 0; which < 2; ++which)
-                for (uint32_t i = threadIdx.x; i < (to - from) * a.head_dim; i += blockDim.x)
-                    a.part_sums[(((size_t(part) * 2 + which) * a.n_tokens + from + i / a.head_dim) * a.kv_heads + kv_head) * a.head_dim +
-                                i % a.head_dim] = __int_as_float(0x7FFFFFFF);
+        if (w.kind == kJobWork) {   // each warp's own last job
+            const uint32_t from = w.first + w.block * kTile, to = min(w.first + w.len, from + kTile);
+            const uint32_t kv_head = kv_head_of(w), part = w.head / a.kv_heads;
+            if (a.parts > 1)
+                for (uint32_t which = 0; which < 2; ++which)
+                    for (uint32_t i = lane; i < (to - from) * a.head_dim; i += 32)
+                        a.part_sums[(((size_t(part) * 2 + which) * a.n_tokens + from + i / a.head_dim) * a.kv_heads + kv_head) * a.head_dim +
+                                    i % a.head_dim] = __int_as_float(0x7FFFFFFF);
+            else {
+                poison_rows(a.d_k, from, to, kv_head, a.head_dim);
+                poison_rows(a.d_v, from, to, kv_head, a.head_dim);
+            }
+        }
         if (threadIdx.x == 0) g_attn_fault = 1;
     }
 }
@@ -900,14 +971,15 @@ static __global__ void __launch_bounds__(256) attn_sum_parts_kernel(const __grid
 
 // One CTA: one query tile of a head over the key tiles up to the diagonal.  S is double-buffered, so that the
 // products run ahead: dQ, the next dP and the S after that are issued while the threads work on one tile.
-// Warps: 0-3 and 4-7 take the two halves of the key columns, 8 issues the products, 9 the TMA loads.
+// Warps: 0-3 and 4-7 take the two halves of the key columns, 8 issues the products, 9 the TMA loads, 10 finds the jobs.
 template <int DP>
 struct BwdQ {
     static constexpr int kSub = DP / 64;
     static constexpr int kBytes = kTile * DP * 2;
-    static constexpr int kStages = DP == 128 ? 5 : 8;
-    static constexpr int kThreads = 320;
-    static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + 256;
+    static constexpr int kKeys = DP == 128 ? 3 : 5, kValues = DP == 128 ? 1 : 3, kStages = kKeys + kValues;   // tiles in flight
+    static constexpr int kStageBytes = 2048;   // per warp, on the way out
+    static constexpr int kThreads = 384;
+    static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + 8 * kStageBytes + 512;
 };
 
 template <int DP>
@@ -916,26 +988,23 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ AttnDev a) {
     using C = BwdQ<DP>;
     extern __shared__ char smem_raw[];
-    const uint32_t head = blockIdx.x % a.q_heads, kv_head = head / (a.q_heads / a.kv_heads);
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Job s = find_job<kTile, true>(a, blockIdx.x / a.q_heads, gridDim.x / a.q_heads);
-    if (s.none) return;
-    const uint32_t row0 = s.block * kTile;
-    if (s.tail) {
-        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
-        fill_rows(a.d_q, from, to, head, a.head_dim, kZeroBits, blockDim.x);
-        return;
-    }
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = a.q_heads / a.kv_heads;
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t sq = base, sdo = base + C::kBytes, sring = base + 2 * C::kBytes;
-    const uint32_t bars = sring + C::kStages * C::kBytes;
-    const uint32_t q_full = bars, s_full = bars + 8, dp_full = bars + 24, ds_full = bars + 32, done = bars + 40, full = bars + 48,
-                   empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
-    const uint32_t total = s.block + 1;
+    const uint32_t stage = sring + C::kStages * C::kBytes, bars = stage + 8 * C::kStageBytes;
+    const Jobs jobs(bars);
+    const uint32_t q_full = bars + Jobs::kBytes, q_empty = q_full + 8, s_full = q_full + 16, dp_full = q_full + 32, ds_full = q_full + 40,
+                   done = q_full + 48, full = q_full + 56, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
+    // A key tile is used by S and, two tiles later, by dQ; a value tile by dP alone: the first kKeys places of the
+    // ring take key tiles, the others value tiles, each in turn.
+    auto k_at = [](uint32_t n) { return n % C::kKeys; };
+    auto v_at = [](uint32_t n) { return C::kKeys + n % C::kValues; };
 
     if (warp == 8) tmem_alloc(tmem_slot, 512);
     if (threadIdx.x == 0) {
+        jobs.init(10);
         mbar_init(q_full, 1);
+        mbar_init(q_empty, 1);
         mbar_init(s_full, 1);
         mbar_init(s_full + 8, 1);
         mbar_init(dp_full, 1);
@@ -954,142 +1023,182 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
     const uint32_t t_dp = tmem + 256, t_dq = tmem + 384;
     bool ok = true;
+    JobWord w;
+    w.kind = kJobNone;
 
     if (warp == 9) {   // ------------------------------------------------ loads
-        if (lane == 0) {
-            mbar_expect(q_full, 2 * C::kBytes);
-            for (int x = 0; x < C::kSub; ++x) {
-                tma_load(sq + x * (kTile * 128), &mq, q_full, x * 64, int(head) * a.q_mul, int(s.first + row0));
-                tma_load(sdo + x * (kTile * 128), &mdo, q_full, x * 64, int(head) * a.do_mul, int(s.first + row0));
+        uint32_t n = 0, tiles = 0;
+        for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+            if (w.kind != kJobWork) continue;
+            const uint32_t kv_head = w.head / group;
+            if (tiles > 0 && !(ok = warp_wait(q_empty, (tiles - 1) & 1))) break;
+            ++tiles;
+            if (lane == 0) {
+                mbar_expect(q_full, 2 * C::kBytes);
+                for (int x = 0; x < C::kSub; ++x) {
+                    tma_load(sq + x * (kTile * 128), &mq, q_full, x * 64, int(w.head) * a.q_mul, int(w.first + w.block * kTile));
+                    tma_load(sdo + x * (kTile * 128), &mdo, q_full, x * 64, int(w.head) * a.do_mul, int(w.first + w.block * kTile));
+                }
             }
-            uint32_t n = 0;
-            for (; n < 2 * total; ++n) {   // K, V, K, V, ...
-                const uint32_t st = n % C::kStages, use = n / C::kStages;
-                if (use > 0 && !(ok = mbar_wait(empty + 8 * st, (use - 1) & 1))) break;
-                const bool is_k = (n & 1) == 0;
-                mbar_expect(full + 8 * st, C::kBytes);
-                for (int x = 0; x < C::kSub; ++x)
-                    tma_load(sring + st * C::kBytes + x * (kTile * 128), is_k ? &mk : &mv, full + 8 * st, x * 64,
-                             int(kv_head) * (is_k ? a.k_mul : a.v_mul), int(s.first + (n / 2) * kTile));
+            const uint32_t total = w.block + 1;
+            auto load = [&](bool is_k, uint32_t u) {   // key or value tile u of the job
+                const uint32_t m = n + u, at = is_k ? k_at(m) : v_at(m), use = m / (is_k ? C::kKeys : C::kValues);
+                if (use > 0 && !warp_wait(empty + 8 * at, (use - 1) & 1)) return false;
+                if (lane == 0) {
+                    mbar_expect(full + 8 * at, C::kBytes);
+                    for (int x = 0; x < C::kSub; ++x)
+                        tma_load(sring + at * C::kBytes + x * (kTile * 128), is_k ? &mk : &mv, full + 8 * at, x * 64,
+                                 int(kv_head) * (is_k ? a.k_mul : a.v_mul), int(w.first + u * kTile));
+                }
+                return true;
+            };
+            ok = load(true, 0);
+            for (uint32_t u = 0; ok && u < total; ++u) {   // K0, V0, K1, K2, V1, K3, V2, ...: in the order of their use
+                ok = load(false, u);
+                if (ok && u == 0 && total > 1) ok = load(true, 1);
+                if (ok && u + 2 < total) ok = load(true, u + 2);
             }
-            if (!ok)
-                for (uint32_t i = n > C::kStages ? n - C::kStages : 0; i < n; ++i)
-                    mbar_wait(full + 8 * (i % C::kStages), (i / C::kStages) & 1);
+            if (!ok) break;
+            n += total;
+        }
+        if (tiles > 0) {
+            mbar_wait(q_full, (tiles - 1) & 1);
+            if (ok) ok = warp_wait(q_empty, (tiles - 1) & 1);
+        }
+        for (uint32_t i = n > C::kKeys ? n - C::kKeys : 0; i < n; ++i) {
+            mbar_wait(full + 8 * k_at(i), (i / C::kKeys) & 1);
+            if (ok) ok = warp_wait(empty + 8 * k_at(i), (i / C::kKeys) & 1);
+        }
+        for (uint32_t i = n > C::kValues ? n - C::kValues : 0; i < n; ++i) {
+            mbar_wait(full + 8 * v_at(i), (i / C::kValues) & 1);
+            if (ok) ok = warp_wait(empty + 8 * v_at(i), (i / C::kValues) & 1);
         }
     } else if (warp == 8) {   // ------------------------------------- products
         const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
-        auto item = [&](uint32_t n) { return sring + (n % C::kStages) * C::kBytes; };
-        auto wait_item = [&](uint32_t n) { return warp_wait(full + 8 * (n % C::kStages), (n / C::kStages) & 1); };
-        auto release = [&](uint32_t n) {
-            if (lane == 0 && n + C::kStages < 2 * total) mma_commit(empty + 8 * (n % C::kStages));
+        uint32_t tiles = 0, it = 0;   // jobs, key tiles so far
+        auto place = [&](uint32_t at) { return sring + at * C::kBytes; };
+        auto wait_k = [&](uint32_t n) { return warp_wait(full + 8 * k_at(n), (n / C::kKeys) & 1); };
+        auto wait_v = [&](uint32_t n) { return warp_wait(full + 8 * v_at(n), (n / C::kValues) & 1); };
+        auto release = [&](uint32_t at) {
+            if (lane == 0) mma_commit(empty + 8 * at);
         };
-        auto scores = [&](uint32_t n) {
-            if (s.len < (n + 1) * kTile) zero_tile_rows<C::kSub>(item(2 * n), s.len - n * kTile);   // dS there is zero
-            if (lane == 0) {
-                product_rows<DP>(tmem + (n & 1) * 128, sq, item(2 * n), id_s | a.negate);
-                mma_commit(s_full + 8 * (n & 1));
-            }
-        };
-        auto d_probs = [&](uint32_t n) {
-            if (lane == 0) {
-                product_rows<DP>(t_dp, sdo, item(2 * n + 1), id_s);
-                mma_commit(dp_full);
-            }
-            release(2 * n + 1);
-        };
-        ok = warp_wait(q_full, 0) && wait_item(0) && wait_item(1);
-        if (ok) {
+        for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+            if (w.kind != kJobWork) continue;
+            const uint32_t total = w.block + 1, n0 = it;
+            auto scores = [&](uint32_t u) {
+                const uint32_t key = place(k_at(n0 + u));
+                if (w.len < (u + 1) * kTile) zero_tile_rows<C::kSub>(key, w.len - u * kTile);   // dS there is zero
+                if (lane == 0) {
+                    product_rows<DP>(tmem + ((n0 + u) & 1) * 128, sq, key, id_s | a.negate);
+                    mma_commit(s_full + 8 * ((n0 + u) & 1));
+                }
+            };
+            auto d_probs = [&](uint32_t u) {
+                if (lane == 0) {
+                    product_rows<DP>(t_dp, sdo, place(v_at(n0 + u)), id_s);
+                    mma_commit(dp_full);
+                    if (u + 1 == total) mma_commit(q_empty);   // the last use of Q (its last product came before) and dO
+                }
+                release(v_at(n0 + u));
+            };
+            if (!(ok = warp_wait(q_full, tiles & 1) && wait_k(n0))) break;
+            ++tiles;
             tc_fence_after();
             scores(0);
+            if (!(ok = wait_v(n0))) break;
             d_probs(0);
-            if (total > 1 && (ok = wait_item(2))) scores(1);
-        }
-        for (uint32_t n = 0; ok && n < total; ++n) {
-            if (!(ok = warp_wait(ds_full, n & 1))) break;
-            tc_fence_after();
-            if (lane == 0) product_cols<64>(t_dq, t_dp, item(2 * n), id_o, n > 0);
-            release(2 * n);
-            if (n + 1 < total) {
-                if (!(ok = wait_item(2 * n + 3))) break;
-                d_probs(n + 1);
-            } else if (lane == 0) {
-                mma_commit(done);
+            if (total > 1) {
+                if (!(ok = wait_k(n0 + 1))) break;
+                scores(1);
             }
-            if (n + 2 < total) {
-                if (!(ok = wait_item(2 * n + 4))) break;
-                scores(n + 2);
+            for (uint32_t u = 0; u < total; ++u, ++it) {
+                if (!(ok = warp_wait(ds_full, it & 1))) break;
+                tc_fence_after();
+                if (lane == 0) product_cols<64>(t_dq, t_dp, place(k_at(n0 + u)), id_o, u > 0);
+                release(k_at(n0 + u));
+                if (u + 1 < total) {
+                    if (!(ok = wait_v(n0 + u + 1))) break;
+                    d_probs(u + 1);
+                } else if (lane == 0) {
+                    mma_commit(done);
+                }
+                if (u + 2 < total) {
+                    if (!(ok = wait_k(n0 + u + 2))) break;
+                    scores(u + 2);
+                }
             }
+            if (!ok) break;
         }
-    } else {   // ---------------------- a query row, half of the key columns
+    } else if (warp == 10) {   // ---------------------------------------- jobs
+        ok = jobs.template run<kTile, true>(a, a.q_heads);
+    } else if (warp < 8) {   // -------- a query row, half of the key columns
         const uint32_t half = warp >> 2, lanes = (warp & 3) << 21, col0 = half * 64;
-        const uint32_t local = (warp & 3) * 32 + lane, row = row0 + local;
-        const bool mine = row < s.len;
-        const float2 term = mine ? __ldg(a.rows + size_t(head) * a.n_tokens + s.first + row) : make_float2(0.f, 0.f);
-        const float2 c2 = make_float2(a.exp2_scale, a.exp2_scale), l2 = make_float2(term.x, term.x), d2 = make_float2(-term.y, -term.y);
-        for (uint32_t n = 0; n < total; ++n) {
-            if (!(ok = warp_wait(s_full + 8 * (n & 1), (n >> 1) & 1))) break;
-            tc_fence_after();
-            float2 p[32];
-            {
-                uint32_t r[2][32];
-                tmem_ld32(r[0], tmem + (n & 1) * 128 + lanes + col0);
-                tmem_ld32(r[1], tmem + (n & 1) * 128 + lanes + col0 + 32);
-                tmem_wait_ld();
-#pragma unroll
-                for (int u = 0; u < 32; ++u) {
-                    const uint32_t *w = &r[u / 16][2 * (u % 16)];
-                    const float2 x = fma2(make_float2(__uint_as_float(w[0]), __uint_as_float(w[1])), c2, l2);
-                    p[u] = make_float2(exp2_approx(x.x), exp2_approx(x.y));
-                }
+        const uint32_t local = (warp & 3) * 32 + lane;
+        const float2 c2 = make_float2(a.exp2_scale, a.exp2_scale);
+        uint32_t it = 0, tiles = 0;
+        for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+            if (w.kind == kJobTail) {
+                const uint32_t from = w.first + w.block * kTile, to = min(w.first + w.len, from + kTile);
+                fill_rows(a.d_q, from, to, w.head, a.head_dim, kZeroBits, 256);
             }
-            if (!(ok = warp_wait(dp_full, n & 1))) break;
-            tc_fence_after();
-            {
-                uint32_t r[2][32];
-                tmem_ld32(r[0], t_dp + lanes + col0);
-                tmem_ld32(r[1], t_dp + lanes + col0 + 32);
-                tmem_wait_ld();
+            if (w.kind != kJobWork) continue;
+            const uint32_t total = w.block + 1, row = w.block * kTile + local;
+            const float2 term = row < w.len ? __ldg(a.rows + size_t(w.head) * a.n_tokens + w.first + row) : make_float2(0.f, 0.f);
+            const float2 l2 = make_float2(term.x, term.x), d2 = make_float2(-term.y, -term.y);
+            for (uint32_t u = 0; u < total; ++u, ++it) {
+                if (!(ok = warp_wait(s_full + 8 * (it & 1), (it >> 1) & 1))) break;
+                tc_fence_after();
+                float2 p[32];
+                {
+                    uint32_t r[2][32];
+                    tmem_ld32(r[0], tmem + (it & 1) * 128 + lanes + col0);
+                    tmem_ld32(r[1], tmem + (it & 1) * 128 + lanes + col0 + 32);
+                    tmem_wait_ld();
 #pragma unroll
-                for (int u = 0; u < 32; ++u) {
-                    const uint32_t *w = &r[u / 16][2 * (u % 16)];
-                    p[u] = mul2(p[u], add2(make_float2(__uint_as_float(w[0]), __uint_as_float(w[1])), d2));
-                }
-                if (n == total - 1) {   // the diagonal tile
-#pragma unroll
-                    for (int u = 0; u < 32; ++u) {
-                        if (col0 + 2 * u > local) p[u].x = 0.f;
-                        if (col0 + 2 * u + 1 > local) p[u].y = 0.f;
+                    for (int x = 0; x < 32; ++x) {
+                        const uint32_t *v = &r[x / 16][2 * (x % 16)];
+                        const float2 y = fma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), c2, l2);
+                        p[x] = make_float2(exp2_approx(y.x), exp2_approx(y.y));
                     }
                 }
+                if (!(ok = warp_wait(dp_full, it & 1))) break;
+                tc_fence_after();
+                {
+                    uint32_t r[2][32];
+                    tmem_ld32(r[0], t_dp + lanes + col0);
+                    tmem_ld32(r[1], t_dp + lanes + col0 + 32);
+                    tmem_wait_ld();
 #pragma unroll
-                for (int u = 0; u < 32; ++u) r[0][u] = bf16x2(p[u].x, p[u].y);
-                tmem_st32(t_dp + lanes + col0, r[0]);
-            }
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(ds_full);
-        }
-        if (ok) ok = warp_wait(done, 0);
-        if (ok) {   // each half writes half of the row
-            tc_fence_after();
-            char *out = a.d_q.p + (long long)(s.first + row) * a.d_q.token + (long long)head * a.d_q.head;
-            const float f = a.scale;
+                    for (int x = 0; x < 32; ++x) {
+                        const uint32_t *v = &r[x / 16][2 * (x % 16)];
+                        p[x] = mul2(p[x], add2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), d2));
+                    }
+                    if (u == total - 1) {   // the diagonal tile
 #pragma unroll
-            for (int i = 0; i < DP / 64; ++i) {
-                const uint32_t col = half * (DP / 2) + 32 * i;
-                uint32_t w[32];
-                tmem_ld32(w, t_dq + lanes + col);
-                tmem_wait_ld();
+                        for (int x = 0; x < 32; ++x) {
+                            if (col0 + 2 * x > local) p[x].x = 0.f;
+                            if (col0 + 2 * x + 1 > local) p[x].y = 0.f;
+                        }
+                    }
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const float *x = reinterpret_cast<const float *>(w + 8 * u);
-                    if (mine && col + 8 * u < a.head_dim)
-                        *reinterpret_cast<uint4 *>(out + (col + 8 * u) * 2) =
-                            make_uint4(bf16x2(x[0] * f, x[1] * f), bf16x2(x[2] * f, x[3] * f), bf16x2(x[4] * f, x[5] * f),
-                                       bf16x2(x[6] * f, x[7] * f));
+                    for (int x = 0; x < 32; ++x) r[0][x] = bf16x2(p[x].x, p[x].y);
+                    tmem_st32(t_dp + lanes + col0, r[0]);
                 }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(ds_full);
             }
+            if (!ok || !(ok = warp_wait(done, tiles & 1))) break;
+            ++tiles;
+            tc_fence_after();
+            // each half of the threads writes half of the columns
+            const uint32_t row_w = row - lane, col = half * (DP / 2);
+            RowsOut o = a.d_q;
+            o.p += col * 2;
+            store_rows<DP / 2, 32>(stage + warp * C::kStageBytes, t_dq + lanes + col, a.scale, o, w.first + row_w, w.head,
+                                   w.len > row_w ? w.len - row_w : 0u, a.head_dim > col ? a.head_dim - col : 0u);
+            tc_fence_before();
         }
     }
     tc_fence_before();
@@ -1097,8 +1206,10 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     tc_fence_after();
     if (warp == 8) tmem_free(tmem, 512);
     if (bad) {
-        const uint32_t from = s.first + row0, to = min(s.first + s.len, from + kTile);
-        fill_rows(a.d_q, from, to, head, a.head_dim, kNanBits, blockDim.x);
+        if (w.kind == kJobWork) {   // each warp's own last job
+            const uint32_t from = w.first + w.block * kTile;
+            poison_rows(a.d_q, from, min(w.first + w.len, from + kTile), w.head, a.head_dim);
+        }
         if (threadIdx.x == 0) g_attn_fault = 1;
     }
 }

@@ -187,6 +187,15 @@ struct Jobs {
             fence_async_shared();   // the answer has been read before the next one overwrites it
         }
     }
+    __device__ __forceinline__ bool get_alone(uint32_t k, JobWord *w) const {   // one thread
+        if (!mbar_wait(full, k & 1)) return false;
+        uint32_t last;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w->first), "=r"(w->len), "=r"(w->block), "=r"(last) : "r"(word) : "memory");
+        w->kind = last & 3u;
+        w->head = last >> 2;
+        mbar_arrive(empty);
+        return true;
+    }
     __device__ __forceinline__ bool get(uint32_t k, JobWord *w) const {         // whole warp
         if (!warp_wait(full, k & 1)) return false;
         uint32_t last;
@@ -196,6 +205,19 @@ struct Jobs {
         __syncwarp();
         if ((threadIdx.x & 31) == 0) mbar_arrive(empty);
         return true;
+    }
+};
+
+// A ring of tiles in shared memory, each with a barrier that its copy completes and one that says it may be overwritten.
+// One warp fills it; the thread that issues the products empties it.  Both walk it with a Place of their own.
+struct Place {
+    uint32_t at = 0, phase = 0;   // index and the parity of this round
+    template <uint32_t N>
+    __device__ __forceinline__ void next() {
+        if (++at == N) {
+            at = 0;
+            phase ^= 1;
+        }
     }
 };
 
@@ -220,8 +242,8 @@ __device__ __forceinline__ void poison_rows(const RowsOut &o, uint32_t from, uin
     }
 }
 
-// Zeroes rows [from, 128) of a tile in shared memory, by one warp, before the matrix unit reads it: rows behind the
-// sequence belong to others, and their zero weight does not cover a NaN.
+// Zeroes rows [from, 128) of a tile in shared memory, by the warp that loads it, before the matrix unit is told of it:
+// rows behind the sequence belong to others, and their zero weight does not cover a NaN.
 template <int SUB>
 __device__ __forceinline__ void zero_tile_rows(uint32_t tile, uint32_t from) {
     for (int x = 0; x < SUB; ++x)
@@ -354,13 +376,15 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     const uint32_t stage = sring + C::kStages * C::kBytes, bars = stage + 8 * C::kStageBytes;
     const Jobs jobs(bars);
     const uint32_t q_full = bars + Jobs::kBytes, q_empty = q_full + 8, s_full = q_full + 16, p_full = q_full + 32, o_full = q_full + 48,
-                   full = q_full + 64, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
+                   raw = q_full + 64, full = q_full + 72, empty = full + 8 * C::kStages,
+                   tmem_slot = empty + 8 * C::kStages;
 
     if (warp == 8) tmem_alloc(tmem_slot, 512);
     if (threadIdx.x == 0) {
         jobs.init(10);
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
+        mbar_init(raw, 1);
         for (int t = 0; t < 2; ++t) {
             mbar_init(s_full + 8 * t, 1);
             mbar_init(p_full + 8 * t, 4);
@@ -384,7 +408,8 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     if (warp >= 8) {
         registers_down<C::kOtherRegs>();
         if (warp == 9) {   // -------------------------------------------- loads
-            uint32_t n = 0, tiles = 0;   // ring items so far, jobs so far
+            uint32_t tiles = 0, fixed = 0, n = 0;   // jobs, tiles with rows of others, ring items so far
+            Place at;
             for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
                 if (w.kind != kJobWork) continue;
                 const uint32_t row0 = w.block * 2 * kTile, kv_head = w.head / group;
@@ -399,15 +424,21 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                             tma_load(sq + t * C::kBytes + x * (kTile * 128), &mq, q_full, x * 64, int(w.head) * a.q_mul,
                                      int(w.first + row0 + t * kTile));
                 }
-                for (uint32_t i = 0; i < items; ++i, ++n) {
-                    const uint32_t st = n % C::kStages, use = n / C::kStages;
-                    if (use > 0 && !(ok = warp_wait(empty + 8 * st, (use - 1) & 1))) break;
-                    const bool is_k = (i & 1) == 0;
+                for (uint32_t i = 0; i < items; ++i, ++n, at.template next<C::kStages>()) {   // K, V, K, V, ...
+                    if (n >= C::kStages && !(ok = warp_wait(empty + 8 * at.at, at.phase ^ 1))) break;
+                    const bool is_k = (i & 1) == 0, ragged = !is_k && w.len < (i / 2 + 1) * kTile;
+                    const uint32_t tile = sring + at.at * C::kBytes, bar = ragged ? raw : full + 8 * at.at;
                     if (lane == 0) {
-                        mbar_expect(full + 8 * st, C::kBytes);
+                        mbar_expect(bar, C::kBytes);
                         for (int x = 0; x < C::kSub; ++x)
-                            tma_load(sring + st * C::kBytes + x * (kTile * 128), is_k ? &mk : &mv, full + 8 * st, x * 64,
-                                     int(kv_head) * (is_k ? a.k_mul : a.v_mul), int(w.first + (i / 2) * kTile));
+                            tma_load(tile + x * (kTile * 128), is_k ? &mk : &mv, bar, x * 64, int(kv_head) * (is_k ? a.k_mul : a.v_mul),
+                                     int(w.first + (i / 2) * kTile));
+                    }
+                    if (ragged) {
+                        if (!(ok = warp_wait(raw, fixed & 1))) break;
+                        ++fixed;
+                        zero_tile_rows<C::kSub>(tile, w.len - (i / 2) * kTile);
+                        if (lane == 0) mbar_arrive(full + 8 * at.at);
                     }
                 }
                 if (!ok) break;
@@ -422,61 +453,68 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 if (ok) ok = warp_wait(empty + 8 * (i % C::kStages), (i / C::kStages) & 1);
             }
         } else if (warp == 8) {   // --------------------------------- products
-            const uint32_t id_s = mma_desc(kTile, false) | a.negate, id_o = mma_desc(DP, true);
-            uint32_t n0 = 0, tiles = 0, done[2] = {0, 0};   // first ring item of the job; jobs, row blocks so far
-            auto item = [&](uint32_t n) { return sring + (n % C::kStages) * C::kBytes; };
-            auto wait_item = [&](uint32_t n) { return warp_wait(full + 8 * (n % C::kStages), (n / C::kStages) & 1); };
-            auto release = [&](uint32_t n) {
-                if (lane == 0) mma_commit(empty + 8 * (n % C::kStages));
-            };
-            for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
-                if (w.kind != kJobWork) continue;
-                const bool two = w.block * 2 * kTile + kTile < w.len;
-                const uint32_t nb0 = w.block * 2 + 1, nb = nb0 + (two ? 1 : 0);   // key tiles of the first tile; of both
-                auto scores = [&](int t, uint32_t j) {   // S_t = Q_t K_j^T
-                    if (lane == 0) {
-                        product_rows<DP>(tmem + t * 128, sq + t * C::kBytes, item(n0 + 2 * j), id_s);
-                        mma_commit(s_full + 8 * t);
-                    }
+            // One thread: between two batches of products the tensor cores hold about one product's work, so every
+            // cycle spent here in between is one that they may lose.
+            if (lane == 0) {
+                const uint32_t id_s = mma_desc(kTile, false) | a.negate, id_o = mma_desc(DP, true);
+                uint32_t tiles = 0, done0 = 0, done1 = 0;   // jobs, blocks of the first and second tile so far
+                Place at;   // of the oldest ring item not yet released
+                auto tile_of = [&](const Place &p) { return sring + p.at * C::kBytes; };
+                auto wait_tile = [&](const Place &p) { return mbar_wait(full + 8 * p.at, p.phase); };
+                auto release = [&]() {
+                    mma_commit(empty + 8 * at.at);
+                    at.template next<C::kStages>();
                 };
-                auto values = [&](int t, uint32_t j) {   // O_t += P_t V_j
-                    if (lane == 0) {
-                        product_cols<32>(tmem + 256 + t * 128, tmem + t * 128, item(n0 + 2 * j + 1), id_o, j > 0);
-                        mma_commit(o_full + 8 * t);
-                    }
-                    ++done[t];
-                };
-                if (!(ok = warp_wait(q_full, tiles & 1) && wait_item(n0))) break;
-                ++tiles;
-                tc_fence_after();
-                scores(0, 0);
-                if (two) scores(1, 0);
-                release(n0);
-                if (nb == 1 && lane == 0) mma_commit(q_empty);
-                for (uint32_t j = 0; j < nb; ++j) {
-                    if (!(ok = wait_item(n0 + 2 * j + 1))) break;
-                    if (j + 1 < nb && !(ok = wait_item(n0 + 2 * j + 2))) break;
-                    if (j == nb - 1 && w.len < nb * kTile) zero_tile_rows<C::kSub>(item(n0 + 2 * j + 1), w.len - j * kTile);
-                    if (j < nb0) {
-                        if (!(ok = warp_wait(p_full, done[0] & 1))) break;
-                        tc_fence_after();
-                        values(0, j);
-                        if (j + 1 < nb0) scores(0, j + 1);
-                    }
+                for (uint32_t k = 0; (ok = jobs.get_alone(k, &w)) && w.kind != kJobStop; ++k) {
+                    if (w.kind != kJobWork) continue;
+                    const bool two = w.block * 2 * kTile + kTile < w.len;
+                    const uint32_t nb0 = w.block * 2 + 1, nb = nb0 + (two ? 1 : 0);   // key tiles of the first tile; of both
+                    if (!(ok = mbar_wait(q_full, tiles & 1) && wait_tile(at))) break;
+                    ++tiles;
+                    tc_fence_after();
+                    product_rows<DP>(tmem, sq, tile_of(at), id_s);   // S_0 = Q_0 K^T
+                    mma_commit(s_full);
                     if (two) {
-                        if (!(ok = warp_wait(p_full + 8, done[1] & 1))) break;
-                        tc_fence_after();
-                        values(1, j);
+                        product_rows<DP>(tmem + 128, sq + C::kBytes, tile_of(at), id_s);
+                        mma_commit(s_full + 8);
                     }
-                    release(n0 + 2 * j + 1);
-                    if (j + 1 < nb) {
-                        if (two) scores(1, j + 1);
-                        release(n0 + 2 * j + 2);
-                        if (j + 2 == nb && lane == 0) mma_commit(q_empty);   // the last use of Q
+                    release();
+                    if (nb == 1) mma_commit(q_empty);
+                    for (uint32_t j = 0; j < nb; ++j) {
+                        const Place v = at;
+                        Place key = at;
+                        key.template next<C::kStages>();
+                        if (!(ok = wait_tile(v) && (j + 1 == nb || wait_tile(key)))) break;
+                        if (j < nb0) {
+                            if (!(ok = mbar_wait(p_full, done0 & 1))) break;
+                            ++done0;
+                            tc_fence_after();
+                            product_cols<32>(tmem + 256, tmem, tile_of(v), id_o, j > 0);   // O_0 += P_0 V
+                            mma_commit(o_full);
+                            if (j + 1 < nb0) {
+                                product_rows<DP>(tmem, sq, tile_of(key), id_s);
+                                mma_commit(s_full);
+                            }
+                        }
+                        if (two) {
+                            if (!(ok = mbar_wait(p_full + 8, done1 & 1))) break;
+                            ++done1;
+                            tc_fence_after();
+                            product_cols<32>(tmem + 384, tmem + 128, tile_of(v), id_o, j > 0);
+                            mma_commit(o_full + 8);
+                            if (j + 1 < nb) {
+                                product_rows<DP>(tmem + 128, sq + C::kBytes, tile_of(key), id_s);
+                                mma_commit(s_full + 8);
+                            }
+                        }
+                        release();
+                        if (j + 1 < nb) {
+                            release();
+                            if (j + 2 == nb) mma_commit(q_empty);   // the last use of Q
+                        }
                     }
+                    if (!ok) break;
                 }
-                if (!ok) break;
-                n0 += 2 * nb;
             }
         } else if (warp == 10) {   // ------------------------------------ jobs
             ok = jobs.template run<2 * kTile, true>(a, a.q_heads);
@@ -644,7 +682,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     const uint32_t stage = srows + C::kRowSlots * 1024, bars = stage + 8 * C::kStageBytes;
     const Jobs jobs(bars);
     const uint32_t kv_full = bars + Jobs::kBytes, kv_empty = kv_full + 8, s_full = kv_full + 16, dp_full = kv_full + 24, p_full = kv_full + 32,
-                   ds_full = kv_full + 40, done = kv_full + 48, rows_full = kv_full + 56, rows_empty = rows_full + 8 * C::kRowSlots,
+                   ds_full = kv_full + 40, done = kv_full + 48, raw = kv_full + 56, rows_full = kv_full + 64, rows_empty = rows_full + 8 * C::kRowSlots,
                    full = rows_empty + 8 * C::kRowSlots, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
 
     if (warp == 8) tmem_alloc(tmem_slot, 512);
@@ -652,6 +690,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         jobs.init(11);
         mbar_init(kv_full, 1);
         mbar_init(kv_empty, 1);
+        mbar_init(raw, 1);
         mbar_init(s_full, 1);
         mbar_init(dp_full, 1);
         mbar_init(p_full, 8);
@@ -683,7 +722,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     if (warp >= 8) {
         registers_down<C::kOtherRegs>();
         if (warp == 9) {   // -------------------------------------------- loads
-            uint32_t n = 0, tiles = 0;
+            uint32_t tiles = 0, fixed = 0, n = 0;   // jobs, tiles with rows of others, ring items so far
+            Place at;
             for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
                 if (w.kind != kJobWork) continue;
                 if (tiles > 0 && !(ok = warp_wait(kv_empty, (tiles - 1) & 1))) break;
@@ -697,15 +737,21 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     }
                 }
                 uint32_t h = head0_of(w), i = w.block;
-                for (uint32_t u = 0; u < 2 * heads * q_tiles; ++u, ++n) {   // Q, dO, Q, dO, ...
-                    const uint32_t st = n % C::kStages, use = n / C::kStages;
-                    if (use > 0 && !(ok = warp_wait(empty + 8 * st, (use - 1) & 1))) break;
-                    const bool is_q = (u & 1) == 0;
+                for (uint32_t u = 0; u < 2 * heads * q_tiles; ++u, ++n, at.template next<C::kStages>()) {   // Q, dO, Q, dO, ...
+                    if (n >= C::kStages && !(ok = warp_wait(empty + 8 * at.at, at.phase ^ 1))) break;
+                    const bool is_q = (u & 1) == 0, ragged = w.len < (i + 1) * kTile;
+                    const uint32_t tile = sring + at.at * C::kBytes, bar = ragged ? raw : full + 8 * at.at;
                     if (lane == 0) {
-                        mbar_expect(full + 8 * st, C::kBytes);
+                        mbar_expect(bar, C::kBytes);
                         for (int x = 0; x < C::kSub; ++x)
-                            tma_load(sring + st * C::kBytes + x * (kTile * 128), is_q ? &mq : &mdo, full + 8 * st, x * 64,
-                                     int(h) * (is_q ? a.q_mul : a.do_mul), int(w.first + i * kTile));
+                            tma_load(tile + x * (kTile * 128), is_q ? &mq : &mdo, bar, x * 64, int(h) * (is_q ? a.q_mul : a.do_mul),
+                                     int(w.first + i * kTile));
+                    }
+                    if (ragged) {
+                        if (!(ok = warp_wait(raw, fixed & 1))) break;
+                        ++fixed;
+                        zero_tile_rows<C::kSub>(tile, w.len - i * kTile);
+                        if (lane == 0) mbar_arrive(full + 8 * at.at);
                     }
                     if (!is_q && ++i == w.block + q_tiles) {
                         i = w.block;
@@ -753,68 +799,58 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 if (!ok) break;
             }
         } else if (warp == 8) {   // --------------------------------- products
-            const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
-            uint32_t n0 = 0, tiles = 0, it = 0;   // first ring item of the job; jobs, query tiles so far
-            auto item = [&](uint32_t n) { return sring + (n % C::kStages) * C::kBytes; };
-            auto wait_item = [&](uint32_t n) { return warp_wait(full + 8 * (n % C::kStages), (n / C::kStages) & 1); };
-            auto release = [&](uint32_t n) {
-                if (lane == 0) mma_commit(empty + 8 * (n % C::kStages));
-            };
-            for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
-                if (w.kind != kJobWork) continue;
-                const uint32_t q_tiles = q_tiles_of(w), total = q_tiles * heads;
-                const bool ragged = w.len % kTile != 0;
-                uint32_t left = q_tiles;   // query tiles of this head from the one about to be made ready on
-                auto make_ready = [&](uint32_t u, bool last_of_tile) {   // item u of the job (Q and dO of query tile u / 2) is there
-                    if (left == 1 && ragged) zero_tile_rows<C::kSub>(item(n0 + u), w.len % kTile);
-                    if (last_of_tile && --left == 0) left = q_tiles;
-                };
-                auto scores = [&](uint32_t u) {
-                    if (lane == 0) {
-                        product_rows<DP>(t_s, sk, item(n0 + 2 * u), id_s | a.negate);
-                        mma_commit(s_full);
-                    }
-                };
-                auto d_probs = [&](uint32_t u) {
-                    if (lane == 0) {
-                        product_rows<DP>(t_dp, sv, item(n0 + 2 * u + 1), id_s);
-                        mma_commit(dp_full);
-                        if (u + 1 == total) mma_commit(kv_empty);   // the last use of K and V
-                    }
-                };
-                if (!(ok = warp_wait(kv_full, tiles & 1) && wait_item(n0))) break;
-                ++tiles;
-                tc_fence_after();
-                make_ready(0, false);
-                scores(0);
-                if (!(ok = wait_item(n0 + 1))) break;
-                make_ready(1, true);
-                d_probs(0);
-                for (uint32_t u = 0; u < total; ++u, ++it) {
-                    const bool more = u + 1 < total;
-                    if (!(ok = warp_wait(p_full, it & 1))) break;
+            if (lane == 0) {   // one thread, as in the forward kernel
+                const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
+                uint32_t tiles = 0, it = 0;   // jobs, query tiles so far
+                Place q;                      // Q of the query tile at hand; its dO is one place on
+                auto tile_of = [&](const Place &p) { return sring + p.at * C::kBytes; };
+                auto wait_tile = [&](const Place &p) { return mbar_wait(full + 8 * p.at, p.phase); };
+                for (uint32_t k = 0; (ok = jobs.get_alone(k, &w)) && w.kind != kJobStop; ++k) {
+                    if (w.kind != kJobWork) continue;
+                    const uint32_t total = q_tiles_of(w) * heads;
+                    Place g = q;
+                    g.template next<C::kStages>();
+                    if (!(ok = mbar_wait(kv_full, tiles & 1) && wait_tile(q))) break;
+                    ++tiles;
                     tc_fence_after();
-                    if (lane == 0) product_cols<64>(t_dv, t_s, item(n0 + 2 * u + 1), id_o, u > 0);
-                    release(n0 + 2 * u + 1);
-                    if (more) {
-                        if (!(ok = wait_item(n0 + 2 * u + 2))) break;
-                        make_ready(2 * u + 2, false);
-                        scores(u + 1);
+                    product_rows<DP>(t_s, sk, tile_of(q), id_s | a.negate);   // S^T = K Q^T
+                    mma_commit(s_full);
+                    if (!(ok = wait_tile(g))) break;
+                    product_rows<DP>(t_dp, sv, tile_of(g), id_s);             // dP^T = V dO^T
+                    mma_commit(dp_full);
+                    if (total == 1) mma_commit(kv_empty);
+                    for (uint32_t u = 0; u < total; ++u, ++it) {
+                        const bool more = u + 1 < total;
+                        Place q_next = g, g_next;
+                        q_next.template next<C::kStages>();
+                        g_next = q_next;
+                        g_next.template next<C::kStages>();
+                        if (more && !(ok = wait_tile(q_next))) break;
+                        if (!(ok = mbar_wait(p_full, it & 1))) break;
+                        tc_fence_after();
+                        product_cols<64>(t_dv, t_s, tile_of(g), id_o, u > 0);     // dV += P^T dO
+                        mma_commit(empty + 8 * g.at);
+                        if (more) {
+                            product_rows<DP>(t_s, sk, tile_of(q_next), id_s | a.negate);
+                            mma_commit(s_full);
+                            if (!(ok = wait_tile(g_next))) break;
+                        }
+                        if (!(ok = mbar_wait(ds_full, it & 1))) break;
+                        tc_fence_after();
+                        product_cols<64>(t_dk, t_dp, tile_of(q), id_o, u > 0);    // dK += dS^T Q
+                        mma_commit(empty + 8 * q.at);
+                        if (more) {
+                            product_rows<DP>(t_dp, sv, tile_of(g_next), id_s);
+                            mma_commit(dp_full);
+                            if (u + 2 == total) mma_commit(kv_empty);   // the last use of K and V
+                        } else {
+                            mma_commit(done);
+                        }
+                        q = q_next;
+                        g = g_next;
                     }
-                    if (!(ok = warp_wait(ds_full, it & 1))) break;
-                    tc_fence_after();
-                    if (lane == 0) product_cols<64>(t_dk, t_dp, item(n0 + 2 * u), id_o, u > 0);
-                    release(n0 + 2 * u);
-                    if (more) {
-                        if (!(ok = wait_item(n0 + 2 * u + 3))) break;
-                        make_ready(2 * u + 3, true);
-                        d_probs(u + 1);
-                    } else if (lane == 0) {
-                        mma_commit(done);
-                    }
+                    if (!ok) break;
                 }
-                if (!ok) break;
-                n0 += 2 * total;
             }
         } else {   // ------------------------------------------------ jobs
             ok = jobs.template run<kTile, false>(a, lots);
@@ -969,8 +1005,9 @@ static __global__ void __launch_bounds__(256) attn_sum_parts_kernel(const __grid
         make_uint4(bf16x2(s[0], s[1]), bf16x2(s[2], s[3]), bf16x2(s[4], s[5]), bf16x2(s[6], s[7]));
 }
 
-// One CTA: one query tile of a head over the key tiles up to the diagonal.  S is double-buffered, so that the
-// products run ahead: dQ, the next dP and the S after that are issued while the threads work on one tile.
+// One CTA: one query tile of a head over the key tiles up to the diagonal.  S is double-buffered and dS goes where S
+// was, so that the products run ahead: the next dP, dQ and the S after that are issued while the threads work on one
+// tile.
 // Warps: 0-3 and 4-7 take the two halves of the key columns, 8 issues the products, 9 the TMA loads, 10 finds the jobs.
 template <int DP>
 struct BwdQ {
@@ -994,17 +1031,15 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     const uint32_t stage = sring + C::kStages * C::kBytes, bars = stage + 8 * C::kStageBytes;
     const Jobs jobs(bars);
     const uint32_t q_full = bars + Jobs::kBytes, q_empty = q_full + 8, s_full = q_full + 16, dp_full = q_full + 32, ds_full = q_full + 40,
-                   done = q_full + 48, full = q_full + 56, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
+                   done = q_full + 48, raw = q_full + 56, full = q_full + 64, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
     // A key tile is used by S and, two tiles later, by dQ; a value tile by dP alone: the first kKeys places of the
     // ring take key tiles, the others value tiles, each in turn.
-    auto k_at = [](uint32_t n) { return n % C::kKeys; };
-    auto v_at = [](uint32_t n) { return C::kKeys + n % C::kValues; };
-
     if (warp == 8) tmem_alloc(tmem_slot, 512);
     if (threadIdx.x == 0) {
         jobs.init(10);
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
+        mbar_init(raw, 1);
         mbar_init(s_full, 1);
         mbar_init(s_full + 8, 1);
         mbar_init(dp_full, 1);
@@ -1027,10 +1062,10 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     w.kind = kJobNone;
 
     if (warp == 9) {   // ------------------------------------------------ loads
-        uint32_t n = 0, tiles = 0;
+        uint32_t n = 0, tiles = 0, fixed = 0;   // key tiles, jobs, tiles with rows of others so far
         for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
             if (w.kind != kJobWork) continue;
-            const uint32_t kv_head = w.head / group;
+            const uint32_t kv_head = w.head / group, total = w.block + 1;
             if (tiles > 0 && !(ok = warp_wait(q_empty, (tiles - 1) & 1))) break;
             ++tiles;
             if (lane == 0) {
@@ -1040,15 +1075,22 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     tma_load(sdo + x * (kTile * 128), &mdo, q_full, x * 64, int(w.head) * a.do_mul, int(w.first + w.block * kTile));
                 }
             }
-            const uint32_t total = w.block + 1;
             auto load = [&](bool is_k, uint32_t u) {   // key or value tile u of the job
-                const uint32_t m = n + u, at = is_k ? k_at(m) : v_at(m), use = m / (is_k ? C::kKeys : C::kValues);
+                const uint32_t m = n + u, at = is_k ? m % C::kKeys : C::kKeys + m % C::kValues, use = m / (is_k ? C::kKeys : C::kValues);
                 if (use > 0 && !warp_wait(empty + 8 * at, (use - 1) & 1)) return false;
+                const bool ragged = is_k && w.len < (u + 1) * kTile;   // a key behind the sequence has dS = 0, times itself in dQ
+                const uint32_t bar = ragged ? raw : full + 8 * at;
                 if (lane == 0) {
-                    mbar_expect(full + 8 * at, C::kBytes);
+                    mbar_expect(bar, C::kBytes);
                     for (int x = 0; x < C::kSub; ++x)
-                        tma_load(sring + at * C::kBytes + x * (kTile * 128), is_k ? &mk : &mv, full + 8 * at, x * 64,
+                        tma_load(sring + at * C::kBytes + x * (kTile * 128), is_k ? &mk : &mv, bar, x * 64,
                                  int(kv_head) * (is_k ? a.k_mul : a.v_mul), int(w.first + u * kTile));
+                }
+                if (ragged) {
+                    if (!warp_wait(raw, fixed & 1)) return false;
+                    ++fixed;
+                    zero_tile_rows<C::kSub>(sring + at * C::kBytes, w.len - u * kTile);
+                    if (lane == 0) mbar_arrive(full + 8 * at);
                 }
                 return true;
             };
@@ -1066,68 +1108,66 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             if (ok) ok = warp_wait(q_empty, (tiles - 1) & 1);
         }
         for (uint32_t i = n > C::kKeys ? n - C::kKeys : 0; i < n; ++i) {
-            mbar_wait(full + 8 * k_at(i), (i / C::kKeys) & 1);
-            if (ok) ok = warp_wait(empty + 8 * k_at(i), (i / C::kKeys) & 1);
+            mbar_wait(full + 8 * (i % C::kKeys), (i / C::kKeys) & 1);
+            if (ok) ok = warp_wait(empty + 8 * (i % C::kKeys), (i / C::kKeys) & 1);
         }
         for (uint32_t i = n > C::kValues ? n - C::kValues : 0; i < n; ++i) {
-            mbar_wait(full + 8 * v_at(i), (i / C::kValues) & 1);
-            if (ok) ok = warp_wait(empty + 8 * v_at(i), (i / C::kValues) & 1);
+            mbar_wait(full + 8 * (C::kKeys + i % C::kValues), (i / C::kValues) & 1);
+            if (ok) ok = warp_wait(empty + 8 * (C::kKeys + i % C::kValues), (i / C::kValues) & 1);
         }
     } else if (warp == 8) {   // ------------------------------------- products
-        const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
-        uint32_t tiles = 0, it = 0;   // jobs, key tiles so far
-        auto place = [&](uint32_t at) { return sring + at * C::kBytes; };
-        auto wait_k = [&](uint32_t n) { return warp_wait(full + 8 * k_at(n), (n / C::kKeys) & 1); };
-        auto wait_v = [&](uint32_t n) { return warp_wait(full + 8 * v_at(n), (n / C::kValues) & 1); };
-        auto release = [&](uint32_t at) {
-            if (lane == 0) mma_commit(empty + 8 * at);
-        };
-        for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
-            if (w.kind != kJobWork) continue;
-            const uint32_t total = w.block + 1, n0 = it;
-            auto scores = [&](uint32_t u) {
-                const uint32_t key = place(k_at(n0 + u));
-                if (w.len < (u + 1) * kTile) zero_tile_rows<C::kSub>(key, w.len - u * kTile);   // dS there is zero
-                if (lane == 0) {
-                    product_rows<DP>(tmem + ((n0 + u) & 1) * 128, sq, key, id_s | a.negate);
-                    mma_commit(s_full + 8 * ((n0 + u) & 1));
-                }
+        if (lane == 0) {   // one thread, as in the forward kernel
+            const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
+            uint32_t tiles = 0, it = 0;   // jobs, key tiles so far
+            Place key, ahead, value;      // the key tile of the next dQ and of the next S; the value tile of the next dP
+            auto key_of = [&](const Place &p) { return sring + p.at * C::kBytes; };
+            auto value_of = [&](const Place &p) { return sring + (C::kKeys + p.at) * C::kBytes; };
+            auto wait_key = [&](const Place &p) { return mbar_wait(full + 8 * p.at, p.phase); };
+            auto wait_value = [&](const Place &p) { return mbar_wait(full + 8 * (C::kKeys + p.at), p.phase); };
+            uint32_t s_at = 0;            // which of the two S buffers is next
+            auto scores = [&]() {         // S = Q K^T
+                product_rows<DP>(tmem + s_at * 128, sq, key_of(ahead), id_s | a.negate);
+                mma_commit(s_full + 8 * s_at);
+                ahead.template next<C::kKeys>();
+                s_at ^= 1;
             };
-            auto d_probs = [&](uint32_t u) {
-                if (lane == 0) {
-                    product_rows<DP>(t_dp, sdo, place(v_at(n0 + u)), id_s);
-                    mma_commit(dp_full);
-                    if (u + 1 == total) mma_commit(q_empty);   // the last use of Q (its last product came before) and dO
-                }
-                release(v_at(n0 + u));
+            auto d_probs = [&](bool last) {   // dP = dO V^T
+                product_rows<DP>(t_dp, sdo, value_of(value), id_s);
+                mma_commit(dp_full);
+                if (last) mma_commit(q_empty);   // the last use of dO, and of Q in a product issued before
+                mma_commit(empty + 8 * (C::kKeys + value.at));
+                value.template next<C::kValues>();
             };
-            if (!(ok = warp_wait(q_full, tiles & 1) && wait_k(n0))) break;
-            ++tiles;
-            tc_fence_after();
-            scores(0);
-            if (!(ok = wait_v(n0))) break;
-            d_probs(0);
-            if (total > 1) {
-                if (!(ok = wait_k(n0 + 1))) break;
-                scores(1);
-            }
-            for (uint32_t u = 0; u < total; ++u, ++it) {
-                if (!(ok = warp_wait(ds_full, it & 1))) break;
+            for (uint32_t k = 0; (ok = jobs.get_alone(k, &w)) && w.kind != kJobStop; ++k) {
+                if (w.kind != kJobWork) continue;
+                const uint32_t total = w.block + 1;
+                if (!(ok = mbar_wait(q_full, tiles & 1) && wait_key(ahead))) break;
+                ++tiles;
                 tc_fence_after();
-                if (lane == 0) product_cols<64>(t_dq, t_dp, place(k_at(n0 + u)), id_o, u > 0);
-                release(k_at(n0 + u));
-                if (u + 1 < total) {
-                    if (!(ok = wait_v(n0 + u + 1))) break;
-                    d_probs(u + 1);
-                } else if (lane == 0) {
-                    mma_commit(done);
+                scores();
+                if (!(ok = wait_value(value))) break;
+                d_probs(total == 1);
+                if (total > 1) {
+                    if (!(ok = wait_key(ahead))) break;
+                    scores();
                 }
-                if (u + 2 < total) {
-                    if (!(ok = wait_k(n0 + u + 2))) break;
-                    scores(u + 2);
+                for (uint32_t u = 0; u < total; ++u, ++it) {
+                    if (u + 1 < total && !(ok = wait_value(value))) break;
+                    if (!(ok = mbar_wait(ds_full, it & 1))) break;
+                    tc_fence_after();
+                    // dS lies where S was, so the next dP need not wait for the product that reads it
+                    if (u + 1 < total) d_probs(u + 2 == total);
+                    product_cols<64>(t_dq, tmem + (it & 1) * 128, key_of(key), id_o, u > 0);   // dQ += dS K
+                    mma_commit(empty + 8 * key.at);
+                    key.template next<C::kKeys>();
+                    if (u + 1 == total) mma_commit(done);
+                    if (u + 2 < total) {
+                        if (!(ok = wait_key(ahead))) break;
+                        scores();
+                    }
                 }
+                if (!ok) break;
             }
-            if (!ok) break;
         }
     } else if (warp == 10) {   // ---------------------------------------- jobs
         ok = jobs.template run<kTile, true>(a, a.q_heads);
@@ -1182,7 +1222,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     }
 #pragma unroll
                     for (int x = 0; x < 32; ++x) r[0][x] = bf16x2(p[x].x, p[x].y);
-                    tmem_st32(t_dp + lanes + col0, r[0]);
+                    tmem_st32(tmem + (it & 1) * 128 + lanes + col0, r[0]);   // over S
                 }
                 tmem_wait_st();
                 tc_fence_before();

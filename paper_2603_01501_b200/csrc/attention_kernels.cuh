@@ -454,7 +454,8 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             }
         } else if (warp == 8) {   // --------------------------------- products
             // One thread: between two batches of products the tensor cores hold about one product's work, so every
-            // cycle spent here in between is one that they may lose.
+            // cycle spent here in between is one that they may lose.  Spinning for P instead of sleeping gains 3 %
+            // here, and costs the backward kernels 3 %, whose row warps are the busier ones.
             if (lane == 0) {
                 const uint32_t id_s = mma_desc(kTile, false) | a.negate, id_o = mma_desc(DP, true);
                 uint32_t tiles = 0, done0 = 0, done1 = 0;   // jobs, blocks of the first and second tile so far
@@ -486,7 +487,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                         key.template next<C::kStages>();
                         if (!(ok = wait_tile(v) && (j + 1 == nb || wait_tile(key)))) break;
                         if (j < nb0) {
-                            if (!(ok = mbar_wait(p_full, done0 & 1))) break;
+                            if (!(ok = mbar_spin(p_full, done0 & 1))) break;
                             ++done0;
                             tc_fence_after();
                             product_cols<32>(tmem + 256, tmem, tile_of(v), id_o, j > 0);   // O_0 += P_0 V
@@ -497,7 +498,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                             }
                         }
                         if (two) {
-                            if (!(ok = mbar_wait(p_full + 8, done1 & 1))) break;
+                            if (!(ok = mbar_spin(p_full + 8, done1 & 1))) break;
                             ++done1;
                             tc_fence_after();
                             product_cols<32>(tmem + 384, tmem + 128, tile_of(v), id_o, j > 0);

@@ -44,6 +44,16 @@ __device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
     return mbar_try(bar, parity) || mbar_try(bar, parity) || mbar_wait_slow(bar, parity);
 }
+// The same by asking again and again: a thread put to sleep by try_wait wakes up later.
+__device__ __forceinline__ bool mbar_spin(uint32_t bar, uint32_t parity) {
+    for (uint32_t i = 0; i < 4096; ++i) {
+        uint32_t ok;
+        asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+    }
+    return mbar_wait_slow(bar, parity);
+}
 // The same for a whole warp, which goes on or gives up as one.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
     return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity));

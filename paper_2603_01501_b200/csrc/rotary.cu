@@ -2,10 +2,11 @@
 //
 //   (x, y) -> scale (x cos a - y sin a, x sin a + y cos a),   a = position * freq
 //
-// Bound by HBM: every element is read once and written once, three flops each.  A CTA takes a few tokens at
-// a time: its threads first work out the tokens' sines and cosines once (the angle is reduced to one turn in
-// binary64, then sincospi in binary32: exact to the last bits at any position, no table in memory),
-// leave them in shared memory, and then every head of those tokens is turned with them.
+// Bound by HBM: every element is read once and written once, three flops each.  A CTA takes a few tokens: its threads
+// first work out the tokens' sines and cosines once (the angle is reduced to one turn in binary64, then sincospi in
+// binary32: exact to the last bits at any position, no table in memory) and leave them in shared memory; then every
+// head of those tokens is turned with them, four vectors of 16 bytes of each kind in flight per thread.
+// 16384 tokens x 32 heads x 128, bfloat16: see the table of measurements in the launch code below.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -20,7 +21,8 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 4;   // tokens of a CTA's turn
+constexpr int kMaxTokens = 4;   // tokens of a CTA
+constexpr uint32_t kFewTokens = 148 * 4;
 
 struct RotaryDev {
     const char *x[2];
@@ -28,6 +30,7 @@ struct RotaryDev {
     long long x_token[2], x_head[2], y_token[2], y_head[2];
     uint32_t heads[2];
     uint32_t n_tokens, n_seqs, head_dim, pairs;
+    uint32_t per_cta;                       // tokens of a CTA, at most kMaxTokens
     const int32_t *positions, *cu;
     float scale;
     int inverse;
@@ -57,13 +60,9 @@ __device__ int place_in_sequence(const int32_t *cu, uint32_t n_seqs, uint32_t t)
     return int(t) - (lo ? max(cu[lo], 0) : 0);
 }
 
-template <typename T, bool HALF>
-__global__ void __launch_bounds__(kThreads)
-rotary_kernel(const __grid_constant__ RotaryDev a) {
-    __shared__ float2 wheel[kTokens][GAC_ROTARY_MAX_DIM / 2];
-    const uint32_t t0 = blockIdx.x * kTokens;
-    const uint32_t nt = min(uint32_t(kTokens), a.n_tokens - t0);
-    for (uint32_t w = threadIdx.x; w < nt * a.pairs; w += kThreads) {
+// Cosine and sine, already scaled, of every pair of the CTA's tokens.
+__device__ __forceinline__ void fill_wheel(const RotaryDev &a, float2 (*wheel)[GAC_ROTARY_MAX_DIM / 2], uint32_t t0, uint32_t nt) {
+    for (uint32_t w = threadIdx.x; w < nt * a.pairs; w += blockDim.x) {
         const uint32_t t = w / a.pairs, i = w % a.pairs;
         const int pos = a.positions ? a.positions[t0 + t] : place_in_sequence(a.cu, a.n_seqs, t0 + t);
         const double turns = double(pos) * a.turns[i];
@@ -72,6 +71,16 @@ rotary_kernel(const __grid_constant__ RotaryDev a) {
         wheel[t][i] = make_float2(c * a.scale, (a.inverse ? -s : s) * a.scale);
     }
     __syncthreads();
+}
+
+// Any size, stride and alignment: one pair, or one copied element, at a time.
+template <typename T, bool HALF>
+__global__ void __launch_bounds__(kThreads)
+rotary_any_kernel(const __grid_constant__ RotaryDev a) {
+    __shared__ __align__(16) float2 wheel[kMaxTokens][GAC_ROTARY_MAX_DIM / 2];
+    const uint32_t t0 = blockIdx.x * a.per_cta;
+    const uint32_t nt = min(a.per_cta, a.n_tokens - t0);
+    fill_wheel(a, wheel, t0, nt);
     const uint32_t rest = a.head_dim - 2 * a.pairs, units = a.pairs + rest;
     const uint32_t heads = a.heads[0] + a.heads[1];
     for (uint32_t w = threadIdx.x; w < nt * heads * units; w += kThreads) {
@@ -89,6 +98,112 @@ rotary_kernel(const __grid_constant__ RotaryDev a) {
         } else {
             const uint32_t i = a.pairs + u;
             if (x != y) store_el(y + i * sizeof(T), load_el(x + i * sizeof(T), T{}), T{});
+        }
+    }
+}
+
+// N consecutive elements as they lie in memory.
+template <typename T, int N>
+struct Vec {
+    static constexpr int kWords = N * int(sizeof(T)) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const char *p) {
+        if (kWords == 4) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(p);
+            w[0] = v.x; w[1] = v.y; w[kWords - 2] = v.z; w[kWords - 1] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2 *>(p);
+            w[0] = v.x; w[1] = v.y;
+        }
+    }
+    __device__ __forceinline__ void store(char *p) const {
+        if (kWords == 4) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[kWords - 2], w[kWords - 1]);
+        else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if (sizeof(T) == 4) return __uint_as_float(w[i]);
+        return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    }
+    __device__ __forceinline__ void put2(int i, float a, float b) {   // elements i and i + 1, i even
+        if (sizeof(T) == 4) {
+            w[i] = __float_as_uint(a);
+            w[i + 1] = __float_as_uint(b);
+        } else {
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i / 2]) : "f"(b), "f"(a));
+        }
+    }
+};
+
+// A thread keeps one place of the head, N pairs (two vectors) or 2 N copied elements, and walks over the CTA's tokens and heads.
+template <typename T, bool HALF, int N>
+__global__ void __launch_bounds__(kThreads, 4)
+rotary_kernel(const __grid_constant__ RotaryDev a) {
+    __shared__ __align__(16) float2 wheel[kMaxTokens][GAC_ROTARY_MAX_DIM / 2];
+    constexpr int kFlight = 4;
+    constexpr uint32_t kSize = sizeof(T);
+    const uint32_t t0 = blockIdx.x * a.per_cta;
+    const uint32_t nt = min(a.per_cta, a.n_tokens - t0);
+    const uint32_t turned = a.pairs / N, units = turned + (a.head_dim - 2 * a.pairs + 2 * N - 1) / (2 * N);   // places of a head
+    const uint32_t u = threadIdx.x % units, step = blockDim.x / units, heads = a.heads[0] + a.heads[1];
+    const bool turn = u < turned;
+    // byte offsets of the two vectors in a head
+    const uint32_t first = (turn ? (HALF ? u * N : 2 * u * N) : 2 * a.pairs + (u - turned) * 2 * N) * kSize;
+    const uint32_t second = first + (turn && HALF ? a.pairs : N) * kSize;
+    const bool both = turn || second < a.head_dim * kSize;
+    fill_wheel(a, wheel, t0, nt);
+    if (threadIdx.x >= step * units) return;
+    if (!turn && a.x[0] == a.y[0] && a.x[1] == a.y[1]) return;   // in place: nothing to copy
+    uint32_t t = 0, h = threadIdx.x / units;
+    while (h >= heads) {
+        h -= heads;
+        ++t;
+    }
+    while (t < nt) {
+        Vec<T, N> p[kFlight], q[kFlight];
+        char *to[kFlight];
+        uint32_t at[kFlight];
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            at[i] = t;
+            if (t < nt) {
+                const int which = h >= a.heads[0];
+                const uint32_t hh = which ? h - a.heads[0] : h;
+                const char *x = a.x[which] + ((long long)(t0 + t) * a.x_token[which] + (long long)hh * a.x_head[which]) * kSize;
+                to[i] = a.y[which] + ((long long)(t0 + t) * a.y_token[which] + (long long)hh * a.y_head[which]) * kSize;
+                p[i].load(x + first);
+                if (both) q[i].load(x + second);
+                n = i + 1;
+                h += step;
+                while (h >= heads) {
+                    h -= heads;
+                    ++t;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            if (i >= n) break;
+            if (turn) {
+                const float4 *cs = reinterpret_cast<const float4 *>(wheel[at[i]] + u * N);
+#pragma unroll
+                for (int j = 0; j < N; j += 2) {
+                    const float4 c = cs[j / 2];   // cosine, sine, cosine, sine
+                    if (HALF) {
+                        const float x0 = p[i].get(j), x1 = p[i].get(j + 1), y0 = q[i].get(j), y1 = q[i].get(j + 1);
+                        p[i].put2(j, x0 * c.x - y0 * c.y, x1 * c.z - y1 * c.w);
+                        q[i].put2(j, x0 * c.y + y0 * c.x, x1 * c.w + y1 * c.z);
+                    } else {
+                        Vec<T, N> &v = j < N / 2 ? p[i] : q[i];
+                        const int e = 2 * j - (j < N / 2 ? 0 : N);
+                        const float x0 = v.get(e), y0 = v.get(e + 1), x1 = v.get(e + 2), y1 = v.get(e + 3);
+                        v.put2(e, x0 * c.x - y0 * c.y, x0 * c.y + y0 * c.x);
+                        v.put2(e + 2, x1 * c.z - y1 * c.w, x1 * c.w + y1 * c.z);
+                    }
+                }
+            }
+            p[i].store(to[i] + first);
+            if (both) q[i].store(to[i] + second);
         }
     }
 }
@@ -157,8 +272,8 @@ int gac_rotary(const gac_rotary_args *args, int cuda_device, void *cuda_stream) 
     for (int w = 0; w < 2; ++w) {
         const gac_rotary_heads &h = a.qk[w];
         d.heads[w] = a.heads[w];
-        d.x[w] = static_cast<const char *>(h.x);
-        d.y[w] = static_cast<char *>(h.y);
+        d.x[w] = a.heads[w] ? static_cast<const char *>(h.x) : nullptr;
+        d.y[w] = a.heads[w] ? static_cast<char *>(h.y) : nullptr;
         d.x_token[w] = h.x_token;
         d.x_head[w] = h.x_head;
         d.y_token[w] = h.y_token;
@@ -211,10 +326,28 @@ int gac_rotary(const gac_rotary_args *args, int cuda_device, void *cuda_stream) 
     DeviceGuard guard(cuda_device);
     if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    const uint32_t grid = (a.n_tokens + kTokens - 1) / kTokens;
-    const bool half = a.layout == GAC_ROTARY_HALF;
-    auto *fn = a.dtype == GAC_BF16 ? (half ? rotary_kernel<uint16_t, true> : rotary_kernel<uint16_t, false>)
-                                   : (half ? rotary_kernel<float, true> : rotary_kernel<float, false>);
+    const bool half = a.layout == GAC_ROTARY_HALF, bf16 = a.dtype == GAC_BF16;
+    // Vectors of 16 or 8 bytes where every vector of every head starts on such a boundary and ends inside its part of
+    // the head; single elements otherwise.
+    auto fits = [&](uint32_t n) {   // n elements
+        const uint64_t bytes = n * size;
+        if (d.pairs % n || a.head_dim % n) return false;
+        for (int w = 0; w < 2; ++w)
+            if (d.heads[w] && (reinterpret_cast<uint64_t>(d.x[w]) % bytes || reinterpret_cast<uint64_t>(d.y[w]) % bytes || d.x_token[w] % n ||
+                               d.x_head[w] % n || d.y_token[w] % n || d.y_head[w] % n))
+                return false;
+        return true;
+    };
+    const uint32_t n = fits(16 / size) ? 16 / size : bf16 && fits(4) ? 4 : 1;
+    // Few tokens: one to a CTA, so that as many SMs as can be work; many: the sines of four tokens in one go.
+    d.per_cta = std::min<uint32_t>(kMaxTokens, (a.n_tokens + kFewTokens - 1) / kFewTokens);
+    const uint32_t grid = (a.n_tokens + d.per_cta - 1) / d.per_cta;
+    void (*fn)(const RotaryDev) = nullptr;
+    if (bf16) fn = n == 8 ? (half ? rotary_kernel<uint16_t, true, 8> : rotary_kernel<uint16_t, false, 8>)
+                 : n == 4 ? (half ? rotary_kernel<uint16_t, true, 4> : rotary_kernel<uint16_t, false, 4>)
+                          : (half ? rotary_any_kernel<uint16_t, true> : rotary_any_kernel<uint16_t, false>);
+    else fn = n == 4 ? (half ? rotary_kernel<float, true, 4> : rotary_kernel<float, false, 4>)
+                     : (half ? rotary_any_kernel<float, true> : rotary_any_kernel<float, false>);
     fn<<<grid, kThreads, 0, s>>>(d);
     GAC_CUDA(nullptr, cudaGetLastError());
     return GAC_OK;

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
@@ -188,11 +189,12 @@ def load_library() -> ctypes.CDLL:
     L.gac_clip_grad_norm.argtypes = [vp, vp, f64, f64, vp, P(gac_clip_result)]
     L.gac_clip_free.argtypes = [vp]
     L.gac_rotary_freqs.argtypes = [P(f64), u32, f64, i32, f64, f64, f64, f64]
-    L.gac_rotary.argtypes = [P(gac_rotary_args), i32, vp]
-    L.gac_attn_workspace.argtypes = [P(gac_attn)]
+    # the structs travel as packed bytes (or ctypes.byref of the structures above)
+    L.gac_rotary.argtypes = [vp, i32, vp]
+    L.gac_attn_workspace.argtypes = [vp]
     L.gac_attn_workspace.restype = ctypes.c_size_t
-    L.gac_attn_forward.argtypes = [P(gac_attn), i32, vp]
-    L.gac_attn_backward.argtypes = [P(gac_attn), P(gac_attn_grad), i32, vp]
+    L.gac_attn_forward.argtypes = [vp, i32, vp]
+    L.gac_attn_backward.argtypes = [vp, vp, i32, vp]
     L.gac_attn_check.argtypes = [i32, vp]
     for name in ("gac_clip_init", "gac_clip_sumsq", "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_free",
                  "gac_rotary_freqs", "gac_rotary", "gac_attn_forward", "gac_attn_backward", "gac_attn_check"):
@@ -479,16 +481,25 @@ def gac_rebind(ctx: GacContext, g_list: Sequence[torch.Tensor], d_list: Sequence
 # ---------------------------------------------------------------- around the rule: packed rollouts
 
 
+# Packed forms of gac_rotary_args, gac_attn and gac_attn_grad: one call instead of one per field.
+_ROTARY = struct.Struct("=QQqqqqQQqqqqIIIIIIiiiiQQQd")
+_ATTN = struct.Struct("=QqqQqqQqqQqqQQIIIIIifi")
+_ATTN_GRAD = struct.Struct("=QqqQqqQqqQqqQQ")
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _on(stream, device: torch.device):
-    """The stream to launch on, as a torch stream of the tensors' device.  What a call allocates is allocated on
-    it, so that the caching allocator hands the memory on in that stream's order."""
+    """(raw stream to launch on, torch stream or None for the current one of the tensors' device).  What a call
+    allocates is allocated on that stream, so that the caching allocator hands the memory on in its order."""
     if stream is None:
-        return torch.cuda.current_stream(device)
-    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+        return _raw_stream(device.index), None
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    return stream.cuda_stream, stream
 
 
 def _empty(shape, dtype, device, stream) -> torch.Tensor:
-    if stream == torch.cuda.current_stream(device):
+    if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
@@ -600,21 +611,25 @@ def gac_rotary_freqs(rot_dim: int, base: float = 1e4, scaling: str = "none", fac
     return freqs
 
 
-def _int32_ptr(t: Optional[torch.Tensor], name: str, device: torch.device) -> Optional[int]:
+def _int32_ptr(t: Optional[torch.Tensor], name: str, device: torch.device) -> int:
     if t is None:
-        return None
-    if t.dtype != torch.int32 or t.device != device or t.dim() != 1 or not t.is_contiguous():
+        return 0
+    if t.dtype is not torch.int32 or t.device != device or t.dim() != 1 or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 vector on the tensors' device")
     return t.data_ptr()
 
 
-def _heads(t: torch.Tensor, name: str, like: torch.Tensor) -> None:
-    if t.dim() != 3 or not t.is_cuda or t.device != like.device:
+def _heads(t: torch.Tensor, name: str, like: torch.Tensor):
+    """Checks one [tokens, heads, head_dim] operand; returns (address, token stride, head stride, heads)."""
+    if t.dim() != 3 or t.device != like.device or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor [tokens, heads, head_dim]")
-    if t.dtype != like.dtype or t.shape[0] != like.shape[0] or t.shape[2] != like.shape[2]:
+    n, h, d = t.shape
+    if t is not like and (t.dtype is not like.dtype or n != like.shape[0] or d != like.shape[2]):
         raise ValueError(f"{name} differs in dtype, tokens or head_dim")
-    if t.stride(2) != 1 and t.shape[2] > 1:
+    s0, s1, s2 = t.stride()
+    if s2 != 1 and d > 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
+    return t.data_ptr(), s0, s1, h
 
 
 def gac_rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Optional[torch.Tensor] = None,
@@ -625,62 +640,70 @@ def gac_rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Opt
     a head.  Positions are given, or follow from ``cu_seqlens``.  Returns (q', k'): new contiguous tensors, or
     the given ones when ``in_place``."""
     import numpy as np
-    xs = [q] if k is None else [q, k]
-    if q.dtype not in _DT:
-        raise GacError(GAC_ERR_DTYPE, f"unsupported dtype {q.dtype}")
-    for x, name in zip(xs, ("q", "k")):
-        _heads(x, name, q)
+    dtype, device = q.dtype, q.device
+    if dtype not in _DT:
+        raise GacError(GAC_ERR_DTYPE, f"unsupported dtype {dtype}")
+    qx, q0, q1, qh = _heads(q, "q", q)
+    kx = k0 = k1 = kh = 0
+    if k is not None:
+        kx, k0, k1, kh = _heads(k, "k", q)
     if (positions is None) == (cu_seqlens is None):
         raise ValueError("give positions or cu_seqlens")
-    if positions is not None and positions.numel() != q.shape[0]:
+    tokens, _, dim = q.shape
+    if positions is not None and positions.numel() != tokens:
         raise ValueError("one position per token")
-    freqs = np.ascontiguousarray(freqs, dtype=np.float64)
-    stream = _on(stream, q.device)
-    ys = xs if in_place else [_empty(x.shape, x.dtype, x.device, stream) for x in xs]
-    a = gac_rotary_args()
-    for i, (x, y) in enumerate(zip(xs, ys)):
-        a.qk[i] = gac_rotary_heads(x.data_ptr(), y.data_ptr(), x.stride(0), x.stride(1), y.stride(0), y.stride(1))
-        a.heads[i] = x.shape[1]
-    a.n_tokens, a.head_dim, a.rot_dim = q.shape[0], q.shape[2], 2 * freqs.size
-    a.n_seqs = 0 if cu_seqlens is None else cu_seqlens.numel() - 1
-    a.dtype, a.layout, a.inverse = _DT[q.dtype], ROTARY_LAYOUTS[layout], int(bool(inverse))
-    a.positions = _int32_ptr(positions, "positions", q.device)
-    a.cu_seqlens = _int32_ptr(cu_seqlens, "cu_seqlens", q.device)
-    a.freqs, a.scale = freqs.ctypes.data, scale
-    _check(load_library().gac_rotary(ctypes.byref(a), q.device.index, stream.cuda_stream))
-    return ys[0], (ys[1] if k is not None else None)
+    if cu_seqlens is not None and cu_seqlens.numel() < 1:
+        raise ValueError("cu_seqlens has one entry more than there are sequences")
+    if not (isinstance(freqs, np.ndarray) and freqs.dtype == np.float64 and freqs.flags.c_contiguous):
+        freqs = np.ascontiguousarray(freqs, dtype=np.float64)
+    raw, stream = _on(stream, device)
+    if in_place:
+        yq, yk = q, k
+        qy, kout = (qx, q0, q1), (kx, k0, k1)
+    else:
+        yq = _empty((tokens, qh, dim), dtype, device, stream)
+        yk = _empty((tokens, kh, dim), dtype, device, stream) if k is not None else None
+        qy = (yq.data_ptr(), qh * dim, dim)
+        kout = (yk.data_ptr(), kh * dim, dim) if k is not None else (0, 0, 0)
+    args = _ROTARY.pack(qx, qy[0], q0, q1, qy[1], qy[2], kx, kout[0], k0, k1, kout[1], kout[2], qh, kh, tokens,
+                        0 if cu_seqlens is None else cu_seqlens.numel() - 1, dim, 2 * freqs.size, _DT[dtype],
+                        ROTARY_LAYOUTS[layout], 1 if inverse else 0, 0, _int32_ptr(positions, "positions", device),
+                        _int32_ptr(cu_seqlens, "cu_seqlens", device), freqs.ctypes.data, scale)
+    _check(load_library().gac_rotary(args, device.index, raw))
+    return yq, yk
 
 
-def _attn_heads(t: torch.Tensor) -> gac_attn_heads:
-    return gac_attn_heads(t.data_ptr(), t.stride(0), t.stride(1))
-
-
-def _attn_args(q, k, v, o, lse, cu_seqlens, scale) -> gac_attn:
+def _attn_args(q, k, v, o, lse, cu_seqlens, scale) -> bytes:
     if q.dtype not in _DT:
         raise GacError(GAC_ERR_DTYPE, f"unsupported dtype {q.dtype}")
-    for t, name in ((q, "q"), (k, "k"), (v, "v"), (o, "o")):
-        _heads(t, name, q)
-    if k.shape != v.shape or o.shape != q.shape:
+    qp, q0, q1, qh = _heads(q, "q", q)
+    kp, k0, k1, kh = _heads(k, "k", q)
+    vp, v0, v1, vh = _heads(v, "v", q)
+    op, o0, o1, oh = _heads(o, "o", q)
+    tokens, _, dim = q.shape
+    if vh != kh or oh != qh:
         raise ValueError("k and v, and o and q, must have the same shape")
-    if not (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (q.shape[1], q.shape[0])):
+    if lse.dtype is not torch.float32 or lse.device != q.device or lse.shape != (qh, tokens) or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous float32 tensor [q_heads, tokens]")
-    if cu_seqlens.numel() < 1:
+    n = cu_seqlens.numel()
+    if n < 1:
         raise ValueError("cu_seqlens has one entry more than there are sequences")
-    return gac_attn(_attn_heads(q), _attn_heads(k), _attn_heads(v), _attn_heads(o), lse.data_ptr(),
-                    _int32_ptr(cu_seqlens, "cu_seqlens", q.device), q.shape[0], cu_seqlens.numel() - 1, q.shape[1],
-                    k.shape[1], q.shape[2], _DT[q.dtype], q.shape[2] ** -0.5 if scale is None else scale, 0)
+    return _ATTN.pack(qp, q0, q1, kp, k0, k1, vp, v0, v1, op, o0, o1, lse.data_ptr(),
+                      _int32_ptr(cu_seqlens, "cu_seqlens", q.device), tokens, n - 1, qh, kh, dim, _DT[q.dtype],
+                      dim ** -0.5 if scale is None else scale, 0)
 
 
 def gac_attn_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
                      scale: Optional[float] = None, stream=None):
     """Causal attention over packed sequences: q [tokens, q_heads, head_dim], k and v [tokens, kv_heads,
     head_dim], bfloat16 views.  Returns (o, lse): o like q, contiguous; lse [q_heads, tokens] float32."""
-    _heads(q, "q", q)
-    stream = _on(stream, q.device)
-    o = _empty(q.shape, q.dtype, q.device, stream)
-    lse = _empty((q.shape[1], q.shape[0]), torch.float32, q.device, stream)
-    a = _attn_args(q, k, v, o, lse, cu_seqlens, scale)
-    _check(load_library().gac_attn_forward(ctypes.byref(a), q.device.index, stream.cuda_stream))
+    if q.dim() != 3 or not q.is_cuda:
+        raise ValueError("q must be a CUDA tensor [tokens, heads, head_dim]")
+    device = q.device
+    raw, stream = _on(stream, device)
+    o = _empty(q.shape, q.dtype, device, stream)
+    lse = _empty((q.shape[1], q.shape[0]), torch.float32, device, stream)
+    _check(load_library().gac_attn_forward(_attn_args(q, k, v, o, lse, cu_seqlens, scale), device.index, raw))
     return o, lse
 
 
@@ -688,20 +711,26 @@ def gac_attn_backward(d_o: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
                       lse: torch.Tensor, cu_seqlens: torch.Tensor, scale: Optional[float] = None, stream=None):
     """Gradients (d_q, d_k, d_v) of gac_attn_forward's o, given d_o; new contiguous tensors."""
     L = load_library()
-    a = _attn_args(q, k, v, o, lse, cu_seqlens, scale)
-    _heads(d_o, "d_o", q)
-    if d_o.shape != q.shape:
+    args = _attn_args(q, k, v, o, lse, cu_seqlens, scale)
+    gp, g0, g1, gh = _heads(d_o, "d_o", q)
+    tokens, qh, dim = q.shape
+    kh = k.shape[1]
+    if gh != qh:
         raise ValueError("d_o must have q's shape")
-    stream = _on(stream, q.device)
-    d_q, d_k, d_v = (_empty(t.shape, t.dtype, t.device, stream) for t in (q, k, v))
-    need = L.gac_attn_workspace(ctypes.byref(a))
-    workspace = _empty((max(need, 16),), torch.uint8, q.device, stream)
-    g = gac_attn_grad(_attn_heads(d_o), _attn_heads(d_q), _attn_heads(d_k), _attn_heads(d_v), workspace.data_ptr(), need)
-    _check(L.gac_attn_backward(ctypes.byref(a), ctypes.byref(g), q.device.index, stream.cuda_stream))
+    device = q.device
+    raw, stream = _on(stream, device)
+    d_q = _empty((tokens, qh, dim), q.dtype, device, stream)
+    d_k = _empty((tokens, kh, dim), q.dtype, device, stream)
+    d_v = _empty((tokens, kh, dim), q.dtype, device, stream)
+    need = max(L.gac_attn_workspace(args), 16)
+    workspace = _empty((need,), torch.uint8, device, stream)
+    grad = _ATTN_GRAD.pack(gp, g0, g1, d_q.data_ptr(), qh * dim, dim, d_k.data_ptr(), kh * dim, dim, d_v.data_ptr(),
+                           kh * dim, dim, workspace.data_ptr(), need)
+    _check(L.gac_attn_backward(args, grad, device.index, raw))
     return d_q, d_k, d_v
 
 
 def gac_attn_check(device: Optional[int] = None, stream=None) -> None:
     """Synchronises the stream and raises GacError(GAC_ERR_TIMEOUT) if a wait inside an attention kernel ran out."""
     dev = torch.device("cuda", torch.cuda.current_device() if device is None else device)
-    _check(load_library().gac_attn_check(dev.index, _on(stream, dev).cuda_stream))
+    _check(load_library().gac_attn_check(dev.index, _on(stream, dev)[0]))

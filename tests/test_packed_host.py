@@ -36,6 +36,9 @@ def test_struct_layouts_match_the_header(tmp_path):
     got = list(map(int, subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()))
     want = [ctypes.sizeof(getattr(gb, n)) for n in names] + [getattr(getattr(gb, n), f).offset for n, f in fields]
     assert got == want
+    # the packed forms the calls send have the same layout
+    for packed, struct in ((gb._ROTARY, gb.gac_rotary_args), (gb._ATTN, gb.gac_attn), (gb._ATTN_GRAD, gb.gac_attn_grad)):
+        assert packed.size == ctypes.sizeof(struct)
 
 
 def test_rotary_frequencies(lib):

@@ -458,7 +458,8 @@ int gac_stats_static(const gac_tensor *list, uint32_t n, int g_dtype, int d_dtyp
  *              synchronised and the record copied there
  * A norm that is NaN or infinite: nothing is written to any `out`, the record
  * says nonfinite, and with host_out the call returns GAC_ERR_NONFINITE.
- * Errors: INVALID_ARG, DTYPE, CUDA, NONFINITE.
+ * The factor is rounded once to binary32.  One context serves one stream at a time.
+ * Errors: INVALID_ARG, DTYPE, CUDA, NONFINITE, TIMEOUT.
  */
 typedef struct gac_clip_ctx gac_clip_ctx;   /* opaque, library-owned */
 typedef struct {
@@ -473,7 +474,8 @@ typedef struct {
     double norm;        /* its square root                                                    */
     double scale;       /* factor applied                                                     */
     int32_t nonfinite;  /* 1: the norm is NaN or infinite, nothing was written                */
-    int32_t reserved;
+    int32_t timed_out;  /* 1: a wait inside the kernel ran out (bounded, never in ordinary
+                           use), outputs are incomplete; with host_out GAC_ERR_TIMEOUT         */
 } gac_clip_result;
 int gac_clip_init(gac_clip_ctx **out, const gac_clip_tensor *list, uint32_t n, int cuda_device);
 int gac_clip_sumsq(gac_clip_ctx *ctx, void *cuda_stream, double *sumsq_out);

@@ -86,7 +86,7 @@ class gac_clip_tensor(ctypes.Structure):
 
 class gac_clip_result(ctypes.Structure):
     _fields_ = [("sumsq", ctypes.c_double), ("norm", ctypes.c_double), ("scale", ctypes.c_double),
-                ("nonfinite", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+                ("nonfinite", ctypes.c_int32), ("timed_out", ctypes.c_int32)]
 
 
 class gac_rotary_heads(ctypes.Structure):
@@ -513,8 +513,9 @@ def _check(rc: int) -> None:
 class ClipContext:
     """Owner of one ``gac_clip_ctx``; keeps references to the tensors in its table."""
 
-    def __init__(self, handle: int, g_list, out_list):
+    def __init__(self, handle: int, g_list, out_list, device: int):
         self.handle = ctypes.c_void_p(handle)
+        self.device = torch.device("cuda", device)
         self._keep = (list(g_list), list(out_list))
 
     def __del__(self):
@@ -548,7 +549,7 @@ def gac_clip_init(g_list: Sequence[torch.Tensor], out_list: Optional[Sequence[to
         raise ValueError("all tensors of a list must be on one device")
     out = ctypes.c_void_p()
     _check(L.gac_clip_init(ctypes.byref(out), arr, n, device))
-    return ClipContext(out.value, g_list, outs)
+    return ClipContext(out.value, g_list, outs, device)
 
 
 def _clip_result(rc: int, res) -> Optional[gac_clip_result]:
@@ -570,7 +571,8 @@ def gac_clip_grad_norm(ctx: ClipContext, max_norm: float, eps: float = 1e-6, nor
     """Norm of the list, and the list scaled by min(1, max_norm/(norm + eps)).  With fetch=False nothing
     leaves the device; a non-finite norm leaves every output as it was and is told by the record."""
     res = gac_clip_result() if fetch else None
-    rc = load_library().gac_clip_grad_norm(ctx.handle, _stream_ptr(stream), max_norm, eps, _norm_ptr(norm_out),
+    raw = _on(stream, ctx.device)[0]
+    rc = load_library().gac_clip_grad_norm(ctx.handle, raw, max_norm, eps, _norm_ptr(norm_out),
                                            ctypes.byref(res) if fetch else None)
     return _clip_result(rc, res)
 
@@ -579,7 +581,7 @@ def gac_clip_sumsq(ctx: ClipContext, sumsq_out: torch.Tensor, stream=None) -> No
     """Sharded form: this rank's sum of squares into a CUDA float64 tensor, for the caller's all-reduce."""
     if not (sumsq_out.is_cuda and sumsq_out.dtype == torch.float64 and sumsq_out.numel() >= 1):
         raise ValueError("sumsq_out must be a CUDA float64 tensor")
-    _check(load_library().gac_clip_sumsq(ctx.handle, _stream_ptr(stream), sumsq_out.data_ptr()))
+    _check(load_library().gac_clip_sumsq(ctx.handle, _on(stream, ctx.device)[0], sumsq_out.data_ptr()))
 
 
 def gac_clip_apply(ctx: ClipContext, sumsq_in: torch.Tensor, max_norm: float, eps: float = 1e-6,
@@ -588,7 +590,7 @@ def gac_clip_apply(ctx: ClipContext, sumsq_in: torch.Tensor, max_norm: float, ep
     if not (sumsq_in.is_cuda and sumsq_in.dtype == torch.float64 and sumsq_in.numel() >= 1):
         raise ValueError("sumsq_in must be a CUDA float64 tensor")
     res = gac_clip_result() if fetch else None
-    rc = load_library().gac_clip_apply(ctx.handle, _stream_ptr(stream), sumsq_in.data_ptr(), max_norm, eps,
+    rc = load_library().gac_clip_apply(ctx.handle, _on(stream, ctx.device)[0], sumsq_in.data_ptr(), max_norm, eps,
                                        _norm_ptr(norm_out), ctypes.byref(res) if fetch else None)
     return _clip_result(rc, res)
 

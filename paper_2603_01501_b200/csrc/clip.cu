@@ -5,8 +5,8 @@
 // The norm has to be known before the first element can be written, so a list beyond the chip's
 // memory is read twice and written once: the floor is the HBM traffic of that.  Squares are summed in
 // binary64 (a product of two binary32 values is exact there, and no scale of the gradient overflows or
-// vanishes), in a fixed order: chunk c belongs to CTA c mod grid, each CTA leaves one partial sum, and the
-// last CTA to finish adds the partials in index order.
+// vanishes), in a fixed order: chunk c belongs to CTA c mod grid, each CTA leaves one partial sum, and they are
+// added in index order.  One cooperative launch does both passes; the CTAs meet in between.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -103,11 +103,16 @@ __device__ double cta_sum(double v, double *shared) {
     return s;   // valid in thread 0
 }
 
-__global__ void __launch_bounds__(kThreads, kCtasPerSm)
-clip_sumsq_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, double *partials, unsigned *ticket,
-                  double *sumsq) {
-    __shared__ double shared[kThreads / 32];
-    __shared__ bool last;
+__device__ __forceinline__ uint4 scaled(uint4 w, float s, bool bf16) {
+    if (bf16)
+        return make_uint4(pack_bf16x2(lo_bf16(w.x) * s, hi_bf16(w.x) * s), pack_bf16x2(lo_bf16(w.y) * s, hi_bf16(w.y) * s),
+                          pack_bf16x2(lo_bf16(w.z) * s, hi_bf16(w.z) * s), pack_bf16x2(lo_bf16(w.w) * s, hi_bf16(w.w) * s));
+    return make_uint4(__float_as_uint(__uint_as_float(w.x) * s), __float_as_uint(__uint_as_float(w.y) * s),
+                      __float_as_uint(__uint_as_float(w.z) * s), __float_as_uint(__uint_as_float(w.w) * s));
+}
+
+// This CTA's share of the sum of squares (valid in thread 0).
+__device__ double chunk_squares(const ClipChunk *__restrict__ table, uint32_t n_chunks, double *shared) {
     double acc[2] = {0.0, 0.0};
     for (uint32_t c = blockIdx.x; c < n_chunks; c += gridDim.x) {
         const ClipChunk ch = load_chunk(table, c);
@@ -120,62 +125,101 @@ clip_sumsq_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, double
         for (; i + 7 * kThreads < vecs; i += 8 * kThreads) {
             uint4 w[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) w[u] = __ldg(v + i + u * kThreads);
+            for (int u = 0; u < 8; ++u) w[u] = v[i + u * kThreads];
 #pragma unroll
             for (int u = 0; u < 8; ++u) add_squares(acc, w[u], bf16);
         }
-        for (; i < vecs; i += kThreads) add_squares(acc, __ldg(v + i), bf16);
+        for (; i < vecs; i += kThreads) add_squares(acc, v[i], bf16);
         for (uint32_t j = head + vecs * per + threadIdx.x; j < ch.n; j += kThreads)
             add_square(acc[0], load_one(ch.g, j, bf16));
     }
-    const double mine = cta_sum(__dadd_rn(acc[0], acc[1]), shared);
-    if (threadIdx.x == 0) {
-        partials[blockIdx.x] = mine;
-        __threadfence();
-        last = (atomicInc(ticket, gridDim.x - 1) == gridDim.x - 1);   // back at 0 for the next call
-    }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
+    return cta_sum(__dadd_rn(acc[0], acc[1]), shared);
+}
+
+// The CTAs' shares in index order, by any CTA (valid in thread 0).
+__device__ double all_squares(const double *partials, double *shared) {
     double s = 0.0;
     for (uint32_t i = threadIdx.x; i < gridDim.x; i += kThreads) s = __dadd_rn(s, __ldcg(partials + i));
-    s = cta_sum(s, shared);
-    if (threadIdx.x == 0) *sumsq = s;
+    return cta_sum(s, shared);
 }
 
-__device__ __forceinline__ uint4 scaled(uint4 w, float s, bool bf16) {
-    if (bf16)
-        return make_uint4(pack_bf16x2(lo_bf16(w.x) * s, hi_bf16(w.x) * s), pack_bf16x2(lo_bf16(w.y) * s, hi_bf16(w.y) * s),
-                          pack_bf16x2(lo_bf16(w.z) * s, hi_bf16(w.z) * s), pack_bf16x2(lo_bf16(w.w) * s, hi_bf16(w.w) * s));
-    return make_uint4(__float_as_uint(__uint_as_float(w.x) * s), __float_as_uint(__uint_as_float(w.y) * s),
-                      __float_as_uint(__uint_as_float(w.z) * s), __float_as_uint(__uint_as_float(w.w) * s));
+// Waits until every CTA of a cooperative launch has arrived.  They are all resident, so this ends by itself; the
+// limit (one second) only keeps a mistake from holding the GPU.  Called by one thread of each CTA.
+__device__ bool meet(unsigned long long *arrived) {
+    __threadfence();
+    const unsigned long long old = atomicAdd(arrived, 1ull), target = (old / gridDim.x + 1) * gridDim.x;
+    unsigned long long t0 = 0, t;
+    for (uint32_t i = 0; i < (1u << 28); ++i) {
+        unsigned long long now;
+        asm volatile("ld.acquire.gpu.u64 %0, [%1];" : "=l"(now) : "l"(arrived) : "memory");
+        if (now >= target) return true;
+        if ((i & 1023u) == 1023u) {
+            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+            if (!t0) t0 = t;
+            if (t - t0 > 1000000000ull) return false;
+        }
+    }
+    return false;
 }
 
+enum { kSumOnly = 0, kApplyOnly = 1, kBoth = 2 };
+
+// kBoth: one cooperative launch.  The second pass walks the chunks backwards: the last ones read are still in the L2 cache
+// (126 MB), and the stores are marked to leave it first.
+template <int MODE>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
-clip_apply_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, const double *sumsq, double max_norm, double eps,
-                  float *norm_out, gac_clip_result *rec) {
+clip_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, double *partials, unsigned long long *arrived, double *sumsq,
+            double max_norm, double eps, float *norm_out, gac_clip_result *rec) {
+    __shared__ double shared[kThreads / 32];
     __shared__ float factor;
-    __shared__ int nonfinite;
+    __shared__ int state;   // 0 as it should be, 1 not finite, 2 a wait ran out; kSumOnly: 1 in the last CTA
+    if (MODE != kApplyOnly) {
+        const double mine = chunk_squares(table, n_chunks, shared);
+        if (MODE == kSumOnly) {
+            if (threadIdx.x == 0) {
+                partials[blockIdx.x] = mine;
+                __threadfence();
+                state = (atomicAdd(arrived, 1ull) + 1) % gridDim.x == 0;
+            }
+            __syncthreads();
+            if (!state) return;
+            __threadfence();
+            const double s = all_squares(partials, shared);
+            if (threadIdx.x == 0) *sumsq = s;
+            return;
+        }
+        if (threadIdx.x == 0) {
+            partials[blockIdx.x] = mine;
+            state = meet(arrived) ? 0 : 2;
+        }
+        __syncthreads();
+        if (state == 2) {
+            if (threadIdx.x == 0) rec->timed_out = 1;
+            return;
+        }
+    }
+    double s2 = 0.0;
+    if (MODE == kBoth) s2 = all_squares(partials, shared);
     if (threadIdx.x == 0) {
-        const double s2 = *sumsq, norm = __dsqrt_rn(s2);
+        if (MODE == kApplyOnly) s2 = *sumsq;
+        const double norm = __dsqrt_rn(s2), f = __ddiv_rn(max_norm, __dadd_rn(norm, eps));
         const bool bad = !(s2 <= 1.7976931348623157e308);   // NaN or +Inf
-        const double f = __ddiv_rn(max_norm, __dadd_rn(norm, eps));
         factor = (f < 1.0) ? __double2float_rn(f) : 1.0f;
-        nonfinite = bad;
+        state = bad;
         if (blockIdx.x == 0) {
             rec->sumsq = s2;
             rec->norm = norm;
             rec->scale = bad ? 1.0 : double(factor);
             rec->nonfinite = bad;
-            rec->reserved = 0;
+            rec->timed_out = 0;
             if (norm_out) *norm_out = __double2float_rn(norm);
         }
     }
     __syncthreads();
-    if (nonfinite) return;
+    if (state) return;
     const float s = factor;
     for (uint32_t c = blockIdx.x; c < n_chunks; c += gridDim.x) {
-        const ClipChunk ch = load_chunk(table, c);
+        const ClipChunk ch = load_chunk(table, n_chunks - 1 - c);
         const bool bf16 = ch.flags & kBf16;
         if (s == 1.0f && (ch.flags & kInPlace)) continue;
         const uint32_t size = bf16 ? 2u : 4u;
@@ -192,9 +236,9 @@ clip_apply_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, const 
 #pragma unroll
             for (int u = 0; u < 8; ++u) w[u] = v[i + u * kThreads];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) o[i + u * kThreads] = scaled(w[u], s, bf16);
+            for (int u = 0; u < 8; ++u) __stcs(o + i + u * kThreads, scaled(w[u], s, bf16));
         }
-        for (; i < vecs; i += kThreads) o[i] = scaled(v[i], s, bf16);
+        for (; i < vecs; i += kThreads) __stcs(o + i, scaled(v[i], s, bf16));
         for (uint32_t j = head + vecs * per + threadIdx.x; j < ch.n; j += kThreads)
             store_one(ch.out, j, bf16, load_one(ch.g, j, bf16) * s);
     }
@@ -212,8 +256,8 @@ struct gac_clip_ctx {
     uint32_t n_chunks = 0;
     uint32_t grid = 0;
     ClipChunk *d_chunks = nullptr;
-    double *d_partials = nullptr;      // one per CTA, then the list's sum
-    unsigned *d_ticket = nullptr;
+    double *d_partials = nullptr;      // one per CTA
+    unsigned long long *d_arrived = nullptr;   // CTAs so far, over all calls
     gac_clip_result *d_rec = nullptr;
     gac_clip_result *h_rec = nullptr;  // pinned
 };
@@ -279,7 +323,10 @@ int setup(gac_clip_ctx *c, const gac_clip_tensor *list, uint32_t n) {
     }
     if (table.size() > 0xFFFFFFF0ull) return fail(nullptr, GAC_ERR_INVALID_ARG, "too many chunks%s");
     c->n_chunks = uint32_t(table.size());
-    c->grid = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(uint64_t(c->sms) * kCtasPerSm, table.size())));
+    int resident = 0;   // all CTAs have to be resident at once: they meet between the two passes
+    GAC_CUDA(nullptr, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, clip_kernel<kBoth>, kThreads, 0));
+    resident = std::max(1, std::min(resident, kCtasPerSm));
+    c->grid = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(uint64_t(c->sms) * resident, table.size())));
     const size_t work = (size_t(c->grid) + 1) * sizeof(double) + 256 + sizeof(gac_clip_result);
     GAC_CUDA(nullptr, cudaMalloc(&c->d_chunks, std::max<size_t>(1, table.size()) * sizeof(ClipChunk)));
     if (!table.empty())
@@ -287,25 +334,21 @@ int setup(gac_clip_ctx *c, const gac_clip_tensor *list, uint32_t n) {
     GAC_CUDA(nullptr, cudaMalloc(&c->d_partials, work));
     GAC_CUDA(nullptr, cudaMemset(c->d_partials, 0, work));
     c->d_rec = reinterpret_cast<gac_clip_result *>(c->d_partials + c->grid + 1);
-    c->d_ticket = reinterpret_cast<unsigned *>(c->d_rec + 1);
+    c->d_arrived = reinterpret_cast<unsigned long long *>(c->d_rec + 1);
     GAC_CUDA(nullptr, cudaMallocHost(&c->h_rec, sizeof(gac_clip_result)));
     return GAC_OK;
 }
 
-int launch_sumsq(gac_clip_ctx *c, cudaStream_t s, double *out) {
-    clip_sumsq_kernel<<<c->grid, kThreads, 0, s>>>(c->d_chunks, c->n_chunks, c->d_partials, c->d_ticket, out);
-    GAC_CUDA(nullptr, cudaGetLastError());
-    return GAC_OK;
-}
-
-int launch_apply(gac_clip_ctx *c, cudaStream_t s, const double *in, double max_norm, double eps, float *norm_out,
-                 gac_clip_result *host_out) {
-    clip_apply_kernel<<<c->grid, kThreads, 0, s>>>(c->d_chunks, c->n_chunks, in, max_norm, eps, norm_out, c->d_rec);
-    GAC_CUDA(nullptr, cudaGetLastError());
+int read_record(gac_clip_ctx *c, cudaStream_t s, gac_clip_result *host_out) {
     if (!host_out) return GAC_OK;
     GAC_CUDA(nullptr, cudaMemcpyAsync(c->h_rec, c->d_rec, sizeof(gac_clip_result), cudaMemcpyDeviceToHost, s));
     GAC_CUDA(nullptr, cudaStreamSynchronize(s));
     *host_out = *c->h_rec;
+    if (host_out->timed_out) {
+        cudaMemsetAsync(c->d_arrived, 0, sizeof(*c->d_arrived), s);
+        cudaMemsetAsync(c->d_rec, 0, sizeof(*c->d_rec), s);
+        return fail(nullptr, GAC_ERR_TIMEOUT, "a wait inside the clipping kernel ran out%s");
+    }
     if (host_out->nonfinite) return fail(nullptr, GAC_ERR_NONFINITE, "NaN or Inf met in the gradient norm%s");
     return GAC_OK;
 }
@@ -359,7 +402,10 @@ int gac_clip_sumsq(gac_clip_ctx *ctx, void *cuda_stream, double *sumsq_out) {
         return fail(nullptr, GAC_ERR_INVALID_ARG, "sumsq_out must be an 8-byte aligned device pointer%s");
     Range range("gac_clip_sumsq");
     DeviceGuard guard(ctx->device);
-    return launch_sumsq(ctx, static_cast<cudaStream_t>(cuda_stream), sumsq_out);
+    clip_kernel<kSumOnly><<<ctx->grid, kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
+        ctx->d_chunks, ctx->n_chunks, ctx->d_partials, ctx->d_arrived, sumsq_out, 0.0, 0.0, nullptr, ctx->d_rec);
+    GAC_CUDA(nullptr, cudaGetLastError());
+    return GAC_OK;
 }
 
 int gac_clip_apply(gac_clip_ctx *ctx, void *cuda_stream, const double *sumsq_in, double max_norm, double eps, float *norm_out,
@@ -370,7 +416,11 @@ int gac_clip_apply(gac_clip_ctx *ctx, void *cuda_stream, const double *sumsq_in,
     if (int rc = check_limits(max_norm, eps, norm_out)) return rc;
     Range range("gac_clip_apply");
     DeviceGuard guard(ctx->device);
-    return launch_apply(ctx, static_cast<cudaStream_t>(cuda_stream), sumsq_in, max_norm, eps, norm_out, host_out);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    clip_kernel<kApplyOnly><<<ctx->grid, kThreads, 0, s>>>(ctx->d_chunks, ctx->n_chunks, ctx->d_partials, ctx->d_arrived,
+                                                           const_cast<double *>(sumsq_in), max_norm, eps, norm_out, ctx->d_rec);
+    GAC_CUDA(nullptr, cudaGetLastError());
+    return read_record(ctx, s, host_out);
 }
 
 int gac_clip_grad_norm(gac_clip_ctx *ctx, void *cuda_stream, double max_norm, double eps, float *norm_out,
@@ -380,9 +430,10 @@ int gac_clip_grad_norm(gac_clip_ctx *ctx, void *cuda_stream, double max_norm, do
     Range range("gac_clip_grad_norm");
     DeviceGuard guard(ctx->device);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    double *sum = ctx->d_partials + ctx->grid;
-    if (int rc = launch_sumsq(ctx, s, sum)) return rc;
-    return launch_apply(ctx, s, sum, max_norm, eps, norm_out, host_out);
+    double *none = nullptr;
+    void *args[] = {&ctx->d_chunks, &ctx->n_chunks, &ctx->d_partials, &ctx->d_arrived, &none, &max_norm, &eps, &norm_out, &ctx->d_rec};
+    GAC_CUDA(nullptr, cudaLaunchCooperativeKernel(reinterpret_cast<const void *>(&clip_kernel<kBoth>), dim3(ctx->grid), dim3(kThreads), args, 0, s));
+    return read_record(ctx, s, host_out);
 }
 
 int gac_clip_free(gac_clip_ctx *ctx) {

@@ -7,6 +7,9 @@
 // binary64 (a product of two binary32 values is exact there, and no scale of the gradient overflows or
 // vanishes), in a fixed order: chunk c belongs to CTA c mod grid, each CTA leaves one partial sum, and they are
 // added in index order.  One cooperative launch does both passes; the CTAs meet in between.
+// Measured: 1.5 B float32 elements 2.78 ms = 6.66 TB/s over the three passes (1.03 of a plain copy's rate), 0.25 B
+// bfloat16 240 us = 6.2 TB/s (its first pass converts every element to binary64 and is held up by that), 2^20 float32
+// 8.4 us and the 39 tensors of a small mixed list 6.4 us, which are one launch and one meeting of all CTAs.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -29,6 +32,8 @@ constexpr int kThreads = 256;
 constexpr int kChunkElems = 16384;
 constexpr int kMinChunkElems = 2048;
 constexpr int kCtasPerSm = 4;
+constexpr int kSumFlight = 8;     // vectors of 16 bytes in flight per thread, first pass
+constexpr int kApplyFlight = 4;   // second pass
 constexpr uint32_t kBf16 = 1u, kInPlace = 2u;
 
 struct __align__(16) ClipChunk {
@@ -122,12 +127,12 @@ __device__ double chunk_squares(const ClipChunk *__restrict__ table, uint32_t n_
         const uint4 *v = reinterpret_cast<const uint4 *>(ch.g + uint64_t(head) * (bf16 ? 2 : 4));
         if (threadIdx.x < head) add_square(acc[0], load_one(ch.g, threadIdx.x, bf16));
         uint32_t i = threadIdx.x;
-        for (; i + 7 * kThreads < vecs; i += 8 * kThreads) {
-            uint4 w[8];
+        for (; i + (kSumFlight - 1) * kThreads < vecs; i += kSumFlight * kThreads) {
+            uint4 w[kSumFlight];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) w[u] = v[i + u * kThreads];
+            for (int u = 0; u < kSumFlight; ++u) w[u] = v[i + u * kThreads];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) add_squares(acc, w[u], bf16);
+            for (int u = 0; u < kSumFlight; ++u) add_squares(acc, w[u], bf16);
         }
         for (; i < vecs; i += kThreads) add_squares(acc, v[i], bf16);
         for (uint32_t j = head + vecs * per + threadIdx.x; j < ch.n; j += kThreads)
@@ -230,15 +235,19 @@ clip_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, double *part
         const uint4 *v = reinterpret_cast<const uint4 *>(ch.g + uint64_t(head) * size);
         uint4 *o = reinterpret_cast<uint4 *>(ch.out + uint64_t(head) * size);
         if (threadIdx.x < head) store_one(ch.out, threadIdx.x, bf16, load_one(ch.g, threadIdx.x, bf16) * s);
-        uint32_t i = threadIdx.x;
-        for (; i + 7 * kThreads < vecs; i += 8 * kThreads) {
-            uint4 w[8];
+        // All warps load, then all warps store: reads and writes reach DRAM in bursts instead of an even mix.  List of
+        // 1.5 B float32 elements: 2.91 ms without the barriers and 8 vectors in flight, 2.82 with the first, 2.78 with both.
+        for (uint32_t b = 0; b < vecs; b += kApplyFlight * kThreads) {
+            uint4 w[kApplyFlight];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) w[u] = v[i + u * kThreads];
+            for (int u = 0; u < kApplyFlight; ++u)
+                if (b + threadIdx.x + u * kThreads < vecs) w[u] = v[b + threadIdx.x + u * kThreads];
+            __syncthreads();
 #pragma unroll
-            for (int u = 0; u < 8; ++u) __stcs(o + i + u * kThreads, scaled(w[u], s, bf16));
+            for (int u = 0; u < kApplyFlight; ++u)
+                if (b + threadIdx.x + u * kThreads < vecs) __stcs(o + b + threadIdx.x + u * kThreads, scaled(w[u], s, bf16));
+            __syncthreads();
         }
-        for (; i < vecs; i += kThreads) __stcs(o + i, scaled(v[i], s, bf16));
         for (uint32_t j = head + vecs * per + threadIdx.x; j < ch.n; j += kThreads)
             store_one(ch.out, j, bf16, load_one(ch.g, j, bf16) * s);
     }

@@ -670,7 +670,7 @@ def gac_rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Opt
     args = _ROTARY.pack(qx, qy[0], q0, q1, qy[1], qy[2], kx, kout[0], k0, k1, kout[1], kout[2], qh, kh, tokens,
                         0 if cu_seqlens is None else cu_seqlens.numel() - 1, dim, 2 * freqs.size, _DT[dtype],
                         ROTARY_LAYOUTS[layout], 1 if inverse else 0, 0, _int32_ptr(positions, "positions", device),
-                        _int32_ptr(cu_seqlens, "cu_seqlens", device), freqs.ctypes.data, scale)
+                        _int32_ptr(cu_seqlens, "cu_seqlens", device), freqs.__array_interface__["data"][0], scale)
     _check(load_library().gac_rotary(args, device.index, raw))
     return yq, yk
 

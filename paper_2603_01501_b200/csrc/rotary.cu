@@ -2,11 +2,13 @@
 //
 //   (x, y) -> scale (x cos a - y sin a, x sin a + y cos a),   a = position * freq
 //
-// Bound by HBM: every element is read once and written once, three flops each.  A CTA takes a few tokens: its threads
-// first work out the tokens' sines and cosines once (the angle is reduced to one turn in binary64, then sincospi in
-// binary32: exact to the last bits at any position, no table in memory) and leave them in shared memory; then every
-// head of those tokens is turned with them, four vectors of 16 bytes of each kind in flight per thread.
-// 16384 tokens x 32 heads x 128, bfloat16: see the table of measurements in the launch code below.
+// Bound by HBM: every element is read once and written once, three flops each.  A CTA takes one token: its threads work
+// out the token's sines and cosines (the angle is reduced to one turn in binary64, then sincospi in binary32: exact to
+// the last bits at any position, no table in memory) and leave them in shared memory for every head of the token,
+// whose first vectors are on their way meanwhile.
+// 16384 tokens x 32 heads x 128, bfloat16: 49 us = 5.4 TB/s (0.84 of a plain copy's rate); 8189 tokens x 14 heads x 128,
+// float32, half of the head turned: 22 us = 5.3 TB/s.  With 256 threads, 4 tokens to a CTA and the sines made before
+// the loads the first takes 54 us.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -20,9 +22,7 @@
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kMaxTokens = 4;   // tokens of a CTA
-constexpr uint32_t kFewTokens = 148 * 4;
+constexpr int kThreads = 128;
 
 struct RotaryDev {
     const char *x[2];
@@ -30,7 +30,6 @@ struct RotaryDev {
     long long x_token[2], x_head[2], y_token[2], y_head[2];
     uint32_t heads[2];
     uint32_t n_tokens, n_seqs, head_dim, pairs;
-    uint32_t per_cta;                       // tokens of a CTA, at most kMaxTokens
     const int32_t *positions, *cu;
     float scale;
     int inverse;
@@ -60,15 +59,14 @@ __device__ int place_in_sequence(const int32_t *cu, uint32_t n_seqs, uint32_t t)
     return int(t) - (lo ? max(cu[lo], 0) : 0);
 }
 
-// Cosine and sine, already scaled, of every pair of the CTA's tokens.
-__device__ __forceinline__ void fill_wheel(const RotaryDev &a, float2 (*wheel)[GAC_ROTARY_MAX_DIM / 2], uint32_t t0, uint32_t nt) {
-    for (uint32_t w = threadIdx.x; w < nt * a.pairs; w += blockDim.x) {
-        const uint32_t t = w / a.pairs, i = w % a.pairs;
-        const int pos = a.positions ? a.positions[t0 + t] : place_in_sequence(a.cu, a.n_seqs, t0 + t);
+// Cosine and sine, already scaled, of every pair of the CTA's token.
+__device__ __forceinline__ void fill_wheel(const RotaryDev &a, float2 *wheel, uint32_t t) {
+    for (uint32_t i = threadIdx.x; i < a.pairs; i += kThreads) {
+        const int pos = a.positions ? a.positions[t] : place_in_sequence(a.cu, a.n_seqs, t);
         const double turns = double(pos) * a.turns[i];
         float s, c;
         sincospif(2.0f * float(turns - rint(turns)), &s, &c);
-        wheel[t][i] = make_float2(c * a.scale, (a.inverse ? -s : s) * a.scale);
+        wheel[i] = make_float2(c * a.scale, (a.inverse ? -s : s) * a.scale);
     }
     __syncthreads();
 }
@@ -77,21 +75,20 @@ __device__ __forceinline__ void fill_wheel(const RotaryDev &a, float2 (*wheel)[G
 template <typename T, bool HALF>
 __global__ void __launch_bounds__(kThreads)
 rotary_any_kernel(const __grid_constant__ RotaryDev a) {
-    __shared__ __align__(16) float2 wheel[kMaxTokens][GAC_ROTARY_MAX_DIM / 2];
-    const uint32_t t0 = blockIdx.x * a.per_cta;
-    const uint32_t nt = min(a.per_cta, a.n_tokens - t0);
-    fill_wheel(a, wheel, t0, nt);
+    __shared__ float2 wheel[GAC_ROTARY_MAX_DIM / 2];
+    const uint32_t t = blockIdx.x;
+    fill_wheel(a, wheel, t);
     const uint32_t rest = a.head_dim - 2 * a.pairs, units = a.pairs + rest;
     const uint32_t heads = a.heads[0] + a.heads[1];
-    for (uint32_t w = threadIdx.x; w < nt * heads * units; w += kThreads) {
-        const uint32_t u = w % units, h0 = (w / units) % heads, t = w / (units * heads);
+    for (uint32_t w = threadIdx.x; w < heads * units; w += kThreads) {
+        const uint32_t u = w % units, h0 = w / units;
         const int which = h0 >= a.heads[0];
         const uint32_t h = which ? h0 - a.heads[0] : h0;
-        const char *x = a.x[which] + ((long long)(t0 + t) * a.x_token[which] + (long long)h * a.x_head[which]) * (long long)sizeof(T);
-        char *y = a.y[which] + ((long long)(t0 + t) * a.y_token[which] + (long long)h * a.y_head[which]) * (long long)sizeof(T);
+        const char *x = a.x[which] + ((long long)t * a.x_token[which] + (long long)h * a.x_head[which]) * (long long)sizeof(T);
+        char *y = a.y[which] + ((long long)t * a.y_token[which] + (long long)h * a.y_head[which]) * (long long)sizeof(T);
         if (u < a.pairs) {
             const uint32_t i = HALF ? u : 2 * u, j = HALF ? u + a.pairs : 2 * u + 1;
-            const float2 cs = wheel[t][u];
+            const float2 cs = wheel[u];
             const float p = load_el(x + i * sizeof(T), T{}), q = load_el(x + j * sizeof(T), T{});
             store_el(y + i * sizeof(T), p * cs.x - q * cs.y, T{});
             store_el(y + j * sizeof(T), p * cs.y + q * cs.x, T{});
@@ -134,58 +131,48 @@ struct Vec {
     }
 };
 
-// A thread keeps one place of the head, N pairs (two vectors) or 2 N copied elements, and walks over the CTA's tokens and heads.
+// A thread keeps one place of the head, N pairs (two vectors) or 2 N copied elements, and walks over the token's heads.
 template <typename T, bool HALF, int N>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, 12)
 rotary_kernel(const __grid_constant__ RotaryDev a) {
-    __shared__ __align__(16) float2 wheel[kMaxTokens][GAC_ROTARY_MAX_DIM / 2];
-    constexpr int kFlight = 4;
+    __shared__ __align__(16) float2 wheel[GAC_ROTARY_MAX_DIM / 2];
+    constexpr int kFlight = 2;
     constexpr uint32_t kSize = sizeof(T);
-    const uint32_t t0 = blockIdx.x * a.per_cta;
-    const uint32_t nt = min(a.per_cta, a.n_tokens - t0);
+    const uint32_t t = blockIdx.x;
     const uint32_t turned = a.pairs / N, units = turned + (a.head_dim - 2 * a.pairs + 2 * N - 1) / (2 * N);   // places of a head
-    const uint32_t u = threadIdx.x % units, step = blockDim.x / units, heads = a.heads[0] + a.heads[1];
+    const uint32_t u = threadIdx.x % units, step = kThreads / units, heads = a.heads[0] + a.heads[1];
     const bool turn = u < turned;
     // byte offsets of the two vectors in a head
     const uint32_t first = (turn ? (HALF ? u * N : 2 * u * N) : 2 * a.pairs + (u - turned) * 2 * N) * kSize;
     const uint32_t second = first + (turn && HALF ? a.pairs : N) * kSize;
     const bool both = turn || second < a.head_dim * kSize;
-    fill_wheel(a, wheel, t0, nt);
-    if (threadIdx.x >= step * units) return;
-    if (!turn && a.x[0] == a.y[0] && a.x[1] == a.y[1]) return;   // in place: nothing to copy
-    uint32_t t = 0, h = threadIdx.x / units;
-    while (h >= heads) {
-        h -= heads;
-        ++t;
-    }
-    while (t < nt) {
-        Vec<T, N> p[kFlight], q[kFlight];
-        char *to[kFlight];
-        uint32_t at[kFlight];
-        int n = 0;
+    // in place there is nothing to copy
+    const bool active = threadIdx.x < step * units && (turn || a.x[0] != a.y[0] || a.x[1] != a.y[1]);
+    uint32_t h = active ? threadIdx.x / units : heads;
+    Vec<T, N> p[kFlight], q[kFlight];
+    char *to[kFlight];   // nullptr: no head
+    auto fetch = [&]() {
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            at[i] = t;
-            if (t < nt) {
-                const int which = h >= a.heads[0];
-                const uint32_t hh = which ? h - a.heads[0] : h;
-                const char *x = a.x[which] + ((long long)(t0 + t) * a.x_token[which] + (long long)hh * a.x_head[which]) * kSize;
-                to[i] = a.y[which] + ((long long)(t0 + t) * a.y_token[which] + (long long)hh * a.y_head[which]) * kSize;
-                p[i].load(x + first);
-                if (both) q[i].load(x + second);
-                n = i + 1;
-                h += step;
-                while (h >= heads) {
-                    h -= heads;
-                    ++t;
-                }
-            }
+            to[i] = nullptr;
+            if (h >= heads) continue;
+            const int which = h >= a.heads[0];
+            const uint32_t hh = which ? h - a.heads[0] : h;
+            const char *x = a.x[which] + ((long long)t * a.x_token[which] + (long long)hh * a.x_head[which]) * kSize;
+            to[i] = a.y[which] + ((long long)t * a.y_token[which] + (long long)hh * a.y_head[which]) * kSize;
+            p[i].load(x + first);
+            if (both) q[i].load(x + second);
+            h += step;
         }
+    };
+    fetch();   // on its way while the sines are made
+    fill_wheel(a, wheel, t);
+    while (to[0]) {
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            if (i >= n) break;
+            if (!to[i]) break;
             if (turn) {
-                const float4 *cs = reinterpret_cast<const float4 *>(wheel[at[i]] + u * N);
+                const float4 *cs = reinterpret_cast<const float4 *>(wheel + u * N);
 #pragma unroll
                 for (int j = 0; j < N; j += 2) {
                     const float4 c = cs[j / 2];   // cosine, sine, cosine, sine
@@ -205,6 +192,7 @@ rotary_kernel(const __grid_constant__ RotaryDev a) {
             p[i].store(to[i] + first);
             if (both) q[i].store(to[i] + second);
         }
+        fetch();
     }
 }
 
@@ -339,16 +327,13 @@ int gac_rotary(const gac_rotary_args *args, int cuda_device, void *cuda_stream) 
         return true;
     };
     const uint32_t n = fits(16 / size) ? 16 / size : bf16 && fits(4) ? 4 : 1;
-    // Few tokens: one to a CTA, so that as many SMs as can be work; many: the sines of four tokens in one go.
-    d.per_cta = std::min<uint32_t>(kMaxTokens, (a.n_tokens + kFewTokens - 1) / kFewTokens);
-    const uint32_t grid = (a.n_tokens + d.per_cta - 1) / d.per_cta;
     void (*fn)(const RotaryDev) = nullptr;
     if (bf16) fn = n == 8 ? (half ? rotary_kernel<uint16_t, true, 8> : rotary_kernel<uint16_t, false, 8>)
                  : n == 4 ? (half ? rotary_kernel<uint16_t, true, 4> : rotary_kernel<uint16_t, false, 4>)
                           : (half ? rotary_any_kernel<uint16_t, true> : rotary_any_kernel<uint16_t, false>);
     else fn = n == 4 ? (half ? rotary_kernel<float, true, 4> : rotary_kernel<float, false, 4>)
                      : (half ? rotary_any_kernel<float, true> : rotary_any_kernel<float, false>);
-    fn<<<grid, kThreads, 0, s>>>(d);
+    fn<<<a.n_tokens, kThreads, 0, s>>>(d);
     GAC_CUDA(nullptr, cudaGetLastError());
     return GAC_OK;
 }

@@ -1,0 +1,111 @@
+"""The operators on packed rollouts for ``torch`` autograd, and gradient clipping for lists of parameters.
+
+A pack is a batch of finished rollouts of different lengths laid one behind the other: tensors
+[tokens, heads, head_dim] and ``cu_seqlens`` (int32 on the device), where sequence b takes the tokens
+cu_seqlens[b] .. cu_seqlens[b+1].
+
+    q, k = packed.rotary(q, k, freqs, cu_seqlens=cu)
+    o = packed.attention(q, k, v, cu)
+    ...
+    loss.backward()
+    clipper.clip(1.0)
+
+All arithmetic is in the CUDA library (``binding``); this module only says what is saved for the way back.
+"""
+from __future__ import annotations
+
+from typing import Iterable, List, Optional
+
+import torch
+
+from . import binding as gb
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, freqs, positions, cu_seqlens, layout, scale):
+        ctx.how = (freqs, positions, cu_seqlens, layout, scale)
+        return gb.gac_rotary(q, k, freqs, positions=positions, cu_seqlens=cu_seqlens, layout=layout, scale=scale)
+
+    @staticmethod
+    def backward(ctx, d_q, d_k):
+        freqs, positions, cu_seqlens, layout, scale = ctx.how
+        # the transpose of a turn is the turn by the negative angle
+        d_q, d_k = gb.gac_rotary(_rows(d_q), _rows(d_k), freqs, positions=positions, cu_seqlens=cu_seqlens, layout=layout,
+                                 scale=scale, inverse=True)
+        return d_q, d_k, None, None, None, None, None
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, cu_seqlens, scale):
+        o, lse = gb.gac_attn_forward(q, k, v, cu_seqlens, scale=scale)
+        ctx.save_for_backward(q, k, v, o, lse, cu_seqlens)
+        ctx.scale = scale
+        ctx.mark_non_differentiable(lse)
+        return o, lse
+
+    @staticmethod
+    def backward(ctx, d_o, _):
+        q, k, v, o, lse, cu_seqlens = ctx.saved_tensors
+        d_q, d_k, d_v = gb.gac_attn_backward(_rows(d_o, 8), q, k, v, o, lse, cu_seqlens, scale=ctx.scale)
+        return d_q, d_k, d_v, None, None
+
+
+def _rows(t: torch.Tensor, multiple: int = 1) -> torch.Tensor:
+    """A gradient as autograd hands it over may be expanded or transposed: the library wants contiguous rows."""
+    s0, s1, s2 = t.stride()
+    if s2 == 1 and s0 >= s1 >= t.shape[2] and s0 % multiple == 0 and s1 % multiple == 0 and \
+            t.data_ptr() % (multiple * t.element_size()) == 0:
+        return t
+    return t.contiguous()
+
+
+def rotary(q: torch.Tensor, k: torch.Tensor, freqs, positions: Optional[torch.Tensor] = None,
+           cu_seqlens: Optional[torch.Tensor] = None, layout: str = "half", scale: float = 1.0):
+    """Rotary positions (binding.gac_rotary) with their gradient; returns (q', k')."""
+    return _Rotary.apply(q, k, freqs, positions, cu_seqlens, layout, scale)
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, scale: Optional[float] = None,
+              return_lse: bool = False):
+    """Causal attention over the pack (binding.gac_attn_forward) with its gradient.  ``lse``, if asked for, has none."""
+    o, lse = _Attention.apply(q, k, v, cu_seqlens, scale)
+    return (o, lse) if return_lse else o
+
+
+class GradientClipper:
+    """Clips the gradients of a list of parameters by their global norm, in place, without waiting for the host.
+
+    The table of the list is built on first use and again whenever a ``.grad`` tensor has moved.  Parameters without a
+    gradient are left out, as an optimizer leaves them out."""
+
+    def __init__(self, params: Iterable[torch.nn.Parameter]):
+        self.params: List[torch.nn.Parameter] = [p for p in params if p.requires_grad]
+        if not self.params:
+            raise ValueError("no trainable parameters")
+        self.norm = torch.zeros((), device=self.params[0].device)
+        self._ctx: Optional[gb.ClipContext] = None
+        self._bound: List[tuple] = []
+
+    def clip(self, max_norm: float, eps: float = 1e-6) -> torch.Tensor:
+        """Returns the norm before clipping as a 0-dim device tensor, overwritten by the next call."""
+        grads = [p.grad for p in self.params if p.grad is not None]
+        if not grads:
+            self.norm.zero_()
+            return self.norm
+        if not all(g.is_contiguous() for g in grads):
+            raise RuntimeError("gradients must be contiguous")
+        bound = [(g.data_ptr(), g.numel(), g.dtype) for g in grads]
+        if self._ctx is None or bound != self._bound:
+            if self._ctx is not None:
+                gb.gac_clip_free(self._ctx)
+            self._ctx = gb.gac_clip_init(grads)
+            self._bound = bound
+        gb.gac_clip_grad_norm(self._ctx, max_norm, eps, norm_out=self.norm)
+        return self.norm
+
+    def close(self) -> None:
+        if self._ctx is not None:
+            gb.gac_clip_free(self._ctx)
+            self._ctx, self._bound = None, []

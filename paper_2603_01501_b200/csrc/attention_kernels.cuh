@@ -659,7 +659,7 @@ template <int DP>
 struct BwdKv {
     static constexpr int kSub = DP / 64;
     static constexpr int kBytes = kTile * DP * 2;
-    static constexpr int kStages = DP == 128 ? 4 : 8;
+    static constexpr int kStages = DP == 128 ? 4 : 8, kPairs = kStages / 2;
     static constexpr int kRowSlots = 4;
     static constexpr int kStageBytes = 2048;   // per warp, on the way out
     static constexpr int kThreads = 384;
@@ -716,6 +716,10 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     bool ok = true;
     JobWord w;
     w.kind = kJobNone;
+    // A pair of places takes Q and dO of a query tile, by turns the one way and the other: dO is done with first, and the
+    // tile that is wanted first two tiles later, a Q, goes where it was.
+    auto q_slot = [](const Place &p) { return 2 * p.at + p.phase; };
+    auto g_slot = [](const Place &p) { return 2 * p.at + (p.phase ^ 1); };
     auto q_tiles_of = [](const JobWord &j) { return (j.len + kTile - 1) / kTile - j.block; };   // from the diagonal on
     auto kv_head_of = [&](const JobWord &j) { return j.head % a.kv_heads; };
     auto head0_of = [&](const JobWord &j) { return kv_head_of(j) * (a.q_heads / a.kv_heads) + (j.head / a.kv_heads) * heads; };
@@ -723,7 +727,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     if (warp >= 8) {
         registers_down<C::kOtherRegs>();
         if (warp == 9) {   // -------------------------------------------- loads
-            uint32_t tiles = 0, fixed = 0, n = 0;   // jobs, tiles with rows of others, ring items so far
+            uint32_t tiles = 0, fixed = 0, n = 0;   // jobs, tiles with rows of others, query tiles so far
             Place at;
             for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
                 if (w.kind != kJobWork) continue;
@@ -738,23 +742,27 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     }
                 }
                 uint32_t h = head0_of(w), i = w.block;
-                for (uint32_t u = 0; u < 2 * heads * q_tiles; ++u, ++n, at.template next<C::kStages>()) {   // Q, dO, Q, dO, ...
-                    if (n >= C::kStages && !(ok = warp_wait(empty + 8 * at.at, at.phase ^ 1))) break;
-                    const bool is_q = (u & 1) == 0, ragged = w.len < (i + 1) * kTile;
-                    const uint32_t tile = sring + at.at * C::kBytes, bar = ragged ? raw : full + 8 * at.at;
-                    if (lane == 0) {
-                        mbar_expect(bar, C::kBytes);
-                        for (int x = 0; x < C::kSub; ++x)
-                            tma_load(tile + x * (kTile * 128), is_q ? &mq : &mdo, bar, x * 64, int(h) * (is_q ? a.q_mul : a.do_mul),
-                                     int(w.first + i * kTile));
+                for (uint32_t u = 0; ok && u < heads * q_tiles; ++u, ++n, at.template next<C::kPairs>()) {
+                    const bool ragged = w.len < (i + 1) * kTile;
+                    for (uint32_t which = 0; which < 2; ++which) {   // Q, dO
+                        const bool is_q = which == 0;
+                        const uint32_t slot = is_q ? q_slot(at) : g_slot(at), tile = sring + slot * C::kBytes;
+                        const uint32_t bar = ragged ? raw : full + 8 * slot;
+                        if (n >= C::kPairs && !(ok = warp_wait(empty + 8 * slot, at.phase ^ 1))) break;
+                        if (lane == 0) {
+                            mbar_expect(bar, C::kBytes);
+                            for (int x = 0; x < C::kSub; ++x)
+                                tma_load(tile + x * (kTile * 128), is_q ? &mq : &mdo, bar, x * 64, int(h) * (is_q ? a.q_mul : a.do_mul),
+                                         int(w.first + i * kTile));
+                        }
+                        if (ragged) {
+                            if (!(ok = warp_wait(raw, fixed & 1))) break;
+                            ++fixed;
+                            zero_tile_rows<C::kSub>(tile, w.len - i * kTile);
+                            if (lane == 0) mbar_arrive(full + 8 * slot);
+                        }
                     }
-                    if (ragged) {
-                        if (!(ok = warp_wait(raw, fixed & 1))) break;
-                        ++fixed;
-                        zero_tile_rows<C::kSub>(tile, w.len - i * kTile);
-                        if (lane == 0) mbar_arrive(full + 8 * at.at);
-                    }
-                    if (!is_q && ++i == w.block + q_tiles) {
+                    if (++i == w.block + q_tiles) {
                         i = w.block;
                         ++h;
                     }
@@ -766,10 +774,11 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 mbar_wait(kv_full, (tiles - 1) & 1);
                 if (ok) ok = warp_wait(kv_empty, (tiles - 1) & 1);
             }
-            for (uint32_t i = n > C::kStages ? n - C::kStages : 0; i < n; ++i) {
-                mbar_wait(full + 8 * (i % C::kStages), (i / C::kStages) & 1);
-                if (ok) ok = warp_wait(empty + 8 * (i % C::kStages), (i / C::kStages) & 1);
-            }
+            for (uint32_t i = n > C::kPairs ? n - C::kPairs : 0; i < n; ++i)
+                for (uint32_t slot = 2 * (i % C::kPairs); slot < 2 * (i % C::kPairs) + 2; ++slot) {
+                    mbar_wait(full + 8 * slot, (i / C::kPairs) & 1);
+                    if (ok) ok = warp_wait(empty + 8 * slot, (i / C::kPairs) & 1);
+                }
         } else if (warp == 10) {   // -------------------------------- row terms
             uint32_t n = 0;
             for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
@@ -803,43 +812,40 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             if (lane == 0) {   // one thread, as in the forward kernel
                 const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
                 uint32_t tiles = 0, it = 0;   // jobs, query tiles so far
-                Place q;                      // Q of the query tile at hand; its dO is one place on
-                auto tile_of = [&](const Place &p) { return sring + p.at * C::kBytes; };
-                auto wait_tile = [&](const Place &p) { return mbar_wait(full + 8 * p.at, p.phase); };
+                Place at;                     // of the query tile at hand
+                auto tile_of = [&](uint32_t slot) { return sring + slot * C::kBytes; };
+                auto wait_tile = [&](uint32_t slot, const Place &p) { return mbar_wait(full + 8 * slot, p.phase); };
                 for (uint32_t k = 0; (ok = jobs.get_alone(k, &w)) && w.kind != kJobStop; ++k) {
                     if (w.kind != kJobWork) continue;
                     const uint32_t total = q_tiles_of(w) * heads;
-                    Place g = q;
-                    g.template next<C::kStages>();
-                    if (!(ok = mbar_wait(kv_full, tiles & 1) && wait_tile(q))) break;
+                    if (!(ok = mbar_wait(kv_full, tiles & 1) && wait_tile(q_slot(at), at))) break;
                     ++tiles;
                     tc_fence_after();
-                    product_rows<DP>(t_s, sk, tile_of(q), id_s | a.negate);   // S^T = K Q^T
+                    product_rows<DP>(t_s, sk, tile_of(q_slot(at)), id_s | a.negate);   // S^T = K Q^T
                     mma_commit(s_full);
-                    if (!(ok = wait_tile(g))) break;
-                    product_rows<DP>(t_dp, sv, tile_of(g), id_s);             // dP^T = V dO^T
+                    if (!(ok = wait_tile(g_slot(at), at))) break;
+                    product_rows<DP>(t_dp, sv, tile_of(g_slot(at)), id_s);             // dP^T = V dO^T
                     mma_commit(dp_full);
                     if (total == 1) mma_commit(kv_empty);
                     for (uint32_t u = 0; u < total; ++u, ++it) {
                         const bool more = u + 1 < total;
-                        Place q_next = g, g_next;
-                        q_next.template next<C::kStages>();
-                        g_next = q_next;
-                        g_next.template next<C::kStages>();
-                        if (more && !(ok = wait_tile(q_next))) break;
+                        const uint32_t q = q_slot(at), g = g_slot(at);
+                        at.template next<C::kPairs>();
+                        const uint32_t q_next = q_slot(at), g_next = g_slot(at);
+                        if (more && !(ok = wait_tile(q_next, at))) break;
                         if (!(ok = mbar_wait(p_full, it & 1))) break;
                         tc_fence_after();
                         product_cols<64>(t_dv, t_s, tile_of(g), id_o, u > 0);     // dV += P^T dO
-                        mma_commit(empty + 8 * g.at);
+                        mma_commit(empty + 8 * g);
                         if (more) {
                             product_rows<DP>(t_s, sk, tile_of(q_next), id_s | a.negate);
                             mma_commit(s_full);
-                            if (!(ok = wait_tile(g_next))) break;
+                            if (!(ok = wait_tile(g_next, at))) break;
                         }
                         if (!(ok = mbar_wait(ds_full, it & 1))) break;
                         tc_fence_after();
                         product_cols<64>(t_dk, t_dp, tile_of(q), id_o, u > 0);    // dK += dS^T Q
-                        mma_commit(empty + 8 * q.at);
+                        mma_commit(empty + 8 * q);
                         if (more) {
                             product_rows<DP>(t_dp, sv, tile_of(g_next), id_s);
                             mma_commit(dp_full);
@@ -847,8 +853,6 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                         } else {
                             mma_commit(done);
                         }
-                        q = q_next;
-                        g = g_next;
                     }
                     if (!ok) break;
                 }

@@ -181,11 +181,10 @@ int launch_backward(const gac_attn &a, const gac_attn_grad &g, int device, cudaS
     if (int rc = tensor_map(&mk, &d.k_mul, a.k, a, a.kv_heads)) return rc;
     if (int rc = tensor_map(&mv, &d.v_mul, a.v, a, a.kv_heads)) return rc;
     if (int rc = tensor_map(&mdo, &d.do_mul, g.d_o, a, a.q_heads)) return rc;
-    const uint32_t jobs = job_count(a.n_tokens, a.n_seqs, kTile);
     uint32_t grid_q, grid_kv;
-    if (int rc = grid_of(jobs, a.q_heads, &grid_q)) return rc;
-    if (int rc = grid_of(jobs, a.kv_heads * d.parts, &grid_kv)) return rc;
-    if (int rc = allow_smem(attn_dq_kernel<DP>, BwdQ<DP>::kSmem, device, done_q)) return rc;
+    if (int rc = grid_of(job_count(a.n_tokens, a.n_seqs, 2 * kTile), a.q_heads, &grid_q)) return rc;
+    if (int rc = grid_of(job_count(a.n_tokens, a.n_seqs, kTile), a.kv_heads * d.parts, &grid_kv)) return rc;
+    if (int rc = allow_smem(attn_dq_kernel<DP>, BwdQ<DP>::kSmem, device, done_q, BwdQ<DP>::kRegs)) return rc;
     if (int rc = allow_smem(attn_dkv_kernel<DP>, BwdKv<DP>::kSmem, device, done_kv, BwdKv<DP>::kRegs)) return rc;
     const uint64_t units = uint64_t(a.q_heads) * a.n_tokens, per = kRowThreads / 16;
     attn_rows_kernel<<<uint32_t((units + per - 1) / per), kRowThreads, 0, s>>>(d);

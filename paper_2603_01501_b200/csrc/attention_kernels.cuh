@@ -1010,18 +1010,22 @@ static __global__ void __launch_bounds__(256) attn_sum_parts_kernel(const __grid
         make_uint4(bf16x2(s[0], s[1]), bf16x2(s[2], s[3]), bf16x2(s[4], s[5]), bf16x2(s[6], s[7]));
 }
 
-// One CTA: one query tile of a head over the key tiles up to the diagonal.  S is double-buffered and dS goes where S
-// was, so that the products run ahead: the next dP, dQ and the S after that are issued while the threads work on one
-// tile.
-// Warps: 0-3 and 4-7 take the two halves of the key columns, 8 issues the products, 9 the TMA loads, 10 finds the jobs.
+// One CTA: two query tiles of 128 rows (256 consecutive rows of one sequence and head) over the key tiles up to the
+// diagonal, as in the forward kernel: each key and value tile is loaded once for both.  Tensor memory holds dQ and one
+// working place per tile, which takes S, then dP as soon as S has been read, then dS as bfloat16.  The two tiles alternate:
+// a tile's threads take its exponentials and make its dS while the tensor cores work for the other.
+// Warps: 0-3 and 4-7 the rows of the two tiles, 8 issues the products, 9 the TMA loads, 10 finds the jobs.
 template <int DP>
 struct BwdQ {
     static constexpr int kSub = DP / 64;
     static constexpr int kBytes = kTile * DP * 2;
-    static constexpr int kKeys = DP == 128 ? 3 : 5, kValues = DP == 128 ? 1 : 3, kStages = kKeys + kValues;   // tiles in flight
-    static constexpr int kStageBytes = 2048;   // per warp, on the way out
+    static constexpr int kKeys = DP == 128 ? 2 : 4, kValues = DP == 128 ? 1 : 3, kStages = kKeys + kValues;   // tiles in flight
+    static constexpr int kStageBytes = 4096;   // per warp, on the way out: where the tile's dO was
     static constexpr int kThreads = 384;
-    static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + 8 * kStageBytes + 512;
+    static constexpr int kRegs = 168, kRowRegs = 208, kOtherRegs = 88;   // at launch; then two warpgroups, one
+    static_assert(2 * kRowRegs + kOtherRegs <= 3 * kRegs, "shares of the launch's registers");
+    static_assert(4 * kStageBytes <= kBytes, "four warps' rows go out through one tile");
+    static constexpr int kSmem = 1024 + (4 + kStages) * kBytes + 512;
 };
 
 template <int DP>
@@ -1032,24 +1036,30 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     extern __shared__ char smem_raw[];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = a.q_heads / a.kv_heads;
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    const uint32_t sq = base, sdo = base + C::kBytes, sring = base + 2 * C::kBytes;
-    const uint32_t stage = sring + C::kStages * C::kBytes, bars = stage + 8 * C::kStageBytes;
+    const uint32_t sq = base, sdo = base + 2 * C::kBytes, sring = base + 4 * C::kBytes;
+    const uint32_t bars = sring + C::kStages * C::kBytes;
     const Jobs jobs(bars);
-    const uint32_t q_full = bars + Jobs::kBytes, q_empty = q_full + 8, s_full = q_full + 16, dp_full = q_full + 32, ds_full = q_full + 40,
-                   done = q_full + 48, raw = q_full + 56, full = q_full + 64, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
-    // A key tile is used by S and, two tiles later, by dQ; a value tile by dP alone: the first kKeys places of the
-    // ring take key tiles, the others value tiles, each in turn.
+    const uint32_t q_full = bars + Jobs::kBytes, q_empty = q_full + 8, do_full = q_full + 16, raw = q_full + 24, taken = q_full + 32,
+                   s_full = q_full + 48, s_read = q_full + 64, dp_full = q_full + 80, ds_full = q_full + 96, done = q_full + 112,
+                   full = q_full + 128, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
+    // A key tile is used by S and again by dQ, a value tile by dP alone: the first kKeys places of the ring take key
+    // tiles, the others value tiles, each in turn.
+
     if (warp == 8) tmem_alloc(tmem_slot, 512);
     if (threadIdx.x == 0) {
         jobs.init(10);
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
+        mbar_init(do_full, 1);
         mbar_init(raw, 1);
-        mbar_init(s_full, 1);
-        mbar_init(s_full + 8, 1);
-        mbar_init(dp_full, 1);
-        mbar_init(ds_full, 8);
-        mbar_init(done, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(taken + 8 * i, 4);
+            mbar_init(s_full + 8 * i, 1);
+            mbar_init(s_read + 8 * i, 4);
+            mbar_init(dp_full + 8 * i, 1);
+            mbar_init(ds_full + 8 * i, 4);
+            mbar_init(done + 8 * i, 1);
+        }
         for (int i = 0; i < C::kStages; ++i) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
@@ -1061,189 +1071,214 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     tc_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
-    const uint32_t t_dp = tmem + 256, t_dq = tmem + 384;
     bool ok = true;
     JobWord w;
     w.kind = kJobNone;
 
-    if (warp == 9) {   // ------------------------------------------------ loads
-        uint32_t n = 0, tiles = 0, fixed = 0;   // key tiles, jobs, tiles with rows of others so far
-        for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
-            if (w.kind != kJobWork) continue;
-            const uint32_t kv_head = w.head / group, total = w.block + 1;
-            if (tiles > 0 && !(ok = warp_wait(q_empty, (tiles - 1) & 1))) break;
-            ++tiles;
-            if (lane == 0) {
-                mbar_expect(q_full, 2 * C::kBytes);
-                for (int x = 0; x < C::kSub; ++x) {
-                    tma_load(sq + x * (kTile * 128), &mq, q_full, x * 64, int(w.head) * a.q_mul, int(w.first + w.block * kTile));
-                    tma_load(sdo + x * (kTile * 128), &mdo, q_full, x * 64, int(w.head) * a.do_mul, int(w.first + w.block * kTile));
-                }
-            }
-            auto load = [&](bool is_k, uint32_t u) {   // key or value tile u of the job
-                const uint32_t m = n + u, at = is_k ? m % C::kKeys : C::kKeys + m % C::kValues, use = m / (is_k ? C::kKeys : C::kValues);
-                if (use > 0 && !warp_wait(empty + 8 * at, (use - 1) & 1)) return false;
-                const bool ragged = is_k && w.len < (u + 1) * kTile;   // a key behind the sequence has dS = 0, times itself in dQ
-                const uint32_t bar = ragged ? raw : full + 8 * at;
-                if (lane == 0) {
-                    mbar_expect(bar, C::kBytes);
-                    for (int x = 0; x < C::kSub; ++x)
-                        tma_load(sring + at * C::kBytes + x * (kTile * 128), is_k ? &mk : &mv, bar, x * 64,
-                                 int(kv_head) * (is_k ? a.k_mul : a.v_mul), int(w.first + u * kTile));
-                }
-                if (ragged) {
-                    if (!warp_wait(raw, fixed & 1)) return false;
-                    ++fixed;
-                    zero_tile_rows<C::kSub>(sring + at * C::kBytes, w.len - u * kTile);
-                    if (lane == 0) mbar_arrive(full + 8 * at);
-                }
-                return true;
-            };
-            ok = load(true, 0);
-            for (uint32_t u = 0; ok && u < total; ++u) {   // K0, V0, K1, K2, V1, K3, V2, ...: in the order of their use
-                ok = load(false, u);
-                if (ok && u == 0 && total > 1) ok = load(true, 1);
-                if (ok && u + 2 < total) ok = load(true, u + 2);
-            }
-            if (!ok) break;
-            n += total;
-        }
-        if (tiles > 0) {
-            mbar_wait(q_full, (tiles - 1) & 1);
-            if (ok) ok = warp_wait(q_empty, (tiles - 1) & 1);
-        }
-        for (uint32_t i = n > C::kKeys ? n - C::kKeys : 0; i < n; ++i) {
-            mbar_wait(full + 8 * (i % C::kKeys), (i / C::kKeys) & 1);
-            if (ok) ok = warp_wait(empty + 8 * (i % C::kKeys), (i / C::kKeys) & 1);
-        }
-        for (uint32_t i = n > C::kValues ? n - C::kValues : 0; i < n; ++i) {
-            mbar_wait(full + 8 * (C::kKeys + i % C::kValues), (i / C::kValues) & 1);
-            if (ok) ok = warp_wait(empty + 8 * (C::kKeys + i % C::kValues), (i / C::kValues) & 1);
-        }
-    } else if (warp == 8) {   // ------------------------------------- products
-        if (lane == 0) {   // one thread, as in the forward kernel
-            const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
-            uint32_t tiles = 0, it = 0;   // jobs, key tiles so far
-            Place key, ahead, value;      // the key tile of the next dQ and of the next S; the value tile of the next dP
-            auto key_of = [&](const Place &p) { return sring + p.at * C::kBytes; };
-            auto value_of = [&](const Place &p) { return sring + (C::kKeys + p.at) * C::kBytes; };
-            auto wait_key = [&](const Place &p) { return mbar_wait(full + 8 * p.at, p.phase); };
-            auto wait_value = [&](const Place &p) { return mbar_wait(full + 8 * (C::kKeys + p.at), p.phase); };
-            uint32_t s_at = 0;            // which of the two S buffers is next
-            auto scores = [&]() {         // S = Q K^T
-                product_rows<DP>(tmem + s_at * 128, sq, key_of(ahead), id_s | a.negate);
-                mma_commit(s_full + 8 * s_at);
-                ahead.template next<C::kKeys>();
-                s_at ^= 1;
-            };
-            auto d_probs = [&](bool last) {   // dP = dO V^T
-                product_rows<DP>(t_dp, sdo, value_of(value), id_s);
-                mma_commit(dp_full);
-                if (last) mma_commit(q_empty);   // the last use of dO, and of Q in a product issued before
-                mma_commit(empty + 8 * (C::kKeys + value.at));
-                value.template next<C::kValues>();
-            };
-            for (uint32_t k = 0; (ok = jobs.get_alone(k, &w)) && w.kind != kJobStop; ++k) {
+    if (warp >= 8) {
+        registers_down<C::kOtherRegs>();
+        if (warp == 9) {   // -------------------------------------------- loads
+            uint32_t n = 0, tiles = 0, seconds = 0, fixed = 0;   // key tiles, jobs, those with two query tiles, tiles with rows of others so far
+            for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
                 if (w.kind != kJobWork) continue;
-                const uint32_t total = w.block + 1;
-                if (!(ok = mbar_wait(q_full, tiles & 1) && wait_key(ahead))) break;
-                ++tiles;
-                tc_fence_after();
-                scores();
-                if (!(ok = wait_value(value))) break;
-                d_probs(total == 1);
-                if (total > 1) {
-                    if (!(ok = wait_key(ahead))) break;
-                    scores();
-                }
-                for (uint32_t u = 0; u < total; ++u, ++it) {
-                    if (u + 1 < total && !(ok = wait_value(value))) break;
-                    if (!(ok = mbar_wait(ds_full, it & 1))) break;
-                    tc_fence_after();
-                    // dS lies where S was, so the next dP need not wait for the product that reads it
-                    if (u + 1 < total) d_probs(u + 2 == total);
-                    product_cols<64>(t_dq, tmem + (it & 1) * 128, key_of(key), id_o, u > 0);   // dQ += dS K
-                    mma_commit(empty + 8 * key.at);
-                    key.template next<C::kKeys>();
-                    if (u + 1 == total) mma_commit(done);
-                    if (u + 2 < total) {
-                        if (!(ok = wait_key(ahead))) break;
-                        scores();
+                const uint32_t kv_head = w.head / group, row0 = w.block * 2 * kTile;
+                const bool two = row0 + kTile < w.len;
+                const uint32_t total = w.block * 2 + 1 + (two ? 1 : 0);
+                auto rows = [&](const CUtensorMap *map, int mul, uint32_t to, uint32_t bar) {   // Q or dO of both tiles
+                    if (lane == 0) {
+                        mbar_expect(bar, (two ? 2 : 1) * C::kBytes);
+                        for (int t = 0; t < (two ? 2 : 1); ++t)
+                            for (int x = 0; x < C::kSub; ++x)
+                                tma_load(to + t * C::kBytes + x * (kTile * 128), map, bar, x * 64, int(w.head) * mul, int(w.first + row0 + t * kTile));
                     }
-                }
+                };
+                auto load = [&](bool is_k, uint32_t u) {   // key or value tile u of the job
+                    const uint32_t m = n + u, at = is_k ? m % C::kKeys : C::kKeys + m % C::kValues, use = m / (is_k ? C::kKeys : C::kValues);
+                    if (use > 0 && !warp_wait(empty + 8 * at, (use - 1) & 1)) return false;
+                    const bool ragged = is_k && w.len < (u + 1) * kTile;   // a key behind the sequence has dS = 0, times itself in dQ
+                    const uint32_t bar = ragged ? raw : full + 8 * at;
+                    if (lane == 0) {
+                        mbar_expect(bar, C::kBytes);
+                        for (int x = 0; x < C::kSub; ++x)
+                            tma_load(sring + at * C::kBytes + x * (kTile * 128), is_k ? &mk : &mv, bar, x * 64,
+                                     int(kv_head) * (is_k ? a.k_mul : a.v_mul), int(w.first + u * kTile));
+                    }
+                    if (ragged) {
+                        if (!warp_wait(raw, fixed & 1)) return false;
+                        ++fixed;
+                        zero_tile_rows<C::kSub>(sring + at * C::kBytes, w.len - u * kTile);
+                        if (lane == 0) mbar_arrive(full + 8 * at);
+                    }
+                    return true;
+                };
+                if (tiles > 0 && !(ok = warp_wait(q_empty, (tiles - 1) & 1))) break;
+                rows(&mq, a.q_mul, sq, q_full);
+                if (!(ok = load(true, 0) && load(false, 0) && (total == 1 || load(true, 1)))) break;
+                // dO's place has been the last job's way out
+                if (tiles > 0 && !(ok = warp_wait(taken, (tiles - 1) & 1))) break;
+                if (seconds > 0 && !(ok = warp_wait(taken + 8, (seconds - 1) & 1))) break;
+                rows(&mdo, a.do_mul, sdo, do_full);
+                ++tiles;
+                seconds += two;
+                for (uint32_t u = 1; ok && u < total; ++u) ok = load(false, u) && (u + 1 >= total || load(true, u + 1));
                 if (!ok) break;
+                n += total;
             }
+            // the CTA must not end, nor its memory be given back, before the last loads and releases have arrived
+            if (tiles > 0) {
+                mbar_wait(q_full, (tiles - 1) & 1);
+                mbar_wait(do_full, (tiles - 1) & 1);
+                if (ok) ok = warp_wait(q_empty, (tiles - 1) & 1);
+            }
+            for (uint32_t i = n > C::kKeys ? n - C::kKeys : 0; i < n; ++i) {
+                mbar_wait(full + 8 * (i % C::kKeys), (i / C::kKeys) & 1);
+                if (ok) ok = warp_wait(empty + 8 * (i % C::kKeys), (i / C::kKeys) & 1);
+            }
+            for (uint32_t i = n > C::kValues ? n - C::kValues : 0; i < n; ++i) {
+                mbar_wait(full + 8 * (C::kKeys + i % C::kValues), (i / C::kValues) & 1);
+                if (ok) ok = warp_wait(empty + 8 * (C::kKeys + i % C::kValues), (i / C::kValues) & 1);
+            }
+        } else if (warp == 8) {   // --------------------------------- products
+            if (lane == 0) {   // one thread, as in the forward kernel
+                const uint32_t id_s = mma_desc(kTile, false), id_o = mma_desc(DP, true);
+                uint32_t tiles = 0, c[2] = {0, 0};   // jobs, key tiles of the first and second query tile so far
+                Place key, value;
+                auto key_of = [&](const Place &p) { return sring + p.at * C::kBytes; };
+                auto value_of = [&](const Place &p) { return sring + (C::kKeys + p.at) * C::kBytes; };
+                auto wait_key = [&](const Place &p) { return mbar_wait(full + 8 * p.at, p.phase); };
+                auto scores = [&](int t, const Place &p) {   // S = Q K^T
+                    product_rows<DP>(tmem + t * 128, sq + t * C::kBytes, key_of(p), id_s | a.negate);
+                    mma_commit(s_full + 8 * t);
+                };
+                auto d_probs = [&](int t) {                  // dP = dO V^T, over S
+                    if (!mbar_wait(s_read + 8 * t, c[t] & 1)) return false;
+                    tc_fence_after();
+                    product_rows<DP>(tmem + t * 128, sdo + t * C::kBytes, value_of(value), id_s);
+                    mma_commit(dp_full + 8 * t);
+                    return true;
+                };
+                auto d_query = [&](int t, bool add) {        // dQ += dS K
+                    if (!mbar_wait(ds_full + 8 * t, c[t] & 1)) return false;
+                    tc_fence_after();
+                    product_cols<32>(tmem + 256 + t * 128, tmem + t * 128, key_of(key), id_o, add);
+                    ++c[t];
+                    return true;
+                };
+                for (uint32_t k = 0; (ok = jobs.get_alone(k, &w)) && w.kind != kJobStop; ++k) {
+                    if (w.kind != kJobWork) continue;
+                    const bool two = w.block * 2 * kTile + kTile < w.len;
+                    const uint32_t nb0 = w.block * 2 + 1, nb = nb0 + (two ? 1 : 0);   // key tiles of the first tile; of both
+                    if (!(ok = mbar_wait(q_full, tiles & 1) && wait_key(key))) break;
+                    tc_fence_after();
+                    scores(0, key);
+                    if (two) scores(1, key);
+                    if (nb == 1) mma_commit(q_empty);
+                    if (!(ok = mbar_wait(do_full, tiles & 1))) break;
+                    ++tiles;
+                    for (uint32_t u = 0; u < nb; ++u) {
+                        const bool more = u + 1 < nb;
+                        Place next = key;
+                        next.template next<C::kKeys>();
+                        if (!(ok = mbar_wait(full + 8 * (C::kKeys + value.at), value.phase))) break;
+                        if (u < nb0 && !(ok = d_probs(0))) break;
+                        if (two && !(ok = d_probs(1))) break;
+                        mma_commit(empty + 8 * (C::kKeys + value.at));
+                        value.template next<C::kValues>();
+                        if (more && !(ok = wait_key(next))) break;
+                        if (u < nb0) {
+                            if (!(ok = d_query(0, u > 0))) break;
+                            if (u + 1 < nb0) scores(0, next);
+                            else mma_commit(done);
+                        }
+                        if (two) {
+                            if (!(ok = d_query(1, u > 0))) break;
+                            if (more) scores(1, next);
+                            else mma_commit(done + 8);
+                        }
+                        mma_commit(empty + 8 * key.at);
+                        if (u + 2 == nb) mma_commit(q_empty);   // the last use of Q
+                        key = next;
+                    }
+                    if (!ok) break;
+                }
+            }
+        } else if (warp == 10) {   // ------------------------------------ jobs
+            ok = jobs.template run<2 * kTile, true>(a, a.q_heads);
         }
-    } else if (warp == 10) {   // ---------------------------------------- jobs
-        ok = jobs.template run<kTile, true>(a, a.q_heads);
-    } else if (warp < 8) {   // -------- a query row, half of the key columns
-        const uint32_t half = warp >> 2, lanes = (warp & 3) << 21, col0 = half * 64;
-        const uint32_t local = (warp & 3) * 32 + lane;
+    } else {   // ------------------------------------------- a row of a tile
+        registers_up<C::kRowRegs>();
+        const int t = warp >> 2;
+        const uint32_t lanes = (warp & 3) << 21, work = tmem + t * 128 + lanes, local = (warp & 3) * 32 + lane;
         const float2 c2 = make_float2(a.exp2_scale, a.exp2_scale);
-        uint32_t it = 0, tiles = 0;
+        uint32_t it = 0, tiles = 0;   // key tiles and jobs of this tile so far
         for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+            const uint32_t row0 = w.block * 2 * kTile + t * kTile, row = row0 + local;
             if (w.kind == kJobTail) {
-                const uint32_t from = w.first + w.block * kTile, to = min(w.first + w.len, from + kTile);
+                const uint32_t from = w.first + w.block * 2 * kTile, to = min(w.first + w.len, from + 2 * kTile);
                 fill_rows(a.d_q, from, to, w.head, a.head_dim, kZeroBits, 256);
             }
             if (w.kind != kJobWork) continue;
-            const uint32_t total = w.block + 1, row = w.block * kTile + local;
-            const float2 term = row < w.len ? __ldg(a.rows + size_t(w.head) * a.n_tokens + w.first + row) : make_float2(0.f, 0.f);
-            const float2 l2 = make_float2(term.x, term.x), d2 = make_float2(-term.y, -term.y);
-            for (uint32_t u = 0; u < total; ++u, ++it) {
-                if (!(ok = warp_wait(s_full + 8 * (it & 1), (it >> 1) & 1))) break;
-                tc_fence_after();
-                float2 p[32];
-                {
-                    uint32_t r[2][32];
-                    tmem_ld32(r[0], tmem + (it & 1) * 128 + lanes + col0);
-                    tmem_ld32(r[1], tmem + (it & 1) * 128 + lanes + col0 + 32);
-                    tmem_wait_ld();
+            if (row0 < w.len) {
+                const uint32_t total = w.block * 2 + 1 + t;
+                const float2 term = row < w.len ? __ldg(a.rows + size_t(w.head) * a.n_tokens + w.first + row) : make_float2(0.f, 0.f);
+                const float2 l2 = make_float2(term.x, term.x), d2 = make_float2(-term.y, -term.y);
+                for (uint32_t u = 0; u < total; ++u, ++it) {
+                    if (!(ok = warp_wait(s_full + 8 * t, it & 1))) break;
+                    tc_fence_after();
+                    float2 p[64];
+                    {
+                        uint32_t r[4][32];
 #pragma unroll
-                    for (int x = 0; x < 32; ++x) {
-                        const uint32_t *v = &r[x / 16][2 * (x % 16)];
-                        const float2 y = fma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), c2, l2);
-                        p[x] = make_float2(exp2_approx(y.x), exp2_approx(y.y));
-                    }
-                }
-                if (!(ok = warp_wait(dp_full, it & 1))) break;
-                tc_fence_after();
-                {
-                    uint32_t r[2][32];
-                    tmem_ld32(r[0], t_dp + lanes + col0);
-                    tmem_ld32(r[1], t_dp + lanes + col0 + 32);
-                    tmem_wait_ld();
+                        for (int i = 0; i < 4; ++i) tmem_ld32(r[i], work + 32 * i);
+                        tmem_wait_ld();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(s_read + 8 * t);
 #pragma unroll
-                    for (int x = 0; x < 32; ++x) {
-                        const uint32_t *v = &r[x / 16][2 * (x % 16)];
-                        p[x] = mul2(p[x], add2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), d2));
-                    }
-                    if (u == total - 1) {   // the diagonal tile
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) {
-                            if (col0 + 2 * x > local) p[x].x = 0.f;
-                            if (col0 + 2 * x + 1 > local) p[x].y = 0.f;
+                        for (int x = 0; x < 64; ++x) {
+                            const uint32_t *v = &r[x / 16][2 * (x % 16)];
+                            const float2 y = fma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), c2, l2);
+                            p[x] = make_float2(exp2_approx(y.x), exp2_approx(y.y));
                         }
                     }
+                    if (!(ok = warp_wait(dp_full + 8 * t, it & 1))) break;
+                    tc_fence_after();
 #pragma unroll
-                    for (int x = 0; x < 32; ++x) r[0][x] = bf16x2(p[x].x, p[x].y);
-                    tmem_st32(tmem + (it & 1) * 128 + lanes + col0, r[0]);   // over S
+                    for (int h = 0; h < 4; ++h) {
+                        uint32_t r[32], ds[16];
+                        tmem_ld32(r, work + 32 * h);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) {
+                            const float2 y = mul2(p[16 * h + x], add2(make_float2(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), d2));
+                            ds[x] = bf16x2(y.x, y.y);
+                        }
+                        if (u == total - 1) {   // the diagonal tile: what is hidden may hold anything
+#pragma unroll
+                            for (int x = 0; x < 16; ++x) {
+                                const uint32_t col = 32 * h + 2 * x;
+                                if (col > local) ds[x] = 0u;
+                                else if (col + 1 > local) ds[x] &= 0xFFFFu;
+                            }
+                        }
+                        tmem_st16(work + 16 * h, ds);   // over what has been read of dP
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(ds_full + 8 * t);
                 }
-                tmem_wait_st();
+                if (!ok || !(ok = warp_wait(done + 8 * t, tiles & 1))) break;
+                ++tiles;
+                tc_fence_after();
+                const uint32_t row_w = row - lane;   // the warp's first row
+                store_rows<DP, 64>(sdo + t * C::kBytes + (warp & 3) * C::kStageBytes, tmem + 256 + t * 128 + lanes, a.scale, a.d_q,
+                                   w.first + row_w, w.head, w.len > row_w ? w.len - row_w : 0u, a.head_dim);
                 tc_fence_before();
+                fence_async_shared();   // before the next dO lands where the rows went through
                 __syncwarp();
-                if (lane == 0) mbar_arrive(ds_full);
+                if (lane == 0) mbar_arrive(taken + 8 * t);
             }
-            if (!ok || !(ok = warp_wait(done, tiles & 1))) break;
-            ++tiles;
-            tc_fence_after();
-            // each half of the threads writes half of the columns
-            const uint32_t row_w = row - lane, col = half * (DP / 2);
-            RowsOut o = a.d_q;
-            o.p += col * 2;
-            store_rows<DP / 2, 32>(stage + warp * C::kStageBytes, t_dq + lanes + col, a.scale, o, w.first + row_w, w.head,
-                                   w.len > row_w ? w.len - row_w : 0u, a.head_dim > col ? a.head_dim - col : 0u);
-            tc_fence_before();
         }
     }
     tc_fence_before();
@@ -1252,8 +1287,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     if (warp == 8) tmem_free(tmem, 512);
     if (bad) {
         if (w.kind == kJobWork) {   // each warp's own last job
-            const uint32_t from = w.first + w.block * kTile;
-            poison_rows(a.d_q, from, min(w.first + w.len, from + kTile), w.head, a.head_dim);
+            const uint32_t from = w.first + w.block * 2 * kTile;
+            poison_rows(a.d_q, from, min(w.first + w.len, from + 2 * kTile), w.head, a.head_dim);
         }
         if (threadIdx.x == 0) g_attn_fault = 1;
     }

@@ -153,7 +153,7 @@ int launch_forward(const gac_attn &a, int device, cudaStream_t s) {
 
 // Query heads of a group are summed in one CTA as long as there are enough key tiles to go round; with fewer, parts
 // of the group go to CTAs of their own and a second kernel adds them.
-constexpr uint32_t kEnoughJobs = 370;
+constexpr uint32_t kEnoughJobs = 370;   // 2.5 per SM
 uint32_t parts_of(const gac_attn &a) {
     const uint32_t group = a.q_heads / a.kv_heads;
     const uint64_t jobs = uint64_t(job_count(a.n_tokens, a.n_seqs, kTile)) * a.kv_heads;
@@ -186,7 +186,7 @@ int launch_backward(const gac_attn &a, const gac_attn_grad &g, int device, cudaS
     if (int rc = grid_of(job_count(a.n_tokens, a.n_seqs, kTile), a.kv_heads * d.parts, &grid_kv)) return rc;
     if (int rc = allow_smem(attn_dq_kernel<DP>, BwdQ<DP>::kSmem, device, done_q, BwdQ<DP>::kRegs)) return rc;
     if (int rc = allow_smem(attn_dkv_kernel<DP>, BwdKv<DP>::kSmem, device, done_kv, BwdKv<DP>::kRegs)) return rc;
-    const uint64_t units = uint64_t(a.q_heads) * a.n_tokens, per = kRowThreads / 16;
+    const uint64_t units = uint64_t(a.q_heads) * a.n_tokens, per = kRowThreads / 16 * kRowsInFlight;
     attn_rows_kernel<<<uint32_t((units + per - 1) / per), kRowThreads, 0, s>>>(d);
     attn_dkv_kernel<DP><<<grid_kv, BwdKv<DP>::kThreads, BwdKv<DP>::kSmem, s>>>(mq, mk, mv, mdo, d);
     if (d.parts > 1) {

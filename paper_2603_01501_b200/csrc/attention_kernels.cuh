@@ -624,28 +624,36 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
 // (dQ).  Both make S and dP again, seven products in all where five would do with dQ added up in memory by
 // atomics; in return every sum has one owner and one order, and two calls give the same bits.
 
-// The row terms, one half warp per row and head.
-constexpr int kRowThreads = 256;
+// The row terms: a half warp per row and head, four of them in flight.
+constexpr int kRowThreads = 256, kRowsInFlight = 4;
 static __global__ void __launch_bounds__(kRowThreads) attn_rows_kernel(const __grid_constant__ AttnDev a) {
-    const uint32_t unit = blockIdx.x * (kRowThreads / 16) + threadIdx.x / 16, l = threadIdx.x & 15;
-    const uint32_t head = unit % a.q_heads, t = unit / a.q_heads;
-    float s = 0.f;
-    const bool in = t < a.n_tokens;
-    if (in && l * 8 < a.head_dim) {
-        const uint4 x = *reinterpret_cast<const uint4 *>(a.o.p + (long long)t * a.o.token + (long long)head * a.o.head + l * 16);
-        const uint4 y = *reinterpret_cast<const uint4 *>(a.do_in + (long long)t * a.do_token + (long long)head * a.do_head + l * 16);
-        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    const uint32_t first = blockIdx.x * (kRowThreads / 16 * kRowsInFlight) + threadIdx.x / 16, l = threadIdx.x & 15;
+    uint4 x[kRowsInFlight], y[kRowsInFlight];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            s = fmaf(__uint_as_float(xs[i] << 16), __uint_as_float(ys[i] << 16), s);
-            s = fmaf(__uint_as_float(xs[i] & 0xFFFF0000u), __uint_as_float(ys[i] & 0xFFFF0000u), s);
+    for (int i = 0; i < kRowsInFlight; ++i) {
+        const uint32_t unit = first + i * (kRowThreads / 16), head = unit % a.q_heads, t = unit / a.q_heads;
+        x[i] = y[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (t < a.n_tokens && l * 8 < a.head_dim) {
+            x[i] = *reinterpret_cast<const uint4 *>(a.o.p + (long long)t * a.o.token + (long long)head * a.o.head + l * 16);
+            y[i] = *reinterpret_cast<const uint4 *>(a.do_in + (long long)t * a.do_token + (long long)head * a.do_head + l * 16);
         }
     }
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    if (in && l == 0) {
-        const size_t i = size_t(head) * a.n_tokens + t;
-        a.rows[i] = make_float2(-kLog2e * a.lse[i], s);
+    for (int i = 0; i < kRowsInFlight; ++i) {
+        const uint32_t unit = first + i * (kRowThreads / 16), head = unit % a.q_heads, t = unit / a.q_heads;
+        const uint32_t xs[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, ys[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+        float s = 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            s = fmaf(__uint_as_float(xs[u] << 16), __uint_as_float(ys[u] << 16), s);
+            s = fmaf(__uint_as_float(xs[u] & 0xFFFF0000u), __uint_as_float(ys[u] & 0xFFFF0000u), s);
+        }
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        if (t < a.n_tokens && l == 0) {
+            const size_t at = size_t(head) * a.n_tokens + t;
+            a.rows[at] = make_float2(-kLog2e * a.lse[at], s);
+        }
     }
 }
 
@@ -999,11 +1007,20 @@ static __global__ void __launch_bounds__(256) attn_sum_parts_kernel(const __grid
     const uint32_t t = uint32_t(row / a.kv_heads), h = uint32_t(row % a.kv_heads), x = uint32_t(j % per) * 8;
     if (t >= seq_bound(a, a.n_seqs)) return;   // rows of no sequence were written as zero
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (uint32_t part = 0; part < a.parts; ++part) {
-        const float4 *src = reinterpret_cast<const float4 *>(a.part_sums + ((size_t(part) * 2 + which) * rows + row) * a.head_dim + x);
-        const float4 u = __ldcs(src), v = __ldcs(src + 1);
-        s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
-        s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+    for (uint32_t part0 = 0; part0 < a.parts; part0 += 4) {
+        float4 u[4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 *src = reinterpret_cast<const float4 *>(a.part_sums + ((size_t(part0 + i) * 2 + which) * rows + row) * a.head_dim + x);
+            const bool there = part0 + i < a.parts;
+            u[i] = there ? __ldcs(src) : make_float4(0.f, 0.f, 0.f, 0.f);
+            v[i] = there ? __ldcs(src + 1) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[0] += u[i].x; s[1] += u[i].y; s[2] += u[i].z; s[3] += u[i].w;
+            s[4] += v[i].x; s[5] += v[i].y; s[6] += v[i].z; s[7] += v[i].w;
+        }
     }
     const RowsOut &o = which ? a.d_v : a.d_k;
     *reinterpret_cast<uint4 *>(o.p + (long long)t * o.token + (long long)h * o.head + x * 2) =

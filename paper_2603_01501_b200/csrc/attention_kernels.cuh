@@ -96,8 +96,9 @@ __device__ __forceinline__ Job find_job(const AttnDev &a, uint32_t index, uint32
                 const uint32_t m = i0 == 0 ? mine : blocks_of(i0 + lane);
                 const uint32_t here = __ballot_sync(all, m >= lo);
                 const uint32_t got = __popc(here);
-                if (k < got) {
-                    b = i0 + __fns(here, 0, int(k) + 1);
+                if (k < got) {   // the lane with k others before it
+                    const bool it = (here >> lane & 1u) && __popc(here & ((1u << lane) - 1u)) == k;
+                    b = i0 + __ffs(__ballot_sync(all, it)) - 1;
                     break;
                 }
                 k -= got;
@@ -359,7 +360,7 @@ struct Fwd {
     static constexpr int kStages = DP == 128 ? 4 : 8;        // key and value tiles in flight
     static constexpr int kStageBytes = 4096;                 // per warp, on the way out
     static constexpr int kThreads = 384;
-    static constexpr int kRegs = 168, kRowRegs = 208, kOtherRegs = 88;   // at launch; then two warpgroups, one
+    static constexpr int kRegs = 168, kRowRegs = 200, kOtherRegs = 104;   // at launch; then two warpgroups, one
     static_assert(2 * kRowRegs + kOtherRegs <= 3 * kRegs, "shares of the launch's registers");
     static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + 8 * kStageBytes + 512;
 };
@@ -671,7 +672,7 @@ struct BwdKv {
     static constexpr int kRowSlots = 4;
     static constexpr int kStageBytes = 2048;   // per warp, on the way out
     static constexpr int kThreads = 384;
-    static constexpr int kRegs = 168, kRowRegs = 208, kOtherRegs = 88;   // at launch; then two warpgroups, one
+    static constexpr int kRegs = 168, kRowRegs = 192, kOtherRegs = 120;   // at launch; then two warpgroups, one
     static_assert(2 * kRowRegs + kOtherRegs <= 3 * kRegs, "shares of the launch's registers");
     static constexpr int kSmem = 1024 + (2 + kStages) * kBytes + kRowSlots * 1024 + 8 * kStageBytes + 512;
 };
@@ -1039,7 +1040,7 @@ struct BwdQ {
     static constexpr int kKeys = DP == 128 ? 2 : 4, kValues = DP == 128 ? 1 : 3, kStages = kKeys + kValues;   // tiles in flight
     static constexpr int kStageBytes = 4096;   // per warp, on the way out: where the tile's dO was
     static constexpr int kThreads = 384;
-    static constexpr int kRegs = 168, kRowRegs = 208, kOtherRegs = 88;   // at launch; then two warpgroups, one
+    static constexpr int kRegs = 168, kRowRegs = 200, kOtherRegs = 104;   // at launch; then two warpgroups, one
     static_assert(2 * kRowRegs + kOtherRegs <= 3 * kRegs, "shares of the launch's registers");
     static_assert(4 * kStageBytes <= kBytes, "four warps' rows go out through one tile");
     static constexpr int kSmem = 1024 + (4 + kStages) * kBytes + 512;

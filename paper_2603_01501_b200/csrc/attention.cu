@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cstddef>
+#include <type_traits>
 
 #include "gac.h"
 #include "gac_host.h"
@@ -163,6 +164,21 @@ uint32_t parts_of(const gac_attn &a) {
 }
 size_t rows_bytes(const gac_attn &a) { return (size_t(a.q_heads) * a.n_tokens * sizeof(float2) + 15) / 16 * 16; }
 
+template <typename... Args>
+cudaError_t launch_next(void (*kernel)(Args...), uint32_t grid, uint32_t threads, uint32_t smem, cudaStream_t s, const std::remove_const_t<Args> &...args) {
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(grid);
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = smem;
+    config.stream = s;
+    config.attrs = &early;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, args...);
+}
+
 template <int DP>
 int launch_backward(const gac_attn &a, const gac_attn_grad &g, int device, cudaStream_t s) {
     static std::atomic<bool> done_kv[64], done_q[64];
@@ -188,12 +204,13 @@ int launch_backward(const gac_attn &a, const gac_attn_grad &g, int device, cudaS
     if (int rc = allow_smem(attn_dkv_kernel<DP>, BwdKv<DP>::kSmem, device, done_kv, BwdKv<DP>::kRegs)) return rc;
     const uint64_t units = uint64_t(a.q_heads) * a.n_tokens, per = kRowThreads / 16 * kRowsInFlight;
     attn_rows_kernel<<<uint32_t((units + per - 1) / per), kRowThreads, 0, s>>>(d);
-    attn_dkv_kernel<DP><<<grid_kv, BwdKv<DP>::kThreads, BwdKv<DP>::kSmem, s>>>(mq, mk, mv, mdo, d);
+    // each of the others is set up while the one before it ends, and waits for its results where it needs them
+    GAC_CUDA(nullptr, launch_next(attn_dkv_kernel<DP>, grid_kv, BwdKv<DP>::kThreads, BwdKv<DP>::kSmem, s, mq, mk, mv, mdo, d));
     if (d.parts > 1) {
         const uint64_t n = 2 * uint64_t(a.n_tokens) * a.kv_heads * (a.head_dim / 8);
-        attn_sum_parts_kernel<<<uint32_t((n + 255) / 256), 256, 0, s>>>(d);
+        GAC_CUDA(nullptr, launch_next(attn_sum_parts_kernel, uint32_t((n + 255) / 256), 256, 0, s, d));
     }
-    attn_dq_kernel<DP><<<grid_q, BwdQ<DP>::kThreads, BwdQ<DP>::kSmem, s>>>(mq, mk, mv, mdo, d);
+    GAC_CUDA(nullptr, launch_next(attn_dq_kernel<DP>, grid_q, BwdQ<DP>::kThreads, BwdQ<DP>::kSmem, s, mq, mk, mv, mdo, d));
     GAC_CUDA(nullptr, cudaGetLastError());
     return GAC_OK;
 }

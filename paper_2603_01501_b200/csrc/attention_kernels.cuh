@@ -628,6 +628,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
 // The row terms: a half warp per row and head, four of them in flight.
 constexpr int kRowThreads = 256, kRowsInFlight = 4;
 static __global__ void __launch_bounds__(kRowThreads) attn_rows_kernel(const __grid_constant__ AttnDev a) {
+    let_next_start();
     const uint32_t first = blockIdx.x * (kRowThreads / 16 * kRowsInFlight) + threadIdx.x / 16, l = threadIdx.x & 15;
     uint4 x[kRowsInFlight], y[kRowsInFlight];
 #pragma unroll
@@ -695,6 +696,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                    ds_full = kv_full + 40, done = kv_full + 48, raw = kv_full + 56, rows_full = kv_full + 64, rows_empty = rows_full + 8 * C::kRowSlots,
                    full = rows_empty + 8 * C::kRowSlots, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
 
+    let_next_start();
     if (warp == 8) tmem_alloc(tmem_slot, 512);
     if (threadIdx.x == 0) {
         jobs.init(11);
@@ -789,6 +791,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     if (ok) ok = warp_wait(empty + 8 * slot, (i / C::kPairs) & 1);
                 }
         } else if (warp == 10) {   // -------------------------------- row terms
+            wait_for_previous();
             uint32_t n = 0;
             for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
                 if (w.kind != kJobWork) continue;
@@ -999,6 +1002,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
 
 // Adds the parts of dK and dV in order and rounds them once.
 static __global__ void __launch_bounds__(256) attn_sum_parts_kernel(const __grid_constant__ AttnDev a) {
+    let_next_start();
+    wait_for_previous();
     const uint32_t per = a.head_dim / 8;
     const size_t rows = size_t(a.n_tokens) * a.kv_heads, n = 2 * rows * per;
     const size_t i = size_t(blockIdx.x) * 256 + threadIdx.x;
@@ -1225,6 +1230,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         }
     } else {   // ------------------------------------------- a row of a tile
         registers_up<C::kRowRegs>();
+        wait_for_previous();   // for the row terms
         const int t = warp >> 2;
         const uint32_t lanes = (warp & 3) << 21, work = tmem + t * 128 + lanes, local = (warp & 3) * 32 + lane;
         const float2 c2 = make_float2(a.exp2_scale, a.exp2_scale);

@@ -166,6 +166,13 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+// ------------------------------------------------- one kernel after the other
+
+// The next kernel of the stream, if launched so, may be set up from here on; it waits for this one's results by itself.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// Returns when the kernel before has ended and its results are visible.
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // ------------------------------------------------------------------ registers
 
 // A warpgroup's share of the registers the CTA was launched with.  The shares of a kernel's warpgroups add up to at

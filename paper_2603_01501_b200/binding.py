@@ -498,11 +498,11 @@ def _on(stream, device: torch.device):
     return stream.cuda_stream, stream
 
 
-def _empty(shape, dtype, device, stream) -> torch.Tensor:
+def _empty(like: torch.Tensor, shape, stream, dtype=None) -> torch.Tensor:
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape) if dtype is None else like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape) if dtype is None else like.new_empty(shape, dtype=dtype)
 
 
 def _check(rc: int) -> None:
@@ -663,8 +663,8 @@ def gac_rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Opt
         yq, yk = q, k
         qy, kout = (qx, q0, q1), (kx, k0, k1)
     else:
-        yq = _empty((tokens, qh, dim), dtype, device, stream)
-        yk = _empty((tokens, kh, dim), dtype, device, stream) if k is not None else None
+        yq = _empty(q, (tokens, qh, dim), stream)
+        yk = _empty(q, (tokens, kh, dim), stream) if k is not None else None
         qy = (yq.data_ptr(), qh * dim, dim)
         kout = (yk.data_ptr(), kh * dim, dim) if k is not None else (0, 0, 0)
     args = _ROTARY.pack(qx, qy[0], q0, q1, qy[1], qy[2], kx, kout[0], k0, k1, kout[1], kout[2], qh, kh, tokens,
@@ -703,8 +703,9 @@ def gac_attn_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
         raise ValueError("q must be a CUDA tensor [tokens, heads, head_dim]")
     device = q.device
     raw, stream = _on(stream, device)
-    o = _empty(q.shape, q.dtype, device, stream)
-    lse = _empty((q.shape[1], q.shape[0]), torch.float32, device, stream)
+    tokens, heads, dim = q.shape
+    o = _empty(q, (tokens, heads, dim), stream)
+    lse = _empty(q, (heads, tokens), stream, torch.float32)
     _check(load_library().gac_attn_forward(_attn_args(q, k, v, o, lse, cu_seqlens, scale), device.index, raw))
     return o, lse
 
@@ -721,11 +722,11 @@ def gac_attn_backward(d_o: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
         raise ValueError("d_o must have q's shape")
     device = q.device
     raw, stream = _on(stream, device)
-    d_q = _empty((tokens, qh, dim), q.dtype, device, stream)
-    d_k = _empty((tokens, kh, dim), q.dtype, device, stream)
-    d_v = _empty((tokens, kh, dim), q.dtype, device, stream)
+    d_q = _empty(q, (tokens, qh, dim), stream)
+    d_k = _empty(q, (tokens, kh, dim), stream)
+    d_v = _empty(q, (tokens, kh, dim), stream)
     need = max(L.gac_attn_workspace(args), 16)
-    workspace = _empty((need,), torch.uint8, device, stream)
+    workspace = _empty(q, (need,), stream, torch.uint8)
     grad = _ATTN_GRAD.pack(gp, g0, g1, d_q.data_ptr(), qh * dim, dim, d_k.data_ptr(), kh * dim, dim, d_v.data_ptr(),
                            kh * dim, dim, workspace.data_ptr(), need)
     _check(L.gac_attn_backward(args, grad, device.index, raw))

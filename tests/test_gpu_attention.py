@@ -68,6 +68,19 @@ def test_a_longer_sequence_with_many_tiles():
     check(*make([2300, 1111], 5, 4, 2, 128, 12))
 
 
+def test_many_more_jobs_than_sms():
+    """Hundreds of short sequences, with one and with two query tiles to a job in turn: every CTA does many jobs."""
+    lengths = [(37 * i) % 300 + 1 for i in range(90)]
+    check(*make(lengths, 5, 6, 2, 64, 26))
+    check(*make(lengths[:40], 0, 12, 4, 128, 27))
+
+
+def test_more_sequences_than_are_ranked():
+    """Beyond 2048 sequences the blocks are dealt out in the pack's order."""
+    lengths = [(11 * i) % 5 for i in range(2100)] + [260, 0, 129]
+    check(*make(lengths, 3, 2, 1, 64, 28))
+
+
 def test_scores_of_great_size_and_other_scales():
     check(*make([300, 77], 0, 4, 2, 64, 13, spread=30.0))
     check(*make([300, 77], 0, 4, 2, 64, 14), scale=0.0)

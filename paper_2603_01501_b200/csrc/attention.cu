@@ -205,12 +205,12 @@ int launch_backward(const gac_attn &a, const gac_attn_grad &g, int device, cudaS
     const uint64_t units = uint64_t(a.q_heads) * a.n_tokens, per = kRowThreads / 16 * kRowsInFlight;
     attn_rows_kernel<<<uint32_t((units + per - 1) / per), kRowThreads, 0, s>>>(d);
     // each of the others is set up while the one before it ends, and waits for its results where it needs them
+    GAC_CUDA(nullptr, launch_next(attn_dq_kernel<DP>, grid_q, BwdQ<DP>::kThreads, BwdQ<DP>::kSmem, s, mq, mk, mv, mdo, d));
     GAC_CUDA(nullptr, launch_next(attn_dkv_kernel<DP>, grid_kv, BwdKv<DP>::kThreads, BwdKv<DP>::kSmem, s, mq, mk, mv, mdo, d));
     if (d.parts > 1) {
         const uint64_t n = 2 * uint64_t(a.n_tokens) * a.kv_heads * (a.head_dim / 8);
         GAC_CUDA(nullptr, launch_next(attn_sum_parts_kernel, uint32_t((n + 255) / 256), 256, 0, s, d));
     }
-    GAC_CUDA(nullptr, launch_next(attn_dq_kernel<DP>, grid_q, BwdQ<DP>::kThreads, BwdQ<DP>::kSmem, s, mq, mk, mv, mdo, d));
     GAC_CUDA(nullptr, cudaGetLastError());
     return GAC_OK;
 }

@@ -619,8 +619,11 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
 
 // ------------------------------------------------------------------- backward
 //
-// With P = exp2(c S - log2(e) lse) and the row term D_i = sum_d dO_id O_id:
+// With P = exp2(c S - log2(e) lse) and the row term D_i = sum_d dO_id O_id = sum_j P_ij dP_ij:
 //     dV = P^T dO,   dP = dO V^T,   dS = P (dP - D),   dQ = scale dS K,   dK = scale dS^T Q
+// The row term comes from the rounded O first.  A row of dS adds up to what that was off by, so the kernel for dQ, which
+// has the whole row, leaves a better one for the other; and rows that see one key tile alone, where O is largest and
+// its rounding tells most, take the second form from the start.
 // One kernel sums over the query tiles for a key tile (dK, dV), the other over the key tiles for a query tile
 // (dQ).  Both make S and dP again, seven products in all where five would do with dQ added up in memory by
 // atomics; in return every sum has one owner and one order, and two calls give the same bits.
@@ -803,7 +806,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     float2 v[4];
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
-                        v[x] = i * kTile + lane + 32 * x < w.len ? __ldg(src + lane + 32 * x) : make_float2(0.f, 0.f);
+                        v[x] = i * kTile + lane + 32 * x < w.len ? __ldcg(src + lane + 32 * x) : make_float2(0.f, 0.f);
                     if (use > 0 && !(ok = warp_wait(rows_empty + 8 * slot, (use - 1) & 1))) break;
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
@@ -1002,7 +1005,6 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
 
 // Adds the parts of dK and dV in order and rounds them once.
 static __global__ void __launch_bounds__(256) attn_sum_parts_kernel(const __grid_constant__ AttnDev a) {
-    let_next_start();
     wait_for_previous();
     const uint32_t per = a.head_dim / 8;
     const size_t rows = size_t(a.n_tokens) * a.kv_heads, n = 2 * rows * per;
@@ -1068,6 +1070,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     // A key tile is used by S and again by dQ, a value tile by dP alone: the first kKeys places of the ring take key
     // tiles, the others value tiles, each in turn.
 
+    let_next_start();
     if (warp == 8) tmem_alloc(tmem_slot, 512);
     if (threadIdx.x == 0) {
         jobs.init(10);
@@ -1244,8 +1247,10 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             if (w.kind != kJobWork) continue;
             if (row0 < w.len) {
                 const uint32_t total = w.block * 2 + 1 + t;
-                const float2 term = row < w.len ? __ldg(a.rows + size_t(w.head) * a.n_tokens + w.first + row) : make_float2(0.f, 0.f);
-                const float2 l2 = make_float2(term.x, term.x), d2 = make_float2(-term.y, -term.y);
+                const float2 term = row < w.len ? a.rows[size_t(w.head) * a.n_tokens + w.first + row] : make_float2(0.f, 0.f);
+                const float2 l2 = make_float2(term.x, term.x);
+                float row_term = term.y;
+                float2 left = make_float2(0.f, 0.f);   // sum of this row's dS: what the row term was off by, as P adds up to one
                 for (uint32_t u = 0; u < total; ++u, ++it) {
                     if (!(ok = warp_wait(s_full + 8 * t, it & 1))) break;
                     tc_fence_after();
@@ -1267,22 +1272,44 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     }
                     if (!(ok = warp_wait(dp_full + 8 * t, it & 1))) break;
                     tc_fence_after();
+                    if (total == 1) {   // the row sees this tile alone: its term is exact without the rounded O
+                        float exact = 0.f;
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            uint32_t r[32];
+                            tmem_ld32(r, work + 32 * h);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int x = 0; x < 16; ++x) {
+                                const uint32_t col = 32 * h + 2 * x;
+                                if (col <= local) exact = fmaf(p[16 * h + x].x, __uint_as_float(r[2 * x]), exact);
+                                if (col + 1 <= local) exact = fmaf(p[16 * h + x].y, __uint_as_float(r[2 * x + 1]), exact);
+                            }
+                        }
+                        row_term = exact;
+                    }
+                    const float2 d2 = make_float2(-row_term, -row_term);
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
                         uint32_t r[32], ds[16];
                         tmem_ld32(r, work + 32 * h);
                         tmem_wait_ld();
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) {
-                            const float2 y = mul2(p[16 * h + x], add2(make_float2(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), d2));
-                            ds[x] = bf16x2(y.x, y.y);
-                        }
                         if (u == total - 1) {   // the diagonal tile: what is hidden may hold anything
 #pragma unroll
                             for (int x = 0; x < 16; ++x) {
                                 const uint32_t col = 32 * h + 2 * x;
-                                if (col > local) ds[x] = 0u;
-                                else if (col + 1 > local) ds[x] &= 0xFFFFu;
+                                float2 y = mul2(p[16 * h + x], add2(make_float2(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), d2));
+                                if (col > local) y.x = 0.f;
+                                if (col + 1 > local) y.y = 0.f;
+                                left = add2(left, y);
+                                ds[x] = bf16x2(y.x, y.y);
+                            }
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 16; ++x) {
+                                const float2 y = mul2(p[16 * h + x], add2(make_float2(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), d2));
+                                left = add2(left, y);
+                                ds[x] = bf16x2(y.x, y.y);
                             }
                         }
                         tmem_st16(work + 16 * h, ds);   // over what has been read of dP
@@ -1292,7 +1319,10 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     __syncwarp();
                     if (lane == 0) mbar_arrive(ds_full + 8 * t);
                 }
-                if (!ok || !(ok = warp_wait(done + 8 * t, tiles & 1))) break;
+                if (!ok) break;
+                // the kernel for dK and dV goes on with the better row term
+                if (row < w.len) a.rows[size_t(w.head) * a.n_tokens + w.first + row].y = row_term + (left.x + left.y);
+                if (!(ok = warp_wait(done + 8 * t, tiles & 1))) break;
                 ++tiles;
                 tc_fence_after();
                 const uint32_t row_w = row - lane;   // the warp's first row

@@ -1,4 +1,5 @@
-// Causal attention over a pack of sequences, grouped heads, forward and backward (gac_attn_* of include/gac.h).
+// Causal attention over a pack of sequences, grouped heads, forward and backward (gac_attn_* of include/gac.h): argument
+// checks, operand descriptions and launches; the kernels and what bounds them are in attention_kernels.cuh.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -153,7 +154,9 @@ int launch_forward(const gac_attn &a, int device, cudaStream_t s) {
 }
 
 // Query heads of a group are summed in one CTA as long as there are enough key tiles to go round; with fewer, parts
-// of the group go to CTAs of their own and a second kernel adds them.
+// of the group go to CTAs of their own and a second kernel adds them.  Backward with this limit, with 250 and with 600
+// jobs: 8192 tokens, 12/2 heads 199 us, 225, 213; 16384 tokens in one sequence 2.33 ms, 2.90, 2.38; 12384 tokens, 28/4
+// heads 0.99 ms, 1.00, 1.06.
 constexpr uint32_t kEnoughJobs = 370;   // 2.5 per SM
 uint32_t parts_of(const gac_attn &a) {
     const uint32_t group = a.q_heads / a.kv_heads;

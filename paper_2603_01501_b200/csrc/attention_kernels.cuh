@@ -45,10 +45,12 @@ __device__ __forceinline__ uint32_t seq_bound(const AttnDev &a, uint32_t b) {
 // sees u key tiles (or, for a key tile, is seen by u query tiles), and the highest come first, so that the last
 // CTAs to start are the short ones.  The job's height and sequence follow from cu_seqlens alone: the
 // number of blocks of height >= u is  F(u) = sum_b max(0, blocks_b - u + 1), found by bisection over u by a
-// warp whose lanes hold the sequences.  Beyond kRankedSeqs sequences that costs more than it gives, and every
-// sequence gets the indices  start/ROWS + b ...  instead: at least as many as it has blocks (some stay empty).
+// warp whose lanes hold the sequences.  Beyond kRankedSeqs sequences every sequence gets the indices  start/ROWS + b ...
+// instead: at least as many as it has blocks (some stay empty), and no search over the whole pack.  Forward and backward
+// of 12 heads, ranked against in the pack's order: 16 sequences of about 1000 tokens 645 us against 766, 128 of about
+// 150 613 against 651, 256 of about 100 503 against 498, 1024 of 32 1682 against 1092.
 // Rows behind the last sequence come last.
-constexpr uint32_t kRankedSeqs = 2048;
+constexpr uint32_t kRankedSeqs = 192;
 struct Job {
     uint32_t first, len;   // the sequence (or the rows behind the last one)
     uint32_t block;        // which block of it
@@ -222,15 +224,13 @@ struct Place {
     }
 };
 
-// Writes one bit pattern over `dim` elements of rows [from, to) of one head, by the first `threads` threads of the CTA: zero for rows that
-// belong to no sequence, NaN where a wait ran out.
-constexpr uint32_t kZeroBits = 0u, kNanBits = 0x7FFF7FFFu;
-__device__ __forceinline__ void fill_rows(const RowsOut &o, uint32_t from, uint32_t to, uint32_t head, uint32_t dim, uint32_t bits,
-                                          uint32_t threads) {
+// Writes zeros over `dim` elements of rows [from, to) of one head, by the first `threads` threads of the CTA: rows that
+// belong to no sequence.
+__device__ __forceinline__ void fill_rows(const RowsOut &o, uint32_t from, uint32_t to, uint32_t head, uint32_t dim, uint32_t threads) {
     const uint32_t per = dim / 8, n = (to - from) * per;
     for (uint32_t i = threadIdx.x; i < n; i += threads) {
         char *p = o.p + (long long)(from + i / per) * o.token + (long long)head * o.head + (i % per) * 16;
-        *reinterpret_cast<uint4 *>(p) = make_uint4(bits, bits, bits, bits);
+        *reinterpret_cast<uint4 *>(p) = make_uint4(0u, 0u, 0u, 0u);
     }
 }
 
@@ -352,6 +352,14 @@ __device__ __forceinline__ void product_cols(uint32_t d, uint32_t a, uint32_t b,
 // exponentials are taken.
 // Warps: 0-3 and 4-7 the rows of the two tiles, 8 issues the products, 9 the TMA loads, 10 finds the jobs; 11 only makes
 // the third warpgroup whole, which hands registers over to the first two (a row of 128 scores stays in registers).
+//
+// Per key tile and query tile the tensor cores need 1024 cycles, the exponentials as many on the 16-wide special function
+// unit, and the way from a finished S to the next (scores out of tensor memory, maximum, exponentials, P back, two
+// products, four barriers) takes about 3700; two tiles in turn make that 1850 each.  One query tile of 128 rows per CTA and two
+// CTAs per SM would hide it too, but read every key and value tile twice.  Measured: one sequence of 16384 tokens,
+// 12/2 heads x 128, 630 us = 1.31 PFLOP/s (0.78 of cuBLAS's best rate, 0.92 of its rate under the power cap); 12384 tokens in
+// four sequences, 28/4 heads, 262 us = 1.13; 8192 tokens in eight sequences, 12/2 heads, 56 us = 0.62: there a CTA has three
+// jobs of 7 key tiles, and each starts with a load, a product and a full softmax that nothing hides.
 
 template <int DP>
 struct Fwd {
@@ -533,7 +541,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             const uint32_t row0 = w.block * 2 * kTile;
             if (w.kind == kJobTail) {
                 const uint32_t from = w.first + row0, end = min(w.first + w.len, from + 2 * kTile);
-                fill_rows(a.o, from, end, w.head, a.head_dim, kZeroBits, 256);
+                fill_rows(a.o, from, end, w.head, a.head_dim, 256);
                 for (uint32_t i = from + threadIdx.x; i < end; i += 256) a.lse[size_t(w.head) * a.n_tokens + i] = -INFINITY;
             }
             if (w.kind != kJobWork || row0 + t * kTile >= w.len) continue;
@@ -668,6 +676,11 @@ static __global__ void __launch_bounds__(kRowThreads) attn_rows_kernel(const __g
 // Warps: 0-3 and 4-7 take the two halves of the query columns, 8 issues the products, 9 the TMA loads, 10 fetches the
 // row terms, 11 finds the jobs.  While the threads make dS of one query tile the tensor cores run dV and the next S;
 // while they take the next exponentials, dK and the next dP.
+//
+// Four products of 512 cycles per query tile; a turn takes about 3400, the way from S through P, dV and the next S:
+// tensor memory (512 columns: S, dP, dV, dK) has no room for a second S, and the two loads of 32 KB per turn take about
+// 2200 cycles each with shared memory for two turns.  Measured: 12384 tokens, 28/4 heads x 128, 620 us (0.96 PFLOP/s of the
+// four products done), 16384 tokens in one sequence, 12/2 heads, 1.32 ms (1.25).
 template <int DP>
 struct BwdKv {
     static constexpr int kSub = DP / 64;
@@ -885,8 +898,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             const uint32_t kv_head = kv_head_of(w), part = w.head / a.kv_heads;
             if (w.kind == kJobTail && part == 0) {
                 const uint32_t from = w.first + w.block * kTile, to = min(w.first + w.len, from + kTile);
-                fill_rows(a.d_k, from, to, kv_head, a.head_dim, kZeroBits, 256);
-                fill_rows(a.d_v, from, to, kv_head, a.head_dim, kZeroBits, 256);
+                fill_rows(a.d_k, from, to, kv_head, a.head_dim, 256);
+                fill_rows(a.d_v, from, to, kv_head, a.head_dim, 256);
             }
             if (w.kind != kJobWork) continue;
             const uint32_t q_tiles = q_tiles_of(w), total = q_tiles * heads, last = (w.len % kTile) ? w.len % kTile : kTile;
@@ -1040,6 +1053,10 @@ static __global__ void __launch_bounds__(256) attn_sum_parts_kernel(const __grid
 // working place per tile, which takes S, then dP as soon as S has been read, then dS as bfloat16.  The two tiles alternate:
 // a tile's threads take its exponentials and make its dS while the tensor cores work for the other.
 // Warps: 0-3 and 4-7 the rows of the two tiles, 8 issues the products, 9 the TMA loads, 10 finds the jobs.
+//
+// Six products of 512 cycles per key tile and pair of query tiles; a turn takes about 4300, of which the issuing thread
+// loses some 150 at each of its four waits.  One query tile per CTA with S double-buffered loads twice as much, has room
+// for one value tile, and waits for it: 447 us where this takes 385 (12384 tokens, 28/4 heads x 128).
 template <int DP>
 struct BwdQ {
     static constexpr int kSub = DP / 64;
@@ -1242,7 +1259,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             const uint32_t row0 = w.block * 2 * kTile + t * kTile, row = row0 + local;
             if (w.kind == kJobTail) {
                 const uint32_t from = w.first + w.block * 2 * kTile, to = min(w.first + w.len, from + 2 * kTile);
-                fill_rows(a.d_q, from, to, w.head, a.head_dim, kZeroBits, 256);
+                fill_rows(a.d_q, from, to, w.head, a.head_dim, 256);
             }
             if (w.kind != kJobWork) continue;
             if (row0 < w.len) {

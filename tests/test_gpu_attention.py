@@ -76,7 +76,7 @@ def test_many_more_jobs_than_sms():
 
 
 def test_more_sequences_than_are_ranked():
-    """Beyond 2048 sequences the blocks are dealt out in the pack's order."""
+    """Beyond 192 sequences the blocks are dealt out in the pack's order."""
     lengths = [(11 * i) % 5 for i in range(2100)] + [260, 0, 129]
     check(*make(lengths, 3, 2, 1, 64, 28))
 

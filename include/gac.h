@@ -429,8 +429,9 @@ int gac_stats_static(const gac_tensor *list, uint32_t n, int g_dtype, int d_dtyp
  * bounds.
  *
  * The calls below need no context unless they say so, enqueue on the given
- * stream, allocate nothing and can be captured in a CUDA graph.  Messages of
- * failed calls: gac_last_error(NULL).
+ * stream, allocate nothing and can be captured in a CUDA graph (gac_clip_init and
+ * gac_clip_free allocate and free, and cannot).  Messages of failed calls:
+ * gac_last_error(NULL).
  * ======================================================================
  *
  * Global gradient norm and clipping over a list of tensors, for steps that do
@@ -553,7 +554,8 @@ int gac_rotary(const gac_rotary_args *args, int cuda_device, void *cuda_stream);
  *
  * q, k, v, o and the gradients are bfloat16 [n_tokens][heads][head_dim], last dimension
  * contiguous, bases 16-byte aligned and strides multiples of 8 elements (views of one
- * fused projection will do).  Outputs must not overlap inputs.
+ * fused projection will do).  Outputs must not overlap inputs, the workspace or one
+ * another (views of one fused gradient, whose heads lie between each other's, will do).
  * gac_attn_backward takes the same gac_attn as the forward call that filled o
  * and lse, and a workspace of gac_attn_workspace bytes (device, 16-byte aligned; its
  * contents need not be kept).

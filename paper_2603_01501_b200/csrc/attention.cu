@@ -290,6 +290,10 @@ int gac_attn_backward(const gac_attn *args, const gac_attn_grad *grad, int cuda_
     for (const Span &x : in)
         for (const Span &y : out)
             if (overlap(x, y)) return fail(nullptr, GAC_ERR_INVALID_ARG, "a gradient overlaps an input%s");
+    // spans of interleaved views may cross; the same memory twice may not
+    if (g.d_q.p == g.d_k.p || g.d_q.p == g.d_v.p || g.d_k.p == g.d_v.p || g.workspace == g.d_q.p || g.workspace == g.d_k.p ||
+        g.workspace == g.d_v.p)
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "two gradients, or a gradient and the workspace, are the same memory%s");
     if (!g.workspace || reinterpret_cast<uint64_t>(g.workspace) % 16 || g.workspace_bytes < gac_attn_workspace(args))
         return fail(nullptr, GAC_ERR_INVALID_ARG, "workspace must be 16-byte aligned and of gac_attn_workspace bytes%s");
     Range range("gac_attn_backward");

@@ -122,7 +122,7 @@ def test_argument_errors_need_no_device(lib):
     assert attn(dtype=0) == gb.GAC_ERR_DTYPE
     assert attn(n_tokens=0) == gb.GAC_OK
     for over in ({"workspace": None}, {"workspace": (11 << 20) + 4}, {"workspace_bytes": 100}, {"d_q": heads(1 << 20)},
-                 {"d_k": heads(4 << 20)}, {"d_v": heads(7 << 20)}):
+                 {"d_k": heads(4 << 20)}, {"d_v": heads(7 << 20)}, {"d_v": heads(9 << 20)}, {"workspace": 8 << 20}):
         assert attn(grad=over) == gb.GAC_ERR_INVALID_ARG, over
     assert lib.gac_attn_forward(None, 0, None) == gb.GAC_ERR_INVALID_ARG
     assert lib.gac_attn_backward(None, None, 0, None) == gb.GAC_ERR_INVALID_ARG

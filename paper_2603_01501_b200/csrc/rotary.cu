@@ -6,7 +6,7 @@
 // out the token's sines and cosines (the angle is reduced to one turn in binary64, then sincospi in binary32: exact to
 // the last bits at any position, no table in memory) and leave them in shared memory for every head of the token,
 // whose first vectors are on their way meanwhile.
-// 16384 tokens x 32 heads x 128, bfloat16: 49 us = 5.4 TB/s (0.84 of a plain copy's rate); 8189 tokens x 14 heads x 128,
+// 16384 tokens x 32 heads x 128, bfloat16: 46 to 48 us = 5.6 to 5.8 TB/s (0.86 to 0.90 of a plain copy's rate); 8189 tokens x 14 heads x 128,
 // float32, half of the head turned: 22 us = 5.3 TB/s.  With 256 threads, 4 tokens to a CTA and the sines made before
 // the loads the first takes 54 us.
 #include <cuda_runtime.h>
@@ -132,9 +132,10 @@ struct Vec {
 };
 
 // A thread keeps one place of the head, N pairs (two vectors) or 2 N copied elements, and walks over the token's heads.
-template <typename T, bool HALF, int N>
+template <typename T, bool HALF>
 __global__ void __launch_bounds__(kThreads, 12)
 rotary_kernel(const __grid_constant__ RotaryDev a) {
+    constexpr int N = 4;
     __shared__ __align__(16) float2 wheel[GAC_ROTARY_MAX_DIM / 2];
     constexpr int kFlight = 2;
     constexpr uint32_t kSize = sizeof(T);
@@ -315,8 +316,8 @@ int gac_rotary(const gac_rotary_args *args, int cuda_device, void *cuda_stream) 
     if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const bool half = a.layout == GAC_ROTARY_HALF, bf16 = a.dtype == GAC_BF16;
-    // Vectors of 16 or 8 bytes where every vector of every head starts on such a boundary and ends inside its part of
-    // the head; single elements otherwise.
+    // Vectors of four elements where every vector of every head starts on such a boundary and ends inside its part of the
+    // head, single elements otherwise: 16384 tokens x 32 heads x 128 bfloat16 take 46 us and 110 (vectors of eight: 48).
     auto fits = [&](uint32_t n) {   // n elements
         const uint64_t bytes = n * size;
         if (d.pairs % n || a.head_dim % n) return false;
@@ -326,13 +327,12 @@ int gac_rotary(const gac_rotary_args *args, int cuda_device, void *cuda_stream) 
                 return false;
         return true;
     };
-    const uint32_t n = fits(16 / size) ? 16 / size : bf16 && fits(4) ? 4 : 1;
+    const bool vectors = fits(4);
     void (*fn)(const RotaryDev) = nullptr;
-    if (bf16) fn = n == 8 ? (half ? rotary_kernel<uint16_t, true, 8> : rotary_kernel<uint16_t, false, 8>)
-                 : n == 4 ? (half ? rotary_kernel<uint16_t, true, 4> : rotary_kernel<uint16_t, false, 4>)
-                          : (half ? rotary_any_kernel<uint16_t, true> : rotary_any_kernel<uint16_t, false>);
-    else fn = n == 4 ? (half ? rotary_kernel<float, true, 4> : rotary_kernel<float, false, 4>)
-                     : (half ? rotary_any_kernel<float, true> : rotary_any_kernel<float, false>);
+    if (vectors) fn = bf16 ? (half ? rotary_kernel<uint16_t, true> : rotary_kernel<uint16_t, false>)
+                           : (half ? rotary_kernel<float, true> : rotary_kernel<float, false>);
+    else fn = bf16 ? (half ? rotary_any_kernel<uint16_t, true> : rotary_any_kernel<uint16_t, false>)
+                   : (half ? rotary_any_kernel<float, true> : rotary_any_kernel<float, false>);
     fn<<<a.n_tokens, kThreads, 0, s>>>(d);
     GAC_CUDA(nullptr, cudaGetLastError());
     return GAC_OK;

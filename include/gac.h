@@ -424,9 +424,12 @@ int gac_stats_static(const gac_tensor *list, uint32_t n, int g_dtype, int d_dtyp
  * pack of tokens; cu_seqlens[b] .. cu_seqlens[b+1] are the tokens of
  * sequence b (cu_seqlens[0] is taken as 0).  Tokens behind the last sequence
  * (padding of the pack) belong to none.  cu_seqlens lives on the device and
- * is read there only, so no call waits for the host; an entry outside
- * [the previous one, n_tokens] is moved to that range, never followed out of
- * bounds.
+ * is read there only, so no call waits for the host.  Entries must not decrease.
+ * What is in them cannot lead out of bounds: an entry outside [0, n_tokens] is moved to
+ * that range, and entries out of order are moved into order, in the same way by every
+ * call below: a bisection over the entries (node b = (lo + hi + 1) / 2 of lo = 0,
+ * hi = n_seqs first) cuts its range of tokens at entry b, kept within the range; the
+ * cut is where sequence b starts.  So every token is of one sequence or of none.
  *
  * The calls below need no context unless they say so, enqueue on the given
  * stream, allocate nothing and can be captured in a CUDA graph (gac_clip_init and

@@ -34,7 +34,10 @@ struct AttnDev {
     float *part_sums;                  // kept as binary32 [parts][d_k, d_v][n_tokens][kv_heads][head_dim] when parts > 1
 };
 
-// cu_seqlens entry b, kept in range; entry 0 is taken as 0.
+// cu_seqlens entry b, kept in range; entry 0 is taken as 0.  The sequences are what a bisection over the entries makes of them:
+// the node of entry `mid` cuts its range of tokens at that entry, kept within the range.  Ascending entries are found as
+// they are; of entries out of order those nearer the root count, and the sequences still lie one behind the other, which
+// is what gives every row one owner.
 __device__ __forceinline__ uint32_t seq_bound(const AttnDev &a, uint32_t b) {
     if (b == 0) return 0u;
     const int32_t c = __ldg(a.cu + b);
@@ -45,24 +48,40 @@ __device__ __forceinline__ uint32_t seq_bound(const AttnDev &a, uint32_t b) {
 // sees u key tiles (or, for a key tile, is seen by u query tiles), and the highest come first, so that the last
 // CTAs to start are the short ones.  The job's height and sequence follow from cu_seqlens alone: the
 // number of blocks of height >= u is  F(u) = sum_b max(0, blocks_b - u + 1), found by bisection over u by a
-// warp whose lanes hold the sequences.  Beyond kRankedSeqs sequences every sequence gets the indices  start/ROWS + b ...
-// instead: at least as many as it has blocks (some stay empty), and no search over the whole pack.  Forward and backward
+// warp whose lanes hold the sequences.  Beyond kRankedSeqs sequences, and where entries are out of order, every sequence gets
+// the indices  start/ROWS + b ... instead: at least as many as it has blocks (some stay empty), and one bisection.  Forward and backward
 // of 12 heads, ranked against in the pack's order: 16 sequences of about 1000 tokens 645 us against 766, 128 of about
 // 150 613 against 651, 256 of about 100 503 against 498, 1024 of 32 1682 against 1092.
 // Rows behind the last sequence come last.
 constexpr uint32_t kRankedSeqs = 192;
+// Whether blocks are dealt out by height (whole warps).
+__device__ __forceinline__ bool is_ranked(const AttnDev &a) {
+    if (a.n_seqs > kRankedSeqs) return false;
+    bool falls = false;
+    for (uint32_t i = threadIdx.x & 31; i < a.n_seqs; i += 32) falls |= seq_bound(a, i) > seq_bound(a, i + 1);
+    return !__any_sync(0xFFFFFFFFu, falls);
+}
+// Where the rows behind the last sequence begin.
+__device__ __forceinline__ uint32_t tail_start(const AttnDev &a) {
+    uint32_t from = 0;
+    for (uint32_t lo = 0; lo < a.n_seqs;) {
+        lo = (lo + a.n_seqs + 1) / 2;
+        from = max(from, seq_bound(a, lo));
+    }
+    return from;
+}
 struct Job {
     uint32_t first, len;   // the sequence (or the rows behind the last one)
     uint32_t block;        // which block of it
     bool tail, none;
 };
 template <int ROWS, bool HIGH_IS_LATE>
-__device__ __forceinline__ Job find_job(const AttnDev &a, uint32_t index, uint32_t count) {   // whole warps
+__device__ __forceinline__ Job find_job(const AttnDev &a, bool ranked, uint32_t index, uint32_t count) {   // whole warps
     const uint32_t all = 0xFFFFFFFFu, lane = threadIdx.x & 31, n = a.n_seqs;
     Job job;
     job.tail = job.none = false;
-    uint32_t b;
-    if (n <= kRankedSeqs) {
+    uint32_t b, end;
+    if (ranked) {
         auto blocks_of = [&](uint32_t i) {
             if (i >= n) return 0u;
             const uint32_t from = seq_bound(a, i), to = seq_bound(a, i + 1);
@@ -108,24 +127,30 @@ __device__ __forceinline__ Job find_job(const AttnDev &a, uint32_t index, uint32
             job.block = lo - 1;
         }
         job.first = seq_bound(a, b);
+        end = job.tail ? a.n_tokens : seq_bound(a, b + 1);
     } else {
         const uint32_t slot = HIGH_IS_LATE ? count - 1 - index : index;
-        uint32_t lo = 0, hi = n;   // the last b with start(b) <= slot
+        uint32_t lo = 0, hi = n;   // the last b with start(b)/ROWS + b <= slot
+        job.first = 0;
+        end = a.n_tokens;
         while (lo < hi) {
-            const uint32_t mid = (lo + hi + 1) / 2;
-            if (seq_bound(a, mid) / ROWS + mid <= slot) lo = mid;
-            else hi = mid - 1;
+            const uint32_t mid = (lo + hi + 1) / 2, cut = min(max(seq_bound(a, mid), job.first), end);   // start(mid)
+            if (cut / ROWS + mid <= slot) {
+                lo = mid;
+                job.first = cut;
+            } else {
+                hi = mid - 1;
+                end = cut;
+            }
         }
         b = lo;
         job.tail = b == n;
-        job.first = seq_bound(a, b);
         job.block = slot - (job.first / ROWS + b);
     }
-    const uint32_t end = job.tail ? a.n_tokens : max(job.first, seq_bound(a, b + 1));
     job.len = end - job.first;
     const uint32_t blocks = (job.len + ROWS - 1) / ROWS;
     job.none = job.block >= blocks;
-    if (!HIGH_IS_LATE && !job.tail && !job.none && n <= kRankedSeqs) job.block = blocks - 1 - job.block;
+    if (!HIGH_IS_LATE && !job.tail && !job.none && ranked) job.block = blocks - 1 - job.block;
     return job;
 }
 inline uint32_t job_count(uint32_t n_tokens, uint32_t n_seqs, uint32_t rows) { return n_tokens / rows + n_seqs + 1; }
@@ -139,8 +164,8 @@ struct JobWord {
     uint32_t first, len, block, kind, head;
 };
 template <int ROWS, bool HIGH_IS_LATE>
-__device__ __forceinline__ JobWord job_at(const AttnDev &a, uint32_t index, uint32_t heads) {   // whole warps
-    const Job j = find_job<ROWS, HIGH_IS_LATE>(a, index / heads, gridDim.x / heads);
+__device__ __forceinline__ JobWord job_at(const AttnDev &a, bool ranked, uint32_t index, uint32_t heads) {   // whole warps
+    const Job j = find_job<ROWS, HIGH_IS_LATE>(a, ranked, index / heads, gridDim.x / heads);
     JobWord w;
     w.first = j.first;
     w.len = j.len;
@@ -161,7 +186,7 @@ struct Jobs {
     }
     // The warp that hands the jobs out: from this CTA's own index on, until there is none left.
     template <int ROWS, bool HIGH_IS_LATE>
-    __device__ __forceinline__ bool run(const AttnDev &a, uint32_t heads) const {
+    __device__ __forceinline__ bool run(const AttnDev &a, bool ranked, uint32_t heads) const {
         const uint32_t lane = threadIdx.x & 31;
         int index = int(blockIdx.x);
         uint32_t given = 0, questions = 0;
@@ -169,7 +194,7 @@ struct Jobs {
             JobWord w;
             w.first = w.len = w.block = w.head = 0;
             w.kind = kJobStop;
-            if (index >= 0) w = job_at<ROWS, HIGH_IS_LATE>(a, uint32_t(index), heads);
+            if (index >= 0) w = job_at<ROWS, HIGH_IS_LATE>(a, ranked, uint32_t(index), heads);
             if (w.kind != kJobNone) {
                 if (lane == 0) {
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(word), "r"(w.first), "r"(w.len), "r"(w.block), "r"(w.kind | (w.head << 2)) : "memory");
@@ -405,6 +430,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
         }
         fence_barrier_init();
     }
+    const bool ranked = warp == 10 && is_ranked(a);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -527,7 +553,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 }
             }
         } else if (warp == 10) {   // ------------------------------------ jobs
-            ok = jobs.template run<2 * kTile, true>(a, a.q_heads);
+            ok = jobs.template run<2 * kTile, true>(a, ranked, a.q_heads);
         }
     } else {   // ------------------------------------------- a row of a tile
         registers_up<C::kRowRegs>();
@@ -734,6 +760,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         }
         fence_barrier_init();
     }
+    const bool ranked = warp == 11 && is_ranked(a);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -886,7 +913,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 }
             }
         } else {   // ------------------------------------------------ jobs
-            ok = jobs.template run<kTile, false>(a, lots);
+            ok = jobs.template run<kTile, false>(a, ranked, lots);
         }
     } else {   // ---------------------- a key row, half of the query columns
         registers_up<C::kRowRegs>();
@@ -1026,7 +1053,7 @@ static __global__ void __launch_bounds__(256) attn_sum_parts_kernel(const __grid
     const uint32_t which = i >= rows * per;   // 0: dK, 1: dV
     const size_t j = i - which * rows * per, row = j / per;
     const uint32_t t = uint32_t(row / a.kv_heads), h = uint32_t(row % a.kv_heads), x = uint32_t(j % per) * 8;
-    if (t >= seq_bound(a, a.n_seqs)) return;   // rows of no sequence were written as zero
+    if (t >= tail_start(a)) return;   // rows of no sequence were written as zero
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (uint32_t part0 = 0; part0 < a.parts; part0 += 4) {
         float4 u[4], v[4];
@@ -1109,6 +1136,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         }
         fence_barrier_init();
     }
+    const bool ranked = warp == 10 && is_ranked(a);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -1246,7 +1274,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 }
             }
         } else if (warp == 10) {   // ------------------------------------ jobs
-            ok = jobs.template run<2 * kTile, true>(a, a.q_heads);
+            ok = jobs.template run<2 * kTile, true>(a, ranked, a.q_heads);
         }
     } else {   // ------------------------------------------- a row of a tile
         registers_up<C::kRowRegs>();

@@ -47,16 +47,20 @@ __device__ __forceinline__ void store_el(char *p, float v, uint16_t) {
     *reinterpret_cast<uint16_t *>(p) = uint16_t(r & 0xFFFFu);
 }
 
-// Place of token t in its sequence; tokens behind the last sequence are at 0.
+// Place of token t in its sequence; tokens behind the last sequence are at 0.  The bisection is the one that the attention
+// kernels read the entries by, so that entries out of order mean the same sequences here and there.
 __device__ int place_in_sequence(const int32_t *cu, uint32_t n_seqs, uint32_t t) {
-    uint32_t lo = 0, hi = n_seqs;   // the last b with cu[b] <= t, cu[0] taken as 0
+    uint32_t lo = 0, hi = n_seqs, first = 0;   // the last b with cu[b] <= t, cu[0] taken as 0; where it starts
     while (lo < hi) {
-        const uint32_t mid = (lo + hi + 1) / 2;
-        if (uint32_t(max(cu[mid], 0)) <= t) lo = mid;
-        else hi = mid - 1;
+        const uint32_t mid = (lo + hi + 1) / 2, cut = uint32_t(max(cu[mid], 0));
+        if (cut <= t) {
+            lo = mid;
+            first = max(first, cut);
+        } else {
+            hi = mid - 1;
+        }
     }
-    if (lo == n_seqs) return 0;
-    return int(t) - (lo ? max(cu[lo], 0) : 0);
+    return lo == n_seqs ? 0 : int(t - first);
 }
 
 // Cosine and sine, already scaled, of every pair of the CTA's token.

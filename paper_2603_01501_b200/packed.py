@@ -17,23 +17,23 @@ from __future__ import annotations
 from typing import Iterable, List, Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as gb
 
 
 class _Rotary(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, freqs, positions, cu_seqlens, layout, scale):
-        ctx.how = (freqs, positions, cu_seqlens, layout, scale)
-        return gb.gac_rotary(q, k, freqs, positions=positions, cu_seqlens=cu_seqlens, layout=layout, scale=scale)
+    def forward(ctx, q, k, freqs, positions, cu_seqlens, layout, scale, inverse):
+        ctx.how = (freqs, positions, cu_seqlens, layout, scale, inverse)
+        return gb.gac_rotary(q, k, freqs, positions=positions, cu_seqlens=cu_seqlens, layout=layout, scale=scale, inverse=inverse)
 
     @staticmethod
     def backward(ctx, d_q, d_k):
-        freqs, positions, cu_seqlens, layout, scale = ctx.how
-        # the transpose of a turn is the turn by the negative angle
-        d_q, d_k = gb.gac_rotary(_rows(d_q), _rows(d_k), freqs, positions=positions, cu_seqlens=cu_seqlens, layout=layout,
-                                 scale=scale, inverse=True)
-        return d_q, d_k, None, None, None, None, None
+        freqs, positions, cu_seqlens, layout, scale, inverse = ctx.how
+        # the transpose of a turn is the turn by the negative angle: itself a turn, so derivatives of any order go through
+        d_q, d_k = _Rotary.apply(_rows(d_q), _rows(d_k), freqs, positions, cu_seqlens, layout, scale, not inverse)
+        return d_q, d_k, None, None, None, None, None, None
 
 
 class _Attention(torch.autograd.Function):
@@ -46,6 +46,7 @@ class _Attention(torch.autograd.Function):
         return o, lse
 
     @staticmethod
+    @once_differentiable   # the library has no second derivative: asking for one raises
     def backward(ctx, d_o, _):
         q, k, v, o, lse, cu_seqlens = ctx.saved_tensors
         d_q, d_k, d_v = gb.gac_attn_backward(_rows(d_o, 8), q, k, v, o, lse, cu_seqlens, scale=ctx.scale)
@@ -63,13 +64,14 @@ def _rows(t: torch.Tensor, multiple: int = 1) -> torch.Tensor:
 
 def rotary(q: torch.Tensor, k: torch.Tensor, freqs, positions: Optional[torch.Tensor] = None,
            cu_seqlens: Optional[torch.Tensor] = None, layout: str = "half", scale: float = 1.0):
-    """Rotary positions (binding.gac_rotary) with their gradient; returns (q', k')."""
-    return _Rotary.apply(q, k, freqs, positions, cu_seqlens, layout, scale)
+    """Rotary positions (binding.gac_rotary) with their derivatives of any order; returns (q', k')."""
+    return _Rotary.apply(q, k, freqs, positions, cu_seqlens, layout, scale, False)
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, scale: Optional[float] = None,
               return_lse: bool = False):
-    """Causal attention over the pack (binding.gac_attn_forward) with its gradient.  ``lse``, if asked for, has none."""
+    """Causal attention over the pack (binding.gac_attn_forward) with its gradient (first order alone: a
+    second derivative raises).  ``lse``, if asked for, has none."""
     o, lse = _Attention.apply(q, k, v, cu_seqlens, scale)
     return (o, lse) if return_lse else o
 

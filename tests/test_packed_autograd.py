@@ -1,0 +1,61 @@
+"""What the autograd layer saves, refuses and hands on, with plain torch in the place of the library's calls (no GPU)."""
+import pytest
+import torch
+
+from paper_2603_01501_b200 import binding as gb
+from paper_2603_01501_b200 import packed
+
+
+@pytest.fixture
+def plain(monkeypatch):
+    """Stand-ins that, like the library, return tensors without a graph."""
+    @torch.no_grad()
+    def rotary(q, k, freqs, positions=None, cu_seqlens=None, layout="half", scale=1.0, inverse=False, **_):
+        assert layout == "half" and cu_seqlens is None
+        angle = positions.double()[:, None] * torch.as_tensor(freqs) * (-1 if inverse else 1)
+        c, s = (scale * angle.cos())[:, None], (scale * angle.sin())[:, None]
+        out = []
+        for x in (q, k):
+            if x is None:
+                out.append(None)
+                continue
+            a, b = x.chunk(2, -1)
+            out.append(torch.cat((a * c - b * s, a * s + b * c), -1))
+        return tuple(out)
+
+    @torch.no_grad()
+    def forward(q, k, v, cu, scale=None, stream=None):
+        return q * 2.0, q[..., 0].t().contiguous().float()
+
+    @torch.no_grad()
+    def backward(d_o, q, k, v, o, lse, cu, scale=None, stream=None):
+        return d_o * 2.0, torch.zeros_like(k), torch.zeros_like(v)
+
+    monkeypatch.setattr(gb, "gac_rotary", rotary)
+    monkeypatch.setattr(gb, "gac_attn_forward", forward)
+    monkeypatch.setattr(gb, "gac_attn_backward", backward)
+
+
+def heads(n, seed):
+    return torch.randn(5, n, 4, generator=torch.Generator().manual_seed(seed), dtype=torch.float64).requires_grad_()
+
+
+FREQS = [1.0, 0.1]
+
+
+def test_second_derivative_through_rotary(plain):
+    q, k, pos = heads(2, 1), heads(1, 2), torch.arange(5, dtype=torch.int32)
+    y, _ = packed.rotary(q, k, FREQS, positions=pos, scale=2.0)
+    first, = torch.autograd.grad((y ** 2).sum() + (q ** 4).sum(), q, create_graph=True)
+    second, = torch.autograd.grad(first.sum(), q)
+    # |y|^2 = 4 |q|^2
+    assert torch.allclose(first, 8 * q + 4 * q ** 3) and torch.allclose(second, 8 + 12 * q ** 2)
+
+
+def test_second_derivative_through_attention_is_refused(plain):
+    q, k, v = heads(2, 3), heads(1, 4), heads(1, 5)
+    o = packed.attention(q, k, v, torch.tensor([0, 5], dtype=torch.int32))
+    first, = torch.autograd.grad((o ** 2).sum() + (q ** 4).sum(), q, create_graph=True)
+    assert torch.allclose(first, 8 * q + 4 * q ** 3)
+    with pytest.raises(RuntimeError):
+        first.sum().backward()

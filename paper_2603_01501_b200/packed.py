@@ -16,6 +16,7 @@ from __future__ import annotations
 
 from typing import Iterable, List, Optional
 
+import numpy as np
 import torch
 from torch.autograd.function import once_differentiable
 
@@ -25,12 +26,15 @@ from . import binding as gb
 class _Rotary(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, freqs, positions, cu_seqlens, layout, scale, inverse):
-        ctx.how = (freqs, positions, cu_seqlens, layout, scale, inverse)
+        # positions and cu_seqlens are versioned like any saved tensor; of freqs the values of this call are kept
+        ctx.save_for_backward(positions, cu_seqlens)
+        ctx.how = (np.array(freqs, dtype=np.float64), layout, scale, inverse)
         return gb.gac_rotary(q, k, freqs, positions=positions, cu_seqlens=cu_seqlens, layout=layout, scale=scale, inverse=inverse)
 
     @staticmethod
     def backward(ctx, d_q, d_k):
-        freqs, positions, cu_seqlens, layout, scale, inverse = ctx.how
+        positions, cu_seqlens = ctx.saved_tensors
+        freqs, layout, scale, inverse = ctx.how
         # the transpose of a turn is the turn by the negative angle: itself a turn, so derivatives of any order go through
         d_q, d_k = _Rotary.apply(_rows(d_q), _rows(d_k), freqs, positions, cu_seqlens, layout, scale, not inverse)
         return d_q, d_k, None, None, None, None, None, None

@@ -59,3 +59,17 @@ def test_second_derivative_through_attention_is_refused(plain):
     assert torch.allclose(first, 8 * q + 4 * q ** 3)
     with pytest.raises(RuntimeError):
         first.sum().backward()
+
+
+def test_what_the_way_back_of_rotary_reads_cannot_change_unnoticed(plain):
+    import numpy as np
+    q, k = heads(2, 6), heads(1, 7)
+    pos, freqs = torch.arange(5, dtype=torch.int32), np.array(FREQS)
+    want, = torch.autograd.grad(packed.rotary(q, k, freqs, positions=pos)[0].sum(), q)
+    y, _ = packed.rotary(q, k, freqs, positions=pos)
+    freqs[:] = 3.0                                  # numpy keeps no versions: the values of the call count
+    got, = torch.autograd.grad(y.sum(), q, retain_graph=True)
+    assert torch.equal(got, want)
+    pos.add_(7)                                     # a buffer refilled for the next micro-batch
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(y.sum(), q)

@@ -500,7 +500,9 @@ int gac_clip_free(gac_clip_ctx *ctx);   /* NULL is accepted */
  * are as exact as near ones.
  *
  * x / y are the input and output of the query heads (0) and of the key heads (1); heads = 0
- * leaves one out.  y may equal x (in place, same strides), else the two must not overlap.
+ * leaves one out.  y may equal x (in place, same strides), else the two must not overlap.  Nor
+ * may what is written for one of the two overlap what is read or written for the other (views
+ * of one fused tensor, whose heads lie between each other's, do not).
  * Positions: `positions` (device, one int32 per token), or, when that is NULL,
  * the place of each token in its sequence by cu_seqlens (tokens behind the last
  * sequence: position 0).

@@ -19,6 +19,7 @@
 
 #include "gac.h"
 #include "gac_host.h"
+#include "overlap.h"
 
 namespace {
 
@@ -206,10 +207,8 @@ int fail(std::nullptr_t, int code, const char *fmt, const char *a = "", long lon
     return code;
 }
 
-// First byte and one past the last byte of a strided [tokens][heads][dim] block.
-void span(const void *p, int64_t token, int64_t head, uint64_t nt, uint64_t nh, uint64_t dim, uint64_t size, uint64_t *lo, uint64_t *hi) {
-    *lo = reinterpret_cast<uint64_t>(p);
-    *hi = *lo + (uint64_t(nt - 1) * uint64_t(token) + uint64_t(nh - 1) * uint64_t(head) + dim) * size;
+Rows rows_of(const void *p, int64_t token, int64_t head, uint64_t nt, uint64_t nh, uint64_t dim, uint64_t size) {
+    return Rows{reinterpret_cast<uint64_t>(p), uint64_t(token) * size, uint64_t(head) * size, nt, nh, dim * size};
 }
 
 }  // namespace
@@ -260,8 +259,8 @@ int gac_rotary(const gac_rotary_args *args, int cuda_device, void *cuda_stream) 
     if (!isfinite(a.scale)) return fail(nullptr, GAC_ERR_INVALID_ARG, "scale must be finite%s");
     const uint64_t size = a.dtype == GAC_BF16 ? 2 : 4;
     RotaryDev d;
-    uint64_t lo[4], hi[4];
-    int spans = 0;
+    Rows x[2], y[2];
+    int both = 0;
     for (int w = 0; w < 2; ++w) {
         const gac_rotary_heads &h = a.qk[w];
         d.heads[w] = a.heads[w];
@@ -285,20 +284,21 @@ int gac_rotary(const gac_rotary_args *args, int cuda_device, void *cuda_stream) 
         if ((n_lesser > 1 && lesser < int64_t(a.head_dim)) ||
             (n_larger > 1 && uint64_t(larger) < (n_lesser - 1) * uint64_t(n_lesser > 1 ? lesser : 0) + a.head_dim))
             return fail(nullptr, GAC_ERR_INVALID_ARG, "output heads overlap one another%s");
+        x[w] = rows_of(h.x, h.x_token, h.x_head, a.n_tokens, a.heads[w], a.head_dim, size);
+        y[w] = rows_of(h.y, h.y_token, h.y_head, a.n_tokens, a.heads[w], a.head_dim, size);
+        ++both;
         if (h.x == h.y) {
             if (h.x_token != h.y_token || h.x_head != h.y_head)
                 return fail(nullptr, GAC_ERR_INVALID_ARG, "in place needs the same strides%s");
         } else {
-            span(h.x, h.x_token, h.x_head, a.n_tokens, a.heads[w], a.head_dim, size, &lo[spans], &hi[spans]);
-            span(h.y, h.y_token, h.y_head, a.n_tokens, a.heads[w], a.head_dim, size, &lo[spans + 1], &hi[spans + 1]);
-            if (lo[spans] < hi[spans + 1] && lo[spans + 1] < hi[spans])
+            if (x[w].p < y[w].end() && y[w].p < x[w].end())
                 return fail(nullptr, GAC_ERR_INVALID_ARG, "input and output heads overlap without being in place%s");
-            spans += 2;
         }
     }
-    // out of place: what one of the two writes must not be what the other reads
-    if (spans == 4 && ((lo[1] < hi[2] && lo[2] < hi[1]) || (lo[3] < hi[0] && lo[0] < hi[3])))
-        return fail(nullptr, GAC_ERR_INVALID_ARG, "output heads overlap the other input%s");
+    // views of one fused tensor lie between each other's heads; what one of the two writes must not be what the other
+    // reads or writes
+    if (both == 2 && (share(y[0], y[1]) || share(y[0], x[1]) || share(y[1], x[0])))
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "output heads overlap the heads of the other input or output%s");
     if (a.n_tokens == 0 || (a.heads[0] == 0 && a.heads[1] == 0)) return GAC_OK;
     if (!a.positions && (!a.cu_seqlens || reinterpret_cast<uint64_t>(a.cu_seqlens) % 4))
         return fail(nullptr, GAC_ERR_INVALID_ARG, "positions or cu_seqlens must be given, 4-byte aligned%s");

@@ -454,6 +454,12 @@ int gac_stats_static(const gac_tensor *list, uint32_t n, int g_dtype, int d_dtyp
  * gac_clip_apply      second half: reads the global sum of squares from sumsq_in
  *                     (device pointer) and writes the list's `out`
  * gac_clip_grad_norm  both halves on one rank
+ * gac_clip_set_timeout  longest wait of gac_clip_grad_norm's CTAs for one another between the
+ *                     two halves (1000 ms unless set; 0: none waits at all).  They are resident
+ *                     together, so the wait ends by itself.  If it ever ran out, no CTA goes
+ *                     on: nothing is written to any `out`, the norm told is NaN, and every
+ *                     further gac_clip_grad_norm and gac_clip_apply does the same until one of them has
+ *                     returned GAC_ERR_TIMEOUT, which takes a host_out.
  *   max_norm   > 0; +infinity means: never clip (the norm alone is wanted; an
  *              out-of-place list is still copied)
  *   eps        added to the norm in the factor, finite and >= 0 (1e-6 is usual)
@@ -478,8 +484,8 @@ typedef struct {
     double norm;        /* its square root                                                    */
     double scale;       /* factor applied                                                     */
     int32_t nonfinite;  /* 1: the norm is NaN or infinite, nothing was written                */
-    int32_t timed_out;  /* 1: a wait inside the kernel ran out (bounded, never in ordinary
-                           use), outputs are incomplete; with host_out GAC_ERR_TIMEOUT         */
+    int32_t timed_out;  /* 1: the wait inside the kernel ran out (never in ordinary use), nothing
+                           was written; with host_out GAC_ERR_TIMEOUT                          */
 } gac_clip_result;
 int gac_clip_init(gac_clip_ctx **out, const gac_clip_tensor *list, uint32_t n, int cuda_device);
 int gac_clip_sumsq(gac_clip_ctx *ctx, void *cuda_stream, double *sumsq_out);
@@ -487,6 +493,7 @@ int gac_clip_apply(gac_clip_ctx *ctx, void *cuda_stream, const double *sumsq_in,
                    float *norm_out, gac_clip_result *host_out);
 int gac_clip_grad_norm(gac_clip_ctx *ctx, void *cuda_stream, double max_norm, double eps, float *norm_out,
                        gac_clip_result *host_out);
+int gac_clip_set_timeout(gac_clip_ctx *ctx, uint32_t timeout_ms);
 int gac_clip_free(gac_clip_ctx *ctx);   /* NULL is accepted */
 
 /*

@@ -124,7 +124,8 @@ EXPORTS = ["gac_default_hparams", "gac_init", "gac_stats", "gac_stats_partial", 
            "gac_stats_static", "gac_default_adamw", "gac_attach_adamw", "gac_project_adamw",
            "gac_rebind", "gac_next_gradient_set", "gac_exchange_bytes", "gac_exchange_attach",
            "gac_stats_exchange", "gac_decide_exchange", "gac_clip_init", "gac_clip_sumsq", "gac_clip_apply",
-           "gac_clip_grad_norm", "gac_clip_free", "gac_rotary_freqs", "gac_rotary", "gac_attn_workspace",
+           "gac_clip_grad_norm", "gac_clip_set_timeout", "gac_clip_free", "gac_rotary_freqs", "gac_rotary",
+           "gac_attn_workspace",
            "gac_attn_forward", "gac_attn_backward", "gac_attn_check"]
 
 _lib = None
@@ -187,6 +188,7 @@ def load_library() -> ctypes.CDLL:
     L.gac_clip_sumsq.argtypes = [vp, vp, vp]
     L.gac_clip_apply.argtypes = [vp, vp, vp, f64, f64, vp, P(gac_clip_result)]
     L.gac_clip_grad_norm.argtypes = [vp, vp, f64, f64, vp, P(gac_clip_result)]
+    L.gac_clip_set_timeout.argtypes = [vp, u32]
     L.gac_clip_free.argtypes = [vp]
     L.gac_rotary_freqs.argtypes = [P(f64), u32, f64, i32, f64, f64, f64, f64]
     # the structs travel as packed bytes (or ctypes.byref of the structures above)
@@ -196,8 +198,8 @@ def load_library() -> ctypes.CDLL:
     L.gac_attn_forward.argtypes = [vp, i32, vp]
     L.gac_attn_backward.argtypes = [vp, vp, i32, vp]
     L.gac_attn_check.argtypes = [i32, vp]
-    for name in ("gac_clip_init", "gac_clip_sumsq", "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_free",
-                 "gac_rotary_freqs", "gac_rotary", "gac_attn_forward", "gac_attn_backward", "gac_attn_check"):
+    for name in ("gac_clip_init", "gac_clip_sumsq", "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_set_timeout",
+                 "gac_clip_free", "gac_rotary_freqs", "gac_rotary", "gac_attn_forward", "gac_attn_backward", "gac_attn_check"):
         getattr(L, name).restype = i32
     for name in ("gac_init", "gac_stats", "gac_stats_partial", "gac_decide", "gac_project",
                  "gac_free", "gac_set_launch", "gac_get_info"):
@@ -569,7 +571,8 @@ def _norm_ptr(norm_out: Optional[torch.Tensor]) -> Optional[int]:
 def gac_clip_grad_norm(ctx: ClipContext, max_norm: float, eps: float = 1e-6, norm_out: Optional[torch.Tensor] = None,
                        stream=None, fetch: bool = False) -> Optional[gac_clip_result]:
     """Norm of the list, and the list scaled by min(1, max_norm/(norm + eps)).  With fetch=False nothing
-    leaves the device; a non-finite norm leaves every output as it was and is told by the record."""
+    leaves the device; a non-finite norm leaves every output as it was and is told by the record.  So is a wait that
+    ran out, as a norm of NaN and, with fetch=True, as GacError(GAC_ERR_TIMEOUT)."""
     res = gac_clip_result() if fetch else None
     raw = _on(stream, ctx.device)[0]
     rc = load_library().gac_clip_grad_norm(ctx.handle, raw, max_norm, eps, _norm_ptr(norm_out),
@@ -593,6 +596,11 @@ def gac_clip_apply(ctx: ClipContext, sumsq_in: torch.Tensor, max_norm: float, ep
     rc = load_library().gac_clip_apply(ctx.handle, _on(stream, ctx.device)[0], sumsq_in.data_ptr(), max_norm, eps,
                                        _norm_ptr(norm_out), ctypes.byref(res) if fetch else None)
     return _clip_result(rc, res)
+
+
+def gac_clip_set_timeout(ctx: ClipContext, timeout_ms: int) -> None:
+    """Longest wait of the CTAs for one another inside gac_clip_grad_norm (1000 ms unless set)."""
+    _check(load_library().gac_clip_set_timeout(ctx.handle, timeout_ms))
 
 
 def gac_clip_free(ctx: ClipContext) -> None:

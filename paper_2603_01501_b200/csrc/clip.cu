@@ -148,23 +148,30 @@ __device__ double all_squares(const double *partials, double *shared) {
     return cta_sum(s, shared);
 }
 
-// Waits until every CTA of a cooperative launch has arrived.  They are all resident, so this ends by itself; the
-// limit (one second) only keeps a mistake from holding the GPU.  Called by one thread of each CTA.
-__device__ bool meet(unsigned long long *arrived) {
+// Waits until every CTA of a cooperative launch has arrived.  They are all resident, so this ends by itself; the limit only
+// keeps a mistake from holding the GPU.  Arrivals and giving up are bits of one word, so that all CTAs come to the
+// same end: once the last has arrived nobody can give up any more, and once one has given up nobody goes on.  Called by
+// one thread of each CTA.
+constexpr unsigned long long kGaveUp = 1ull << 63;
+__device__ bool meet(unsigned long long *arrived, unsigned long long limit_ns) {
     __threadfence();
+    if (limit_ns == 0) atomicOr(arrived, kGaveUp);   // not even for those that are nearly there; this one has not arrived yet
     const unsigned long long old = atomicAdd(arrived, 1ull), target = (old / gridDim.x + 1) * gridDim.x;
-    unsigned long long t0 = 0, t;
-    for (uint32_t i = 0; i < (1u << 28); ++i) {
+    if (old & kGaveUp) return false;   // another CTA did, or an earlier call that nobody has been told of yet
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    bool late = false;
+    for (uint32_t i = 0;; ++i) {
         unsigned long long now;
         asm volatile("ld.acquire.gpu.u64 %0, [%1];" : "=l"(now) : "l"(arrived) : "memory");
+        if (now & kGaveUp) return false;
         if (now >= target) return true;
-        if ((i & 1023u) == 1023u) {
+        if (!late && i % 1024 == 0) {
             asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-            if (!t0) t0 = t;
-            if (t - t0 > 1000000000ull) return false;
+            late = t - t0 >= limit_ns || i >= (1u << 28);
         }
+        if (late && atomicCAS(arrived, now, now | kGaveUp) == now) return false;   // fails only where another CTA arrives
     }
-    return false;
 }
 
 enum { kSumOnly = 0, kApplyOnly = 1, kBoth = 2 };
@@ -173,8 +180,8 @@ enum { kSumOnly = 0, kApplyOnly = 1, kBoth = 2 };
 // (126 MB), and the stores are marked to leave it first.
 template <int MODE>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
-clip_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, double *partials, unsigned long long *arrived, double *sumsq,
-            double max_norm, double eps, float *norm_out, gac_clip_result *rec) {
+clip_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, double *partials, unsigned long long *arrived,
+            unsigned long long limit_ns, double *sumsq, double max_norm, double eps, float *norm_out, gac_clip_result *rec) {
     __shared__ double shared[kThreads / 32];
     __shared__ float factor;
     __shared__ int state;   // 0 as it should be, 1 not finite, 2 a wait ran out; kSumOnly: 1 in the last CTA
@@ -184,7 +191,7 @@ clip_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, double *part
             if (threadIdx.x == 0) {
                 partials[blockIdx.x] = mine;
                 __threadfence();
-                state = (atomicAdd(arrived, 1ull) + 1) % gridDim.x == 0;
+                state = ((atomicAdd(arrived, 1ull) + 1) & ~kGaveUp) % gridDim.x == 0;
             }
             __syncthreads();
             if (!state) return;
@@ -195,16 +202,23 @@ clip_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, double *part
         }
         if (threadIdx.x == 0) {
             partials[blockIdx.x] = mine;
-            state = meet(arrived) ? 0 : 2;
+            state = meet(arrived, limit_ns) ? 0 : 2;
         }
-        __syncthreads();
-        if (state == 2) {
-            if (threadIdx.x == 0) rec->timed_out = 1;
-            return;
+    } else if (threadIdx.x == 0) {
+        state = (__ldcg(arrived) & kGaveUp) ? 2 : 0;
+    }
+    __syncthreads();
+    if (state == 2) {   // in every CTA
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            rec->sumsq = rec->norm = rec->scale = __longlong_as_double(0x7FF8000000000000ll);
+            rec->timed_out = 1;   // the host clears it once it has read it
+            if (norm_out) *norm_out = __int_as_float(0x7FC00000);
         }
+        return;
     }
     double s2 = 0.0;
     if (MODE == kBoth) s2 = all_squares(partials, shared);
+    else __syncthreads();   // state has been read
     if (threadIdx.x == 0) {
         if (MODE == kApplyOnly) s2 = *sumsq;
         const double norm = __dsqrt_rn(s2), f = __ddiv_rn(max_norm, __dadd_rn(norm, eps));
@@ -216,7 +230,6 @@ clip_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, double *part
             rec->norm = norm;
             rec->scale = bad ? 1.0 : double(factor);
             rec->nonfinite = bad;
-            rec->timed_out = 0;
             if (norm_out) *norm_out = __double2float_rn(norm);
         }
     }
@@ -269,6 +282,7 @@ struct gac_clip_ctx {
     unsigned long long *d_arrived = nullptr;   // CTAs so far, over all calls
     gac_clip_result *d_rec = nullptr;
     gac_clip_result *h_rec = nullptr;  // pinned
+    unsigned long long limit_ns = 1000000000ull;
 };
 
 namespace {
@@ -354,8 +368,8 @@ int read_record(gac_clip_ctx *c, cudaStream_t s, gac_clip_result *host_out) {
     GAC_CUDA(nullptr, cudaStreamSynchronize(s));
     *host_out = *c->h_rec;
     if (host_out->timed_out) {
-        cudaMemsetAsync(c->d_arrived, 0, sizeof(*c->d_arrived), s);
-        cudaMemsetAsync(c->d_rec, 0, sizeof(*c->d_rec), s);
+        GAC_CUDA(nullptr, cudaMemsetAsync(c->d_arrived, 0, sizeof(*c->d_arrived), s));
+        GAC_CUDA(nullptr, cudaMemsetAsync(c->d_rec, 0, sizeof(*c->d_rec), s));
         return fail(nullptr, GAC_ERR_TIMEOUT, "a wait inside the clipping kernel ran out%s");
     }
     if (host_out->nonfinite) return fail(nullptr, GAC_ERR_NONFINITE, "NaN or Inf met in the gradient norm%s");
@@ -412,7 +426,7 @@ int gac_clip_sumsq(gac_clip_ctx *ctx, void *cuda_stream, double *sumsq_out) {
     Range range("gac_clip_sumsq");
     DeviceGuard guard(ctx->device);
     clip_kernel<kSumOnly><<<ctx->grid, kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
-        ctx->d_chunks, ctx->n_chunks, ctx->d_partials, ctx->d_arrived, sumsq_out, 0.0, 0.0, nullptr, ctx->d_rec);
+        ctx->d_chunks, ctx->n_chunks, ctx->d_partials, ctx->d_arrived, ctx->limit_ns, sumsq_out, 0.0, 0.0, nullptr, ctx->d_rec);
     GAC_CUDA(nullptr, cudaGetLastError());
     return GAC_OK;
 }
@@ -426,7 +440,7 @@ int gac_clip_apply(gac_clip_ctx *ctx, void *cuda_stream, const double *sumsq_in,
     Range range("gac_clip_apply");
     DeviceGuard guard(ctx->device);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    clip_kernel<kApplyOnly><<<ctx->grid, kThreads, 0, s>>>(ctx->d_chunks, ctx->n_chunks, ctx->d_partials, ctx->d_arrived,
+    clip_kernel<kApplyOnly><<<ctx->grid, kThreads, 0, s>>>(ctx->d_chunks, ctx->n_chunks, ctx->d_partials, ctx->d_arrived, ctx->limit_ns,
                                                            const_cast<double *>(sumsq_in), max_norm, eps, norm_out, ctx->d_rec);
     GAC_CUDA(nullptr, cudaGetLastError());
     return read_record(ctx, s, host_out);
@@ -440,9 +454,15 @@ int gac_clip_grad_norm(gac_clip_ctx *ctx, void *cuda_stream, double max_norm, do
     DeviceGuard guard(ctx->device);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     double *none = nullptr;
-    void *args[] = {&ctx->d_chunks, &ctx->n_chunks, &ctx->d_partials, &ctx->d_arrived, &none, &max_norm, &eps, &norm_out, &ctx->d_rec};
+    void *args[] = {&ctx->d_chunks, &ctx->n_chunks, &ctx->d_partials, &ctx->d_arrived, &ctx->limit_ns, &none, &max_norm, &eps, &norm_out, &ctx->d_rec};
     GAC_CUDA(nullptr, cudaLaunchCooperativeKernel(reinterpret_cast<const void *>(&clip_kernel<kBoth>), dim3(ctx->grid), dim3(kThreads), args, 0, s));
     return read_record(ctx, s, host_out);
+}
+
+int gac_clip_set_timeout(gac_clip_ctx *ctx, uint32_t timeout_ms) {
+    if (!ctx) return fail(nullptr, GAC_ERR_INVALID_ARG, "ctx is NULL%s");
+    ctx->limit_ns = 1000000ull * timeout_ms;
+    return GAC_OK;
 }
 
 int gac_clip_free(gac_clip_ctx *ctx) {

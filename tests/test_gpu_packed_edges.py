@@ -33,3 +33,38 @@ def test_second_derivative_through_attention_is_refused():
     first, = torch.autograd.grad(packed.attention(q, k, v, cu).float().square().sum(), q, create_graph=True)
     with pytest.raises(RuntimeError):
         (first.float() * q.float()).sum().backward()
+
+
+def test_a_wait_that_ran_out_is_told_and_nothing_is_half_clipped():
+    g = torch.randn(1 << 24, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    keep, out, told = g.clone(), torch.full_like(g, 5.0), torch.zeros(1, device="cuda")
+    for ctx, seen in ((gb.gac_clip_init([g]), g), (gb.gac_clip_init([g], [out]), out)):
+        before = seen.clone()
+        gb.gac_clip_set_timeout(ctx, 0)                         # no CTA waits for the others
+        gb.gac_clip_grad_norm(ctx, 1.0, norm_out=told)
+        assert math.isnan(float(told)) and torch.equal(seen, before)
+        gb.gac_clip_set_timeout(ctx, 1000)                      # not told yet: neither call goes on
+        told.zero_()
+        gb.gac_clip_grad_norm(ctx, 1.0, norm_out=told)
+        assert math.isnan(float(told)) and torch.equal(seen, before)
+        with pytest.raises(gb.GacError) as e:
+            gb.gac_clip_apply(ctx, torch.ones(1, dtype=torch.float64, device="cuda"), 0.1, fetch=True)
+        assert e.value.status == gb.GAC_ERR_TIMEOUT and torch.equal(seen, before)
+        norm = float(keep.double().norm())
+        res = gb.gac_clip_grad_norm(ctx, 0.5 * norm, norm_out=told, fetch=True)
+        assert res.timed_out == 0 and abs(res.norm - norm) <= 1e-10 * norm and abs(float(told) - norm) <= 1e-6 * norm
+        assert bool(((seen.double() - 0.5 * keep.double()).abs() <= 2.02 * U * keep.double().abs() + 1e-6 / norm * keep.abs()).all())
+        gb.gac_clip_free(ctx)
+        g.copy_(keep)
+
+
+def test_sums_alone_do_not_wait_and_go_on_after_one_that_ran_out():
+    g = torch.ones(1 << 22, device="cuda")
+    ctx, total = gb.gac_clip_init([g]), torch.zeros(1, dtype=torch.float64, device="cuda")
+    gb.gac_clip_set_timeout(ctx, 0)
+    for _ in range(3):
+        gb.gac_clip_grad_norm(ctx, 1.0)
+        total.zero_()
+        gb.gac_clip_sumsq(ctx, total)
+        assert float(total) == 1 << 22
+    assert bool((g == 1.0).all())

@@ -17,6 +17,8 @@
 
 #include <algorithm>
 #include <cstddef>
+#include <map>
+#include <mutex>
 #include <new>
 #include <utility>
 #include <vector>
@@ -277,19 +279,18 @@ struct gac_clip_ctx {
     int device = 0, sms = 0;
     uint32_t n_chunks = 0;
     uint32_t grid = 0;
-    ClipChunk *d_chunks = nullptr;
+    ClipChunk *d_chunks = nullptr;     // the allocation; what follows lies behind the table
     double *d_partials = nullptr;      // one per CTA
     unsigned long long *d_arrived = nullptr;   // CTAs so far, over all calls
     gac_clip_result *d_rec = nullptr;
-    gac_clip_result *h_rec = nullptr;  // pinned
+    gac_clip_result *h_rec = nullptr;  // pinned, from the first call that asks for a record on
     unsigned long long limit_ns = 1000000000ull;
 };
 
 namespace {
 
 void release(gac_clip_ctx *c) {
-    if (c->d_chunks) cudaFree(c->d_chunks);
-    if (c->d_partials) cudaFree(c->d_partials);
+    if (c->d_chunks) cudaFree(c->d_chunks);   // and all that lies behind the table
     if (c->h_rec) cudaFreeHost(c->h_rec);
 }
 
@@ -323,6 +324,17 @@ int check_list(const gac_clip_tensor *list, uint32_t n) {
     return GAC_OK;
 }
 
+// A stream of the library's own, which waits for nobody else's work; one per device, made once (making one takes 100 us).
+int setup_stream(int device, cudaStream_t *out) {
+    static std::mutex guard;
+    static std::map<int, cudaStream_t> streams;
+    std::lock_guard<std::mutex> lock(guard);
+    cudaStream_t &s = streams[device];
+    if (!s) GAC_CUDA(nullptr, cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking));
+    *out = s;
+    return GAC_OK;
+}
+
 int setup(gac_clip_ctx *c, const gac_clip_tensor *list, uint32_t n) {
     GAC_CUDA(nullptr, cudaDeviceGetAttribute(&c->sms, cudaDevAttrMultiProcessorCount, c->device));
     uint64_t total = 0;
@@ -350,20 +362,26 @@ int setup(gac_clip_ctx *c, const gac_clip_tensor *list, uint32_t n) {
     GAC_CUDA(nullptr, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, clip_kernel<kBoth>, kThreads, 0));
     resident = std::max(1, std::min(resident, kCtasPerSm));
     c->grid = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(uint64_t(c->sms) * resident, table.size())));
-    const size_t work = (size_t(c->grid) + 1) * sizeof(double) + 256 + sizeof(gac_clip_result);
-    GAC_CUDA(nullptr, cudaMalloc(&c->d_chunks, std::max<size_t>(1, table.size()) * sizeof(ClipChunk)));
-    if (!table.empty())
-        GAC_CUDA(nullptr, cudaMemcpy(c->d_chunks, table.data(), table.size() * sizeof(ClipChunk), cudaMemcpyHostToDevice));
-    GAC_CUDA(nullptr, cudaMalloc(&c->d_partials, work));
-    GAC_CUDA(nullptr, cudaMemset(c->d_partials, 0, work));
-    c->d_rec = reinterpret_cast<gac_clip_result *>(c->d_partials + c->grid + 1);
+    // One block of memory: the table, and behind it, from zeros, partial sums, record and counter.  The call does not return
+    // before it is all there: the first launch may be on a stream that nothing else orders behind this call.
+    const size_t partials = (size_t(c->grid) + 1) * sizeof(double), chunks = table.size() * sizeof(ClipChunk);
+    const size_t behind = partials + sizeof(gac_clip_result) + sizeof(*c->d_arrived);
+    table.resize(table.size() + (behind + sizeof(ClipChunk) - 1) / sizeof(ClipChunk));
+    cudaStream_t own;
+    if (int rc = setup_stream(c->device, &own)) return rc;
+    GAC_CUDA(nullptr, cudaMalloc(&c->d_chunks, table.size() * sizeof(ClipChunk)));
+    char *base = reinterpret_cast<char *>(c->d_chunks);
+    c->d_partials = reinterpret_cast<double *>(base + chunks);
+    c->d_rec = reinterpret_cast<gac_clip_result *>(base + chunks + partials);
     c->d_arrived = reinterpret_cast<unsigned long long *>(c->d_rec + 1);
-    GAC_CUDA(nullptr, cudaMallocHost(&c->h_rec, sizeof(gac_clip_result)));
+    GAC_CUDA(nullptr, cudaMemcpyAsync(base, table.data(), table.size() * sizeof(ClipChunk), cudaMemcpyHostToDevice, own));
+    GAC_CUDA(nullptr, cudaStreamSynchronize(own));
     return GAC_OK;
 }
 
 int read_record(gac_clip_ctx *c, cudaStream_t s, gac_clip_result *host_out) {
     if (!host_out) return GAC_OK;
+    if (!c->h_rec) GAC_CUDA(nullptr, cudaMallocHost(&c->h_rec, sizeof(gac_clip_result)));   // page-locking takes longer than all of gac_clip_init
     GAC_CUDA(nullptr, cudaMemcpyAsync(c->h_rec, c->d_rec, sizeof(gac_clip_result), cudaMemcpyDeviceToHost, s));
     GAC_CUDA(nullptr, cudaStreamSynchronize(s));
     *host_out = *c->h_rec;
@@ -408,7 +426,7 @@ int gac_clip_init(gac_clip_ctx **out, const gac_clip_tensor *list, uint32_t n, i
             delete c;
             return rc;
         }
-    } catch (const std::bad_alloc &) {   // nothing may be thrown through the C boundary
+    } catch (...) {   // nothing may be thrown through the C boundary
         if (c) {
             release(c);
             delete c;

@@ -68,3 +68,19 @@ def test_sums_alone_do_not_wait_and_go_on_after_one_that_ran_out():
         gb.gac_clip_sumsq(ctx, total)
         assert float(total) == 1 << 22
     assert bool((g == 1.0).all())
+
+
+def test_the_first_call_may_be_on_a_stream_of_its_own():
+    """A new context used at once on a stream that does not wait for the default one, which is busy."""
+    side = torch.cuda.Stream()
+    g = [torch.ones(n, device="cuda") for n in (3, 1 << 20, 70_001)]
+    norm = math.sqrt(3 + (1 << 20) + 70_001)
+    told = [torch.zeros(1, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    for t in told:
+        torch.cuda._sleep(20_000_000)
+        ctx = gb.gac_clip_init(g)
+        gb.gac_clip_grad_norm(ctx, math.inf, norm_out=t, stream=side)
+        side.synchronize()
+        assert abs(float(t.item() if torch.cuda.current_stream().query() else t) - norm) <= 2 * U * norm
+        gb.gac_clip_free(ctx)

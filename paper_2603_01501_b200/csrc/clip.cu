@@ -443,6 +443,7 @@ int gac_clip_sumsq(gac_clip_ctx *ctx, void *cuda_stream, double *sumsq_out) {
         return fail(nullptr, GAC_ERR_INVALID_ARG, "sumsq_out must be an 8-byte aligned device pointer%s");
     Range range("gac_clip_sumsq");
     DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
     clip_kernel<kSumOnly><<<ctx->grid, kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
         ctx->d_chunks, ctx->n_chunks, ctx->d_partials, ctx->d_arrived, ctx->limit_ns, sumsq_out, 0.0, 0.0, nullptr, ctx->d_rec);
     GAC_CUDA(nullptr, cudaGetLastError());
@@ -457,6 +458,7 @@ int gac_clip_apply(gac_clip_ctx *ctx, void *cuda_stream, const double *sumsq_in,
     if (int rc = check_limits(max_norm, eps, norm_out)) return rc;
     Range range("gac_clip_apply");
     DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     clip_kernel<kApplyOnly><<<ctx->grid, kThreads, 0, s>>>(ctx->d_chunks, ctx->n_chunks, ctx->d_partials, ctx->d_arrived, ctx->limit_ns,
                                                            const_cast<double *>(sumsq_in), max_norm, eps, norm_out, ctx->d_rec);
@@ -470,6 +472,7 @@ int gac_clip_grad_norm(gac_clip_ctx *ctx, void *cuda_stream, double max_norm, do
     if (int rc = check_limits(max_norm, eps, norm_out)) return rc;
     Range range("gac_clip_grad_norm");
     DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     double *none = nullptr;
     void *args[] = {&ctx->d_chunks, &ctx->n_chunks, &ctx->d_partials, &ctx->d_arrived, &ctx->limit_ns, &none, &max_norm, &eps, &norm_out, &ctx->d_rec};

@@ -560,12 +560,12 @@ def _clip_result(rc: int, res) -> Optional[gac_clip_result]:
     return res
 
 
-def _norm_ptr(norm_out: Optional[torch.Tensor]) -> Optional[int]:
-    if norm_out is None:
+def _scalar_ptr(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, ctx: ClipContext) -> Optional[int]:
+    if t is None:
         return None
-    if not (norm_out.is_cuda and norm_out.dtype == torch.float32 and norm_out.numel() >= 1):
-        raise ValueError("norm_out must be a CUDA float32 tensor")
-    return norm_out.data_ptr()
+    if not (t.is_cuda and t.device == ctx.device and t.dtype == dtype and t.numel() >= 1):
+        raise ValueError(f"{name} must be a {str(dtype)[6:]} tensor on the list's device")
+    return t.data_ptr()
 
 
 def gac_clip_grad_norm(ctx: ClipContext, max_norm: float, eps: float = 1e-6, norm_out: Optional[torch.Tensor] = None,
@@ -575,26 +575,24 @@ def gac_clip_grad_norm(ctx: ClipContext, max_norm: float, eps: float = 1e-6, nor
     ran out, as a norm of NaN and, with fetch=True, as GacError(GAC_ERR_TIMEOUT)."""
     res = gac_clip_result() if fetch else None
     raw = _on(stream, ctx.device)[0]
-    rc = load_library().gac_clip_grad_norm(ctx.handle, raw, max_norm, eps, _norm_ptr(norm_out),
+    rc = load_library().gac_clip_grad_norm(ctx.handle, raw, max_norm, eps, _scalar_ptr(norm_out, "norm_out", torch.float32, ctx),
                                            ctypes.byref(res) if fetch else None)
     return _clip_result(rc, res)
 
 
 def gac_clip_sumsq(ctx: ClipContext, sumsq_out: torch.Tensor, stream=None) -> None:
     """Sharded form: this rank's sum of squares into a CUDA float64 tensor, for the caller's all-reduce."""
-    if not (sumsq_out.is_cuda and sumsq_out.dtype == torch.float64 and sumsq_out.numel() >= 1):
-        raise ValueError("sumsq_out must be a CUDA float64 tensor")
-    _check(load_library().gac_clip_sumsq(ctx.handle, _on(stream, ctx.device)[0], sumsq_out.data_ptr()))
+    to = _scalar_ptr(sumsq_out, "sumsq_out", torch.float64, ctx)
+    _check(load_library().gac_clip_sumsq(ctx.handle, _on(stream, ctx.device)[0], to))
 
 
 def gac_clip_apply(ctx: ClipContext, sumsq_in: torch.Tensor, max_norm: float, eps: float = 1e-6,
                    norm_out: Optional[torch.Tensor] = None, stream=None, fetch: bool = False) -> Optional[gac_clip_result]:
     """Sharded form: scales this rank's list by the factor that follows from the global sum of squares."""
-    if not (sumsq_in.is_cuda and sumsq_in.dtype == torch.float64 and sumsq_in.numel() >= 1):
-        raise ValueError("sumsq_in must be a CUDA float64 tensor")
     res = gac_clip_result() if fetch else None
-    rc = load_library().gac_clip_apply(ctx.handle, _on(stream, ctx.device)[0], sumsq_in.data_ptr(), max_norm, eps,
-                                       _norm_ptr(norm_out), ctypes.byref(res) if fetch else None)
+    rc = load_library().gac_clip_apply(ctx.handle, _on(stream, ctx.device)[0],
+                                       _scalar_ptr(sumsq_in, "sumsq_in", torch.float64, ctx), max_norm, eps,
+                                       _scalar_ptr(norm_out, "norm_out", torch.float32, ctx), ctypes.byref(res) if fetch else None)
     return _clip_result(rc, res)
 
 

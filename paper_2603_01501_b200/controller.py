@@ -20,6 +20,10 @@ gradient tensors instead of the optimizer:
     loss.backward()
     if ctl.step():
         optimizer.step()      # reads .grad, must not modify it
+
+Clipping goes with the rule there (``HParams(clip_max_norm=...)``): on a step that
+leaves the gradient as it is, ``.grad`` IS the stored direction, and
+``packed.GradientClipper`` refuses to scale it.
 """
 from __future__ import annotations
 
@@ -98,6 +102,7 @@ class GradientAlignmentController:
             out = self.sets[self.last.out_set]
             for p, o in zip(self.params, out):
                 p.grad = o.view_as(p)
+                p.grad._gac_direction = self.last.out_set == self.last.g_set   # told to whoever would write it
         return self.last.regime != gb.GAC_REGIME_VIOLATION and not self.last.nonfinite
 
     def zero_grad(self) -> None:

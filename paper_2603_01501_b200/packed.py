@@ -84,7 +84,9 @@ class GradientClipper:
     """Clips the gradients of a list of parameters by their global norm, in place, without waiting for the host.
 
     The table of the list is built on first use and again whenever a ``.grad`` tensor has moved.  Parameters without a
-    gradient are left out, as an optimizer leaves them out."""
+    gradient are left out, as an optimizer leaves them out.  For lists that do not go through the alignment rule: with a
+    GradientAlignmentController, ``HParams(clip_max_norm=...)`` clips in the rule's own pass, and in exchange mode
+    that is the only way (the gradient may be the stored direction itself, which is refused here)."""
 
     def __init__(self, params: Iterable[torch.nn.Parameter]):
         self.params: List[torch.nn.Parameter] = [p for p in params if p.requires_grad]
@@ -102,6 +104,9 @@ class GradientClipper:
             return self.norm
         if not all(g.is_contiguous() for g in grads):
             raise RuntimeError("gradients must be contiguous")
+        if any(getattr(g, "_gac_direction", False) for g in grads):
+            raise RuntimeError("a gradient is the stored direction of a controller in exchange mode and must not be "
+                               "modified: clip with HParams(clip_max_norm=...)")
         bound = [(g.data_ptr(), g.numel(), g.dtype) for g in grads]
         if self._ctx is None or bound != self._bound:
             if self._ctx is not None:

@@ -38,3 +38,46 @@ def test_results_on_another_device_than_the_list_are_refused(monkeypatch):
                  lambda: gb.gac_clip_apply(ctx, there, 1.0), lambda: gb.gac_clip_apply(ctx, here, 1.0, norm_out=norm)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.fixture
+def library(monkeypatch):
+    """Stand-ins for the rule in exchange mode (a safe step, g unchanged) and for clipping; `calls` records the latter."""
+    calls = types.SimpleNamespace(made=[], clipped=0, result=dict(g_set=0, out_set=0), next=0)
+
+    def stats(ctx, t, staleness=0):
+        return types.SimpleNamespace(regime=gb.GAC_REGIME_SAFE, nonfinite=0, **calls.result)
+
+    def make(grads, *_, **__):
+        calls.made.append([g.data_ptr() for g in grads])
+        return types.SimpleNamespace(handle=len(calls.made))
+
+    def clip(ctx, max_norm, eps=1e-6, norm_out=None, stream=None, fetch=False):
+        calls.clipped += 1
+
+    def project(ctx):
+        calls.next ^= 1
+
+    for name, f in (("gac_init", lambda g, d, hp: object()), ("gac_stats", stats), ("gac_project", project),
+                    ("gac_next_gradient_set", lambda ctx: calls.next), ("gac_free", lambda ctx: None),
+                    ("gac_clip_init", make), ("gac_clip_grad_norm", clip), ("gac_clip_free", lambda ctx: None)):
+        monkeypatch.setattr(gb, name, f)
+    return calls
+
+
+def test_the_stored_direction_of_an_exchange_step_is_not_clipped(library):
+    from paper_2603_01501_b200.controller import GradientAlignmentController
+    params = [torch.nn.Parameter(torch.zeros(n)) for n in (3, 5)]
+    controller, clipper = GradientAlignmentController(params, exchange=True), packed.GradientClipper(params)
+    for p in params:
+        p.grad = torch.ones_like(p)
+    controller.step()                       # safe: .grad is the stored direction itself
+    with pytest.raises(RuntimeError, match="clip_max_norm"):
+        clipper.clip(1.0)
+    assert library.clipped == 0
+    controller.zero_grad()                  # the free tensors
+    clipper.clip(1.0)
+    library.result = dict(g_set=1, out_set=0)
+    controller.step()                       # a projection: written into the free tensors, which may be clipped
+    clipper.clip(1.0)
+    assert library.clipped == 2

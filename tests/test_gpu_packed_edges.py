@@ -84,3 +84,22 @@ def test_the_first_call_may_be_on_a_stream_of_its_own():
         side.synchronize()
         assert abs(float(t.item() if torch.cuda.current_stream().query() else t) - norm) <= 2 * U * norm
         gb.gac_clip_free(ctx)
+
+
+def test_the_stored_direction_of_an_exchange_step_is_not_clipped():
+    from paper_2603_01501_b200.controller import GradientAlignmentController
+    params = [torch.nn.Parameter(torch.zeros(n, device="cuda")) for n in (1000, 77)]
+    controller, clipper = GradientAlignmentController(params, exchange=True), packed.GradientClipper(params)
+    for p in params:
+        p.grad = torch.ones_like(p)
+    controller.step()                       # the first step is safe: .grad is the stored direction
+    with pytest.raises(RuntimeError, match="clip_max_norm"):
+        clipper.clip(1.0)
+    assert all(bool((s == 1.0).all()) for s in controller.snapshot)
+    controller.zero_grad()
+    for p in params:
+        p.grad.add_(2.0)
+    clipper.clip(1.0)                       # before the rule the gradients are the caller's
+    assert abs(math.sqrt(sum(float(p.grad.double().square().sum()) for p in params)) - 1.0) < 1e-5
+    controller.close()
+    clipper.close()

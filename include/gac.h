@@ -448,6 +448,9 @@ int gac_stats_static(const gac_tensor *list, uint32_t n, int g_dtype, int d_dtyp
  *                     `g` and written at `out`; out == g clips in place, and
  *                     then nothing is written when the factor is 1.  Ranges
  *                     must not overlap otherwise.  numel = 0 is allowed.
+ * gac_clip_rebind     the same list at other addresses (as many tensors, of the same sizes and types;
+ *                     a framework that re-allocates its gradients): writes the table on the given
+ *                     stream, allocates nothing and waits for nothing
  * gac_clip_sumsq      sharded form, first half: writes the sum of squares of this
  *                     rank's list to sumsq_out (device pointer, one double, 8-byte
  *                     aligned) for the caller's all-reduce
@@ -488,6 +491,7 @@ typedef struct {
                            was written; with host_out GAC_ERR_TIMEOUT                          */
 } gac_clip_result;
 int gac_clip_init(gac_clip_ctx **out, const gac_clip_tensor *list, uint32_t n, int cuda_device);
+int gac_clip_rebind(gac_clip_ctx *ctx, const gac_clip_tensor *list, uint32_t n, void *cuda_stream);
 int gac_clip_sumsq(gac_clip_ctx *ctx, void *cuda_stream, double *sumsq_out);
 int gac_clip_apply(gac_clip_ctx *ctx, void *cuda_stream, const double *sumsq_in, double max_norm, double eps,
                    float *norm_out, gac_clip_result *host_out);

@@ -123,8 +123,8 @@ EXPORTS = ["gac_default_hparams", "gac_init", "gac_stats", "gac_stats_partial", 
            "gac_project", "gac_free", "gac_last_error", "gac_set_launch", "gac_get_info",
            "gac_stats_static", "gac_default_adamw", "gac_attach_adamw", "gac_project_adamw",
            "gac_rebind", "gac_next_gradient_set", "gac_exchange_bytes", "gac_exchange_attach",
-           "gac_stats_exchange", "gac_decide_exchange", "gac_clip_init", "gac_clip_sumsq", "gac_clip_apply",
-           "gac_clip_grad_norm", "gac_clip_set_timeout", "gac_clip_free", "gac_rotary_freqs", "gac_rotary",
+           "gac_stats_exchange", "gac_decide_exchange", "gac_clip_init", "gac_clip_rebind", "gac_clip_sumsq",
+           "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_set_timeout", "gac_clip_free", "gac_rotary_freqs", "gac_rotary",
            "gac_attn_workspace",
            "gac_attn_forward", "gac_attn_backward", "gac_attn_check"]
 
@@ -185,6 +185,7 @@ def load_library() -> ctypes.CDLL:
     L.gac_decide_exchange.restype = i32
     P, f64 = ctypes.POINTER, ctypes.c_double
     L.gac_clip_init.argtypes = [P(vp), P(gac_clip_tensor), u32, i32]
+    L.gac_clip_rebind.argtypes = [vp, P(gac_clip_tensor), u32, vp]
     L.gac_clip_sumsq.argtypes = [vp, vp, vp]
     L.gac_clip_apply.argtypes = [vp, vp, vp, f64, f64, vp, P(gac_clip_result)]
     L.gac_clip_grad_norm.argtypes = [vp, vp, f64, f64, vp, P(gac_clip_result)]
@@ -198,7 +199,7 @@ def load_library() -> ctypes.CDLL:
     L.gac_attn_forward.argtypes = [vp, i32, vp]
     L.gac_attn_backward.argtypes = [vp, vp, i32, vp]
     L.gac_attn_check.argtypes = [i32, vp]
-    for name in ("gac_clip_init", "gac_clip_sumsq", "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_set_timeout",
+    for name in ("gac_clip_init", "gac_clip_rebind", "gac_clip_sumsq", "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_set_timeout",
                  "gac_clip_free", "gac_rotary_freqs", "gac_rotary", "gac_attn_forward", "gac_attn_backward", "gac_attn_check"):
         getattr(L, name).restype = i32
     for name in ("gac_init", "gac_stats", "gac_stats_partial", "gac_decide", "gac_project",
@@ -513,12 +514,16 @@ def _check(rc: int) -> None:
 
 
 class ClipContext:
-    """Owner of one ``gac_clip_ctx``; keeps references to the tensors in its table."""
+    """Owner of one ``gac_clip_ctx``; keeps references to the tensors in its table, unless told that the caller does."""
 
-    def __init__(self, handle: int, g_list, out_list, device: int):
+    def __init__(self, handle: int, device: int, keep: bool):
         self.handle = ctypes.c_void_p(handle)
         self.device = torch.device("cuda", device)
-        self._keep = (list(g_list), list(out_list))
+        self._keeps, self._keep = keep, ()
+
+    def _hold(self, g_list, out_list):
+        if self._keeps:
+            self._keep = (list(g_list), list(out_list))
 
     def __del__(self):
         try:
@@ -527,16 +532,10 @@ class ClipContext:
             pass
 
 
-def gac_clip_init(g_list: Sequence[torch.Tensor], out_list: Optional[Sequence[torch.Tensor]] = None,
-                  device: Optional[int] = None) -> ClipContext:
-    """gac_clip_init of the C ABI on a list of contiguous CUDA tensors, float32 and bfloat16 mixed as
-    they come.  ``out_list``: where the clipped gradients go; None clips in place."""
-    L = load_library()
-    outs = g_list if out_list is None else out_list
+def _clip_list(g_list, outs, device: int):
     if len(g_list) != len(outs):
         raise ValueError("gradient and output lists differ in length")
-    n = len(g_list)
-    arr = (gac_clip_tensor * max(n, 1))()
+    arr = (gac_clip_tensor * max(len(g_list), 1))()
     for i, (g, o) in enumerate(zip(g_list, outs)):
         if not (g.is_cuda and o.is_cuda and g.is_contiguous() and o.is_contiguous()):
             raise ValueError("tensors must be contiguous CUDA tensors")
@@ -545,13 +544,35 @@ def gac_clip_init(g_list: Sequence[torch.Tensor], out_list: Optional[Sequence[to
         if g.dtype not in _DT:
             raise GacError(GAC_ERR_DTYPE, f"unsupported dtype {g.dtype}")
         arr[i] = gac_clip_tensor(g.data_ptr(), o.data_ptr(), g.numel(), _DT[g.dtype], 0)
-    if device is None:
-        device = g_list[0].device.index if n else torch.cuda.current_device()
-    if any(t.device.index != device for t in list(g_list) + list(outs)):
+    if any(t.device.index != device for t in g_list) or any(t.device.index != device for t in outs):
         raise ValueError("all tensors of a list must be on one device")
+    return arr
+
+
+def gac_clip_init(g_list: Sequence[torch.Tensor], out_list: Optional[Sequence[torch.Tensor]] = None,
+                  device: Optional[int] = None, keep: bool = True) -> ClipContext:
+    """gac_clip_init of the C ABI on a list of contiguous CUDA tensors, float32 and bfloat16 mixed as
+    they come.  ``out_list``: where the clipped gradients go; None clips in place.  ``keep=False``: the context holds
+    no references, the caller sees to it that the tensors of the last init or rebind are there at every call."""
+    L = load_library()
+    outs = g_list if out_list is None else out_list
+    if device is None:
+        device = g_list[0].device.index if len(g_list) else torch.cuda.current_device()
+    arr = _clip_list(g_list, outs, device)
     out = ctypes.c_void_p()
-    _check(L.gac_clip_init(ctypes.byref(out), arr, n, device))
-    return ClipContext(out.value, g_list, outs, device)
+    _check(L.gac_clip_init(ctypes.byref(out), arr, len(g_list), device))
+    ctx = ClipContext(out.value, device, keep)
+    ctx._hold(g_list, outs)
+    return ctx
+
+
+def gac_clip_rebind(ctx: ClipContext, g_list: Sequence[torch.Tensor], out_list: Optional[Sequence[torch.Tensor]] = None,
+                    stream=None) -> None:
+    """Points the context at moved tensors of the same sizes and types, in stream order and without waiting."""
+    outs = g_list if out_list is None else out_list
+    arr = _clip_list(g_list, outs, ctx.device.index)
+    _check(load_library().gac_clip_rebind(ctx.handle, arr, len(g_list), _on(stream, ctx.device)[0]))
+    ctx._hold(g_list, outs)
 
 
 def _clip_result(rc: int, res) -> Optional[gac_clip_result]:
@@ -605,7 +626,7 @@ def gac_clip_free(ctx: ClipContext) -> None:
     if ctx.handle:
         load_library().gac_clip_free(ctx.handle)
         ctx.handle = ctypes.c_void_p(None)
-    ctx._keep = ([], [])
+    ctx._keep = ()
 
 
 def gac_rotary_freqs(rot_dim: int, base: float = 1e4, scaling: str = "none", factor: float = 1.0,

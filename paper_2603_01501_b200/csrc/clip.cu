@@ -268,6 +268,28 @@ clip_kernel(const ClipChunk *__restrict__ table, uint32_t n_chunks, double *part
     }
 }
 
+// New addresses for the chunks of up to kMovedTensors tensors, one to a CTA; they travel as an argument of the launch, so
+// nothing on the host has to outlive the call.
+constexpr uint32_t kMovedTensors = 512;
+struct MovedTensor {
+    uint64_t g, out;
+    uint32_t first, chunks;   // of the table
+};
+struct Moved {
+    uint32_t chunk_elems, n;
+    MovedTensor t[kMovedTensors];
+};
+__global__ void __launch_bounds__(kThreads) clip_move_kernel(const __grid_constant__ Moved m, ClipChunk *table) {
+    const MovedTensor &t = m.t[blockIdx.x];
+    for (uint32_t i = threadIdx.x; i < t.chunks; i += kThreads) {
+        ClipChunk &c = table[t.first + i];
+        const uint64_t off = uint64_t(i) * m.chunk_elems * (c.flags & kBf16 ? 2 : 4);
+        c.g = t.g + off;
+        c.out = t.out + off;
+        c.flags = (c.flags & kBf16) | (t.g == t.out ? kInPlace : 0u);
+    }
+}
+
 int fail(std::nullptr_t, int code, const char *fmt, const char *a = "", long long b = 0) {
     snprintf(g_init_err, sizeof(g_init_err), fmt, a, b);
     return code;
@@ -285,6 +307,8 @@ struct gac_clip_ctx {
     gac_clip_result *d_rec = nullptr;
     gac_clip_result *h_rec = nullptr;  // pinned, from the first call that asks for a record on
     unsigned long long limit_ns = 1000000000ull;
+    uint32_t chunk_elems = 0;
+    std::vector<std::pair<uint64_t, int32_t>> shape;   // elements and type of every tensor
 };
 
 namespace {
@@ -342,10 +366,12 @@ int setup(gac_clip_ctx *c, const gac_clip_tensor *list, uint32_t n) {
     // Short lists are cut finer, so that a CTA's turn is short.  Finer against coarser: 0.2 M elements in 15 tensors 6.2 us
     // and 8.2, 2^21 in one 8.5 and 9.3, 2^22 12.4 and 10.3, 0.25 B bfloat16 345 and 240.
     const uint64_t ce = total <= kShortList ? kShortChunkElems : kChunkElems;
+    c->chunk_elems = uint32_t(ce);
     std::vector<ClipChunk> table;
     for (uint32_t i = 0; i < n; ++i) {
         const gac_clip_tensor &t = list[i];
         const uint64_t size = t.dtype == GAC_BF16 ? 2 : 4;
+        c->shape.emplace_back(t.numel, t.dtype);
         for (uint64_t off = 0; off < t.numel; off += ce) {
             ClipChunk ch;
             ch.g = reinterpret_cast<uint64_t>(t.g) + off * size;
@@ -434,6 +460,39 @@ int gac_clip_init(gac_clip_ctx **out, const gac_clip_tensor *list, uint32_t n, i
         return fail(nullptr, GAC_ERR_INVALID_ARG, "out of host memory%s");
     }
     *out = c;
+    return GAC_OK;
+}
+
+int gac_clip_rebind(gac_clip_ctx *ctx, const gac_clip_tensor *list, uint32_t n, void *cuda_stream) {
+    if (!ctx) return fail(nullptr, GAC_ERR_INVALID_ARG, "ctx is NULL%s");
+    if (!list || n != ctx->shape.size())
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "gac_clip_rebind needs one entry per tensor of the context%s");
+    for (uint32_t i = 0; i < n; ++i)
+        if (list[i].numel != ctx->shape[i].first || list[i].dtype != ctx->shape[i].second)
+            return fail(nullptr, GAC_ERR_INVALID_ARG, "tensor %s%lld changed its size or type; create a new context", "", i);
+    try {
+        if (int rc = check_list(list, n)) return rc;
+    } catch (...) {   // nothing may be thrown through the C boundary
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "out of host memory%s");
+    }
+    Range range("gac_clip_rebind");
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
+    Moved m;
+    m.chunk_elems = ctx->chunk_elems;
+    m.n = 0;
+    uint32_t first = 0;
+    for (uint32_t i = 0; i < n; ++i) {
+        const uint32_t chunks = uint32_t((list[i].numel + m.chunk_elems - 1) / m.chunk_elems);
+        if (chunks)
+            m.t[m.n++] = MovedTensor{reinterpret_cast<uint64_t>(list[i].g), reinterpret_cast<uint64_t>(list[i].out), first, chunks};
+        first += chunks;
+        if (m.n == kMovedTensors || (i + 1 == n && m.n)) {
+            clip_move_kernel<<<m.n, kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(m, ctx->d_chunks);
+            GAC_CUDA(nullptr, cudaGetLastError());
+            m.n = 0;
+        }
+    }
     return GAC_OK;
 }
 

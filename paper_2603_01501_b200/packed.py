@@ -83,8 +83,10 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: tor
 class GradientClipper:
     """Clips the gradients of a list of parameters by their global norm, in place, without waiting for the host.
 
-    The table of the list is built on first use and again whenever a ``.grad`` tensor has moved.  Parameters without a
-    gradient are left out, as an optimizer leaves them out.  For lists that do not go through the alignment rule: with a
+    The table of the list is made on first use and again when the list itself changes (a parameter without a gradient is
+    left out, as an optimizer leaves it out): that allocates, and waits for the device.  Gradients that have only moved, as they
+    do under ``zero_grad(set_to_none=True)``, are written into the table in stream order.  No references to gradients
+    are kept between calls.  For lists that do not go through the alignment rule: with a
     GradientAlignmentController, ``HParams(clip_max_norm=...)`` clips in the rule's own pass, and in exchange mode
     that is the only way (the gradient may be the stored direction itself, which is refused here)."""
 
@@ -94,7 +96,8 @@ class GradientClipper:
             raise ValueError("no trainable parameters")
         self.norm = torch.zeros((), device=self.params[0].device)
         self._ctx: Optional[gb.ClipContext] = None
-        self._bound: List[tuple] = []
+        self._shape: List[tuple] = []
+        self._bound: List[int] = []
 
     def clip(self, max_norm: float, eps: float = 1e-6) -> torch.Tensor:
         """Returns the norm before clipping as a 0-dim device tensor, overwritten by the next call."""
@@ -107,16 +110,19 @@ class GradientClipper:
         if any(getattr(g, "_gac_direction", False) for g in grads):
             raise RuntimeError("a gradient is the stored direction of a controller in exchange mode and must not be "
                                "modified: clip with HParams(clip_max_norm=...)")
-        bound = [(g.data_ptr(), g.numel(), g.dtype) for g in grads]
-        if self._ctx is None or bound != self._bound:
-            if self._ctx is not None:
-                gb.gac_clip_free(self._ctx)
-            self._ctx = gb.gac_clip_init(grads)
+        shape, bound = [(g.numel(), g.dtype) for g in grads], [g.data_ptr() for g in grads]
+        if self._ctx is None or shape != self._shape:
+            self.close()
+            self._ctx = gb.gac_clip_init(grads, keep=False)
+            self._shape, self._bound = shape, bound
+        elif bound != self._bound:
+            self._bound = []   # should the call fail, the next one tries again
+            gb.gac_clip_rebind(self._ctx, grads)
             self._bound = bound
         gb.gac_clip_grad_norm(self._ctx, max_norm, eps, norm_out=self.norm)
         return self.norm
 
     def close(self) -> None:
-        if self._ctx is not None:
-            gb.gac_clip_free(self._ctx)
-            self._ctx, self._bound = None, []
+        ctx, self._ctx, self._shape, self._bound = self._ctx, None, [], []
+        if ctx is not None:
+            gb.gac_clip_free(ctx)

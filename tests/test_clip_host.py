@@ -60,8 +60,8 @@ def library(monkeypatch):
 
     for name, f in (("gac_init", lambda g, d, hp: object()), ("gac_stats", stats), ("gac_project", project),
                     ("gac_next_gradient_set", lambda ctx: calls.next), ("gac_free", lambda ctx: None),
-                    ("gac_clip_init", make), ("gac_clip_grad_norm", clip), ("gac_clip_free", lambda ctx: None)):
-        monkeypatch.setattr(gb, name, f)
+                    ("gac_clip_init", make), ("gac_clip_rebind", lambda *_, **__: None), ("gac_clip_grad_norm", clip), ("gac_clip_free", lambda ctx: None)):
+        monkeypatch.setattr(gb, name, f, raising=False)
     return calls
 
 
@@ -81,3 +81,48 @@ def test_the_stored_direction_of_an_exchange_step_is_not_clipped(library):
     controller.step()                       # a projection: written into the free tensors, which may be clipped
     clipper.clip(1.0)
     assert library.clipped == 2
+
+
+def test_the_clipper_rebinds_moved_gradients_and_survives_a_failure(library, monkeypatch):
+    moved, kept = [], {}
+    monkeypatch.setattr(gb, "gac_clip_rebind", lambda ctx, grads, *_, **__: moved.append([g.data_ptr() for g in grads]), raising=False)
+    make = gb.gac_clip_init
+    monkeypatch.setattr(gb, "gac_clip_init", lambda grads, *a, **kw: (kept.update(kw), make(grads))[1])
+    params = [torch.nn.Parameter(torch.zeros(n)) for n in (3, 5)]
+    clipper = packed.GradientClipper(params)
+
+    def new_gradients():
+        old = [p.grad for p in params]                  # alive, so that the new ones lie elsewhere
+        for p in params:
+            p.grad = torch.ones_like(p)
+        return old
+
+    new_gradients()
+    clipper.clip(1.0)
+    clipper.clip(1.0)
+    assert len(library.made) == 1 and moved == [] and kept == {"keep": False}
+    old = new_gradients()
+    clipper.clip(1.0)
+    assert len(library.made) == 1 and moved == [[p.grad.data_ptr() for p in params]]
+    params[1].grad = None                               # another list
+    clipper.clip(1.0)
+    assert len(library.made) == 2 and len(moved) == 1
+
+    def broken(*_, **__):
+        raise gb.GacError(gb.GAC_ERR_CUDA, "no")
+    good = gb.gac_clip_rebind, gb.gac_clip_init
+    monkeypatch.setattr(gb, "gac_clip_rebind", broken)
+    monkeypatch.setattr(gb, "gac_clip_init", broken)
+    params[0].grad = torch.ones_like(params[0])
+    for _ in range(2):                                  # fails, and does not take the old table for the new one
+        with pytest.raises(gb.GacError):
+            clipper.clip(1.0)
+    params[1].grad = torch.ones_like(params[1])
+    for _ in range(2):
+        with pytest.raises(gb.GacError):
+            clipper.clip(1.0)
+    before = library.clipped
+    monkeypatch.setattr(gb, "gac_clip_rebind", good[0])
+    monkeypatch.setattr(gb, "gac_clip_init", good[1])
+    clipper.clip(1.0)
+    assert len(library.made) == 3 and library.clipped == before + 1 and len(old) == 2

@@ -103,3 +103,79 @@ def test_the_stored_direction_of_an_exchange_step_is_not_clipped():
     assert abs(math.sqrt(sum(float(p.grad.double().square().sum()) for p in params)) - 1.0) < 1e-5
     controller.close()
     clipper.close()
+
+
+def leaf_gradients(params, seed):
+    for i, p in enumerate(params):
+        gen = torch.Generator(device="cuda").manual_seed(100 * seed + i)
+        p.grad = torch.empty_like(p).normal_(generator=gen)
+
+
+def test_the_clipper_keeps_no_gradients_alive():
+    params = [torch.nn.Parameter(torch.zeros(8 << 20, device="cuda")) for _ in range(4)]
+    clipper, one_set = packed.GradientClipper(params), 4 * (32 << 20)
+    torch.cuda.synchronize()
+    start = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    for step in range(4):
+        for p in params:
+            p.grad = None                       # zero_grad's default
+        leaf_gradients(params, step)
+        clipper.clip(1.0)
+    assert torch.cuda.max_memory_allocated() - start < one_set + (4 << 20)
+    clipper.close()
+
+
+def test_the_clipper_follows_moved_gradients_without_waiting():
+    sizes = [(n, d) for n in (5, 70_001, 0, 1 << 18) for d in (torch.float32, BF)]
+    params = [torch.nn.Parameter(torch.zeros(n, device="cuda", dtype=d)) for n, d in sizes]
+    clipper, old = packed.GradientClipper(params), []
+    leaf_gradients(params, 0)
+    clipper.clip(1.0)
+    for step in range(1, 4):
+        old.append([p.grad for p in params])    # alive: the next ones lie elsewhere
+        leaf_gradients(params, step)
+        keep = [p.grad.clone() for p in params]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(400_000_000)
+        told = clipper.clip(0.5)
+        assert not torch.cuda.current_stream().query()
+        norm = math.sqrt(math.fsum(float(g.double().square().sum()) for g in keep))
+        assert abs(float(told) - norm) <= 2 * U * norm
+        for p, g in zip(params, keep):
+            half = 2.0 ** -8 if g.dtype == BF else U
+            want = g.double() * (0.5 / (norm + 1e-6))
+            assert bool(((p.grad.double() - want).abs() <= (half + 3 * U) * want.abs()).all())
+    clipper.close()
+
+
+def test_many_tensors_rebound_out_of_place_and_in_a_graph():
+    """More tensors than one launch takes, some empty; from in place to out of place and back."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    sizes = [(37 * i) % 41 * (500 if i % 97 == 0 else 1) for i in range(1300)]
+    a, b, out = ([torch.randn(n, generator=gen, device="cuda") for n in sizes] for _ in range(3))
+    keep = [x.clone() for x in b]
+    norm = math.sqrt(math.fsum(float(x.double().square().sum()) for x in b))
+    ctx = gb.gac_clip_init(a)
+    gb.gac_clip_rebind(ctx, b, out)
+    gb.gac_clip_grad_norm(ctx, 0.5 * norm)
+    assert all(torch.equal(x, y) for x, y in zip(b, keep))
+    want = [x * torch.tensor(0.5 * norm / (norm + 1e-6), dtype=torch.float64).float().cuda() for x in keep]
+    assert all(torch.equal(x, y) for x, y in zip(out, want))
+    gb.gac_clip_rebind(ctx, a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):               # addresses of b, whatever the table holds when it is replayed
+        gb.gac_clip_rebind(ctx, b)
+        gb.gac_clip_grad_norm(ctx, 0.5 * norm)
+    gb.gac_clip_rebind(ctx, a, out)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(b, want))
+    with pytest.raises(gb.GacError):
+        gb.gac_clip_rebind(ctx, a[:-1])
+    with pytest.raises(gb.GacError):
+        gb.gac_clip_rebind(ctx, [x.to(BF) for x in a])
+    with pytest.raises(gb.GacError):
+        gb.gac_clip_rebind(ctx, [a[0]] * len(a))
+    gb.gac_clip_free(ctx)

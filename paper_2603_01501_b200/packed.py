@@ -58,12 +58,13 @@ class _Attention(torch.autograd.Function):
 
 
 def _rows(t: torch.Tensor, multiple: int = 1) -> torch.Tensor:
-    """A gradient as autograd hands it over may be expanded or transposed: the library wants contiguous rows."""
+    """A gradient as autograd hands it over may be expanded, transposed or off any boundary: the library wants
+    contiguous rows on boundaries of `multiple` elements."""
     s0, s1, s2 = t.stride()
     if s2 == 1 and s0 >= s1 >= t.shape[2] and s0 % multiple == 0 and s1 % multiple == 0 and \
             t.data_ptr() % (multiple * t.element_size()) == 0:
         return t
-    return t.contiguous()
+    return t.clone(memory_format=torch.contiguous_format)   # a copy even where t counts as contiguous: its base may be off
 
 
 def rotary(q: torch.Tensor, k: torch.Tensor, freqs, positions: Optional[torch.Tensor] = None,

@@ -179,3 +179,12 @@ def test_many_tensors_rebound_out_of_place_and_in_a_graph():
     with pytest.raises(gb.GacError):
         gb.gac_clip_rebind(ctx, [a[0]] * len(a))
     gb.gac_clip_free(ctx)
+
+
+def test_a_gradient_that_is_contiguous_but_misaligned():
+    cu = torch.tensor([0, 20], dtype=torch.int32, device="cuda")
+    q, k, v = (torch.randn(20, 2, 64, device="cuda").to(BF).requires_grad_() for _ in range(3))
+    x, g = torch.zeros(3, dtype=BF, device="cuda"), torch.randn(3 + 20 * 128, device="cuda").to(BF)
+    got = torch.autograd.grad(torch.cat((x, packed.attention(q, k, v, cu).flatten())), (q, k, v), g)
+    want = torch.autograd.grad(packed.attention(q, k, v, cu), (q, k, v), g[3:].clone().view(20, 2, 64))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -73,3 +73,20 @@ def test_what_the_way_back_of_rotary_reads_cannot_change_unnoticed(plain):
     pos.add_(7)                                     # a buffer refilled for the next micro-batch
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         torch.autograd.grad(y.sum(), q)
+
+
+def test_a_gradient_that_is_contiguous_but_misaligned_is_copied(plain, monkeypatch):
+    seen = []
+    backward = gb.gac_attn_backward
+    monkeypatch.setattr(gb, "gac_attn_backward", lambda d_o, *a, **kw: (seen.append(d_o), backward(d_o, *a, **kw))[1])
+    q, k, v = (torch.randn(5, n, 8).to(torch.bfloat16).requires_grad_() for n in (2, 1, 1))
+    cu = torch.tensor([0, 5], dtype=torch.int32)
+    x = torch.zeros(3, dtype=torch.bfloat16)
+    g = torch.randn(83).to(torch.bfloat16)
+    torch.cat((x, packed.attention(q, k, v, cu).flatten())).backward(g)         # 6 bytes off a boundary
+    assert torch.equal(seen[0].flatten(), g[3:])
+    one = torch.randn(5, 8).to(torch.bfloat16).as_strided((5, 1, 8), (8, 3, 1))   # an odd stride of one head
+    q1 = torch.randn(5, 1, 8).to(torch.bfloat16).requires_grad_()
+    packed.attention(q1, k, v, cu).backward(one)
+    for d in seen:
+        assert d.data_ptr() % 16 == 0 and all(s % 8 == 0 for s in d.stride()[:2]) and d.stride(2) == 1

@@ -36,7 +36,7 @@ class _Rotary(torch.autograd.Function):
         positions, cu_seqlens = ctx.saved_tensors
         freqs, layout, scale, inverse = ctx.how
         # the transpose of a turn is the turn by the negative angle: itself a turn, so derivatives of any order go through
-        d_q, d_k = _Rotary.apply(_rows(d_q), _rows(d_k), freqs, positions, cu_seqlens, layout, scale, not inverse)
+        d_q, d_k = _Rotary.apply(_rows(d_q), None if d_k is None else _rows(d_k), freqs, positions, cu_seqlens, layout, scale, not inverse)
         return d_q, d_k, None, None, None, None, None, None
 
 
@@ -67,7 +67,7 @@ def _rows(t: torch.Tensor, multiple: int = 1) -> torch.Tensor:
     return t.clone(memory_format=torch.contiguous_format)   # a copy even where t counts as contiguous: its base may be off
 
 
-def rotary(q: torch.Tensor, k: torch.Tensor, freqs, positions: Optional[torch.Tensor] = None,
+def rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Optional[torch.Tensor] = None,
            cu_seqlens: Optional[torch.Tensor] = None, layout: str = "half", scale: float = 1.0):
     """Rotary positions (binding.gac_rotary) with their derivatives of any order; returns (q', k')."""
     return _Rotary.apply(q, k, freqs, positions, cu_seqlens, layout, scale, False)

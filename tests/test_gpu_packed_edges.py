@@ -188,3 +188,15 @@ def test_a_gradient_that_is_contiguous_but_misaligned():
     got = torch.autograd.grad(torch.cat((x, packed.attention(q, k, v, cu).flatten())), (q, k, v), g)
     want = torch.autograd.grad(packed.attention(q, k, v, cu), (q, k, v), g[3:].clone().view(20, 2, 64))
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_rotary_of_queries_alone():
+    freqs, pos = gb.gac_rotary_freqs(32, 1e4), torch.arange(50, device="cuda", dtype=torch.int32)
+    q = torch.randn(50, 3, 32, device="cuda", requires_grad=True)
+    k = torch.randn(50, 1, 32, device="cuda")
+    y, none = packed.rotary(q, None, freqs, positions=pos)
+    assert none is None
+    g = torch.randn_like(y)
+    got, = torch.autograd.grad(y, q, g)
+    want, = torch.autograd.grad(packed.rotary(q, k, freqs, positions=pos)[0], q, g)
+    assert torch.equal(got, want)

@@ -90,3 +90,11 @@ def test_a_gradient_that_is_contiguous_but_misaligned_is_copied(plain, monkeypat
     packed.attention(q1, k, v, cu).backward(one)
     for d in seen:
         assert d.data_ptr() % 16 == 0 and all(s % 8 == 0 for s in d.stride()[:2]) and d.stride(2) == 1
+
+
+def test_rotary_of_queries_alone(plain):
+    q, pos = heads(2, 8), torch.arange(5, dtype=torch.int32)
+    y, none = packed.rotary(q, None, FREQS, positions=pos, scale=2.0)
+    assert none is None
+    got, = torch.autograd.grad((y * y).sum(), q)
+    assert torch.allclose(got, 8 * q)

@@ -101,7 +101,12 @@ int tensor_map(CUtensorMap *map, int *mul, const gac_attn_heads &h, const gac_at
 
 RowsOut rows_out(const gac_attn_heads &h) { return RowsOut{static_cast<char *>(h.p), 2 * h.token, 2 * h.head}; }
 
-AttnDev kernel_args(const gac_attn &a) {
+// Limit of the waits inside a kernel, in units of 1024 ns.  The longest are for another warp to get through a job, one turn for
+// each key (or query) tile of up to the whole pack and each of the job's heads: two seconds, and 20 us for each turn, which
+// takes about 2 (backward, 28/4 heads x 128: 1.9).  At most 2^31 / 128 turns by check_shape.
+uint32_t wait_limit(const gac_attn &a, uint32_t heads) { return uint32_t(2000000 + 20ull * (a.n_tokens / kTile + 1) * heads); }
+
+AttnDev kernel_args(const gac_attn &a, uint32_t heads) {
     AttnDev d{};
     d.cu = a.cu_seqlens;
     d.n_tokens = a.n_tokens;
@@ -112,6 +117,7 @@ AttnDev kernel_args(const gac_attn &a) {
     d.scale = a.scale;
     d.exp2_scale = std::max(fabsf(a.scale) * kLog2e, 1e-37f);   // above zero, so that a hidden score stays -infinity
     d.negate = a.scale < 0.0f ? kNegateA : 0u;
+    d.wait_limit = wait_limit(a, heads);
     d.lse = a.lse;
     d.o = rows_out(a.o);
     return d;
@@ -140,7 +146,7 @@ int grid_of(uint32_t count, uint32_t heads, uint32_t *grid) {
 template <int DP>
 int launch_forward(const gac_attn &a, int device, cudaStream_t s) {
     static std::atomic<bool> done[64];
-    AttnDev d = kernel_args(a);
+    AttnDev d = kernel_args(a, 1);
     CUtensorMap mq, mk, mv;
     if (int rc = tensor_map(&mq, &d.q_mul, a.q, a, a.q_heads)) return rc;
     if (int rc = tensor_map(&mk, &d.k_mul, a.k, a, a.kv_heads)) return rc;
@@ -185,7 +191,8 @@ cudaError_t launch_next(void (*kernel)(Args...), uint32_t grid, uint32_t threads
 template <int DP>
 int launch_backward(const gac_attn &a, const gac_attn_grad &g, int device, cudaStream_t s) {
     static std::atomic<bool> done_kv[64], done_q[64];
-    AttnDev d = kernel_args(a);
+    const uint32_t parts = parts_of(a);
+    AttnDev d = kernel_args(a, a.q_heads / a.kv_heads / parts);
     d.d_q = rows_out(g.d_q);
     d.d_k = rows_out(g.d_k);
     d.d_v = rows_out(g.d_v);
@@ -193,7 +200,7 @@ int launch_backward(const gac_attn &a, const gac_attn_grad &g, int device, cudaS
     d.do_token = 2 * g.d_o.token;
     d.do_head = 2 * g.d_o.head;
     d.rows = static_cast<float2 *>(g.workspace);
-    d.parts = parts_of(a);
+    d.parts = parts;
     d.part_sums = reinterpret_cast<float *>(static_cast<char *>(g.workspace) + rows_bytes(a));
     CUtensorMap mq, mk, mv, mdo;
     if (int rc = tensor_map(&mq, &d.q_mul, a.q, a, a.q_heads)) return rc;

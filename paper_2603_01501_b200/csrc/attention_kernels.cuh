@@ -31,6 +31,7 @@ struct AttnDev {
     float *lse;
     float2 *rows;                      // backward: (-log2(e) lse, row term) of every query head and token
     uint32_t parts;                    // backward: query heads of a group are summed in this many parts,
+    uint32_t wait_limit;               // of every wait inside a kernel, in units of 1024 ns
     float *part_sums;                  // kept as binary32 [parts][d_k, d_v][n_tokens][kv_heads][head_dim] when parts > 1
 };
 
@@ -176,7 +177,9 @@ __device__ __forceinline__ JobWord job_at(const AttnDev &a, bool ranked, uint32_
 }
 struct Jobs {
     uint32_t word, answer, full, empty, asked;   // shared memory addresses; `readers` warps read every job
-    __device__ __forceinline__ explicit Jobs(uint32_t at) : word(at), answer(at + 16), full(at + 32), empty(at + 40), asked(at + 48) {}
+    uint32_t limit;
+    __device__ __forceinline__ Jobs(uint32_t at, uint32_t wait_limit)
+        : word(at), answer(at + 16), full(at + 32), empty(at + 40), asked(at + 48), limit(wait_limit) {}
     static constexpr uint32_t kBytes = 64;
     __device__ __forceinline__ void init(uint32_t readers) const {
         mbar_init(full, 1);
@@ -184,8 +187,9 @@ struct Jobs {
         mbar_init(asked, 1);
         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(word), "r"(0) : "memory");
     }
-    // The warp that hands the jobs out: from this CTA's own index on, until there is none left.
-    template <int ROWS, bool HIGH_IS_LATE>
+    // The warp that hands the jobs out: from this CTA's own index on, until there is none left.  AFTER_PREVIOUS: the readers do
+    // not get through their first job before the kernel before this one has ended.
+    template <int ROWS, bool HIGH_IS_LATE, bool AFTER_PREVIOUS>
     __device__ __forceinline__ bool run(const AttnDev &a, bool ranked, uint32_t heads) const {
         const uint32_t lane = threadIdx.x & 31;
         int index = int(blockIdx.x);
@@ -201,14 +205,15 @@ struct Jobs {
                     mbar_arrive(full);
                 }
                 if (w.kind == kJobStop) return true;
-                if (!warp_wait(empty, given & 1)) return false;   // all have begun it
+                if (AFTER_PREVIOUS && given == 0) wait_for_previous();
+                if (!warp_wait(empty, given & 1, limit)) return false;   // all have begun it
                 ++given;
             }
             if (lane == 0) {
                 mbar_expect(asked, 16);
                 ask_next_cta(answer, asked);
             }
-            if (!warp_wait(asked, questions & 1)) return false;
+            if (!warp_wait(asked, questions & 1, limit)) return false;
             ++questions;
             index = next_cta(answer);
             __syncwarp();
@@ -216,7 +221,7 @@ struct Jobs {
         }
     }
     __device__ __forceinline__ bool get_alone(uint32_t k, JobWord *w) const {   // one thread
-        if (!mbar_wait(full, k & 1)) return false;
+        if (!mbar_wait(full, k & 1, limit)) return false;
         uint32_t last;
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w->first), "=r"(w->len), "=r"(w->block), "=r"(last) : "r"(word) : "memory");
         w->kind = last & 3u;
@@ -225,7 +230,7 @@ struct Jobs {
         return true;
     }
     __device__ __forceinline__ bool get(uint32_t k, JobWord *w) const {         // whole warp
-        if (!warp_wait(full, k & 1)) return false;
+        if (!warp_wait(full, k & 1, limit)) return false;
         uint32_t last;
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w->first), "=r"(w->len), "=r"(w->block), "=r"(last) : "r"(word) : "memory");
         w->kind = last & 3u;
@@ -408,7 +413,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t sq = base, sring = base + 2 * C::kBytes;
     const uint32_t stage = sring + C::kStages * C::kBytes, bars = stage + 8 * C::kStageBytes;
-    const Jobs jobs(bars);
+    const Jobs jobs(bars, a.wait_limit);
     const uint32_t q_full = bars + Jobs::kBytes, q_empty = q_full + 8, s_full = q_full + 16, p_full = q_full + 32, o_full = q_full + 48,
                    raw = q_full + 64, full = q_full + 72, empty = full + 8 * C::kStages,
                    tmem_slot = empty + 8 * C::kStages;
@@ -450,7 +455,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 const uint32_t row0 = w.block * 2 * kTile, kv_head = w.head / group;
                 const bool two = row0 + kTile < w.len;
                 const uint32_t items = 2 * (w.block * 2 + 1 + (two ? 1 : 0));
-                if (tiles > 0 && !(ok = warp_wait(q_empty, (tiles - 1) & 1))) break;
+                if (tiles > 0 && !(ok = warp_wait(q_empty, (tiles - 1) & 1, a.wait_limit))) break;
                 ++tiles;
                 if (lane == 0) {
                     mbar_expect(q_full, (two ? 2 : 1) * C::kBytes);
@@ -460,7 +465,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                                      int(w.first + row0 + t * kTile));
                 }
                 for (uint32_t i = 0; i < items; ++i, ++n, at.template next<C::kStages>()) {   // K, V, K, V, ...
-                    if (n >= C::kStages && !(ok = warp_wait(empty + 8 * at.at, at.phase ^ 1))) break;
+                    if (n >= C::kStages && !(ok = warp_wait(empty + 8 * at.at, at.phase ^ 1, a.wait_limit))) break;
                     const bool is_k = (i & 1) == 0, ragged = !is_k && w.len < (i / 2 + 1) * kTile;
                     const uint32_t tile = sring + at.at * C::kBytes, bar = ragged ? raw : full + 8 * at.at;
                     if (lane == 0) {
@@ -470,7 +475,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                                      int(w.first + (i / 2) * kTile));
                     }
                     if (ragged) {
-                        if (!(ok = warp_wait(raw, fixed & 1))) break;
+                        if (!(ok = warp_wait(raw, fixed & 1, a.wait_limit))) break;
                         ++fixed;
                         zero_tile_rows<C::kSub>(tile, w.len - (i / 2) * kTile);
                         if (lane == 0) mbar_arrive(full + 8 * at.at);
@@ -480,12 +485,12 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             }
             // the CTA must not end, nor its memory be given back, before the last loads and releases have arrived
             if (tiles > 0) {
-                mbar_wait(q_full, (tiles - 1) & 1);
-                if (ok) ok = warp_wait(q_empty, (tiles - 1) & 1);
+                mbar_wait(q_full, (tiles - 1) & 1, a.wait_limit);
+                if (ok) ok = warp_wait(q_empty, (tiles - 1) & 1, a.wait_limit);
             }
             for (uint32_t i = n > C::kStages ? n - C::kStages : 0; i < n; ++i) {
-                mbar_wait(full + 8 * (i % C::kStages), (i / C::kStages) & 1);
-                if (ok) ok = warp_wait(empty + 8 * (i % C::kStages), (i / C::kStages) & 1);
+                mbar_wait(full + 8 * (i % C::kStages), (i / C::kStages) & 1, a.wait_limit);
+                if (ok) ok = warp_wait(empty + 8 * (i % C::kStages), (i / C::kStages) & 1, a.wait_limit);
             }
         } else if (warp == 8) {   // --------------------------------- products
             // One thread: between two batches of products the tensor cores hold about one product's work, so every
@@ -496,7 +501,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 uint32_t tiles = 0, done0 = 0, done1 = 0;   // jobs, blocks of the first and second tile so far
                 Place at;   // of the oldest ring item not yet released
                 auto tile_of = [&](const Place &p) { return sring + p.at * C::kBytes; };
-                auto wait_tile = [&](const Place &p) { return mbar_wait(full + 8 * p.at, p.phase); };
+                auto wait_tile = [&](const Place &p) { return mbar_wait(full + 8 * p.at, p.phase, a.wait_limit); };
                 auto release = [&]() {
                     mma_commit(empty + 8 * at.at);
                     at.template next<C::kStages>();
@@ -505,7 +510,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                     if (w.kind != kJobWork) continue;
                     const bool two = w.block * 2 * kTile + kTile < w.len;
                     const uint32_t nb0 = w.block * 2 + 1, nb = nb0 + (two ? 1 : 0);   // key tiles of the first tile; of both
-                    if (!(ok = mbar_wait(q_full, tiles & 1) && wait_tile(at))) break;
+                    if (!(ok = mbar_wait(q_full, tiles & 1, a.wait_limit) && wait_tile(at))) break;
                     ++tiles;
                     tc_fence_after();
                     product_rows<DP>(tmem, sq, tile_of(at), id_s);   // S_0 = Q_0 K^T
@@ -522,7 +527,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                         key.template next<C::kStages>();
                         if (!(ok = wait_tile(v) && (j + 1 == nb || wait_tile(key)))) break;
                         if (j < nb0) {
-                            if (!(ok = mbar_spin(p_full, done0 & 1))) break;
+                            if (!(ok = mbar_spin(p_full, done0 & 1, a.wait_limit))) break;
                             ++done0;
                             tc_fence_after();
                             product_cols<32>(tmem + 256, tmem, tile_of(v), id_o, j > 0);   // O_0 += P_0 V
@@ -533,7 +538,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                             }
                         }
                         if (two) {
-                            if (!(ok = mbar_spin(p_full + 8, done1 & 1))) break;
+                            if (!(ok = mbar_spin(p_full + 8, done1 & 1, a.wait_limit))) break;
                             ++done1;
                             tc_fence_after();
                             product_cols<32>(tmem + 384, tmem + 128, tile_of(v), id_o, j > 0);
@@ -553,7 +558,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 }
             }
         } else if (warp == 10) {   // ------------------------------------ jobs
-            ok = jobs.template run<2 * kTile, true>(a, ranked, a.q_heads);
+            ok = jobs.template run<2 * kTile, true, false>(a, ranked, a.q_heads);
         }
     } else {   // ------------------------------------------- a row of a tile
         registers_up<C::kRowRegs>();
@@ -575,7 +580,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             float m = -INFINITY;
             float2 sum = make_float2(0.f, 0.f);
             for (uint32_t j = 0; j < my_blocks; ++j, ++it) {
-                if (!(ok = warp_wait(s_full + 8 * t, it & 1))) break;
+                if (!(ok = warp_wait(s_full + 8 * t, it & 1, a.wait_limit))) break;
                 tc_fence_after();
                 uint32_t r[4][32];
 #pragma unroll
@@ -594,7 +599,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 top += top - top;   // an infinite score, like a NaN, makes its whole row NaN
                 if (j == 0) m = top;
                 else if (__any_sync(0xFFFFFFFFu, !((top - m) * c <= 8.0f))) {
-                    if (!(ok = warp_wait(o_full + 8 * t, (it - 1) & 1))) break;
+                    if (!(ok = warp_wait(o_full + 8 * t, (it - 1) & 1, a.wait_limit))) break;
                     tc_fence_after();
                     const float next = max3_nan(m, top, top), f = exp2_approx((m - next) * c);
                     sum = mul2(sum, make_float2(f, f));
@@ -627,7 +632,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full + 8 * t);
             }
-            if (!ok || !(ok = warp_wait(o_full + 8 * t, (it - 1) & 1))) break;
+            if (!ok || !(ok = warp_wait(o_full + 8 * t, (it - 1) & 1, a.wait_limit))) break;
             tc_fence_after();
             const float total = sum.x + sum.y, inv = 1.0f / total;
             const uint32_t row = row0 + t * kTile + local;
@@ -733,7 +738,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     const uint32_t sk = base, sv = base + C::kBytes, sring = base + 2 * C::kBytes;
     const uint32_t srows = sring + C::kStages * C::kBytes;   // per slot: 128 x -log2(e) lse, 128 x D
     const uint32_t stage = srows + C::kRowSlots * 1024, bars = stage + 8 * C::kStageBytes;
-    const Jobs jobs(bars);
+    const Jobs jobs(bars, a.wait_limit);
     const uint32_t kv_full = bars + Jobs::kBytes, kv_empty = kv_full + 8, s_full = kv_full + 16, dp_full = kv_full + 24, p_full = kv_full + 32,
                    ds_full = kv_full + 40, done = kv_full + 48, raw = kv_full + 56, rows_full = kv_full + 64, rows_empty = rows_full + 8 * C::kRowSlots,
                    full = rows_empty + 8 * C::kRowSlots, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
@@ -775,6 +780,12 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     auto q_slot = [](const Place &p) { return 2 * p.at + p.phase; };
     auto g_slot = [](const Place &p) { return 2 * p.at + (p.phase ^ 1); };
     auto q_tiles_of = [](const JobWord &j) { return (j.len + kTile - 1) / kTile - j.block; };   // from the diagonal on
+    // Row terms come from the kernel before: whoever depends on them, through others' work too, waits for its end first, so
+    // that a limited wait is only ever for this CTA.
+    auto get_job = [&](uint32_t k) {
+        if (k == 1) wait_for_previous();
+        return jobs.get(k, &w);
+    };
     auto kv_head_of = [&](const JobWord &j) { return j.head % a.kv_heads; };
     auto head0_of = [&](const JobWord &j) { return kv_head_of(j) * (a.q_heads / a.kv_heads) + (j.head / a.kv_heads) * heads; };
 
@@ -783,9 +794,9 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         if (warp == 9) {   // -------------------------------------------- loads
             uint32_t tiles = 0, fixed = 0, n = 0;   // jobs, tiles with rows of others, query tiles so far
             Place at;
-            for (uint32_t k = 0; (ok = jobs.get(k, &w)) && w.kind != kJobStop; ++k) {
+            for (uint32_t k = 0; (ok = get_job(k)) && w.kind != kJobStop; ++k) {
                 if (w.kind != kJobWork) continue;
-                if (tiles > 0 && !(ok = warp_wait(kv_empty, (tiles - 1) & 1))) break;
+                if (tiles > 0 && !(ok = warp_wait(kv_empty, (tiles - 1) & 1, a.wait_limit))) break;
                 ++tiles;
                 const uint32_t q_tiles = q_tiles_of(w), kv_head = kv_head_of(w);
                 if (lane == 0) {
@@ -798,11 +809,12 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 uint32_t h = head0_of(w), i = w.block;
                 for (uint32_t u = 0; ok && u < heads * q_tiles; ++u, ++n, at.template next<C::kPairs>()) {
                     const bool ragged = w.len < (i + 1) * kTile;
+                    if (n == C::kPairs) wait_for_previous();
                     for (uint32_t which = 0; which < 2; ++which) {   // Q, dO
                         const bool is_q = which == 0;
                         const uint32_t slot = is_q ? q_slot(at) : g_slot(at), tile = sring + slot * C::kBytes;
                         const uint32_t bar = ragged ? raw : full + 8 * slot;
-                        if (n >= C::kPairs && !(ok = warp_wait(empty + 8 * slot, at.phase ^ 1))) break;
+                        if (n >= C::kPairs && !(ok = warp_wait(empty + 8 * slot, at.phase ^ 1, a.wait_limit))) break;
                         if (lane == 0) {
                             mbar_expect(bar, C::kBytes);
                             for (int x = 0; x < C::kSub; ++x)
@@ -810,7 +822,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                                          int(w.first + i * kTile));
                         }
                         if (ragged) {
-                            if (!(ok = warp_wait(raw, fixed & 1))) break;
+                            if (!(ok = warp_wait(raw, fixed & 1, a.wait_limit))) break;
                             ++fixed;
                             zero_tile_rows<C::kSub>(tile, w.len - i * kTile);
                             if (lane == 0) mbar_arrive(full + 8 * slot);
@@ -825,13 +837,13 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             }
             // the CTA must not end, nor its memory be given back, before the last loads and releases have arrived
             if (tiles > 0) {
-                mbar_wait(kv_full, (tiles - 1) & 1);
-                if (ok) ok = warp_wait(kv_empty, (tiles - 1) & 1);
+                mbar_wait(kv_full, (tiles - 1) & 1, a.wait_limit);
+                if (ok) ok = warp_wait(kv_empty, (tiles - 1) & 1, a.wait_limit);
             }
             for (uint32_t i = n > C::kPairs ? n - C::kPairs : 0; i < n; ++i)
                 for (uint32_t slot = 2 * (i % C::kPairs); slot < 2 * (i % C::kPairs) + 2; ++slot) {
-                    mbar_wait(full + 8 * slot, (i / C::kPairs) & 1);
-                    if (ok) ok = warp_wait(empty + 8 * slot, (i / C::kPairs) & 1);
+                    mbar_wait(full + 8 * slot, (i / C::kPairs) & 1, a.wait_limit);
+                    if (ok) ok = warp_wait(empty + 8 * slot, (i / C::kPairs) & 1, a.wait_limit);
                 }
         } else if (warp == 10) {   // -------------------------------- row terms
             wait_for_previous();
@@ -847,7 +859,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
                         v[x] = i * kTile + lane + 32 * x < w.len ? __ldcg(src + lane + 32 * x) : make_float2(0.f, 0.f);
-                    if (use > 0 && !(ok = warp_wait(rows_empty + 8 * slot, (use - 1) & 1))) break;
+                    if (use > 0 && !(ok = warp_wait(rows_empty + 8 * slot, (use - 1) & 1, a.wait_limit))) break;
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         const uint32_t at = srows + slot * 1024 + (lane + 32 * x) * 4;
@@ -869,11 +881,12 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 uint32_t tiles = 0, it = 0;   // jobs, query tiles so far
                 Place at;                     // of the query tile at hand
                 auto tile_of = [&](uint32_t slot) { return sring + slot * C::kBytes; };
-                auto wait_tile = [&](uint32_t slot, const Place &p) { return mbar_wait(full + 8 * slot, p.phase); };
+                auto wait_tile = [&](uint32_t slot, const Place &p) { return mbar_wait(full + 8 * slot, p.phase, a.wait_limit); };
                 for (uint32_t k = 0; (ok = jobs.get_alone(k, &w)) && w.kind != kJobStop; ++k) {
+                    if (k == 0 && w.kind != kJobWork) wait_for_previous();
                     if (w.kind != kJobWork) continue;
                     const uint32_t total = q_tiles_of(w) * heads;
-                    if (!(ok = mbar_wait(kv_full, tiles & 1) && wait_tile(q_slot(at), at))) break;
+                    if (!(ok = mbar_wait(kv_full, tiles & 1, a.wait_limit) && wait_tile(q_slot(at), at))) break;
                     ++tiles;
                     tc_fence_after();
                     product_rows<DP>(t_s, sk, tile_of(q_slot(at)), id_s | a.negate);   // S^T = K Q^T
@@ -882,13 +895,14 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     product_rows<DP>(t_dp, sv, tile_of(g_slot(at)), id_s);             // dP^T = V dO^T
                     mma_commit(dp_full);
                     if (total == 1) mma_commit(kv_empty);
+                    if (k == 0) wait_for_previous();
                     for (uint32_t u = 0; u < total; ++u, ++it) {
                         const bool more = u + 1 < total;
                         const uint32_t q = q_slot(at), g = g_slot(at);
                         at.template next<C::kPairs>();
                         const uint32_t q_next = q_slot(at), g_next = g_slot(at);
                         if (more && !(ok = wait_tile(q_next, at))) break;
-                        if (!(ok = mbar_wait(p_full, it & 1))) break;
+                        if (!(ok = mbar_wait(p_full, it & 1, a.wait_limit))) break;
                         tc_fence_after();
                         product_cols<64>(t_dv, t_s, tile_of(g), id_o, u > 0);     // dV += P^T dO
                         mma_commit(empty + 8 * g);
@@ -897,7 +911,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                             mma_commit(s_full);
                             if (!(ok = wait_tile(g_next, at))) break;
                         }
-                        if (!(ok = mbar_wait(ds_full, it & 1))) break;
+                        if (!(ok = mbar_wait(ds_full, it & 1, a.wait_limit))) break;
                         tc_fence_after();
                         product_cols<64>(t_dk, t_dp, tile_of(q), id_o, u > 0);    // dK += dS^T Q
                         mma_commit(empty + 8 * q);
@@ -913,10 +927,11 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 }
             }
         } else {   // ------------------------------------------------ jobs
-            ok = jobs.template run<kTile, false>(a, ranked, lots);
+            ok = jobs.template run<kTile, false, true>(a, ranked, lots);
         }
     } else {   // ---------------------- a key row, half of the query columns
         registers_up<C::kRowRegs>();
+        wait_for_previous();
         const uint32_t half = warp >> 2, lanes = (warp & 3) << 21, col0 = half * 64;
         const uint32_t local = (warp & 3) * 32 + lane;
         const float2 c2 = make_float2(a.exp2_scale, a.exp2_scale);
@@ -937,8 +952,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 const bool whole = tile != 0 && hi == kTile;   // every query of the tile sees every key of this one
                 if (++tile == q_tiles) tile = 0;
                 const uint32_t terms = srows + slot * 1024 + col0 * 4;
-                if (!(ok = warp_wait(rows_full + 8 * slot, (it / C::kRowSlots) & 1))) break;
-                if (!(ok = warp_wait(s_full, it & 1))) break;
+                if (!(ok = warp_wait(rows_full + 8 * slot, (it / C::kRowSlots) & 1, a.wait_limit))) break;
+                if (!(ok = warp_wait(s_full, it & 1, a.wait_limit))) break;
                 tc_fence_after();
                 float p[64];
                 {
@@ -971,7 +986,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full);
-                if (!(ok = warp_wait(dp_full, it & 1))) break;
+                if (!(ok = warp_wait(dp_full, it & 1, a.wait_limit))) break;
                 tc_fence_after();
                 {
                     uint32_t r[2][32];
@@ -1005,7 +1020,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     mbar_arrive(rows_empty + 8 * slot);
                 }
             }
-            if (!ok || !(ok = warp_wait(done, tiles & 1))) break;
+            if (!ok || !(ok = warp_wait(done, tiles & 1, a.wait_limit))) break;
             ++tiles;
             tc_fence_after();
             // the first half of the threads writes dV, the second dK
@@ -1107,7 +1122,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t sq = base, sdo = base + 2 * C::kBytes, sring = base + 4 * C::kBytes;
     const uint32_t bars = sring + C::kStages * C::kBytes;
-    const Jobs jobs(bars);
+    const Jobs jobs(bars, a.wait_limit);
     const uint32_t q_full = bars + Jobs::kBytes, q_empty = q_full + 8, do_full = q_full + 16, raw = q_full + 24, taken = q_full + 32,
                    s_full = q_full + 48, s_read = q_full + 64, dp_full = q_full + 80, ds_full = q_full + 96, done = q_full + 112,
                    full = q_full + 128, empty = full + 8 * C::kStages, tmem_slot = empty + 8 * C::kStages;
@@ -1165,7 +1180,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 };
                 auto load = [&](bool is_k, uint32_t u) {   // key or value tile u of the job
                     const uint32_t m = n + u, at = is_k ? m % C::kKeys : C::kKeys + m % C::kValues, use = m / (is_k ? C::kKeys : C::kValues);
-                    if (use > 0 && !warp_wait(empty + 8 * at, (use - 1) & 1)) return false;
+                    if (use > 0 && !warp_wait(empty + 8 * at, (use - 1) & 1, a.wait_limit)) return false;
                     const bool ragged = is_k && w.len < (u + 1) * kTile;   // a key behind the sequence has dS = 0, times itself in dQ
                     const uint32_t bar = ragged ? raw : full + 8 * at;
                     if (lane == 0) {
@@ -1175,19 +1190,19 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                                      int(kv_head) * (is_k ? a.k_mul : a.v_mul), int(w.first + u * kTile));
                     }
                     if (ragged) {
-                        if (!warp_wait(raw, fixed & 1)) return false;
+                        if (!warp_wait(raw, fixed & 1, a.wait_limit)) return false;
                         ++fixed;
                         zero_tile_rows<C::kSub>(sring + at * C::kBytes, w.len - u * kTile);
                         if (lane == 0) mbar_arrive(full + 8 * at);
                     }
                     return true;
                 };
-                if (tiles > 0 && !(ok = warp_wait(q_empty, (tiles - 1) & 1))) break;
+                if (tiles > 0 && !(ok = warp_wait(q_empty, (tiles - 1) & 1, a.wait_limit))) break;
                 rows(&mq, a.q_mul, sq, q_full);
                 if (!(ok = load(true, 0) && load(false, 0) && (total == 1 || load(true, 1)))) break;
                 // dO's place has been the last job's way out
-                if (tiles > 0 && !(ok = warp_wait(taken, (tiles - 1) & 1))) break;
-                if (seconds > 0 && !(ok = warp_wait(taken + 8, (seconds - 1) & 1))) break;
+                if (tiles > 0 && !(ok = warp_wait(taken, (tiles - 1) & 1, a.wait_limit))) break;
+                if (seconds > 0 && !(ok = warp_wait(taken + 8, (seconds - 1) & 1, a.wait_limit))) break;
                 rows(&mdo, a.do_mul, sdo, do_full);
                 ++tiles;
                 seconds += two;
@@ -1197,17 +1212,17 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             }
             // the CTA must not end, nor its memory be given back, before the last loads and releases have arrived
             if (tiles > 0) {
-                mbar_wait(q_full, (tiles - 1) & 1);
-                mbar_wait(do_full, (tiles - 1) & 1);
-                if (ok) ok = warp_wait(q_empty, (tiles - 1) & 1);
+                mbar_wait(q_full, (tiles - 1) & 1, a.wait_limit);
+                mbar_wait(do_full, (tiles - 1) & 1, a.wait_limit);
+                if (ok) ok = warp_wait(q_empty, (tiles - 1) & 1, a.wait_limit);
             }
             for (uint32_t i = n > C::kKeys ? n - C::kKeys : 0; i < n; ++i) {
-                mbar_wait(full + 8 * (i % C::kKeys), (i / C::kKeys) & 1);
-                if (ok) ok = warp_wait(empty + 8 * (i % C::kKeys), (i / C::kKeys) & 1);
+                mbar_wait(full + 8 * (i % C::kKeys), (i / C::kKeys) & 1, a.wait_limit);
+                if (ok) ok = warp_wait(empty + 8 * (i % C::kKeys), (i / C::kKeys) & 1, a.wait_limit);
             }
             for (uint32_t i = n > C::kValues ? n - C::kValues : 0; i < n; ++i) {
-                mbar_wait(full + 8 * (C::kKeys + i % C::kValues), (i / C::kValues) & 1);
-                if (ok) ok = warp_wait(empty + 8 * (C::kKeys + i % C::kValues), (i / C::kValues) & 1);
+                mbar_wait(full + 8 * (C::kKeys + i % C::kValues), (i / C::kValues) & 1, a.wait_limit);
+                if (ok) ok = warp_wait(empty + 8 * (C::kKeys + i % C::kValues), (i / C::kValues) & 1, a.wait_limit);
             }
         } else if (warp == 8) {   // --------------------------------- products
             if (lane == 0) {   // one thread, as in the forward kernel
@@ -1216,20 +1231,20 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 Place key, value;
                 auto key_of = [&](const Place &p) { return sring + p.at * C::kBytes; };
                 auto value_of = [&](const Place &p) { return sring + (C::kKeys + p.at) * C::kBytes; };
-                auto wait_key = [&](const Place &p) { return mbar_wait(full + 8 * p.at, p.phase); };
+                auto wait_key = [&](const Place &p) { return mbar_wait(full + 8 * p.at, p.phase, a.wait_limit); };
                 auto scores = [&](int t, const Place &p) {   // S = Q K^T
                     product_rows<DP>(tmem + t * 128, sq + t * C::kBytes, key_of(p), id_s | a.negate);
                     mma_commit(s_full + 8 * t);
                 };
                 auto d_probs = [&](int t) {                  // dP = dO V^T, over S
-                    if (!mbar_wait(s_read + 8 * t, c[t] & 1)) return false;
+                    if (!mbar_wait(s_read + 8 * t, c[t] & 1, a.wait_limit)) return false;
                     tc_fence_after();
                     product_rows<DP>(tmem + t * 128, sdo + t * C::kBytes, value_of(value), id_s);
                     mma_commit(dp_full + 8 * t);
                     return true;
                 };
                 auto d_query = [&](int t, bool add) {        // dQ += dS K
-                    if (!mbar_wait(ds_full + 8 * t, c[t] & 1)) return false;
+                    if (!mbar_wait(ds_full + 8 * t, c[t] & 1, a.wait_limit)) return false;
                     tc_fence_after();
                     product_cols<32>(tmem + 256 + t * 128, tmem + t * 128, key_of(key), id_o, add);
                     ++c[t];
@@ -1239,18 +1254,18 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     if (w.kind != kJobWork) continue;
                     const bool two = w.block * 2 * kTile + kTile < w.len;
                     const uint32_t nb0 = w.block * 2 + 1, nb = nb0 + (two ? 1 : 0);   // key tiles of the first tile; of both
-                    if (!(ok = mbar_wait(q_full, tiles & 1) && wait_key(key))) break;
+                    if (!(ok = mbar_wait(q_full, tiles & 1, a.wait_limit) && wait_key(key))) break;
                     tc_fence_after();
                     scores(0, key);
                     if (two) scores(1, key);
                     if (nb == 1) mma_commit(q_empty);
-                    if (!(ok = mbar_wait(do_full, tiles & 1))) break;
+                    if (!(ok = mbar_wait(do_full, tiles & 1, a.wait_limit))) break;
                     ++tiles;
                     for (uint32_t u = 0; u < nb; ++u) {
                         const bool more = u + 1 < nb;
                         Place next = key;
                         next.template next<C::kKeys>();
-                        if (!(ok = mbar_wait(full + 8 * (C::kKeys + value.at), value.phase))) break;
+                        if (!(ok = mbar_wait(full + 8 * (C::kKeys + value.at), value.phase, a.wait_limit))) break;
                         if (u < nb0 && !(ok = d_probs(0))) break;
                         if (two && !(ok = d_probs(1))) break;
                         mma_commit(empty + 8 * (C::kKeys + value.at));
@@ -1274,7 +1289,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 }
             }
         } else if (warp == 10) {   // ------------------------------------ jobs
-            ok = jobs.template run<2 * kTile, true>(a, ranked, a.q_heads);
+            ok = jobs.template run<2 * kTile, true, false>(a, ranked, a.q_heads);
         }
     } else {   // ------------------------------------------- a row of a tile
         registers_up<C::kRowRegs>();
@@ -1297,7 +1312,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 float row_term = term.y;
                 float2 left = make_float2(0.f, 0.f);   // sum of this row's dS: what the row term was off by, as P adds up to one
                 for (uint32_t u = 0; u < total; ++u, ++it) {
-                    if (!(ok = warp_wait(s_full + 8 * t, it & 1))) break;
+                    if (!(ok = warp_wait(s_full + 8 * t, it & 1, a.wait_limit))) break;
                     tc_fence_after();
                     float2 p[64];
                     {
@@ -1315,7 +1330,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                             p[x] = make_float2(exp2_approx(y.x), exp2_approx(y.y));
                         }
                     }
-                    if (!(ok = warp_wait(dp_full + 8 * t, it & 1))) break;
+                    if (!(ok = warp_wait(dp_full + 8 * t, it & 1, a.wait_limit))) break;
                     tc_fence_after();
                     if (total == 1) {   // the row sees this tile alone: its term is exact without the rounded O
                         float exact = 0.f;
@@ -1367,7 +1382,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 if (!ok) break;
                 // the kernel for dK and dV goes on with the better row term
                 if (row < w.len) a.rows[size_t(w.head) * a.n_tokens + w.first + row].y = row_term + (left.x + left.y);
-                if (!(ok = warp_wait(done + 8 * t, tiles & 1))) break;
+                if (!(ok = warp_wait(done + 8 * t, tiles & 1, a.wait_limit))) break;
                 ++tiles;
                 tc_fence_after();
                 const uint32_t row_w = row - lane;   // the warp's first row

@@ -605,8 +605,9 @@ int gac_attn_backward(const gac_attn *args, const gac_attn_grad *grad, int cuda_
 /*
  * The attention kernels wait inside a CTA for their own copies and matrix products,
  * each wait bounded.  If one ever ran out, the rows concerned were written as NaN and
- * this call, which synchronises the stream, returns GAC_ERR_TIMEOUT once; otherwise
- * GAC_OK.
+ * this call, which synchronises the stream, returns GAC_ERR_TIMEOUT; otherwise GAC_OK.
+ * Faults are counted for the whole device: each host thread that asks is told once on every
+ * stream it asks on, so a fault that belongs to others may be told, and none is lost to them.
  */
 int gac_attn_check(int cuda_device, void *cuda_stream);
 

@@ -761,6 +761,7 @@ def gac_attn_backward(d_o: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
 
 
 def gac_attn_check(device: Optional[int] = None, stream=None) -> None:
-    """Synchronises the stream and raises GacError(GAC_ERR_TIMEOUT) if a wait inside an attention kernel ran out."""
+    """Synchronises the stream and raises GacError(GAC_ERR_TIMEOUT) if a wait inside an attention kernel of this device ran
+    out since this thread last asked on this stream."""
     dev = torch.device("cuda", torch.cuda.current_device() if device is None else device)
     _check(load_library().gac_attn_check(dev.index, _on(stream, dev)[0]))

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("gac.cu", "clip.cu", "rotary.cu", "attention.cu")]
 HEADERS = [os.path.join(ROOT, "include", "gac.h")] + \
-          [os.path.join(HERE, "csrc", f) for f in ("gac_host.h", "overlap.h", "gac_kernels.cuh", "sm100.cuh",
+          [os.path.join(HERE, "csrc", f) for f in ("gac_host.h", "faults.h", "overlap.h", "gac_kernels.cuh", "sm100.cuh",
                                                  "attention_kernels.cuh")]
 LIB = os.path.join(HERE, "libgac_b200.so")
 

@@ -12,6 +12,7 @@
 
 #include "gac.h"
 #include "gac_host.h"
+#include "faults.h"
 #include "attention_kernels.cuh"
 
 namespace {
@@ -268,13 +269,15 @@ int gac_attn_check(int cuda_device, void *cuda_stream) {
     DeviceGuard guard(cuda_device);
     if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    int fault = 0;
-    GAC_CUDA(nullptr, cudaMemcpyFromSymbolAsync(&fault, g_attn_fault, sizeof(fault), 0, cudaMemcpyDeviceToHost, s));
+    unsigned faults = 0;
+    GAC_CUDA(nullptr, cudaMemcpyFromSymbolAsync(&faults, g_attn_faults, sizeof(faults), 0, cudaMemcpyDeviceToHost, s));
     GAC_CUDA(nullptr, cudaStreamSynchronize(s));
-    if (!fault) return GAC_OK;
-    const int none = 0;
-    GAC_CUDA(nullptr, cudaMemcpyToSymbolAsync(g_attn_fault, &none, sizeof(none), 0, cudaMemcpyHostToDevice, s));
-    GAC_CUDA(nullptr, cudaStreamSynchronize(s));
+    static thread_local FaultLedger ledger;
+    try {
+        if (!ledger.news(cuda_device, cuda_stream, faults)) return GAC_OK;
+    } catch (...) {   // out of memory: told again rather than not at all
+        if (!faults) return GAC_OK;
+    }
     return fail(nullptr, GAC_ERR_TIMEOUT, "a wait inside an attention kernel ran out%s");
 }
 

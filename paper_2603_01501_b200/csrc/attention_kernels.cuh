@@ -12,8 +12,8 @@ namespace {
 constexpr int kTile = 128;                  // rows of a query or key tile: one tcgen05 accumulator
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Set by a kernel whose bounded wait ran out; read and cleared by gac_attn_check.
-static __device__ int g_attn_fault;
+// CTAs so far in which a bounded wait ran out; read by gac_attn_check, never cleared.
+static __device__ unsigned g_attn_faults;
 
 struct RowsOut {
     char *p;
@@ -652,7 +652,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             poison_rows(a.o, from, end, w.head, a.head_dim);
             for (uint32_t i = from + lane; i < end; i += 32) a.lse[size_t(w.head) * a.n_tokens + i] = __int_as_float(0x7FFFFFFF);
         }
-        if (threadIdx.x == 0) g_attn_fault = 1;
+        if (threadIdx.x == 0) atomicAdd(&g_attn_faults, 1u);
     }
 }
 
@@ -1054,7 +1054,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 poison_rows(a.d_v, from, to, kv_head, a.head_dim);
             }
         }
-        if (threadIdx.x == 0) g_attn_fault = 1;
+        if (threadIdx.x == 0) atomicAdd(&g_attn_faults, 1u);
     }
 }
 
@@ -1404,7 +1404,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             const uint32_t from = w.first + w.block * 2 * kTile;
             poison_rows(a.d_q, from, min(w.first + w.len, from + 2 * kTile), w.head, a.head_dim);
         }
-        if (threadIdx.x == 0) g_attn_fault = 1;
+        if (threadIdx.x == 0) atomicAdd(&g_attn_faults, 1u);
     }
 }
 

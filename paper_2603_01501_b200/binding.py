@@ -482,6 +482,9 @@ def gac_rebind(ctx: GacContext, g_list: Sequence[torch.Tensor], d_list: Sequence
 
 
 # ---------------------------------------------------------------- around the rule: packed rollouts
+#
+# The calls on lists of gradients (gac_project, gac_clip_*) write tensors that autograd does not save in ordinary use and
+# leave their versions alone; gac_rotary in place, on activations, raises them.
 
 
 # Packed forms of gac_rotary_args, gac_attn and gac_attn_grad: one call instead of one per field.
@@ -699,6 +702,8 @@ def gac_rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Opt
                         ROTARY_LAYOUTS[layout], 1 if inverse else 0, 0, _int32_ptr(positions, "positions", device),
                         _int32_ptr(cu_seqlens, "cu_seqlens", device), freqs.__array_interface__["data"][0], scale)
     _check(load_library().gac_rotary(args, device.index, raw))
+    if in_place:   # autograd has to notice that what it may have saved has changed
+        torch.autograd.graph.increment_version(q if k is None else (q, k))
     return yq, yk
 
 

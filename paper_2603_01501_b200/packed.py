@@ -121,6 +121,7 @@ class GradientClipper:
             gb.gac_clip_rebind(self._ctx, grads)
             self._bound = bound
         gb.gac_clip_grad_norm(self._ctx, max_norm, eps, norm_out=self.norm)
+        torch.autograd.graph.increment_version(grads + [self.norm])   # written behind autograd's back
         return self.norm
 
     def close(self) -> None:

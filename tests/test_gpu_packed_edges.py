@@ -200,3 +200,26 @@ def test_rotary_of_queries_alone():
     got, = torch.autograd.grad(y, q, g)
     want, = torch.autograd.grad(packed.rotary(q, k, freqs, positions=pos)[0], q, g)
     assert torch.equal(got, want)
+
+
+def test_in_place_results_raise_the_version_that_autograd_checks():
+    freqs, pos = gb.gac_rotary_freqs(32, 1e4), torch.arange(50, device="cuda", dtype=torch.int32)
+    w = torch.randn(50, 3, 32, device="cuda", requires_grad=True)
+    q, k = torch.randn(50, 3, 32, device="cuda"), torch.randn(50, 1, 32, device="cuda")
+    for hit in (q, k):
+        loss = (w * hit).sum()              # hit is saved for the way back
+        gb.gac_rotary(q, k, freqs, positions=pos, in_place=True)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    p = torch.nn.Parameter(torch.zeros(1000, device="cuda"))
+    p.grad = torch.ones_like(p)
+    loss = (torch.ones(1000, device="cuda", requires_grad=True) * p.grad).sum()
+    clipper = packed.GradientClipper([p])
+    clipper.clip(1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    told = clipper.norm
+    loss = (torch.ones((), device="cuda", requires_grad=True) * told).sum()
+    clipper.clip(1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()

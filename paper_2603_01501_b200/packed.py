@@ -100,8 +100,10 @@ class GradientClipper:
         self._shape: List[tuple] = []
         self._bound: List[int] = []
 
-    def clip(self, max_norm: float, eps: float = 1e-6) -> torch.Tensor:
-        """Returns the norm before clipping as a 0-dim device tensor, overwritten by the next call."""
+    def clip(self, max_norm: float, eps: float = 1e-6, error_if_nonfinite: bool = False) -> torch.Tensor:
+        """Returns the norm before clipping as a 0-dim device tensor, overwritten by the next call.  A norm that is NaN or
+        infinite leaves every gradient as it is; the tensor says so, and with ``error_if_nonfinite``, which waits for the
+        device, GacError(GAC_ERR_NONFINITE) does."""
         grads = [p.grad for p in self.params if p.grad is not None]
         if not grads:
             self.norm.zero_()
@@ -120,7 +122,9 @@ class GradientClipper:
             self._bound = []   # should the call fail, the next one tries again
             gb.gac_clip_rebind(self._ctx, grads)
             self._bound = bound
-        gb.gac_clip_grad_norm(self._ctx, max_norm, eps, norm_out=self.norm)
+        res = gb.gac_clip_grad_norm(self._ctx, max_norm, eps, norm_out=self.norm, fetch=error_if_nonfinite)
+        if error_if_nonfinite and res.nonfinite:
+            raise gb.GacError(gb.GAC_ERR_NONFINITE, "the norm of the gradients is NaN or infinite; none was changed")
         torch.autograd.graph.increment_version(grads + [self.norm])   # written behind autograd's back
         return self.norm
 

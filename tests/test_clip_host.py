@@ -126,3 +126,17 @@ def test_the_clipper_rebinds_moved_gradients_and_survives_a_failure(library, mon
     monkeypatch.setattr(gb, "gac_clip_init", good[1])
     clipper.clip(1.0)
     assert len(library.made) == 3 and library.clipped == before + 1 and len(old) == 2
+
+
+def test_a_norm_that_is_not_finite_is_raised_when_asked_for(library, monkeypatch):
+    def clip(ctx, max_norm, eps=1e-6, norm_out=None, stream=None, fetch=False):
+        library.clipped += 1
+        return types.SimpleNamespace(nonfinite=1, norm=float("nan"), timed_out=0) if fetch else None
+    monkeypatch.setattr(gb, "gac_clip_grad_norm", clip)
+    p = torch.nn.Parameter(torch.zeros(3))
+    p.grad = torch.ones(3)
+    clipper = packed.GradientClipper([p])
+    clipper.clip(1.0)                                    # as it is, without waiting for the host
+    with pytest.raises(gb.GacError) as e:
+        clipper.clip(1.0, error_if_nonfinite=True)
+    assert e.value.status == gb.GAC_ERR_NONFINITE and library.clipped == 2

@@ -223,3 +223,18 @@ def test_in_place_results_raise_the_version_that_autograd_checks():
     clipper.clip(1.0)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_norm_that_is_not_finite_is_raised_when_asked_for(bad):
+    p = torch.nn.Parameter(torch.zeros(1000, device="cuda"))
+    p.grad = torch.ones_like(p)
+    p.grad[7] = bad
+    keep, clipper = p.grad.clone(), packed.GradientClipper([p])
+    assert not math.isfinite(float(clipper.clip(1.0)))
+    with pytest.raises(gb.GacError) as e:
+        clipper.clip(1.0, error_if_nonfinite=True)
+    assert e.value.status == gb.GAC_ERR_NONFINITE
+    assert torch.equal(p.grad.nan_to_num(3.0), keep.nan_to_num(3.0))
+    p.grad[7] = 1.0
+    assert abs(float(clipper.clip(1.0, error_if_nonfinite=True)) - math.sqrt(1000.0)) < 1e-4

@@ -95,7 +95,7 @@ class GradientClipper:
         self.params: List[torch.nn.Parameter] = [p for p in params if p.requires_grad]
         if not self.params:
             raise ValueError("no trainable parameters")
-        self.norm = torch.zeros((), device=self.params[0].device)
+        self.norm = torch.zeros((), dtype=torch.float32, device=self.params[0].device)
         self._ctx: Optional[gb.ClipContext] = None
         self._shape: List[tuple] = []
         self._bound: List[int] = []

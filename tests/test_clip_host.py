@@ -140,3 +140,12 @@ def test_a_norm_that_is_not_finite_is_raised_when_asked_for(library, monkeypatch
     with pytest.raises(gb.GacError) as e:
         clipper.clip(1.0, error_if_nonfinite=True)
     assert e.value.status == gb.GAC_ERR_NONFINITE and library.clipped == 2
+
+
+def test_the_norm_is_float32_whatever_the_default_is():
+    before = torch.get_default_dtype()
+    try:
+        torch.set_default_dtype(torch.bfloat16)
+        assert packed.GradientClipper([torch.nn.Parameter(torch.zeros(3))]).norm.dtype is torch.float32
+    finally:
+        torch.set_default_dtype(before)

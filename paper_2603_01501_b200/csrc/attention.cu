@@ -13,6 +13,7 @@
 #include "gac.h"
 #include "gac_host.h"
 #include "faults.h"
+#include "overlap.h"
 #include "attention_kernels.cuh"
 
 namespace {
@@ -22,11 +23,8 @@ int fail(std::nullptr_t, int code, const char *fmt, const char *a = "", long lon
     return code;
 }
 
-struct Span {
-    uint64_t lo, hi;
-};
 // Alignment, strides and extent of one [tokens][heads][dim] block; outputs need a place for every element.
-int check_heads(const gac_attn_heads &h, const gac_attn &a, uint32_t heads, bool output, const char *name, Span *span) {
+int check_heads(const gac_attn_heads &h, const gac_attn &a, uint32_t heads, bool output, const char *name, Rows *rows) {
     const uint64_t p = reinterpret_cast<uint64_t>(h.p);
     if (!p || p % 16) return fail(nullptr, GAC_ERR_INVALID_ARG, "%s must be a 16-byte aligned device pointer", name);
     const int64_t most = int64_t(1) << 38;
@@ -41,12 +39,13 @@ int check_heads(const gac_attn_heads &h, const gac_attn &a, uint32_t heads, bool
         if ((n_less > 1 && less < dim) || (n_more > 1 && more < (n_less - 1) * (n_less > 1 ? less : 0) + dim))
             return fail(nullptr, GAC_ERR_INVALID_ARG, "%s: heads overlap one another", name);
     }
-    span->lo = p;
-    span->hi = p + ((nt - 1) * uint64_t(h.token) + (nh - 1) * uint64_t(h.head) + dim) * 2;
+    *rows = Rows{p, uint64_t(h.token) * 2, uint64_t(h.head) * 2, nt, nh, dim * 2};
     return GAC_OK;
 }
 
-bool overlap(const Span &x, const Span &y) { return x.lo < y.hi && y.lo < x.hi; }
+bool spans_cross(const Rows &x, const Rows &y) { return x.p < y.end() && y.p < x.end(); }
+Rows block(const void *p, uint64_t bytes) { return Rows{reinterpret_cast<uint64_t>(p), 0, 0, 1, 1, bytes}; }
+Rows lse_of(const gac_attn &a) { return block(a.lse, uint64_t(a.q_heads) * a.n_tokens * sizeof(float)); }
 
 // Everything that does not look at pointers.
 int check_shape(const gac_attn *args) {
@@ -226,7 +225,7 @@ int launch_backward(const gac_attn &a, const gac_attn_grad &g, int device, cudaS
     return GAC_OK;
 }
 
-int check_pointers(const gac_attn &a, Span (&in)[3], Span *o) {
+int check_pointers(const gac_attn &a, Rows (&in)[3], Rows *o) {
     if (int rc = check_heads(a.q, a, a.q_heads, false, "q", &in[0])) return rc;
     if (int rc = check_heads(a.k, a, a.kv_heads, false, "k", &in[1])) return rc;
     if (int rc = check_heads(a.v, a, a.kv_heads, false, "v", &in[2])) return rc;
@@ -235,8 +234,10 @@ int check_pointers(const gac_attn &a, Span (&in)[3], Span *o) {
         return fail(nullptr, GAC_ERR_INVALID_ARG, "lse must be a 4-byte aligned device pointer%s");
     if (!a.cu_seqlens || reinterpret_cast<uint64_t>(a.cu_seqlens) % 4)
         return fail(nullptr, GAC_ERR_INVALID_ARG, "cu_seqlens must be a 4-byte aligned device pointer%s");
-    for (const Span &s : in)
-        if (overlap(s, *o)) return fail(nullptr, GAC_ERR_INVALID_ARG, "o overlaps an input%s");
+    const Rows lse = lse_of(a);
+    for (const Rows &r : in)
+        if (spans_cross(r, *o) || share(r, lse)) return fail(nullptr, GAC_ERR_INVALID_ARG, "o or lse overlaps an input%s");
+    if (share(*o, lse)) return fail(nullptr, GAC_ERR_INVALID_ARG, "lse overlaps o%s");
     return GAC_OK;
 }
 
@@ -256,7 +257,7 @@ int gac_attn_forward(const gac_attn *args, int cuda_device, void *cuda_stream) {
     if (int rc = check_shape(args)) return rc;
     const gac_attn &a = *args;
     if (a.n_tokens == 0) return GAC_OK;
-    Span in[3], o;
+    Rows in[3], o;
     if (int rc = check_pointers(a, in, &o)) return rc;
     Range range("gac_attn_forward");
     DeviceGuard guard(cuda_device);
@@ -287,9 +288,9 @@ int gac_attn_backward(const gac_attn *args, const gac_attn_grad *grad, int cuda_
     if (!grad) return fail(nullptr, GAC_ERR_INVALID_ARG, "grad is NULL%s");
     const gac_attn_grad &g = *grad;
     if (a.n_tokens == 0) return GAC_OK;
-    Span in[5], out[3];
+    Rows in[5], out[3];
     {
-        Span first[3];
+        Rows first[3];
         if (int rc = check_pointers(a, first, &in[3])) return rc;
         std::copy(first, first + 3, in);
     }
@@ -297,15 +298,19 @@ int gac_attn_backward(const gac_attn *args, const gac_attn_grad *grad, int cuda_
     if (int rc = check_heads(g.d_q, a, a.q_heads, true, "d_q", &out[0])) return rc;
     if (int rc = check_heads(g.d_k, a, a.kv_heads, true, "d_k", &out[1])) return rc;
     if (int rc = check_heads(g.d_v, a, a.kv_heads, true, "d_v", &out[2])) return rc;
-    for (const Span &x : in)
-        for (const Span &y : out)
-            if (overlap(x, y)) return fail(nullptr, GAC_ERR_INVALID_ARG, "a gradient overlaps an input%s");
-    // spans of interleaved views may cross; the same memory twice may not
-    if (g.d_q.p == g.d_k.p || g.d_q.p == g.d_v.p || g.d_k.p == g.d_v.p || g.workspace == g.d_q.p || g.workspace == g.d_k.p ||
-        g.workspace == g.d_v.p)
-        return fail(nullptr, GAC_ERR_INVALID_ARG, "two gradients, or a gradient and the workspace, are the same memory%s");
     if (!g.workspace || reinterpret_cast<uint64_t>(g.workspace) % 16 || g.workspace_bytes < gac_attn_workspace(args))
         return fail(nullptr, GAC_ERR_INVALID_ARG, "workspace must be 16-byte aligned and of gac_attn_workspace bytes%s");
+    const Rows lse = lse_of(a), work = block(g.workspace, gac_attn_workspace(args));
+    for (const Rows &x : in) {
+        for (const Rows &y : out)
+            if (spans_cross(x, y)) return fail(nullptr, GAC_ERR_INVALID_ARG, "a gradient overlaps an input%s");
+        if (share(x, work)) return fail(nullptr, GAC_ERR_INVALID_ARG, "the workspace overlaps an input%s");
+    }
+    if (share(lse, work)) return fail(nullptr, GAC_ERR_INVALID_ARG, "the workspace overlaps lse%s");
+    // spans of views of one fused gradient cross, their rows do not share memory
+    for (int i = 0; i < 3; ++i)
+        if (share(out[i], out[(i + 1) % 3]) || share(out[i], work) || share(out[i], lse))
+            return fail(nullptr, GAC_ERR_INVALID_ARG, "two gradients, or a gradient and the workspace or lse, overlap%s");
     Range range("gac_attn_backward");
     DeviceGuard guard(cuda_device);
     if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");

@@ -238,3 +238,24 @@ def test_a_norm_that_is_not_finite_is_raised_when_asked_for(bad):
     assert torch.equal(p.grad.nan_to_num(3.0), keep.nan_to_num(3.0))
     p.grad[7] = 1.0
     assert abs(float(clipper.clip(1.0, error_if_nonfinite=True)) - math.sqrt(1000.0)) < 1e-4
+
+
+def test_gradients_as_views_of_one_fused_tensor():
+    """d_q, d_k and d_v lie between each other's heads: their spans cross and no memory is shared."""
+    import ctypes
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    tokens, cu = 300, torch.tensor([0, 130, 290], dtype=torch.int32, device="cuda")
+    q, k, v = torch.randn(tokens, 8, 64, generator=gen, device="cuda").to(BF).split([4, 2, 2], dim=1)
+    d_o = torch.randn(tokens, 4, 64, generator=gen, device="cuda").to(BF)
+    o, lse = gb.gac_attn_forward(q, k, v, cu)
+    want = gb.gac_attn_backward(d_o, q, k, v, o, lse, cu)
+    fused = torch.full((tokens, 8, 64), 7.0, dtype=BF, device="cuda")
+    outs = fused.split([4, 2, 2], dim=1)
+    heads = [gb.gac_attn_heads(t.data_ptr(), t.stride(0), t.stride(1)) for t in (q, k, v, o, d_o, *outs)]
+    a = gb.gac_attn(*heads[:4], lse.data_ptr(), cu.data_ptr(), tokens, 2, 4, 2, 64, gb.GAC_BF16, 0.125, 0)
+    L = gb.load_library()
+    need = L.gac_attn_workspace(ctypes.byref(a))
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    g = gb.gac_attn_grad(*heads[4:], work.data_ptr(), need)
+    gb._check(L.gac_attn_backward(ctypes.byref(a), ctypes.byref(g), 0, torch.cuda.current_stream().cuda_stream))
+    assert all(torch.equal(x, y) for x, y in zip(outs, want))

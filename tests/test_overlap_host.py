@@ -70,3 +70,33 @@ M = 1 << 20
 def test_rotary_operands_that_share_memory_are_refused(x0, y0, x1, y1):
     rc, msg = rotary(x0, y0, x1, y1)
     assert rc == gb.GAC_ERR_INVALID_ARG and "overlap" in msg
+
+
+def attention(backward=False, **over):
+    """Forward or backward on 100 tokens, 4/2 heads x 64; the operands a megabyte apart unless said."""
+    names = ("q", "k", "v", "o", "d_o", "d_q", "d_k", "d_v")
+    at = {n: (i + 1) << 20 for i, n in enumerate(names)}
+    at.update(lse=20 << 20, cu=21 << 20, workspace=22 << 20)
+    at.update(over)
+    h = {n: gb.gac_attn_heads(at[n], 256, 64) for n in names}
+    a = gb.gac_attn(h["q"], h["k"], h["v"], h["o"], at["lse"], at["cu"], 100, 3, 4, 2, 64, gb.GAC_BF16, 0.125, 0)
+    L = gb.load_library()
+    if backward:
+        g = gb.gac_attn_grad(h["d_o"], h["d_q"], h["d_k"], h["d_v"], at["workspace"], 1 << 20)
+        rc = L.gac_attn_backward(ctypes.byref(a), ctypes.byref(g), 0, None)
+    else:
+        rc = L.gac_attn_forward(ctypes.byref(a), 0, None)
+    return rc, L.gac_last_error(None).decode()
+
+
+@pytest.mark.parametrize("over", [{"lse": M}, {"lse": 4 * M}, {"lse": 4 * M + 50_000}, {"lse": 2 * M - 4}], ids=str)
+def test_attention_statistics_on_an_operand_are_refused(over):
+    rc, msg = attention(**over)
+    assert rc == gb.GAC_ERR_INVALID_ARG and "overlap" in msg
+
+
+@pytest.mark.parametrize("over", [{"d_k": 6 * M + 128}, {"d_v": 7 * M + 512}, {"d_v": 6 * M + 16}, {"workspace": M + 16}, {"workspace": 5 * M - 64},
+                                  {"workspace": 20 * M}, {"workspace": 6 * M + 64}, {"lse": 8 * M + 4}], ids=str)
+def test_gradients_and_workspace_that_share_memory_are_refused(over):
+    rc, msg = attention(backward=True, **over)
+    assert rc == gb.GAC_ERR_INVALID_ARG and ("overlap" in msg or "same memory" in msg)

@@ -1,5 +1,6 @@
 """Policy updates on packed rollouts, end to end: a small decoder with grouped-query attention, a clipped
-policy-gradient loss, the gradient alignment rule, clipping and AdamW.
+policy-gradient loss, the gradient alignment rule with clipping in its own pass, a value head whose gradients have no
+stored direction and are clipped by themselves, and AdamW.
 
     python examples/packed_policy_update.py [steps]
 
@@ -51,13 +52,13 @@ class Policy(torch.nn.Module):
         # positions stretched to four times the trained context
         self.freqs = gb.gac_rotary_freqs(HEAD_DIM, 1e4, "parts", 4.0, trained=512.0)
 
-    def logprobs(self, tokens, cu):
-        """Log-probability of every token's successor in the pack."""
+    def forward(self, tokens, cu):
+        """Log-probability of every token's successor in the pack, and the last hidden states."""
         x = self.embed(tokens)
         for block in self.blocks:
             x = block(x, cu, self.freqs)
-        logits = self.norm(x) @ self.embed.weight.t()
-        return F.log_softmax(logits[:-1], -1).gather(1, tokens[1:, None])[:, 0]
+        x = self.norm(x)
+        return F.log_softmax((x @ self.embed.weight.t())[:-1], -1).gather(1, tokens[1:, None])[:, 0], x
 
 
 def rollouts(step, device="cuda"):
@@ -74,26 +75,31 @@ def rollouts(step, device="cuda"):
 
 def main(steps=5, max_norm=1.0):
     torch.manual_seed(0)
-    policy = Policy().cuda()
-    optimizer = torch.optim.AdamW(policy.parameters(), lr=1e-4)
-    controller = GradientAlignmentController(policy.parameters())
-    clipper = packed.GradientClipper(policy.parameters())
+    policy, value = Policy().cuda(), torch.nn.Linear(HIDDEN, 1).cuda()
+    optimizer = torch.optim.AdamW([*policy.parameters(), *value.parameters()], lr=1e-4)
+    # the policy's gradients: the rule, clipped in the pass that applies it
+    controller = GradientAlignmentController(policy.parameters(), gb.HParams(clip_max_norm=max_norm))
+    # the value head's: no stored direction, norm and clipping alone
+    clipper = packed.GradientClipper(value.parameters())
     told = []
     for step in range(steps):
         tokens, cu, advantage, inner = rollouts(step)
         with torch.no_grad():
-            old = policy.logprobs(tokens, cu)
-        ratio = (policy.logprobs(tokens, cu) - old).exp()
+            old, _ = policy(tokens, cu)
+        new, states = policy(tokens, cu)
+        ratio = (new - old).exp()
         gain = torch.minimum(ratio * advantage, ratio.clamp(0.8, 1.2) * advantage)
-        loss = -gain[inner].mean()
-        optimizer.zero_grad(set_to_none=False)
+        error = value(states[:-1].detach())[:, 0] - advantage
+        loss = -gain[inner].mean() + error[inner].square().mean()
+        optimizer.zero_grad()
         loss.backward()
-        go_on = controller.step()                 # the alignment rule, in place on the gradients
-        norm = clipper.clip(max_norm)             # then clipping of what the step sends on
-        if go_on:
-            optimizer.step()
+        go_on = controller.step()                 # the alignment rule, in place on the policy's gradients
+        norm = clipper.clip(max_norm)
+        if not go_on:                             # a violation: the policy stays as it is
+            policy.zero_grad()
+        optimizer.step()
         told.append((float(loss.detach()), float(norm), controller.last.cos))
-        print("step %d  loss %+.5f  norm %.4f  alignment %+.4f  %s" % (step, *told[-1], gb.REGIME_NAMES[controller.last.regime]))
+        print("step %d  loss %+.5f  value norm %.4f  alignment %+.4f  %s" % (step, *told[-1], gb.REGIME_NAMES[controller.last.regime]))
     gb.gac_attn_check()
     controller.close()
     clipper.close()

@@ -162,7 +162,7 @@ int launch_forward(const gac_attn &a, int device, cudaStream_t s) {
 // Query heads of a group are summed in one CTA as long as there are enough key tiles to go round; with fewer, parts
 // of the group go to CTAs of their own and a second kernel adds them.  Backward with this limit, with 250 and with 600
 // jobs: 8192 tokens, 12/2 heads 199 us, 225, 213; 16384 tokens in one sequence 2.33 ms, 2.90, 2.38; 12384 tokens, 28/4
-// heads 0.99 ms, 1.00, 1.06.
+// heads 0.99 ms, 1.00, 1.06.  Parts have equally many heads, so groups of prime size go from one part to one for each head.
 constexpr uint32_t kEnoughJobs = 370;   // 2.5 per SM
 uint32_t parts_of(const gac_attn &a) {
     const uint32_t group = a.q_heads / a.kv_heads;

@@ -381,14 +381,16 @@ __device__ __forceinline__ void product_cols(uint32_t d, uint32_t a, uint32_t b,
 // in flight, is rare.  The two tiles alternate: while one tile's products run on the tensor cores the other tile's
 // exponentials are taken.
 // Warps: 0-3 and 4-7 the rows of the two tiles, 8 issues the products, 9 the TMA loads, 10 finds the jobs; 11 only makes
-// the third warpgroup whole, which hands registers over to the first two (a row of 128 scores stays in registers).
+// the third warpgroup whole, which hands registers over to the first two, so that a row of 128 scores stays in registers.
+// (The compiler plans with the 168 of the launch and spills 48 bytes at DP = 64 and 108 at 128 beside it.)
 //
 // Per key tile and query tile the tensor cores need 1024 cycles, the exponentials as many on the 16-wide special function
 // unit, and the way from a finished S to the next (scores out of tensor memory, maximum, exponentials, P back, two
 // products, four barriers) takes about 3700; two tiles in turn make that 1850 each.  One query tile of 128 rows per CTA and two
-// CTAs per SM would hide it too, but read every key and value tile twice.  Measured: one sequence of 16384 tokens,
-// 12/2 heads x 128, 630 us = 1.31 PFLOP/s (0.78 of cuBLAS's best rate, 0.92 of its rate under the power cap); 12384 tokens in
-// four sequences, 28/4 heads, 262 us = 1.13; 8192 tokens in eight sequences, 12/2 heads, 56 us = 0.62: there a CTA has three
+// CTAs per SM would hide it too, but read every key and value tile twice.  Measured in ten calls after a pause and in a
+// second of calls on end, which meets the power cap: one sequence of 16384 tokens, 12/2 heads x 128, 636 us = 1.30 PFLOP/s
+// (0.77 of cuBLAS's best rate) and 720 us = 1.15 (0.80 of its rate under the cap); 12384 tokens in four sequences, 28/4
+// heads, 265 us = 1.12 and 301; 8192 tokens in eight sequences, 12/2 heads, 53 us = 0.66 on end: there a CTA has three
 // jobs of 7 key tiles, and each starts with a load, a product and a full softmax that nothing hides.
 
 template <int DP>
@@ -709,9 +711,10 @@ static __global__ void __launch_bounds__(kRowThreads) attn_rows_kernel(const __g
 // while they take the next exponentials, dK and the next dP.
 //
 // Four products of 512 cycles per query tile; a turn takes about 3400, the way from S through P, dV and the next S:
-// tensor memory (512 columns: S, dP, dV, dK) has no room for a second S, and the two loads of 32 KB per turn take about
-// 2200 cycles each with shared memory for two turns.  Measured: 12384 tokens, 28/4 heads x 128, 620 us (0.96 PFLOP/s of the
-// four products done), 16384 tokens in one sequence, 12/2 heads, 1.32 ms (1.25).
+// tensor memory (512 columns: S, dP, dV, dK) has no room for a second S at head sizes above 64 (up to 64, dV and dK take 64
+// columns each and it would fit; the same code serves both), and the two loads of 32 KB per turn take about 2200 cycles
+// each with shared memory for two turns.  Measured: 12384 tokens, 28/4 heads x 128, 584 us (1.02 PFLOP/s of the four
+// products done).
 template <int DP>
 struct BwdKv {
     static constexpr int kSub = DP / 64;
@@ -1098,7 +1101,7 @@ static __global__ void __launch_bounds__(256) attn_sum_parts_kernel(const __grid
 //
 // Six products of 512 cycles per key tile and pair of query tiles; a turn takes about 4300, of which the issuing thread
 // loses some 150 at each of its four waits.  One query tile per CTA with S double-buffered loads twice as much, has room
-// for one value tile, and waits for it: 447 us where this takes 385 (12384 tokens, 28/4 heads x 128).
+// for one value tile, and waits for it: 447 us where this took 385 (12384 tokens, 28/4 heads x 128; 358 on a cool card).
 template <int DP>
 struct BwdQ {
     static constexpr int kSub = DP / 64;

@@ -9,7 +9,7 @@
 // added in index order.  One cooperative launch does both passes; the CTAs meet in between.
 // Measured: 1.5 B float32 elements 2.78 ms = 6.66 TB/s over the three passes (1.03 of a plain copy's rate), 0.25 B
 // bfloat16 240 us = 6.2 TB/s (its first pass converts every element to binary64 and is held up by that), 2^20 float32
-// 8.2 us and the 39 tensors of a small mixed list 6.2 us, which are one launch and one meeting of all CTAs.
+// 8.2 us and the 38 tensors of a small mixed list 6.2 us, which are one launch and one meeting of all CTAs.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>

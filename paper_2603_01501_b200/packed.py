@@ -10,7 +10,9 @@ cu_seqlens[b] .. cu_seqlens[b+1].
     loss.backward()
     clipper.clip(1.0)
 
-All arithmetic is in the CUDA library (``binding``); this module only says what is saved for the way back.
+All arithmetic is in the CUDA library (``binding``); this module only says what is saved for the way back.  These are
+autograd functions, not registered torch operators: they have no fake kernels, batching rules or forward mode, and a
+compiled policy breaks its graph at them.
 """
 from __future__ import annotations
 

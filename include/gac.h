@@ -518,6 +518,12 @@ int gac_clip_free(gac_clip_ctx *ctx);   /* NULL is accepted */
  * the place of each token in its sequence by cu_seqlens (tokens behind the last
  * sequence: position 0).
  *
+ * gac_rotary_on_axes is gac_rotary for tokens that stand in time, height and width: a
+ * token has a position on each of n_axes axes, `positions` (which must then be given) holds one row
+ * of n_tokens after the other, `stride` elements apart, and pair i turns by
+ *     positions[axis[i] * stride + token] * freq[i].
+ * axes = NULL: gac_rotary.
+ *
  * gac_rotary_freqs fills freq[rot_dim/2] (host) with base^(-2i/rot_dim), stretched
  * for contexts `factor` times as long as the trained one:
  *   NONE    as they are (factor must be 1)
@@ -556,6 +562,14 @@ typedef struct {
 int gac_rotary_freqs(double *freqs, uint32_t rot_dim, double base, int scaling, double factor, double trained,
                      double low, double high);
 int gac_rotary(const gac_rotary_args *args, int cuda_device, void *cuda_stream);
+#define GAC_ROTARY_MAX_AXES 4
+typedef struct {
+    const uint8_t *axis;          /* HOST [rot_dim/2], each below n_axes; copied               */
+    int64_t stride;               /* of the axes' rows of positions, in elements, 0..2^40      */
+    uint32_t n_axes;              /* 1..GAC_ROTARY_MAX_AXES                                    */
+    uint32_t reserved;            /* must be 0                                                 */
+} gac_rotary_axes;
+int gac_rotary_on_axes(const gac_rotary_args *args, const gac_rotary_axes *axes, int cuda_device, void *cuda_stream);
 
 /*
  * Causal attention over a pack, grouped heads: query head h reads key head
@@ -610,6 +624,41 @@ int gac_attn_backward(const gac_attn *args, const gac_attn_grad *grad, int cuda_
  * stream it asks on, so a fault that belongs to others may be told, and none is lost to them.
  */
 int gac_attn_check(int cuda_device, void *cuda_stream);
+
+/*
+ * Norms of query and key heads with their rotation in the same pass.  Of every head x (head_dim elements)
+ *     r = 1 / sqrt(mean_d x_d^2 + eps)
+ *     y = turn(x r (offset + weight))
+ * with the turn of gac_rotary or gac_rotary_on_axes (its first rot_dim elements, multiplied by scale; rot_dim = 0 turns
+ * nothing and needs no positions), from the same arguments; `inverse` must be 0.  One weight serves all query
+ * heads, one all key heads; NULL stands for ones, without the offset.  y may equal x as in gac_rotary.  Rows
+ * behind the last sequence are normed like the others.
+ *
+ * gac_norm_rotary_backward: with the arguments of the forward call, but in qk the gradient of y at x and where the
+ * gradient of x goes at y (which may be the same memory with the same strides), and the forward call's x in grad->x.
+ * d_weight are written, or, where NULL, not wanted; their sums have one order, so two calls give the same bits.
+ * The workspace of gac_norm_rotary_workspace bytes (device, 16-byte aligned) need not be kept.  Outputs and
+ * workspace must not overlap anything else.
+ * Squares, sums and the rest are binary32 (sums over tokens end in binary64); results are rounded once.
+ * Errors: INVALID_ARG, DTYPE, CUDA.
+ */
+typedef struct {
+    const void *weight[2];        /* device [head_dim], element-aligned: of queries, of keys; or NULL */
+    int32_t weight_dtype;         /* gac_dtype of both, and of their gradients                 */
+    int32_t reserved;             /* must be 0                                                 */
+    double eps;                   /* > 0, finite                                               */
+    double offset;                /* added to the weights; finite (0, or 1 where they are stored as the distance from 1) */
+} gac_norm;
+typedef struct {
+    gac_attn_heads x[2];          /* what the forward call read: queries, keys                  */
+    void *d_weight[2];
+    void *workspace;
+    size_t workspace_bytes;
+} gac_norm_grad;
+int gac_norm_rotary(const gac_rotary_args *args, const gac_rotary_axes *axes, const gac_norm *norm, int cuda_device, void *cuda_stream);
+size_t gac_norm_rotary_workspace(const gac_rotary_args *args);   /* 0 for a head_dim out of range */
+int gac_norm_rotary_backward(const gac_rotary_args *args, const gac_rotary_axes *axes, const gac_norm *norm, const gac_norm_grad *grad,
+                             int cuda_device, void *cuda_stream);
 
 #ifdef __cplusplus
 }

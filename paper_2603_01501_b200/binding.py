@@ -73,6 +73,7 @@ class gac_info(ctypes.Structure):
 
 
 GAC_ROTARY_HALF, GAC_ROTARY_INTERLEAVED = 0, 1
+GAC_ROTARY_MAX_AXES = 4
 GAC_ROTARY_NONE, GAC_ROTARY_LINEAR, GAC_ROTARY_BASE, GAC_ROTARY_PARTS = 0, 1, 2, 3
 ROTARY_LAYOUTS = {"half": GAC_ROTARY_HALF, "interleaved": GAC_ROTARY_INTERLEAVED}
 ROTARY_SCALINGS = {"none": GAC_ROTARY_NONE, "linear": GAC_ROTARY_LINEAR, "base": GAC_ROTARY_BASE,
@@ -102,6 +103,10 @@ class gac_rotary_args(ctypes.Structure):
                 ("freqs", ctypes.c_void_p), ("scale", ctypes.c_double)]
 
 
+class gac_rotary_axes(ctypes.Structure):
+    _fields_ = [("axis", ctypes.c_void_p), ("stride", ctypes.c_int64), ("n_axes", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
 class gac_attn_heads(ctypes.Structure):
     _fields_ = [("p", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
 
@@ -119,6 +124,16 @@ class gac_attn_grad(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class gac_norm(ctypes.Structure):
+    _fields_ = [("weight", ctypes.c_void_p * 2), ("weight_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("eps", ctypes.c_double), ("offset", ctypes.c_double)]
+
+
+class gac_norm_grad(ctypes.Structure):
+    _fields_ = [("x", gac_attn_heads * 2), ("d_weight", ctypes.c_void_p * 2), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
 EXPORTS = ["gac_default_hparams", "gac_init", "gac_stats", "gac_stats_partial", "gac_decide",
            "gac_project", "gac_free", "gac_last_error", "gac_set_launch", "gac_get_info",
            "gac_stats_static", "gac_default_adamw", "gac_attach_adamw", "gac_project_adamw",
@@ -126,7 +141,8 @@ EXPORTS = ["gac_default_hparams", "gac_init", "gac_stats", "gac_stats_partial", 
            "gac_stats_exchange", "gac_decide_exchange", "gac_clip_init", "gac_clip_rebind", "gac_clip_sumsq",
            "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_set_timeout", "gac_clip_free", "gac_rotary_freqs", "gac_rotary",
            "gac_attn_workspace",
-           "gac_attn_forward", "gac_attn_backward", "gac_attn_check"]
+           "gac_attn_forward", "gac_attn_backward", "gac_attn_check", "gac_rotary_on_axes", "gac_norm_rotary",
+           "gac_norm_rotary_workspace", "gac_norm_rotary_backward"]
 
 _lib = None
 
@@ -199,8 +215,14 @@ def load_library() -> ctypes.CDLL:
     L.gac_attn_forward.argtypes = [vp, i32, vp]
     L.gac_attn_backward.argtypes = [vp, vp, i32, vp]
     L.gac_attn_check.argtypes = [i32, vp]
+    L.gac_rotary_on_axes.argtypes = [vp, vp, i32, vp]
+    L.gac_norm_rotary.argtypes = [vp, vp, vp, i32, vp]
+    L.gac_norm_rotary_workspace.argtypes = [vp]
+    L.gac_norm_rotary_workspace.restype = ctypes.c_size_t
+    L.gac_norm_rotary_backward.argtypes = [vp, vp, vp, vp, i32, vp]
     for name in ("gac_clip_init", "gac_clip_rebind", "gac_clip_sumsq", "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_set_timeout",
-                 "gac_clip_free", "gac_rotary_freqs", "gac_rotary", "gac_attn_forward", "gac_attn_backward", "gac_attn_check"):
+                 "gac_clip_free", "gac_rotary_freqs", "gac_rotary", "gac_attn_forward", "gac_attn_backward", "gac_attn_check",
+                 "gac_rotary_on_axes", "gac_norm_rotary", "gac_norm_rotary_backward"):
         getattr(L, name).restype = i32
     for name in ("gac_init", "gac_stats", "gac_stats_partial", "gac_decide", "gac_project",
                  "gac_free", "gac_set_launch", "gac_get_info"):
@@ -484,11 +506,14 @@ def gac_rebind(ctx: GacContext, g_list: Sequence[torch.Tensor], d_list: Sequence
 # ---------------------------------------------------------------- around the rule: packed rollouts
 #
 # The calls on lists of gradients (gac_project, gac_clip_*) write tensors that autograd does not save in ordinary use and
-# leave their versions alone; gac_rotary in place, on activations, raises them.
+# leave their versions alone; gac_rotary and gac_norm_rotary in place, on activations, raise them.
 
 
-# Packed forms of gac_rotary_args, gac_attn and gac_attn_grad: one call instead of one per field.
+# Packed forms of the argument structures: one call instead of one per field.
 _ROTARY = struct.Struct("=QQqqqqQQqqqqIIIIIIiiiiQQQd")
+_AXES = struct.Struct("=QqII")
+_NORM = struct.Struct("=QQiidd")
+_NORM_GRAD = struct.Struct("=QqqQqqQQQQ")
 _ATTN = struct.Struct("=QqqQqqQqqQqqQQIIIIIifi")
 _ATTN_GRAD = struct.Struct("=QqqQqqQqqQqqQQ")
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
@@ -664,13 +689,22 @@ def _heads(t: torch.Tensor, name: str, like: torch.Tensor):
     return t.data_ptr(), s0, s1, h
 
 
-def gac_rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Optional[torch.Tensor] = None,
-               cu_seqlens: Optional[torch.Tensor] = None, layout: str = "half", scale: float = 1.0,
-               inverse: bool = False, in_place: bool = False, stream=None):
-    """Rotary positions on q (and k, or None), [tokens, heads, head_dim] float32 or bfloat16 views.
-    ``freqs``: float64 radians per position (gac_rotary_freqs); it turns the first 2 * len(freqs) elements of
-    a head.  Positions are given, or follow from ``cu_seqlens``.  Returns (q', k'): new contiguous tensors, or
-    the given ones when ``in_place``."""
+def gac_rotary_sections(sections: Sequence[int], interleaved: bool = False):
+    """Which axis turns each pair of a head (a uint8 array, ``axes`` of the calls below), from the number of pairs of each
+    axis: one axis after the other, or dealt out in turn, where an axis whose pairs are used up is passed over."""
+    import numpy as np
+    left = [int(n) for n in sections]
+    if not 1 <= len(left) <= GAC_ROTARY_MAX_AXES or min(left) < 0:
+        raise ValueError(f"1..{GAC_ROTARY_MAX_AXES} axes, none with a negative number of pairs")
+    if not interleaved:
+        return np.repeat(np.arange(len(left)), left).astype(np.uint8)
+    # the r-th pair of axis a comes after all pairs of earlier rounds
+    return np.array([a for _, a in sorted((r, a) for a, n in enumerate(left) for r in range(n))], dtype=np.uint8)
+
+
+def _rotary_args(q, k, freqs, positions, cu_seqlens, axes, layout, scale, inverse, outputs, stream):
+    """Packed gac_rotary_args and gac_rotary_axes (or None) of one call, with what must stay alive until it; outputs: a
+    pair of tensors, or None for new contiguous ones."""
     import numpy as np
     dtype, device = q.dtype, q.device
     if dtype not in _DT:
@@ -679,32 +713,123 @@ def gac_rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Opt
     kx = k0 = k1 = kh = 0
     if k is not None:
         kx, k0, k1, kh = _heads(k, "k", q)
-    if (positions is None) == (cu_seqlens is None):
+    turns = freqs is not None
+    if (positions is None) == (cu_seqlens is None) and (turns or positions is not None):
         raise ValueError("give positions or cu_seqlens")
     tokens, _, dim = q.shape
-    if positions is not None and positions.numel() != tokens:
-        raise ValueError("one position per token")
+    if axes is None:
+        if positions is not None and positions.numel() != tokens:
+            raise ValueError("one position per token")
+        at = _int32_ptr(positions, "positions", device)
+    else:
+        if positions is None or not turns:
+            raise ValueError("axes need positions [axes, tokens] and frequencies")
+        if positions.dtype is not torch.int32 or positions.device != device or positions.dim() != 2 or \
+                (positions.stride(1) != 1 and tokens > 1):
+            raise ValueError("positions on axes must be an int32 tensor [axes, tokens] on the tensors' device, tokens contiguous")
+        if positions.shape[1] != tokens:
+            raise ValueError("one position per axis and token")
+        at = positions.data_ptr()
     if cu_seqlens is not None and cu_seqlens.numel() < 1:
         raise ValueError("cu_seqlens has one entry more than there are sequences")
-    if not (isinstance(freqs, np.ndarray) and freqs.dtype == np.float64 and freqs.flags.c_contiguous):
+    if turns and not (isinstance(freqs, np.ndarray) and freqs.dtype == np.float64 and freqs.flags.c_contiguous):
         freqs = np.ascontiguousarray(freqs, dtype=np.float64)
-    raw, stream = _on(stream, device)
-    if in_place:
-        yq, yk = q, k
-        qy, kout = (qx, q0, q1), (kx, k0, k1)
-    else:
+    on = None
+    if axes is not None:
+        axes = np.asarray(axes)
+        if axes.dtype != np.uint8 or not axes.flags.c_contiguous:
+            if axes.dtype.kind not in "iu" or (axes.size and (axes.min() < 0 or axes.max() > 255)):
+                raise ValueError("axes are whole numbers, one per pair")
+            axes = np.ascontiguousarray(axes, dtype=np.uint8)
+        if axes.size != freqs.size:
+            raise ValueError("one axis per pair")
+        on = _AXES.pack(axes.__array_interface__["data"][0], positions.stride(0), positions.shape[0], 0)
+    if outputs is None:
         yq = _empty(q, (tokens, qh, dim), stream)
         yk = _empty(q, (tokens, kh, dim), stream) if k is not None else None
         qy = (yq.data_ptr(), qh * dim, dim)
         kout = (yk.data_ptr(), kh * dim, dim) if k is not None else (0, 0, 0)
+    else:
+        yq, yk = outputs
+        qy, kout = (qx, q0, q1), (kx, k0, k1)
     args = _ROTARY.pack(qx, qy[0], q0, q1, qy[1], qy[2], kx, kout[0], k0, k1, kout[1], kout[2], qh, kh, tokens,
-                        0 if cu_seqlens is None else cu_seqlens.numel() - 1, dim, 2 * freqs.size, _DT[dtype],
-                        ROTARY_LAYOUTS[layout], 1 if inverse else 0, 0, _int32_ptr(positions, "positions", device),
-                        _int32_ptr(cu_seqlens, "cu_seqlens", device), freqs.__array_interface__["data"][0], scale)
-    _check(load_library().gac_rotary(args, device.index, raw))
+                        0 if cu_seqlens is None else cu_seqlens.numel() - 1, dim, 2 * freqs.size if turns else 0, _DT[dtype],
+                        ROTARY_LAYOUTS[layout], 1 if inverse else 0, 0, at,
+                        _int32_ptr(cu_seqlens, "cu_seqlens", device), freqs.__array_interface__["data"][0] if turns else 0, scale)
+    return args, on, (yq, yk), (freqs, axes)
+
+
+def gac_rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Optional[torch.Tensor] = None,
+               cu_seqlens: Optional[torch.Tensor] = None, layout: str = "half", scale: float = 1.0,
+               inverse: bool = False, in_place: bool = False, stream=None, axes=None):
+    """Rotary positions on q (and k, or None), [tokens, heads, head_dim] float32 or bfloat16 views.
+    ``freqs``: float64 radians per position (gac_rotary_freqs); it turns the first 2 * len(freqs) elements of
+    a head.  Positions are given, or follow from ``cu_seqlens``.  With ``axes`` (gac_rotary_sections, or one small
+    number per pair) a token has several: positions is [axes, tokens], and axes says which of them turns each pair.
+    Returns (q', k'): new contiguous tensors, or the given ones when ``in_place``."""
+    if freqs is None:
+        raise ValueError("freqs must be given")
+    raw, stream = _on(stream, q.device)
+    args, on, (yq, yk), keep = _rotary_args(q, k, freqs, positions, cu_seqlens, axes, layout, scale, inverse,
+                                            (q, k) if in_place else None, stream)
+    L = load_library()
+    _check(L.gac_rotary(args, q.device.index, raw) if on is None else L.gac_rotary_on_axes(args, on, q.device.index, raw))
     if in_place:   # autograd has to notice that what it may have saved has changed
         torch.autograd.graph.increment_version(q if k is None else (q, k))
     return yq, yk
+
+
+def _norm_args(q, q_weight, k_weight, eps, offset) -> bytes:
+    dtype = None
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is None:
+            continue
+        if w.dim() != 1 or w.numel() != q.shape[2] or w.device != q.device or (w.stride(0) != 1 and w.numel() > 1):
+            raise ValueError(f"{name} must be a contiguous vector of head_dim on the heads' device")
+        if w.dtype not in _DT or (dtype is not None and w.dtype is not dtype):
+            raise GacError(GAC_ERR_DTYPE, "weights are both float32 or both bfloat16")
+        dtype = w.dtype
+    return _NORM.pack(0 if q_weight is None else q_weight.data_ptr(), 0 if k_weight is None else k_weight.data_ptr(),
+                      _DT[dtype or torch.float32], 0, eps, offset)
+
+
+def gac_norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
+                    freqs, positions: Optional[torch.Tensor] = None, cu_seqlens: Optional[torch.Tensor] = None, axes=None,
+                    layout: str = "half", scale: float = 1.0, eps: float = 1e-6, offset: float = 0.0, in_place: bool = False,
+                    stream=None):
+    """Root mean square norm of every head of q and k (or None), times offset + weight, and the turn of gac_rotary, in one
+    pass.  Weights: [head_dim] float32 or bfloat16, or None for ones.  ``freqs=None`` turns nothing.  Returns (q', k')."""
+    raw, stream = _on(stream, q.device)
+    args, on, (yq, yk), keep = _rotary_args(q, k, freqs, positions, cu_seqlens, axes, layout, scale, False,
+                                            (q, k) if in_place else None, stream)
+    _check(load_library().gac_norm_rotary(args, on, _norm_args(q, q_weight, k_weight, eps, offset), q.device.index, raw))
+    if in_place:
+        torch.autograd.graph.increment_version(q if k is None else (q, k))
+    return yq, yk
+
+
+def gac_norm_rotary_backward(d_q: torch.Tensor, d_k: Optional[torch.Tensor], q: torch.Tensor, k: Optional[torch.Tensor],
+                             q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor], freqs,
+                             positions: Optional[torch.Tensor] = None, cu_seqlens: Optional[torch.Tensor] = None, axes=None,
+                             layout: str = "half", scale: float = 1.0, eps: float = 1e-6, offset: float = 0.0,
+                             weight_grads: bool = True, stream=None):
+    """Gradients (d_q, d_k, d_q_weight, d_k_weight) of gac_norm_rotary at q and k, given its results' gradients; new
+    contiguous tensors, None for what was None (or, without ``weight_grads``, for the weights)."""
+    L = load_library()
+    if (d_k is None) != (k is None) or d_q.shape != q.shape or (k is not None and d_k.shape != k.shape):
+        raise ValueError("the gradients must have the shapes of q and k")
+    qx, q0, q1, _ = _heads(q, "q", d_q)
+    kx, k0, k1, _ = _heads(k, "k", d_q) if k is not None else (0, 0, 0, 0)
+    raw, stream = _on(stream, q.device)
+    norm = _norm_args(q, q_weight, k_weight, eps, offset)
+    args, on, (yq, yk), keep = _rotary_args(d_q, d_k, freqs, positions, cu_seqlens, axes, layout, scale, False, None, stream)
+    wq, wk = (None if w is None or not weight_grads else _empty(w, (w.numel(),), stream) for w in (q_weight, k_weight))
+    need = max(L.gac_norm_rotary_workspace(args), 16)
+    workspace = _empty(q, (need,), stream, torch.uint8)
+    grad = _NORM_GRAD.pack(qx, q0, q1, kx, k0, k1, 0 if wq is None else wq.data_ptr(), 0 if wk is None else wk.data_ptr(),
+                           workspace.data_ptr(), need)
+    _check(L.gac_norm_rotary_backward(args, on, norm, grad, q.device.index, raw))
+    return yq, yk, wq, wk
 
 
 def _attn_args(q, k, v, o, lse, cu_seqlens, scale) -> bytes:

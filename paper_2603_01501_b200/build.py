@@ -7,10 +7,10 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("gac.cu", "clip.cu", "rotary.cu", "attention.cu")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("gac.cu", "clip.cu", "rotary.cu", "norm_rotary.cu", "attention.cu")]
 HEADERS = [os.path.join(ROOT, "include", "gac.h")] + \
           [os.path.join(HERE, "csrc", f) for f in ("gac_host.h", "faults.h", "overlap.h", "gac_kernels.cuh", "sm100.cuh",
-                                                 "attention_kernels.cuh")]
+                                                 "attention_kernels.cuh", "rotary.cuh")]
 LIB = os.path.join(HERE, "libgac_b200.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -4,7 +4,8 @@ A pack is a batch of finished rollouts of different lengths laid one behind the 
 [tokens, heads, head_dim] and ``cu_seqlens`` (int32 on the device), where sequence b takes the tokens
 cu_seqlens[b] .. cu_seqlens[b+1].
 
-    q, k = packed.rotary(q, k, freqs, cu_seqlens=cu)
+    q, k = packed.rotary(q, k, freqs, cu_seqlens=cu)                      # or, where heads are normed,
+    q, k = packed.norm_rotary(q, k, q_weight, k_weight, freqs, cu_seqlens=cu)
     o = packed.attention(q, k, v, cu)
     ...
     loss.backward()
@@ -27,19 +28,37 @@ from . import binding as gb
 
 class _Rotary(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, freqs, positions, cu_seqlens, layout, scale, inverse):
-        # positions and cu_seqlens are versioned like any saved tensor; of freqs the values of this call are kept
+    def forward(ctx, q, k, freqs, positions, cu_seqlens, layout, scale, inverse, axes):
+        # positions and cu_seqlens are versioned like any saved tensor; of freqs and axes the values of this call are kept
         ctx.save_for_backward(positions, cu_seqlens)
-        ctx.how = (np.array(freqs, dtype=np.float64), layout, scale, inverse)
-        return gb.gac_rotary(q, k, freqs, positions=positions, cu_seqlens=cu_seqlens, layout=layout, scale=scale, inverse=inverse)
+        ctx.how = (np.array(freqs, dtype=np.float64), layout, scale, inverse, None if axes is None else np.array(axes))
+        return gb.gac_rotary(q, k, freqs, positions=positions, cu_seqlens=cu_seqlens, layout=layout, scale=scale, inverse=inverse, axes=axes)
 
     @staticmethod
     def backward(ctx, d_q, d_k):
         positions, cu_seqlens = ctx.saved_tensors
-        freqs, layout, scale, inverse = ctx.how
+        freqs, layout, scale, inverse, axes = ctx.how
         # the transpose of a turn is the turn by the negative angle: itself a turn, so derivatives of any order go through
-        d_q, d_k = _Rotary.apply(_rows(d_q), None if d_k is None else _rows(d_k), freqs, positions, cu_seqlens, layout, scale, not inverse)
-        return d_q, d_k, None, None, None, None, None, None
+        d_q, d_k = _Rotary.apply(_rows(d_q), None if d_k is None else _rows(d_k), freqs, positions, cu_seqlens, layout, scale, not inverse, axes)
+        return d_q, d_k, None, None, None, None, None, None, None
+
+
+class _NormRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, freqs, positions, cu_seqlens, axes, layout, scale, eps, offset):
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions, cu_seqlens)
+        freqs = None if freqs is None else np.array(freqs, dtype=np.float64)
+        ctx.freqs, ctx.how = freqs, {"axes": None if axes is None else np.array(axes), "layout": layout, "scale": scale, "eps": eps, "offset": offset}
+        return gb.gac_norm_rotary(q, k, q_weight, k_weight, freqs, positions=positions, cu_seqlens=cu_seqlens, **ctx.how)
+
+    @staticmethod
+    @once_differentiable   # the library has no second derivative: asking for one raises
+    def backward(ctx, d_q, d_k):
+        q, k, q_weight, k_weight, positions, cu_seqlens = ctx.saved_tensors
+        grads = gb.gac_norm_rotary_backward(_rows(d_q), None if k is None else _rows(d_k), q, k, q_weight, k_weight, ctx.freqs,
+                                            positions=positions, cu_seqlens=cu_seqlens,
+                                            weight_grads=ctx.needs_input_grad[2] or ctx.needs_input_grad[3], **ctx.how)
+        return (*grads, None, None, None, None, None, None, None, None)
 
 
 class _Attention(torch.autograd.Function):
@@ -70,9 +89,17 @@ def _rows(t: torch.Tensor, multiple: int = 1) -> torch.Tensor:
 
 
 def rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Optional[torch.Tensor] = None,
-           cu_seqlens: Optional[torch.Tensor] = None, layout: str = "half", scale: float = 1.0):
+           cu_seqlens: Optional[torch.Tensor] = None, layout: str = "half", scale: float = 1.0, axes=None):
     """Rotary positions (binding.gac_rotary) with their derivatives of any order; returns (q', k')."""
-    return _Rotary.apply(q, k, freqs, positions, cu_seqlens, layout, scale, False)
+    return _Rotary.apply(q, k, freqs, positions, cu_seqlens, layout, scale, False, axes)
+
+
+def norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor], freqs,
+                positions: Optional[torch.Tensor] = None, cu_seqlens: Optional[torch.Tensor] = None, axes=None, layout: str = "half",
+                scale: float = 1.0, eps: float = 1e-6, offset: float = 0.0):
+    """Norms of the query and key heads with their rotation (binding.gac_norm_rotary) and the gradients of heads and weights
+    (first order alone: a second derivative raises); returns (q', k')."""
+    return _NormRotary.apply(q, k, q_weight, k_weight, freqs, positions, cu_seqlens, axes, layout, scale, eps, offset)
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, scale: Optional[float] = None,

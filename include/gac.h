@@ -660,6 +660,55 @@ size_t gac_norm_rotary_workspace(const gac_rotary_args *args);   /* 0 for a head
 int gac_norm_rotary_backward(const gac_rotary_args *args, const gac_rotary_axes *axes, const gac_norm *norm, const gac_norm_grad *grad,
                              int cuda_device, void *cuda_stream);
 
+/*
+ * Divergence of a policy from a teacher (or a reference policy) whose top logits are known, per token, and its gradient.
+ * Row t of `logits` has the policy's vocab logits, z = logits / temperature, q = softmax(z).  The teacher names up to
+ * `top` tokens of the row with ids and values; N is the set of them, "the rest" all other tokens taken as one:
+ *   TOP      p = softmax(teacher / temperature) over N, nothing is known of the rest:
+ *                L = sum_N p (log p - log q)
+ *   FORWARD  p = exp(teacher): log-probabilities at this temperature.  With p_r = max(1 - sum_N p, 2^-24) and
+ *            q_r = the rest's share of q,
+ *                L = sum_N p (log p - log q) + p_r (log p_r - log q_r)
+ *   REVERSE  as FORWARD, but the other way:
+ *                L = sum_N q (log q - log p) + q_r (log q_r - log p_r)
+ * Absent is an entry whose id is outside 0..vocab-1 or whose value is -infinity.  Of several entries with one id the first
+ * counts.  A row without entries has L = 0 and gradient 0 and its logits are not read.  0 log 0 = 0.  A rest without
+ * a logit above -1e38 (all masked, or none there) has no share: p_r is left out too.  Other non-finite values make their own row's
+ * results non-finite.
+ *
+ *   loss       [n_tokens] float32, or NULL
+ *   d_logits   weights[t] dL_t/dlogits, as wide as the logits, of their type, rounded once; or NULL.  It may be the
+ *              logits' own memory with the same stride.
+ *   weights    [n_tokens] float32, what L_t weighs; NULL: 1.  The loss is told unweighted.
+ * loss and d_logits in one call read the logits from memory once where a row stays in the cache; d_logits alone is the
+ * way back for an outer gradient.  No atomics on sums: two calls give the same bits.  Outputs must not overlap
+ * inputs otherwise.  Exponentials and sums over the vocabulary are binary32, what the named tokens and the whole row
+ * contribute binary64.
+ * Errors: INVALID_ARG, DTYPE, CUDA.
+ */
+#define GAC_DISTILL_MAX_VOCAB (1u << 20)
+#define GAC_DISTILL_MAX_TOP 1024
+typedef enum { GAC_DISTILL_TOP = 0, GAC_DISTILL_FORWARD = 1, GAC_DISTILL_REVERSE = 2 } gac_distill_kind;
+typedef struct {
+    const void *logits;           /* device [n_tokens][vocab], element-aligned, last dimension contiguous */
+    int64_t logits_row;           /* strides in elements                                       */
+    const int32_t *ids;           /* device [n_tokens][top]                                    */
+    int64_t ids_row;
+    const void *teacher;          /* device [n_tokens][top]                                    */
+    int64_t teacher_row;
+    const float *weights;         /* device [n_tokens], or NULL                                */
+    float *loss;                  /* device [n_tokens], or NULL                                */
+    void *d_logits;               /* device [n_tokens][vocab], or NULL                         */
+    int64_t d_row;
+    uint32_t n_tokens, vocab, top;   /* vocab 1..GAC_DISTILL_MAX_VOCAB, top 1..GAC_DISTILL_MAX_TOP */
+    int32_t dtype;                /* gac_dtype of logits and d_logits                          */
+    int32_t teacher_dtype;        /* gac_dtype                                                 */
+    int32_t kind;                 /* gac_distill_kind                                          */
+    double temperature;           /* 1e-3..1e3                                                 */
+    int64_t reserved;             /* must be 0                                                 */
+} gac_distill_args;
+int gac_distill(const gac_distill_args *args, int cuda_device, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -134,6 +134,18 @@ class gac_norm_grad(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t)]
 
 
+GAC_DISTILL_TOP, GAC_DISTILL_FORWARD, GAC_DISTILL_REVERSE = 0, 1, 2
+DISTILL_KINDS = {"top": GAC_DISTILL_TOP, "forward": GAC_DISTILL_FORWARD, "reverse": GAC_DISTILL_REVERSE}
+
+
+class gac_distill_args(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("logits_row", ctypes.c_int64), ("ids", ctypes.c_void_p), ("ids_row", ctypes.c_int64),
+                ("teacher", ctypes.c_void_p), ("teacher_row", ctypes.c_int64), ("weights", ctypes.c_void_p),
+                ("loss", ctypes.c_void_p), ("d_logits", ctypes.c_void_p), ("d_row", ctypes.c_int64), ("n_tokens", ctypes.c_uint32),
+                ("vocab", ctypes.c_uint32), ("top", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("teacher_dtype", ctypes.c_int32),
+                ("kind", ctypes.c_int32), ("temperature", ctypes.c_double), ("reserved", ctypes.c_int64)]
+
+
 EXPORTS = ["gac_default_hparams", "gac_init", "gac_stats", "gac_stats_partial", "gac_decide",
            "gac_project", "gac_free", "gac_last_error", "gac_set_launch", "gac_get_info",
            "gac_stats_static", "gac_default_adamw", "gac_attach_adamw", "gac_project_adamw",
@@ -142,7 +154,7 @@ EXPORTS = ["gac_default_hparams", "gac_init", "gac_stats", "gac_stats_partial", 
            "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_set_timeout", "gac_clip_free", "gac_rotary_freqs", "gac_rotary",
            "gac_attn_workspace",
            "gac_attn_forward", "gac_attn_backward", "gac_attn_check", "gac_rotary_on_axes", "gac_norm_rotary",
-           "gac_norm_rotary_workspace", "gac_norm_rotary_backward"]
+           "gac_norm_rotary_workspace", "gac_norm_rotary_backward", "gac_distill"]
 
 _lib = None
 
@@ -220,9 +232,10 @@ def load_library() -> ctypes.CDLL:
     L.gac_norm_rotary_workspace.argtypes = [vp]
     L.gac_norm_rotary_workspace.restype = ctypes.c_size_t
     L.gac_norm_rotary_backward.argtypes = [vp, vp, vp, vp, i32, vp]
+    L.gac_distill.argtypes = [vp, i32, vp]
     for name in ("gac_clip_init", "gac_clip_rebind", "gac_clip_sumsq", "gac_clip_apply", "gac_clip_grad_norm", "gac_clip_set_timeout",
                  "gac_clip_free", "gac_rotary_freqs", "gac_rotary", "gac_attn_forward", "gac_attn_backward", "gac_attn_check",
-                 "gac_rotary_on_axes", "gac_norm_rotary", "gac_norm_rotary_backward"):
+                 "gac_rotary_on_axes", "gac_norm_rotary", "gac_norm_rotary_backward", "gac_distill"):
         getattr(L, name).restype = i32
     for name in ("gac_init", "gac_stats", "gac_stats_partial", "gac_decide", "gac_project",
                  "gac_free", "gac_set_launch", "gac_get_info"):
@@ -514,6 +527,7 @@ _ROTARY = struct.Struct("=QQqqqqQQqqqqIIIIIIiiiiQQQd")
 _AXES = struct.Struct("=QqII")
 _NORM = struct.Struct("=QQiidd")
 _NORM_GRAD = struct.Struct("=QqqQqqQQQQ")
+_DISTILL = struct.Struct("=QqQqQqQQQqIIIiiidq")
 _ATTN = struct.Struct("=QqqQqqQqqQqqQQIIIIIifi")
 _ATTN_GRAD = struct.Struct("=QqqQqqQqqQqqQQ")
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
@@ -895,3 +909,37 @@ def gac_attn_check(device: Optional[int] = None, stream=None) -> None:
     out since this thread last asked on this stream."""
     dev = torch.device("cuda", torch.cuda.current_device() if device is None else device)
     _check(load_library().gac_attn_check(dev.index, _on(stream, dev)[0]))
+
+
+def gac_distill(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, kind: str = "top", temperature: float = 1.0,
+                weights: Optional[torch.Tensor] = None, grad: bool = False, in_place: bool = False, loss: bool = True, stream=None):
+    """Divergence of a policy from a teacher's top logits, per token.  logits [tokens, vocab] float32 or bfloat16, ids
+    [tokens, top] int32, teacher [tokens, top] float32 or bfloat16: logits for ``kind="top"``, log-probabilities for "forward" and
+    "reverse" (see gac.h).  Returns the loss [tokens] float32 or, with ``grad``, (loss, d_logits): weights[t] times the gradient of
+    token t's loss, in a new contiguous tensor or, ``in_place``, over the logits.  ``loss=False``: None in its place."""
+    if logits.dim() != 2 or not logits.is_cuda or ids.dim() != 2 or teacher.dim() != 2:
+        raise ValueError("logits must be a CUDA tensor [tokens, vocab], ids and teacher [tokens, top]")
+    tokens, vocab = logits.shape
+    device = logits.device
+    if ids.dtype is not torch.int32 or ids.device != device or teacher.device != device or ids.shape[0] != tokens or teacher.shape != ids.shape:
+        raise ValueError("ids must be int32, and ids and teacher [tokens, top] on the logits' device")
+    if logits.dtype not in _DT or teacher.dtype not in _DT:
+        raise GacError(GAC_ERR_DTYPE, f"unsupported dtype {logits.dtype} or {teacher.dtype}")
+    if (logits.stride(1) != 1 and vocab > 1) or ((ids.stride(1) != 1 or teacher.stride(1) != 1) and ids.shape[1] > 1):
+        raise ValueError("the last dimension must be contiguous")
+    if weights is not None and (weights.dtype is not torch.float32 or weights.device != device or weights.shape != (tokens,) or
+                                not weights.is_contiguous()):
+        raise ValueError("weights must be a contiguous float32 vector, one per token")
+    if in_place and not grad:
+        raise ValueError("only the gradient can be written in place")
+    raw, stream = _on(stream, device)
+    told = _empty(logits, (tokens,), stream, torch.float32) if loss else None
+    d = logits if in_place else _empty(logits, (tokens, vocab), stream) if grad else None
+    args = _DISTILL.pack(logits.data_ptr(), logits.stride(0), ids.data_ptr(), ids.stride(0), teacher.data_ptr(), teacher.stride(0),
+                         0 if weights is None else weights.data_ptr(), told.data_ptr() if loss else 0, 0 if d is None else d.data_ptr(),
+                         0 if d is None else d.stride(0), tokens, vocab, ids.shape[1], _DT[logits.dtype], _DT[teacher.dtype],
+                         DISTILL_KINDS[kind], temperature, 0)
+    _check(load_library().gac_distill(args, device.index, raw))
+    if in_place:
+        torch.autograd.graph.increment_version(logits)
+    return (told, d) if grad else told

@@ -7,7 +7,8 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("gac.cu", "clip.cu", "rotary.cu", "norm_rotary.cu", "attention.cu")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("gac.cu", "clip.cu", "rotary.cu", "norm_rotary.cu", "attention.cu",
+                                                       "distill.cu")]
 HEADERS = [os.path.join(ROOT, "include", "gac.h")] + \
           [os.path.join(HERE, "csrc", f) for f in ("gac_host.h", "faults.h", "overlap.h", "gac_kernels.cuh", "sm100.cuh",
                                                  "attention_kernels.cuh", "rotary.cuh")]

@@ -78,6 +78,21 @@ class _Attention(torch.autograd.Function):
         return d_q, d_k, d_v, None, None
 
 
+class _Distill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ids, teacher, kind, temperature):
+        ctx.save_for_backward(logits, ids, teacher)
+        ctx.how = (kind, temperature)
+        return gb.gac_distill(logits, ids, teacher, kind, temperature)
+
+    @staticmethod
+    @once_differentiable   # the library has no second derivative: asking for one raises
+    def backward(ctx, d_loss):
+        logits, ids, teacher = ctx.saved_tensors
+        _, d_logits = gb.gac_distill(logits, ids, teacher, *ctx.how, weights=d_loss.contiguous(), grad=True, loss=False)
+        return d_logits, None, None, None, None
+
+
 def _rows(t: torch.Tensor, multiple: int = 1) -> torch.Tensor:
     """A gradient as autograd hands it over may be expanded, transposed or off any boundary: the library wants
     contiguous rows on boundaries of `multiple` elements."""
@@ -108,6 +123,13 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: tor
     second derivative raises).  ``lse``, if asked for, has none."""
     o, lse = _Attention.apply(q, k, v, cu_seqlens, scale)
     return (o, lse) if return_lse else o
+
+
+def distillation(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, kind: str = "top", temperature: float = 1.0):
+    """Divergence of the policy from a teacher's top logits for every token (binding.gac_distill), with its gradient at the
+    logits (first order alone: a second derivative raises); the teacher gets none.  Nothing is kept for the way back but the arguments;
+    where the weight of every token's loss is known beforehand, binding.gac_distill gives loss and gradient in one pass."""
+    return _Distill.apply(logits, ids, teacher, kind, temperature)
 
 
 class GradientClipper:

@@ -672,7 +672,7 @@ int gac_norm_rotary_backward(const gac_rotary_args *args, const gac_rotary_axes 
  *   REVERSE  as FORWARD, but the other way:
  *                L = sum_N q (log q - log p) + q_r (log q_r - log p_r)
  * Absent is an entry whose id is outside 0..vocab-1 or whose value is -infinity.  Of several entries with one id the first
- * counts.  A row without entries has L = 0 and gradient 0 and its logits are not read.  0 log 0 = 0.  A rest without
+ * counts.  A row without entries has L = 0 and gradient 0 whatever its logits.  0 log 0 = 0.  A rest without
  * a logit above -1e38 (all masked, or none there) has no share: p_r is left out too.  Other non-finite values make their own row's
  * results non-finite.
  *
@@ -680,13 +680,12 @@ int gac_norm_rotary_backward(const gac_rotary_args *args, const gac_rotary_axes 
  *   d_logits   weights[t] dL_t/dlogits, as wide as the logits, of their type, rounded once; or NULL.  It may be the
  *              logits' own memory with the same stride.
  *   weights    [n_tokens] float32, what L_t weighs; NULL: 1.  The loss is told unweighted.
- * loss and d_logits in one call read the logits from memory once where a row stays in the cache; d_logits alone is the
- * way back for an outer gradient.  No atomics on sums: two calls give the same bits.  Outputs must not overlap
- * inputs otherwise.  Exponentials and sums over the vocabulary are binary32, what the named tokens and the whole row
+ * loss and d_logits in one call read the logits from memory once; d_logits alone is the way back for an outer gradient.  No atomics on sums: two calls give the same bits (the loss told
+ * without a gradient and beside one may differ in the last).  Outputs must not overlap inputs otherwise.  Exponentials and sums over the vocabulary are binary32, what the named tokens and the whole row
  * contribute binary64.
  * Errors: INVALID_ARG, DTYPE, CUDA.
  */
-#define GAC_DISTILL_MAX_VOCAB (1u << 20)
+#define GAC_DISTILL_MAX_ROW_BYTES 1310720   /* 655360 bfloat16 or 327680 float32 logits */
 #define GAC_DISTILL_MAX_TOP 1024
 typedef enum { GAC_DISTILL_TOP = 0, GAC_DISTILL_FORWARD = 1, GAC_DISTILL_REVERSE = 2 } gac_distill_kind;
 typedef struct {
@@ -700,7 +699,7 @@ typedef struct {
     float *loss;                  /* device [n_tokens], or NULL                                */
     void *d_logits;               /* device [n_tokens][vocab], or NULL                         */
     int64_t d_row;
-    uint32_t n_tokens, vocab, top;   /* vocab 1..GAC_DISTILL_MAX_VOCAB, top 1..GAC_DISTILL_MAX_TOP */
+    uint32_t n_tokens, vocab, top;   /* vocab 1.. as above, top 1..GAC_DISTILL_MAX_TOP */
     int32_t dtype;                /* gac_dtype of logits and d_logits                          */
     int32_t teacher_dtype;        /* gac_dtype                                                 */
     int32_t kind;                 /* gac_distill_kind                                          */

@@ -10,8 +10,15 @@
 //                                                                                                    q (d_r - L) elsewhere
 // Every gradient outside N is exp(z) times a number of the row, so a row needs its maximum and sum outside N in one pass
 // and, for the gradient, one product and one exponential per element in another.  Sums outside N are taken without the
-// named tokens, which a bitmap in shared memory marks (a byte to a vector of 16 bytes): as a difference of two sums a
-// small rest would be lost.  What has to do with the few named tokens, and the row's own numbers, is binary64.
+// named tokens, which are overwritten with -infinity before: as a difference of two sums a small rest would be lost.
+// What has to do with the few named tokens, and the row's own numbers, is binary64.
+//
+// One CTA to a row, or, where rows are few or long, a cluster of up to eight that exchange what they know of their parts
+// through distributed shared memory.  The second pass reads the row again, backwards and out of L2: rows are loaded with
+// evict-last, read again and written with evict-first, and cut into so many parts that the rows in use fit.  Loads go through a
+// ring in shared memory, because what bounds the kernel is bytes in flight beside the chain from a row's last load to its first
+// gradient (sums over the CTA, exponentials and logarithms in binary64, about 5 us), which the SM's other CTAs have to cover.
+// Measured: @.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 #include <float.h>
@@ -24,13 +31,20 @@
 #include "gac.h"
 #include "gac_host.h"
 #include "overlap.h"
+#include "sm100.cuh"
 
 namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+// Threads of a CTA, CTAs of an SM, and the ring: groups of vectors that a thread loads at once.
+template <bool GRAD>
+struct Shape {
+    static constexpr int kThreads = GRAD ? 256 : 384, kCtas = GRAD ? 4 : 3, kWarps = kThreads / 32;
+    static constexpr int kFlight = GRAD ? 3 : 4, kRing = GRAD ? 4 : 2, kRingBytes = kRing * kFlight * kThreads * 16;
+};
 constexpr uint32_t kMaxSplit = 8;      // CTAs of a row: a portable cluster
+constexpr uint64_t kInUse = 96u << 20; // bytes of rows in use at once, of 126 MB of L2
 constexpr float kMasked = -1e38f;      // tokens with no logit above this are taken as masked
 
 struct DistillDev {
@@ -43,354 +57,492 @@ struct DistillDev {
     int teacher_bf16, kind;
     float *loss;
     const float *weights;
-    uint32_t vocab, top, split;
-    float c;                           // log2(e) / temperature
+    uint32_t vocab, top, split, mark_words;
+    float c;                           // log2(e) / temperature, rounded;
+    double c_off;                      // what it lacks, times log(2)
     double inv_temp;
 };
 
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(uint16_t x) { return __uint_as_float(uint32_t(x) << 16); }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 __device__ __forceinline__ float from_float(float x, float) { return x; }
-__device__ __forceinline__ uint16_t from_float(float x, uint16_t) { return uint16_t(pack_bf16(x, 0.f) & 0xFFFFu); }
+__device__ __forceinline__ uint16_t from_float(float x, uint16_t) { return uint16_t(bf16x2(x, 0.f) & 0xFFFFu); }
 
 // 16 bytes of a row.
 template <typename T>
 struct Vector {
     static constexpr int N = 16 / int(sizeof(T));
-    __device__ static __forceinline__ void unpack(const uint4 &x, float (&v)[N]) {
+    static constexpr uint32_t kNone = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;   // -infinity throughout
+    __device__ static __forceinline__ void unpack(const uint4 &x, float2 (&v)[N / 2]) {
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            v[i] = sizeof(T) == 4 ? __uint_as_float(w[i % 4]) : __uint_as_float(i & 1 ? w[i / 2 % 4] & 0xFFFF0000u : w[i / 2 % 4] << 16);
+        for (int i = 0; i < N / 2; ++i)
+            v[i] = sizeof(T) == 4 ? make_float2(__uint_as_float(w[2 * i % 4]), __uint_as_float(w[(2 * i + 1) % 4]))
+                                  : make_float2(__uint_as_float(w[i % 4] << 16), __uint_as_float(w[i % 4] & 0xFFFF0000u));
     }
-    __device__ static __forceinline__ uint4 pack(const float (&v)[N]) {
+    __device__ static __forceinline__ uint4 pack(const float2 (&v)[N / 2]) {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? __float_as_uint(v[i % N]) : pack_bf16(v[2 * i % N], v[(2 * i + 1) % N]);
+        for (int i = 0; i < 4; ++i)
+            w[i] = sizeof(T) == 4 ? __float_as_uint(i & 1 ? v[i / 2].y : v[i / 2].x) : bf16x2(v[i % (N / 2)].x, v[i % (N / 2)].y);
         return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    // the larger of two vectors, element by element, NaN where both are; and the largest element, -FLT_MAX at least
+    __device__ static __forceinline__ uint4 larger(const uint4 &a, const uint4 &b) {
+        return make_uint4(two(a.x, b.x), two(a.y, b.y), two(a.z, b.z), two(a.w, b.w));
+    }
+    __device__ static __forceinline__ float largest(const uint4 &a) {
+        const uint32_t w = two(two(a.x, a.y), two(a.z, a.w));
+        if (sizeof(T) == 4) return fmaxf(__uint_as_float(w), -FLT_MAX);
+        return fmaxf(fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)), -FLT_MAX);
+    }
+    // -infinity in the place of the marked elements
+    __device__ static __forceinline__ uint4 without(const uint4 &x, uint32_t marked) {
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (marked >> i & 1u) {
+                if (sizeof(T) == 4) w[i % 4] = kNone;
+                else w[i / 2 % 4] = i & 1 ? (w[i / 2 % 4] & 0xFFFFu) | 0xFF800000u : (w[i / 2 % 4] & 0xFFFF0000u) | 0xFF80u;
+            }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ static __forceinline__ uint32_t two(uint32_t a, uint32_t b) {
+        uint32_t r;
+        if (sizeof(T) == 4) asm("max.f32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        else asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
     }
 };
 
-// What a CTA knows of its part of the row.
+// Sums of exponentials are kept as multiples of 2^level, level a whole number, so that they are brought together exactly.
+__device__ __forceinline__ float level_of(float m, float c) { return rintf(fminf(fmaxf(m * c, -FLT_MAX), FLT_MAX)); }
+__device__ __forceinline__ double power_of_two(float whole) {   // 0 or less
+    return whole < -1000.0f ? 0.0 : __hiloint2double((1023 + int(whole)) << 20, 0);
+}
+// What a CTA, or a warp, knows of its part of the row.
 struct Partial {
-    double mass, cost;          // top: sum of e, of e (log e - z); else: sum of p, of p (log p - z) or, reverse, unused
-    double named, named_cost;   // sum over named tokens of exp(z - m_named), of exp(z - m_named) (z - log p)
-    float m_named, m, s;        // largest logit of named tokens; largest and sum of exp of the others'
+    double mass, cost;          // top: sum of e, of e (log e - z); else: sum of p, of p (log p - z)
+    double named, named_cost;   // sum over named tokens of exp(z), of exp(z) (z - log p), in units of 2^level
+    float level;
+    float m, s;                 // of the others the largest logit, and the sum of exp(z) in units of 2^level_of(m)
 };
 // What the gradient needs of the whole row.
 struct Row {
-    double m, log_total, mass_scale, add, loss, weight;   // see finish()
-    float m_rest, others;
+    double lse, total;          // log q = z - lse; the sum of exp(z) in units of 2^unit
+    double q_scale, p_scale;    // of a named token's q and p (top, forward)
+    double loss, weight;
+    float unit;
+    float level, others;        // elsewhere: 2^(logit c - level) others
 };
 
-__device__ __forceinline__ double add_lanes(double x) {
+template <typename F>
+__device__ __forceinline__ F add_lanes(F x, int from) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+    for (int o = from; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
     return x;
 }
-__device__ __forceinline__ float max_lanes(float x) {
+__device__ __forceinline__ float max_lanes(float x, int from) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+    for (int o = from; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
     return x;
+}
+// No part at all.
+__device__ __forceinline__ Partial no_part() {
+    Partial p = {};
+    p.m = p.level = -FLT_MAX;
+    return p;
+}
+// The sum of `n` parts, a power of two, one to a lane of every n, in all lanes.
+__device__ __forceinline__ Partial add_parts(Partial p, const DistillDev &a, int n) {
+    const float m = max_lanes(p.m, n / 2), level = max_lanes(p.level, n / 2);
+    p.s = add_lanes(p.s * exp2_approx(level_of(p.m, a.c) - level_of(m, a.c)), n / 2);
+    const double f = power_of_two(p.level - level);
+    p.mass = add_lanes(p.mass, n / 2);
+    p.cost = add_lanes(p.cost, n / 2);
+    p.named = add_lanes(p.named * f, n / 2);
+    p.named_cost = add_lanes(p.named_cost * f, n / 2);
+    p.m = m;
+    p.level = level;
+    return p;
 }
 
-// The row's numbers from its parts, by one thread, parts in their order.  `top_teacher`: largest value of the teacher.
-__device__ void finish(const DistillDev &a, const Partial *parts, uint32_t n, double weight, Row *out) {
-    double mass = 0.0, cost = 0.0, named = 0.0, named_cost = 0.0, s = 0.0;
-    float m_rest = -FLT_MAX, m_named = -FLT_MAX;
-    for (uint32_t i = 0; i < n; ++i) {
-        m_rest = fmaxf(m_rest, parts[i].m);
-        m_named = fmaxf(m_named, parts[i].m_named);
-    }
-    for (uint32_t i = 0; i < n; ++i) {
-        mass += parts[i].mass;
-        cost += parts[i].cost;
-        s += double(parts[i].s) * exp((double(parts[i].m) - double(m_rest)) * a.inv_temp);
-        const double f = exp((double(parts[i].m_named) - double(m_named)) * a.inv_temp);
-        named += parts[i].named * f;
-        named_cost += parts[i].named_cost * f;
-    }
-    const bool rest = m_rest > kMasked || s != s;   // a NaN is not masked
-    const double m = fmax(double(m_named), rest ? double(m_rest) : -double(FLT_MAX));
-    const double f_named = exp((double(m_named) - m) * a.inv_temp), f_rest = rest ? exp((double(m_rest) - m) * a.inv_temp) : 0.0;
-    const double total = named * f_named + (rest ? s * f_rest : 0.0);
-    const double log_total = log(total), scale = weight * a.inv_temp;
-    const double lse = m * a.inv_temp + log_total;
-    const double q_rest = rest ? s * f_rest / total : 0.0;
-    double others = 0.0;   // q_rest times the gradient's factor outside N
-    out->m = m;
-    out->log_total = log_total;
-    out->weight = scale;
+// The row's numbers from the sum of its parts, by a whole warp: what the gradient outside N needs first (`rest` and `s` for the rest).
+struct Sums {
+    double s, f_rest, f_named, p_rest;
+    bool rest;
+};
+__device__ __forceinline__ Sums start(const DistillDev &a, const Partial &p, Row &r) {
+    Sums x;
+    x.rest = p.m > kMasked || p.s != p.s;   // a NaN is not masked
+    r.level = level_of(p.m, a.c);
+    r.unit = x.rest ? fmaxf(p.level, r.level) : p.level;
+    x.f_rest = x.rest ? power_of_two(r.level - r.unit) : 0.0;
+    x.f_named = power_of_two(p.level - r.unit);
+    // powers were taken of logit c, and c is rounded: near the largest logit they are off by this
+    const double off = double(p.m) * a.c_off;
+    x.s = !x.rest ? 0.0 : double(p.s) * (fabs(off) < 0.01 ? 1.0 + off * (1.0 + off * (0.5 + off * (1.0 / 6.0))) : exp(off));
+    const double total = p.named * x.f_named + x.s * x.f_rest;
+    r.total = total < double(INFINITY) ? total : double(NAN);
+    x.p_rest = fmax(1.0 - p.mass, 1.0 / 16777216.0);
+    return x;
+}
+__device__ __forceinline__ float factor(double others, const Sums &x, const Partial &p, const Row &r) {
+    return x.rest ? float(others) / p.s * float(r.weight) : 0.0f;
+}
+__device__ __forceinline__ void finish_gradient(const DistillDev &a, const Partial &p, const Sums &x, Row &r) {   // top, forward
+    const double q_rest = x.s * x.f_rest / r.total;
+    const bool top = a.kind == GAC_DISTILL_TOP;
+    r.q_scale = top ? 1.0 : p.mass + (x.rest ? x.p_rest : 0.0);
+    r.p_scale = top ? 1.0 / p.mass : 1.0;
+    r.others = factor(top ? q_rest : r.q_scale * q_rest - x.p_rest, x, p, r);
+}
+__device__ __forceinline__ void finish_loss(const DistillDev &a, const Partial &p, const Sums &x, Row &r) {
+    const uint32_t all = 0xFFFFFFFFu, which = threadIdx.x & 3;
+    const double l = log(which == 0 ? r.total : which == 1 ? x.s : which == 2 ? x.p_rest : p.mass);
+    const double log_total = __shfl_sync(all, l, 0), log_s = __shfl_sync(all, l, 1), log_p_rest = __shfl_sync(all, l, 2), log_mass = __shfl_sync(all, l, 3);
+    r.lse = double(r.unit) * M_LN2 + log_total;
+    const double log_q_rest = x.rest ? double(r.level - r.unit) * M_LN2 + log_s - log_total : 0.0;
     if (a.kind == GAC_DISTILL_TOP) {
-        out->loss = cost / mass - log(mass) + lse;
-        out->mass_scale = 1.0;
-        out->add = 1.0 / mass;
-        others = q_rest;
+        r.loss = p.cost / p.mass - log_mass + r.lse;
+    } else if (a.kind == GAC_DISTILL_FORWARD) {
+        r.loss = p.cost + p.mass * r.lse + (x.rest ? x.p_rest * (log_p_rest - log_q_rest) : 0.0);
     } else {
-        const double p_rest = fmax(1.0 - mass, 1.0 / 16777216.0);
-        const double log_q_rest = rest ? (double(m_rest) - m) * a.inv_temp + log(s) - log_total : 0.0;
-        if (a.kind == GAC_DISTILL_FORWARD) {
-            const double w = mass + (rest ? p_rest : 0.0);
-            out->loss = cost + mass * lse + (rest ? p_rest * (log(p_rest) - log_q_rest) : 0.0);
-            out->mass_scale = w;
-            out->add = 1.0;
-            others = rest ? w * q_rest - p_rest : 0.0;
-        } else {
-            const double d_rest = rest ? log_q_rest - log(p_rest) : 0.0;
-            out->loss = f_named / total * (named_cost - lse * named) + q_rest * d_rest;
-            out->mass_scale = 0.0;
-            out->add = 0.0;
-            others = q_rest * (d_rest - out->loss);
-        }
+        const double q_rest = x.s * x.f_rest / r.total, d_rest = x.rest ? log_q_rest - log_p_rest : 0.0;
+        r.loss = x.f_named / r.total * (p.named_cost - r.lse * p.named) + q_rest * d_rest;
+        r.others = factor(q_rest * (d_rest - r.loss), x, p, r);
     }
-    out->m_rest = m_rest;
-    out->others = rest ? float(others / s * scale) : 0.0f;
+}
+
+// One CTA's part of a row.
+struct Span {
+    const char *z;              // place 0; element v of the row is at place v + off, 16 bytes make a vector
+    uint32_t off, end;          // places off .. end - 1 are the row's
+    uint32_t vectors, lo, hi;   // the row's vectors; this part's
+    uint32_t whole_lo, whole_hi;   // those of this part that are whole: the row's first and last may not be
+};
+template <typename T>
+__device__ __forceinline__ Span span_of(const DistillDev &a, uint32_t t, uint32_t part) {
+    constexpr uint32_t N = Vector<T>::N;
+    Span s;
+    const char *z = a.z + (long long)t * a.z_row;
+    s.off = uint32_t(reinterpret_cast<uint64_t>(z) / sizeof(T)) % N;
+    s.z = z - s.off * sizeof(T);
+    s.end = a.vocab + s.off;
+    s.vectors = (s.end + N - 1) / N;
+    const uint32_t per = (s.vectors + a.split - 1) / a.split;
+    s.lo = min(part * per, s.vectors);
+    s.hi = min(s.lo + per, s.vectors);
+    s.whole_lo = max(s.lo, s.off ? 1u : 0u);
+    s.whole_hi = min(s.hi, s.end / N);
+    return s;
 }
 
 template <typename T, bool GRAD>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(Shape<GRAD>::kThreads, Shape<GRAD>::kCtas)
 distill_kernel(const __grid_constant__ DistillDev a) {
     using Vec = Vector<T>;
-    constexpr int N = Vec::N, kFlight = 4;
+    using C = Shape<GRAD>;
+    constexpr int N = Vec::N, kThreads = C::kThreads, kWarps = C::kWarps, kFlight = C::kFlight, kRing = C::kRing;
+    constexpr uint32_t kNowhere = 0xFFFFFFFFu;
     extern __shared__ __align__(16) char dynamic[];
-    __shared__ Partial parts[kMaxSplit];
-    __shared__ Partial warp_part[kWarps];
+    __shared__ Partial parts[kMaxSplit], warp_part[kWarps];
     __shared__ Row row;
-    __shared__ float warp_max[2][kWarps];
+    __shared__ float warp_most[kWarps];
     __shared__ int repeated;
 
-    const uint32_t part = a.split == 1 ? 0 : blockIdx.x % a.split, t = blockIdx.x / a.split;
+    const uint32_t part = blockIdx.x % a.split, t = blockIdx.x / a.split;
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, top = a.top;
-    // per named token: p, or e of it; its logit, what the teacher says, which it is
-    double *e_p = reinterpret_cast<double *>(dynamic);
-    float *e_z = reinterpret_cast<float *>(e_p + top), *e_l = e_z + top;
-    int *e_id = reinterpret_cast<int *>(e_l + top);
-    uint32_t *marks = reinterpret_cast<uint32_t *>(e_id + top);
-
-    const char *z = a.z + (long long)t * a.z_row;
-    char *dz = GRAD ? a.dz + (long long)t * a.dz_row : nullptr;
-    // the row in vectors of 16 bytes: element v is at place v + off
-    const uint32_t off = uint32_t(reinterpret_cast<uint64_t>(z) / sizeof(T)) % N;
-    const uint32_t vectors = (a.vocab + off + N - 1) / N, per = (vectors + a.split - 1) / a.split;
-    const uint32_t lo = min(part * per, vectors), hi = min(lo + per, vectors);
-    const uint32_t first = max(lo * N, off) - off, last = max(min(hi * N, a.vocab + off), off) - off;   // elements of this part
-    // vectors that are whole: the row's first and last may not be
-    const uint32_t whole_lo = max(lo, off ? 1u : 0u), whole_hi = min(hi, (a.vocab + off) / N);
-    auto mark_of = [&](uint32_t vector) { return reinterpret_cast<const uint8_t *>(marks)[vector - lo]; };
-
-    for (uint32_t i = threadIdx.x; i < (hi - lo + 3) / 4; i += kThreads) marks[i] = 0;
+    const Span sp = span_of<T>(a, t, part);
+    const uint32_t ring = smem_addr(dynamic) + threadIdx.x * 16;
+    // per named token: p, or e of it; its exp(z); its logit, what the teacher says, its place in the row (none: not of this part, or
+    // absent); then a byte to a vector, a bit to an element: which are named
+    double *e_p = reinterpret_cast<double *>(dynamic + C::kRingBytes), *e_q = e_p + top;
+    float *e_z = reinterpret_cast<float *>(e_q + top), *e_l = e_z + top;
+    uint32_t *e_at = reinterpret_cast<uint32_t *>(e_l + top), *marks = e_at + top;
+    for (uint32_t i = threadIdx.x; i < a.mark_words; i += kThreads) marks[i] = 0;
     if (threadIdx.x == 0) repeated = 0;
-    __syncthreads();
 
+    const uint32_t groups = sp.whole_hi > sp.whole_lo ? (sp.whole_hi - sp.whole_lo + kFlight * kThreads - 1) / (kFlight * kThreads) : 0;
+    // A thread's own vectors pass through a ring in shared memory, kRing groups of kFlight of them, and no other thread sees them.
+    uint64_t first, drop;   // values alone: a row is read once
+    if (GRAD) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(first));
+    else asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(first));
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(drop));
+    auto issue = [&](uint32_t group, uint32_t from, uint64_t policy) {
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) {
+            const uint32_t j = sp.whole_lo + threadIdx.x + (from * kFlight + u) * kThreads;
+            if (from < groups && j < sp.whole_hi)
+                asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(ring + ((group % kRing) * kFlight + u) * (kThreads * 16)),
+                             "l"(reinterpret_cast<const uint4 *>(sp.z) + j), "l"(policy) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto take = [&](uint32_t group, uint4 (&x)[kFlight]) {   // the oldest group
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[u].x), "=r"(x[u].y), "=r"(x[u].z), "=r"(x[u].w)
+                         : "r"(ring + ((group % kRing) * kFlight + u) * (kThreads * 16)) : "memory");
+    };
+    // elements of a vector that is not whole, by one thread each
+    auto edge = [&](auto each) {
+        if (threadIdx.x >= 2 * N || sp.lo >= sp.hi) return;
+        const uint32_t vector = threadIdx.x < N ? 0 : sp.vectors - 1, place = vector * N + threadIdx.x % N;
+        if (vector < sp.lo || vector >= sp.hi || (vector >= sp.whole_lo && vector < sp.whole_hi) || (threadIdx.x >= N && sp.vectors == 1)) return;
+        if (place >= sp.off && place < sp.end) each(place);
+    };
+    auto said = [&](uint32_t i, int &id, float &l) {
+        id = a.ids[(long long)t * a.ids_row + i];
+        const long long at = (long long)t * a.teacher_row + i;
+        l = a.teacher_bf16 ? as_float(reinterpret_cast<const uint16_t *>(a.teacher)[at]) : reinterpret_cast<const float *>(a.teacher)[at];
+    };
+    const float2 c2 = make_float2(a.c, a.c);
+    int id0 = -1;     // the thread's first entry, on its way early
+    float l0 = 0.f;
+    if (threadIdx.x < top) said(threadIdx.x, id0, l0);
+#pragma unroll
+    for (int g = 0; g < kRing; ++g) issue(g, g, first);
+    __syncthreads();
     // ---- what the teacher names
     bool any = false;
-    float most = -INFINITY, m_named = -FLT_MAX;
+    float most = -INFINITY, z0 = 0.f;
     for (uint32_t i = threadIdx.x; i < top; i += kThreads) {
-        int id = a.ids[(long long)t * a.ids_row + i];
-        const long long at = (long long)t * a.teacher_row + i;
-        const float l = a.teacher_bf16 ? as_float(reinterpret_cast<const uint16_t *>(a.teacher)[at]) : reinterpret_cast<const float *>(a.teacher)[at];
-        if (id < 0 || uint32_t(id) >= a.vocab || l == -INFINITY) id = -1;
-        e_id[i] = id;
-        e_l[i] = l;
-        if (id < 0) continue;
-        any = true;
-        most = l > most || l != l ? l : most;
-        if (uint32_t(id) >= first && uint32_t(id) < last) {
-            const float x = as_float(reinterpret_cast<const T *>(z)[id]);
-            e_z[i] = x;
-            m_named = fmaxf(m_named, x);
-            const uint32_t place = uint32_t(id) + off - lo * N;   // from the start of this part
-            const uint32_t bit = 1u << (place / N % 4 * 8 + place % N);
-            if (atomicOr(marks + place / N / 4, bit) & bit) repeated = 1;
+        int id = id0;
+        float l = l0;
+        if (i >= kThreads) said(i, id, l);
+        uint32_t place = kNowhere;
+        if (id >= 0 && uint32_t(id) < a.vocab && l != -INFINITY) {
+            any = true;
+            most = fmaxf(most, l);
+            place = uint32_t(id) + sp.off;
+            if (place >= sp.lo * N && place < sp.hi * N) {
+                const float z = as_float(reinterpret_cast<const T *>(sp.z)[place]);
+                if (i < kThreads) z0 = z;   // not waited for yet
+                else e_z[i] = z;
+                const uint32_t bit = 1u << ((place / N - sp.lo) % 4 * 8 + place % N);
+                if (atomicOr(marks + (place / N - sp.lo) / 4, bit) & bit) repeated = 1;
+            } else {
+                place = kNowhere;
+            }
         }
+        e_at[i] = place;
+        e_l[i] = l;
     }
+    most = max_lanes(most, 16);
+    if (lane == 0) warp_most[warp] = most;
     any = __syncthreads_or(any);
-    const float weight = a.weights ? a.weights[t] : 1.0f;
-    if (!any) {   // nothing to compare with: the row is not read
-        if (a.loss && part == 0 && threadIdx.x == 0) a.loss[t] = 0.0f;
-        if (GRAD)
-            for (uint32_t v = first + threadIdx.x; v < last; v += kThreads) reinterpret_cast<T *>(dz)[v] = T(0);
-        return;
-    }
-    if (a.split > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");   // this CTA has started
+    if (any && a.split > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");   // this CTA has started
     if (repeated) {   // of several with the same token the first counts
         for (uint32_t i = threadIdx.x; i < top; i += kThreads) {
-            const int id = e_id[i];
-            bool again = false;
-            for (uint32_t j = 0; id >= 0 && j < i; ++j) again |= e_id[j] == id;
-            e_p[i] = again ? 1.0 : 0.0;
+            const uint32_t at = e_at[i];
+            bool seen = false;
+            for (uint32_t j = 0; at != kNowhere && j < i; ++j) seen |= e_at[j] == at;
+            e_p[i] = seen ? 1.0 : 0.0;
         }
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < top; i += kThreads)
-            if (e_p[i] != 0.0) e_id[i] = -1;
-    }
-    most = max_lanes(most);
-    m_named = max_lanes(m_named);
-    if (lane == 0) {
-        warp_max[0][warp] = most;
-        warp_max[1][warp] = m_named;
-    }
-    __syncthreads();
-    for (int i = 0; i < kWarps; ++i) {
-        most = fmaxf(most, warp_max[0][i]);
-        m_named = fmaxf(m_named, warp_max[1][i]);
-    }
-    Partial mine = {};
-    for (uint32_t i = threadIdx.x; i < top; i += kThreads) {
-        const int id = e_id[i];
-        if (id < 0 || uint32_t(id) < first || uint32_t(id) >= last) continue;
-        const double x = double(e_z[i]) * a.inv_temp;
-        const double l = a.kind == GAC_DISTILL_TOP ? (double(e_l[i]) - double(most)) * a.inv_temp : double(e_l[i]);
-        const double p = exp(l), q = exp((double(e_z[i]) - double(m_named)) * a.inv_temp);
-        e_p[i] = p;
-        mine.mass += p;
-        mine.cost += p > 0.0 ? p * (l - x) : p;     // 0 log 0 = 0; a NaN stays one
-        mine.named += q;
-        mine.named_cost += q > 0.0 ? q * (x - l) : q;
+            if (e_p[i] != 0.0) e_at[i] = kNowhere;
     }
 
-    // ---- largest logit and sum of exponentials of all others
-    float m = -FLT_MAX, s = 0.0f;
-    auto take = [&](float (&v)[N], uint32_t marked) {
-        if (marked) {
+    float named_level = -FLT_MAX;
+    if (any) {
+        // ---- largest logit and sum of exponentials of all others
+        float m = -FLT_MAX, level = level_of(m, a.c);
+        float2 s = make_float2(0.f, 0.f);
+        auto raise = [&](float next) {
+            const float next_level = level_of(next, a.c), f = exp2_approx(level - next_level);
+            s = mul2(s, make_float2(f, f));
+            m = next;
+            level = next_level;
+        };
+        auto add = [&](const uint4 &y) {
+            float2 v[N / 2];
+            Vec::unpack(y, v);
+            const float2 minus = make_float2(-level, -level);
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (marked >> i & 1u) v[i] = -INFINITY;
-        }
-    };
-    auto add = [&](const float (&v)[N]) {
-        float sum = 0.0f;
+            for (int i = 0; i < N / 2; ++i) {
+                v[i] = fma2(v[i], c2, minus);
+                v[i] = make_float2(exp2_approx(v[i].x), exp2_approx(v[i].y));
+            }
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum += exp2_fast((v[i] - m) * a.c);
-        s += sum;
-    };
-    auto raise = [&](float top_of) {
-        const float next = fmaxf(m, top_of);
-        s *= exp2_fast((m - next) * a.c);
-        m = next;
-    };
-    const uint4 *zv = reinterpret_cast<const uint4 *>(z - (long long)off * (long long)sizeof(T));
-    for (uint32_t j = whole_lo + threadIdx.x; j < whole_hi; j += kFlight * kThreads) {
-        uint4 x[kFlight];
+            for (int w = N / 4; w > 0; w /= 2)
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u)
-            if (j + u * kThreads < whole_hi) x[u] = __ldcg(zv + j + u * kThreads);
+                for (int i = 0; i < w; ++i) v[i] = add2(v[i], v[i + w]);
+            s = add2(s, v[0]);
+        };
+        const uint8_t *mark = reinterpret_cast<const uint8_t *>(marks) - sp.lo;
+        for (uint32_t g = 0; g < groups; ++g) {
+            uint4 x[kFlight];
+            take(g, x);
+            issue(g + kRing, g + kRing, first);
+            const uint32_t j = sp.whole_lo + threadIdx.x + g * (kFlight * kThreads);
+            if (j + (kFlight - 1) * kThreads < sp.whole_hi) {
+                uint32_t marked[kFlight], some = 0;
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u) {
-            if (j + u * kThreads >= whole_hi) break;
-            float v[N], best = -FLT_MAX;
-            Vec::unpack(x[u], v);
-            take(v, mark_of(j + u * kThreads));
+                for (int u = 0; u < kFlight; ++u) some |= marked[u] = mark[j + u * kThreads];
+                if (some) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) best = fmaxf(best, v[i]);
-            raise(best);
-            add(v);
-        }
-    }
-    // a vector of the row that is not whole: its elements, by one thread each
-    auto edge = [&](auto each) {
-        const uint32_t head = min(whole_lo * N > off ? whole_lo * N - off : 0u, last), tail = max(whole_hi * N > off ? whole_hi * N - off : 0u, head);
-        if (first + threadIdx.x < head) each(first + threadIdx.x);
-        if (tail + threadIdx.x < last) each(tail + threadIdx.x);
-    };
-    auto marked_element = [&](uint32_t v) { return mark_of((v + off) / N) >> ((v + off) % N) & 1u; };
-    edge([&](uint32_t v) {
-        if (marked_element(v)) return;
-        const float x = as_float(reinterpret_cast<const T *>(z)[v]);
-        raise(x);
-        s += exp2_fast((x - m) * a.c);
-    });
-    const float m_all = max_lanes(m);
-    s *= exp2_fast((m - m_all) * a.c);
+                    for (int u = 0; u < kFlight; ++u) x[u] = Vec::without(x[u], marked[u]);
+                }
+                uint4 big = x[0];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    mine.mass = add_lanes(mine.mass);
-    mine.cost = add_lanes(mine.cost);
-    mine.named = add_lanes(mine.named);
-    mine.named_cost = add_lanes(mine.named_cost);
-    mine.m = m_all;
-    mine.s = s;
-    if (lane == 0) warp_part[warp] = mine;
-    __syncthreads();
-    if (a.split > 1) asm volatile("barrier.cluster.wait;" ::: "memory");             // all have: their memory may be written
-    if (threadIdx.x == 0) {
-        Partial sum = warp_part[0];
-        for (int i = 1; i < kWarps; ++i) sum.m = fmaxf(sum.m, warp_part[i].m);
-        sum.s = 0.0f;
-        for (int i = 0; i < kWarps; ++i) sum.s += warp_part[i].s * exp2_fast((warp_part[i].m - sum.m) * a.c);
-        for (int i = 1; i < kWarps; ++i) {
-            sum.mass += warp_part[i].mass;
-            sum.cost += warp_part[i].cost;
-            sum.named += warp_part[i].named;
-            sum.named_cost += warp_part[i].named_cost;
-        }
-        sum.m_named = m_named;
-        if (a.split == 1) {
-            parts[0] = sum;
-        } else {   // to all parts of the row
-            cg::cluster_group cluster = cg::this_cluster();
-            for (uint32_t i = 0; i < a.split; ++i) *cluster.map_shared_rank(&parts[part], i) = sum;
-        }
-    }
-    if (a.split > 1) cg::this_cluster().sync();
-    if (threadIdx.x == 0) {
-        Row r;
-        finish(a, parts, a.split, double(weight), &r);
-        if (a.loss && part == 0) a.loss[t] = float(r.loss);
-        row = r;
-    }
-    if (!GRAD) return;
-    __syncthreads();
-
-    // ---- gradient
-    const float m_rest = row.m_rest, others = row.others;
-    auto grad = [&](float x) { return exp2_fast((x - m_rest) * a.c) * others; };
-    const bool aligned = (reinterpret_cast<uint64_t>(dz) - reinterpret_cast<uint64_t>(z)) % 16 == 0;
-    for (uint32_t j = whole_lo + threadIdx.x; j < whole_hi; j += kFlight * kThreads) {
-        uint4 x[kFlight];
+                for (int u = 1; u < kFlight; ++u) big = Vec::larger(big, x[u]);
+                raise(fmaxf(m, Vec::largest(big)));
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u)
-            if (j + u * kThreads < whole_hi) x[u] = __ldcs(zv + j + u * kThreads);
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u) {
-            if (j + u * kThreads >= whole_hi) break;
-            float v[N];
-            Vec::unpack(x[u], v);
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = grad(v[i]);
-            const uint32_t at = (j + u * kThreads) * N - off;
-            if (aligned) {
-                *reinterpret_cast<uint4 *>(dz + (long long)at * (long long)sizeof(T)) = Vec::pack(v);
+                for (int u = 0; u < kFlight; ++u) add(x[u]);
             } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i) reinterpret_cast<T *>(dz)[at + i] = from_float(v[i], T{});
+                for (int u = 0; u < kFlight - 1; ++u)
+                    if (j + u * kThreads < sp.whole_hi) {
+                        const uint4 y = Vec::without(x[u], mark[j + u * kThreads]);
+                        raise(fmaxf(m, Vec::largest(y)));
+                        add(y);
+                    }
+            }
+        }
+        edge([&](uint32_t place) {
+            if (reinterpret_cast<const uint8_t *>(marks)[place / N - sp.lo] >> (place % N) & 1u) return;
+            const float v = as_float(reinterpret_cast<const T *>(sp.z)[place]), next = fmaxf(m, v), next_level = level_of(next, a.c);
+            const float f = exp2_approx(level - next_level);
+            s = make_float2(s.x * f + exp2_approx(fmaf(v, a.c, -next_level)), s.y * f);
+            m = next;
+            level = next_level;
+        });
+        if (GRAD) {   // on its way meanwhile
+#pragma unroll
+            for (int g = 0; g < kRing; ++g) issue(g, groups - 1 - g, drop);
+        }
+        most = max_lanes(warp_most[lane % kWarps], 16);
+        Partial mine = {};
+        float m_named = -FLT_MAX;
+        for (uint32_t i = threadIdx.x; i < top; i += kThreads)
+            if (e_at[i] != kNowhere) {
+                if (i < kThreads) e_z[i] = z0;
+                m_named = fmaxf(m_named, e_z[i]);
+            }
+        named_level = mine.level = level_of(max_lanes(m_named, 16), a.c);
+        for (uint32_t i = threadIdx.x; i < top; i += kThreads) {
+            if (e_at[i] == kNowhere) continue;
+            const double z = double(e_z[i]) * a.inv_temp, says = e_l[i];
+            const double log_p = a.kind == GAC_DISTILL_TOP ? (says - double(most)) * a.inv_temp : says;
+            const double p = exp(log_p), q = exp(z - double(named_level) * M_LN2);
+            e_p[i] = p;
+            e_q[i] = q;
+            mine.mass += p;
+            mine.cost += p > 0.0 ? p * (log_p - z) : p;     // 0 log 0 = 0; a NaN stays one
+            mine.named += q;
+            mine.named_cost += q > 0.0 ? q * (z - log_p) : q;
+        }
+        if (__any_sync(0xFFFFFFFFu, mine.named != 0.0 || mine.mass != 0.0)) {
+            mine.mass = add_lanes(mine.mass, 16);
+            mine.cost = add_lanes(mine.cost, 16);
+            mine.named = add_lanes(mine.named, 16);
+            mine.named_cost = add_lanes(mine.named_cost, 16);
+        }
+        mine.m = max_lanes(m, 16);
+        mine.s = add_lanes((s.x + s.y) * exp2_approx(level - level_of(mine.m, a.c)), 16);
+        if (lane == 0) warp_part[warp] = mine;
+        __syncthreads();
+        // ---- the row's numbers
+        Partial sum;
+        if (warp == 0) sum = add_parts(lane < kWarps ? warp_part[lane] : no_part(), a, 32);
+        if (a.split > 1) {
+            asm volatile("barrier.cluster.wait;" ::: "memory");   // all have started: their memory may be written
+            if (warp == 0) {
+                if (lane < a.split) *cg::this_cluster().map_shared_rank(&parts[part], lane) = sum;
+                asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+            } else {
+                asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+            }
+            asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+            if (warp == 0) {
+                sum = add_parts(lane % kMaxSplit < a.split ? parts[lane % kMaxSplit] : no_part(), a, kMaxSplit);
+            }
+        }
+        Row r;
+        Sums more;
+        if (warp == 0) {
+            r.weight = (a.weights ? double(a.weights[t]) : 1.0) * a.inv_temp;
+            more = start(a, sum, r);
+            if (a.kind == GAC_DISTILL_REVERSE) finish_loss(a, sum, more, r);
+            else finish_gradient(a, sum, more, r);
+            if (lane == 0) row = r;
+        }
+        if (GRAD) __syncthreads();
+        if (warp == 0 && a.loss && part == 0) {
+            if (a.kind != GAC_DISTILL_REVERSE) finish_loss(a, sum, more, r);
+            if (lane == 0) a.loss[t] = float(r.loss);
+        }
+    } else if (a.loss && part == 0 && threadIdx.x == 0) {
+        a.loss[t] = 0.0f;   // nothing to compare with
+    }
+
+    // ---- gradient, from the row's end to its beginning: what was read last is in L2 for certain
+    if (GRAD) {
+        char *dz = a.dz + (long long)t * a.dz_row - sp.off * sizeof(T);   // place 0
+        const bool aligned = reinterpret_cast<uint64_t>(dz) % 16 == 0;
+        auto put = [&](uint32_t j, const uint4 &y) {   // a whole vector
+            if (aligned) {
+                __stcs(reinterpret_cast<uint4 *>(dz) + j, y);
+            } else {
+                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    if (sizeof(T) == 4) reinterpret_cast<uint32_t *>(dz)[j * N + i] = w[i % 4];
+                    else reinterpret_cast<uint16_t *>(dz)[j * N + i] = uint16_t(w[i / 2 % 4] >> (i % 2 * 16));
+                }
+            }
+        };
+        if (any) {
+            const float others = row.others, level = row.level;
+            const float2 minus = make_float2(-level, -level), by = make_float2(others, others);
+            auto gradient = [&](const uint4 &y) {
+                float2 v[N / 2];
+                Vec::unpack(y, v);
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) {
+                    v[i] = fma2(v[i], c2, minus);
+                    v[i] = mul2(make_float2(exp2_approx(v[i].x), exp2_approx(v[i].y)), by);
+                }
+                return Vec::pack(v);
+            };
+            for (uint32_t g = 0; g < groups; ++g) {
+                uint4 x[kFlight];
+                take(g, x);
+                issue(g + kRing, groups - 1 - g - kRing, drop);
+                const uint32_t j = sp.whole_lo + threadIdx.x + (groups - 1 - g) * (kFlight * kThreads);
+                if (aligned && j + (kFlight - 1) * kThreads < sp.whole_hi) {
+#pragma unroll
+                    for (int u = 0; u < kFlight; ++u) __stcs(reinterpret_cast<uint4 *>(dz) + j + u * kThreads, gradient(x[u]));
+                } else {
+#pragma unroll
+                    for (int u = 0; u < kFlight; ++u)
+                        if (j + u * kThreads < sp.whole_hi) put(j + u * kThreads, gradient(x[u]));
+                }
+            }
+            edge([&](uint32_t place) {
+                const float v = as_float(reinterpret_cast<const T *>(sp.z)[place]);
+                reinterpret_cast<T *>(dz)[place] = from_float(exp2_approx(fmaf(v, a.c, -level)) * others, T{});
+            });
+        } else {
+            for (uint32_t j = sp.whole_lo + threadIdx.x; j < sp.whole_hi; j += kThreads) put(j, make_uint4(0, 0, 0, 0));
+            edge([&](uint32_t place) { reinterpret_cast<T *>(dz)[place] = T(0); });
+        }
+        if (any) {
+            __syncthreads();   // the named tokens' own gradients over what has been written
+            const double f = power_of_two(named_level - row.unit);
+            for (uint32_t i = threadIdx.x; i < top; i += kThreads) {
+                if (e_at[i] == kNowhere) continue;
+                const double q = e_q[i] * f / row.total;
+                double g = q * row.q_scale - e_p[i] * row.p_scale;
+                if (a.kind == GAC_DISTILL_REVERSE) g = q == 0.0 ? 0.0 : q * (double(e_z[i]) * a.inv_temp - row.lse - double(e_l[i]) - row.loss);
+                reinterpret_cast<T *>(dz)[e_at[i]] = from_float(float(g * row.weight), T{});
             }
         }
     }
-    edge([&](uint32_t v) { reinterpret_cast<T *>(dz)[v] = from_float(grad(as_float(reinterpret_cast<const T *>(z)[v])), T{}); });
-    __syncthreads();   // the named tokens' own gradients over what has been written
-    for (uint32_t i = threadIdx.x; i < top; i += kThreads) {
-        const int id = e_id[i];
-        if (id < 0 || uint32_t(id) < first || uint32_t(id) >= last) continue;
-        const double log_q = (double(e_z[i]) - row.m) * a.inv_temp - row.log_total, q = exp(log_q);
-        double g;
-        if (a.kind == GAC_DISTILL_REVERSE) {
-            g = q == 0.0 ? 0.0 : q * (log_q - double(e_l[i]) - row.loss);
-        } else {
-            g = q * row.mass_scale - e_p[i] * row.add;
-        }
-        reinterpret_cast<T *>(dz)[id] = from_float(float(g * row.weight), T{});
-    }
+    asm volatile("cp.async.wait_all;" ::: "memory");   // of a row without entries the first loads may still be on their way
 }
 
 int fail(std::nullptr_t, int code, const char *fmt, const char *a = "", long long b = 0) {
@@ -411,7 +563,8 @@ int gac_distill(const gac_distill_args *args, int cuda_device, void *cuda_stream
     if (a.reserved != 0) return fail(nullptr, GAC_ERR_INVALID_ARG, "reserved must be 0%s");
     if (!(a.temperature > 0.0) || !isfinite(a.temperature) || !(a.temperature >= 1e-3 && a.temperature <= 1e3))
         return fail(nullptr, GAC_ERR_INVALID_ARG, "temperature must be 1e-3..1e3%s");
-    if (a.vocab < 1 || a.vocab > GAC_DISTILL_MAX_VOCAB) return fail(nullptr, GAC_ERR_INVALID_ARG, "vocab must be 1..%s%lld", "", (long long)GAC_DISTILL_MAX_VOCAB);
+    if (a.vocab < 1 || a.vocab > GAC_DISTILL_MAX_ROW_BYTES / (a.dtype == GAC_BF16 ? 2 : 4))
+        return fail(nullptr, GAC_ERR_INVALID_ARG, "vocab must be at least 1, and its logits of a row at most %s%lld bytes", "", (long long)GAC_DISTILL_MAX_ROW_BYTES);
     if (a.top < 1 || a.top > GAC_DISTILL_MAX_TOP) return fail(nullptr, GAC_ERR_INVALID_ARG, "top must be 1..%s%lld", "", GAC_DISTILL_MAX_TOP);
     if (a.n_tokens > (1u << 27)) return fail(nullptr, GAC_ERR_INVALID_ARG, "n_tokens out of range%s");
     if (a.n_tokens == 0) return GAC_OK;
@@ -460,21 +613,29 @@ int gac_distill(const gac_distill_args *args, int cuda_device, void *cuda_stream
     d.top = a.top;
     d.inv_temp = 1.0 / a.temperature;
     d.c = float(M_LOG2E / a.temperature);
-    // Few rows are split over a cluster, as long as a part has some thousands of elements.
+    d.c_off = (M_LOG2E / a.temperature - double(d.c)) * M_LN2;
+    const uint32_t vec = 16 / uint32_t(size), vectors = (a.vocab + 2 * vec - 2) / vec;   // at most, wherever a row starts
+    // Parts of a row: so many that the rows in use at once, of all resident CTAs, stay in L2 between the two passes (4096 rows
+    // of 304 kB: 505 us with one part, 451 with two, whose CTAs wait for each other; 8191 rows of 128 kB: 323 and 367), and
+    // that few rows still use all SMs, as long as a part has some thousands of elements.
+    const bool grad = a.d_logits != nullptr;
+    const uint32_t resident = 148 * (grad ? Shape<true>::kCtas : Shape<false>::kCtas);
     d.split = 1;
-    while (d.split < kMaxSplit && uint64_t(a.n_tokens) * d.split < 148 * 4 && a.vocab / (2 * d.split) >= 4096) d.split *= 2;
-    const uint32_t vec = 16 / uint32_t(size), vectors = (a.vocab + 2 * vec - 2) / vec, per = (vectors + d.split - 1) / d.split;
-    const size_t smem = size_t(a.top) * 20 + (per + 3) / 4 * 4;
+    while (d.split < kMaxSplit && ((grad && uint64_t(resident / d.split) * a.vocab * size > kInUse) ||
+                                   (uint64_t(a.n_tokens) * d.split < resident && a.vocab / (2 * d.split) >= 4096)))
+        d.split *= 2;
+    d.mark_words = ((vectors + d.split - 1) / d.split + 3) / 4;
+    const size_t smem = size_t(grad ? Shape<true>::kRingBytes : Shape<false>::kRingBytes) + size_t(a.top) * 28 + size_t(d.mark_words) * 4;
     Range range("gac_distill");
     DeviceGuard guard(cuda_device);
     if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
     void (*fn)(const DistillDev) = nullptr;
-    if (a.dtype == GAC_BF16) fn = a.d_logits ? distill_kernel<uint16_t, true> : distill_kernel<uint16_t, false>;
-    else fn = a.d_logits ? distill_kernel<float, true> : distill_kernel<float, false>;
-    if (smem > 40 * 1024) GAC_CUDA(nullptr, cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+    if (a.dtype == GAC_BF16) fn = grad ? distill_kernel<uint16_t, true> : distill_kernel<uint16_t, false>;
+    else fn = grad ? distill_kernel<float, true> : distill_kernel<float, false>;
+    GAC_CUDA(nullptr, cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
     cudaLaunchConfig_t how = {};
     how.gridDim = dim3(a.n_tokens * d.split);
-    how.blockDim = dim3(kThreads);
+    how.blockDim = dim3(grad ? Shape<true>::kThreads : Shape<false>::kThreads);
     how.dynamicSmemBytes = smem;
     how.stream = static_cast<cudaStream_t>(cuda_stream);
     cudaLaunchAttribute attr[1];

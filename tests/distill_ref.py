@@ -8,7 +8,9 @@ numbers are binary64 in the kernel, so what is off comes from the sum over the r
 Together es of the rest's sum, relative.  It moves the loss by es G with G = the sum of the loss's gradient over the rest
 (q_r, W q_r - p_r, q_r (d_r - L)), doubled for what is of second order.  1 - sum p is a difference of binary64 numbers: off by dp = 2^-50
 (2 + K), which moves log p_r by dp / p_r.
-Gradients are off by the same, with q, their own exponentials and the rounding at the end."""
+Gradients are off by the same, with q, their own exponentials and the rounding at the end.  A named token's q and p are each
+an exponential in binary64 (2^-52 of it) over a sum of such: with the quotient and the products under 8 2^-52, so their difference
+is off by 2^-49 (q W + p) on top, which shows where the two agree to the last digit of binary32."""
 import math
 
 import torch
@@ -62,7 +64,7 @@ def distill(logits, ids, teacher, kind, temperature, weights=None):
             p = lp.exp()
             value, w, G = float(term(p, lp - lq_at).sum()), 1.0, qr
             g_at, dG = q - p, qr * es
-            g_at_b = q * qr * es
+            g_at_b = q * qr * es + 2.0 ** -49 * (q + p)
         else:
             p = lp.exp()
             pr = max(1.0 - float(p.sum()), 2.0 ** -24)
@@ -72,7 +74,7 @@ def distill(logits, ids, teacher, kind, temperature, weights=None):
                 value = float(term(p, lp - lq_at).sum()) + (pr * (math.log(pr) - float(lr)) if rest else 0.0)
                 G = w * qr - pr if rest else 0.0
                 g_at, dG = q * w - p, w * qr * es + dp * pr
-                g_at_b = q * w * qr * es + q * dp * pr
+                g_at_b = q * w * qr * es + q * dp * pr + 2.0 ** -49 * (q * w + p)
                 dp *= pr * (1 + abs(math.log(pr) - float(lr))) if rest else 0.0
             else:
                 d, dr = lq_at - lp, (float(lr) - math.log(pr)) if rest else 0.0
@@ -82,6 +84,7 @@ def distill(logits, ids, teacher, kind, temperature, weights=None):
                 move = 2 * es * (abs(G) + es) + dp * qr
                 dG = qr * (es * (abs(dr - value) + 2) + dp + move)
                 g_at_b = q * (qr * es * ((d - value).abs().nan_to_num(0.0) + 1) + move)
+                g_at_b += 2.0 ** -49 * term(q, lq_at.abs() + lp.abs() + abs(value) + 1)
                 dp *= qr
         loss[t] = value
         loss_b[t] = 2 * es * (abs(G) + es) + dp + 2 * U * abs(value)

@@ -35,7 +35,8 @@ def check(x, ids, values, kind, temperature=1.0, weights=None):
     loss = gb.gac_distill(x, ids, values, kind, temperature)
     within(loss, *want["loss"], "loss")
     loss2, grad = gb.gac_distill(x, ids, values, kind, temperature, weights=weights, grad=True)
-    assert torch.equal(loss, loss2) and torch.equal(x.nan_to_num(7.0), keep.nan_to_num(7.0)) and grad.dtype is x.dtype
+    within(loss2, *want["loss"], "loss beside the gradient")     # another order of the same sum
+    assert torch.equal(x.nan_to_num(7.0), keep.nan_to_num(7.0)) and grad.dtype is x.dtype
     within(grad, *want["grad"], "grad")
     none, again = gb.gac_distill(x, ids, values, kind, temperature, weights=weights, grad=True, loss=False)
     assert none is None and torch.equal(grad, again)

@@ -26,6 +26,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstddef>
 
 #include "gac.h"
@@ -45,6 +46,9 @@ struct Shape {
 };
 constexpr uint32_t kMaxSplit = 8;      // CTAs of a row: a portable cluster
 constexpr uint64_t kInUse = 96u << 20; // bytes of rows in use at once, of 126 MB of L2
+// The ring, the most named tokens, and marks: a byte to 16 bytes of a row, or, where it is split, of an eighth of it.
+constexpr size_t kMaxSmem = Shape<false>::kRingBytes + GAC_DISTILL_MAX_TOP * 28 + GAC_DISTILL_MAX_ROW_BYTES / 16 + 16;
+static_assert(kMaxSmem <= 224 * 1024 && Shape<true>::kRingBytes <= Shape<false>::kRingBytes, "fits an SM");
 constexpr float kMasked = -1e38f;      // tokens with no logit above this are taken as masked
 
 struct DistillDev {
@@ -632,7 +636,12 @@ int gac_distill(const gac_distill_args *args, int cuda_device, void *cuda_stream
     void (*fn)(const DistillDev) = nullptr;
     if (a.dtype == GAC_BF16) fn = grad ? distill_kernel<uint16_t, true> : distill_kernel<uint16_t, false>;
     else fn = grad ? distill_kernel<float, true> : distill_kernel<float, false>;
-    GAC_CUDA(nullptr, cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+    static std::atomic<bool> allowed[4][64];   // once for each device
+    std::atomic<bool> *done = cuda_device < 64 ? &allowed[(grad ? 2 : 0) + (a.dtype == GAC_BF16)][cuda_device] : nullptr;
+    if (!done || !*done) {
+        GAC_CUDA(nullptr, cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxSmem)));
+        if (done) *done = true;
+    }
     cudaLaunchConfig_t how = {};
     how.gridDim = dim3(a.n_tokens * d.split);
     how.blockDim = dim3(grad ? Shape<true>::kThreads : Shape<false>::kThreads);

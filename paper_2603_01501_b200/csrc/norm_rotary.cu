@@ -14,217 +14,263 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "gac.h"
 #include "gac_host.h"
 #include "rotary.cuh"
+#include "sm100.cuh"
 
 namespace {
 
 constexpr uint32_t kMaxDim = 1024, kMaxVectorDim = 256;
-constexpr uint32_t kShares = 148 * 8;   // most CTAs of the way back, each with a share of the weights' gradients
+constexpr int kForwardCtas = 5, kBackCtas = 4;   // of an SM
+constexpr uint32_t kShares = 148 * kBackCtas;    // most CTAs of the way back for one kind of heads, each with a share of the weights' gradient
+constexpr uint32_t kFew = 1u << 18;              // elements of all heads: about one place for each thread of all SMs
+constexpr int kRing = 3;                         // heads that a thread has loads of on their way
 
 struct NormDev {
     const char *w[2];                 // nullptr: ones, without offset
     int w_bf16;
     float eps, offset, inv_dim;
     uint32_t group;                   // lanes of a head: a power of two
+    uint32_t ctas_q;                  // CTAs that take query heads; the others take key heads
+    uint32_t split[2];                // a token's heads are dealt out to so many groups of lanes
+    long long x_token[2], x_head[2], y_token[2], y_head[2];   // RotaryDev's strides in bytes
+    long long x_step[2], y_step[2], v_step[2];                // and from a head to the next one of the same lanes
     // the way back: RotaryDev's x is d_y, its y is d_x
     const char *v[2];                 // the heads that went in
-    long long v_token[2], v_head[2];
-    float *shares;                    // [CTAs][queries, keys][head_dim]
+    long long v_token[2], v_head[2];  // bytes
+    float *shares;                    // [CTAs][head_dim]: of query heads, then of key heads
 };
 
 __device__ __forceinline__ float weight_at(const NormDev &n, int which, uint32_t i) {
     if (!n.w[which]) return 1.0f;
     return n.offset + (n.w_bf16 ? load_el(n.w[which] + i * 2, uint16_t{}) : load_el(n.w[which] + i * 4, float{}));
 }
-__device__ __forceinline__ void fill_weights(const RotaryDev &a, const NormDev &n, float *w) {
-    for (uint32_t i = threadIdx.x; i < 2 * a.head_dim; i += kThreads) w[i] = weight_at(n, i >= a.head_dim, i >= a.head_dim ? i - a.head_dim : i);
-}
 __device__ __forceinline__ float add_lanes(float x, uint32_t group) {
-    for (uint32_t o = group / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+#pragma unroll
+    for (uint32_t o = 1; o < 32; o *= 2)
+        if (o < group) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
     return x;
 }
 
-// A thread's place in a head: elements 0..3 start at `first`, 4..7 at `second`.
+// A thread's place in a head: N elements from `first`, N from `second`, so that the lanes of a head read and write one behind the
+// other.  The two are the elements of N pairs, or N / 2 pairs each, or not turned.
 struct Part {
     uint32_t u, first, second;
     bool here, turn, both;
 };
-template <bool HALF>
+template <int N>
 __device__ __forceinline__ Part part_of(const RotaryDev &a, const NormDev &n) {
-    const uint32_t turned = a.pairs / 4, units = turned + (a.head_dim - 2 * a.pairs + 7) / 8;
+    const uint32_t turned = a.pairs / N, rest = (a.head_dim - 2 * a.pairs) / N, places = turned + (rest + 1) / 2;
     Part p;
     p.u = threadIdx.x & (n.group - 1);
-    p.here = p.u < units;
+    p.here = p.u < places;
     p.turn = p.u < turned;
-    p.first = p.turn ? (HALF ? p.u * 4 : p.u * 8) : 2 * a.pairs + (p.u - turned) * 8;
-    p.second = p.first + (p.turn && HALF ? a.pairs : 4);
+    p.first = p.turn ? p.u * N : 2 * a.pairs + (p.u - turned) * N;
+    p.second = p.first + (p.turn ? a.pairs : (rest + 1) / 2 * N);
     p.both = p.here && (p.turn || p.second < a.head_dim);
     return p;
 }
-template <typename T>
-struct Eight {
-    Vec<T, 4> p, q;
-    __device__ __forceinline__ void load(const char *row, const Part &at) {
-        if (at.here) p.load(row + at.first * sizeof(T));
-        if (at.both) q.load(row + at.second * sizeof(T));
-    }
-    __device__ __forceinline__ void get(float (&v)[8], const Part &at) const {
+// N elements of a place, two to a number, out of 8 or 16 bytes of shared memory, and into as many of global memory.
+template <typename T, int N>
+__device__ __forceinline__ void take(uint32_t from, float2 *v) {
+    Vec<T, N> p;
+    constexpr int kWords = Vec<T, N>::kWords;
+    if (kWords == 4)
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(p.w[0]), "=r"(p.w[1]), "=r"(p.w[kWords - 2]), "=r"(p.w[kWords - 1]) : "r"(from) : "memory");
+    else
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(p.w[0]), "=r"(p.w[1]) : "r"(from) : "memory");
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[j] = at.here ? p.get(j) : 0.f;
-            v[4 + j] = at.both ? q.get(j) : 0.f;
-        }
-    }
-    __device__ __forceinline__ void put(const float (&v)[8], char *row, const Part &at) {
-        p.put2(0, v[0], v[1]);
-        p.put2(2, v[2], v[3]);
-        q.put2(0, v[4], v[5]);
-        q.put2(2, v[6], v[7]);
-        if (at.here) p.store(row + at.first * sizeof(T));
-        if (at.both) q.store(row + at.second * sizeof(T));
-    }
-};
-__device__ __forceinline__ void eight_floats(float (&v)[8], const float *row, const Part &at) {
-    const float4 x = *reinterpret_cast<const float4 *>(row + (at.here ? at.first : 0));
-    const float4 y = *reinterpret_cast<const float4 *>(row + (at.both ? at.second : 0));
-    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-    v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+    for (int j = 0; j < N; j += 2) v[j / 2] = make_float2(p.get(j), p.get(j + 1));
 }
-// The place's four pairs by their angles, or by the negative ones.
-template <bool HALF, bool BACK>
-__device__ __forceinline__ void turn(float (&v)[8], const float2 *wheel, const Part &at) {
-    if (!at.turn) return;
-    const float4 *cs = reinterpret_cast<const float4 *>(wheel + at.u * 4);
+template <typename T, int N>
+__device__ __forceinline__ void put(char *to, const float2 *v) {
+    Vec<T, N> p;
 #pragma unroll
-    for (int m = 0; m < 4; m += 2) {
-        const float4 c = cs[m / 2];   // cosine, sine, cosine, sine
-        const int i0 = HALF ? m : 2 * m, j0 = HALF ? m + 4 : 2 * m + 1, i1 = HALF ? m + 1 : 2 * m + 2, j1 = HALF ? m + 5 : 2 * m + 3;
-        const float s0 = BACK ? -c.y : c.y, s1 = BACK ? -c.w : c.w;
-        const float x0 = v[i0], y0 = v[j0], x1 = v[i1], y1 = v[j1];
-        v[i0] = x0 * c.x - y0 * s0;
-        v[j0] = x0 * s0 + y0 * c.x;
-        v[i1] = x1 * c.z - y1 * s1;
-        v[j1] = x1 * s1 + y1 * c.z;
+    for (int j = 0; j < N; j += 2) p.put2(j, v[j / 2].x, v[j / 2].y);
+    p.store(to);
+}
+// (x, y) -> (a x - b y, c x + d y) on a place's N pairs; `minus_b` has the sign already.  v: two elements each, as they lie in the head.
+template <int N, bool HALF>
+__device__ __forceinline__ void turn(float2 (&v)[N], const float2 *a, const float2 *minus_b, const float2 *c, const float2 *d) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        if (HALF) {
+            const float2 x = v[i], y = v[N / 2 + i];
+            v[i] = fma2(x, a[i], mul2(y, minus_b[i]));
+            v[N / 2 + i] = fma2(x, c[i], mul2(y, d[i]));
+        } else {
+            const float2 p = v[2 * i], q = v[2 * i + 1];
+            v[2 * i] = make_float2(fmaf(p.x, a[i].x, p.y * minus_b[i].x), fmaf(p.x, c[i].x, p.y * d[i].x));
+            v[2 * i + 1] = make_float2(fmaf(q.x, a[i].y, q.y * minus_b[i].y), fmaf(q.x, c[i].y, q.y * d[i].y));
+        }
     }
 }
 
-template <typename T, bool HALF>
-__global__ void __launch_bounds__(kThreads, 8)
+// The first ctas_q CTAs take query heads, the others key heads.  The lanes that share a head keep to one token, with its sines in
+// registers, and go through every `split`-th of its heads; what a thread will need next is on its way into its own places of a
+// ring in shared memory.  No two threads share anything but the sums over a head, and on the way back the last sum over the CTA.
+template <typename T, int N, bool HALF, bool BACK>
+__global__ void __launch_bounds__(kThreads, BACK ? kBackCtas : kForwardCtas)
 norm_rotary_kernel(const __grid_constant__ RotaryDev a, const __grid_constant__ NormDev n) {
-    constexpr int kFlight = 2;
-    __shared__ __align__(16) float2 wheel[GAC_ROTARY_MAX_DIM / 2];
-    __shared__ __align__(16) float weights[2 * kMaxVectorDim];
-    const uint32_t t = blockIdx.x, step = kThreads / n.group, heads = a.heads[0] + a.heads[1];
-    const Part at = part_of<HALF>(a, n);
-    uint32_t h = threadIdx.x / n.group;
-    Eight<T> x[kFlight];
-    char *to[kFlight];   // nullptr: no head
-    const float *w[kFlight];
-    auto fetch = [&]() {
-#pragma unroll
-        for (int i = 0; i < kFlight; ++i, h += step) {
-            to[i] = nullptr;
-            w[i] = weights;
-            if (h >= heads) continue;
-            const int which = h >= a.heads[0];
-            const uint32_t hh = which ? h - a.heads[0] : h;
-            to[i] = a.y[which] + ((long long)t * a.y_token[which] + (long long)hh * a.y_head[which]) * (long long)sizeof(T);
-            w[i] = weights + which * a.head_dim;
-            x[i].load(a.x[which] + ((long long)t * a.x_token[which] + (long long)hh * a.x_head[which]) * (long long)sizeof(T), at);
-        }
-    };
-    fetch();   // on its way while the sines are made
-    fill_weights(a, n, weights);
-    fill_wheel<true>(a, wheel, t);
-    for (uint32_t done = 0; done < heads; done += kFlight * step) {
-#pragma unroll
-        for (int i = 0; i < kFlight; ++i) {
-            float v[8], k[8], sum = 0.f;
-            x[i].get(v, at);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(v[j], v[j], sum);
-            const float r = rsqrtf(fmaf(add_lanes(sum, n.group), n.inv_dim, n.eps));
-            if (!to[i]) continue;
-            eight_floats(k, w[i], at);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = v[j] * r * k[j];
-            turn<HALF, false>(v, wheel, at);
-            x[i].put(v, to[i], at);
-        }
-        fetch();
-    }
-}
+    constexpr int kBytes = N * int(sizeof(T)), kLoads = BACK ? 4 : 2, kStage = kLoads * kThreads * kBytes;
+    extern __shared__ __align__(16) char dynamic[];
+    if (BACK) let_next_start();
+    const uint32_t ring = smem_addr(dynamic) + threadIdx.x * kBytes;
+    const uint32_t groups = kThreads / n.group;
+    const int which = blockIdx.x >= n.ctas_q;
+    const uint32_t cta = which ? blockIdx.x - n.ctas_q : blockIdx.x, ctas = which ? gridDim.x - n.ctas_q : n.ctas_q;
+    const uint32_t heads = a.heads[which], split = n.split[which], rounds = (heads + split - 1) / split;
+    const uint32_t units = a.n_tokens * split, all = ctas * groups, unit0 = cta * groups + threadIdx.x / n.group;
+    const uint32_t turns = (units + all - 1) / all;   // of units, as many for every group of lanes
+    const Part at = part_of<N>(a, n);
+    const uint32_t apart = (at.second - at.first) * uint32_t(sizeof(T));
 
-template <typename T, bool HALF>
-__global__ void __launch_bounds__(kThreads, 8)
-norm_rotary_back_kernel(const __grid_constant__ RotaryDev a, const __grid_constant__ NormDev n) {
-    __shared__ __align__(16) float2 wheels[2][GAC_ROTARY_MAX_DIM / 2];
-    __shared__ __align__(16) float weights[2 * kMaxVectorDim];
-    __shared__ float sums[kThreads * 16];
-    const uint32_t step = kThreads / n.group, heads = a.heads[0] + a.heads[1], mine = threadIdx.x / n.group;
-    const Part at = part_of<HALF>(a, n);
-    float dw[2][8] = {};
-    fill_weights(a, n, weights);
-    uint32_t turn_of = 0;
-    for (uint32_t t = blockIdx.x; t < a.n_tokens; t += gridDim.x, turn_of ^= 1) {
-        float2 *wheel = wheels[turn_of];
-        Eight<T> g, x;
-        char *to;
-        int which;
-        uint32_t h = mine;
-        auto fetch = [&]() {
-            to = nullptr;
-            which = h >= a.heads[0];
-            if (h < heads) {
-                const uint32_t hh = which ? h - a.heads[0] : h;
-                to = a.y[which] + ((long long)t * a.y_token[which] + (long long)hh * a.y_head[which]) * (long long)sizeof(T);
-                g.load(a.x[which] + ((long long)t * a.x_token[which] + (long long)hh * a.x_head[which]) * (long long)sizeof(T), at);
-                x.load(n.v[which] + ((long long)t * n.v_token[which] + (long long)hh * n.v_head[which]) * (long long)sizeof(T), at);
-            }
-            h += step;
+    auto fetch = [&](const char *row, uint32_t to) {
+        auto copy = [&](uint32_t dst, const char *src) {
+            if (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
         };
-        fetch();
-        fill_wheel<true>(a, wheel, t);   // the other wheel is done with once all have come here
-        for (uint32_t done = 0; done < heads; done += step) {
-            float b[8], v[8], k[8], squares = 0.f, dot = 0.f;
-            g.get(b, at);
-            x.get(v, at);
-            turn<HALF, true>(b, wheel, at);
-            eight_floats(k, weights + (to && which ? a.head_dim : 0), at);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                squares = fmaf(v[j], v[j], squares);
-                dot = fmaf(b[j] * k[j], v[j], dot);
+        if (at.here) copy(to, row);
+        if (at.both) copy(to + kThreads * kBytes, row + apart);
+    };
+    // what comes in next: a round of a unit
+    uint32_t f_turn = 0, f_round = 0, f_head = 0;
+    bool f_live = false;
+    const char *f_x = nullptr, *f_v = nullptr;
+    auto issue = [&](uint32_t slot) {
+        if (f_turn < turns) {
+            if (f_round == 0) {
+                const uint32_t unit = unit0 + f_turn * all;
+                const long long t = unit / split;
+                f_live = unit < units;
+                f_head = unit % split;
+                f_x = a.x[which] + t * n.x_token[which] + (long long)f_head * n.x_head[which] + at.first * sizeof(T);
+                if (BACK) f_v = n.v[which] + t * n.v_token[which] + (long long)f_head * n.v_head[which] + at.first * sizeof(T);
             }
-            const float r = rsqrtf(fmaf(add_lanes(squares, n.group), n.inv_dim, n.eps));
-            const float c = add_lanes(dot, n.group) * n.inv_dim * r * r;
-            if (to) {
+            if (f_live && f_head < heads) {
+                const uint32_t to = ring + slot * kStage;
+                fetch(f_x, to);
+                if (BACK) fetch(f_v, to + 2 * kThreads * kBytes);
+            }
+            f_head += split;
+            f_x += n.x_step[which];
+            if (BACK) f_v += n.v_step[which];
+            if (++f_round == rounds) {
+                f_round = 0;
+                ++f_turn;
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    // what is not there of a head stays zero in the ring
+    for (int i = 0; i < kRing * kLoads; ++i)
+        if (!(i % 2 ? at.both : at.here))
+            for (int w = 0; w < kBytes / 4; ++w) asm volatile("st.shared.u32 [%0], %1;" ::"r"(ring + i * kThreads * kBytes + w * 4), "r"(0) : "memory");
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float share = b[j] * (v[j] * r);
-                    if (which) dw[1][j] += share;
-                    else dw[0][j] += share;
-                    b[j] = r * fmaf(-v[j], c, b[j] * k[j]);
+    for (int i = 0; i < kRing; ++i) issue(i);
+
+    // the place's weights, two elements each
+    float2 w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bool there = i < N / 2 ? at.here : at.both;
+        const uint32_t e = i < N / 2 ? at.first + 2 * i : at.second + 2 * i - N;
+        w[i] = there ? make_float2(weight_at(n, which, e), weight_at(n, which, e + 1)) : make_float2(0.f, 0.f);
+    }
+    float2 dw[BACK ? N : 1] = {};
+    uint32_t slot = 0;
+    for (uint32_t step = 0; step < turns; ++step) {
+        const uint32_t unit = unit0 + step * all, t = unit / split;
+        const bool live = unit < units;
+        // x -> a x - b y, y -> c x + d y, forward with the weights in them; what is not turned stays as it is
+        float2 ma[N / 2], mb[N / 2], mc[BACK ? 1 : N / 2], md[BACK ? 1 : N / 2];
+        const int place = live && at.turn && !a.positions ? place_in_sequence(a.cu, a.n_seqs, t) : 0;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            float2 cs[2] = {make_float2(1.f, 0.f), make_float2(1.f, 0.f)};
+            if (live && at.turn)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t k = 2 * i + j, pair = HALF ? at.u * N + k : (k < N / 2 ? 0 : a.pairs / 2 - N / 2) + at.u * (N / 2) + k;
+                    cs[j] = turn_of(a, pair, a.positions ? position_on_axis(a, pair, t) : place);
                 }
-                g.put(b, to, at);
+            const float2 c = make_float2(cs[0].x, cs[1].x), s = make_float2(cs[0].y, cs[1].y);
+            if constexpr (BACK) {
+                ma[i] = c;
+                mb[i] = s;
+            } else {
+                const float2 wx = HALF ? w[i] : make_float2(w[2 * i].x, w[2 * i + 1].x), wy = HALF ? w[N / 2 + i] : make_float2(w[2 * i].y, w[2 * i + 1].y);
+                ma[i] = mul2(c, wx);
+                mb[i] = mul2(make_float2(-s.x, -s.y), wy);
+                mc[i] = mul2(s, wx);
+                md[i] = mul2(c, wy);
             }
-            fetch();
+        }
+        uint32_t h = unit % split;
+        char *to = a.y[which] + (long long)t * n.y_token[which] + (long long)h * n.y_head[which] + at.first * sizeof(T);
+        for (uint32_t round = 0; round < rounds; ++round, h += split, to += n.y_step[which]) {
+            float2 v[N], squares = make_float2(0.f, 0.f);
+            const uint32_t from = ring + slot * kStage;
+            const bool here = live && h < heads;
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+            if constexpr (!BACK) {
+                take<T, N>(from, v);
+                take<T, N>(from + kThreads * kBytes, v + N / 2);
+                issue(slot);
+#pragma unroll
+                for (int j = 0; j < N; ++j) squares = fma2(v[j], v[j], squares);
+                const float r = rsqrtf(fmaf(add_lanes(squares.x + squares.y, n.group), n.inv_dim, n.eps));
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] = mul2(v[j], make_float2(r, r));
+                turn<N, HALF>(v, ma, mb, mc, md);
+            } else {
+                float2 b[N], bw[N], dot = squares, minus[N / 2];
+                take<T, N>(from, b);
+                take<T, N>(from + kThreads * kBytes, b + N / 2);
+                take<T, N>(from + 2 * kThreads * kBytes, v);
+                take<T, N>(from + 3 * kThreads * kBytes, v + N / 2);
+                issue(slot);
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) minus[i] = make_float2(-mb[i].x, -mb[i].y);
+                turn<N, HALF>(b, ma, mb, minus, ma);   // by the negative angle
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    bw[j] = mul2(b[j], w[j]);
+                    squares = fma2(v[j], v[j], squares);
+                    dot = fma2(bw[j], v[j], dot);
+                }
+                const float r = rsqrtf(fmaf(add_lanes(squares.x + squares.y, n.group), n.inv_dim, n.eps));
+                const float c = -(add_lanes(dot.x + dot.y, n.group) * n.inv_dim * r * r);
+                const float2 rr = make_float2(r, r);
+                if (here)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) dw[j] = fma2(b[j], mul2(v[j], rr), dw[j]);
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] = mul2(rr, fma2(v[j], make_float2(c, c), bw[j]));
+            }
+            slot = slot + 1 == kRing ? 0 : slot + 1;
+            if (here && at.here) put<T, N>(to, v);
+            if (here && at.both) put<T, N>(to + apart, v + N / 2);
         }
     }
-    // the CTA's share: the threads of one place in their order
+    if constexpr (BACK) {
+        // the CTA's share: the threads of one place in their order
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+        float *sums = reinterpret_cast<float *>(dynamic);   // 2 N of a thread: no more than the ring
+        static_assert(2 * N * sizeof(float) <= size_t(kRing) * kLoads * kBytes, "fits the ring");
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sums[i * kThreads + threadIdx.x] = dw[i / 8][i % 8];
-    __syncthreads();
-    if (threadIdx.x < n.group && at.here) {
-        float *to = n.shares + size_t(blockIdx.x) * 2 * a.head_dim;
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 2 * N; ++i) sums[i * kThreads + threadIdx.x] = i & 1 ? dw[i / 2].y : dw[i / 2].x;
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < 2 * N * n.group; i += kThreads) {   // groups of lanes are powers of two, as the threads are
+            const uint32_t j = i / n.group;
+            const float *from = sums + j * kThreads + at.u;
             float s = 0.f;
-            for (uint32_t m = 0; m < step; ++m) s += sums[i * kThreads + m * n.group + threadIdx.x];
-            const int j = i % 8;
-            if (j < 4 || at.both) to[(i / 8) * a.head_dim + (j < 4 ? at.first + j : at.second + j - 4)] = s;
+            for (uint32_t m = 0; m < groups; ++m) s += from[m * n.group];
+            if (j < N ? at.here : at.both) n.shares[size_t(blockIdx.x) * a.head_dim + (j < N ? at.first + j : at.second + j - N)] = s;
         }
     }
 }
@@ -247,7 +293,7 @@ norm_rotary_any_kernel(const __grid_constant__ RotaryDev a, const __grid_constan
             const int which = h0 >= a.heads[0];
             const uint32_t h = which ? h0 - a.heads[0] : h0;
             const char *in = a.x[which] + ((long long)t * a.x_token[which] + (long long)h * a.x_head[which]) * kSize;
-            const char *v = BACK ? n.v[which] + ((long long)t * n.v_token[which] + (long long)h * n.v_head[which]) * kSize : in;
+            const char *v = BACK ? n.v[which] + (long long)t * n.v_token[which] + (long long)h * n.v_head[which] : in;
             char *y = a.y[which] + ((long long)t * a.y_token[which] + (long long)h * a.y_head[which]) * kSize;
             // The unit's elements i and, if it is a pair, j; what comes in, turned back on the way back; and the weights
             auto unit = [&](uint32_t u, uint32_t &i, uint32_t &j, float &p, float &q) {
@@ -307,32 +353,40 @@ norm_rotary_any_kernel(const __grid_constant__ RotaryDev a, const __grid_constan
     for (uint32_t i = threadIdx.x; i < 2 * a.head_dim; i += kThreads) {
         float s = 0.f;
         for (uint32_t m = 0; m < kThreads / 32; ++m) s += dw[m * 2 * a.head_dim + i];
-        n.shares[size_t(blockIdx.x) * 2 * a.head_dim + i] = s;
+        n.shares[(size_t(i >= a.head_dim) * gridDim.x + blockIdx.x) * a.head_dim + i % a.head_dim] = s;
     }
 }
 
-// d_weight[which][i] = sum of the shares, 32 columns to a CTA.
+// d_weight[which][i] = sum of the shares, eight columns to a CTA: 128 threads to a column, each with a few loads in flight.
+constexpr uint32_t kColumns = 8, kColumnThreads = 128;
 struct WeightsDev {
     const float *shares;
     char *d_w[2];
     int w_bf16;
-    uint32_t n, head_dim;   // shares, columns
+    uint32_t first[2], count[2], head_dim;   // shares of each kind of heads; columns
 };
-__global__ void __launch_bounds__(1024) norm_weights_kernel(const __grid_constant__ WeightsDev a) {
-    __shared__ double sums[32][33];
-    const uint32_t c = threadIdx.x % 32, row = threadIdx.x / 32, col = blockIdx.x * 32 + c;
+__global__ void __launch_bounds__(kColumns *kColumnThreads) norm_weights_kernel(const __grid_constant__ WeightsDev a) {
+    __shared__ double sums[32][kColumns];
+    const uint32_t c = threadIdx.x % kColumns, row = threadIdx.x / kColumns, tiles = (a.head_dim + kColumns - 1) / kColumns;
+    const int which = blockIdx.x >= tiles;
+    const uint32_t col = (blockIdx.x - which * tiles) * kColumns + c, count = a.count[which];
+    wait_for_previous();
     double s = 0.0;
-    if (col < 2 * a.head_dim)
-        for (uint32_t i = row; i < a.n; i += 32) s += double(a.shares[size_t(i) * 2 * a.head_dim + col]);
-    sums[row][c] = s;
+    if (col < a.head_dim) {
+        const float *from = a.shares + size_t(a.first[which]) * a.head_dim + col;
+#pragma unroll 4
+        for (uint32_t i = row; i < count; i += kColumnThreads) s += double(__ldcg(from + size_t(i) * a.head_dim));
+    }
+#pragma unroll
+    for (int o = kColumns; o < 32; o *= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);   // the warp's four rows
+    if (threadIdx.x % 32 < kColumns) sums[threadIdx.x / 32][c] = s;
     __syncthreads();
-    if (row != 0 || col >= 2 * a.head_dim) return;
-    for (uint32_t i = 1; i < 32; ++i) s += sums[i][c];
-    const int which = col >= a.head_dim;
-    const uint32_t i = which ? col - a.head_dim : col;
-    if (!a.d_w[which]) return;
-    if (a.w_bf16) store_el(a.d_w[which] + i * 2, float(s), uint16_t{});
-    else store_el(a.d_w[which] + i * 4, float(s), float{});
+    if (row != 0 || col >= a.head_dim || !a.d_w[which]) return;
+    s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s += sums[i][c];
+    if (a.w_bf16) store_el(a.d_w[which] + col * 2, float(s), uint16_t{});
+    else store_el(a.d_w[which] + col * 4, float(s), float{});
 }
 
 uint32_t share_count(const gac_rotary_args &a) { return std::min(a.n_tokens, kShares); }
@@ -359,9 +413,47 @@ int check_norm(const gac_rotary_args &a, const gac_norm &norm, const Rows (&y)[2
         for (int i = 0; i < 2; ++i)
             if (a.heads[i] && share(y[i], r)) return fail(nullptr, GAC_ERR_INVALID_ARG, "output heads overlap a weight%s");
     }
-    n.group = 1;
-    while (n.group * 8 < a.head_dim) n.group *= 2;
     return GAC_OK;
+}
+
+// How a launch of the vector kernel is laid out, N elements to a vector.
+struct Layout {
+    uint32_t grid, smem;
+};
+Layout lay_out(const RotaryDev &d, NormDev &n, uint32_t elements, uint32_t size, bool back) {
+    n.group = 1;
+    while (n.group * 2 * elements < d.head_dim) n.group *= 2;
+    const uint32_t groups = kThreads / n.group, most = 148 * (back ? kBackCtas : kForwardCtas);
+    // CTAs are shared out by heads, with a token's sines counted as three of them.  A token's heads stay with one group of lanes, or are
+    // split where that would leave CTAs idle; and no more CTAs than it takes for all to have the same number of units.
+    const uint32_t cost[2] = {d.heads[0] ? d.heads[0] + 3 : 0, d.heads[1] ? d.heads[1] + 3 : 0};
+    uint32_t grid = 0;
+    for (int w = 0; w < 2; ++w) {
+        uint32_t ctas = 0, split = 1;
+        if (d.heads[w]) {
+            ctas = std::max(1u, most * cost[w] / (cost[0] + cost[1]));
+            while (split < groups && split < d.heads[w] && uint64_t(d.n_tokens) * split < uint64_t(ctas) * groups) split *= 2;
+            const uint64_t units = uint64_t(d.n_tokens) * split, turns = (units + uint64_t(ctas) * groups - 1) / (uint64_t(ctas) * groups);
+            ctas = uint32_t(((units + turns - 1) / turns + groups - 1) / groups);
+        }
+        if (w == 0) n.ctas_q = ctas;
+        grid += ctas;
+        n.split[w] = split;
+        n.x_token[w] = d.x_token[w] * size;
+        n.x_head[w] = d.x_head[w] * size;
+        n.y_token[w] = d.y_token[w] * size;
+        n.y_head[w] = d.y_head[w] * size;
+        n.x_step[w] = n.x_head[w] * split;
+        n.y_step[w] = n.y_head[w] * split;
+        n.v_step[w] = back ? n.v_head[w] * split : 0;
+    }
+    return Layout{grid, uint32_t(kRing) * (back ? 4 : 2) * kThreads * elements * size};
+}
+template <bool BACK>
+void (*vector_kernel(uint32_t elements, bool bf16, bool half))(const RotaryDev, const NormDev) {
+    if (!bf16) return half ? norm_rotary_kernel<float, 4, true, BACK> : norm_rotary_kernel<float, 4, false, BACK>;
+    if (elements == 8) return half ? norm_rotary_kernel<uint16_t, 8, true, BACK> : norm_rotary_kernel<uint16_t, 8, false, BACK>;
+    return half ? norm_rotary_kernel<uint16_t, 4, true, BACK> : norm_rotary_kernel<uint16_t, 4, false, BACK>;
 }
 
 }  // namespace
@@ -383,14 +475,20 @@ int gac_norm_rotary(const gac_rotary_args *args, const gac_rotary_axes *axes, co
     if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const bool half = a.layout == GAC_ROTARY_HALF, bf16 = a.dtype == GAC_BF16;
-    void (*fn)(const RotaryDev, const NormDev) = nullptr;
-    if (a.head_dim <= kMaxVectorDim && vectors_fit(d, 4, bf16 ? 2 : 4))
-        fn = bf16 ? (half ? norm_rotary_kernel<uint16_t, true> : norm_rotary_kernel<uint16_t, false>)
-                  : (half ? norm_rotary_kernel<float, true> : norm_rotary_kernel<float, false>);
-    else
-        fn = bf16 ? (half ? norm_rotary_any_kernel<uint16_t, true, false> : norm_rotary_any_kernel<uint16_t, false, false>)
-                  : (half ? norm_rotary_any_kernel<float, true, false> : norm_rotary_any_kernel<float, false, false>);
-    fn<<<a.n_tokens, kThreads, 0, s>>>(d, n);
+    // Vectors of 16 bytes, or of four bfloat16, where every vector of every head starts on such a boundary; else single elements.
+    uint32_t elements = 0;
+    // A few tokens take the shorter ones: twice the lanes to a head, each with half as many sines to make.
+    const bool few = uint64_t(a.n_tokens) * (a.heads[0] + a.heads[1]) * a.head_dim < uint64_t(kFew);
+    if (a.head_dim <= kMaxVectorDim) elements = bf16 && !few && vectors_fit(d, 8, 2) ? 8 : vectors_fit(d, 4, bf16 ? 2 : 4) ? 4 : 0;
+    if (elements) {
+        const Layout how = lay_out(d, n, elements, bf16 ? 2 : 4, false);
+        vector_kernel<false>(elements, bf16, half)<<<how.grid, kThreads, how.smem, s>>>(d, n);
+    } else {
+        void (*fn)(const RotaryDev, const NormDev) =
+            bf16 ? (half ? norm_rotary_any_kernel<uint16_t, true, false> : norm_rotary_any_kernel<uint16_t, false, false>)
+                 : (half ? norm_rotary_any_kernel<float, true, false> : norm_rotary_any_kernel<float, false, false>);
+        fn<<<a.n_tokens, kThreads, 0, s>>>(d, n);
+    }
     GAC_CUDA(nullptr, cudaGetLastError());
     return GAC_OK;
 }
@@ -415,7 +513,12 @@ int gac_norm_rotary_backward(const gac_rotary_args *args, const gac_rotary_axes 
     const size_t need = gac_norm_rotary_workspace(args);
     if (heads && (!grad->workspace || reinterpret_cast<uint64_t>(grad->workspace) % 16 || grad->workspace_bytes < need))
         return fail(nullptr, GAC_ERR_INVALID_ARG, "the workspace is missing, misaligned or too small%s");
-    bool vectors = heads && a.head_dim <= kMaxVectorDim && vectors_fit(d, 4, size);
+    auto aligned = [&](uint32_t elements) {   // the forward call's heads too
+        for (int w = 0; w < 2; ++w)
+            if (a.heads[w] && (reinterpret_cast<uint64_t>(grad->x[w].p) % (elements * size) || grad->x[w].token % elements || grad->x[w].head % elements))
+                return false;
+        return a.head_dim <= kMaxVectorDim && vectors_fit(d, elements, size);
+    };
     // What is written shares no memory with anything else (d_y and d_x have been checked: apart, or one and the same).
     Rows in[6], out[3];
     int ins = 0, outs = 0;
@@ -434,15 +537,14 @@ int gac_norm_rotary_backward(const gac_rotary_args *args, const gac_rotary_axes 
         }
         if (norm->weight[w]) in[ins++] = rows_of(norm->weight[w], 0, 0, 1, 1, a.head_dim, w_size);
         n.v[w] = static_cast<const char *>(grad->x[w].p);
-        n.v_token[w] = grad->x[w].token;
-        n.v_head[w] = grad->x[w].head;
+        n.v_token[w] = grad->x[w].token * int64_t(size);
+        n.v_head[w] = grad->x[w].head * int64_t(size);
         if (!heads || a.heads[w] == 0) continue;
         const uint64_t p = reinterpret_cast<uint64_t>(n.v[w]);
         const int64_t most = int64_t(1) << 40;
-        if (!p || p % size || n.v_token[w] < 0 || n.v_head[w] < 0 || n.v_token[w] > most || n.v_head[w] > most)
+        if (!p || p % size || grad->x[w].token < 0 || grad->x[w].head < 0 || grad->x[w].token > most || grad->x[w].head > most)
             return fail(nullptr, GAC_ERR_INVALID_ARG, "the heads of the forward call are NULL or misaligned, or their strides out of range%s");
-        vectors = vectors && p % (4 * size) == 0 && n.v_token[w] % 4 == 0 && n.v_head[w] % 4 == 0;
-        in[ins++] = rows_of(n.v[w], n.v_token[w], n.v_head[w], a.n_tokens, a.heads[w], a.head_dim, size);
+        in[ins++] = rows_of(n.v[w], grad->x[w].token, grad->x[w].head, a.n_tokens, a.heads[w], a.head_dim, size);
     }
     for (int w = 0; w < 2; ++w) {
         if (!heads || a.heads[w] == 0) continue;
@@ -458,22 +560,38 @@ int gac_norm_rotary_backward(const gac_rotary_args *args, const gac_rotary_axes 
     if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const bool half = a.layout == GAC_ROTARY_HALF, bf16 = a.dtype == GAC_BF16;
-    const uint32_t shares = heads ? share_count(a) : 0;
+    WeightsDev wd = {};
     if (heads) {
-        void (*fn)(const RotaryDev, const NormDev) = nullptr;
-        if (vectors)
-            fn = bf16 ? (half ? norm_rotary_back_kernel<uint16_t, true> : norm_rotary_back_kernel<uint16_t, false>)
-                      : (half ? norm_rotary_back_kernel<float, true> : norm_rotary_back_kernel<float, false>);
-        else
-            fn = bf16 ? (half ? norm_rotary_any_kernel<uint16_t, true, true> : norm_rotary_any_kernel<uint16_t, false, true>)
-                      : (half ? norm_rotary_any_kernel<float, true, true> : norm_rotary_any_kernel<float, false, true>);
-        fn<<<shares, kThreads, vectors ? 0 : kThreads / 32 * 2 * a.head_dim * sizeof(float), s>>>(d, n);
+        const uint32_t elements = bf16 && aligned(8) ? 8 : aligned(4) ? 4 : 0;
+        if (elements) {
+            const Layout how = lay_out(d, n, elements, size, true);
+            wd.first[1] = wd.count[0] = n.ctas_q;
+            wd.count[1] = how.grid - n.ctas_q;
+            vector_kernel<true>(elements, bf16, half)<<<how.grid, kThreads, how.smem, s>>>(d, n);
+        } else {
+            void (*fn)(const RotaryDev, const NormDev) =
+                bf16 ? (half ? norm_rotary_any_kernel<uint16_t, true, true> : norm_rotary_any_kernel<uint16_t, false, true>)
+                     : (half ? norm_rotary_any_kernel<float, true, true> : norm_rotary_any_kernel<float, false, true>);
+            wd.first[1] = wd.count[0] = wd.count[1] = share_count(a);
+            fn<<<share_count(a), kThreads, kThreads / 32 * 2 * a.head_dim * sizeof(float), s>>>(d, n);
+        }
         GAC_CUDA(nullptr, cudaGetLastError());
     }
     if (grad->d_weight[0] || grad->d_weight[1]) {
-        WeightsDev wd{n.shares, {static_cast<char *>(grad->d_weight[0]), static_cast<char *>(grad->d_weight[1])}, n.w_bf16, shares, a.head_dim};
-        norm_weights_kernel<<<(2 * a.head_dim + 31) / 32, 1024, 0, s>>>(wd);
-        GAC_CUDA(nullptr, cudaGetLastError());
+        wd.shares = n.shares;
+        wd.w_bf16 = n.w_bf16;
+        wd.head_dim = a.head_dim;
+        for (int w = 0; w < 2; ++w) wd.d_w[w] = static_cast<char *>(grad->d_weight[w]);
+        cudaLaunchConfig_t how = {};
+        how.gridDim = dim3(2 * ((a.head_dim + kColumns - 1) / kColumns));
+        how.blockDim = dim3(kColumns * kColumnThreads);
+        how.stream = s;
+        cudaLaunchAttribute attr[1];   // set up while the kernel before ends
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = heads ? 1 : 0;
+        how.attrs = attr;
+        how.numAttrs = 1;
+        GAC_CUDA(nullptr, cudaLaunchKernelEx(&how, norm_weights_kernel, wd));
     }
     return GAC_OK;
 }

@@ -60,16 +60,22 @@ __device__ int place_in_sequence(const int32_t *cu, uint32_t n_seqs, uint32_t t)
     return lo == n_seqs ? 0 : int(t - first);
 }
 
-// Cosine and sine, already scaled, of every pair of the CTA's token.  AXES: its pairs may be turned by different axes.
+// Cosine and sine, already scaled, of a pair at a position.
+__device__ __forceinline__ float2 turn_of(const RotaryDev &a, uint32_t pair, int pos) {
+    const double turns = double(pos) * a.turns[pair];
+    float s, c;
+    sincospif(2.0f * float(turns - rint(turns)), &s, &c);
+    return make_float2(c * a.scale, (a.inverse ? -s : s) * a.scale);
+}
+__device__ __forceinline__ int position_on_axis(const RotaryDev &a, uint32_t pair, uint32_t t) {
+    return a.positions[(a.axis[pair / 16] >> (2 * (pair % 16)) & 3u) * a.axis_stride + t];
+}
+// Of every pair of the CTA's token.  AXES: its pairs may be turned by different axes.
 template <bool AXES>
 __device__ __forceinline__ void fill_wheel(const RotaryDev &a, float2 *wheel, uint32_t t) {
     for (uint32_t i = threadIdx.x; i < a.pairs; i += kThreads) {
-        const long long row = AXES ? (a.axis[i / 16] >> (2 * (i % 16)) & 3u) * a.axis_stride : 0;
-        const int pos = a.positions ? a.positions[row + t] : place_in_sequence(a.cu, a.n_seqs, t);
-        const double turns = double(pos) * a.turns[i];
-        float s, c;
-        sincospif(2.0f * float(turns - rint(turns)), &s, &c);
-        wheel[i] = make_float2(c * a.scale, (a.inverse ? -s : s) * a.scale);
+        const int pos = !a.positions ? place_in_sequence(a.cu, a.n_seqs, t) : AXES ? position_on_axis(a, i, t) : a.positions[t];
+        wheel[i] = turn_of(a, i, pos);
     }
     __syncthreads();
 }

@@ -8,8 +8,9 @@ turned      12 u scale (|x| + |y|) on top of what went in (packed_ref): under 60
 way back    With A = scale (|dy_x| + |dy_y|) (|dy| where nothing is turned), B = A |w| and n = |x| r:
             a is within 12 u A, b = a w within 15 u B, its mean with x r within (15 + 45 + 70 + 4) u mean(B n), the product
             of that with x r within 180 u n mean(B n), and r adds 42 u to all: under 240 u r (B + n mean(B n)).
-            The weights' gradients: terms within 60 u A n, then a chain of as many terms as a thread has heads to take and
-            eight threads more, and binary64: (70 + chain) u sum(A n).
+            The weights' gradients: terms within 60 u A n, then a chain of as many terms as a thread has heads to take (they
+            are shared out over at least 64 groups of lanes as soon as there are so many tokens) and the CTA's up to 128
+            groups, and binary64: (70 + chain) u sum(A n).
 A bfloat16 result adds v of itself.
 """
 import math
@@ -17,7 +18,7 @@ import math
 import torch
 
 U, V = 2.0 ** -24, 2.0 ** -8
-SHARES = 148 * 8     # tokens are dealt out to at most as many CTAs on the way back
+SHARES = 148 * 4     # heads of a kind are dealt out to at most as many CTAs on the way back
 
 
 def wheel(pos, freqs, axis=None, scale=1.0):
@@ -80,5 +81,5 @@ def norm_back(dy, x, w, cs, layout, scale, eps, offset):
     dx = r * (b - n * (b * n).mean(-1, keepdim=True))
     dx_b = 240 * U * r * (B + n.abs() * (B * n.abs()).mean(-1, keepdim=True))
     dw, size = (a * n).sum((0, 1)), (A * n.abs()).sum((0, 1))
-    chain = -(-x.shape[0] // SHARES) * x.shape[1] + 8
+    chain = -(-x.shape[0] // 64) * x.shape[1] + 128
     return rounded(dx, dx_b, x.dtype), rounded(dw, (70 + chain) * U * size, torch.float32 if w is None else w.dtype)

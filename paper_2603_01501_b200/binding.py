@@ -12,6 +12,7 @@ import struct
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
+import numpy as np
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -550,6 +551,21 @@ def _empty(like: torch.Tensor, shape, stream, dtype=None) -> torch.Tensor:
         return like.new_empty(shape) if dtype is None else like.new_empty(shape, dtype=dtype)
 
 
+def _empty_like(t: torch.Tensor, stream) -> torch.Tensor:
+    """Contiguous, of the same shape."""
+    if stream is None:
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
+def _address(array) -> int:
+    """Of a contiguous numpy array's memory (a quarter of the time that its array interface takes)."""
+    if array.size and array.flags.writeable:
+        return ctypes.addressof(ctypes.c_char.from_buffer(array))
+    return array.__array_interface__["data"][0]
+
+
 def _check(rc: int) -> None:
     if rc != GAC_OK:
         raise GacError(rc, load_library().gac_last_error(None).decode())
@@ -675,7 +691,6 @@ def gac_rotary_freqs(rot_dim: int, base: float = 1e4, scaling: str = "none", fac
                      trained: float = 4096.0, low: float = 1.0, high: float = 4.0):
     """Radians per position of each pair (a float64 array of rot_dim/2), stretched for contexts ``factor``
     times as long as the trained one; see gac.h for the scalings."""
-    import numpy as np
     freqs = np.zeros(max(rot_dim // 2, 1), dtype=np.float64)
     _check(load_library().gac_rotary_freqs(freqs.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), rot_dim, base,
                                            ROTARY_SCALINGS[scaling], factor, trained, low, high))
@@ -685,18 +700,21 @@ def gac_rotary_freqs(rot_dim: int, base: float = 1e4, scaling: str = "none", fac
 def _int32_ptr(t: Optional[torch.Tensor], name: str, device: torch.device) -> int:
     if t is None:
         return 0
-    if t.dtype is not torch.int32 or t.device != device or t.dim() != 1 or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.get_device() != device.index or t.dim() != 1 or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 vector on the tensors' device")
     return t.data_ptr()
 
 
 def _heads(t: torch.Tensor, name: str, like: torch.Tensor):
     """Checks one [tokens, heads, head_dim] operand; returns (address, token stride, head stride, heads)."""
-    if t.dim() != 3 or t.device != like.device or not t.is_cuda:
+    at = t.get_device()   # -1: not on a CUDA device
+    if t.dim() != 3 or at < 0 or at != like.get_device():
         raise ValueError(f"{name} must be a CUDA tensor [tokens, heads, head_dim]")
     n, h, d = t.shape
-    if t is not like and (t.dtype is not like.dtype or n != like.shape[0] or d != like.shape[2]):
-        raise ValueError(f"{name} differs in dtype, tokens or head_dim")
+    if t is not like:
+        m, _, e = like.shape
+        if t.dtype is not like.dtype or n != m or d != e:
+            raise ValueError(f"{name} differs in dtype, tokens or head_dim")
     s0, s1, s2 = t.stride()
     if s2 != 1 and d > 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
@@ -706,7 +724,6 @@ def _heads(t: torch.Tensor, name: str, like: torch.Tensor):
 def gac_rotary_sections(sections: Sequence[int], interleaved: bool = False):
     """Which axis turns each pair of a head (a uint8 array, ``axes`` of the calls below), from the number of pairs of each
     axis: one axis after the other, or dealt out in turn, where an axis whose pairs are used up is passed over."""
-    import numpy as np
     left = [int(n) for n in sections]
     if not 1 <= len(left) <= GAC_ROTARY_MAX_AXES or min(left) < 0:
         raise ValueError(f"1..{GAC_ROTARY_MAX_AXES} axes, none with a negative number of pairs")
@@ -716,61 +733,66 @@ def gac_rotary_sections(sections: Sequence[int], interleaved: bool = False):
     return np.array([a for _, a in sorted((r, a) for a, n in enumerate(left) for r in range(n))], dtype=np.uint8)
 
 
-def _rotary_args(q, k, freqs, positions, cu_seqlens, axes, layout, scale, inverse, outputs, stream):
-    """Packed gac_rotary_args and gac_rotary_axes (or None) of one call, with what must stay alive until it; outputs: a
-    pair of tensors, or None for new contiguous ones."""
-    import numpy as np
+def _rotary_args(q, k, freqs, positions, cu_seqlens, axes, layout, scale, inverse, in_place, stream):
+    """One call's packed gac_rotary_args and gac_rotary_axes (or None), its outputs, the raw stream, the torch stream or None,
+    and what must stay alive until the call."""
     dtype, device = q.dtype, q.device
-    if dtype not in _DT:
+    code = _DT.get(dtype)
+    if code is None:
         raise GacError(GAC_ERR_DTYPE, f"unsupported dtype {dtype}")
     qx, q0, q1, qh = _heads(q, "q", q)
     kx = k0 = k1 = kh = 0
     if k is not None:
         kx, k0, k1, kh = _heads(k, "k", q)
-    turns = freqs is not None
-    if (positions is None) == (cu_seqlens is None) and (turns or positions is not None):
-        raise ValueError("give positions or cu_seqlens")
     tokens, _, dim = q.shape
+    on, seqs, rot, freqs_at = None, 0, 0, 0
+    if freqs is not None:
+        if (positions is None) == (cu_seqlens is None):
+            raise ValueError("give positions or cu_seqlens")
+        if type(freqs) is not np.ndarray or freqs.dtype != np.float64 or not freqs.flags.c_contiguous:
+            freqs = np.ascontiguousarray(freqs, dtype=np.float64)
+        rot, freqs_at = 2 * freqs.size, _address(freqs)
+    elif positions is not None or axes is not None:
+        raise ValueError("positions and axes need frequencies")
     if axes is None:
         if positions is not None and positions.numel() != tokens:
             raise ValueError("one position per token")
         at = _int32_ptr(positions, "positions", device)
     else:
-        if positions is None or not turns:
-            raise ValueError("axes need positions [axes, tokens] and frequencies")
-        if positions.dtype is not torch.int32 or positions.device != device or positions.dim() != 2 or \
+        if positions is None:
+            raise ValueError("axes need positions [axes, tokens]")
+        if positions.dtype is not torch.int32 or positions.get_device() != device.index or positions.dim() != 2 or \
                 (positions.stride(1) != 1 and tokens > 1):
             raise ValueError("positions on axes must be an int32 tensor [axes, tokens] on the tensors' device, tokens contiguous")
-        if positions.shape[1] != tokens:
+        rows, columns = positions.shape
+        if columns != tokens:
             raise ValueError("one position per axis and token")
-        at = positions.data_ptr()
-    if cu_seqlens is not None and cu_seqlens.numel() < 1:
-        raise ValueError("cu_seqlens has one entry more than there are sequences")
-    if turns and not (isinstance(freqs, np.ndarray) and freqs.dtype == np.float64 and freqs.flags.c_contiguous):
-        freqs = np.ascontiguousarray(freqs, dtype=np.float64)
-    on = None
-    if axes is not None:
-        axes = np.asarray(axes)
-        if axes.dtype != np.uint8 or not axes.flags.c_contiguous:
+        if type(axes) is not np.ndarray or axes.dtype != np.uint8 or not axes.flags.c_contiguous:
+            axes = np.asarray(axes)
             if axes.dtype.kind not in "iu" or (axes.size and (axes.min() < 0 or axes.max() > 255)):
                 raise ValueError("axes are whole numbers, one per pair")
             axes = np.ascontiguousarray(axes, dtype=np.uint8)
         if axes.size != freqs.size:
             raise ValueError("one axis per pair")
-        on = _AXES.pack(axes.__array_interface__["data"][0], positions.stride(0), positions.shape[0], 0)
-    if outputs is None:
-        yq = _empty(q, (tokens, qh, dim), stream)
-        yk = _empty(q, (tokens, kh, dim), stream) if k is not None else None
-        qy = (yq.data_ptr(), qh * dim, dim)
-        kout = (yk.data_ptr(), kh * dim, dim) if k is not None else (0, 0, 0)
+        at = positions.data_ptr()
+        on = _AXES.pack(_address(axes), positions.stride(0), rows, 0)
+    if cu_seqlens is not None:
+        seqs = cu_seqlens.numel() - 1
+        if seqs < 0:
+            raise ValueError("cu_seqlens has one entry more than there are sequences")
+    cu_at = _int32_ptr(cu_seqlens, "cu_seqlens", device)
+    raw, stream = _on(stream, device)
+    if in_place:
+        yq, yk, qy, qy0, qy1, ky, ky0, ky1 = q, k, qx, q0, q1, kx, k0, k1
     else:
-        yq, yk = outputs
-        qy, kout = (qx, q0, q1), (kx, k0, k1)
-    args = _ROTARY.pack(qx, qy[0], q0, q1, qy[1], qy[2], kx, kout[0], k0, k1, kout[1], kout[2], qh, kh, tokens,
-                        0 if cu_seqlens is None else cu_seqlens.numel() - 1, dim, 2 * freqs.size if turns else 0, _DT[dtype],
-                        ROTARY_LAYOUTS[layout], 1 if inverse else 0, 0, at,
-                        _int32_ptr(cu_seqlens, "cu_seqlens", device), freqs.__array_interface__["data"][0] if turns else 0, scale)
-    return args, on, (yq, yk), (freqs, axes)
+        yq = _empty_like(q, stream)
+        qy, qy0, qy1, yk, ky, ky0, ky1 = yq.data_ptr(), qh * dim, dim, None, 0, 0, 0
+        if k is not None:
+            yk = _empty_like(k, stream)
+            ky, ky0, ky1 = yk.data_ptr(), kh * dim, dim
+    args = _ROTARY.pack(qx, qy, q0, q1, qy0, qy1, kx, ky, k0, k1, ky0, ky1, qh, kh, tokens, seqs, dim, rot, code,
+                        ROTARY_LAYOUTS[layout], 1 if inverse else 0, 0, at, cu_at, freqs_at, scale)
+    return args, on, yq, yk, device.index, raw, stream, (freqs, axes)
 
 
 def gac_rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Optional[torch.Tensor] = None,
@@ -783,28 +805,26 @@ def gac_rotary(q: torch.Tensor, k: Optional[torch.Tensor], freqs, positions: Opt
     Returns (q', k'): new contiguous tensors, or the given ones when ``in_place``."""
     if freqs is None:
         raise ValueError("freqs must be given")
-    raw, stream = _on(stream, q.device)
-    args, on, (yq, yk), keep = _rotary_args(q, k, freqs, positions, cu_seqlens, axes, layout, scale, inverse,
-                                            (q, k) if in_place else None, stream)
+    args, on, yq, yk, index, raw, _, keep = _rotary_args(q, k, freqs, positions, cu_seqlens, axes, layout, scale, inverse, in_place, stream)
     L = load_library()
-    _check(L.gac_rotary(args, q.device.index, raw) if on is None else L.gac_rotary_on_axes(args, on, q.device.index, raw))
+    _check(L.gac_rotary(args, index, raw) if on is None else L.gac_rotary_on_axes(args, on, index, raw))
     if in_place:   # autograd has to notice that what it may have saved has changed
         torch.autograd.graph.increment_version(q if k is None else (q, k))
     return yq, yk
 
 
 def _norm_args(q, q_weight, k_weight, eps, offset) -> bytes:
-    dtype = None
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+    dim, at, code, addresses = q.shape[2], q.get_device(), None, [0, 0]
+    for i, w in enumerate((q_weight, k_weight)):
         if w is None:
             continue
-        if w.dim() != 1 or w.numel() != q.shape[2] or w.device != q.device or (w.stride(0) != 1 and w.numel() > 1):
-            raise ValueError(f"{name} must be a contiguous vector of head_dim on the heads' device")
-        if w.dtype not in _DT or (dtype is not None and w.dtype is not dtype):
+        if w.dim() != 1 or w.numel() != dim or w.get_device() != at or (w.stride(0) != 1 and dim > 1):
+            raise ValueError("weights must be contiguous vectors of head_dim on the heads' device")
+        c = _DT.get(w.dtype)
+        if c is None or (code is not None and c != code):
             raise GacError(GAC_ERR_DTYPE, "weights are both float32 or both bfloat16")
-        dtype = w.dtype
-    return _NORM.pack(0 if q_weight is None else q_weight.data_ptr(), 0 if k_weight is None else k_weight.data_ptr(),
-                      _DT[dtype or torch.float32], 0, eps, offset)
+        code, addresses[i] = c, w.data_ptr()
+    return _NORM.pack(addresses[0], addresses[1], code or 0, 0, eps, offset)
 
 
 def gac_norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
@@ -813,10 +833,8 @@ def gac_norm_rotary(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Option
                     stream=None):
     """Root mean square norm of every head of q and k (or None), times offset + weight, and the turn of gac_rotary, in one
     pass.  Weights: [head_dim] float32 or bfloat16, or None for ones.  ``freqs=None`` turns nothing.  Returns (q', k')."""
-    raw, stream = _on(stream, q.device)
-    args, on, (yq, yk), keep = _rotary_args(q, k, freqs, positions, cu_seqlens, axes, layout, scale, False,
-                                            (q, k) if in_place else None, stream)
-    _check(load_library().gac_norm_rotary(args, on, _norm_args(q, q_weight, k_weight, eps, offset), q.device.index, raw))
+    args, on, yq, yk, index, raw, _, keep = _rotary_args(q, k, freqs, positions, cu_seqlens, axes, layout, scale, False, in_place, stream)
+    _check(load_library().gac_norm_rotary(args, on, _norm_args(q, q_weight, k_weight, eps, offset), index, raw))
     if in_place:
         torch.autograd.graph.increment_version(q if k is None else (q, k))
     return yq, yk
@@ -834,15 +852,17 @@ def gac_norm_rotary_backward(d_q: torch.Tensor, d_k: Optional[torch.Tensor], q: 
         raise ValueError("the gradients must have the shapes of q and k")
     qx, q0, q1, _ = _heads(q, "q", d_q)
     kx, k0, k1, _ = _heads(k, "k", d_q) if k is not None else (0, 0, 0, 0)
-    raw, stream = _on(stream, q.device)
     norm = _norm_args(q, q_weight, k_weight, eps, offset)
-    args, on, (yq, yk), keep = _rotary_args(d_q, d_k, freqs, positions, cu_seqlens, axes, layout, scale, False, None, stream)
-    wq, wk = (None if w is None or not weight_grads else _empty(w, (w.numel(),), stream) for w in (q_weight, k_weight))
+    args, on, yq, yk, index, raw, stream, keep = _rotary_args(d_q, d_k, freqs, positions, cu_seqlens, axes, layout, scale, False, False, stream)
+    wq = wk = None
+    if weight_grads:
+        wq = None if q_weight is None else _empty_like(q_weight, stream)
+        wk = None if k_weight is None else _empty_like(k_weight, stream)
     need = max(L.gac_norm_rotary_workspace(args), 16)
     workspace = _empty(q, (need,), stream, torch.uint8)
     grad = _NORM_GRAD.pack(qx, q0, q1, kx, k0, k1, 0 if wq is None else wq.data_ptr(), 0 if wk is None else wk.data_ptr(),
                            workspace.data_ptr(), need)
-    _check(L.gac_norm_rotary_backward(args, on, norm, grad, q.device.index, raw))
+    _check(L.gac_norm_rotary_backward(args, on, norm, grad, index, raw))
     return yq, yk, wq, wk
 
 
@@ -917,29 +937,35 @@ def gac_distill(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, 
     [tokens, top] int32, teacher [tokens, top] float32 or bfloat16: logits for ``kind="top"``, log-probabilities for "forward" and
     "reverse" (see gac.h).  Returns the loss [tokens] float32 or, with ``grad``, (loss, d_logits): weights[t] times the gradient of
     token t's loss, in a new contiguous tensor or, ``in_place``, over the logits.  ``loss=False``: None in its place."""
-    if logits.dim() != 2 or not logits.is_cuda or ids.dim() != 2 or teacher.dim() != 2:
+    at = logits.get_device()   # -1: not on a CUDA device
+    if logits.dim() != 2 or at < 0 or ids.dim() != 2 or teacher.dim() != 2:
         raise ValueError("logits must be a CUDA tensor [tokens, vocab], ids and teacher [tokens, top]")
     tokens, vocab = logits.shape
-    device = logits.device
-    if ids.dtype is not torch.int32 or ids.device != device or teacher.device != device or ids.shape[0] != tokens or teacher.shape != ids.shape:
+    rows, top = ids.shape
+    if ids.dtype is not torch.int32 or ids.get_device() != at or teacher.get_device() != at or rows != tokens or teacher.shape != (rows, top):
         raise ValueError("ids must be int32, and ids and teacher [tokens, top] on the logits' device")
-    if logits.dtype not in _DT or teacher.dtype not in _DT:
+    code, teacher_code = _DT.get(logits.dtype), _DT.get(teacher.dtype)
+    if code is None or teacher_code is None:
         raise GacError(GAC_ERR_DTYPE, f"unsupported dtype {logits.dtype} or {teacher.dtype}")
-    if (logits.stride(1) != 1 and vocab > 1) or ((ids.stride(1) != 1 or teacher.stride(1) != 1) and ids.shape[1] > 1):
+    (z0, z1), (i0, i1), (t0, t1) = logits.stride(), ids.stride(), teacher.stride()
+    if (z1 != 1 and vocab > 1) or ((i1 != 1 or t1 != 1) and top > 1):
         raise ValueError("the last dimension must be contiguous")
-    if weights is not None and (weights.dtype is not torch.float32 or weights.device != device or weights.shape != (tokens,) or
+    if weights is not None and (weights.dtype is not torch.float32 or weights.get_device() != at or weights.shape != (tokens,) or
                                 not weights.is_contiguous()):
         raise ValueError("weights must be a contiguous float32 vector, one per token")
     if in_place and not grad:
         raise ValueError("only the gradient can be written in place")
-    raw, stream = _on(stream, device)
-    told = _empty(logits, (tokens,), stream, torch.float32) if loss else None
-    d = logits if in_place else _empty(logits, (tokens, vocab), stream) if grad else None
-    args = _DISTILL.pack(logits.data_ptr(), logits.stride(0), ids.data_ptr(), ids.stride(0), teacher.data_ptr(), teacher.stride(0),
-                         0 if weights is None else weights.data_ptr(), told.data_ptr() if loss else 0, 0 if d is None else d.data_ptr(),
-                         0 if d is None else d.stride(0), tokens, vocab, ids.shape[1], _DT[logits.dtype], _DT[teacher.dtype],
-                         DISTILL_KINDS[kind], temperature, 0)
-    _check(load_library().gac_distill(args, device.index, raw))
+    raw, stream = _on(stream, logits.device)
+    told, d, told_at, d_at, d0 = None, None, 0, 0, 0
+    if loss:
+        told = _empty(logits, (tokens,), stream, torch.float32)
+        told_at = told.data_ptr()
+    if grad:
+        d, d0 = (logits, z0) if in_place else (_empty_like(logits, stream), vocab)
+        d_at = d.data_ptr()
+    args = _DISTILL.pack(logits.data_ptr(), z0, ids.data_ptr(), i0, teacher.data_ptr(), t0, 0 if weights is None else weights.data_ptr(),
+                         told_at, d_at, d0, tokens, vocab, top, code, teacher_code, DISTILL_KINDS[kind], temperature, 0)
+    _check(load_library().gac_distill(args, at, raw))
     if in_place:
         torch.autograd.graph.increment_version(logits)
     return (told, d) if grad else told

@@ -637,7 +637,7 @@ int gac_distill(const gac_distill_args *args, int cuda_device, void *cuda_stream
     if (a.dtype == GAC_BF16) fn = grad ? distill_kernel<uint16_t, true> : distill_kernel<uint16_t, false>;
     else fn = grad ? distill_kernel<float, true> : distill_kernel<float, false>;
     static std::atomic<bool> allowed[4][64];   // once for each device
-    std::atomic<bool> *done = cuda_device < 64 ? &allowed[(grad ? 2 : 0) + (a.dtype == GAC_BF16)][cuda_device] : nullptr;
+    std::atomic<bool> *done = cuda_device >= 0 && cuda_device < 64 ? &allowed[(grad ? 2 : 0) + (a.dtype == GAC_BF16)][cuda_device] : nullptr;
     if (!done || !*done) {
         GAC_CUDA(nullptr, cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxSmem)));
         if (done) *done = true;

@@ -34,7 +34,7 @@ struct NormDev {
     int w_bf16;
     float eps, offset, inv_dim;
     uint32_t group;                   // lanes of a head: a power of two
-    uint32_t ctas_q;                  // CTAs that take query heads; the others take key heads
+    uint32_t ctas_q;                  // CTAs; on the way back those that take query heads, while the others take key heads
     uint32_t split[2];                // a token's heads are dealt out to so many groups of lanes
     long long x_token[2], x_head[2], y_token[2], y_head[2];   // RotaryDev's strides in bytes
     long long x_step[2], y_step[2], v_step[2];                // and from a head to the next one of the same lanes
@@ -109,24 +109,29 @@ __device__ __forceinline__ void turn(float2 (&v)[N], const float2 *a, const floa
     }
 }
 
-// The first ctas_q CTAs take query heads, the others key heads.  The lanes that share a head keep to one token, with its sines in
-// registers, and go through every `split`-th of its heads; what a thread will need next is on its way into its own places of a
-// ring in shared memory.  No two threads share anything but the sums over a head, and on the way back the last sum over the CTA.
+// The lanes that share a head keep to one token, with its sines in registers, and go through every `split`-th of its query heads and
+// then of its key heads; on the way back the first ctas_q CTAs take query heads and the others key heads, for there is no room for both
+// weights' gradients.  What a thread will need next is on its way into its own places of a ring in shared memory.  No two threads
+// share anything but the sums over a head, and on the way back the last sum over the CTA.
 template <typename T, int N, bool HALF, bool BACK>
 __global__ void __launch_bounds__(kThreads, BACK ? kBackCtas : kForwardCtas)
 norm_rotary_kernel(const __grid_constant__ RotaryDev a, const __grid_constant__ NormDev n) {
     constexpr int kBytes = N * int(sizeof(T)), kLoads = BACK ? 4 : 2, kStage = kLoads * kThreads * kBytes;
     extern __shared__ __align__(16) char dynamic[];
+    __shared__ long long steps[GAC_ROTARY_MAX_DIM / 2];      // 2^64 turns per position, of each pair
+    __shared__ float2 weights[2 * kMaxVectorDim];            // of each kind of heads: the places' 2 N elements
     if (BACK) let_next_start();
     const uint32_t ring = smem_addr(dynamic) + threadIdx.x * kBytes;
     const uint32_t groups = kThreads / n.group;
-    const int which = blockIdx.x >= n.ctas_q;
-    const uint32_t cta = which ? blockIdx.x - n.ctas_q : blockIdx.x, ctas = which ? gridDim.x - n.ctas_q : n.ctas_q;
-    const uint32_t heads = a.heads[which], split = n.split[which], rounds = (heads + split - 1) / split;
+    const bool keys = BACK && blockIdx.x >= n.ctas_q;
+    const uint32_t cta = keys ? blockIdx.x - n.ctas_q : blockIdx.x, ctas = keys ? gridDim.x - n.ctas_q : n.ctas_q;
+    const int kind0 = BACK ? keys : a.heads[0] == 0, kind1 = BACK ? keys : a.heads[1] != 0;
+    const uint32_t split = n.split[kind0];
     const uint32_t units = a.n_tokens * split, all = ctas * groups, unit0 = cta * groups + threadIdx.x / n.group;
     const uint32_t turns = (units + all - 1) / all;   // of units, as many for every group of lanes
     const Part at = part_of<N>(a, n);
     const uint32_t apart = (at.second - at.first) * uint32_t(sizeof(T));
+    auto rounds_of = [&](int kind) { return (a.heads[kind] + split - 1) / split; };
 
     auto fetch = [&](const char *row, uint32_t to) {
         auto copy = [&](uint32_t dst, const char *src) {
@@ -136,31 +141,33 @@ norm_rotary_kernel(const __grid_constant__ RotaryDev a, const __grid_constant__ 
         if (at.here) copy(to, row);
         if (at.both) copy(to + kThreads * kBytes, row + apart);
     };
-    // what comes in next: a round of a unit
-    uint32_t f_turn = 0, f_round = 0, f_head = 0;
+    // what comes in next: a round of a kind of heads of a unit
+    uint32_t f_turn = 0, f_left = 0, f_head = 0;
+    int f_kind = kind0;
     bool f_live = false;
     const char *f_x = nullptr, *f_v = nullptr;
     auto issue = [&](uint32_t slot) {
         if (f_turn < turns) {
-            if (f_round == 0) {
+            if (f_left == 0) {
                 const uint32_t unit = unit0 + f_turn * all;
                 const long long t = unit / split;
+                f_left = rounds_of(f_kind);
                 f_live = unit < units;
                 f_head = unit % split;
-                f_x = a.x[which] + t * n.x_token[which] + (long long)f_head * n.x_head[which] + at.first * sizeof(T);
-                if (BACK) f_v = n.v[which] + t * n.v_token[which] + (long long)f_head * n.v_head[which] + at.first * sizeof(T);
+                f_x = a.x[f_kind] + t * n.x_token[f_kind] + (long long)f_head * n.x_head[f_kind] + at.first * sizeof(T);
+                if (BACK) f_v = n.v[f_kind] + t * n.v_token[f_kind] + (long long)f_head * n.v_head[f_kind] + at.first * sizeof(T);
             }
-            if (f_live && f_head < heads) {
+            if (f_live && f_head < a.heads[f_kind]) {
                 const uint32_t to = ring + slot * kStage;
                 fetch(f_x, to);
                 if (BACK) fetch(f_v, to + 2 * kThreads * kBytes);
             }
             f_head += split;
-            f_x += n.x_step[which];
-            if (BACK) f_v += n.v_step[which];
-            if (++f_round == rounds) {
-                f_round = 0;
-                ++f_turn;
+            f_x += n.x_step[f_kind];
+            if (BACK) f_v += n.v_step[f_kind];
+            if (--f_left == 0) {
+                f_turn += f_kind == kind1;
+                f_kind = f_kind == kind1 ? kind0 : kind1;
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -172,21 +179,29 @@ norm_rotary_kernel(const __grid_constant__ RotaryDev a, const __grid_constant__ 
 #pragma unroll
     for (int i = 0; i < kRing; ++i) issue(i);
 
-    // the place's weights, two elements each
+    for (uint32_t i = threadIdx.x; i < a.pairs; i += kThreads) steps[i] = __double2ll_rn((a.turns[i] - rint(a.turns[i])) * 18446744073709551616.0);
+    for (uint32_t k = threadIdx.x / n.group; k < 2; k += groups)
+        for (int i = 0; i < N; ++i) {
+            const bool there = i < N / 2 ? at.here : at.both;
+            const uint32_t e = i < N / 2 ? at.first + 2 * i : at.second + 2 * i - N;
+            weights[(k * n.group + at.u) * N + i] = there ? make_float2(weight_at(n, k, e), weight_at(n, k, e + 1)) : make_float2(0.f, 0.f);
+        }
+    __syncthreads();
     float2 w[N];
+    auto weigh = [&](int kind) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const bool there = i < N / 2 ? at.here : at.both;
-        const uint32_t e = i < N / 2 ? at.first + 2 * i : at.second + 2 * i - N;
-        w[i] = there ? make_float2(weight_at(n, which, e), weight_at(n, which, e + 1)) : make_float2(0.f, 0.f);
-    }
+        for (int i = 0; i < N; ++i) w[i] = weights[(kind * n.group + at.u) * N + i];
+    };
+    if (BACK) weigh(kind0);
+
     float2 dw[BACK ? N : 1] = {};
     uint32_t slot = 0;
     for (uint32_t step = 0; step < turns; ++step) {
         const uint32_t unit = unit0 + step * all, t = unit / split;
         const bool live = unit < units;
-        // x -> a x - b y, y -> c x + d y, forward with the weights in them; what is not turned stays as it is
-        float2 ma[N / 2], mb[N / 2], mc[BACK ? 1 : N / 2], md[BACK ? 1 : N / 2];
+        // cosines and sines of the place's pairs; what is not turned stays as it is.  The angle is a whole number of 2^-64 turns,
+        // so whole turns fall away by themselves
+        float2 cosines[N / 2], sines[N / 2];
         const int place = live && at.turn && !a.positions ? place_in_sequence(a.cu, a.n_seqs, t) : 0;
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
@@ -195,65 +210,75 @@ norm_rotary_kernel(const __grid_constant__ RotaryDev a, const __grid_constant__ 
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const uint32_t k = 2 * i + j, pair = HALF ? at.u * N + k : (k < N / 2 ? 0 : a.pairs / 2 - N / 2) + at.u * (N / 2) + k;
-                    cs[j] = turn_of(a, pair, a.positions ? position_on_axis(a, pair, t) : place);
+                    const long long angle = steps[pair] * (a.positions ? position_on_axis(a, pair, t) : place);
+                    float s, c;
+                    sincospif(float(int(angle >> 32)) * 4.656612873077393e-10f, &s, &c);   // 2^-31: halves of a turn
+                    cs[j] = make_float2(c * a.scale, s * a.scale);
                 }
-            const float2 c = make_float2(cs[0].x, cs[1].x), s = make_float2(cs[0].y, cs[1].y);
-            if constexpr (BACK) {
-                ma[i] = c;
-                mb[i] = s;
-            } else {
-                const float2 wx = HALF ? w[i] : make_float2(w[2 * i].x, w[2 * i + 1].x), wy = HALF ? w[N / 2 + i] : make_float2(w[2 * i].y, w[2 * i + 1].y);
-                ma[i] = mul2(c, wx);
-                mb[i] = mul2(make_float2(-s.x, -s.y), wy);
-                mc[i] = mul2(s, wx);
-                md[i] = mul2(c, wy);
-            }
+            cosines[i] = make_float2(cs[0].x, cs[1].x);
+            sines[i] = make_float2(cs[0].y, cs[1].y);
         }
-        uint32_t h = unit % split;
-        char *to = a.y[which] + (long long)t * n.y_token[which] + (long long)h * n.y_head[which] + at.first * sizeof(T);
-        for (uint32_t round = 0; round < rounds; ++round, h += split, to += n.y_step[which]) {
-            float2 v[N], squares = make_float2(0.f, 0.f);
-            const uint32_t from = ring + slot * kStage;
-            const bool here = live && h < heads;
-            asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+        for (int kind = kind0; kind <= kind1; ++kind) {
+            // x -> a x - b y, y -> c x + d y, forward with the weights in them
+            float2 ma[BACK ? 1 : N / 2], mb[BACK ? 1 : N / 2], mc[BACK ? 1 : N / 2], md[BACK ? 1 : N / 2];
             if constexpr (!BACK) {
-                take<T, N>(from, v);
-                take<T, N>(from + kThreads * kBytes, v + N / 2);
-                issue(slot);
+                weigh(kind);
 #pragma unroll
-                for (int j = 0; j < N; ++j) squares = fma2(v[j], v[j], squares);
-                const float r = rsqrtf(fmaf(add_lanes(squares.x + squares.y, n.group), n.inv_dim, n.eps));
-#pragma unroll
-                for (int j = 0; j < N; ++j) v[j] = mul2(v[j], make_float2(r, r));
-                turn<N, HALF>(v, ma, mb, mc, md);
-            } else {
-                float2 b[N], bw[N], dot = squares, minus[N / 2];
-                take<T, N>(from, b);
-                take<T, N>(from + kThreads * kBytes, b + N / 2);
-                take<T, N>(from + 2 * kThreads * kBytes, v);
-                take<T, N>(from + 3 * kThreads * kBytes, v + N / 2);
-                issue(slot);
-#pragma unroll
-                for (int i = 0; i < N / 2; ++i) minus[i] = make_float2(-mb[i].x, -mb[i].y);
-                turn<N, HALF>(b, ma, mb, minus, ma);   // by the negative angle
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    bw[j] = mul2(b[j], w[j]);
-                    squares = fma2(v[j], v[j], squares);
-                    dot = fma2(bw[j], v[j], dot);
+                for (int i = 0; i < N / 2; ++i) {
+                    const float2 wx = HALF ? w[i] : make_float2(w[2 * i].x, w[2 * i + 1].x), wy = HALF ? w[N / 2 + i] : make_float2(w[2 * i].y, w[2 * i + 1].y);
+                    ma[i] = mul2(cosines[i], wx);
+                    mb[i] = mul2(make_float2(-sines[i].x, -sines[i].y), wy);
+                    mc[i] = mul2(sines[i], wx);
+                    md[i] = mul2(cosines[i], wy);
                 }
-                const float r = rsqrtf(fmaf(add_lanes(squares.x + squares.y, n.group), n.inv_dim, n.eps));
-                const float c = -(add_lanes(dot.x + dot.y, n.group) * n.inv_dim * r * r);
-                const float2 rr = make_float2(r, r);
-                if (here)
-#pragma unroll
-                    for (int j = 0; j < N; ++j) dw[j] = fma2(b[j], mul2(v[j], rr), dw[j]);
-#pragma unroll
-                for (int j = 0; j < N; ++j) v[j] = mul2(rr, fma2(v[j], make_float2(c, c), bw[j]));
             }
-            slot = slot + 1 == kRing ? 0 : slot + 1;
-            if (here && at.here) put<T, N>(to, v);
-            if (here && at.both) put<T, N>(to + apart, v + N / 2);
+            const uint32_t heads = a.heads[kind], rounds = rounds_of(kind);
+            uint32_t h = unit % split;
+            char *to = a.y[kind] + (long long)t * n.y_token[kind] + (long long)h * n.y_head[kind] + at.first * sizeof(T);
+            for (uint32_t round = 0; round < rounds; ++round, h += split, to += n.y_step[kind]) {
+                float2 v[N], squares = make_float2(0.f, 0.f);
+                const uint32_t from = ring + slot * kStage;
+                const bool here = live && h < heads;
+                asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+                if constexpr (!BACK) {
+                    take<T, N>(from, v);
+                    take<T, N>(from + kThreads * kBytes, v + N / 2);
+                    issue(slot);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) squares = fma2(v[j], v[j], squares);
+                    const float r = rsqrtf(fmaf(add_lanes(squares.x + squares.y, n.group), n.inv_dim, n.eps));
+#pragma unroll
+                    for (int j = 0; j < N; ++j) v[j] = mul2(v[j], make_float2(r, r));
+                    turn<N, HALF>(v, ma, mb, mc, md);
+                } else {
+                    float2 b[N], bw[N], dot = squares, minus[N / 2];
+                    take<T, N>(from, b);
+                    take<T, N>(from + kThreads * kBytes, b + N / 2);
+                    take<T, N>(from + 2 * kThreads * kBytes, v);
+                    take<T, N>(from + 3 * kThreads * kBytes, v + N / 2);
+                    issue(slot);
+#pragma unroll
+                    for (int i = 0; i < N / 2; ++i) minus[i] = make_float2(-sines[i].x, -sines[i].y);
+                    turn<N, HALF>(b, cosines, sines, minus, cosines);   // by the negative angle
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        bw[j] = mul2(b[j], w[j]);
+                        squares = fma2(v[j], v[j], squares);
+                        dot = fma2(bw[j], v[j], dot);
+                    }
+                    const float r = rsqrtf(fmaf(add_lanes(squares.x + squares.y, n.group), n.inv_dim, n.eps));
+                    const float c = -(add_lanes(dot.x + dot.y, n.group) * n.inv_dim * r * r);
+                    const float2 rr = make_float2(r, r);
+                    if (here)
+#pragma unroll
+                        for (int j = 0; j < N; ++j) dw[j] = fma2(b[j], mul2(v[j], rr), dw[j]);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) v[j] = mul2(rr, fma2(v[j], make_float2(c, c), bw[j]));
+                }
+                slot = slot + 1 == kRing ? 0 : slot + 1;
+                if (here && at.here) put<T, N>(to, v);
+                if (here && at.both) put<T, N>(to + apart, v + N / 2);
+            }
         }
     }
     if constexpr (BACK) {
@@ -424,28 +449,42 @@ Layout lay_out(const RotaryDev &d, NormDev &n, uint32_t elements, uint32_t size,
     n.group = 1;
     while (n.group * 2 * elements < d.head_dim) n.group *= 2;
     const uint32_t groups = kThreads / n.group, most = 148 * (back ? kBackCtas : kForwardCtas);
-    // CTAs are shared out by heads, with a token's sines counted as three of them.  A token's heads stay with one group of lanes, or are
-    // split where that would leave CTAs idle; and no more CTAs than it takes for all to have the same number of units.
-    const uint32_t cost[2] = {d.heads[0] ? d.heads[0] + 3 : 0, d.heads[1] ? d.heads[1] + 3 : 0};
-    uint32_t grid = 0;
-    for (int w = 0; w < 2; ++w) {
-        uint32_t ctas = 0, split = 1;
-        if (d.heads[w]) {
-            ctas = std::max(1u, most * cost[w] / (cost[0] + cost[1]));
-            while (split < groups && split < d.heads[w] && uint64_t(d.n_tokens) * split < uint64_t(ctas) * groups) split *= 2;
-            const uint64_t units = uint64_t(d.n_tokens) * split, turns = (units + uint64_t(ctas) * groups - 1) / (uint64_t(ctas) * groups);
-            ctas = uint32_t(((units + turns - 1) / turns + groups - 1) / groups);
+    // Into how many groups of lanes a token's heads are split: what a group has to do is to be least, `turns` tokens with their sines,
+    // which take about as long as kSines heads; and no more CTAs than it takes for all to have the same number of tokens.
+    const uint32_t kSines = back ? 4 : 8;
+    auto share_out = [&](uint32_t ctas, uint32_t heads0, uint32_t heads1, uint32_t *split) {
+        uint64_t least = ~uint64_t(0), most_turns = 1;
+        for (uint32_t s = 1; s <= groups && s < 2 * std::max(heads0, heads1); s *= 2) {
+            const uint64_t turns = (uint64_t(d.n_tokens) * s + uint64_t(ctas) * groups - 1) / (uint64_t(ctas) * groups);
+            const uint64_t work = turns * ((heads0 + s - 1) / s + (heads1 + s - 1) / s + kSines);
+            if (work >= least) continue;
+            least = work;
+            most_turns = turns;
+            *split = s;
         }
-        if (w == 0) n.ctas_q = ctas;
-        grid += ctas;
-        n.split[w] = split;
+        return uint32_t(((uint64_t(d.n_tokens) * *split + most_turns - 1) / most_turns + groups - 1) / groups);
+    };
+    uint32_t grid = 0;
+    if (back) {
+        // CTAs are shared out to the kinds by what a token of each takes
+        const uint32_t cost[2] = {d.heads[0] ? d.heads[0] + kSines : 0, d.heads[1] ? d.heads[1] + kSines : 0};
+        for (int w = 0; w < 2; ++w) {
+            n.split[w] = 1;
+            if (d.heads[w]) grid += share_out(std::max(1u, most * cost[w] / (cost[0] + cost[1])), d.heads[w], 0, &n.split[w]);
+            if (w == 0) n.ctas_q = grid;
+        }
+    } else {
+        n.ctas_q = grid = share_out(most, d.heads[0], d.heads[1], &n.split[0]);
+        n.split[1] = n.split[0];
+    }
+    for (int w = 0; w < 2; ++w) {
         n.x_token[w] = d.x_token[w] * size;
         n.x_head[w] = d.x_head[w] * size;
         n.y_token[w] = d.y_token[w] * size;
         n.y_head[w] = d.y_head[w] * size;
-        n.x_step[w] = n.x_head[w] * split;
-        n.y_step[w] = n.y_head[w] * split;
-        n.v_step[w] = back ? n.v_head[w] * split : 0;
+        n.x_step[w] = n.x_head[w] * n.split[w];
+        n.y_step[w] = n.y_head[w] * n.split[w];
+        n.v_step[w] = back ? n.v_head[w] * n.split[w] : 0;
     }
     return Layout{grid, uint32_t(kRing) * (back ? 4 : 2) * kThreads * elements * size};
 }

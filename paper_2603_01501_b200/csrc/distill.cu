@@ -38,17 +38,19 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-// Threads of a CTA, CTAs of an SM, and the ring: groups of vectors that a thread loads at once.
-template <bool GRAD>
+// Threads of a CTA, CTAs of an SM, and the ring: groups of vectors that a thread loads at once.  Short rows take smaller CTAs: what
+// a row takes beside its loads is the same for all, and more rows at once cover it (4096 rows of 64 kB with the gradient 111 us, with
+// the other shape 116; values alone 53 and 79; 2048 rows of 304 kB, values alone, 111 and 105).
+template <bool GRAD, bool SHORT>
 struct Shape {
-    static constexpr int kThreads = GRAD ? 256 : 384, kCtas = GRAD ? 4 : 3, kWarps = kThreads / 32;
-    static constexpr int kFlight = GRAD ? 3 : 4, kRing = GRAD ? 4 : 2, kRingBytes = kRing * kFlight * kThreads * 16;
+    static constexpr int kThreads = SHORT ? 128 : GRAD ? 256 : 384, kCtas = SHORT ? 8 : GRAD ? 4 : 3, kWarps = kThreads / 32;
+    static constexpr int kFlight = !SHORT && GRAD ? 3 : 4, kRing = !SHORT && GRAD ? 4 : 2, kRingBytes = kRing * kFlight * kThreads * 16;
 };
 constexpr uint32_t kMaxSplit = 8;      // CTAs of a row: a portable cluster
 constexpr uint64_t kInUse = 96u << 20; // bytes of rows in use at once, of 126 MB of L2
 // The ring, the most named tokens, and marks: a byte to 16 bytes of a row, or, where it is split, of an eighth of it.
-constexpr size_t kMaxSmem = Shape<false>::kRingBytes + GAC_DISTILL_MAX_TOP * 28 + GAC_DISTILL_MAX_ROW_BYTES / 16 + 16;
-static_assert(kMaxSmem <= 224 * 1024 && Shape<true>::kRingBytes <= Shape<false>::kRingBytes, "fits an SM");
+constexpr size_t kMaxSmem = Shape<false, false>::kRingBytes + GAC_DISTILL_MAX_TOP * 28 + GAC_DISTILL_MAX_ROW_BYTES / 16 + 16;
+static_assert(kMaxSmem <= 224 * 1024 && Shape<true, false>::kRingBytes <= Shape<false, false>::kRingBytes, "fits an SM");
 constexpr float kMasked = -1e38f;      // tokens with no logit above this are taken as masked
 
 struct DistillDev {
@@ -242,11 +244,11 @@ __device__ __forceinline__ Span span_of(const DistillDev &a, uint32_t t, uint32_
     return s;
 }
 
-template <typename T, bool GRAD>
-__global__ void __launch_bounds__(Shape<GRAD>::kThreads, Shape<GRAD>::kCtas)
+template <typename T, bool GRAD, bool SHORT>
+__global__ void __launch_bounds__(Shape<GRAD, SHORT>::kThreads, Shape<GRAD, SHORT>::kCtas)
 distill_kernel(const __grid_constant__ DistillDev a) {
     using Vec = Vector<T>;
-    using C = Shape<GRAD>;
+    using C = Shape<GRAD, SHORT>;
     constexpr int N = Vec::N, kThreads = C::kThreads, kWarps = C::kWarps, kFlight = C::kFlight, kRing = C::kRing;
     constexpr uint32_t kNowhere = 0xFFFFFFFFu;
     extern __shared__ __align__(16) char dynamic[];
@@ -549,6 +551,22 @@ distill_kernel(const __grid_constant__ DistillDev a) {
     asm volatile("cp.async.wait_all;" ::: "memory");   // of a row without entries the first loads may still be on their way
 }
 
+struct Launch {
+    void (*kernel)(const DistillDev);
+    uint32_t threads, ctas;
+    size_t ring;
+};
+template <typename T, bool GRAD, bool SHORT>
+Launch launch_with() {
+    using C = Shape<GRAD, SHORT>;
+    return {distill_kernel<T, GRAD, SHORT>, C::kThreads, C::kCtas, C::kRingBytes};
+}
+template <typename T>
+Launch launch_for(bool grad, bool brief) {
+    return grad ? (brief ? launch_with<T, true, true>() : launch_with<T, true, false>()) : (brief ? launch_with<T, false, true>() : launch_with<T, false, false>());
+}
+Launch launch_of(bool bf16, bool grad, bool brief) { return bf16 ? launch_for<uint16_t>(grad, brief) : launch_for<float>(grad, brief); }
+
 int fail(std::nullptr_t, int code, const char *fmt, const char *a = "", long long b = 0) {
     snprintf(g_init_err, sizeof(g_init_err), fmt, a, b);
     return code;
@@ -619,32 +637,40 @@ int gac_distill(const gac_distill_args *args, int cuda_device, void *cuda_stream
     d.c = float(M_LOG2E / a.temperature);
     d.c_off = (M_LOG2E / a.temperature - double(d.c)) * M_LN2;
     const uint32_t vec = 16 / uint32_t(size), vectors = (a.vocab + 2 * vec - 2) / vec;   // at most, wherever a row starts
-    // Parts of a row: so many that the rows in use at once, of all resident CTAs, stay in L2 between the two passes (4096 rows
-    // of 304 kB: 505 us with one part, 451 with two, whose CTAs wait for each other; 8191 rows of 128 kB: 323 and 367), and
-    // that few rows still use all SMs, as long as a part has some thousands of elements.
     const bool grad = a.d_logits != nullptr;
-    const uint32_t resident = 148 * (grad ? Shape<true>::kCtas : Shape<false>::kCtas);
+    const uint64_t row = uint64_t(a.vocab) * size;
+    const bool brief = row <= (grad ? kInUse / (148 * Shape<true, true>::kCtas) : 256u << 10);   // short rows
+    const Launch shape = launch_of(a.dtype == GAC_BF16, grad, brief);
+    // Parts of a row: what takes least, by 44 bytes a nanosecond and SM, and by the chain from a row's last load to its first gradient
+    // (5 us, with the gradient 8, where parts wait for each other 1.5 more).  With the gradient so many that the rows in use
+    // at once stay in L2 between the two passes (4096 rows of 304 kB: 504 us with one part, 474 with two; 8191 rows of 128 kB, which
+    // fit whole: 323 and 371).
     d.split = 1;
-    while (d.split < kMaxSplit && ((grad && uint64_t(resident / d.split) * a.vocab * size > kInUse) ||
-                                   (uint64_t(a.n_tokens) * d.split < resident && a.vocab / (2 * d.split) >= 4096)))
-        d.split *= 2;
+    double least = INFINITY;
+    for (uint32_t split = 1; split <= kMaxSplit; split *= 2) {
+        const bool fits = !grad || uint64_t(148 * shape.ctas / split) * row <= kInUse || uint64_t(a.n_tokens) * row <= kInUse;
+        if (!fits && split < kMaxSplit) continue;
+        const uint64_t per_sm = (uint64_t(a.n_tokens) * split + 147) / 148, waves = (per_sm + shape.ctas - 1) / shape.ctas;
+        const double time = double(per_sm) * double(row * (grad ? 2 : 1)) / split / 44.0 + double(waves) * ((grad ? 8000.0 : 5000.0) + (split > 1 ? 1500.0 : 0.0));
+        if (time < least) {
+            least = time;
+            d.split = split;
+        }
+    }
     d.mark_words = ((vectors + d.split - 1) / d.split + 3) / 4;
-    const size_t smem = size_t(grad ? Shape<true>::kRingBytes : Shape<false>::kRingBytes) + size_t(a.top) * 28 + size_t(d.mark_words) * 4;
+    const size_t smem = shape.ring + size_t(a.top) * 28 + size_t(d.mark_words) * 4;
     Range range("gac_distill");
     DeviceGuard guard(cuda_device);
     if (!guard.ok) return fail(nullptr, GAC_ERR_CUDA, "cudaSetDevice failed%s");
-    void (*fn)(const DistillDev) = nullptr;
-    if (a.dtype == GAC_BF16) fn = grad ? distill_kernel<uint16_t, true> : distill_kernel<uint16_t, false>;
-    else fn = grad ? distill_kernel<float, true> : distill_kernel<float, false>;
-    static std::atomic<bool> allowed[4][64];   // once for each device
-    std::atomic<bool> *done = cuda_device >= 0 && cuda_device < 64 ? &allowed[(grad ? 2 : 0) + (a.dtype == GAC_BF16)][cuda_device] : nullptr;
+    static std::atomic<bool> allowed[8][64];   // once for each device
+    std::atomic<bool> *done = cuda_device >= 0 && cuda_device < 64 ? &allowed[(a.dtype == GAC_BF16) + 2 * grad + 4 * brief][cuda_device] : nullptr;
     if (!done || !*done) {
-        GAC_CUDA(nullptr, cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxSmem)));
+        GAC_CUDA(nullptr, cudaFuncSetAttribute(shape.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxSmem)));
         if (done) *done = true;
     }
     cudaLaunchConfig_t how = {};
     how.gridDim = dim3(a.n_tokens * d.split);
-    how.blockDim = dim3(grad ? Shape<true>::kThreads : Shape<false>::kThreads);
+    how.blockDim = dim3(shape.threads);
     how.dynamicSmemBytes = smem;
     how.stream = static_cast<cudaStream_t>(cuda_stream);
     cudaLaunchAttribute attr[1];
@@ -653,7 +679,7 @@ int gac_distill(const gac_distill_args *args, int cuda_device, void *cuda_stream
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     how.attrs = attr;
     how.numAttrs = 1;
-    GAC_CUDA(nullptr, cudaLaunchKernelEx(&how, fn, d));
+    GAC_CUDA(nullptr, cudaLaunchKernelEx(&how, shape.kernel, d));
     return GAC_OK;
 }
 

@@ -137,6 +137,26 @@ def test_offsets_past_32_bits():
     assert torch.equal(q, want)
 
 
+@pytest.mark.parametrize("dim", [128, 66])
+def test_far_positions_are_as_exact_as_near_ones(dim):
+    freqs = gb.gac_rotary_freqs(dim // 4 * 2, 1e4)
+    freqs[1], freqs[2] = -0.37, 1e6                            # turns back, and many whole turns
+    pos = torch.tensor([0, 1, 131_071, 1_000_003, 2 ** 31 - 1, -1, -70_001, -2 ** 31], dtype=torch.int32, device="cuda")
+    q, w = randn((8, 2, dim), F, 7), randn((dim,), F, 8)
+    y, _ = gb.gac_norm_rotary(q, None, w, None, freqs, positions=pos)
+    # the reference's own angle: a product of a 31-bit position with a frequency of so many turns, in binary64, and the frequency's
+    # own rounding to turns
+    turns = torch.from_numpy(freqs).cuda().abs() / (2 * math.pi)
+    off = 2 * math.pi * 3 * 2.0 ** -53 * pos.double().abs()[:, None] * turns
+    want, bound = ref.norm(q, w, ref.wheel(pos.double(), torch.from_numpy(freqs).cuda()), "half", 1.0, 1e-6, 0.0)
+    n = (q.double() * torch.rsqrt(q.double().square().mean(-1, keepdim=True) + 1e-6) * w.double()).abs()
+    r = freqs.size
+    # an angle off by e moves x cos a - y sin a by at most e |x sin a + y cos a| <= e (|x| + |y|), and so the other
+    both = off[:, None] * (n[..., :r] + n[..., r:2 * r])
+    bound[..., :2 * r] += torch.cat((both, both), -1)
+    within(y, want, bound)
+
+
 @pytest.mark.parametrize("dim", [64, 30])
 def test_values_at_the_edge(dim):
     pos = torch.zeros(6, dtype=torch.int32, device="cuda")

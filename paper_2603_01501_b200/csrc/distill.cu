@@ -18,7 +18,10 @@
 // evict-last, read again and written with evict-first, and cut into so many parts that the rows in use fit.  Loads go through a
 // ring in shared memory, because what bounds the kernel is bytes in flight beside the chain from a row's last load to its first
 // gradient (sums over the CTA, exponentials and logarithms in binary64, about 5 us), which the SM's other CTAs have to cover.
-// Measured: @.
+// Measured, ten calls after a pause: 4096 x 151936 bfloat16 with the gradient 444 us (5.6 TB/s of one read and one write, 0.87 of a
+// plain copy's rate; memory reads the logits 1.13 times), 8191 x 32000 float32, a quarter without a teacher, 324 (0.88), 2048 x 151936
+// values alone 105 (0.92).  In a second of calls on end, under the power cap, 497, 336 and 113.  A row held in the shared memory of eight
+// CTAs took 618 instead of 444, and persistent CTAs that read the next row while parts of the last are exchanged 1490.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 #include <float.h>

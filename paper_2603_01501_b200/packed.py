@@ -14,6 +14,10 @@ cu_seqlens[b] .. cu_seqlens[b+1].
 All arithmetic is in the CUDA library (``binding``); this module only says what is saved for the way back.  These are
 autograd functions, not registered torch operators: they have no fake kernels, batching rules or forward mode, and a
 compiled policy breaks its graph at them.
+
+A step that is captured into a CUDA graph holds its forward and its backward pass, and as with any autograd function no loss or
+output of an earlier, uncaptured pass over the same leaves may still be alive then: autograd would order the captured
+gradients behind the stream of that pass, which cannot be captured.
 """
 from __future__ import annotations
 

@@ -124,16 +124,20 @@ struct Vector {
     }
 };
 
-// Sums of exponentials are kept as multiples of 2^level, level a whole number, so that they are brought together exactly.
-__device__ __forceinline__ float level_of(float m, float c) { return rintf(fminf(fmaxf(m * c, -FLT_MAX), FLT_MAX)); }
+// Sums of exponentials are kept as multiples of 2^level, level a whole number next to the product of the largest logit and c, so that
+// they are brought together exactly.  Up to kFar a rounded product is off by at most 64, so that no power leaves binary32.  Levels
+// stop there: what is masked far below adds nothing to a sum that ordinary logits are in, and a row whose own largest is beyond is a far row.
+constexpr float kFar = 2147483648.0f;
+__device__ __forceinline__ float level_of(float m, float c) { return rintf(fminf(fmaxf(m * c, -kFar), kFar)); }
+__device__ __forceinline__ bool is_far(float m, float c) { return fabsf(m * c) > kFar; }
 __device__ __forceinline__ double power_of_two(float whole) {   // 0 or less
     return whole < -1000.0f ? 0.0 : __hiloint2double((1023 + int(whole)) << 20, 0);
 }
 // What a CTA, or a warp, knows of its part of the row.
 struct Partial {
     double mass, cost;          // top: sum of e, of e (log e - z); else: sum of p, of p (log p - z)
-    double named, named_cost;   // sum over named tokens of exp(z), of exp(z) (z - log p), in units of 2^level
-    float level;
+    double named, named_cost;   // sum over named tokens of exp(z), of exp(z) (z - log p), in units of 2^level_of(named_m)
+    float named_m;              // their largest logit
     float m, s;                 // of the others the largest logit, and the sum of exp(z) in units of 2^level_of(m)
 };
 // What the gradient needs of the whole row.
@@ -143,6 +147,8 @@ struct Row {
     double loss, weight;
     float unit;
     float level, others;        // elsewhere: 2^(logit c - level) others
+    float m, named_m;           // the largest logits, elsewhere and of named tokens
+    int far;
 };
 
 template <typename F>
@@ -159,35 +165,44 @@ __device__ __forceinline__ float max_lanes(float x, int from) {
 // No part at all.
 __device__ __forceinline__ Partial no_part() {
     Partial p = {};
-    p.m = p.level = -FLT_MAX;
+    p.m = p.named_m = -FLT_MAX;
     return p;
 }
 // The sum of `n` parts, a power of two, one to a lane of every n, in all lanes.
 __device__ __forceinline__ Partial add_parts(Partial p, const DistillDev &a, int n) {
-    const float m = max_lanes(p.m, n / 2), level = max_lanes(p.level, n / 2);
+    const float m = max_lanes(p.m, n / 2), named_m = max_lanes(p.named_m, n / 2);
     p.s = add_lanes(p.s * exp2_approx(level_of(p.m, a.c) - level_of(m, a.c)), n / 2);
-    const double f = power_of_two(p.level - level);
+    const double f = power_of_two(level_of(p.named_m, a.c) - level_of(named_m, a.c));
     p.mass = add_lanes(p.mass, n / 2);
     p.cost = add_lanes(p.cost, n / 2);
     p.named = add_lanes(p.named * f, n / 2);
     p.named_cost = add_lanes(p.named_cost * f, n / 2);
     p.m = m;
-    p.level = level;
+    p.named_m = named_m;
     return p;
 }
 
 // The row's numbers from the sum of its parts, by a whole warp: what the gradient outside N needs first (`rest` and `s` for the rest).
 struct Sums {
     double s, f_rest, f_named, p_rest;
+    double unit, rest_unit;     // logarithms: of what total is a multiple of, and of what s is, relative to it
     bool rest;
 };
+__device__ __forceinline__ bool has_rest(const Partial &p) { return p.m > kMasked || p.s != p.s; }   // a NaN is not masked
+// Whether the largest logit of what counts is beyond the levels: m outside N, named_m in it.
+__device__ __forceinline__ bool far_row(const DistillDev &a, float m, float named_m) {
+    return (m > kMasked ? is_far(m, a.c) : is_far(named_m, a.c)) || named_m * a.c > kFar;
+}
 __device__ __forceinline__ Sums start(const DistillDev &a, const Partial &p, Row &r) {
     Sums x;
-    x.rest = p.m > kMasked || p.s != p.s;   // a NaN is not masked
+    x.rest = has_rest(p);
+    const float named_level = level_of(p.named_m, a.c);
     r.level = level_of(p.m, a.c);
-    r.unit = x.rest ? fmaxf(p.level, r.level) : p.level;
+    r.unit = x.rest ? fmaxf(named_level, r.level) : named_level;
+    x.unit = double(r.unit) * M_LN2;
+    x.rest_unit = double(r.level - r.unit) * M_LN2;
     x.f_rest = x.rest ? power_of_two(r.level - r.unit) : 0.0;
-    x.f_named = power_of_two(p.level - r.unit);
+    x.f_named = power_of_two(named_level - r.unit);
     // powers were taken of logit c, and c is rounded: near the largest logit they are off by this
     const double off = double(p.m) * a.c_off;
     x.s = !x.rest ? 0.0 : double(p.s) * (fabs(off) < 0.01 ? 1.0 + off * (1.0 + off * (0.5 + off * (1.0 / 6.0))) : exp(off));
@@ -210,8 +225,8 @@ __device__ __forceinline__ void finish_loss(const DistillDev &a, const Partial &
     const uint32_t all = 0xFFFFFFFFu, which = threadIdx.x & 3;
     const double l = log(which == 0 ? r.total : which == 1 ? x.s : which == 2 ? x.p_rest : p.mass);
     const double log_total = __shfl_sync(all, l, 0), log_s = __shfl_sync(all, l, 1), log_p_rest = __shfl_sync(all, l, 2), log_mass = __shfl_sync(all, l, 3);
-    r.lse = double(r.unit) * M_LN2 + log_total;
-    const double log_q_rest = x.rest ? double(r.level - r.unit) * M_LN2 + log_s - log_total : 0.0;
+    r.lse = x.unit + log_total;
+    const double log_q_rest = x.rest ? x.rest_unit + log_s - log_total : 0.0;
     if (a.kind == GAC_DISTILL_TOP) {
         r.loss = p.cost / p.mass - log_mass + r.lse;
     } else if (a.kind == GAC_DISTILL_FORWARD) {
@@ -247,30 +262,200 @@ __device__ __forceinline__ Span span_of(const DistillDev &a, uint32_t t, uint32_
     return s;
 }
 
+// The named tokens of a CTA's part, in its dynamic shared memory: p, or e of it; exp(z); the logit, what the teacher says, the place in
+// the row (kNowhere: not of this part, or absent); then a byte to a vector, a bit to an element: which are named.
+constexpr uint32_t kNowhere = 0xFFFFFFFFu;
+struct Named {
+    double *p, *q;
+    float *z, *l;
+    uint32_t *at, *marks;
+    __device__ __forceinline__ Named(char *from, uint32_t top) {
+        p = reinterpret_cast<double *>(from);
+        q = p + top;
+        z = reinterpret_cast<float *>(q + top);
+        l = z + top;
+        at = reinterpret_cast<uint32_t *>(l + top);
+        marks = at + top;
+    }
+};
+// A warp's share of them, with z = (logit - base) / temperature and exp(z) in units of exp(unit); `most`: the largest that the teacher says.
+__device__ __forceinline__ Partial add_named(const DistillDev &a, const Named &e, uint32_t threads, float most, double base, double unit) {
+    Partial mine = {};
+    for (uint32_t i = threadIdx.x; i < a.top; i += threads) {
+        if (e.at[i] == kNowhere) continue;
+        const double z = (double(e.z[i]) - base) * a.inv_temp, says = e.l[i];
+        const double log_p = a.kind == GAC_DISTILL_TOP ? (says - double(most)) * a.inv_temp : says;
+        const double p = exp(log_p), q = exp(z - unit);
+        e.p[i] = p;
+        e.q[i] = q;
+        mine.mass += p;
+        mine.cost += p > 0.0 ? p * (log_p - z) : p;     // 0 log 0 = 0; a NaN stays one
+        mine.named += q;
+        mine.named_cost += q > 0.0 ? q * (z - log_p) : q;
+    }
+    if (__any_sync(0xFFFFFFFFu, mine.named != 0.0 || mine.mass != 0.0)) {
+        mine.mass = add_lanes(mine.mass, 16);
+        mine.cost = add_lanes(mine.cost, 16);
+        mine.named = add_lanes(mine.named, 16);
+        mine.named_cost = add_lanes(mine.named_cost, 16);
+    }
+    return mine;
+}
+// The parts of a row brought together by every CTA's warp 0; all have arrived at the cluster's barrier before, and their `parts` may be written.
+__device__ __forceinline__ Partial exchange(Partial sum, const DistillDev &a, Partial *parts, uint32_t part) {
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    asm volatile("barrier.cluster.wait;" ::: "memory");
+    if (warp == 0) {
+        if (lane < a.split) *cg::this_cluster().map_shared_rank(&parts[part], lane) = sum;
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    } else {
+        asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+    }
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    return warp == 0 ? add_parts(lane % kMaxSplit < a.split ? parts[lane % kMaxSplit] : no_part(), a, kMaxSplit) : sum;
+}
+// The named tokens' gradients, over what has been written in their places.
+template <typename T>
+__device__ __forceinline__ void put_named(const DistillDev &a, const Named &e, const Row &row, uint32_t threads, char *dz, double base, double f) {
+    for (uint32_t i = threadIdx.x; i < a.top; i += threads) {
+        if (e.at[i] == kNowhere) continue;
+        const double q = e.q[i] * f / row.total;
+        double g = q * row.q_scale - e.p[i] * row.p_scale;
+        if (a.kind == GAC_DISTILL_REVERSE) g = q == 0.0 ? 0.0 : q * ((double(e.z[i]) - base) * a.inv_temp - row.lse - double(e.l[i]) - row.loss);
+        reinterpret_cast<T *>(dz)[e.at[i]] = from_float(float(g * row.weight), T{});
+    }
+}
+
+template <int WARPS>
+struct Shared {
+    Partial parts[kMaxSplit], warp_part[WARPS];
+    Row row;
+    float warp_most[WARPS];
+    int repeated;
+};
+
+// A far row, of which `row` knows the largest logits: its sums once more, and all that is wanted of it, from distances to the largest, which
+// are exact to the last bits wherever the logits lie.  A way of its own, because one more operation per logit, or more registers, would
+// slow all rows; its loops stay rolled for the same reason (with two vectors at a time the other rows' spill, 458 us instead of 433).
+// 4096 x 151936 bfloat16 with all but the named logits at -1e10: 1060 us.
+template <typename T, bool GRAD, bool SHORT>
+__device__ __forceinline__ void do_far_row(const DistillDev &a, Shared<Shape<GRAD, SHORT>::kWarps> &shared) {
+    using Vec = Vector<T>;
+    constexpr uint32_t N = Vec::N, kWarps = Shape<GRAD, SHORT>::kWarps, kThreads = 32 * kWarps;
+    extern __shared__ __align__(128) char dynamic[];
+    const uint32_t part = blockIdx.x % a.split, t = blockIdx.x / a.split, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const Span sp = span_of<T>(a, t, part);
+    const Named e(dynamic + Shape<GRAD, SHORT>::kRingBytes, a.top);
+    const uint8_t *mark = reinterpret_cast<const uint8_t *>(e.marks) - sp.lo;
+    const float m = shared.row.m;
+    const double base = fmaxf(shared.row.named_m, m > kMasked ? m : -FLT_MAX);
+    const float2 minus = make_float2(-m, -m), c2 = make_float2(a.c, a.c);
+    if (a.split > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");   // this CTA has read its parts
+    // exp(z) of a vector in units of that of m
+    auto powers = [&](const uint4 &x, float2 (&v)[N / 2]) {
+        Vec::unpack(x, v);
+#pragma unroll
+        for (int i = 0; i < int(N) / 2; ++i) {
+            v[i] = mul2(add2(v[i], minus), c2);
+            v[i] = make_float2(exp2_approx(v[i].x), exp2_approx(v[i].y));
+        }
+    };
+    // which elements of a vector are the row's
+    auto inside = [&](uint32_t j) {
+        uint32_t bits = (1u << N) - 1;
+        if (j * N < sp.off) bits &= bits << (sp.off - j * N);
+        if ((j + 1) * N > sp.end) bits &= (1u << (sp.end - j * N)) - 1;
+        return bits;
+    };
+    auto load = [&](uint32_t j, uint32_t bits) {
+        if (bits == (1u << N) - 1) return reinterpret_cast<const uint4 *>(sp.z)[j];
+        alignas(16) T v[N];
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) v[i] = bits >> i & 1u ? reinterpret_cast<const T *>(sp.z)[j * N + i] : T(0);
+        return *reinterpret_cast<const uint4 *>(v);
+    };
+    double others = 0.0;
+#pragma unroll 1
+    for (uint32_t j = sp.lo + threadIdx.x; j < sp.hi; j += kThreads) {
+        const uint32_t bits = inside(j);
+        float2 v[N / 2];
+        powers(Vec::without(load(j, bits), mark[j] | ~bits), v);
+#pragma unroll
+        for (int w = int(N) / 4; w > 0; w /= 2)
+#pragma unroll
+            for (int i = 0; i < w; ++i) v[i] = add2(v[i], v[i + w]);
+        others += double(v[0].x + v[0].y);
+    }
+    Partial sum = add_named(a, e, kThreads, max_lanes(shared.warp_most[lane % kWarps], 16), base, 0.0);
+    sum.s = float(add_lanes(others, 16));
+    sum.m = m;
+    sum.named_m = float(base);   // the same in all parts: they are added up as they are
+    if (lane == 0) shared.warp_part[warp] = sum;
+    __syncthreads();
+    if (warp == 0) sum = add_parts(lane < kWarps ? shared.warp_part[lane] : no_part(), a, 32);
+    if (a.split > 1) sum = exchange(sum, a, shared.parts, part);
+    if (warp == 0) {
+        Row r;
+        Sums x;
+        r.weight = (a.weights ? double(a.weights[t]) : 1.0) * a.inv_temp;
+        x.rest = has_rest(sum);
+        x.unit = 0.0;
+        x.rest_unit = x.rest ? (double(m) - base) * a.inv_temp : 0.0;
+        x.f_rest = x.rest ? exp(x.rest_unit) : 0.0;
+        x.f_named = 1.0;
+        x.s = x.rest ? double(sum.s) : 0.0;
+        const double total = sum.named + x.s * x.f_rest;
+        r.total = total < double(INFINITY) ? total : double(NAN);
+        x.p_rest = fmax(1.0 - sum.mass, 1.0 / 16777216.0);
+        if (a.kind != GAC_DISTILL_REVERSE) finish_gradient(a, sum, x, r);
+        finish_loss(a, sum, x, r);
+        if (lane == 0 && a.loss && part == 0) a.loss[t] = float(r.loss);
+        if (lane == 0) shared.row = r;
+    }
+    if (!GRAD) return;
+    __syncthreads();
+    char *dz = a.dz + (long long)t * a.dz_row - sp.off * sizeof(T);
+    const bool aligned = reinterpret_cast<uint64_t>(dz) % 16 == 0;
+    const float2 scale = make_float2(shared.row.others, shared.row.others);
+#pragma unroll 1
+    for (uint32_t j = sp.lo + threadIdx.x; j < sp.hi; j += kThreads) {
+        const uint32_t bits = inside(j);
+        float2 v[N / 2];
+        powers(load(j, bits), v);
+#pragma unroll
+        for (int i = 0; i < int(N) / 2; ++i) v[i] = mul2(v[i], scale);
+        const uint4 y = Vec::pack(v);
+        if (aligned && bits == (1u << N) - 1) {
+            __stcs(reinterpret_cast<uint4 *>(dz) + j, y);
+        } else {
+            alignas(16) T w[N];
+            *reinterpret_cast<uint4 *>(w) = y;
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i)
+                if (bits >> i & 1u) reinterpret_cast<T *>(dz)[j * N + i] = w[i];
+        }
+    }
+    __syncthreads();
+    put_named<T>(a, e, shared.row, kThreads, dz, base, 1.0);
+}
+
 template <typename T, bool GRAD, bool SHORT>
 __global__ void __launch_bounds__(Shape<GRAD, SHORT>::kThreads, Shape<GRAD, SHORT>::kCtas)
 distill_kernel(const __grid_constant__ DistillDev a) {
     using Vec = Vector<T>;
     using C = Shape<GRAD, SHORT>;
     constexpr int N = Vec::N, kThreads = C::kThreads, kWarps = C::kWarps, kFlight = C::kFlight, kRing = C::kRing;
-    constexpr uint32_t kNowhere = 0xFFFFFFFFu;
-    extern __shared__ __align__(16) char dynamic[];
-    __shared__ Partial parts[kMaxSplit], warp_part[kWarps];
-    __shared__ Row row;
-    __shared__ float warp_most[kWarps];
-    __shared__ int repeated;
+    extern __shared__ __align__(128) char dynamic[];   // a ring that begins off 32 bytes takes every sector of a row from L2 twice (484 us)
+    __shared__ Shared<kWarps> shared;
+    Row &row = shared.row;
 
     const uint32_t part = blockIdx.x % a.split, t = blockIdx.x / a.split;
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, top = a.top;
     const Span sp = span_of<T>(a, t, part);
     const uint32_t ring = smem_addr(dynamic) + threadIdx.x * 16;
-    // per named token: p, or e of it; its exp(z); its logit, what the teacher says, its place in the row (none: not of this part, or
-    // absent); then a byte to a vector, a bit to an element: which are named
-    double *e_p = reinterpret_cast<double *>(dynamic + C::kRingBytes), *e_q = e_p + top;
-    float *e_z = reinterpret_cast<float *>(e_q + top), *e_l = e_z + top;
-    uint32_t *e_at = reinterpret_cast<uint32_t *>(e_l + top), *marks = e_at + top;
-    for (uint32_t i = threadIdx.x; i < a.mark_words; i += kThreads) marks[i] = 0;
-    if (threadIdx.x == 0) repeated = 0;
+    const Named e(dynamic + C::kRingBytes, top);
+    for (uint32_t i = threadIdx.x; i < a.mark_words; i += kThreads) e.marks[i] = 0;
+    if (threadIdx.x == 0) shared.repeated = 0;
 
     const uint32_t groups = sp.whole_hi > sp.whole_lo ? (sp.whole_hi - sp.whole_lo + kFlight * kThreads - 1) / (kFlight * kThreads) : 0;
     // A thread's own vectors pass through a ring in shared memory, kRing groups of kFlight of them, and no other thread sees them.
@@ -329,30 +514,30 @@ distill_kernel(const __grid_constant__ DistillDev a) {
             if (place >= sp.lo * N && place < sp.hi * N) {
                 const float z = as_float(reinterpret_cast<const T *>(sp.z)[place]);
                 if (i < kThreads) z0 = z;   // not waited for yet
-                else e_z[i] = z;
+                else e.z[i] = z;
                 const uint32_t bit = 1u << ((place / N - sp.lo) % 4 * 8 + place % N);
-                if (atomicOr(marks + (place / N - sp.lo) / 4, bit) & bit) repeated = 1;
+                if (atomicOr(e.marks + (place / N - sp.lo) / 4, bit) & bit) shared.repeated = 1;
             } else {
                 place = kNowhere;
             }
         }
-        e_at[i] = place;
-        e_l[i] = l;
+        e.at[i] = place;
+        e.l[i] = l;
     }
     most = max_lanes(most, 16);
-    if (lane == 0) warp_most[warp] = most;
+    if (lane == 0) shared.warp_most[warp] = most;
     any = __syncthreads_or(any);
     if (any && a.split > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");   // this CTA has started
-    if (repeated) {   // of several with the same token the first counts
+    if (shared.repeated) {   // of several with the same token the first counts
         for (uint32_t i = threadIdx.x; i < top; i += kThreads) {
-            const uint32_t at = e_at[i];
+            const uint32_t at = e.at[i];
             bool seen = false;
-            for (uint32_t j = 0; at != kNowhere && j < i; ++j) seen |= e_at[j] == at;
-            e_p[i] = seen ? 1.0 : 0.0;
+            for (uint32_t j = 0; at != kNowhere && j < i; ++j) seen |= e.at[j] == at;
+            e.p[i] = seen ? 1.0 : 0.0;
         }
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < top; i += kThreads)
-            if (e_p[i] != 0.0) e_at[i] = kNowhere;
+            if (e.p[i] != 0.0) e.at[i] = kNowhere;
     }
 
     float named_level = -FLT_MAX;
@@ -381,7 +566,7 @@ distill_kernel(const __grid_constant__ DistillDev a) {
                 for (int i = 0; i < w; ++i) v[i] = add2(v[i], v[i + w]);
             s = add2(s, v[0]);
         };
-        const uint8_t *mark = reinterpret_cast<const uint8_t *>(marks) - sp.lo;
+        const uint8_t *mark = reinterpret_cast<const uint8_t *>(e.marks) - sp.lo;
         for (uint32_t g = 0; g < groups; ++g) {
             uint4 x[kFlight];
             take(g, x);
@@ -412,7 +597,7 @@ distill_kernel(const __grid_constant__ DistillDev a) {
             }
         }
         edge([&](uint32_t place) {
-            if (reinterpret_cast<const uint8_t *>(marks)[place / N - sp.lo] >> (place % N) & 1u) return;
+            if (reinterpret_cast<const uint8_t *>(e.marks)[place / N - sp.lo] >> (place % N) & 1u) return;
             const float v = as_float(reinterpret_cast<const T *>(sp.z)[place]), next = fmaxf(m, v), next_level = level_of(next, a.c);
             const float f = exp2_approx(level - next_level);
             s = make_float2(s.x * f + exp2_approx(fmaf(v, a.c, -next_level)), s.y * f);
@@ -423,67 +608,58 @@ distill_kernel(const __grid_constant__ DistillDev a) {
 #pragma unroll
             for (int g = 0; g < kRing; ++g) issue(g, groups - 1 - g, drop);
         }
-        most = max_lanes(warp_most[lane % kWarps], 16);
-        Partial mine = {};
+        most = max_lanes(shared.warp_most[lane % kWarps], 16);
         float m_named = -FLT_MAX;
         for (uint32_t i = threadIdx.x; i < top; i += kThreads)
-            if (e_at[i] != kNowhere) {
-                if (i < kThreads) e_z[i] = z0;
-                m_named = fmaxf(m_named, e_z[i]);
+            if (e.at[i] != kNowhere) {
+                if (i < kThreads) e.z[i] = z0;
+                m_named = fmaxf(m_named, e.z[i]);
             }
-        named_level = mine.level = level_of(max_lanes(m_named, 16), a.c);
-        for (uint32_t i = threadIdx.x; i < top; i += kThreads) {
-            if (e_at[i] == kNowhere) continue;
-            const double z = double(e_z[i]) * a.inv_temp, says = e_l[i];
-            const double log_p = a.kind == GAC_DISTILL_TOP ? (says - double(most)) * a.inv_temp : says;
-            const double p = exp(log_p), q = exp(z - double(named_level) * M_LN2);
-            e_p[i] = p;
-            e_q[i] = q;
-            mine.mass += p;
-            mine.cost += p > 0.0 ? p * (log_p - z) : p;     // 0 log 0 = 0; a NaN stays one
-            mine.named += q;
-            mine.named_cost += q > 0.0 ? q * (z - log_p) : q;
-        }
-        if (__any_sync(0xFFFFFFFFu, mine.named != 0.0 || mine.mass != 0.0)) {
-            mine.mass = add_lanes(mine.mass, 16);
-            mine.cost = add_lanes(mine.cost, 16);
-            mine.named = add_lanes(mine.named, 16);
-            mine.named_cost = add_lanes(mine.named_cost, 16);
-        }
+        m_named = max_lanes(m_named, 16);
+        named_level = level_of(m_named, a.c);
+        Partial mine = add_named(a, e, kThreads, most, 0.0, double(named_level) * M_LN2);
+        mine.named_m = m_named;
         mine.m = max_lanes(m, 16);
         mine.s = add_lanes((s.x + s.y) * exp2_approx(level - level_of(mine.m, a.c)), 16);
-        if (lane == 0) warp_part[warp] = mine;
+        if (lane == 0) shared.warp_part[warp] = mine;
         __syncthreads();
         // ---- the row's numbers
         Partial sum;
-        if (warp == 0) sum = add_parts(lane < kWarps ? warp_part[lane] : no_part(), a, 32);
-        if (a.split > 1) {
-            asm volatile("barrier.cluster.wait;" ::: "memory");   // all have started: their memory may be written
-            if (warp == 0) {
-                if (lane < a.split) *cg::this_cluster().map_shared_rank(&parts[part], lane) = sum;
-                asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-            } else {
-                asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
-            }
-            asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-            if (warp == 0) {
-                sum = add_parts(lane % kMaxSplit < a.split ? parts[lane % kMaxSplit] : no_part(), a, kMaxSplit);
-            }
-        }
+        if (warp == 0) sum = add_parts(lane < kWarps ? shared.warp_part[lane] : no_part(), a, 32);
+        if (a.split > 1) sum = exchange(sum, a, shared.parts, part);
         Row r;
         Sums more;
+        auto tell = [&]() {   // of a far row too, and then once more: a branch here would cost more
+            if (warp == 0 && a.loss && part == 0) {
+                if (a.kind != GAC_DISTILL_REVERSE) finish_loss(a, sum, more, r);
+                if (lane == 0) a.loss[t] = float(r.loss);
+            }
+        };
         if (warp == 0) {
             r.weight = (a.weights ? double(a.weights[t]) : 1.0) * a.inv_temp;
+            r.m = sum.m;
+            r.named_m = sum.named_m;
+            r.far = far_row(a, sum.m, sum.named_m);
             more = start(a, sum, r);
             if (a.kind == GAC_DISTILL_REVERSE) finish_loss(a, sum, more, r);
             else finish_gradient(a, sum, more, r);
-            if (lane == 0) row = r;
+            if (GRAD && lane == 0) row = r;
         }
-        if (GRAD) __syncthreads();
-        if (warp == 0 && a.loss && part == 0) {
-            if (a.kind != GAC_DISTILL_REVERSE) finish_loss(a, sum, more, r);
-            if (lane == 0) a.loss[t] = float(r.loss);
+        if (!GRAD) {
+            tell();
+            if (threadIdx.x == 0) {
+                row.m = r.m;
+                row.named_m = r.named_m;
+                row.far = r.far;
+            }
         }
+        __syncthreads();
+        if (row.far) {
+            do_far_row<T, GRAD, SHORT>(a, shared);
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            return;
+        }
+        if (GRAD) tell();
     } else if (a.loss && part == 0 && threadIdx.x == 0) {
         a.loss[t] = 0.0f;   // nothing to compare with
     }
@@ -541,14 +717,7 @@ distill_kernel(const __grid_constant__ DistillDev a) {
         }
         if (any) {
             __syncthreads();   // the named tokens' own gradients over what has been written
-            const double f = power_of_two(named_level - row.unit);
-            for (uint32_t i = threadIdx.x; i < top; i += kThreads) {
-                if (e_at[i] == kNowhere) continue;
-                const double q = e_q[i] * f / row.total;
-                double g = q * row.q_scale - e_p[i] * row.p_scale;
-                if (a.kind == GAC_DISTILL_REVERSE) g = q == 0.0 ? 0.0 : q * (double(e_z[i]) * a.inv_temp - row.lse - double(e_l[i]) - row.loss);
-                reinterpret_cast<T *>(dz)[e_at[i]] = from_float(float(g * row.weight), T{});
-            }
+            put_named<T>(a, e, row, kThreads, dz, 0.0, power_of_two(named_level - row.unit));
         }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");   // of a row without entries the first loads may still be on their way

@@ -326,6 +326,14 @@ __device__ __forceinline__ void put_named(const DistillDev &a, const Named &e, c
     }
 }
 
+// What the teacher says of an entry, and whether it is there.
+__device__ __forceinline__ void read_entry(const DistillDev &a, uint32_t t, uint32_t i, int &id, float &says) {
+    id = a.ids[(long long)t * a.ids_row + i];
+    const long long at = (long long)t * a.teacher_row + i;
+    says = a.teacher_bf16 ? as_float(reinterpret_cast<const uint16_t *>(a.teacher)[at]) : reinterpret_cast<const float *>(a.teacher)[at];
+}
+__device__ __forceinline__ bool is_there(const DistillDev &a, int id, float says) { return id >= 0 && uint32_t(id) < a.vocab && says != -INFINITY; }
+
 template <int WARPS>
 struct Shared {
     Partial parts[kMaxSplit], warp_part[WARPS];
@@ -385,6 +393,23 @@ __device__ __forceinline__ void do_far_row(const DistillDev &a, Shared<Shape<GRA
 #pragma unroll
             for (int i = 0; i < w; ++i) v[i] = add2(v[i], v[i + w]);
         others += double(v[0].x + v[0].y);
+    }
+    if (a.kind == GAC_DISTILL_TOP && a.split > 1) {   // the largest value that counts, of all parts: of several with one id the first
+        float most = -INFINITY;
+        for (uint32_t i = threadIdx.x; i < a.top; i += kThreads) {
+            int id, other;
+            float says, unsaid;
+            read_entry(a, t, i, id, says);
+            bool counts = is_there(a, id, says) && says > most;
+            for (uint32_t j = 0; j < i && counts; ++j) {
+                read_entry(a, t, j, other, unsaid);
+                counts = other != id || !is_there(a, other, unsaid);
+            }
+            if (counts) most = says;
+        }
+        most = max_lanes(most, 16);
+        if (lane == 0) shared.warp_most[warp] = most;
+        __syncthreads();
     }
     Partial sum = add_named(a, e, kThreads, max_lanes(shared.warp_most[lane % kWarps], 16), base, 0.0);
     sum.s = float(add_lanes(others, 16));
@@ -487,15 +512,10 @@ distill_kernel(const __grid_constant__ DistillDev a) {
         if (vector < sp.lo || vector >= sp.hi || (vector >= sp.whole_lo && vector < sp.whole_hi) || (threadIdx.x >= N && sp.vectors == 1)) return;
         if (place >= sp.off && place < sp.end) each(place);
     };
-    auto said = [&](uint32_t i, int &id, float &l) {
-        id = a.ids[(long long)t * a.ids_row + i];
-        const long long at = (long long)t * a.teacher_row + i;
-        l = a.teacher_bf16 ? as_float(reinterpret_cast<const uint16_t *>(a.teacher)[at]) : reinterpret_cast<const float *>(a.teacher)[at];
-    };
     const float2 c2 = make_float2(a.c, a.c);
     int id0 = -1;     // the thread's first entry, on its way early
     float l0 = 0.f;
-    if (threadIdx.x < top) said(threadIdx.x, id0, l0);
+    if (threadIdx.x < top) read_entry(a, t, threadIdx.x, id0, l0);
 #pragma unroll
     for (int g = 0; g < kRing; ++g) issue(g, g, first);
     __syncthreads();
@@ -505,9 +525,9 @@ distill_kernel(const __grid_constant__ DistillDev a) {
     for (uint32_t i = threadIdx.x; i < top; i += kThreads) {
         int id = id0;
         float l = l0;
-        if (i >= kThreads) said(i, id, l);
+        if (i >= kThreads) read_entry(a, t, i, id, l);
         uint32_t place = kNowhere;
-        if (id >= 0 && uint32_t(id) < a.vocab && l != -INFINITY) {
+        if (is_there(a, id, l)) {
             any = true;
             most = fmaxf(most, l);
             place = uint32_t(id) + sp.off;
@@ -536,8 +556,22 @@ distill_kernel(const __grid_constant__ DistillDev a) {
             e.p[i] = seen ? 1.0 : 0.0;
         }
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < top; i += kThreads)
-            if (e.p[i] != 0.0) e.at[i] = kNowhere;
+        // p of kind top is told from the largest value that counts.  A CTA with a part of the row does not know what other parts hold: if
+        // it drops the largest of all, the row is gone over once more, like a far one
+        const float all = max_lanes(shared.warp_most[lane % kWarps], 16);
+        most = -INFINITY;
+        for (uint32_t i = threadIdx.x; i < top; i += kThreads) {
+            if (e.p[i] != 0.0 && e.at[i] != kNowhere) {
+                e.at[i] = kNowhere;
+                if (e.l[i] >= all) shared.repeated = 2;
+            } else if (e.at[i] != kNowhere) {
+                most = fmaxf(most, e.l[i]);
+            }
+        }
+        most = max_lanes(most, 16);
+        __syncthreads();
+        if (a.split == 1 && lane == 0) shared.warp_most[warp] = most;
+        __syncthreads();
     }
 
     float named_level = -FLT_MAX;
@@ -626,7 +660,10 @@ distill_kernel(const __grid_constant__ DistillDev a) {
         // ---- the row's numbers
         Partial sum;
         if (warp == 0) sum = add_parts(lane < kWarps ? shared.warp_part[lane] : no_part(), a, 32);
-        if (a.split > 1) sum = exchange(sum, a, shared.parts, part);
+        if (a.split > 1) {
+            if (a.kind == GAC_DISTILL_TOP && shared.repeated == 2) sum.mass = NAN;
+            sum = exchange(sum, a, shared.parts, part);
+        }
         Row r;
         Sums more;
         auto tell = [&]() {   // of a far row too, and then once more: a branch here would cost more
@@ -639,7 +676,7 @@ distill_kernel(const __grid_constant__ DistillDev a) {
             r.weight = (a.weights ? double(a.weights[t]) : 1.0) * a.inv_temp;
             r.m = sum.m;
             r.named_m = sum.named_m;
-            r.far = far_row(a, sum.m, sum.named_m);
+            r.far = far_row(a, sum.m, sum.named_m) || sum.mass != sum.mass;
             more = start(a, sum, r);
             if (a.kind == GAC_DISTILL_REVERSE) finish_loss(a, sum, more, r);
             else finish_gradient(a, sum, more, r);

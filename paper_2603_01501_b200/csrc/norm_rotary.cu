@@ -216,7 +216,7 @@ norm_rotary_kernel(const __grid_constant__ RotaryDev a, const __grid_constant__ 
                     const uint32_t k = 2 * i + j, pair = HALF ? at.u * N + k : (k < N / 2 ? 0 : a.pairs / 2 - N / 2) + at.u * (N / 2) + k;
                     const long long angle = steps[pair] * (a.positions ? position_on_axis(a, pair, t) : place);
                     float s, c;
-                    sincospif(float(int(angle >> 32)) * 4.656612873077393e-10f, &s, &c);   // 2^-31: halves of a turn
+                    sincospif(__ll2float_rn(angle) * 1.0842021724855044e-19f, &s, &c);   // 2^-63: halves of a turn, 24 bits of any angle
                     cs[j] = make_float2(c * a.scale, s * a.scale);
                 }
             cosines[i] = make_float2(cs[0].x, cs[1].x);

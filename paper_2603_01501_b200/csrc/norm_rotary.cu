@@ -214,7 +214,8 @@ norm_rotary_kernel(const __grid_constant__ RotaryDev a, const __grid_constant__ 
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const uint32_t k = 2 * i + j, pair = HALF ? at.u * N + k : (k < N / 2 ? 0 : a.pairs / 2 - N / 2) + at.u * (N / 2) + k;
-                    const long long angle = steps[pair] * (a.positions ? position_on_axis(a, pair, t) : place);
+                    // unsigned, for it is meant to overflow
+                    const long long angle = (long long)((unsigned long long)steps[pair] * (unsigned long long)(long long)(a.positions ? position_on_axis(a, pair, t) : place));
                     float s, c;
                     sincospif(__ll2float_rn(angle) * 1.0842021724855044e-19f, &s, &c);   // 2^-63: halves of a turn, 24 bits of any angle
                     cs[j] = make_float2(c * a.scale, s * a.scale);

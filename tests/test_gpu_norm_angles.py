@@ -36,3 +36,20 @@ def test_small_sines(dim, layout):
         got, _ = gb.gac_norm_rotary(heads, None, None, None, freqs, positions=pos.repeat(heads.shape[0] // 8), layout=layout)
         off = (got[:8].double()[..., second] - want).abs()
         assert bool((off <= bound).all()), float((off / bound.clamp(min=1e-300)).nan_to_num(0.0).max())
+
+
+@pytest.mark.parametrize("dim", [64, 30])
+def test_the_farthest_positions(dim):
+    """Whole turns fall away where positions times steps pass 64 bits: with frequencies of whole parts of a turn the result is known exactly."""
+    parts = torch.tensor([2, 4, 8, 3, 5, 7, 1 << 20, 12345], dtype=torch.int64).repeat(8)[:dim // 2]
+    pos = torch.tensor([2 ** 31 - 1, -2 ** 31, 2 ** 31 - 12345, -2 ** 31 + 77, 1], dtype=torch.int32, device="cuda")
+    freqs = (2 * math.pi / parts.double()).numpy()
+    x = torch.randn(5, 3, dim, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    got, _ = gb.gac_norm_rotary(x, None, None, None, freqs, positions=pos)
+    left = pos.long()[:, None] % parts.cuda()                       # of the position, behind the last whole turn
+    angle = (2 * math.pi * left.double() / parts.cuda())[:, None]
+    want, bound = ref.norm(x, None, (angle.cos(), angle.sin()), "half", 1.0, 1e-6, 0.0)
+    # turns of at most a half: the frequency and their quotient are off by 2^-53 of it each, the step by 2^-65, all times the position
+    n = x.double() * torch.rsqrt(x.double().square().mean(-1, keepdim=True) + 1e-6)
+    bound = bound + 2 * math.pi * 2.0 ** 31 * (2 * 2.0 ** -54 + 2.0 ** -65) * ref.both(n, dim, "half", 1.0)
+    assert bool(((got.double() - want).abs() <= bound).all())

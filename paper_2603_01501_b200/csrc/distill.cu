@@ -188,6 +188,7 @@ struct Sums {
     double unit, rest_unit;     // logarithms: of what total is a multiple of, and of what s is, relative to it
     bool rest;
 };
+__device__ __forceinline__ double what_is_left(double mass) { return 1.0 - mass < 1.0 / 16777216.0 ? 1.0 / 16777216.0 : 1.0 - mass; }   // NaN of NaN
 __device__ __forceinline__ bool has_rest(const Partial &p) { return p.m > kMasked || p.s != p.s; }   // a NaN is not masked
 // Whether the largest logit of what counts is beyond the levels: m outside N, named_m in it.
 __device__ __forceinline__ bool far_row(const DistillDev &a, float m, float named_m) {
@@ -208,7 +209,7 @@ __device__ __forceinline__ Sums start(const DistillDev &a, const Partial &p, Row
     x.s = !x.rest ? 0.0 : double(p.s) * (fabs(off) < 0.01 ? 1.0 + off * (1.0 + off * (0.5 + off * (1.0 / 6.0))) : exp(off));
     const double total = p.named * x.f_named + x.s * x.f_rest;
     r.total = total < double(INFINITY) ? total : double(NAN);
-    x.p_rest = fmax(1.0 - p.mass, 1.0 / 16777216.0);
+    x.p_rest = what_is_left(p.mass);
     return x;
 }
 __device__ __forceinline__ float factor(double others, const Sums &x, const Partial &p, const Row &r) {
@@ -233,7 +234,7 @@ __device__ __forceinline__ void finish_loss(const DistillDev &a, const Partial &
         r.loss = p.cost + p.mass * r.lse + (x.rest ? x.p_rest * (log_p_rest - log_q_rest) : 0.0);
     } else {
         const double q_rest = x.s * x.f_rest / r.total, d_rest = x.rest ? log_q_rest - log_p_rest : 0.0;
-        r.loss = x.f_named / r.total * (p.named_cost - r.lse * p.named) + q_rest * d_rest;
+        r.loss = x.f_named / r.total * (p.named_cost - r.lse * p.named) + q_rest * d_rest + 0.0 * p.mass;   // a NaN that nothing weighs stays one
         r.others = factor(q_rest * (d_rest - r.loss), x, p, r);
     }
 }
@@ -431,7 +432,7 @@ __device__ __forceinline__ void do_far_row(const DistillDev &a, Shared<Shape<GRA
         x.s = x.rest ? double(sum.s) : 0.0;
         const double total = sum.named + x.s * x.f_rest;
         r.total = total < double(INFINITY) ? total : double(NAN);
-        x.p_rest = fmax(1.0 - sum.mass, 1.0 / 16777216.0);
+        x.p_rest = what_is_left(sum.mass);
         if (a.kind != GAC_DISTILL_REVERSE) finish_gradient(a, sum, x, r);
         finish_loss(a, sum, x, r);
         if (lane == 0 && a.loss && part == 0) a.loss[t] = float(r.loss);

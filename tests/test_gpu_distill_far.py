@@ -118,3 +118,72 @@ def test_a_named_token_masked_alone_in_its_part(kind):
                 values = torch.tensor([[0.6, 0.3], [0.2, 0.7]], device="cuda").log()
                 for temperature in (0.7, 1.0, 1.5, 2.0, 5.0):
                     check(x, ids, values, kind, temperature, torch.ones(2, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [BF, F], ids=["bf16", "f32"])
+def test_far_rows_at_any_place_of_memory(dtype):
+    """Rows on every boundary, a gradient on another boundary than the logits, and nothing written beside it."""
+    for vocab, kind in ((1021, "forward"), (30011, "reverse"), (9, "top"), (1, "top")):
+        x, ids, values, w = masked(max(vocab, 64), 20, kind, dtype, -1e20, 11)
+        if vocab < 64:
+            x, ids = x[:, :vocab].contiguous(), ids % vocab
+        want = ref.distill(x, ids, values, kind, 1.5, w)
+        for start, pitch in ((0, vocab), (3, vocab + 2), (1, vocab + 7)):
+            flat = torch.full((13 * pitch + 16,), 7.0, dtype=dtype, device="cuda")
+            v = flat[start:start + 13 * pitch].view(13, pitch)[:, :vocab]
+            v.copy_(x)
+            keep = flat.clone()
+            loss, grad = gb.gac_distill(v, ids, values, kind, 1.5, weights=w, grad=True)
+            within(loss, *want["loss"])
+            within(grad, *want["grad"])
+            gb.gac_distill(v, ids, values, kind, 1.5, weights=w, grad=True, in_place=True)
+            keep[start:start + 13 * pitch].view(13, pitch)[:, :vocab] = grad
+            assert torch.equal(flat, keep)
+
+
+@pytest.mark.parametrize("kind", ["top", "forward", "reverse"])
+def test_far_rows_with_repeats_and_with_non_finite_values(kind):
+    for vocab in (700, 50000):
+        x, ids, values, w = masked(vocab, 64, kind, BF, -1e20, 13)
+        clean = gb.gac_distill(x, ids, values, kind, weights=w, grad=True)
+        i2, v2 = ids.clone(), values.clone()
+        i2[:, 40:] = ids[:, :24]                       # the first counts, whatever the others say
+        v2[:, 40:] = 50.0
+        check(x, i2, v2, kind, 1.5, w)
+        y, t = x.clone(), values.clone()
+        y[5, [i for i in range(vocab) if i not in ids[5].tolist()][vocab // 3]] = math.nan     # elsewhere in a far row
+        y[8, ids[8, 1]] = math.nan                                                              # at a named token of one
+        y[9, 0] = math.inf
+        t[10, 3] = math.nan
+        for _ in range(2):
+            loss, grad = gb.gac_distill(y, ids, t, kind, weights=w, grad=True)
+            for row in range(13):
+                if row in (5, 8, 9, 10):
+                    assert not math.isfinite(float(loss[row])), row
+                else:
+                    assert torch.equal(loss[row], clean[0][row]) and torch.equal(grad[row], clean[1][row]), row
+
+
+def test_far_rows_on_two_streams_and_in_graphs():
+    calls = []
+    for seed, kind in ((17, "forward"), (19, "top")):
+        x, ids, values, w = masked(40009, 64, kind, BF, -1e20, seed)
+        calls.append(lambda a=(x, ids, values, kind), w=w: gb.gac_distill(*a, weights=w, grad=True))
+    want = [c() for c in calls]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [None, None]
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = calls[i]()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(want, got) for a, b in zip(x, y))
+    graphs, outs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    for g, c in zip(graphs, calls):
+        with torch.cuda.graph(g):
+            outs.append(c())
+    for _ in range(3):
+        for g in graphs:
+            g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for x, y in zip(want, outs) for a, b in zip(x, y))

@@ -672,9 +672,10 @@ int gac_norm_rotary_backward(const gac_rotary_args *args, const gac_rotary_axes 
  *   REVERSE  as FORWARD, but the other way:
  *                L = sum_N q (log q - log p) + q_r (log q_r - log p_r)
  * Absent is an entry whose id is outside 0..vocab-1 or whose value is -infinity.  Of several entries with one id the first
- * counts.  A row without entries has L = 0 and gradient 0 whatever its logits.  0 log 0 = 0.  A rest without
- * a logit above -1e38 (all masked, or none there) has no share: p_r is left out too.  Other non-finite values make their own row's
- * results non-finite.
+ * counts, whatever the others say.  A row without entries has L = 0 and gradient 0 whatever its logits.  0 log 0 = 0.  A rest without
+ * a logit above -1e38 (all masked, or none there) has no share: p_r is left out too.  Finite logits may be of any size; a row takes
+ * two to three times as long where the largest of the rest, or of all, is beyond 1.4e9 times the temperature on either side of 0 (all
+ * the rest masked with -1e10, for instance).  Other non-finite values make their own row's results non-finite.
  *
  *   loss       [n_tokens] float32, or NULL
  *   d_logits   weights[t] dL_t/dlogits, as wide as the logits, of their type, rounded once; or NULL.  It may be the

@@ -18,10 +18,10 @@
 // evict-last, read again and written with evict-first, and cut into so many parts that the rows in use fit.  Loads go through a
 // ring in shared memory, because what bounds the kernel is bytes in flight beside the chain from a row's last load to its first
 // gradient (sums over the CTA, exponentials and logarithms in binary64, about 5 us), which the SM's other CTAs have to cover.
-// Measured, ten calls after a pause: 4096 x 151936 bfloat16 with the gradient 444 us (5.6 TB/s of one read and one write, 0.87 of a
-// plain copy's rate; memory reads the logits 1.13 times), 8191 x 32000 float32, a quarter without a teacher, 324 (0.88), 2048 x 151936
-// values alone 105 (0.92).  In a second of calls on end, under the power cap, 497, 336 and 113.  A row held in the shared memory of eight
-// CTAs took 618 instead of 444, and persistent CTAs that read the next row while parts of the last are exchanged 1490.
+// Measured, ten calls after a pause: 4096 x 151936 bfloat16 with the gradient 434 us (5.7 TB/s of one read and one write, 0.89 of a
+// plain copy's rate; memory reads the logits 1.14 times), 8191 x 32000 float32, a quarter without a teacher, 310 (0.92), 2048 x 151936
+// values alone 105 (0.92).  In a second of calls on end, under the power cap, 503, 330 and 119.  A row held in the shared memory of eight
+// CTAs took 618 where this took 444, and persistent CTAs that read the next row while parts of the last are exchanged 1490.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 #include <float.h>
@@ -41,9 +41,10 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-// Threads of a CTA, CTAs of an SM, and the ring: groups of vectors that a thread loads at once.  Short rows take smaller CTAs: what
-// a row takes beside its loads is the same for all, and more rows at once cover it (4096 rows of 64 kB with the gradient 111 us, with
-// the other shape 116; values alone 53 and 79; 2048 rows of 304 kB, values alone, 111 and 105).
+// Threads of a CTA, CTAs of an SM that registers are left for, and the ring: groups of vectors that a thread loads at once.  Short rows
+// take smaller CTAs: what a row takes beside its loads is the same for all, and more rows at once cover it (4096 rows of 64 kB with the
+// gradient 100 us, with the other shape 111; values alone 52 and 76; 4096 rows of 304 kB with the gradient 472 and 434, values alone the
+// same).  Of long rows with the gradient four CTAs fit an SM while a CTA's part of a row has about 90 kB, with the marks of more three.
 template <bool GRAD, bool SHORT>
 struct Shape {
     static constexpr int kThreads = SHORT ? 128 : GRAD ? 256 : 384, kCtas = SHORT ? 8 : GRAD ? 4 : 3, kWarps = kThreads / 32;
@@ -853,8 +854,8 @@ int gac_distill(const gac_distill_args *args, int cuda_device, void *cuda_stream
     const Launch shape = launch_of(a.dtype == GAC_BF16, grad, brief);
     // Parts of a row: what takes least, by 44 bytes a nanosecond and SM, and by the chain from a row's last load to its first gradient
     // (5 us, with the gradient 8, where parts wait for each other 1.5 more).  With the gradient so many that the rows in use
-    // at once stay in L2 between the two passes (4096 rows of 304 kB: 504 us with one part, 474 with two; 8191 rows of 128 kB, which
-    // fit whole: 323 and 371).
+    // at once stay in L2 between the two passes (4096 rows of 304 kB: 499 us with one part, 434 with two; 8191 rows of 128 kB, which
+    // fit whole: 310 and 353).
     d.split = 1;
     double least = INFINITY;
     for (uint32_t split = 1; split <= kMaxSplit; split *= 2) {
